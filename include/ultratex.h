@@ -465,6 +465,163 @@ ut_status ut_token_mask_from_alpha(const uint8_t* alpha, int32_t V, int32_t Hp,
                                    int32_t radius, uint8_t* token_mask, void* workspace,
                                    size_t workspace_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Rotary positions with several axes (view, row, column; time, height, width)
+ * on query and key rows, with the per-head RMS norm of queries and keys in
+ * front where the model has one. Kept tokens rotate by their positions in the
+ * full multi-view grid (Sec. 3.2), which they read through kept_idx.
+ *
+ *   pairs p = 0 .. R/2 - 1 of a head's first R = sum of the axes' sizes d_a
+ *   elements; pair p is the i-th of its axis a, in the order of the axes:
+ *   angle = pos[row, a] * theta^(-2 i / d_a),
+ *   (u, v) -> (u cos - v sin, v cos + u sin); elements R .. D - 1 pass through.
+ *   With weights, before that: x -> x / sqrt(mean(x^2) + eps) * weight per head.
+ *
+ * q, k       [n, Hq, D] and [n, Hk, D] rows, UT_BF16 or UT_F32 (`dtype`),
+ *            16-byte aligned; Hk = 0: no keys (k, k_out ignored). A batch of
+ *            B samples is n = B N rows.
+ * q_out, k_out  outputs; q_out may be q and k_out k (with equal strides), and
+ *            otherwise must not overlap the inputs.
+ * strides_host  HOST array of the elements from token to token of {q, k, q_out,
+ *            k_out}, or NULL for rows back to back; each at least H D and a
+ *            multiple of 8 (bf16) or 4 (fp32). A token's heads are contiguous.
+ * D          head_dim, a multiple of 8 up to 256.
+ * pos        fp32 [pos_rows, n_axes] coordinates (fractions are fine).
+ * token_idx  int32 [n]: token i reads row token_idx[i] (the kept_idx of
+ *            ut_drop_background); an index outside [0, pos_rows) is not rotated,
+ *            the norm still applies. NULL: token i reads row i mod pos_rows.
+ * axis_dims_host  HOST array of the n_axes (1 to 4) sizes d_a, positive and even.
+ * theta      base of the frequencies, finite and > 0.
+ * pairs      UT_ROPE_NEAR: pair p is elements 2p and 2p + 1; UT_ROPE_FAR: p and
+ *            p + R/2 (R a multiple of 8).
+ * q_weight, k_weight  [D] norm weights (`w_dtype`), or both NULL: no norm.
+ * eps        finite and > 0 where there are weights, else ignored.
+ * Angles are formed in fp64 and reduced to one turn, everything else is fp32
+ * with one rounding to `dtype`. n = 0 is a no-op.
+ * Errors: sizes, strides, axes, theta or eps out of range, null or misaligned
+ *         pointers, one weight without the other -> UT_ERR_INVALID_ARG; a
+ *         head_dim outside the above, far pairs with R % 8 != 0, a stride of
+ *         2^31 or more -> UT_ERR_UNSUPPORTED.
+ *
+ * Backward: from the gradients of q_out and k_out those of q and k, and with
+ * weights those of the weights, summed over tokens and heads.
+ *
+ * dq_out, dk_out  gradients of the outputs, as q_out and k_out.
+ * q, k       the forward's inputs; read only with weights, else may be NULL.
+ * dq, dk     outputs; dq may be dq_out and dk dk_out (with equal strides).
+ * strides_host  {dq_out, dk_out, q, k, dq, dk}, or NULL.
+ * dq_weight, dk_weight  fp32 [D] outputs, written (not added to); required
+ *            with weights (dk_weight only with Hk > 0), else ignored.
+ * workspace  with weights, device scratch of ut_qk_rope_bwd_workspace_size(D)
+ *            bytes, 16-byte aligned; else unused.
+ * No atomics: results are deterministic. With n = 0 the weights' gradients
+ * are set to 0.
+ * Errors: as the forward, plus UT_ERR_WORKSPACE.
+ * ---------------------------------------------------------------------- */
+typedef enum {
+  UT_ROPE_NEAR = 0,
+  UT_ROPE_FAR = 1
+} ut_rope_pairs;
+ut_status ut_qk_rope_fwd(const void* q, const void* k, void* q_out, void* k_out,
+                         const int64_t* strides_host, ut_dtype dtype, int64_t n, int32_t Hq,
+                         int32_t Hk, int32_t D, const float* pos, int64_t pos_rows,
+                         const int32_t* token_idx, const int32_t* axis_dims_host, int32_t n_axes,
+                         double theta, ut_rope_pairs pairs, const void* q_weight,
+                         const void* k_weight, ut_dtype w_dtype, float eps, hipStream_t stream);
+size_t ut_qk_rope_bwd_workspace_size(int32_t D);
+ut_status ut_qk_rope_bwd(const void* dq_out, const void* dk_out, const void* q, const void* k,
+                         void* dq, void* dk, const int64_t* strides_host, ut_dtype dtype, int64_t n,
+                         int32_t Hq, int32_t Hk, int32_t D, const float* pos, int64_t pos_rows,
+                         const int32_t* token_idx, const int32_t* axis_dims_host, int32_t n_axes,
+                         double theta, ut_rope_pairs pairs, const void* q_weight,
+                         const void* k_weight, ut_dtype w_dtype, float eps, float* dq_weight,
+                         float* dk_weight, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Cross attention: the image tokens' queries attend to an encoder's states
+ * (text, a reference image) of another length, O = softmax(Q K^T * scale) V
+ * over the keys in use, every query of a sample to every key of it.
+ *
+ * q, o, dout, dq  bf16 [B, Nq, Hq, D]; k, v, dk, dv  bf16 [B, Nk, Hk, D]; Hq a
+ *           multiple of Hk: query head h reads key head h / (Hq / Hk), whose
+ *           gradients are summed over its query heads. 16-byte aligned. Outputs
+ *           must not overlap inputs. Nq, Nk >= 0.
+ * D         head_dim, a multiple of 8 up to 128.
+ * lse       fp32 [B, Hq, Nq]: natural-log log-sum-exp of each row's scaled
+ *           scores; -inf for a row without keys in use (its O row is 0, its dQ
+ *           row 0).
+ * strides_host  HOST array of the elements from token to token, in the order
+ *           {q, k, v, o} forward and {q, k, v, o, dout, dq, dk, dv} backward, or
+ *           NULL for rows back to back; each at least H D, a multiple of 8 and
+ *           below 2^22. Samples follow each other: sample b starts N strides
+ *           after sample b - 1. A token's heads are contiguous.
+ * key_mask  uint8 [B, Nk], nonzero = in use, or NULL: all in use. Rows of k and
+ *           v that are not in use may hold anything (NaN included) and get zero
+ *           gradients. Any alignment.
+ * softmax_scale  finite and > 0.
+ * workspace device scratch of the size query's bytes (0 for most shapes of the
+ *           forward: it is used where few queries meet many keys), 16-byte
+ *           aligned; need not be initialised. Two calls that may run at the same
+ *           time need one each.
+ * No atomics: results are deterministic.
+ * Errors: sizes or strides out of range, Hq % Hk != 0, 2^27 rows of a head or
+ *         more (B Nq Hq, B Nk Hk), null or misaligned pointers ->
+ *         UT_ERR_INVALID_ARG; a head_dim outside the above, a stride of 2^22 or
+ *         more -> UT_ERR_UNSUPPORTED; UT_ERR_WORKSPACE. The size queries return 0
+ *         for sizes that the calls refuse.
+ *
+ * Backward: dS = P o (dO V^T - rowsum(dO o O)), dQ = scale dS K,
+ * dK = scale dS^T Q, dV = P^T dO; o and lse from the forward.
+ *
+ * Variable lengths: B samples packed back to back on both sides.
+ *
+ * q, o, dout, dq  bf16 [Tq, Hq, D]; k, v, dk, dv  bf16 [Tk, Hk, D]; lse fp32
+ *           [Hq, Tq]; key_mask uint8 [Tk] or NULL.
+ * cu_seqlens_q, cu_seqlens_k  device int32 [B + 1]: sample b holds query tokens
+ *           [cu_q[b], cu_q[b+1]) and key tokens [cu_k[b], cu_k[b+1]); they start
+ *           at 0, never decrease and end at or before Tq and Tk. A sample may
+ *           have no queries or no keys.
+ * max_seqlen_q, max_seqlen_k  at least every sample's lengths.
+ * zero_rest 0: rows at and past cu_seqlens[B] of the outputs are left as they
+ *           were; else they are set to 0 and lse there to -inf.
+ * Offsets are clamped to [0, T] and lengths to max_seqlen inside the kernels, so
+ * bad offsets cannot reach outside the tensors. With UT_VALIDATE set both offset
+ * arrays are checked first (UT_ERR_INVALID_ARG otherwise).
+ * ---------------------------------------------------------------------- */
+size_t ut_xattn_fwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk,
+                                   int32_t D);
+ut_status ut_xattn_fwd(const void* q, const void* k, const void* v, void* o, float* lse,
+                       const int64_t* strides_host, const uint8_t* key_mask, int32_t B, int32_t Nq,
+                       int32_t Nk, int32_t Hq, int32_t Hk, int32_t D, float softmax_scale,
+                       void* workspace, size_t workspace_bytes, hipStream_t stream);
+size_t ut_xattn_fwd_varlen_workspace_size(int32_t B, int64_t Tq, int32_t max_seqlen_q,
+                                          int32_t max_seqlen_k, int32_t Hq, int32_t Hk, int32_t D);
+ut_status ut_xattn_fwd_varlen(const void* q, const void* k, const void* v, void* o, float* lse,
+                              const int64_t* strides_host, const uint8_t* key_mask,
+                              const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t B,
+                              int64_t Tq, int64_t Tk, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                              int32_t Hq, int32_t Hk, int32_t D, float softmax_scale,
+                              int32_t zero_rest, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream);
+size_t ut_xattn_bwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk,
+                                   int32_t D);
+ut_status ut_xattn_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                       const float* lse, void* dq, void* dk, void* dv, const int64_t* strides_host,
+                       const uint8_t* key_mask, int32_t B, int32_t Nq, int32_t Nk, int32_t Hq,
+                       int32_t Hk, int32_t D, float softmax_scale, void* workspace,
+                       size_t workspace_bytes, hipStream_t stream);
+size_t ut_xattn_bwd_varlen_workspace_size(int32_t B, int64_t Tq, int64_t Tk, int32_t max_seqlen_q,
+                                          int32_t max_seqlen_k, int32_t Hq, int32_t Hk, int32_t D);
+ut_status ut_xattn_bwd_varlen(const void* q, const void* k, const void* v, const void* o,
+                              const void* dout, const float* lse, void* dq, void* dk, void* dv,
+                              const int64_t* strides_host, const uint8_t* key_mask,
+                              const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t B,
+                              int64_t Tq, int64_t Tk, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                              int32_t Hq, int32_t Hk, int32_t D, float softmax_scale,
+                              int32_t zero_rest, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

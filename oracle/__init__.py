@@ -34,6 +34,13 @@ Paper sections (arXiv 2609.23169, "UltraTex"):
     attention but prints no gradient formula; the oracle differentiates Eq. 8
     with the mask held constant (the standard softmax-attention gradient
     restricted to the retained pairs).
+  * Rotary positions: the kept tokens rotate by their positions in the full
+    grid (Sec. 3.2). The paper gives no formula; the reading taken is the usual
+    one of image and video transformers, several axes sharing a head, with the
+    per-head RMS norm of queries and keys in front.
+  * Cross attention: Eq. 5 with queries and keys of different sequences (the
+    image tokens and an encoder's states), a mask over the keys and query heads
+    that share key heads.
   * Batches of differing lengths: training buckets samples by their
     foreground token count (Sec. 4.1, Implementation Details), so the kept
     counts within a batch are close but not equal. The reading taken: the
@@ -49,6 +56,7 @@ __all__ = [
     "block_pool", "topk_block_mask",
     "euler_update_fg", "fg_flow_loss",
     "composite_latent", "token_mask_from_alpha",
+    "rope_fwd", "rope_bwd", "xattn_fwd", "xattn_bwd",
 ]
 
 
@@ -431,3 +439,115 @@ def token_mask_from_alpha(alpha, patch: int, radius: int, threshold: int = 0) ->
                 x0, x1 = max(0, x - radius), min(gw, x + radius + 1)
                 out[v, y, x] = 1 if pooled[v, y0:y1, x0:x1].any() else 0
     return out
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions with several axes and the per-head norm (Sec. 3.2)
+# ---------------------------------------------------------------------------
+
+def _rope_angles(n: int, pos, axis_dims, theta: float, token_idx=None) -> np.ndarray:
+    """Angles [n, R/2], the pairs of each axis in turn. A token reads row
+    token_idx[t] of pos (row t mod rows without indices); an index outside the
+    table has angle 0."""
+    P = np.asarray(pos, np.float64)
+    rows = np.arange(n) % P.shape[0] if token_idx is None else np.asarray(token_idx, np.int64)
+    ok = (rows >= 0) & (rows < P.shape[0])
+    at = P[np.where(ok, rows, 0)]
+    cols = []
+    for a, d in enumerate(axis_dims):
+        for i in range(d // 2):
+            cols.append(np.where(ok, at[:, a] * theta ** (-2.0 * i / d), 0.0))
+    return np.stack(cols, 1)
+
+
+def _rope_turn(x: np.ndarray, ang: np.ndarray, interleaved: bool) -> np.ndarray:
+    """x [n, H, D] with each pair's two elements rotated by its angle."""
+    half = ang.shape[1]
+    p = np.arange(half)
+    i, j = (2 * p, 2 * p + 1) if interleaved else (p, p + half)
+    c, s = np.cos(ang)[:, None], np.sin(ang)[:, None]
+    y = x.copy()
+    y[:, :, i] = x[:, :, i] * c - x[:, :, j] * s
+    y[:, :, j] = x[:, :, j] * c + x[:, :, i] * s
+    return y
+
+
+def rope_fwd(x, pos, axis_dims, theta: float, token_idx=None, weight=None, eps: float = 1e-6,
+             interleaved: bool = True) -> np.ndarray:
+    """x [n, H, D] -> rotated rows, after x / sqrt(mean(x^2) + eps) * weight
+    where a weight [D] is given."""
+    X = _f64(x)
+    if weight is not None:
+        X = X / np.sqrt((X * X).mean(-1, keepdims=True) + eps) * _f64(weight)
+    return _rope_turn(X, _rope_angles(X.shape[0], pos, axis_dims, theta, token_idx), interleaved)
+
+
+def rope_bwd(dy, pos, axis_dims, theta: float, token_idx=None, x=None, weight=None, eps: float = 1e-6,
+             interleaved: bool = True):
+    """(dx, dweight or None) of rope_fwd for the output's gradient dy."""
+    G = _f64(dy)
+    G = _rope_turn(G, -_rope_angles(G.shape[0], pos, axis_dims, theta, token_idx), interleaved)
+    if weight is None:
+        return G, None
+    X, w = _f64(x), _f64(weight)
+    rstd = 1.0 / np.sqrt((X * X).mean(-1, keepdims=True) + eps)
+    hat = X * rstd
+    dw = (G * hat).sum((0, 1))
+    Gw = G * w
+    return rstd * (Gw - hat * (Gw * hat).mean(-1, keepdims=True)), dw
+
+
+# ---------------------------------------------------------------------------
+# Cross attention
+# ---------------------------------------------------------------------------
+
+def _xattn_p(Q, K, scale: float, used):
+    """Probabilities [Nq, Nk] and log-sum-exp [Nq] of one head (rows without
+    keys: 0 and -inf)."""
+    S = np.where(used[None], (Q @ K.T) * scale, -np.inf)
+    if not used.any():
+        return np.zeros_like(S), np.full(S.shape[0], -np.inf)
+    m = S.max(1, keepdims=True)
+    E = np.exp(S - m)
+    l = E.sum(1, keepdims=True)
+    return E / l, (m + np.log(l))[:, 0]
+
+
+def _used(key_mask, b: int, Nk: int) -> np.ndarray:
+    return np.ones(Nk, bool) if key_mask is None else np.asarray(key_mask)[b].astype(bool)
+
+
+def xattn_fwd(q, k, v, scale: float, key_mask=None):
+    """q [B, Nq, Hq, D], k, v [B, Nk, Hk, D], key_mask [B, Nk]: (O, LSE
+    [B, Hq, Nq]); query head h reads key head h / (Hq / Hk). Keys not in use
+    contribute nothing, whatever they hold."""
+    Q, K, V = _f64(q), _f64(k), _f64(v)
+    B, Nq, Hq, _ = Q.shape
+    G = Hq // K.shape[2]
+    O, LSE = np.zeros_like(Q), np.zeros((B, Hq, Nq))
+    for b in range(B):
+        used = _used(key_mask, b, K.shape[1])
+        for h in range(Hq):
+            Kh, Vh = (np.where(used[:, None], x[b, :, h // G], 0.0) for x in (K, V))
+            P, LSE[b, h] = _xattn_p(Q[b, :, h], Kh, scale, used)
+            O[b, :, h] = P @ Vh
+    return O, LSE
+
+
+def xattn_bwd(q, k, v, dout, scale: float, key_mask=None):
+    """(dQ, dK, dV) of xattn_fwd: the formulas of bsattn_bwd, a key head's
+    gradients summed over its query heads."""
+    Q, K, V, dO = _f64(q), _f64(k), _f64(v), _f64(dout)
+    G = Q.shape[2] // K.shape[2]
+    dQ, dK, dV = np.zeros_like(Q), np.zeros_like(K), np.zeros_like(V)
+    for b in range(Q.shape[0]):
+        used = _used(key_mask, b, K.shape[1])
+        for h in range(Q.shape[2]):
+            Kh, Vh = (np.where(used[:, None], x[b, :, h // G], 0.0) for x in (K, V))
+            P, _ = _xattn_p(Q[b, :, h], Kh, scale, used)
+            dP = dO[b, :, h] @ Vh.T
+            dS = P * (dP - (P * dP).sum(1, keepdims=True))
+            dQ[b, :, h] = scale * (dS @ Kh)
+            dK[b, :, h // G] += scale * (dS.T @ Q[b, :, h])
+            dV[b, :, h // G] += P.T @ dO[b, :, h]
+    return dQ, dK, dV

@@ -13,6 +13,7 @@ UltraTexError on a non-zero status.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -25,6 +26,7 @@ LIB_PATH = os.environ.get("UT_LIBRARY") or os.path.join(HERE, "libultratex.so")
 
 UT_OK, UT_ERR_INVALID_ARG, UT_ERR_UNSUPPORTED, UT_ERR_WORKSPACE, UT_ERR_CAPACITY, UT_ERR_HIP = range(6)
 UT_BF16, UT_F32 = 0, 1
+UT_ROPE_NEAR, UT_ROPE_FAR = 0, 1
 STATUS_NAMES = ["UT_OK", "UT_ERR_INVALID_ARG", "UT_ERR_UNSUPPORTED", "UT_ERR_WORKSPACE",
                 "UT_ERR_CAPACITY", "UT_ERR_HIP"]
 
@@ -40,6 +42,10 @@ EXPORTS = [
     "ut_topk_block_mask_workspace_size", "ut_topk_block_mask",
     "ut_euler_update_foreground", "ut_fg_flow_loss_workspace_size", "ut_fg_flow_loss",
     "ut_composite_latent", "ut_token_mask_workspace_size", "ut_token_mask_from_alpha",
+    "ut_qk_rope_fwd", "ut_qk_rope_bwd_workspace_size", "ut_qk_rope_bwd",
+    "ut_xattn_fwd_workspace_size", "ut_xattn_fwd", "ut_xattn_fwd_varlen_workspace_size",
+    "ut_xattn_fwd_varlen", "ut_xattn_bwd_workspace_size", "ut_xattn_bwd",
+    "ut_xattn_bwd_varlen_workspace_size", "ut_xattn_bwd_varlen",
 ]
 
 
@@ -91,6 +97,20 @@ _SIGS = {
     "ut_token_mask_from_alpha": (_c.c_int, [_vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _sz, _vp]),
     "ut_fg_flow_loss": (_c.c_int, [_vp, _c.c_int, _vp, _vp, _c.c_int, _i64, _i64, _vp, _i64, _vp, _vp,
                                    _vp, _sz, _vp]),
+    "ut_qk_rope_fwd": (_c.c_int, [_vp] * 5 + [_c.c_int, _i64, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _i32,
+                                              _c.c_double, _c.c_int, _vp, _vp, _c.c_int, _f32, _vp]),
+    "ut_qk_rope_bwd_workspace_size": (_sz, [_i32]),
+    "ut_qk_rope_bwd": (_c.c_int, [_vp] * 7 + [_c.c_int, _i64, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _i32,
+                                              _c.c_double, _c.c_int, _vp, _vp, _c.c_int, _f32, _vp, _vp, _vp,
+                                              _sz, _vp]),
+    "ut_xattn_fwd_workspace_size": (_sz, [_i32] * 6),
+    "ut_xattn_fwd": (_c.c_int, [_vp] * 7 + [_i32] * 6 + [_f32, _vp, _sz, _vp]),
+    "ut_xattn_fwd_varlen_workspace_size": (_sz, [_i32, _i64] + [_i32] * 5),
+    "ut_xattn_fwd_varlen": (_c.c_int, [_vp] * 9 + [_i32, _i64, _i64] + [_i32] * 5 + [_f32, _i32, _vp, _sz, _vp]),
+    "ut_xattn_bwd_workspace_size": (_sz, [_i32] * 6),
+    "ut_xattn_bwd": (_c.c_int, [_vp] * 11 + [_i32] * 6 + [_f32, _vp, _sz, _vp]),
+    "ut_xattn_bwd_varlen_workspace_size": (_sz, [_i32, _i64, _i64] + [_i32] * 5),
+    "ut_xattn_bwd_varlen": (_c.c_int, [_vp] * 13 + [_i32, _i64, _i64] + [_i32] * 5 + [_f32, _i32, _vp, _sz, _vp]),
 }
 
 _lib = None
@@ -417,6 +437,241 @@ def ut_token_mask_from_alpha(alpha, patch: int, threshold: int, radius: int, tok
                                           _p(workspace), ws_bytes, _stream(stream))
 
 
+# The rotary and cross-attention calls take views as well: a token's heads have
+# to be contiguous, the tokens one stride apart (a slice of a fused projection).
+
+def _token_stride(x, name: str) -> int:
+    """Elements from token to token of [..., H, D] rows."""
+    _need(isinstance(x, torch.Tensor) and x.dim() >= 3, f"{name}: rows [..., H, D]")
+    H, D = x.shape[-2:]
+    lead, strides = x.shape[:-2], x.stride()
+    row = H * D
+    if x.numel() == 0:
+        return row
+    _need((D == 1 or strides[-1] == 1) and (H == 1 or strides[-2] == D), f"{name}: heads must be contiguous")
+    step, tokens = 0, 1   # stride of a token, tokens seen from the inner dimensions
+    for n, st in zip(reversed(lead), reversed(strides[:-2])):
+        if n == 1:
+            continue
+        if step == 0:
+            step = st
+        _need(st == step * tokens, f"{name}: tokens must be evenly strided")
+        tokens *= n
+    step = step or row
+    _need(step >= row, f"{name}: tokens overlap")
+    return step
+
+
+def _pv(t, name: str):
+    """Pointer of a (possibly strided) device tensor (None -> NULL)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live in GPU memory")
+    return t.data_ptr()
+
+
+def _same_device(first, *others):
+    for t in others:
+        _need(t is None or t.device == first.device, "tensors on different devices")
+
+
+def _strides(pairs):
+    """Host array of token strides for (tensor or None, name) pairs."""
+    return (ctypes.c_int64 * len(pairs))(*[_token_stride(t, n) if t is not None else 0 for t, n in pairs])
+
+
+def _stream_of(stream, t):
+    """The stream to launch on: the given one, else the current one of t's device."""
+    s = stream if stream is not None else torch.cuda.current_stream(t.device if t.is_cuda else None)
+    _need(s.device == t.device, "the stream belongs to another device than the tensors")
+    return ctypes.c_void_p(s.cuda_stream)
+
+
+def _on(t):
+    """Makes t's device current around a launch."""
+    return torch.cuda.device(t.device) if t.is_cuda else contextlib.nullcontext()
+
+
+def _rope_args(x, y, pos, axis_dims, token_idx, weights):
+    """Checks of the two rotary calls: (n, Hq, Hk, D, axes, weight dtype)."""
+    D, Hq = x.shape[-1], x.shape[-2]
+    n = x.numel() // max(Hq * D, 1)
+    _need(n * Hq * D == x.numel() and Hq * D > 0, "q: rows [..., Hq, D]")
+    Hk = 0
+    if y is not None:
+        _need(y.dim() >= 3 and y.shape[-1] == D and y.dtype == x.dtype, "k: rows [..., Hk, D] of q's head_dim and dtype")
+        Hk = y.shape[-2]
+        _need(Hk > 0 and y.numel() == n * Hk * D, "k: as many tokens as q")
+    _need(pos.dtype == torch.float32 and pos.dim() == 2 and pos.is_contiguous() and pos.shape[1] == len(axis_dims),
+          "pos: contiguous fp32 [rows, axes], a column for each of axis_dims")
+    if token_idx is not None:
+        _need(token_idx.dtype == torch.int32 and token_idx.is_contiguous() and token_idx.numel() == n,
+              "token_idx: contiguous int32 [n]")
+    wd = UT_BF16
+    for w in weights:
+        if w is not None:
+            _need(w.numel() == D and w.is_contiguous(), "weights: contiguous [D]")
+            _need(w.dtype == weights[0].dtype if weights[0] is not None else True, "weights: one dtype")
+            wd = _dtype_code(w)
+    return n, Hq, Hk, D, (ctypes.c_int32 * len(axis_dims))(*axis_dims), wd
+
+
+def ut_qk_rope_fwd(q, k, q_out, k_out, pos, axis_dims, theta: float, token_idx=None, q_weight=None,
+                   k_weight=None, eps: float = 1e-6, interleaved: bool = True, stream=None) -> int:
+    _need(q.dim() >= 3, "q: rows [..., Hq, D]")
+    n, Hq, Hk, D, axes, wd = _rope_args(q, k, pos, axis_dims, token_idx, (q_weight, k_weight))
+    _need(q_out.shape == q.shape and q_out.dtype == q.dtype, "q_out: like q")
+    _need((k_out is None) == (k is None), "k_out goes with k")
+    _need(k is None or (k_out.shape == k.shape and k_out.dtype == k.dtype), "k_out: like k")
+    _same_device(q, k, q_out, k_out, pos, token_idx, q_weight, k_weight)
+    strides = _strides([(q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out")])
+    with _on(q):
+        return lib().ut_qk_rope_fwd(_pv(q, "q"), _pv(k, "k"), _pv(q_out, "q_out"), _pv(k_out, "k_out"), strides,
+                                    _dtype_code(q), n, Hq, Hk, D, _pv(pos, "pos"), pos.shape[0],
+                                    _pv(token_idx, "token_idx"), axes, len(axis_dims), theta,
+                                    UT_ROPE_NEAR if interleaved else UT_ROPE_FAR, _pv(q_weight, "q_weight"),
+                                    _pv(k_weight, "k_weight"), wd, eps, _stream_of(stream, q))
+
+
+def ut_qk_rope_bwd_workspace_size(D: int) -> int:
+    return int(lib().ut_qk_rope_bwd_workspace_size(D))
+
+
+def ut_qk_rope_bwd(dq_out, dk_out, q, k, dq, dk, pos, axis_dims, theta: float, token_idx=None, q_weight=None,
+                   k_weight=None, eps: float = 1e-6, interleaved: bool = True, dq_weight=None, dk_weight=None,
+                   workspace=None, stream=None) -> int:
+    _need(dq_out.dim() >= 3, "dq_out: rows [..., Hq, D]")
+    n, Hq, Hk, D, axes, wd = _rope_args(dq_out, dk_out, pos, axis_dims, token_idx, (q_weight, k_weight))
+    for t, like, nm in ((q, dq_out, "q"), (dq, dq_out, "dq"), (k, dk_out, "k"), (dk, dk_out, "dk")):
+        _need(t is None or (like is not None and t.shape == like.shape and t.dtype == like.dtype),
+              f"{nm}: like its output's gradient")
+    _need(dq is not None and (dk is None) == (dk_out is None), "dq, and dk with dk_out")
+    if q_weight is not None:
+        _need(q is not None and (dk_out is None or k is not None), "q and k are needed with weights")
+    for g in (dq_weight, dk_weight):
+        _need(g is None or (g.dtype == torch.float32 and g.numel() == D and g.is_contiguous()),
+              "dq_weight, dk_weight: contiguous fp32 [D]")
+    _same_device(dq_out, dk_out, q, k, dq, dk, pos, token_idx, q_weight, k_weight, dq_weight, dk_weight, workspace)
+    strides = _strides([(dq_out, "dq_out"), (dk_out, "dk_out"), (q, "q"), (k, "k"), (dq, "dq"), (dk, "dk")])
+    with _on(dq_out):
+        return lib().ut_qk_rope_bwd(_pv(dq_out, "dq_out"), _pv(dk_out, "dk_out"), _pv(q, "q"), _pv(k, "k"),
+                                    _pv(dq, "dq"), _pv(dk, "dk"), strides, _dtype_code(dq_out), n, Hq, Hk, D,
+                                    _pv(pos, "pos"), pos.shape[0], _pv(token_idx, "token_idx"), axes, len(axis_dims),
+                                    theta, UT_ROPE_NEAR if interleaved else UT_ROPE_FAR, _pv(q_weight, "q_weight"),
+                                    _pv(k_weight, "k_weight"), wd, eps, _pv(dq_weight, "dq_weight"),
+                                    _pv(dk_weight, "dk_weight"), _p(workspace),
+                                    _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, dq_out))
+
+
+def _xattn_args(q, k, v, key_mask, dims: int):
+    """Checks of the cross-attention calls: (shape in front of the heads of q, of k, Hq, Hk, D)."""
+    lay = "[B, N, H, D]" if dims == 4 else "[T, H, D]"
+    for t, nm in ((q, "q"), (k, "k"), (v, "v")):
+        _need(t.dim() == dims and t.dtype == torch.bfloat16, f"{nm}: bf16 {lay}")
+    _need(k.shape == v.shape and k.shape[-1] == q.shape[-1], "k, v: one shape, q's head_dim")
+    _need(dims == 3 or k.shape[0] == q.shape[0], "q, k, v: one batch size")
+    if key_mask is not None:
+        _need(key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == k.shape[:-2]
+              and key_mask.is_contiguous(), "key_mask: contiguous uint8 or bool, one value a key token")
+    return q.shape[:-2], k.shape[:-2], q.shape[-2], k.shape[-2], q.shape[-1]
+
+
+def _check_like(t, like, nm):
+    _need(t.shape == like.shape and t.dtype == like.dtype, f"{nm}: bf16, the shape of its counterpart")
+
+
+def _check_cu(cu_q, cu_k):
+    for cu in (cu_q, cu_k):
+        _need(cu.dtype == torch.int32 and cu.dim() == 1 and cu.numel() >= 2 and cu.is_contiguous(),
+              "cu_seqlens: contiguous int32 [B+1]")
+    _need(cu_q.numel() == cu_k.numel(), "cu_seqlens_q and cu_seqlens_k: one number of samples")
+    return cu_q.numel() - 1
+
+
+def ut_xattn_fwd_workspace_size(B: int, Nq: int, Nk: int, Hq: int, Hk: int, D: int) -> int:
+    return int(lib().ut_xattn_fwd_workspace_size(B, Nq, Nk, Hq, Hk, D))
+
+
+def ut_xattn_fwd(q, k, v, o, lse, softmax_scale: float, key_mask=None, workspace=None, stream=None) -> int:
+    (B, Nq), (_, Nk), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 4)
+    _check_like(o, q, "o")
+    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() >= B * Hq * Nq, "lse: fp32 [B,Hq,Nq]")
+    _same_device(q, k, v, o, lse, key_mask, workspace)
+    strides = _strides([(q, "q"), (k, "k"), (v, "v"), (o, "o")])
+    with _on(q):
+        return lib().ut_xattn_fwd(_pv(q, "q"), _pv(k, "k"), _pv(v, "v"), _pv(o, "o"), _pv(lse, "lse"), strides,
+                                  _pv(key_mask, "key_mask"), B, Nq, Nk, Hq, Hk, D, softmax_scale, _p(workspace),
+                                  _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, q))
+
+
+def ut_xattn_fwd_varlen_workspace_size(B: int, Tq: int, max_seqlen_q: int, max_seqlen_k: int, Hq: int, Hk: int,
+                                       D: int) -> int:
+    return int(lib().ut_xattn_fwd_varlen_workspace_size(B, Tq, max_seqlen_q, max_seqlen_k, Hq, Hk, D))
+
+
+def ut_xattn_fwd_varlen(q, k, v, o, lse, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k, max_seqlen_k: int,
+                        softmax_scale: float, key_mask=None, zero_rest: bool = False, workspace=None,
+                        stream=None) -> int:
+    (Tq,), (Tk,), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 3)
+    B = _check_cu(cu_seqlens_q, cu_seqlens_k)
+    _check_like(o, q, "o")
+    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() >= Hq * Tq, "lse: fp32 [Hq,Tq]")
+    _same_device(q, k, v, o, lse, key_mask, cu_seqlens_q, cu_seqlens_k, workspace)
+    strides = _strides([(q, "q"), (k, "k"), (v, "v"), (o, "o")])
+    with _on(q):
+        return lib().ut_xattn_fwd_varlen(_pv(q, "q"), _pv(k, "k"), _pv(v, "v"), _pv(o, "o"), _pv(lse, "lse"), strides,
+                                         _pv(key_mask, "key_mask"), _pv(cu_seqlens_q, "cu_seqlens_q"),
+                                         _pv(cu_seqlens_k, "cu_seqlens_k"), B, Tq, Tk, max_seqlen_q, max_seqlen_k,
+                                         Hq, Hk, D, softmax_scale, int(zero_rest), _p(workspace),
+                                         _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, q))
+
+
+def ut_xattn_bwd_workspace_size(B: int, Nq: int, Nk: int, Hq: int, Hk: int, D: int) -> int:
+    return int(lib().ut_xattn_bwd_workspace_size(B, Nq, Nk, Hq, Hk, D))
+
+
+def _bwd_tensors(q, k, v, o, dout, dq, dk, dv):
+    for t, like, nm in ((o, q, "o"), (dout, q, "dout"), (dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv")):
+        _check_like(t, like, nm)
+    return _strides([(q, "q"), (k, "k"), (v, "v"), (o, "o"), (dout, "dout"), (dq, "dq"), (dk, "dk"), (dv, "dv")])
+
+
+def ut_xattn_bwd(q, k, v, o, dout, lse, dq, dk, dv, softmax_scale: float, key_mask=None, workspace=None,
+                 stream=None) -> int:
+    (B, Nq), (_, Nk), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 4)
+    strides = _bwd_tensors(q, k, v, o, dout, dq, dk, dv)
+    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() >= B * Hq * Nq, "lse: fp32 [B,Hq,Nq]")
+    _same_device(q, k, v, o, dout, lse, dq, dk, dv, key_mask, workspace)
+    with _on(q):
+        return lib().ut_xattn_bwd(_pv(q, "q"), _pv(k, "k"), _pv(v, "v"), _pv(o, "o"), _pv(dout, "dout"),
+                                  _pv(lse, "lse"), _pv(dq, "dq"), _pv(dk, "dk"), _pv(dv, "dv"), strides,
+                                  _pv(key_mask, "key_mask"), B, Nq, Nk, Hq, Hk, D, softmax_scale, _p(workspace),
+                                  _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, q))
+
+
+def ut_xattn_bwd_varlen_workspace_size(B: int, Tq: int, Tk: int, max_seqlen_q: int, max_seqlen_k: int, Hq: int,
+                                       Hk: int, D: int) -> int:
+    return int(lib().ut_xattn_bwd_varlen_workspace_size(B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D))
+
+
+def ut_xattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k,
+                        max_seqlen_k: int, softmax_scale: float, key_mask=None, zero_rest: bool = False,
+                        workspace=None, stream=None) -> int:
+    (Tq,), (Tk,), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 3)
+    B = _check_cu(cu_seqlens_q, cu_seqlens_k)
+    strides = _bwd_tensors(q, k, v, o, dout, dq, dk, dv)
+    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() >= Hq * Tq, "lse: fp32 [Hq,Tq]")
+    _same_device(q, k, v, o, dout, lse, dq, dk, dv, key_mask, cu_seqlens_q, cu_seqlens_k, workspace)
+    with _on(q):
+        return lib().ut_xattn_bwd_varlen(_pv(q, "q"), _pv(k, "k"), _pv(v, "v"), _pv(o, "o"), _pv(dout, "dout"),
+                                         _pv(lse, "lse"), _pv(dq, "dq"), _pv(dk, "dk"), _pv(dv, "dv"), strides,
+                                         _pv(key_mask, "key_mask"), _pv(cu_seqlens_q, "cu_seqlens_q"),
+                                         _pv(cu_seqlens_k, "cu_seqlens_k"), B, Tq, Tk, max_seqlen_q, max_seqlen_k,
+                                         Hq, Hk, D, softmax_scale, int(zero_rest), _p(workspace),
+                                         _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, q))
+
+
 # ---------------------------------------------------------------------------
 # Allocating helpers (raise on error)
 # ---------------------------------------------------------------------------
@@ -596,3 +851,105 @@ def token_mask_from_alpha(alpha, patch: int = 16, threshold: int = 0, radius: in
     _raise("ut_token_mask_from_alpha", ut_token_mask_from_alpha(alpha, patch, threshold, radius, out, ws,
                                                                 stream))
     return out
+
+
+def _alloc_on(stream):
+    """Allocations of a call on `stream` belong to it: the allocator must not
+    hand a workspace on while the kernels still use it."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def _scratch(size: int, device):
+    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+
+
+def qk_rope_fwd(q, k, pos, axis_dims, theta: float = 10000.0, token_idx=None, q_weight=None, k_weight=None,
+                eps: float = 1e-6, interleaved: bool = True, stream=None):
+    """Rotated rows (q_out, k_out) of q [..., Hq, D] and k [..., Hk, D] (None: no
+    keys): positions pos [rows, axes] read through token_idx (kept_idx), axis a
+    taking axis_dims[a] elements of the head; with weights [D] the per-head RMS
+    norm first. interleaved: pairs (2p, 2p + 1), else (p, p + R/2)."""
+    with _alloc_on(stream):
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k is not None else None
+    _raise("ut_qk_rope_fwd", ut_qk_rope_fwd(q, k, q_out, k_out, pos, axis_dims, theta, token_idx, q_weight, k_weight,
+                                            eps, interleaved, stream))
+    return q_out, k_out
+
+
+def qk_rope_bwd(dq_out, dk_out, pos, axis_dims, theta: float = 10000.0, token_idx=None, q=None, k=None,
+                q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = True, workspace=None, stream=None):
+    """(dq, dk, dq_weight, dk_weight) of qk_rope_fwd. With weights, q and k are the
+    forward's inputs and the weights' gradients are fp32 [D]; without, they are
+    None."""
+    dev, D = dq_out.device, dq_out.shape[-1]
+    dqw = dkw = None
+    with _alloc_on(stream):
+        dq = torch.empty(dq_out.shape, dtype=dq_out.dtype, device=dev)
+        dk = torch.empty(dk_out.shape, dtype=dk_out.dtype, device=dev) if dk_out is not None else None
+        if q_weight is not None:
+            dqw = torch.empty(D, dtype=torch.float32, device=dev)
+            dkw = torch.empty(D, dtype=torch.float32, device=dev) if dk_out is not None else None
+            if workspace is None:
+                workspace = _scratch(ut_qk_rope_bwd_workspace_size(D), dev)
+    _raise("ut_qk_rope_bwd", ut_qk_rope_bwd(dq_out, dk_out, q, k, dq, dk, pos, axis_dims, theta, token_idx, q_weight,
+                                            k_weight, eps, interleaved, dqw, dkw, workspace, stream))
+    return dq, dk, dqw, dkw
+
+
+def xattn_fwd(q, k, v, softmax_scale: float, key_mask=None, workspace=None, stream=None):
+    """Cross attention of q [B, Nq, Hq, D] to k, v [B, Nk, Hk, D], key_mask
+    [B, Nk] (nonzero: in use): (o like q, lse [B, Hq, Nq])."""
+    B, Nq, Hq, D = q.shape
+    with _alloc_on(stream):
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty((B, Hq, Nq), dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = _scratch(ut_xattn_fwd_workspace_size(B, Nq, k.shape[1], Hq, k.shape[2], D), q.device)
+    _raise("ut_xattn_fwd", ut_xattn_fwd(q, k, v, o, lse, softmax_scale, key_mask, workspace, stream))
+    return o, lse
+
+
+def xattn_bwd(q, k, v, o, dout, lse, softmax_scale: float, key_mask=None, workspace=None, stream=None):
+    """(dq, dk, dv) of xattn_fwd."""
+    B, Nq, Hq, D = q.shape
+    with _alloc_on(stream):
+        dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
+        if workspace is None:
+            workspace = _scratch(ut_xattn_bwd_workspace_size(B, Nq, k.shape[1], Hq, k.shape[2], D), q.device)
+    _raise("ut_xattn_bwd", ut_xattn_bwd(q, k, v, o, dout, lse, dq, dk, dv, softmax_scale, key_mask, workspace, stream))
+    return dq, dk, dv
+
+
+def xattn_fwd_varlen(q, k, v, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k, max_seqlen_k: int, softmax_scale: float,
+                     key_mask=None, workspace=None, stream=None):
+    """Cross attention of packed samples: q [Tq, Hq, D] to k, v [Tk, Hk, D], sample
+    b between its offsets on both sides: (o like q, lse [Hq, Tq]). Rows behind
+    the last sample are 0 and -inf."""
+    Tq, Hq, D = q.shape
+    with _alloc_on(stream):
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty((Hq, Tq), dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = _scratch(ut_xattn_fwd_varlen_workspace_size(cu_seqlens_q.numel() - 1, Tq, max_seqlen_q,
+                                                                    max_seqlen_k, Hq, k.shape[1], D), q.device)
+    _raise("ut_xattn_fwd_varlen",
+           ut_xattn_fwd_varlen(q, k, v, o, lse, cu_seqlens_q, max_seqlen_q, cu_seqlens_k, max_seqlen_k, softmax_scale,
+                               key_mask, True, workspace, stream))
+    return o, lse
+
+
+def xattn_bwd_varlen(q, k, v, o, dout, lse, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k, max_seqlen_k: int,
+                     softmax_scale: float, key_mask=None, workspace=None, stream=None):
+    """(dq, dk, dv) of xattn_fwd_varlen; rows behind the last sample are 0."""
+    Tq, Hq, D = q.shape
+    with _alloc_on(stream):
+        dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
+        if workspace is None:
+            workspace = _scratch(ut_xattn_bwd_varlen_workspace_size(cu_seqlens_q.numel() - 1, Tq, k.shape[0],
+                                                                    max_seqlen_q, max_seqlen_k, Hq, k.shape[1], D),
+                                 q.device)
+    _raise("ut_xattn_bwd_varlen",
+           ut_xattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_seqlen_q, cu_seqlens_k,
+                               max_seqlen_k, softmax_scale, key_mask, True, workspace, stream))
+    return dq, dk, dv

@@ -668,4 +668,389 @@ ut_status ut_token_mask_from_alpha(const uint8_t* alpha, int32_t V, int32_t Hp, 
                    "token mask launch");
 }
 
+namespace {
+// Shape, strides and positions shared by the two rotary calls; fills sh.
+ut_status check_rope(const char* fn, int64_t n, int32_t Hq, int32_t Hk, int32_t D, ut_dtype dtype,
+                     const float* pos, int64_t pos_rows, const int32_t* token_idx,
+                     const int32_t* axis_dims_host, int32_t n_axes, double theta,
+                     ut_rope_pairs pairs, const void* q_weight, const void* k_weight,
+                     ut_dtype w_dtype, float eps, RopeShape* sh) {
+  if (n < 0 || n >= ((int64_t)1 << 31))
+    return fail(UT_ERR_INVALID_ARG, "%s: n must be in [0, 2^31) (got %lld)", fn, (long long)n);
+  if (Hq < 1 || Hk < 0)
+    return fail(UT_ERR_INVALID_ARG, "%s: Hq must be >= 1 and Hk >= 0 (got %d, %d)", fn, Hq, Hk);
+  if (Hq > 65536 || Hk > 65536)
+    return fail(UT_ERR_INVALID_ARG, "%s: more than 65536 heads (%d, %d)", fn, Hq, Hk);
+  if (D < 8 || D % 8 != 0 || D > kRopeMaxDim)
+    return fail(UT_ERR_UNSUPPORTED, "%s: head_dim %d unsupported (a multiple of 8 up to %d)", fn, D,
+                kRopeMaxDim);
+  if (dtype != UT_BF16 && dtype != UT_F32)
+    return fail(UT_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, (int)dtype);
+  if (pairs != UT_ROPE_NEAR && pairs != UT_ROPE_FAR)
+    return fail(UT_ERR_INVALID_ARG, "%s: unknown pair layout %d", fn, (int)pairs);
+  if (!axis_dims_host || n_axes < 1 || n_axes > kRopeMaxAxes)
+    return fail(UT_ERR_INVALID_ARG, "%s: 1 to %d axes and their sizes are needed (got %d)", fn,
+                kRopeMaxAxes, n_axes);
+  int64_t sum = 0;
+  for (int x = 0; x < n_axes; ++x) {
+    if (axis_dims_host[x] < 2 || axis_dims_host[x] % 2 != 0)
+      return fail(UT_ERR_INVALID_ARG, "%s: axis %d: size must be positive and even (got %d)", fn, x,
+                  axis_dims_host[x]);
+    sh->dims[x] = axis_dims_host[x];
+    sum += axis_dims_host[x];
+  }
+  if (sum > D)
+    return fail(UT_ERR_INVALID_ARG, "%s: the axes take %lld elements of a head of %d", fn,
+                (long long)sum, D);
+  if (pairs == UT_ROPE_FAR && sum % 8 != 0)
+    return fail(UT_ERR_UNSUPPORTED, "%s: far pairs need axes of a multiple of 8 in all (got %lld)",
+                fn, (long long)sum);
+  if (!std::isfinite(theta) || !(theta > 0.0))
+    return fail(UT_ERR_INVALID_ARG, "%s: theta must be finite and > 0 (got %g)", fn, theta);
+  if (pos_rows < 1 || pos_rows >= ((int64_t)1 << 31))
+    return fail(UT_ERR_INVALID_ARG, "%s: pos_rows must be in [1, 2^31) (got %lld)", fn,
+                (long long)pos_rows);
+  UT_TRY(check_ptr(fn, "pos", pos, 4));
+  if (token_idx && !aligned(token_idx, 4))
+    return fail(UT_ERR_INVALID_ARG, "%s: token_idx must be 4-byte aligned", fn);
+  if (Hk > 0 && (q_weight == nullptr) != (k_weight == nullptr))
+    return fail(UT_ERR_INVALID_ARG, "%s: q_weight and k_weight must both be NULL or both set", fn);
+  if (q_weight) {
+    if (w_dtype != UT_BF16 && w_dtype != UT_F32)
+      return fail(UT_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, (int)w_dtype);
+    const uintptr_t wa = w_dtype == UT_BF16 ? 2 : 4;
+    UT_TRY(check_ptr(fn, "q_weight", q_weight, wa));
+    if (Hk > 0) UT_TRY(check_ptr(fn, "k_weight", k_weight, wa));
+    if (!std::isfinite(eps) || !(eps > 0.f))
+      return fail(UT_ERR_INVALID_ARG, "%s: eps must be finite and > 0 (got %g)", fn, (double)eps);
+  }
+  sh->n = n;
+  sh->D = D;
+  sh->bf16 = dtype == UT_BF16;
+  sh->w_bf16 = w_dtype == UT_BF16;
+  sh->far_pairs = pairs == UT_ROPE_FAR;
+  sh->pos = pos;
+  sh->pos_rows = pos_rows;
+  sh->idx = token_idx;
+  sh->n_axes = n_axes;
+  sh->theta = theta;
+  sh->eps = eps;
+  return UT_OK;
+}
+
+// Token stride i of `strides_host` (NULL: rows of H heads back to back): whole
+// rows apart, and in steps of `step` elements, so that rows stay aligned.
+ut_status check_stride(const char* fn, const char* name, const int64_t* strides_host, int i,
+                       int64_t row, int64_t step, int64_t limit, int64_t* out) {
+  *out = strides_host ? strides_host[i] : row;
+  if (*out < row || *out % step != 0)
+    return fail(UT_ERR_INVALID_ARG,
+                "%s: stride of %s must be a multiple of %lld and at least a row of %lld (got %lld)", fn,
+                name, (long long)step, (long long)row, (long long)*out);
+  if (*out >= limit)
+    return fail(UT_ERR_UNSUPPORTED, "%s: stride of %s must be below %lld elements (got %lld)", fn,
+                name, (long long)limit, (long long)*out);
+  return UT_OK;
+}
+constexpr int64_t kRopeMaxStride = (int64_t)1 << 31;
+}  // namespace
+
+ut_status ut_qk_rope_fwd(const void* q, const void* k, void* q_out, void* k_out,
+                         const int64_t* strides_host, ut_dtype dtype, int64_t n, int32_t Hq,
+                         int32_t Hk, int32_t D, const float* pos, int64_t pos_rows,
+                         const int32_t* token_idx, const int32_t* axis_dims_host, int32_t n_axes,
+                         double theta, ut_rope_pairs pairs, const void* q_weight,
+                         const void* k_weight, ut_dtype w_dtype, float eps, hipStream_t stream) {
+  static const char* fn = "ut_qk_rope_fwd";
+  g_last_error[0] = 0;
+  RopeShape sh{};
+  UT_TRY(check_rope(fn, n, Hq, Hk, D, dtype, pos, pos_rows, token_idx, axis_dims_host, n_axes, theta,
+                    pairs, q_weight, k_weight, w_dtype, eps, &sh));
+  const int64_t step = dtype == UT_BF16 ? 8 : 4;
+  RopeSide side[2] = {};
+  side[0] = RopeSide{q, nullptr, q_out, q_weight, 0, 0, 0, Hq};
+  UT_TRY(check_stride(fn, "q", strides_host, 0, (int64_t)Hq * D, step, kRopeMaxStride, &side[0].sx));
+  UT_TRY(check_stride(fn, "q_out", strides_host, 2, (int64_t)Hq * D, step, kRopeMaxStride, &side[0].so));
+  if (Hk > 0) {
+    side[1] = RopeSide{k, nullptr, k_out, k_weight, 0, 0, 0, Hk};
+    UT_TRY(check_stride(fn, "k", strides_host, 1, (int64_t)Hk * D, step, kRopeMaxStride, &side[1].sx));
+    UT_TRY(check_stride(fn, "k_out", strides_host, 3, (int64_t)Hk * D, step, kRopeMaxStride, &side[1].so));
+  }
+  if (n == 0) return UT_OK;
+  UT_TRY(check_ptr(fn, "q", q, 16));
+  UT_TRY(check_ptr(fn, "q_out", q_out, 16));
+  if (Hk > 0) {
+    UT_TRY(check_ptr(fn, "k", k, 16));
+    UT_TRY(check_ptr(fn, "k_out", k_out, 16));
+  }
+  return check_hip(launch_qk_rope(sh, side, false, nullptr, nullptr, nullptr, stream), "rotary launch");
+}
+
+size_t ut_qk_rope_bwd_workspace_size(int32_t D) {
+  if (D < 1 || D > kRopeMaxDim) return 0;
+  return (size_t)kRopeParts * 2 * D * sizeof(float);
+}
+
+ut_status ut_qk_rope_bwd(const void* dq_out, const void* dk_out, const void* q, const void* k,
+                         void* dq, void* dk, const int64_t* strides_host, ut_dtype dtype, int64_t n,
+                         int32_t Hq, int32_t Hk, int32_t D, const float* pos, int64_t pos_rows,
+                         const int32_t* token_idx, const int32_t* axis_dims_host, int32_t n_axes,
+                         double theta, ut_rope_pairs pairs, const void* q_weight,
+                         const void* k_weight, ut_dtype w_dtype, float eps, float* dq_weight,
+                         float* dk_weight, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream) {
+  static const char* fn = "ut_qk_rope_bwd";
+  g_last_error[0] = 0;
+  RopeShape sh{};
+  UT_TRY(check_rope(fn, n, Hq, Hk, D, dtype, pos, pos_rows, token_idx, axis_dims_host, n_axes, theta,
+                    pairs, q_weight, k_weight, w_dtype, eps, &sh));
+  const int64_t step = dtype == UT_BF16 ? 8 : 4;
+  const bool norm = q_weight != nullptr;
+  RopeSide side[2] = {};
+  side[0] = RopeSide{q, dq_out, dq, q_weight, 0, 0, 0, Hq};
+  UT_TRY(check_stride(fn, "dq_out", strides_host, 0, (int64_t)Hq * D, step, kRopeMaxStride, &side[0].sdy));
+  if (norm) UT_TRY(check_stride(fn, "q", strides_host, 2, (int64_t)Hq * D, step, kRopeMaxStride, &side[0].sx));
+  UT_TRY(check_stride(fn, "dq", strides_host, 4, (int64_t)Hq * D, step, kRopeMaxStride, &side[0].so));
+  if (Hk > 0) {
+    side[1] = RopeSide{k, dk_out, dk, k_weight, 0, 0, 0, Hk};
+    UT_TRY(check_stride(fn, "dk_out", strides_host, 1, (int64_t)Hk * D, step, kRopeMaxStride, &side[1].sdy));
+    if (norm) UT_TRY(check_stride(fn, "k", strides_host, 3, (int64_t)Hk * D, step, kRopeMaxStride, &side[1].sx));
+    UT_TRY(check_stride(fn, "dk", strides_host, 5, (int64_t)Hk * D, step, kRopeMaxStride, &side[1].so));
+  }
+  if (n > 0) {
+    UT_TRY(check_ptr(fn, "dq_out", dq_out, 16));
+    UT_TRY(check_ptr(fn, "dq", dq, 16));
+    if (norm) UT_TRY(check_ptr(fn, "q", q, 16));
+    if (Hk > 0) {
+      UT_TRY(check_ptr(fn, "dk_out", dk_out, 16));
+      UT_TRY(check_ptr(fn, "dk", dk, 16));
+      if (norm) UT_TRY(check_ptr(fn, "k", k, 16));
+    }
+  }
+  if (norm) {
+    UT_TRY(check_ptr(fn, "dq_weight", dq_weight, 4));
+    if (Hk > 0) UT_TRY(check_ptr(fn, "dk_weight", dk_weight, 4));
+    const size_t need = ut_qk_rope_bwd_workspace_size(D);
+    if (!workspace || workspace_bytes < need)
+      return fail(UT_ERR_WORKSPACE, "%s: workspace of %zu bytes required (got %zu)", fn, need,
+                  workspace ? workspace_bytes : (size_t)0);
+    UT_TRY(check_ptr(fn, "workspace", workspace, 16));
+  } else if (n == 0) {
+    return UT_OK;
+  }
+  return check_hip(launch_qk_rope(sh, side, true, static_cast<float*>(workspace), dq_weight,
+                                  Hk > 0 ? dk_weight : nullptr, stream),
+                   "rotary backward launch");
+}
+
+namespace {
+// Sizes shared by the cross-attention calls; fills a (T = 0 and null cu: uniform).
+ut_status check_xattn(const char* fn, int32_t B, int64_t Tq, int64_t Tk, int32_t Nq, int32_t Nk,
+                      int32_t Hq, int32_t Hk, int32_t D, float scale, XArgs* a) {
+  if (B < 1 || Nq < 0 || Nk < 0 || Hq < 1 || Hk < 1)
+    return fail(UT_ERR_INVALID_ARG, "%s: B, Hq, Hk must be >= 1, lengths >= 0 (got %d, %d, %d, %d, %d)",
+                fn, B, Hq, Hk, Nq, Nk);
+  if (Hq % Hk != 0)
+    return fail(UT_ERR_INVALID_ARG, "%s: Hq = %d is no multiple of Hk = %d", fn, Hq, Hk);
+  if (D < 8 || D % 8 != 0 || D > 128)
+    return fail(UT_ERR_UNSUPPORTED, "%s: head_dim %d unsupported (a multiple of 8 up to 128)", fn, D);
+  // as in the block-sparse calls: a running maximum of the scaled scores
+  if (!std::isfinite(scale) || !(scale > 0.f))
+    return fail(UT_ERR_INVALID_ARG, "%s: softmax_scale must be finite and > 0 (got %g)", fn,
+                (double)scale);
+  if (Tq < 0 || Tk < 0 || Tq >= ((int64_t)1 << 31) || Tk >= ((int64_t)1 << 31))
+    return fail(UT_ERR_INVALID_ARG, "%s: token counts %lld, %lld outside [0, 2^31)", fn,
+                (long long)Tq, (long long)Tk);
+  // one thread or more a row, launches of less than 2^32 threads
+  const int64_t most = (int64_t)1 << 27;
+  if (Tq * Hq >= most || Tk * Hk >= most || (int64_t)B * Nq * Hq >= most || (int64_t)B * Nk * Hk >= most)
+    return fail(UT_ERR_INVALID_ARG, "%s: problem too large (2^27 rows of a head or more)", fn);
+  a->B = B;
+  a->Nq = Nq;
+  a->Nk = Nk;
+  a->Hq = Hq;
+  a->Hk = Hk;
+  a->G = Hq / Hk;
+  a->D = D;
+  a->Tq = Tq;
+  a->Tk = Tk;
+  a->scale = scale;
+  return UT_OK;
+}
+
+// Sample offsets of one side; under UT_VALIDATE copied to the host and checked
+// (they may end before T: the tokens behind belong to no sample).
+ut_status check_cu(const char* fn, const char* name, const int32_t* cu, int32_t B, int64_t T,
+                   int32_t max_seqlen, hipStream_t stream) {
+  UT_TRY(check_ptr(fn, name, cu, 4));
+  if (!validate_mode()) return UT_OK;
+  std::vector<int32_t> v((size_t)B + 1);
+  UT_TRY(check_hip(hipMemcpyAsync(v.data(), cu, v.size() * sizeof(int32_t), hipMemcpyDeviceToHost,
+                                  stream),
+                   "validate copy"));
+  UT_TRY(check_hip(hipStreamSynchronize(stream), "validate sync"));
+  if (v[(size_t)B] > T)
+    return fail(UT_ERR_INVALID_ARG, "%s: %s ends at %d, past T = %lld", fn, name, v[(size_t)B],
+                (long long)T);
+  return check_cu_seqlens(fn, v.data(), B, v[(size_t)B], max_seqlen);
+}
+
+struct XTensor {
+  const char* name;
+  const void* p;
+  int* stride;      // in XArgs
+  bool keys;        // rows of Hk heads for Tk tokens, else Hq and Tq
+};
+ut_status check_xtensors(const char* fn, const XTensor* t, int count, const int64_t* strides_host,
+                         const XArgs& a) {
+  for (int i = 0; i < count; ++i) {
+    int64_t s = 0;
+    UT_TRY(check_stride(fn, t[i].name, strides_host, i, (int64_t)(t[i].keys ? a.Hk : a.Hq) * a.D, 8,
+                        kXMaxStride, &s));
+    *t[i].stride = (int)s;
+    if ((t[i].keys ? a.Tk : a.Tq) > 0) UT_TRY(check_ptr(fn, t[i].name, t[i].p, 16));
+  }
+  return UT_OK;
+}
+
+ut_status check_space(const char* fn, size_t need, const void* workspace, size_t bytes) {
+  if (need == 0) return UT_OK;
+  if (!workspace || bytes < need)
+    return fail(UT_ERR_WORKSPACE, "%s: workspace of %zu bytes required (got %zu)", fn, need,
+                workspace ? bytes : (size_t)0);
+  return check_ptr(fn, "workspace", workspace, 16);
+}
+
+ut_status xattn_fwd(const char* fn, XArgs& a, const void* q, const void* k, const void* v, void* o,
+                    float* lse, const int64_t* strides_host, const uint8_t* key_mask, void* workspace,
+                    size_t workspace_bytes, bool zero_rest, hipStream_t stream) {
+  const XTensor t[] = {{"q", q, &a.sq, false}, {"k", k, &a.sk, true}, {"v", v, &a.sv, true},
+                       {"o", o, &a.so, false}};
+  UT_TRY(check_xtensors(fn, t, 4, strides_host, a));
+  if (a.Tq > 0) UT_TRY(check_ptr(fn, "lse", lse, 4));
+  UT_TRY(check_space(fn, xattn_fwd_workspace(a), workspace, workspace_bytes));
+  a.q = q, a.k = k, a.v = v, a.o = o, a.lse = lse, a.mask = key_mask;
+  if (a.Tq == 0) return UT_OK;
+  if (zero_rest)
+    UT_TRY(check_hip(launch_xattn_clear(a.cuq, a.B, a.Tq, a.Hq * a.D, o, a.so, nullptr, 0, lse, a.Hq, stream),
+                     "clear launch"));
+  if (a.Nq == 0) return UT_OK;
+  return check_hip(launch_xattn_fwd(a, workspace, stream), "cross attention launch");
+}
+
+ut_status xattn_bwd(const char* fn, XArgs& a, const void* q, const void* k, const void* v,
+                    const void* o, const void* dout, const float* lse, void* dq, void* dk, void* dv,
+                    const int64_t* strides_host, const uint8_t* key_mask, void* workspace,
+                    size_t workspace_bytes, bool zero_rest, hipStream_t stream) {
+  const XTensor t[] = {{"q", q, &a.sq, false},     {"k", k, &a.sk, true},    {"v", v, &a.sv, true},
+                       {"o", o, &a.so, false},     {"dout", dout, &a.sdo, false},
+                       {"dq", dq, &a.sdq, false},  {"dk", dk, &a.sdk, true}, {"dv", dv, &a.sdv, true}};
+  UT_TRY(check_xtensors(fn, t, 8, strides_host, a));
+  if (a.Tq > 0) UT_TRY(check_ptr(fn, "lse", lse, 4));
+  UT_TRY(check_space(fn, xattn_bwd_workspace(a), workspace, workspace_bytes));
+  a.q = q, a.k = k, a.v = v, a.o_in = o, a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv;
+  a.lse = const_cast<float*>(lse), a.mask = key_mask;
+  if (a.Tq == 0 && a.Tk == 0) return UT_OK;
+  if (zero_rest && a.Tq > 0)
+    UT_TRY(check_hip(launch_xattn_clear(a.cuq, a.B, a.Tq, a.Hq * a.D, dq, a.sdq, nullptr, 0, nullptr, 0, stream),
+                     "clear launch"));
+  if (zero_rest && a.Tk > 0)
+    UT_TRY(check_hip(launch_xattn_clear(a.cuk, a.B, a.Tk, a.Hk * a.D, dk, a.sdk, dv, a.sdv, nullptr, 0, stream),
+                     "clear launch"));
+  return check_hip(launch_xattn_bwd(a, workspace, stream), "cross attention backward launch");
+}
+
+// Workspace sizes: 0 for sizes that the calls refuse.
+bool xattn_sizes(int32_t B, int64_t Tq, int64_t Tk, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk,
+                 int32_t D, XArgs* a) {
+  const bool ok = check_xattn("ut_xattn", B, Tq, Tk, Nq, Nk, Hq, Hk, D, 1.f, a) == UT_OK;
+  g_last_error[0] = 0;
+  return ok;
+}
+}  // namespace
+
+size_t ut_xattn_fwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk, int32_t D) {
+  XArgs a{};
+  return xattn_sizes(B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, &a) ? xattn_fwd_workspace(a) : 0;
+}
+
+ut_status ut_xattn_fwd(const void* q, const void* k, const void* v, void* o, float* lse,
+                       const int64_t* strides_host, const uint8_t* key_mask, int32_t B, int32_t Nq,
+                       int32_t Nk, int32_t Hq, int32_t Hk, int32_t D, float softmax_scale,
+                       void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  static const char* fn = "ut_xattn_fwd";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_xattn(fn, B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, softmax_scale, &a));
+  return xattn_fwd(fn, a, q, k, v, o, lse, strides_host, key_mask, workspace, workspace_bytes, false,
+                   stream);
+}
+
+size_t ut_xattn_fwd_varlen_workspace_size(int32_t B, int64_t Tq, int32_t max_seqlen_q,
+                                          int32_t max_seqlen_k, int32_t Hq, int32_t Hk, int32_t D) {
+  XArgs a{};
+  return xattn_sizes(B, Tq, 0, max_seqlen_q, max_seqlen_k, Hq, Hk, D, &a) ? xattn_fwd_workspace(a) : 0;
+}
+
+ut_status ut_xattn_fwd_varlen(const void* q, const void* k, const void* v, void* o, float* lse,
+                              const int64_t* strides_host, const uint8_t* key_mask,
+                              const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t B,
+                              int64_t Tq, int64_t Tk, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                              int32_t Hq, int32_t Hk, int32_t D, float softmax_scale,
+                              int32_t zero_rest, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream) {
+  static const char* fn = "ut_xattn_fwd_varlen";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_xattn(fn, B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, softmax_scale, &a));
+  UT_TRY(check_cu(fn, "cu_seqlens_q", cu_seqlens_q, B, Tq, max_seqlen_q, stream));
+  UT_TRY(check_cu(fn, "cu_seqlens_k", cu_seqlens_k, B, Tk, max_seqlen_k, stream));
+  a.cuq = cu_seqlens_q, a.cuk = cu_seqlens_k;
+  return xattn_fwd(fn, a, q, k, v, o, lse, strides_host, key_mask, workspace, workspace_bytes,
+                   zero_rest != 0, stream);
+}
+
+size_t ut_xattn_bwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk, int32_t D) {
+  XArgs a{};
+  return xattn_sizes(B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, &a) ? xattn_bwd_workspace(a) : 0;
+}
+
+ut_status ut_xattn_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                       const float* lse, void* dq, void* dk, void* dv, const int64_t* strides_host,
+                       const uint8_t* key_mask, int32_t B, int32_t Nq, int32_t Nk, int32_t Hq,
+                       int32_t Hk, int32_t D, float softmax_scale, void* workspace,
+                       size_t workspace_bytes, hipStream_t stream) {
+  static const char* fn = "ut_xattn_bwd";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_xattn(fn, B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, softmax_scale, &a));
+  return xattn_bwd(fn, a, q, k, v, o, dout, lse, dq, dk, dv, strides_host, key_mask, workspace,
+                   workspace_bytes, false, stream);
+}
+
+size_t ut_xattn_bwd_varlen_workspace_size(int32_t B, int64_t Tq, int64_t Tk, int32_t max_seqlen_q,
+                                          int32_t max_seqlen_k, int32_t Hq, int32_t Hk, int32_t D) {
+  XArgs a{};
+  return xattn_sizes(B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, &a) ? xattn_bwd_workspace(a) : 0;
+}
+
+ut_status ut_xattn_bwd_varlen(const void* q, const void* k, const void* v, const void* o,
+                              const void* dout, const float* lse, void* dq, void* dk, void* dv,
+                              const int64_t* strides_host, const uint8_t* key_mask,
+                              const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t B,
+                              int64_t Tq, int64_t Tk, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                              int32_t Hq, int32_t Hk, int32_t D, float softmax_scale,
+                              int32_t zero_rest, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream) {
+  static const char* fn = "ut_xattn_bwd_varlen";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_xattn(fn, B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, softmax_scale, &a));
+  UT_TRY(check_cu(fn, "cu_seqlens_q", cu_seqlens_q, B, Tq, max_seqlen_q, stream));
+  UT_TRY(check_cu(fn, "cu_seqlens_k", cu_seqlens_k, B, Tk, max_seqlen_k, stream));
+  a.cuq = cu_seqlens_q, a.cuk = cu_seqlens_k;
+  return xattn_bwd(fn, a, q, k, v, o, dout, lse, dq, dk, dv, strides_host, key_mask, workspace,
+                   workspace_bytes, zero_rest != 0, stream);
+}
+
 }  // extern "C"

@@ -159,10 +159,10 @@ __device__ inline __amdgpu_buffer_rsrc_t buffer_rsrc(const void* base, int bytes
 }
 
 // One 16-byte-per-lane buffer load straight into LDS: lane L writes at
-// lds + 16 L (lds must be wave-uniform).
-__device__ inline void buffer_load_lds16(__amdgpu_buffer_rsrc_t rs, char* lds, int voffset) {
+// lds + 16 L (lds must be wave-uniform). soffset: a uniform part of the offset.
+__device__ inline void buffer_load_lds16(__amdgpu_buffer_rsrc_t rs, char* lds, int voffset, int soffset = 0) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)lds, 16,
-                                           voffset, 0, 0, 0);
+                                           voffset, soffset, 0, 0);
 }
 
 // Tile lt = bh nblk + i of this workgroup and its list, entries p0 .. p1 - 1: in

@@ -175,4 +175,60 @@ hipError_t launch_composite(const void* packed, int64_t n_kept, const int32_t* i
 hipError_t launch_token_mask(const uint8_t* alpha, int V, int Hp, int Wp, int patch, int thr,
                              int radius, uint8_t* out, uint8_t* pooled, hipStream_t s);
 
+// ---- Rotary positions with the per-head norm (rope.hip) ----
+constexpr int kRopeMaxDim = 256, kRopeMaxAxes = 4;
+constexpr int kRopeParts = 1024;   // partial rows of the weights' gradients (fixed order)
+// Queries (side 0) or keys (side 1): rows of H heads, token strides in elements.
+struct RopeSide {
+  const void* x;    // rows in (backward: the forward's, with the norm only)
+  const void* dy;   // backward: gradient of the rows out
+  void* out;        // rows out (backward: gradient of the rows in)
+  const void* w;    // [D] norm weights, or null without the norm
+  int64_t sx, sdy, so;
+  int H;
+};
+struct RopeShape {
+  int64_t n;
+  int D;
+  bool bf16, w_bf16, far_pairs;
+  const float* pos;
+  int64_t pos_rows;
+  const int32_t* idx;
+  int dims[kRopeMaxAxes], n_axes;
+  double theta;
+  float eps;
+};
+// part, dwq, dwk: backward with the norm only (dwq, dwk may be null).
+hipError_t launch_qk_rope(const RopeShape& sh, const RopeSide (&side)[2], bool bwd, float* part,
+                          float* dwq, float* dwk, hipStream_t s);
+
+// ---- Cross attention (xattn_fwd.hip, xattn_bwd.hip) ----
+// Uniform batches: cuq = cuk = null, Tq = B Nq, Tk = B Nk. Packed samples: both
+// set, Nq and Nk the longest. Strides in elements from token to token, below
+// kXMaxStride, so that a 64-row tile stays within 32-bit offsets.
+constexpr int kXMaxStride = 1 << 22;
+struct XArgs {
+  const void *q, *k, *v, *dout;
+  const void* o_in;                // backward: the forward's output
+  void *o, *dq, *dk, *dv;
+  float* lse;
+  const uint8_t* mask;             // a byte a key token, or null
+  const int32_t *cuq, *cuk;
+  int64_t Tq, Tk;
+  int B, Nq, Nk, Hq, Hk, G, D;     // G = Hq / Hk
+  int sq, sk, sv, so, sdo, sdq, sdk, sdv;
+  float scale;
+};
+// Key ranges of the forward (1: one range, no workspace) and, for more, the
+// bytes of the ranges' partial results.
+int xattn_fwd_splits(const XArgs& a);
+size_t xattn_fwd_workspace(const XArgs& a);
+hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s);
+size_t xattn_bwd_workspace(const XArgs& a);
+hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s);
+// Packed rows x (and y, unless null) of `width` elements at and past the last
+// sample's end to 0, and lse [H, T] there (unless null) to -inf.
+hipError_t launch_xattn_clear(const int32_t* cu, int B, int64_t T, int width, void* x, int sx, void* y, int sy,
+                              float* lse, int H, hipStream_t s);
+
 }  // namespace ut

@@ -1,0 +1,536 @@
+// Attention of image tokens to an encoder's states of another length, backward,
+// on gfx950. With P = exp(S scale - LSE) over the keys in use, delta =
+// rowsum(dO o O) and dS = P o (dO V^T - delta):
+//   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO,
+// dK and dV summed over the query heads that share the key head. Launches:
+//
+//   prep  : per query row, LSE log2(e) and -delta (fp32, two planes of the
+//           workspace);
+//   dK/dV : key-stationary. A workgroup owns 128 keys of a key head, one wave
+//           per 32, and walks the 32-token tiles of every query head of the
+//           group: S and dP on 32x32x16 bf16 MFMA, dV^T += dO^T P and
+//           dK^T += Q^T dS on 16x16x32, accumulators in fp32 registers. Few keys
+//           (an encoder's states against a picture's tokens) make few
+//           workgroups, so the query tiles are split over workgroups, each
+//           writes fp32 partial sums, and a join adds them in a fixed order;
+//   dQ    : query-stationary, S and dP computed again, dQ^T += K^T dS^T; with
+//           few rows the keys are split the same way.
+//
+// Rounding: P and dS to bf16 before their second products (half a step each,
+// 2^-9 relative), all sums in fp32. No atomics: equal results on every run.
+// Keys not in use: the dQ pass reads zeros in their place and sets their P to
+// 0; in the dK/dV pass a key is a column of its own, whatever it holds, and is
+// stored as 0.
+#include <algorithm>
+#include <type_traits>
+
+#include "xattn_util.h"
+
+namespace ut {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kBwdKeys = 128;   // keys of a dK/dV workgroup
+constexpr int kRowTile = 32;    // query tokens of a dK/dV step
+
+// ---------------------------------------------------------------------------
+// prep
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void xattn_prep_kernel(const XArgs a, float* __restrict__ aux) {
+  const int64_t rows = a.Tq * a.Hq;
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);   // token-major
+  const int c = threadIdx.x & 15;
+  const int64_t tok = row / a.Hq;
+  const int h = (int)(row - tok * a.Hq);
+  float acc = 0.f;
+  if (row < rows && 8 * c < a.D) {
+    const bf16x8 o = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.o_in) + tok * a.so + h * a.D + 8 * c);
+    const bf16x8 d = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.dout) + tok * a.sdo + h * a.D + 8 * c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc += (float)o[e] * (float)d[e];
+  }
+#pragma unroll
+  for (int m = 8; m >= 1; m >>= 1) acc += __shfl_xor(acc, m, 64);
+  if (row < rows && c == 0) {
+    const int64_t r = a.cuq ? (int64_t)h * a.Tq + tok : (tok / a.Nq * a.Hq + h) * a.Nq + tok % a.Nq;
+    aux[r] = a.lse[r] * kLog2e;
+    aux[rows + r] = -acc;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dQ
+// ---------------------------------------------------------------------------
+// part: fp32 [split][token][Hq][D], null with one split.
+template <int DP, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_dq_kernel(const XArgs a, const float* __restrict__ aux,
+                                                                            const unsigned rtiles, const unsigned splits,
+                                                                            const bool by_xcd, float* __restrict__ part) {
+  constexpr int ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
+  __shared__ __attribute__((aligned(1024))) char k_lds0[TILEB];
+  __shared__ __attribute__((aligned(1024))) char k_lds1[TILEB];
+  __shared__ __attribute__((aligned(1024))) char v_lds0[TILEB];
+  __shared__ __attribute__((aligned(1024))) char v_lds1[TILEB];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
+
+  const unsigned item = xcd_item(blockIdx.x, gridDim.x, by_xcd);
+  const unsigned rt = item % rtiles, sp = item / rtiles % splits, bh = item / rtiles / splits;
+  const int hk = (int)(bh % (unsigned)a.Hk), b = (int)(bh / (unsigned)a.Hk);
+  const XSample sm = x_sample(a, b);
+  const int rows = sm.nq * a.G;
+  const int row0 = (int)rt * 32 * NW;
+  if (row0 >= rows) return;   // uniform over the workgroup
+  const int ntiles = (sm.nk + kXKeys - 1) / kXKeys, per = (ntiles + (int)splits - 1) / (int)splits;
+  const int t_begin = min((int)sp * per, ntiles), t_end = min(t_begin + per, ntiles);
+  KeyTiles tiles(a.mask ? a.mask + sm.k0 : nullptr, sm.nk, t_begin, t_end);
+
+  bf16x8 qop[KS], doop[KS];
+  float lse2, ndl;   // LSE log2 e, -delta
+  {
+    const int row = min(row0 + 32 * w + l32, rows - 1), tok = row / a.G, head = hk * a.G + row - tok * a.G;
+    const __bf16* qp = static_cast<const __bf16*>(a.q) + (sm.q0 + tok) * a.sq + head * a.D;
+    const __bf16* dp = static_cast<const __bf16*>(a.dout) + (sm.q0 + tok) * a.sdo + head * a.D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qop[ks] = doop[ks] = bf16x8{};
+      if (16 * ks + 8 * g < a.D) {
+        qop[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks + 8 * g);
+        doop[ks] = *reinterpret_cast<const bf16x8*>(dp + 16 * ks + 8 * g);
+      }
+    }
+    const int64_t stat = sm.stat0 + head * sm.hstep + tok;
+    lse2 = aux[stat];
+    ndl = aux[a.Tq * a.Hq + stat];
+  }
+  const TileLoad<DP, NW> load_k(lane, a.D, a.sk), load_v(lane, a.D, a.sv);
+  const __bf16* const kb = static_cast<const __bf16*>(a.k) + sm.k0 * a.sk + hk * a.D;
+  const __bf16* const vb = static_cast<const __bf16*>(a.v) + sm.k0 * a.sv + hk * a.D;
+  auto load_tile = [&](int t, uint64_t bits, char* kd, char* vd) __attribute__((always_inline)) {
+    load_k(kb + (int64_t)t * kXKeys * a.sk, a.sk, bits, kd, w, lane);
+    load_v(vb + (int64_t)t * kXKeys * a.sv, a.sv, bits, vd, w, lane);
+  };
+  int koff[KS], ktr[DT];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) koff[ks] = lds_off<CPR>(l32, 2 * ks + g);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    const int d = 16 * dt + 4 * (c16 & 3);
+    ktr[dt] = lds_off<CPR>(8 * (gq & 1) + 4 * (gq >> 1) + (c16 >> 2), d >> 3) + 2 * (d & 7);
+  }
+  const float c2 = a.scale * kLog2e;
+  // dq[dt][qg]: lane holds dQ^T[16 dt + 4 gq + (0..3)][row 32 w + 16 qg + c16]
+  f32x4 dq[DT][2];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};
+
+  // A tile as two 32-key halves: S^T and dP^T, dS^T, its exchange to the
+  // 16x16 operand layout, and the half's dQ product.
+  auto step = [&](uint64_t bits, const char* kt_lds, const char* vt_lds) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int off = koff[ks] + kt * 32 * ROWB;
+        s = mfma32(*reinterpret_cast<const bf16x8*>(kt_lds + off), qop[ks], s);
+        dp = mfma32(*reinterpret_cast<const bf16x8*>(vt_lds + off), doop[ks], dp);
+      }
+      if (bits != ~(uint64_t)0) {   // uniform
+        const unsigned mine = (unsigned)(bits >> (32 * kt)) >> (4 * g);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          s[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[e] : -INFINITY;
+      }
+      u32x4 pq[2];
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const float p0 = fast_exp2(__builtin_fmaf(s[e], c2, -lse2));
+        const float p1 = fast_exp2(__builtin_fmaf(s[e + 1], c2, -lse2));
+        pq[(e >> 2) & 1][((e & 3) >> 1) + 2 * (e >> 3)] = pack_bf16x2(p0 * (dp[e] + ndl), p1 * (dp[e + 1] + ndl));
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const auto r = __builtin_amdgcn_permlane16_swap(pq[0][v], pq[1][v], false, false);
+        pq[0][v] = r[0];
+        pq[1][v] = r[1];
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const char* kbuf = kt_lds + 32 * kt * ROWB + ktr[dt];
+        const s16x4 lo = lds_read_tr16(kbuf);
+        const s16x4 hi = lds_read_tr16(kbuf + 16 * ROWB);
+        const s16x8 k8 = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        const bf16x8 av = __builtin_bit_cast(bf16x8, k8);
+        dq[dt][0] = mfma16(av, __builtin_bit_cast(bf16x8, pq[0]), dq[dt][0]);
+        dq[dt][1] = mfma16(av, __builtin_bit_cast(bf16x8, pq[1]), dq[dt][1]);
+      }
+    }
+  };
+  int tile = 0;
+  uint64_t bits = 0;
+  bool more = tiles.next(tile, bits);
+  auto iter = [&](auto par) __attribute__((always_inline)) {
+    constexpr int P = decltype(par)::value;
+    const uint64_t now = bits;
+    more = tiles.next(tile, bits);
+    if (more) load_tile(tile, bits, P ? k_lds0 : k_lds1, P ? v_lds0 : v_lds1);
+    step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+  };
+  if (more) {
+    load_tile(tile, bits, k_lds0, v_lds0);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    while (true) {
+      iter(std::integral_constant<int, 0>{});
+      if (!more) break;
+      iter(std::integral_constant<int, 1>{});
+      if (!more) break;
+    }
+  }
+
+#pragma unroll
+  for (int qg = 0; qg < 2; ++qg) {
+    const int ro = row0 + 32 * w + 16 * qg + c16;
+    if (ro >= rows) continue;
+    const int tok = ro / a.G, head = hk * a.G + ro - tok * a.G;
+    float* pp = part + ((sp * a.Tq + sm.q0 + tok) * a.Hq + head) * a.D + 4 * gq;
+    __bf16* op = static_cast<__bf16*>(a.dq) + (sm.q0 + tok) * a.sdq + head * a.D + 4 * gq;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      if (16 * dt + 4 * gq >= a.D) continue;
+      const f32x4 x = dq[dt][qg] * a.scale;
+      if (part) *reinterpret_cast<f32x4*>(pp + 16 * dt) = x;
+      else *reinterpret_cast<bf16x4*>(op + 16 * dt) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dK, dV
+// ---------------------------------------------------------------------------
+// part: fp32 [dK, dV][split][token][Hk][D], null with one split.
+template <int DP>
+__global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const float* __restrict__ aux,
+                                                            const unsigned ktiles, const unsigned splits,
+                                                            const bool by_xcd, float* __restrict__ part) {
+  constexpr int NW = 4, ROWB = DP * 2, CPR = DP / 8, KS = DP / 16, DT = DP / 16;
+  constexpr int TILEB = kRowTile * ROWB, RPI = 1024 / ROWB, IPW = TILEB / 1024 / NW, VIPW = kBwdKeys * ROWB / 1024 / NW;
+  __shared__ __attribute__((aligned(1024))) char q_lds0[TILEB];
+  __shared__ __attribute__((aligned(1024))) char q_lds1[TILEB];
+  __shared__ __attribute__((aligned(1024))) char o_lds0[TILEB];
+  __shared__ __attribute__((aligned(1024))) char o_lds1[TILEB];
+  __shared__ __attribute__((aligned(1024))) char a_lds0[2048];
+  __shared__ __attribute__((aligned(1024))) char a_lds1[2048];
+  __shared__ __attribute__((aligned(1024))) char vblk_lds[kBwdKeys * ROWB];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
+
+  const unsigned item = xcd_item(blockIdx.x, gridDim.x, by_xcd);
+  const unsigned kt = item % ktiles, sp = item / ktiles % splits, bh = item / ktiles / splits;
+  const int hk = (int)(bh % (unsigned)a.Hk), b = (int)(bh / (unsigned)a.Hk);
+  const XSample sm = x_sample(a, b);
+  const int key0 = (int)kt * kBwdKeys;
+  if (key0 >= sm.nk) return;   // uniform over the workgroup
+
+  // Steps: the 32-token tiles of each head of the group; this split's share.
+  const int ttiles = (sm.nq + kRowTile - 1) / kRowTile, all = ttiles * a.G;
+  const int per = (all + (int)splits - 1) / (int)splits;
+  const int s_begin = min((int)sp * per, all), s_end = min(s_begin + per, all);
+
+  f32x4 dk[DT][2], dv[DT][2];   // [dt][kg]: lane holds X^T[16 dt + 4 gq + (0..3)][key 32 w + 16 kg + c16]
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) dk[dt][0] = dk[dt][1] = dv[dt][0] = dv[dt][1] = f32x4{};
+
+  if (s_begin < s_end) {
+    const __bf16* const kb = static_cast<const __bf16*>(a.k) + sm.k0 * a.sk + hk * a.D;
+    bf16x8 kop[KS];
+    {
+      const __bf16* kp = kb + (int64_t)min(key0 + 32 * w + l32, sm.nk - 1) * a.sk + 8 * g;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        kop[ks] = bf16x8{};
+        if (16 * ks + 8 * g < a.D) kop[ks] = *reinterpret_cast<const bf16x8*>(kp + 16 * ks);
+      }
+    }
+    int qoff[IPW], ooff[IPW];
+#pragma unroll
+    for (int u = 0; u < IPW; ++u) {
+      const int r = (w * IPW + u) * RPI + lane / CPR, c = (lds_off<CPR>(r, lane % CPR) >> 4) & (CPR - 1);
+      qoff[u] = c < a.D / 8 ? r * a.sq * 2 + 16 * c : kXOut;
+      ooff[u] = c < a.D / 8 ? r * a.sdo * 2 + 16 * c : kXOut;
+    }
+    {   // the workgroup's V rows (rows past the sample's keys read zeros)
+      const int left = min(sm.nk - key0, kBwdKeys);
+      const __amdgpu_buffer_rsrc_t rv = buffer_rsrc(
+          static_cast<const __bf16*>(a.v) + (sm.k0 + key0) * a.sv + hk * a.D, (left - 1) * a.sv * 2 + 2 * a.D);
+#pragma unroll
+      for (int u = 0; u < VIPW; ++u) {
+        const int r = (w * VIPW + u) * RPI + lane / CPR, c = (lds_off<CPR>(r, lane % CPR) >> 4) & (CPR - 1);
+        buffer_load_lds16(rv, vblk_lds + (w * VIPW + u) * 1024, c < a.D / 8 ? r * a.sv * 2 + 16 * c : kXOut);
+      }
+    }
+    const char* const vrow = vblk_lds + 32 * w * ROWB;   // this wave's keys
+    int roff[KS], rtr[DT];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) roff[ks] = lds_off<CPR>(l32, 2 * ks + g);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const int d = 16 * dt + 4 * (c16 & 3);
+      rtr[dt] = lds_off<CPR>(8 * (gq & 1) + 4 * (gq >> 1) + (c16 >> 2), d >> 3) + 2 * (d & 7);
+    }
+    // Step i: 32 rows of Q and dO and their statistics (rows past the sample read zeros).
+    const __bf16* const qb = static_cast<const __bf16*>(a.q) + sm.q0 * a.sq + hk * a.G * a.D;
+    const __bf16* const ob = static_cast<const __bf16*>(a.dout) + sm.q0 * a.sdo + hk * a.G * a.D;
+    auto load_step = [&](int head, int tt, char* qd, char* od, char* ad) __attribute__((always_inline)) {
+      const int t0 = tt * kRowTile, left = min(sm.nq - t0, kRowTile);
+      const __amdgpu_buffer_rsrc_t rq = buffer_rsrc(qb + (int64_t)t0 * a.sq + head * a.D, (left - 1) * a.sq * 2 + 2 * a.D);
+      const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(ob + (int64_t)t0 * a.sdo + head * a.D, (left - 1) * a.sdo * 2 + 2 * a.D);
+#pragma unroll
+      for (int u = 0; u < IPW; ++u) {
+        buffer_load_lds16(rq, qd + (w * IPW + u) * 1024, qoff[u]);
+        buffer_load_lds16(ro, od + (w * IPW + u) * 1024, ooff[u]);
+      }
+      if (w == 0) {
+        const float* const st = aux + sm.stat0 + (hk * a.G + head) * sm.hstep + t0;
+        buffer_load_lds16(buffer_rsrc(st, left * 4), ad, 16 * lane);
+        buffer_load_lds16(buffer_rsrc(st + a.Tq * a.Hq, left * 4), ad + 1024, 16 * lane);
+      }
+    };
+    const float c2 = a.scale * kLog2e;
+    auto step = [&](const char* qt_lds, const char* ot_lds, const char* at_lds) __attribute__((always_inline)) {
+      const float* const a_pl = reinterpret_cast<const float*>(at_lds) + 4 * g;
+      f32x16 s = f32x16{}, dp;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {   // dP - delta directly: start at -delta
+        const f32x4 y = *reinterpret_cast<const f32x4*>(a_pl + 256 + 8 * x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dp[4 * x + e] = y[e];
+      }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mfma32(*reinterpret_cast<const bf16x8*>(qt_lds + roff[ks]), kop[ks], s);
+        const bf16x8 vop = *reinterpret_cast<const bf16x8*>(vrow + roff[ks]);
+        dp = mfma32(*reinterpret_cast<const bf16x8*>(ot_lds + roff[ks]), vop, dp);
+      }
+      u32x4 pp[2], pd[2];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const f32x4 ls = *reinterpret_cast<const f32x4*>(a_pl + 8 * x);
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const int i = 4 * x + e;
+          const float p0 = fast_exp2(__builtin_fmaf(s[i], c2, -ls[e]));
+          const float p1 = fast_exp2(__builtin_fmaf(s[i + 1], c2, -ls[e + 1]));
+          const int r = (i >> 2) & 1, c = ((i & 3) >> 1) + 2 * (i >> 3);
+          pp[r][c] = pack_bf16x2(p0, p1);
+          pd[r][c] = pack_bf16x2(p0 * dp[i], p1 * dp[i + 1]);
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const auto r0 = __builtin_amdgcn_permlane16_swap(pp[0][v], pp[1][v], false, false);
+        pp[0][v] = r0[0];
+        pp[1][v] = r0[1];
+        const auto r1 = __builtin_amdgcn_permlane16_swap(pd[0][v], pd[1][v], false, false);
+        pd[0][v] = r1[0];
+        pd[1][v] = r1[1];
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const s16x4 o_lo = lds_read_tr16(ot_lds + rtr[dt]), o_hi = lds_read_tr16(ot_lds + rtr[dt] + 16 * ROWB);
+        const s16x4 q_lo = lds_read_tr16(qt_lds + rtr[dt]), q_hi = lds_read_tr16(qt_lds + rtr[dt] + 16 * ROWB);
+        const s16x8 o8 = {o_lo[0], o_lo[1], o_lo[2], o_lo[3], o_hi[0], o_hi[1], o_hi[2], o_hi[3]};
+        const s16x8 q8 = {q_lo[0], q_lo[1], q_lo[2], q_lo[3], q_hi[0], q_hi[1], q_hi[2], q_hi[3]};
+        const bf16x8 ao = __builtin_bit_cast(bf16x8, o8), aq = __builtin_bit_cast(bf16x8, q8);
+#pragma unroll
+        for (int kg = 0; kg < 2; ++kg) {
+          dv[dt][kg] = mfma16(ao, __builtin_bit_cast(bf16x8, pp[kg]), dv[dt][kg]);
+          dk[dt][kg] = mfma16(aq, __builtin_bit_cast(bf16x8, pd[kg]), dk[dt][kg]);
+        }
+      }
+    };
+    int head = s_begin / ttiles, tt = s_begin - head * ttiles;
+    auto advance = [&]() __attribute__((always_inline)) {
+      if (++tt == ttiles) tt = 0, ++head;
+    };
+    auto iter = [&](int i, auto par) __attribute__((always_inline)) {
+      constexpr int P = decltype(par)::value;
+      advance();
+      if (i + 1 < s_end) load_step(head, tt, P ? q_lds0 : q_lds1, P ? o_lds0 : o_lds1, P ? a_lds0 : a_lds1);
+      step(P ? q_lds1 : q_lds0, P ? o_lds1 : o_lds0, P ? a_lds1 : a_lds0);
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+    };
+    load_step(head, tt, q_lds0, o_lds0, a_lds0);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    int i = s_begin;
+    for (; i + 1 < s_end; i += 2) {
+      iter(i, std::integral_constant<int, 0>{});
+      iter(i + 1, std::integral_constant<int, 1>{});
+    }
+    if (i < s_end) iter(i, std::integral_constant<int, 0>{});
+  }
+
+#pragma unroll
+  for (int kg = 0; kg < 2; ++kg) {
+    const int key = key0 + 32 * w + 16 * kg + c16;
+    if (key >= sm.nk) continue;
+    const bool used = !a.mask || a.mask[sm.k0 + key];
+    const int64_t tok = sm.k0 + key;
+    float* const pk = part + ((sp * a.Tk + tok) * a.Hk + hk) * a.D + 4 * gq;
+    float* const pv = pk + splits * a.Tk * a.Hk * a.D;
+    __bf16* const ok = static_cast<__bf16*>(a.dk) + tok * a.sdk + hk * a.D + 4 * gq;
+    __bf16* const ov = static_cast<__bf16*>(a.dv) + tok * a.sdv + hk * a.D + 4 * gq;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      if (16 * dt + 4 * gq >= a.D) continue;
+      const f32x4 x = used ? dk[dt][kg] * a.scale : f32x4{}, y = used ? dv[dt][kg] : f32x4{};
+      if (part) {
+        *reinterpret_cast<f32x4*>(pk + 16 * dt) = x;
+        *reinterpret_cast<f32x4*>(pv + 16 * dt) = y;
+      } else {
+        *reinterpret_cast<bf16x4*>(ok + 16 * dt) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+        *reinterpret_cast<bf16x4*>(ov + 16 * dt) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// join: out[token][row of the token's heads] = the sum of the splits, in order.
+// Four elements a thread; tokens of no sample are left as they are.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void xattn_sum_kernel(const float* __restrict__ part, int splits, int64_t T, int width,
+                                                        __bf16* __restrict__ out, int stride,
+                                                        const int32_t* __restrict__ cu, int B, int N) {
+  const int64_t total = T * width, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= total) return;
+  const int64_t tok = i / width;
+  if (cu && !in_sample(cu, T, B, N, tok)) return;
+  f32x4 x = f32x4{};
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) x += *reinterpret_cast<const f32x4*>(part + s * total + i);
+  *reinterpret_cast<bf16x4*>(out + tok * stride + (i - tok * width)) =
+      bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+}
+
+// Rows at and past the last sample's end become 0 (statistics: -inf).
+__global__ __launch_bounds__(256) void xattn_clear_kernel(const int32_t* __restrict__ cu, int B, int64_t T, int width,
+                                                          __bf16* __restrict__ x, int sx, __bf16* __restrict__ y, int sy,
+                                                          float* __restrict__ lse, int H) {
+  const int64_t end = min(max((int64_t)cu[B], (int64_t)0), T);
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  const int per = width / 8;
+  for (int64_t i = end * per + at; i < T * per; i += step) {
+    const int64_t tok = i / per;
+    *reinterpret_cast<bf16x8*>(x + tok * sx + 8 * (i - tok * per)) = bf16x8{};
+    if (y) *reinterpret_cast<bf16x8*>(y + tok * sy + 8 * (i - tok * per)) = bf16x8{};
+  }
+  if (lse)
+    for (int64_t i = at; i < (T - end) * H; i += step) lse[i / (T - end) * T + end + i % (T - end)] = -INFINITY;
+}
+
+int dq_waves(const XArgs& a) {
+  const int64_t rows = (int64_t)a.Nq * a.G;
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+}
+int64_t dq_groups(const XArgs& a) {
+  const int64_t per = 32 * dq_waves(a);
+  return (int64_t)a.B * a.Hk * (((int64_t)a.Nq * a.G + per - 1) / per);
+}
+int64_t dkdv_groups(const XArgs& a) {
+  return (int64_t)a.B * a.Hk * (((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys);
+}
+// Workgroups that fit at once: two a CU. Splits below four tiles are not worth their join.
+int dq_splits(const XArgs& a) {
+  const int64_t groups = dq_groups(a), tiles = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
+  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(512 / groups, tiles / 4));
+}
+int dkdv_splits(const XArgs& a) {
+  const int64_t groups = dkdv_groups(a), steps = (int64_t)a.G * (((int64_t)a.Nq + kRowTile - 1) / kRowTile);
+  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(512 / groups, steps / 8));
+}
+size_t aux_bytes(const XArgs& a) { return ((size_t)a.Tq * a.Hq * 2 * sizeof(float) + 255) / 256 * 256; }
+size_t dq_part(const XArgs& a) {
+  const int n = dq_splits(a);
+  return n > 1 ? (size_t)n * a.Tq * a.Hq * a.D * sizeof(float) : 0;
+}
+size_t dkdv_part(const XArgs& a) {
+  const int n = dkdv_splits(a);
+  return n > 1 ? (size_t)n * a.Tk * a.Hk * a.D * 2 * sizeof(float) : 0;
+}
+
+template <int DP, int NW>
+void launch_dq(const XArgs& a, const float* aux, int splits, float* part, hipStream_t s) {
+  const unsigned rtiles = (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW));
+  const bool by_xcd = (int64_t)a.Nk * a.D * 4 <= kXcdHeadBytes;
+  TraceScope ts_(s, "xattn_dq", DP, NW);
+  hipLaunchKernelGGL((xattn_dq_kernel<DP, NW>), dim3((unsigned)(dq_groups(a) * splits)), dim3(64 * NW), 0, s, a, aux,
+                     rtiles, (unsigned)splits, by_xcd, part);
+}
+template <int DP>
+void launch_dkdv(const XArgs& a, const float* aux, int splits, float* part, hipStream_t s) {
+  const unsigned ktiles = (unsigned)(((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys);
+  TraceScope ts_(s, "xattn_dkdv", DP);
+  hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), dim3((unsigned)(dkdv_groups(a) * splits)), dim3(256), 0, s, a, aux,
+                     ktiles, (unsigned)splits, true, part);
+}
+void launch_sum(const float* part, int splits, int64_t T, int width, void* out, int stride, const int32_t* cu, int B,
+                int N, hipStream_t s) {
+  if (T == 0) return;
+  TraceScope ts_(s, "xattn_sum");
+  hipLaunchKernelGGL(xattn_sum_kernel, dim3((unsigned)((T * width / 4 + 255) / 256)), dim3(256), 0, s, part, splits, T,
+                     width, static_cast<__bf16*>(out), stride, cu, B, N);
+}
+
+}  // namespace
+
+size_t xattn_bwd_workspace(const XArgs& a) { return aux_bytes(a) + std::max(dq_part(a), dkdv_part(a)); }
+
+hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
+  float* const aux = static_cast<float*>(workspace);
+  float* const part = reinterpret_cast<float*>(static_cast<char*>(workspace) + aux_bytes(a));   // both joins' in turn
+  if (a.Tq > 0 && a.Nq > 0) {
+    TraceScope ts_(s, "xattn_prep", a.D);
+    hipLaunchKernelGGL(xattn_prep_kernel, dim3((unsigned)((a.Tq * a.Hq + 15) / 16)), dim3(256), 0, s, a, aux);
+  }
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (dkdv_groups(a) > 0) {
+    const int n = dkdv_splits(a);
+    float* const p = n > 1 ? part : nullptr;
+    a.D <= 64 ? launch_dkdv<64>(a, aux, n, p, s) : launch_dkdv<128>(a, aux, n, p, s);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (n > 1) {
+      launch_sum(part, n, a.Tk, a.Hk * a.D, a.dk, a.sdk, a.cuk, a.B, a.Nk, s);
+      launch_sum(part + (size_t)n * a.Tk * a.Hk * a.D, n, a.Tk, a.Hk * a.D, a.dv, a.sdv, a.cuk, a.B, a.Nk, s);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+  }
+  if (dq_groups(a) > 0) {
+    const int n = dq_splits(a), nw = dq_waves(a);
+    float* const p = n > 1 ? part : nullptr;
+    if (a.D <= 64)
+      nw == 1 ? launch_dq<64, 1>(a, aux, n, p, s) : nw == 2 ? launch_dq<64, 2>(a, aux, n, p, s) : launch_dq<64, 4>(a, aux, n, p, s);
+    else
+      nw == 1 ? launch_dq<128, 1>(a, aux, n, p, s) : nw == 2 ? launch_dq<128, 2>(a, aux, n, p, s) : launch_dq<128, 4>(a, aux, n, p, s);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (n > 1) launch_sum(part, n, a.Tq, a.Hq * a.D, a.dq, a.sdq, a.cuq, a.B, a.Nq, s);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_xattn_clear(const int32_t* cu, int B, int64_t T, int width, void* x, int sx, void* y, int sy,
+                              float* lse, int H, hipStream_t s) {
+  TraceScope ts_(s, "xattn_clear");
+  hipLaunchKernelGGL(xattn_clear_kernel, dim3(256), dim3(256), 0, s, cu, B, T, width, static_cast<__bf16*>(x), sx,
+                     static_cast<__bf16*>(y), sy, lse, H);
+  return hipGetLastError();
+}
+
+}  // namespace ut
