@@ -4,17 +4,19 @@
 //   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO,
 // dK and dV summed over the query heads that share the key head. Launches:
 //
-//   prep  : per query row, LSE log2(e) and -delta (fp32, two planes of the
-//           workspace);
+//   dQ    : query-stationary, first: it forms the rows' statistics LSE log2(e) and
+//           -delta (fp32, two planes of the workspace) from LSE, O and the dO
+//           rows that it holds anyway. S and dP on 32x32x16 bf16 MFMA,
+//           dQ^T += K^T dS^T on 16x16x32; with few rows the keys are split as
+//           below. The workgroups are persistent: the rows and the first tile of
+//           the next item load beside the last tile of the one before;
 //   dK/dV : key-stationary. A workgroup owns 128 keys of a key head, one wave
 //           per 32, and walks the 32-token tiles of every query head of the
 //           group: S and dP on 32x32x16 bf16 MFMA, dV^T += dO^T P and
 //           dK^T += Q^T dS on 16x16x32, accumulators in fp32 registers. Few keys
 //           (an encoder's states against a picture's tokens) make few
 //           workgroups, so the query tiles are split over workgroups, each
-//           writes fp32 partial sums, and a join adds them in a fixed order;
-//   dQ    : query-stationary, S and dP computed again, dQ^T += K^T dS^T; with
-//           few rows the keys are split the same way.
+//           writes fp32 partial sums, and a join adds them in a fixed order.
 //
 // Rounding: P and dS to bf16 before their second products (half a step each,
 // 2^-9 relative), all sums in fp32. No atomics: equal results on every run.
@@ -34,38 +36,13 @@ constexpr int kBwdKeys = 128;   // keys of a dK/dV workgroup
 constexpr int kRowTile = 32;    // query tokens of a dK/dV step
 
 // ---------------------------------------------------------------------------
-// prep
-// ---------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void xattn_prep_kernel(const XArgs a, float* __restrict__ aux) {
-  const int64_t rows = a.Tq * a.Hq;
-  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);   // token-major
-  const int c = threadIdx.x & 15;
-  const int64_t tok = row / a.Hq;
-  const int h = (int)(row - tok * a.Hq);
-  float acc = 0.f;
-  if (row < rows && 8 * c < a.D) {
-    const bf16x8 o = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.o_in) + tok * a.so + h * a.D + 8 * c);
-    const bf16x8 d = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.dout) + tok * a.sdo + h * a.D + 8 * c);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc += (float)o[e] * (float)d[e];
-  }
-#pragma unroll
-  for (int m = 8; m >= 1; m >>= 1) acc += __shfl_xor(acc, m, 64);
-  if (row < rows && c == 0) {
-    const int64_t r = a.cuq ? (int64_t)h * a.Tq + tok : (tok / a.Nq * a.Hq + h) * a.Nq + tok % a.Nq;
-    aux[r] = a.lse[r] * kLog2e;
-    aux[rows + r] = -acc;
-  }
-}
-
-// ---------------------------------------------------------------------------
 // dQ
 // ---------------------------------------------------------------------------
 // part: fp32 [split][token][Hq][D], null with one split.
 template <int DP, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_dq_kernel(const XArgs a, const float* __restrict__ aux,
-                                                                            const unsigned rtiles, const unsigned splits,
-                                                                            const bool by_xcd, float* __restrict__ part) {
+__global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_dq_kernel(const XArgs a, float* __restrict__ aux,
+                                                                            const XOrder order, const bool by_xcd,
+                                                                            float* __restrict__ part) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
   __shared__ __attribute__((aligned(1024))) char k_lds0[TILEB];
   __shared__ __attribute__((aligned(1024))) char k_lds1[TILEB];
@@ -75,69 +52,96 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_dq_kernel(cons
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
-  const unsigned item = xcd_item(blockIdx.x, gridDim.x, by_xcd);
-  const unsigned rt = item % rtiles, sp = item / rtiles % splits, bh = item / rtiles / splits;
-  const int hk = (int)(bh % (unsigned)a.Hk), b = (int)(bh / (unsigned)a.Hk);
-  const XSample sm = x_sample(a, b);
-  const int rows = sm.nq * a.G;
-  const int row0 = (int)rt * 32 * NW;
-  if (row0 >= rows) return;   // uniform over the workgroup
-  const int ntiles = (sm.nk + kXKeys - 1) / kXKeys, per = (ntiles + (int)splits - 1) / (int)splits;
-  const int t_begin = min((int)sp * per, ntiles), t_end = min(t_begin + per, ntiles);
-  KeyTiles tiles(a.mask ? a.mask + sm.k0 : nullptr, sm.nk, t_begin, t_end);
-
-  bf16x8 qop[KS], doop[KS];
-  float lse2, ndl;   // LSE log2 e, -delta
-  {
-    const int row = min(row0 + 32 * w + l32, rows - 1), tok = row / a.G, head = hk * a.G + row - tok * a.G;
-    const __bf16* qp = static_cast<const __bf16*>(a.q) + (sm.q0 + tok) * a.sq + head * a.D;
-    const __bf16* dp = static_cast<const __bf16*>(a.dout) + (sm.q0 + tok) * a.sdo + head * a.D;
+  // A row's Q and dO (the operands), O and LSE.
+  bf16x8 qop[KS], doop[KS], orow[KS];
+  float lse, lse2, ndl;   // LSE; LSE log2 e and -delta
+  auto load_rows = [&](const XItem& at) __attribute__((always_inline)) {
+    const XArgs& x = *x_args_again();
+    const XSample sm = x_sample(x, at.b);
+    const int r0 = at.tile * 32 * NW + 32 * w;
+    const XRow r = x_row(r0, r0 + l32, sm.nq * x.G, x.G);
+    const int64_t tok0 = sm.q0 + r.first, head0 = (int64_t)at.hk * x.G * x.D;
+    const __amdgpu_buffer_rsrc_t rq = buffer_rsrc(static_cast<const __bf16*>(x.q) + tok0 * x.sq + head0, kXOut);
+    const __amdgpu_buffer_rsrc_t rd = buffer_rsrc(static_cast<const __bf16*>(x.dout) + tok0 * x.sdo + head0, kXOut);
+    const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(static_cast<const __bf16*>(x.o_in) + tok0 * x.so + head0, kXOut);
+    const int t = r.tok - r.first, c = r.head * x.D + 8 * g;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      qop[ks] = doop[ks] = bf16x8{};
-      if (16 * ks + 8 * g < a.D) {
-        qop[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks + 8 * g);
-        doop[ks] = *reinterpret_cast<const bf16x8*>(dp + 16 * ks + 8 * g);
-      }
+      const bool in = 16 * ks + 8 * g < x.D;
+      qop[ks] = x_load16(rq, in ? (t * x.sq + c) * 2 + 32 * ks : kXOut);
+      doop[ks] = x_load16(rd, in ? (t * x.sdo + c) * 2 + 32 * ks : kXOut);
+      orow[ks] = x_load16(ro, in ? (t * x.so + c) * 2 + 32 * ks : kXOut);
     }
-    const int64_t stat = sm.stat0 + head * sm.hstep + tok;
-    lse2 = aux[stat];
-    ndl = aux[a.Tq * a.Hq + stat];
-  }
-  const TileLoad<DP, NW> load_k(lane, a.D, a.sk), load_v(lane, a.D, a.sv);
-  const __bf16* const kb = static_cast<const __bf16*>(a.k) + sm.k0 * a.sk + hk * a.D;
-  const __bf16* const vb = static_cast<const __bf16*>(a.v) + sm.k0 * a.sv + hk * a.D;
-  auto load_tile = [&](int t, uint64_t bits, char* kd, char* vd) __attribute__((always_inline)) {
-    load_k(kb + (int64_t)t * kXKeys * a.sk, a.sk, bits, kd, w, lane);
-    load_v(vb + (int64_t)t * kXKeys * a.sv, a.sv, bits, vd, w, lane);
+    lse = x.lse[sm.stat0 + (at.hk * x.G + r.head) * sm.hstep + r.tok];
   };
-  int koff[KS], ktr[DT];
+  // The statistics of those rows, for the dK/dV pass too (part 0 writes them). A row
+  // without keys has LSE -inf; any finite value keeps its P at 0.
+  auto row_stats = [&](const XItem& at) __attribute__((always_inline)) {
+    float sum = 0.f;
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) koff[ks] = lds_off<CPR>(l32, 2 * ks + g);
+    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    const int d = 16 * dt + 4 * (c16 & 3);
-    ktr[dt] = lds_off<CPR>(8 * (gq & 1) + 4 * (gq >> 1) + (c16 >> 2), d >> 3) + 2 * (d & 7);
-  }
+      for (int e = 0; e < 8; ++e) sum += (float)orow[ks][e] * (float)doop[ks][e];
+    lse2 = lse == -INFINITY ? 0.f : lse * kLog2e;
+    ndl = -pair_sum(sum);
+    const XArgs& x = *x_args_again();
+    const XSample sm = x_sample(x, at.b);
+    const int row = at.tile * 32 * NW + 32 * w + l32, tok = row_token(row, x.G);
+    if (at.part == 0 && g == 0 && row < sm.nq * x.G) {
+      const int64_t stat = sm.stat0 + (at.hk * x.G + row - tok * x.G) * sm.hstep + tok;
+      aux[stat] = lse2;
+      aux[x.Tq * x.Hq + stat] = ndl;
+    }
+  };
+  const TileLoad<DP, NW> load_k(lane, a.sk), load_v(lane, a.sv);
+  // LDS offsets, as in the forward: chunk 2 ks + g of row l32, and K^T's operand.
+  // The swizzle is an exclusive or, and so is the step to another ks or dt: one
+  // register each and an instruction a use, where sixteen would not fit.
+  const int koff0 = lds_off<CPR>(l32, g);
+  const int ktr0 = lds_off<CPR>(8 * (gq & 1) + 4 * (gq >> 1) + (c16 >> 2), (c16 & 3) >> 1) + 8 * (c16 & 1);
   const float c2 = a.scale * kLog2e;
   // dq[dt][qg]: lane holds dQ^T[16 dt + 4 gq + (0..3)][row 32 w + 16 qg + c16]
   f32x4 dq[DT][2];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};
 
+  TileSeq seq;
+
   // A tile as two 32-key halves: S^T and dP^T, dS^T, its exchange to the
-  // 16x16 operand layout, and the half's dQ product.
-  auto step = [&](uint64_t bits, const char* kt_lds, const char* vt_lds) __attribute__((always_inline)) {
+  // 16x16 operand layout, and the half's dQ product. With `swap` the next item's
+  // rows take the place of this one's after the last score products.
+  auto step = [&](uint64_t bits, const char* kt_lds, const char* vt_lds, bool swap)
+      __attribute__((always_inline)) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       f32x16 s = f32x16{}, dp = f32x16{};
+      int ko = koff0, kx = ktr0;
+      pin_value(ko);
+      pin_value(kx);
+      // S^T and dP^T in turn, operands read kAhead products before their use
+      constexpr int kAhead = DP == 64 ? 2 : 4;
+      bf16x8 op[kAhead];
+      auto read_op = [&](int n) __attribute__((always_inline)) {
+        return *reinterpret_cast<const bf16x8*>((n & 1 ? vt_lds : kt_lds) + (ko ^ (32 * (n >> 1))) + kt * 32 * ROWB);
+      };
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int off = koff[ks] + kt * 32 * ROWB;
-        s = mfma32(*reinterpret_cast<const bf16x8*>(kt_lds + off), qop[ks], s);
-        dp = mfma32(*reinterpret_cast<const bf16x8*>(vt_lds + off), doop[ks], dp);
+      for (int n = 0; n < kAhead; ++n) op[n] = read_op(n);
+#pragma unroll
+      for (int n = 0; n < 2 * KS; ++n) {
+        if (n & 1) dp = mfma32(op[n % kAhead], doop[n >> 1], dp);
+        else s = mfma32(op[n % kAhead], qop[n >> 1], s);
+        if (n + kAhead < 2 * KS) op[n % kAhead] = read_op(n + kAhead);
       }
-      if (bits != ~(uint64_t)0) {   // uniform
+      __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);   // DS read
+#pragma unroll
+      for (int n = 0; n + kAhead < 2 * KS; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // MFMA
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // DS read
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+      const float l2 = lse2, nd = ndl;
+      if (kt == 1 && swap) load_rows(seq.cold.item(TileSeq::kAt));   // uniform
+      if (bits != ~(uint64_t)0) {             // uniform
         const unsigned mine = (unsigned)(bits >> (32 * kt)) >> (4 * g);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -146,9 +150,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_dq_kernel(cons
       u32x4 pq[2];
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        const float p0 = fast_exp2(__builtin_fmaf(s[e], c2, -lse2));
-        const float p1 = fast_exp2(__builtin_fmaf(s[e + 1], c2, -lse2));
-        pq[(e >> 2) & 1][((e & 3) >> 1) + 2 * (e >> 3)] = pack_bf16x2(p0 * (dp[e] + ndl), p1 * (dp[e + 1] + ndl));
+        const float p0 = fast_exp2(__builtin_fmaf(s[e], c2, -l2));
+        const float p1 = fast_exp2(__builtin_fmaf(s[e + 1], c2, -l2));
+        pq[(e >> 2) & 1][((e & 3) >> 1) + 2 * (e >> 3)] = pack_bf16x2(p0 * (dp[e] + nd), p1 * (dp[e + 1] + nd));
       }
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
@@ -158,7 +162,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_dq_kernel(cons
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        const char* kbuf = kt_lds + 32 * kt * ROWB + ktr[dt];
+        const char* kbuf = kt_lds + 32 * kt * ROWB + (kx ^ (32 * dt));
         const s16x4 lo = lds_read_tr16(kbuf);
         const s16x4 hi = lds_read_tr16(kbuf + 16 * ROWB);
         const s16x8 k8 = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -168,44 +172,63 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_dq_kernel(cons
       }
     }
   };
-  int tile = 0;
-  uint64_t bits = 0;
-  bool more = tiles.next(tile, bits);
-  auto iter = [&](auto par) __attribute__((always_inline)) {
-    constexpr int P = decltype(par)::value;
-    const uint64_t now = bits;
-    more = tiles.next(tile, bits);
-    if (more) load_tile(tile, bits, P ? k_lds0 : k_lds1, P ? v_lds0 : v_lds1);
-    step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
+  auto finish = [&](const XItem& at) __attribute__((always_inline)) {
+    const XArgs& x = *x_args_again();
+    const XSample sm = x_sample(x, at.b);
+    const int rows = sm.nq * x.G, r0 = at.tile * 32 * NW + 32 * w;
+#pragma unroll
+    for (int qg = 0; qg < 2; ++qg) {
+      const int ro = r0 + 16 * qg + c16;
+      const XRow r = x_row(r0, ro, rows, x.G);
+      const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(
+          static_cast<__bf16*>(x.dq) + (sm.q0 + r.first) * x.sdq + (int64_t)at.hk * x.G * x.D, kXOut);
+      const int off = ro < rows ? ((r.tok - r.first) * x.sdq + r.head * x.D + 4 * gq) * 2 : kXOut;
+      float* const pp = part + ((at.part * x.Tq + sm.q0 + r.tok) * x.Hq + at.hk * x.G + r.head) * x.D + 4 * gq;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const f32x4 y = dq[dt][qg] * a.scale;
+        if (!part)
+          x_store8(bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]}, rs,
+                   16 * dt + 4 * gq < x.D ? off + 32 * dt : kXOut);
+        else if (ro < rows && 16 * dt + 4 * gq < x.D)
+          *reinterpret_cast<f32x4*>(pp + 16 * dt) = y;
+      }
+    }
   };
-  if (more) {
-    load_tile(tile, bits, k_lds0, v_lds0);
+
+  // A workgroup's items in turn, their tiles as one sequence, as in the forward.
+  seq.begin(x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk, by_xcd));
+  bool have = false;   // a tile lies in the current stage
+  auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
+    constexpr int P = decltype(par)::value;
+    const uint64_t now = seq.bits;
+    bool changed;
+    const bool more = seq.next(order, 32 * NW, changed);
+    if (!have && !more) return false;
+    if (more) {
+      const int64_t key = seq.k0 + (int64_t)seq.tile * kXKeys;
+      const __amdgpu_buffer_rsrc_t rk = load_k.tile(static_cast<const __bf16*>(a.k) + key * a.sk + seq.hk * a.D, a.sk);
+      const __amdgpu_buffer_rsrc_t rv = load_v.tile(static_cast<const __bf16*>(a.v) + key * a.sv + seq.hk * a.D, a.sv);
+      load_k.masked(rk, a.sk, seq.bits, P ? k_lds0 : k_lds1, w, lane, a.D);
+      load_v.masked(rv, a.sv, seq.bits, P ? v_lds0 : v_lds1, w, lane, a.D);
+    }
+    // before the first tile too, beside its loads: what it leaves is not used
+    step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more);
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    while (true) {
-      iter(std::integral_constant<int, 0>{});
-      if (!more) break;
-      iter(std::integral_constant<int, 1>{});
-      if (!more) break;
-    }
-  }
-
+    if (changed) {
+      // its stores end beside the next item's first tile
+      if (have) finish(seq.cold.item(TileSeq::kCur));
+      const XItem at = seq.cold.item(TileSeq::kAt);
+      seq.cold.put(TileSeq::kCur, at);
+      if (more) row_stats(at);
 #pragma unroll
-  for (int qg = 0; qg < 2; ++qg) {
-    const int ro = row0 + 32 * w + 16 * qg + c16;
-    if (ro >= rows) continue;
-    const int tok = ro / a.G, head = hk * a.G + ro - tok * a.G;
-    float* pp = part + ((sp * a.Tq + sm.q0 + tok) * a.Hq + head) * a.D + 4 * gq;
-    __bf16* op = static_cast<__bf16*>(a.dq) + (sm.q0 + tok) * a.sdq + head * a.D + 4 * gq;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      if (16 * dt + 4 * gq >= a.D) continue;
-      const f32x4 x = dq[dt][qg] * a.scale;
-      if (part) *reinterpret_cast<f32x4*>(pp + 16 * dt) = x;
-      else *reinterpret_cast<bf16x4*>(op + 16 * dt) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+      for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};
     }
+    have = true;
+    return more;
+  };
+  while (iter(std::integral_constant<int, 0>{}) && iter(std::integral_constant<int, 1>{})) {
   }
 }
 
@@ -215,8 +238,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_dq_kernel(cons
 // part: fp32 [dK, dV][split][token][Hk][D], null with one split.
 template <int DP>
 __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const float* __restrict__ aux,
-                                                            const unsigned ktiles, const unsigned splits,
-                                                            const bool by_xcd, float* __restrict__ part) {
+                                                            const XOrder order, const bool by_xcd,
+                                                            float* __restrict__ part) {
   constexpr int NW = 4, ROWB = DP * 2, CPR = DP / 8, KS = DP / 16, DT = DP / 16;
   constexpr int TILEB = kRowTile * ROWB, RPI = 1024 / ROWB, IPW = TILEB / 1024 / NW, VIPW = kBwdKeys * ROWB / 1024 / NW;
   __shared__ __attribute__((aligned(1024))) char q_lds0[TILEB];
@@ -230,16 +253,18 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
-  const unsigned item = xcd_item(blockIdx.x, gridDim.x, by_xcd);
-  const unsigned kt = item % ktiles, sp = item / ktiles % splits, bh = item / ktiles / splits;
-  const int hk = (int)(bh % (unsigned)a.Hk), b = (int)(bh / (unsigned)a.Hk);
-  const XSample sm = x_sample(a, b);
+  const XItems items = x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk, by_xcd);
+  if (items.first >= items.end) return;
+  const XItem at = x_item(items.first, (unsigned)a.B, order);
+  const unsigned kt = at.tile, sp = at.part;
+  const int hk = at.hk;
+  const XSample sm = x_sample(a, at.b);
   const int key0 = (int)kt * kBwdKeys;
   if (key0 >= sm.nk) return;   // uniform over the workgroup
 
   // Steps: the 32-token tiles of each head of the group; this split's share.
   const int ttiles = (sm.nq + kRowTile - 1) / kRowTile, all = ttiles * a.G;
-  const int per = (all + (int)splits - 1) / (int)splits;
+  const int per = (all + (int)order.splits - 1) / (int)order.splits;
   const int s_begin = min((int)sp * per, all), s_end = min(s_begin + per, all);
 
   f32x4 dk[DT][2], dv[DT][2];   // [dt][kg]: lane holds X^T[16 dt + 4 gq + (0..3)][key 32 w + 16 kg + c16]
@@ -384,7 +409,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
     const bool used = !a.mask || a.mask[sm.k0 + key];
     const int64_t tok = sm.k0 + key;
     float* const pk = part + ((sp * a.Tk + tok) * a.Hk + hk) * a.D + 4 * gq;
-    float* const pv = pk + splits * a.Tk * a.Hk * a.D;
+    float* const pv = pk + order.splits * a.Tk * a.Hk * a.D;
     __bf16* const ok = static_cast<__bf16*>(a.dk) + tok * a.sdk + hk * a.D + 4 * gq;
     __bf16* const ov = static_cast<__bf16*>(a.dv) + tok * a.sdv + hk * a.D + 4 * gq;
 #pragma unroll
@@ -466,20 +491,25 @@ size_t dkdv_part(const XArgs& a) {
   return n > 1 ? (size_t)n * a.Tk * a.Hk * a.D * 2 * sizeof(float) : 0;
 }
 
+// Workgroups that fill the chip, as in the forward.
 template <int DP, int NW>
-void launch_dq(const XArgs& a, const float* aux, int splits, float* part, hipStream_t s) {
-  const unsigned rtiles = (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW));
-  const bool by_xcd = (int64_t)a.Nk * a.D * 4 <= kXcdHeadBytes;
+constexpr int64_t kResident = 256 * (DP == 128 ? 2 : NW == 4 ? 3 : 4);
+
+template <int DP, int NW>
+void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t s) {
+  const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
+  const bool by_xcd = (int64_t)a.B * a.Nk * a.D * 4 <= kXcdHeadBytes;
+  const int64_t items = dq_groups(a) * splits;
+  const dim3 grid((unsigned)(std::min<int64_t>(items, kResident<DP, NW>) + 7) / 8 * 8);
   TraceScope ts_(s, "xattn_dq", DP, NW);
-  hipLaunchKernelGGL((xattn_dq_kernel<DP, NW>), dim3((unsigned)(dq_groups(a) * splits)), dim3(64 * NW), 0, s, a, aux,
-                     rtiles, (unsigned)splits, by_xcd, part);
+  hipLaunchKernelGGL((xattn_dq_kernel<DP, NW>), grid, dim3(64 * NW), 0, s, a, aux, order, by_xcd, part);
 }
 template <int DP>
 void launch_dkdv(const XArgs& a, const float* aux, int splits, float* part, hipStream_t s) {
-  const unsigned ktiles = (unsigned)(((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys);
+  const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys), (unsigned)splits};
   TraceScope ts_(s, "xattn_dkdv", DP);
-  hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), dim3((unsigned)(dkdv_groups(a) * splits)), dim3(256), 0, s, a, aux,
-                     ktiles, (unsigned)splits, true, part);
+  hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), dim3((unsigned)(dkdv_groups(a) * splits + 7) / 8 * 8), dim3(256), 0, s,
+                     a, aux, order, true, part);
 }
 void launch_sum(const float* part, int splits, int64_t T, int width, void* out, int stride, const int32_t* cu, int B,
                 int N, hipStream_t s) {
@@ -496,22 +526,6 @@ size_t xattn_bwd_workspace(const XArgs& a) { return aux_bytes(a) + std::max(dq_p
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
   float* const aux = static_cast<float*>(workspace);
   float* const part = reinterpret_cast<float*>(static_cast<char*>(workspace) + aux_bytes(a));   // both joins' in turn
-  if (a.Tq > 0 && a.Nq > 0) {
-    TraceScope ts_(s, "xattn_prep", a.D);
-    hipLaunchKernelGGL(xattn_prep_kernel, dim3((unsigned)((a.Tq * a.Hq + 15) / 16)), dim3(256), 0, s, a, aux);
-  }
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (dkdv_groups(a) > 0) {
-    const int n = dkdv_splits(a);
-    float* const p = n > 1 ? part : nullptr;
-    a.D <= 64 ? launch_dkdv<64>(a, aux, n, p, s) : launch_dkdv<128>(a, aux, n, p, s);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (n > 1) {
-      launch_sum(part, n, a.Tk, a.Hk * a.D, a.dk, a.sdk, a.cuk, a.B, a.Nk, s);
-      launch_sum(part + (size_t)n * a.Tk * a.Hk * a.D, n, a.Tk, a.Hk * a.D, a.dv, a.sdv, a.cuk, a.B, a.Nk, s);
-      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
-  }
   if (dq_groups(a) > 0) {
     const int n = dq_splits(a), nw = dq_waves(a);
     float* const p = n > 1 ? part : nullptr;
@@ -521,6 +535,16 @@ hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
       nw == 1 ? launch_dq<128, 1>(a, aux, n, p, s) : nw == 2 ? launch_dq<128, 2>(a, aux, n, p, s) : launch_dq<128, 4>(a, aux, n, p, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (n > 1) launch_sum(part, n, a.Tq, a.Hq * a.D, a.dq, a.sdq, a.cuq, a.B, a.Nq, s);
+  }
+  if (dkdv_groups(a) > 0) {
+    const int n = dkdv_splits(a);
+    float* const p = n > 1 ? part : nullptr;
+    a.D <= 64 ? launch_dkdv<64>(a, aux, n, p, s) : launch_dkdv<128>(a, aux, n, p, s);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (n > 1) {
+      launch_sum(part, n, a.Tk, a.Hk * a.D, a.dk, a.sdk, a.cuk, a.B, a.Nk, s);
+      launch_sum(part + (size_t)n * a.Tk * a.Hk * a.D, n, a.Tk, a.Hk * a.D, a.dv, a.sdv, a.cuk, a.B, a.Nk, s);
+    }
   }
   return hipGetLastError();
 }

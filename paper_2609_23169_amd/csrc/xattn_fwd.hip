@@ -7,8 +7,11 @@
 // 64-key tiles, K and V double-buffered in LDS by direct loads. As in the
 // block-sparse forward the scores are formed transposed, S^T = K Q^T on 32x32x16
 // bf16 MFMA, so that a lane holds one row's scores and the softmax needs no
-// exchange but one; the exponentials run against the maximum of the first tile,
-// which is replaced when a lane's tile sum leaves fp32's safe range; then
+// exchange but one. The exponentials run against the maximum of the item's first
+// 32 keys; another one is taken (O and the sum rescaled, the half tile's
+// exponentials formed again) only when a lane's sum of a half tile leaves fp32's
+// safe range, above 2^64: O and the sum always use the same reference, so the
+// result is exact in real arithmetic. Then
 // O^T += V^T P^T on 16x16x32 after one v_permlane16_swap per register. Sums,
 // maxima and O are fp32; P is rounded to bf16 for the second product (half a
 // step, 2^-9 relative, as large as that of V itself).
@@ -38,8 +41,8 @@ struct Parts {
 };
 
 template <int DP, int NW, bool SPLIT>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_fwd_kernel(const XArgs a, const unsigned rtiles,
-                                                               const unsigned splits, const bool by_xcd,
+__global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_fwd_kernel(const XArgs a, const XOrder order,
+                                                               const bool by_xcd,
                                                                const Parts parts) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
   __shared__ __attribute__((aligned(1024))) char k_lds0[TILEB];
@@ -50,46 +53,23 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_fwd_kernel(con
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
-  const unsigned item = xcd_item(blockIdx.x, gridDim.x, by_xcd);
-  const unsigned rt = item % rtiles, sp = SPLIT ? item / rtiles % splits : 0;
-  const unsigned bh = item / rtiles / (SPLIT ? splits : 1);
-  const int hk = (int)(bh % (unsigned)a.Hk), b = (int)(bh / (unsigned)a.Hk);
-  const XSample sm = x_sample(a, b);
-  const int rows = sm.nq * a.G;
-  const int row0 = (int)rt * 32 * NW;
-  if (row0 >= rows) return;   // uniform over the workgroup
-
-  // This split's tiles.
-  const int ntiles = (sm.nk + kXKeys - 1) / kXKeys;
-  int t_begin = 0, t_end = ntiles;
-  if constexpr (SPLIT) {
-    const int per = (ntiles + (int)splits - 1) / (int)splits;
-    t_begin = min((int)sp * per, ntiles);
-    t_end = min(t_begin + per, ntiles);
-  }
-  KeyTiles tiles(a.mask ? a.mask + sm.k0 : nullptr, sm.nk, t_begin, t_end);
-
   // Q operand (B of S^T = K Q^T): lane holds Q[row][16 ks + 8 g .. +7].
   bf16x8 qop[KS];
-  const int row = min(row0 + 32 * w + l32, rows - 1);
-  {
-    const int tok = row / a.G;
-    const __bf16* qp = static_cast<const __bf16*>(a.q) + (sm.q0 + tok) * a.sq + (hk * a.G + row - tok * a.G) * a.D;
+  auto load_rows = [&](const XItem& at) __attribute__((always_inline)) {
+    const XArgs& x = *x_args_again();
+    const XSample sm = x_sample(x, at.b);
+    const int r0 = at.tile * 32 * NW + 32 * w;
+    const XRow r = x_row(r0, r0 + l32, sm.nq * x.G, x.G);
+    const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(
+        static_cast<const __bf16*>(x.q) + (sm.q0 + r.first) * x.sq + (int64_t)at.hk * x.G * x.D, kXOut);
+    const int off = ((r.tok - r.first) * x.sq + r.head * x.D + 8 * g) * 2;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      qop[ks] = bf16x8{};
-      if (16 * ks + 8 * g < a.D) qop[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks + 8 * g);
-    }
-  }
-  const TileLoad<DP, NW> load_k(lane, a.D, a.sk), load_v(lane, a.D, a.sv);
-  const __bf16* const kb = static_cast<const __bf16*>(a.k) + sm.k0 * a.sk + hk * a.D;
-  const __bf16* const vb = static_cast<const __bf16*>(a.v) + sm.k0 * a.sv + hk * a.D;
-  auto load_tile = [&](int t, uint64_t bits, char* kd, char* vd) __attribute__((always_inline)) {
-    load_k(kb + (int64_t)t * kXKeys * a.sk, a.sk, bits, kd, w, lane);
-    load_v(vb + (int64_t)t * kXKeys * a.sv, a.sv, bits, vd, w, lane);
+    for (int ks = 0; ks < KS; ++ks) qop[ks] = x_load16(rs, 16 * ks + 8 * g < x.D ? off + 32 * ks : kXOut);
   };
+  const TileLoad<DP, NW> load_k(lane, a.sk), load_v(lane, a.sv);
 
-  // LDS lane offsets of the two products, as in the block-sparse forward.
+  // LDS offsets of the two products: chunk 2 ks + g of row l32, and V^T's operand
+  // as in the block-sparse forward.
   int koff[KS], voff[DT];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) koff[ks] = lds_off<CPR>(l32, 2 * ks + g);
@@ -103,167 +83,253 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void xattn_fwd_kernel(con
   f32x4 oacc[DT][2];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) oacc[dt][0] = oacc[dt][1] = f32x4{};
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = 0.f, l_run = 0.f;
+  bool fresh = true;                   // no key of the item seen yet: no reference (uniform)
 
-  auto step = [&](uint64_t bits, const char* kt_lds, const char* vt_lds) __attribute__((always_inline)) {
-    f32x16 s[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const bf16x8 av = *reinterpret_cast<const bf16x8*>(kt_lds + koff[ks] + kt * 32 * ROWB);
-        s[kt] = mfma32(av, qop[ks], s[kt]);
-      }
-    if (bits != ~(uint64_t)0) {   // uniform
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const unsigned mine = (unsigned)(bits >> (32 * kt)) >> (4 * g);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[kt][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[kt][e] : -INFINITY;
-      }
-    }
-    u32x4 pq[2][2];
-    float lsum = 0.f;
-    auto expo = [&]() __attribute__((always_inline)) {
-      const float m_use = m_run == -INFINITY ? 0.f : m_run;
-      lsum = 0.f;
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const float p0 = fast_exp2(__builtin_fmaf(s[kt][e], c2, -m_use));
-          const float p1 = fast_exp2(__builtin_fmaf(s[kt][e + 1], c2, -m_use));
-          lsum += p0;
-          lsum += p1;
-          pq[kt][(e >> 2) & 1][((e & 3) >> 1) + 2 * (e >> 3)] = pack_bf16x2(p0, p1);
-        }
+  TileSeq seq;
+
+  // One tile in two 32-key halves, so that a wave's vector work has matrix work of
+  // its own beside it: S of half 1 runs beside the exponentials of half 0, and the
+  // second product of half 0 beside the exponentials of half 1. With `swap` the
+  // rows of the next item take the place of this one's once the scores are formed.
+  // The next tile's loads (load(u), u < 2 IPW) stand between the first products.
+  using Load = TileLoad<DP, NW>;
+  auto step = [&](uint64_t bits, const char* kt_lds, const char* vt_lds, bool swap, bool loads,
+                  auto load) __attribute__((always_inline)) {
+    constexpr int kAhead = 4, kPre = 4;
+    bf16x8 kop[kAhead], vop[kPre];
+    auto read_k = [&](int n) __attribute__((always_inline)) {   // product n: half n / KS, ks n % KS
+      return *reinterpret_cast<const bf16x8*>(kt_lds + koff[n % KS] + n / KS * 32 * ROWB);
     };
-    constexpr int kPairs = 2 * DT, kPre = 4;
-    bf16x8 vop[kPre];
-    auto read_v = [&](int pp) __attribute__((always_inline)) {
-      const char* vbuf = vt_lds + 32 * (pp & 1) * ROWB + voff[pp >> 1];
+    auto read_v = [&](int n) __attribute__((always_inline)) {   // half n / DT, d tile n % DT
+      const char* vbuf = vt_lds + n / DT * 32 * ROWB + voff[n % DT];
       const s16x4 lo = lds_read_tr16(vbuf);
       const s16x4 hi = lds_read_tr16(vbuf + 16 * ROWB);
       const s16x8 v8 = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       return __builtin_bit_cast(bf16x8, v8);
     };
+    f32x16 s[2];
+    u32x4 pq[2];      // a half's P as bf16 pairs, as in the block-sparse forward
+    float lsum = 0.f, x[2], m_use = 0.f;
+    // Elements 2 i and 2 i + 1 of half h: their exponents, and their P with its sums.
+    auto expo0 = [&](int h, int i) __attribute__((always_inline)) {
+      x[0] = __builtin_fmaf(s[h][2 * i], c2, -m_use);
+      x[1] = __builtin_fmaf(s[h][2 * i + 1], c2, -m_use);
+    };
+    auto expo1 = [&](int i) __attribute__((always_inline)) {
+      const float p0 = fast_exp2(x[0]), p1 = fast_exp2(x[1]);
+      lsum += p0;
+      lsum += p1;
+      const int e = 2 * i;
+      unsigned q = pack_bf16x2(p0, p1);
+      pin_value(q);      // here, not at its use behind the matrix instructions
+      pin_value(lsum);
+      pq[(e >> 2) & 1][((e & 3) >> 1) + 2 * (e >> 3)] = q;
+    };
+    auto half_max = [&](int h) __attribute__((always_inline)) {
+      float mx = s[h][0];
 #pragma unroll
-    for (int pp = 0; pp < kPre; ++pp) vop[pp] = read_v(pp);
-    bool redo = __ballot(m_run == -INFINITY) != 0;
-    if (!redo) {
-      expo();
-      redo = __ballot(!(lsum <= kSumGuard)) != 0;   // also catches inf and NaN
-    }
-    if (redo) {
-      float mx = s[0][0];
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[h][e]);
+      return fmaxf(pair_max(mx) * c2, -3.0e38f);
+    };
+    // Before half h's exponentials: unused keys, and the item's reference.
+    auto prepare = [&](int h) __attribute__((always_inline)) {
+      const unsigned half = (unsigned)(bits >> (32 * h));
+      if (half != ~0u) {   // uniform
+        const unsigned mine = half >> (4 * g);
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int e = (kt == 0 ? 1 : 0); e < 16; ++e) mx = fmaxf(mx, s[kt][e]);
-      mx = pair_max(mx) * c2;
-      float alpha = 1.f;
-      if (mx > m_run) {
-        alpha = fast_exp2(m_run - mx);   // 0 on the first tile
+        for (int e = 0; e < 16; ++e) s[h][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[h][e] : -INFINITY;
+      }
+      if (fresh && half) {   // uniform
+        m_run = half_max(h);
+        fresh = false;
+      }
+      m_use = m_run;
+      lsum = 0.f;
+    };
+    // After them: another reference where a lane's sum left fp32's safe range (or
+    // is inf or NaN), then P to the operand layout of two 16-row groups.
+    bf16x8 pop[2];
+    auto settle = [&](int h) __attribute__((always_inline)) {
+      if (__ballot(!(lsum <= kSumGuard)) != 0) {
+        const float to = fmaxf(half_max(h), m_run), alpha = fast_exp2(m_run - to);
         l_run *= alpha;
-        m_run = mx;
-      }
-      const auto ar = __builtin_amdgcn_permlane16_swap(__float_as_uint(alpha), __float_as_uint(alpha), false, false);
+        m_run = m_use = to;
+        const auto ar = __builtin_amdgcn_permlane16_swap(__float_as_uint(alpha), __float_as_uint(alpha), false, false);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        oacc[dt][0] *= __uint_as_float(ar[0]);
-        oacc[dt][1] *= __uint_as_float(ar[1]);
-      }
-      expo();
-    }
-    l_run += lsum;
-    bf16x8 pop[2][2];
+        for (int dt = 0; dt < DT; ++dt) {
+          oacc[dt][0] *= __uint_as_float(ar[0]);
+          oacc[dt][1] *= __uint_as_float(ar[1]);
+        }
+        lsum = 0.f;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const u32x4 x = pq[kt][0], y = pq[kt][1];
+        for (int i = 0; i < 8; ++i) {
+          expo0(h, i);
+          expo1(i);
+        }
+      }
+      l_run += lsum;
       u32x4 nx, ny;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const auto r = __builtin_amdgcn_permlane16_swap(x[v], y[v], false, false);
+        const auto r = __builtin_amdgcn_permlane16_swap(pq[0][v], pq[1][v], false, false);
         nx[v] = r[0];
         ny[v] = r[1];
       }
-      pop[kt][0] = __builtin_bit_cast(bf16x8, nx);
-      pop[kt][1] = __builtin_bit_cast(bf16x8, ny);
-    }
-#pragma unroll
-    for (int pp = 0; pp < kPairs; ++pp) {
-      const bf16x8 av = vop[pp % kPre];
-      if (pp + kPre < kPairs) vop[pp % kPre] = read_v(pp + kPre);
-      oacc[pp >> 1][0] = mfma16(av, pop[pp & 1][0], oacc[pp >> 1][0]);
-      oacc[pp >> 1][1] = mfma16(av, pop[pp & 1][1], oacc[pp >> 1][1]);
-    }
-#pragma unroll
-    for (int pp = 0; pp + kPre < kPairs; ++pp) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);   // MFMA
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);   // DS read
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, 2 * kPre, 0);
-  };
+      pop[0] = __builtin_bit_cast(bf16x8, nx);
+      pop[1] = __builtin_bit_cast(bf16x8, ny);
+    };
 
-  // Tile in stage P: its successor's loads into the other stage (read in the
-  // iteration before, behind the last barrier), its products, the wait.
-  int tile = 0;
-  uint64_t bits = 0;
-  bool more = tiles.next(tile, bits);
-  auto iter = [&](auto par) __attribute__((always_inline)) {
-    constexpr int P = decltype(par)::value;
-    const uint64_t now = bits;
-    more = tiles.next(tile, bits);
-    if (more) load_tile(tile, bits, P ? k_lds0 : k_lds1, P ? v_lds0 : v_lds1);
-    step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-  };
-  if (more) {
-    load_tile(tile, bits, k_lds0, v_lds0);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    while (true) {
-      iter(std::integral_constant<int, 0>{});
-      if (!more) break;
-      iter(std::integral_constant<int, 1>{});
-      if (!more) break;
-    }
-  }
-
-  // O = O^T / l, LSE = (m + log2 l) ln 2; a row without keys: 0 and -inf.
-  const float l_tot = pair_sum(l_run);
-  const bool none = l_tot == 0.f;
-  if (row0 + 32 * w + l32 < rows && g == 0) {
-    const int tok = row / a.G;
-    const int64_t stat = sm.stat0 + (hk * a.G + row - tok * a.G) * sm.hstep + tok;
-    if constexpr (SPLIT) parts.sums[sp * parts.stats + stat] = make_float2(m_run, l_tot);
-    else a.lse[stat] = none ? -INFINITY : (m_run + __log2f(l_tot)) * kLn2;
-  }
-  const float inv = SPLIT ? 1.f : none ? 0.f : 1.f / l_tot;
-  const auto ir = __builtin_amdgcn_permlane16_swap(__float_as_uint(inv), __float_as_uint(inv), false, false);
 #pragma unroll
-  for (int qg = 0; qg < 2; ++qg) {
-    const int ro = row0 + 32 * w + 16 * qg + c16;
-    if (ro >= rows) continue;
-    const int tok = ro / a.G, head = hk * a.G + ro - tok * a.G;
-    const float iv = __uint_as_float(ir[qg]);
-    if constexpr (SPLIT) {
-      float* op = parts.o + (sp * parts.stats + sm.stat0 + head * sm.hstep + tok) * a.D + 4 * gq;
+    for (int n = 0; n < kAhead; ++n) kop[n] = read_k(n);
+    pin_order();
+    // S^T of half 0, its K operands read kAhead products before their use
+    s[0] = f32x16{};
+    if (loads) {   // uniform
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        if (16 * dt + 4 * gq < a.D) *reinterpret_cast<f32x4*>(op + 16 * dt) = oacc[dt][qg];
+      for (int n = 0; n < KS; ++n) {
+        s[0] = mfma32(kop[n % kAhead], qop[n], s[0]);
+        kop[n % kAhead] = read_k(n + kAhead);
+#pragma unroll
+        for (int u = n * 2 * Load::IPW / KS; u < (n + 1) * 2 * Load::IPW / KS; ++u) load(u);
+        pin_order();
+      }
     } else {
-      __bf16* op = static_cast<__bf16*>(a.o) + (sm.q0 + tok) * a.so + head * a.D + 4 * gq;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        bf16x4 v4;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v4[e] = (__bf16)(oacc[dt][qg][e] * iv);
-        if (16 * dt + 4 * gq < a.D) *reinterpret_cast<bf16x4*>(op + 16 * dt) = v4;
+      for (int n = 0; n < KS; ++n) {
+        s[0] = mfma32(kop[n % kAhead], qop[n], s[0]);
+        kop[n % kAhead] = read_k(n + kAhead);
+        pin_order();
       }
     }
+    prepare(0);
+    pin_order();
+    // S^T of half 1 beside the exponentials of half 0
+    s[1] = f32x16{};
+#pragma unroll
+    for (int n = 0; n < KS; ++n) {
+      s[1] = mfma32(kop[n % kAhead], qop[n], s[1]);
+      if (n + kAhead < KS) kop[n % kAhead] = read_k(KS + n + kAhead);
+      else if (n + kAhead - KS < kPre) vop[n + kAhead - KS] = read_v(n + kAhead - KS);
+#pragma unroll
+      for (int i = n * 8 / KS; i < (n + 1) * 8 / KS; ++i) {
+        expo0(0, i);
+        expo1(i);
+      }
+      pin_order();
+    }
+    if (swap) load_rows(seq.cold.item(TileSeq::kAt));   // uniform
+    settle(0);
+    prepare(1);
+    pin_order();
+    // O^T += V^T P^T of half 0 beside the exponentials of half 1
+#pragma unroll
+    for (int n = 0; n < DT; ++n) {
+      const bf16x8 av = vop[n % kPre];
+      oacc[n][0] = mfma16(av, pop[0], oacc[n][0]);
+      oacc[n][1] = mfma16(av, pop[1], oacc[n][1]);
+      vop[n % kPre] = read_v(n + kPre);
+#pragma unroll
+      for (int i = n * 8 / DT; i < (n + 1) * 8 / DT; ++i) {
+        expo0(1, i);
+        expo1(i);
+      }
+      pin_order();
+    }
+    settle(1);
+    pin_order();
+#pragma unroll
+    for (int n = 0; n < DT; ++n) {
+      const bf16x8 av = vop[n % kPre];
+      oacc[n][0] = mfma16(av, pop[0], oacc[n][0]);
+      oacc[n][1] = mfma16(av, pop[1], oacc[n][1]);
+      if (n + kPre < DT) vop[n % kPre] = read_v(DT + n + kPre);
+      pin_order();
+    }
+  };
+
+  // O = O^T / l, LSE = (m + log2 l) ln 2; a row without keys: 0 and -inf.
+  auto finish = [&](const XItem& at) __attribute__((always_inline)) {
+    const XArgs& x = *x_args_again();
+    const XSample sm = x_sample(x, at.b);
+    const int rows = sm.nq * x.G, r0 = at.tile * 32 * NW + 32 * w;
+    const float l_tot = pair_sum(l_run);
+    const bool none = l_tot == 0.f;
+    if (r0 + l32 < rows && g == 0) {
+      const int row = r0 + l32, tok = row_token(row, x.G);
+      const int64_t stat = sm.stat0 + (at.hk * x.G + row - tok * x.G) * sm.hstep + tok;
+      if constexpr (SPLIT) parts.sums[at.part * parts.stats + stat] = make_float2(m_run, l_tot);
+      else x.lse[stat] = none ? -INFINITY : (m_run + __log2f(l_tot)) * kLn2;
+    }
+    const float inv = SPLIT ? 1.f : none ? 0.f : 1.f / l_tot;
+    const auto ir = __builtin_amdgcn_permlane16_swap(__float_as_uint(inv), __float_as_uint(inv), false, false);
+#pragma unroll
+    for (int qg = 0; qg < 2; ++qg) {
+      const int ro = r0 + 16 * qg + c16;
+      const XRow r = x_row(r0, ro, rows, x.G);
+      const float iv = __uint_as_float(ir[qg]);
+      if constexpr (SPLIT) {
+        if (ro >= rows) continue;
+        float* op = parts.o +
+                    (at.part * parts.stats + sm.stat0 + (at.hk * x.G + r.head) * sm.hstep + r.tok) * x.D + 4 * gq;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          if (16 * dt + 4 * gq < x.D) *reinterpret_cast<f32x4*>(op + 16 * dt) = oacc[dt][qg];
+      } else {
+        const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(
+            static_cast<__bf16*>(x.o) + (sm.q0 + r.first) * x.so + (int64_t)at.hk * x.G * x.D, kXOut);
+        const int off = ro < rows ? ((r.tok - r.first) * x.so + r.head * x.D + 4 * gq) * 2 : kXOut;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          bf16x4 v4;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v4[e] = (__bf16)(oacc[dt][qg][e] * iv);
+          x_store8(v4, rs, 16 * dt + 4 * gq < x.D ? off + 32 * dt : kXOut);
+        }
+      }
+    }
+  };
+
+  // A workgroup's items in turn, their tiles as one sequence: a tile's loads are
+  // issued while the tile before it is worked on, across items too.
+  seq.begin(x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk, by_xcd));
+  bool have = false;   // a tile lies in the current stage
+  auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
+    constexpr int P = decltype(par)::value;
+    const uint64_t now = seq.bits;
+    bool changed;
+    const bool more = seq.next(order, 32 * NW, changed);
+    if (!have && !more) return false;
+    char* const kn = P ? k_lds0 : k_lds1;
+    char* const vn = P ? v_lds0 : v_lds1;
+    const int64_t key = seq.k0 + (int64_t)seq.tile * kXKeys;
+    const __amdgpu_buffer_rsrc_t rk = load_k.tile(static_cast<const __bf16*>(a.k) + key * a.sk + seq.hk * a.D, a.sk);
+    const __amdgpu_buffer_rsrc_t rv = load_v.tile(static_cast<const __bf16*>(a.v) + key * a.sv + seq.hk * a.D, a.sv);
+    const bool all = more && seq.bits == ~(uint64_t)0;
+    if (more && !all) {
+      load_k.masked(rk, a.sk, seq.bits, kn, w, lane, a.D);
+      load_v.masked(rv, a.sv, seq.bits, vn, w, lane, a.D);
+    }
+    // before the first tile too, beside its loads: what it leaves is not used
+    step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, all, [&](int u) __attribute__((always_inline)) {
+      if (u < Load::IPW) load_k.one(rk, a.sk, kn, w, u, a.D);
+      else load_v.one(rv, a.sv, vn, w, u - Load::IPW, a.D);
+    });
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (changed) {
+      // its stores end beside the next item's first tile
+      if (have) finish(seq.cold.item(TileSeq::kCur));
+      seq.cold.put(TileSeq::kCur, seq.cold.item(TileSeq::kAt));
+      m_run = l_run = 0.f;
+      fresh = true;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) oacc[dt][0] = oacc[dt][1] = f32x4{};
+    }
+    have = true;
+    return more;
+  };
+  while (iter(std::integral_constant<int, 0>{}) && iter(std::integral_constant<int, 1>{})) {
   }
 }
 
@@ -348,16 +414,23 @@ int64_t fwd_groups(const XArgs& a) {
 }
 int64_t stats_of(const XArgs& a) { return a.Tq * a.Hq; }
 
+// Workgroups that a grid needs to fill the chip: those that fit 256 CUs at once,
+// by LDS (64 KB at 128 columns, 32 KB at 64) and by registers (four waves of 128
+// columns or eight to twelve of 64 on a CU's four SIMDs).
+template <int DP, int NW>
+constexpr int64_t kResident = 256 * (DP == 128 ? 2 : NW == 4 ? 3 : 4);
+
 template <int DP, int NW>
 void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
-  const unsigned rtiles = (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW));
-  const dim3 grid((unsigned)(fwd_groups(a) * splits));
-  const bool by_xcd = (int64_t)a.Nk * a.D * 4 <= kXcdHeadBytes;
+  const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
+  const int64_t items = fwd_groups(a) * splits;
+  const dim3 grid((unsigned)(std::min<int64_t>(items, kResident<DP, NW>) + 7) / 8 * 8);
+  const bool by_xcd = (int64_t)a.B * a.Nk * a.D * 4 <= kXcdHeadBytes;
   TraceScope ts_(s, splits > 1 ? "xattn_fwd_split" : "xattn_fwd", DP, NW);
   if (splits > 1)
-    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, true>), grid, dim3(64 * NW), 0, s, a, rtiles, (unsigned)splits, by_xcd, parts);
+    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, true>), grid, dim3(64 * NW), 0, s, a, order, by_xcd, parts);
   else
-    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, false>), grid, dim3(64 * NW), 0, s, a, rtiles, 1u, by_xcd, parts);
+    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, false>), grid, dim3(64 * NW), 0, s, a, order, by_xcd, parts);
 }
 template <int GPR>
 void launch_join(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {

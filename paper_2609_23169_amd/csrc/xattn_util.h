@@ -11,14 +11,65 @@ namespace ut {
 constexpr int kXKeys = 64;                 // keys of a tile
 constexpr int kXOut = 0x40000000;          // a byte offset past every descriptor's range: reads zeros
 
-// Work item of workgroup wg: the items are numbered so that neighbours share
-// keys, and each XCD (workgroups go to the eight in turn) takes one run of them.
-// With by_xcd false they are taken in plain order.
-__device__ inline unsigned xcd_item(unsigned wg, unsigned n, bool by_xcd) {
-  if (!by_xcd) return wg;
-  const unsigned x = wg & 7, q = n >> 3, r = n & 7;
-  return x * q + min(x, r) + (wg >> 3);
+// The kernel's arguments (an XArgs in front of the others), read again where they
+// are used: work done once an item would otherwise hold some fifty scalar
+// registers through the loop over the tiles, which the compiler then spills.
+__device__ inline const XArgs* x_args_again() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto p = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return (const XArgs*)p;
+#else
+  return nullptr;
+#endif
 }
+
+// The work items of a persistent workgroup: first, first + step, ... below end.
+// Each XCD (workgroups go to the eight in turn) takes one run of the items, its
+// workgroups in turn, so that they share keys in their L2; with by_xcd false all
+// workgroups take the items in turn. The grid is a multiple of 8 with by_xcd.
+struct XItems {
+  unsigned first, step, end;
+};
+__device__ inline XItems x_items(unsigned total, bool by_xcd) {
+  const unsigned wg = blockIdx.x;
+  if (!by_xcd) return XItems{wg, gridDim.x, total};
+  const unsigned x = wg & 7, q = total >> 3, r = total & 7, start = x * q + min(x, r);
+  return XItems{start + (wg >> 3), gridDim.x >> 3, start + q + (x < r ? 1 : 0)};
+}
+// How item numbers are read: `heads` key heads of a group fastest (their rows lie
+// side by side), then samples, whose lengths may differ, so that every run holds
+// alike parts of all of them, then tiles, parts of a split, groups of heads.
+struct XOrder {
+  unsigned heads, tiles, splits;
+};
+// Heads of a group: an eighth of them, so that each XCD has a group of its own
+// and the runs are alike whatever the samples' lengths.
+inline unsigned head_group(const XArgs& a) { return a.Hk % 8 == 0 ? (unsigned)a.Hk / 8 : 1; }
+struct XItem {
+  int b, tile, part, hk;
+};
+__device__ inline XItem x_item(unsigned it, unsigned B, const XOrder& o) {
+  const unsigned r = it / o.heads, s = r / B, t = s / o.tiles, u = t / o.splits;
+  return XItem{(int)(r - s * B), (int)(s - t * o.tiles), (int)(t - u * o.splits), (int)(u * o.heads + it - r * o.heads)};
+}
+
+// Uniform values that a change of item needs, in the lanes of one vector register:
+// the scalar registers are left to the loop over the tiles.
+struct ColdItems {
+  unsigned v = 0;
+  __device__ inline void put(int i, unsigned x) { v = (int)(threadIdx.x & 63) == i ? x : v; }
+  __device__ inline unsigned get(int i) const { return __builtin_amdgcn_readlane(v, i); }
+  __device__ inline void put(int slot, const XItem& x) {
+    put(4 * slot, (unsigned)x.b);
+    put(4 * slot + 1, (unsigned)x.tile);
+    put(4 * slot + 2, (unsigned)x.part);
+    put(4 * slot + 3, (unsigned)x.hk);
+  }
+  __device__ inline XItem item(int slot) const {
+    return XItem{(int)get(4 * slot), (int)get(4 * slot + 1), (int)get(4 * slot + 2), (int)get(4 * slot + 3)};
+  }
+};
 
 // The key tiles of one sample that hold a key in use, and which keys of each:
 // 64 tiles at a time, one a lane, as 64-bit masks, so that a step to the next
@@ -29,8 +80,13 @@ struct KeyTiles {
   int n, end, base;
   uint64_t mine, left;   // this lane's tile; the group's tiles not yet visited
 
-  __device__ inline KeyTiles(const uint8_t* m, int keys, int begin, int stop)
-      : mask(m), n(keys), end(stop), base(begin - 64), mine(0), left(0) {}
+  __device__ inline void open(const uint8_t* m, int keys, int begin, int stop) {
+    mask = m;
+    n = keys;
+    end = stop;
+    base = begin - 64;
+    mine = left = 0;
+  }
 
   __device__ inline void group() {
     const int lane = threadIdx.x & 63, t = base + lane;
@@ -87,10 +143,29 @@ struct XSample {
   int64_t stat0;      // statistics of (head 0, the first token)
   int64_t hstep;      // statistics from one head to the next
 };
+// Offset i of a sample array, as a scalar load (the array is not written while the
+// kernel runs).
+__device__ inline int x_cu(const int32_t* cu, int i) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return ((const __attribute__((address_space(4))) int32_t*)cu)[i];
+#else
+  return cu[i];
+#endif
+}
 __device__ inline XSample x_sample(const XArgs& a, int b) {
-  const SampleRows q = sample_rows(a.cuq, a.Tq, b, 0, a.Hq, a.Nq);
-  const SampleRows k = sample_rows(a.cuk, a.Tk, b, 0, 1, a.Nk);
-  return XSample{q.tok0, k.tok0, q.n, k.n, q.stat0, a.cuq ? a.Tq : (int64_t)a.Nq};
+  if (!a.cuq)
+    return XSample{(int64_t)b * a.Nq, (int64_t)b * a.Nk, a.Nq, a.Nk, (int64_t)b * a.Hq * a.Nq, (int64_t)a.Nq};
+  // clamped as in sample_rows: no offsets can send an access outside the tensors
+  const int64_t q0 = min(max((int64_t)x_cu(a.cuq, b), (int64_t)0), a.Tq);
+  const int64_t q1 = min(max((int64_t)x_cu(a.cuq, b + 1), q0), a.Tq);
+  const int64_t k0 = min(max((int64_t)x_cu(a.cuk, b), (int64_t)0), a.Tk);
+  const int64_t k1 = min(max((int64_t)x_cu(a.cuk, b + 1), k0), a.Tk);
+  return XSample{q0, k0, (int)min(q1 - q0, (int64_t)a.Nq), (int)min(k1 - k0, (int64_t)a.Nk), q0, a.Tq};
+}
+// Token of row `row` (the division is skipped where every head has its own keys).
+__device__ inline int row_token(int row, int G) {
+  if (G == 1) return row;
+  return (int)((unsigned)row / (unsigned)G);
 }
 
 // Whether packed token `tok` belongs to one of the B samples (lengths up to N).
@@ -102,10 +177,92 @@ __device__ inline bool in_sample(const int32_t* __restrict__ cu, int64_t T, int 
   return false;
 }
 
+// The tiles of a persistent workgroup's items as one sequence. The code of a change
+// of item stands once in the loop: an item whose keys are not in use yields one
+// tile without keys (bits 0), so that it is finished like the others.
+struct TileSeq {
+  KeyTiles tiles;
+  ColdItems cold;     // slots kAt (the item of the last tile given), kItems, and the caller's
+  static constexpr int kAt = 0, kItems = 1, kCur = 2;
+  int tile;
+  uint64_t bits;
+  bool fresh;         // that item has given no tile yet
+  int64_t k0;         // its sample's first key
+  int hk;             // its key head
+
+  __device__ inline void begin(const XItems& i) {
+    cold.put(4 * kItems, i.first);
+    cold.put(4 * kItems + 1, i.step);
+    cold.put(4 * kItems + 2, i.end);
+    tiles.open(nullptr, 0, 0, 0);
+    tile = hk = 0;
+    k0 = 0;
+    bits = 0;
+    fresh = false;
+  }
+  // The next tile; false at the end. changed: it is another item's than the one before.
+  __device__ inline bool next(const XOrder& order, int rows_per_item, bool& changed) {
+    changed = false;
+    while (true) {
+      if (tiles.next(tile, bits)) break;
+      if (fresh) {
+        bits = 0;
+        break;
+      }
+      changed = true;
+      bool found = false;
+      unsigned it = cold.get(4 * kItems);
+      const unsigned step = cold.get(4 * kItems + 1), end = cold.get(4 * kItems + 2);
+      while (it < end && !found) {
+        const XArgs& x = *x_args_again();
+        const XItem at = x_item(it, (unsigned)x.B, order);
+        it += step;
+        const XSample sm = x_sample(x, at.b);
+        const int n = (sm.nk + kXKeys - 1) / kXKeys;
+        int t0 = 0, t1 = n;
+        if (order.splits > 1) {
+          const int per = (n + (int)order.splits - 1) / (int)order.splits;
+          t0 = min(at.part * per, n);
+          t1 = min(t0 + per, n);
+        }
+        tiles.open(x.mask ? x.mask + sm.k0 : nullptr, sm.nk, t0, t1);
+        k0 = sm.k0;
+        hk = at.hk;
+        cold.put(kAt, at);
+        found = at.tile * rows_per_item < sm.nq * x.G;
+      }
+      cold.put(4 * kItems, it);
+      if (!found) return false;
+      fresh = true;
+    }
+    fresh = false;
+    return true;
+  }
+};
+
+// Lane offsets of operand rows: a wave's 32 rows r0 .. of an item, row r = token
+// r / G and head r % G, rows past the sample's last repeated. `first` is the
+// token that the byte offsets count from (rows of 128 tokens stay below kXOut).
+struct XRow {
+  int first, tok, head;   // tokens within the sample; head within the group
+};
+__device__ inline XRow x_row(int r0, int row, int rows, int G) {
+  const int r = min(row, rows - 1), tok = row_token(r, G);
+  return XRow{__builtin_amdgcn_readfirstlane(row_token(min(r0, rows - 1), G)), tok, r - tok * G};
+}
+// 16 bytes a lane, or zeros for an offset of kXOut and more.
+__device__ inline bf16x8 x_load16(__amdgpu_buffer_rsrc_t rs, int off) {
+  return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
+}
+__device__ inline void x_store8(bf16x4 v, __amdgpu_buffer_rsrc_t rs, int off) {   // dropped from kXOut on
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), rs, off, 0, 0);
+}
+
 // Direct loads of 64-row tiles into LDS by NW waves, in rows of DP elements:
-// instruction u of wave w writes 1 KB of rows. The swizzle repeats every 16
-// rows, so a lane keeps one offset for each of the instructions of 16 rows, and
-// the rest of the row's offset is a scalar.
+// instruction u of wave w writes 1 KB of rows. Within 16 rows the swizzle only
+// flips bits of the column that the instruction's number gives, so a lane keeps
+// its row's offset and its column, and the rest is scalar.
 template <int DP, int NW>
 struct TileLoad {
   static constexpr int ROWB = DP * 2, CPR = DP / 8;
@@ -113,34 +270,42 @@ struct TileLoad {
   static constexpr int IPW = kXKeys * ROWB / 1024 / NW;        // instructions per wave
   static constexpr int REP = 16 / RPI;                         // instructions of 16 rows
   static_assert(IPW % REP == 0, "a wave takes whole runs of 16 rows");
-  int off[REP];
+  int row;      // bytes from the instruction's first row to this lane's
+  int column;   // this lane's byte in it, instruction 0
 
-  __device__ inline TileLoad(int lane, int D, int stride) {
-#pragma unroll
-    for (int u = 0; u < REP; ++u) {
-      const int r = u * RPI + lane / CPR, p = lane % CPR;
-      const int c = (lds_off<CPR>(r, p) >> 4) & (CPR - 1);
-      off[u] = c < D / 8 ? r * stride * 2 + 16 * c : kXOut;    // columns past D read zeros
-    }
+  __device__ inline TileLoad(int lane, int stride) {
+    row = lane / CPR * stride * 2;
+    column = (lds_off<CPR>(lane / CPR, lane % CPR) & (ROWB - 1));
   }
-  // Tile at `src` (its first key's row of this head), keys in `bits`; other rows
-  // become zeros, whatever memory holds there, and are not read.
-  __device__ inline void operator()(const __bf16* src, int stride, uint64_t bits, char* dst, int w, int lane) const {
-    const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(src, (kXKeys - 1) * stride * 2 + DP * 2);
-    if (bits == ~(uint64_t)0) {
+  // Instruction u's column: rows u RPI further on differ in the swizzle by u's
+  // bits (CPR 16: rows 4 u + r, CPR 8: rows 8 u + r).
+  static constexpr int flip(int u) { return CPR == 16 ? u << 4 : (4 * u) << 4; }
+
+  // A tile's descriptor, from its first key's row of this head.
+  __device__ inline __amdgpu_buffer_rsrc_t tile(const __bf16* src, int stride) const {
+    const uint64_t p = (uint64_t)src;   // uniform: kept in scalar registers
+    const uint64_t u = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((unsigned)(p >> 32)) << 32 |
+                       (unsigned)__builtin_amdgcn_readfirstlane((unsigned)p);
+    return buffer_rsrc((const void*)u, (kXKeys - 1) * stride * 2 + DP * 2);
+  }
+  // Instruction u of wave w of a tile whose keys are all in use. Columns past D
+  // become zeros.
+  __device__ inline void one(__amdgpu_buffer_rsrc_t rs, int stride, char* dst, int w, int u, int D) const {
+    const int i = w * IPW + u, c = column ^ flip(u % REP);
+    int step = RPI * stride * 2;   // not kept in a register for each instruction
+    UT_DEV_ASM("" : "+s"(step));
+    buffer_load_lds16(rs, dst + i * 1024, c < 2 * D ? row + c : kXOut, i * step);
+  }
+  // All of them, keys in `bits`: other rows become zeros too, whatever memory holds
+  // there, and are not read.
+  __device__ inline void masked(__amdgpu_buffer_rsrc_t rs, int stride, uint64_t bits, char* dst, int w, int lane,
+                                int D) const {
 #pragma unroll
-      for (int u = 0; u < IPW; ++u) {
-        const int i = w * IPW + u;
-        buffer_load_lds16(rs, dst + i * 1024, off[u % REP], i / REP * 16 * stride * 2);
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < IPW; ++u) {
-        const int i = w * IPW + u;
-        const unsigned run = (unsigned)(bits >> (i / REP * 16)) >> (u % REP * RPI);   // scalar
-        buffer_load_lds16(rs, dst + i * 1024, run >> (lane / CPR) & 1 ? off[u % REP] : kXOut,
-                          i / REP * 16 * stride * 2);
-      }
+    for (int u = 0; u < IPW; ++u) {
+      const int i = w * IPW + u, c = column ^ flip(u % REP);
+      const unsigned run = (unsigned)(bits >> (i * RPI));   // scalar: this instruction's rows
+      buffer_load_lds16(rs, dst + i * 1024, run >> (lane / CPR) & 1 && c < 2 * D ? row + c : kXOut,
+                        i * RPI * stride * 2);
     }
   }
 };
