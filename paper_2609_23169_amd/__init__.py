@@ -439,15 +439,17 @@ def ut_token_mask_from_alpha(alpha, patch: int, threshold: int, radius: int, tok
 
 # The rotary and cross-attention calls take views as well: a token's heads have
 # to be contiguous, the tokens one stride apart (a slice of a fused projection).
+# They are called once a layer on small tensors too, so their checks are written
+# to cost little where nothing is wrong.
 
 def _token_stride(x, name: str) -> int:
     """Elements from token to token of [..., H, D] rows."""
     _need(isinstance(x, torch.Tensor) and x.dim() >= 3, f"{name}: rows [..., H, D]")
     H, D = x.shape[-2:]
-    lead, strides = x.shape[:-2], x.stride()
     row = H * D
-    if x.numel() == 0:
+    if x.is_contiguous() or x.numel() == 0:
         return row
+    lead, strides = x.shape[:-2], x.stride()
     _need((D == 1 or strides[-1] == 1) and (H == 1 or strides[-2] == D), f"{name}: heads must be contiguous")
     step, tokens = 0, 1   # stride of a token, tokens seen from the inner dimensions
     for n, st in zip(reversed(lead), reversed(strides[:-2])):
@@ -462,76 +464,98 @@ def _token_stride(x, name: str) -> int:
     return step
 
 
-def _pv(t, name: str):
-    """Pointer of a (possibly strided) device tensor (None -> NULL)."""
-    if t is None:
-        return None
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live in GPU memory")
-    return t.data_ptr()
+class _Args:
+    """Collects the tensors of a call: one device, their pointers, and the token
+    strides of the rows among them."""
+    __slots__ = ("device", "strides", "plain")
+
+    def __init__(self, first):
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+            raise ValueError("tensors must live in GPU memory")
+        self.device, self.strides, self.plain = first.get_device(), [], True
+
+    def ptr(self, t, name: str):
+        if t is None:
+            return None
+        if not t.is_cuda or t.get_device() != self.device:
+            raise ValueError(f"{name} must live on the device of the first tensor")
+        return t.data_ptr()
+
+    def rows(self, t, name: str):
+        """Pointer of [..., H, D] rows; notes their stride."""
+        if t is None:
+            self.strides.append(0)
+            return None
+        if t.is_contiguous():
+            self.strides.append(t.shape[-1] * t.shape[-2])
+        else:
+            self.strides.append(_token_stride(t, name))
+            self.plain = False
+        return self.ptr(t, name)
+
+    def host_strides(self):
+        """Host array of the strides, NULL where all rows lie back to back."""
+        return None if self.plain else (ctypes.c_int64 * len(self.strides))(*self.strides)
+
+    def call(self, fn, args, workspace, stream):
+        """fn(*args, workspace, its bytes, stream) on the tensors' device."""
+        ws, bytes_ = None, 0
+        if workspace is not None:
+            if not workspace.is_contiguous():
+                raise ValueError("workspace must be contiguous")
+            ws, bytes_ = self.ptr(workspace, "workspace"), _nbytes(workspace)
+        s = stream if stream is not None else torch.cuda.current_stream(self.device)
+        if s.device_index != self.device:
+            raise ValueError("the stream belongs to another device than the tensors")
+        if torch.cuda.current_device() == self.device:
+            return fn(*args, ws, bytes_, s.cuda_stream)
+        with torch.cuda.device(self.device):
+            return fn(*args, ws, bytes_, s.cuda_stream)
 
 
-def _same_device(first, *others):
-    for t in others:
-        _need(t is None or t.device == first.device, "tensors on different devices")
+def _like(t, like, name: str):
+    if t.shape != like.shape or t.dtype != like.dtype:
+        raise ValueError(f"{name}: the shape and dtype of its counterpart")
 
 
-def _strides(pairs):
-    """Host array of token strides for (tensor or None, name) pairs."""
-    return (ctypes.c_int64 * len(pairs))(*[_token_stride(t, n) if t is not None else 0 for t, n in pairs])
-
-
-def _stream_of(stream, t):
-    """The stream to launch on: the given one, else the current one of t's device."""
-    s = stream if stream is not None else torch.cuda.current_stream(t.device if t.is_cuda else None)
-    _need(s.device == t.device, "the stream belongs to another device than the tensors")
-    return ctypes.c_void_p(s.cuda_stream)
-
-
-def _on(t):
-    """Makes t's device current around a launch."""
-    return torch.cuda.device(t.device) if t.is_cuda else contextlib.nullcontext()
-
-
-def _rope_args(x, y, pos, axis_dims, token_idx, weights):
+def _rope_args(x, y, pos, axis_dims, token_idx, q_weight, k_weight):
     """Checks of the two rotary calls: (n, Hq, Hk, D, axes, weight dtype)."""
-    D, Hq = x.shape[-1], x.shape[-2]
-    n = x.numel() // max(Hq * D, 1)
-    _need(n * Hq * D == x.numel() and Hq * D > 0, "q: rows [..., Hq, D]")
-    Hk = 0
+    _need(x.dim() >= 3, "q: rows [..., Hq, D]")
+    Hq, D = x.shape[-2:]
+    _need(Hq * D > 0, "q: rows [..., Hq, D]")
+    n, Hk = x.numel() // (Hq * D), 0
     if y is not None:
         _need(y.dim() >= 3 and y.shape[-1] == D and y.dtype == x.dtype, "k: rows [..., Hk, D] of q's head_dim and dtype")
         Hk = y.shape[-2]
         _need(Hk > 0 and y.numel() == n * Hk * D, "k: as many tokens as q")
     _need(pos.dtype == torch.float32 and pos.dim() == 2 and pos.is_contiguous() and pos.shape[1] == len(axis_dims),
           "pos: contiguous fp32 [rows, axes], a column for each of axis_dims")
-    if token_idx is not None:
-        _need(token_idx.dtype == torch.int32 and token_idx.is_contiguous() and token_idx.numel() == n,
-              "token_idx: contiguous int32 [n]")
+    _need(token_idx is None or (token_idx.dtype == torch.int32 and token_idx.is_contiguous()
+                                and token_idx.numel() == n), "token_idx: contiguous int32 [n]")
     wd = UT_BF16
-    for w in weights:
-        if w is not None:
-            _need(w.numel() == D and w.is_contiguous(), "weights: contiguous [D]")
-            _need(w.dtype == weights[0].dtype if weights[0] is not None else True, "weights: one dtype")
-            wd = _dtype_code(w)
+    if q_weight is not None or k_weight is not None:
+        for w in (q_weight, k_weight):
+            _need(w is None or (w.numel() == D and w.is_contiguous()), "weights: contiguous [D]")
+        _need(q_weight is None or k_weight is None or q_weight.dtype == k_weight.dtype, "weights: one dtype")
+        wd = _dtype_code(q_weight if q_weight is not None else k_weight)
     return n, Hq, Hk, D, (ctypes.c_int32 * len(axis_dims))(*axis_dims), wd
 
 
 def ut_qk_rope_fwd(q, k, q_out, k_out, pos, axis_dims, theta: float, token_idx=None, q_weight=None,
                    k_weight=None, eps: float = 1e-6, interleaved: bool = True, stream=None) -> int:
-    _need(q.dim() >= 3, "q: rows [..., Hq, D]")
-    n, Hq, Hk, D, axes, wd = _rope_args(q, k, pos, axis_dims, token_idx, (q_weight, k_weight))
-    _need(q_out.shape == q.shape and q_out.dtype == q.dtype, "q_out: like q")
+    n, Hq, Hk, D, axes, wd = _rope_args(q, k, pos, axis_dims, token_idx, q_weight, k_weight)
+    _like(q_out, q, "q_out")
     _need((k_out is None) == (k is None), "k_out goes with k")
-    _need(k is None or (k_out.shape == k.shape and k_out.dtype == k.dtype), "k_out: like k")
-    _same_device(q, k, q_out, k_out, pos, token_idx, q_weight, k_weight)
-    strides = _strides([(q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out")])
-    with _on(q):
-        return lib().ut_qk_rope_fwd(_pv(q, "q"), _pv(k, "k"), _pv(q_out, "q_out"), _pv(k_out, "k_out"), strides,
-                                    _dtype_code(q), n, Hq, Hk, D, _pv(pos, "pos"), pos.shape[0],
-                                    _pv(token_idx, "token_idx"), axes, len(axis_dims), theta,
-                                    UT_ROPE_NEAR if interleaved else UT_ROPE_FAR, _pv(q_weight, "q_weight"),
-                                    _pv(k_weight, "k_weight"), wd, eps, _stream_of(stream, q))
+    if k is not None:
+        _like(k_out, k, "k_out")
+    a = _Args(q)
+    rows = (a.rows(q, "q"), a.rows(k, "k"), a.rows(q_out, "q_out"), a.rows(k_out, "k_out"))
+    args = rows + (a.host_strides(), _dtype_code(q), n, Hq, Hk, D, a.ptr(pos, "pos"), pos.shape[0],
+                   a.ptr(token_idx, "token_idx"), axes, len(axis_dims), theta,
+                   UT_ROPE_NEAR if interleaved else UT_ROPE_FAR, a.ptr(q_weight, "q_weight"),
+                   a.ptr(k_weight, "k_weight"), wd, eps)
+    fn = lib().ut_qk_rope_fwd
+    return a.call(lambda *x: fn(*x[:-3], x[-1]), args, None, stream)   # it takes no workspace
 
 
 def ut_qk_rope_bwd_workspace_size(D: int) -> int:
@@ -541,52 +565,50 @@ def ut_qk_rope_bwd_workspace_size(D: int) -> int:
 def ut_qk_rope_bwd(dq_out, dk_out, q, k, dq, dk, pos, axis_dims, theta: float, token_idx=None, q_weight=None,
                    k_weight=None, eps: float = 1e-6, interleaved: bool = True, dq_weight=None, dk_weight=None,
                    workspace=None, stream=None) -> int:
-    _need(dq_out.dim() >= 3, "dq_out: rows [..., Hq, D]")
-    n, Hq, Hk, D, axes, wd = _rope_args(dq_out, dk_out, pos, axis_dims, token_idx, (q_weight, k_weight))
-    for t, like, nm in ((q, dq_out, "q"), (dq, dq_out, "dq"), (k, dk_out, "k"), (dk, dk_out, "dk")):
-        _need(t is None or (like is not None and t.shape == like.shape and t.dtype == like.dtype),
-              f"{nm}: like its output's gradient")
+    n, Hq, Hk, D, axes, wd = _rope_args(dq_out, dk_out, pos, axis_dims, token_idx, q_weight, k_weight)
     _need(dq is not None and (dk is None) == (dk_out is None), "dq, and dk with dk_out")
+    for t, like, nm in ((q, dq_out, "q"), (dq, dq_out, "dq"), (k, dk_out, "k"), (dk, dk_out, "dk")):
+        if t is not None:
+            _need(like is not None, "k goes with dk_out")
+            _like(t, like, nm)
     if q_weight is not None:
         _need(q is not None and (dk_out is None or k is not None), "q and k are needed with weights")
     for g in (dq_weight, dk_weight):
         _need(g is None or (g.dtype == torch.float32 and g.numel() == D and g.is_contiguous()),
               "dq_weight, dk_weight: contiguous fp32 [D]")
-    _same_device(dq_out, dk_out, q, k, dq, dk, pos, token_idx, q_weight, k_weight, dq_weight, dk_weight, workspace)
-    strides = _strides([(dq_out, "dq_out"), (dk_out, "dk_out"), (q, "q"), (k, "k"), (dq, "dq"), (dk, "dk")])
-    with _on(dq_out):
-        return lib().ut_qk_rope_bwd(_pv(dq_out, "dq_out"), _pv(dk_out, "dk_out"), _pv(q, "q"), _pv(k, "k"),
-                                    _pv(dq, "dq"), _pv(dk, "dk"), strides, _dtype_code(dq_out), n, Hq, Hk, D,
-                                    _pv(pos, "pos"), pos.shape[0], _pv(token_idx, "token_idx"), axes, len(axis_dims),
-                                    theta, UT_ROPE_NEAR if interleaved else UT_ROPE_FAR, _pv(q_weight, "q_weight"),
-                                    _pv(k_weight, "k_weight"), wd, eps, _pv(dq_weight, "dq_weight"),
-                                    _pv(dk_weight, "dk_weight"), _p(workspace),
-                                    _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, dq_out))
+    a = _Args(dq_out)
+    rows = (a.rows(dq_out, "dq_out"), a.rows(dk_out, "dk_out"), a.rows(q, "q"), a.rows(k, "k"), a.rows(dq, "dq"),
+            a.rows(dk, "dk"))
+    args = rows + (a.host_strides(), _dtype_code(dq_out), n, Hq, Hk, D, a.ptr(pos, "pos"), pos.shape[0],
+                   a.ptr(token_idx, "token_idx"), axes, len(axis_dims), theta,
+                   UT_ROPE_NEAR if interleaved else UT_ROPE_FAR, a.ptr(q_weight, "q_weight"),
+                   a.ptr(k_weight, "k_weight"), wd, eps, a.ptr(dq_weight, "dq_weight"), a.ptr(dk_weight, "dk_weight"))
+    return a.call(lib().ut_qk_rope_bwd, args, workspace, stream)
 
 
 def _xattn_args(q, k, v, key_mask, dims: int):
     """Checks of the cross-attention calls: (shape in front of the heads of q, of k, Hq, Hk, D)."""
-    lay = "[B, N, H, D]" if dims == 4 else "[T, H, D]"
-    for t, nm in ((q, "q"), (k, "k"), (v, "v")):
-        _need(t.dim() == dims and t.dtype == torch.bfloat16, f"{nm}: bf16 {lay}")
-    _need(k.shape == v.shape and k.shape[-1] == q.shape[-1], "k, v: one shape, q's head_dim")
-    _need(dims == 3 or k.shape[0] == q.shape[0], "q, k, v: one batch size")
-    if key_mask is not None:
-        _need(key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == k.shape[:-2]
-              and key_mask.is_contiguous(), "key_mask: contiguous uint8 or bool, one value a key token")
-    return q.shape[:-2], k.shape[:-2], q.shape[-2], k.shape[-2], q.shape[-1]
+    bf, sq, sk = torch.bfloat16, q.shape, k.shape
+    if (q.dtype != bf or k.dtype != bf or v.dtype != bf or len(sq) != dims or len(sk) != dims or v.shape != sk
+            or sk[-1] != sq[-1] or (dims == 4 and sk[0] != sq[0])):
+        raise ValueError("q, k, v: bf16 " + ("[B, N, H, D], one batch size" if dims == 4 else "[T, H, D]")
+                         + ", one head_dim; k and v of one shape")
+    _need(key_mask is None or (key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == sk[:-2]
+                               and key_mask.is_contiguous()),
+          "key_mask: contiguous uint8 or bool, one value a key token")
+    return sq[:-2], sk[:-2], sq[-2], sk[-2], sq[-1]
 
 
-def _check_like(t, like, nm):
-    _need(t.shape == like.shape and t.dtype == like.dtype, f"{nm}: bf16, the shape of its counterpart")
-
-
-def _check_cu(cu_q, cu_k):
+def _check_cu(cu_q, cu_k) -> int:
     for cu in (cu_q, cu_k):
         _need(cu.dtype == torch.int32 and cu.dim() == 1 and cu.numel() >= 2 and cu.is_contiguous(),
               "cu_seqlens: contiguous int32 [B+1]")
     _need(cu_q.numel() == cu_k.numel(), "cu_seqlens_q and cu_seqlens_k: one number of samples")
     return cu_q.numel() - 1
+
+
+def _check_lse(lse, n: int):
+    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() >= n, "lse: contiguous fp32, a value a row")
 
 
 def ut_xattn_fwd_workspace_size(B: int, Nq: int, Nk: int, Hq: int, Hk: int, D: int) -> int:
@@ -595,14 +617,12 @@ def ut_xattn_fwd_workspace_size(B: int, Nq: int, Nk: int, Hq: int, Hk: int, D: i
 
 def ut_xattn_fwd(q, k, v, o, lse, softmax_scale: float, key_mask=None, workspace=None, stream=None) -> int:
     (B, Nq), (_, Nk), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 4)
-    _check_like(o, q, "o")
-    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() >= B * Hq * Nq, "lse: fp32 [B,Hq,Nq]")
-    _same_device(q, k, v, o, lse, key_mask, workspace)
-    strides = _strides([(q, "q"), (k, "k"), (v, "v"), (o, "o")])
-    with _on(q):
-        return lib().ut_xattn_fwd(_pv(q, "q"), _pv(k, "k"), _pv(v, "v"), _pv(o, "o"), _pv(lse, "lse"), strides,
-                                  _pv(key_mask, "key_mask"), B, Nq, Nk, Hq, Hk, D, softmax_scale, _p(workspace),
-                                  _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, q))
+    _like(o, q, "o")
+    _check_lse(lse, B * Hq * Nq)
+    a = _Args(q)
+    rows = (a.rows(q, "q"), a.rows(k, "k"), a.rows(v, "v"), a.rows(o, "o"))
+    return a.call(lib().ut_xattn_fwd, rows + (a.ptr(lse, "lse"), a.host_strides(), a.ptr(key_mask, "key_mask"), B, Nq,
+                                              Nk, Hq, Hk, D, softmax_scale), workspace, stream)
 
 
 def ut_xattn_fwd_varlen_workspace_size(B: int, Tq: int, max_seqlen_q: int, max_seqlen_k: int, Hq: int, Hk: int,
@@ -615,39 +635,35 @@ def ut_xattn_fwd_varlen(q, k, v, o, lse, cu_seqlens_q, max_seqlen_q: int, cu_seq
                         stream=None) -> int:
     (Tq,), (Tk,), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 3)
     B = _check_cu(cu_seqlens_q, cu_seqlens_k)
-    _check_like(o, q, "o")
-    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() >= Hq * Tq, "lse: fp32 [Hq,Tq]")
-    _same_device(q, k, v, o, lse, key_mask, cu_seqlens_q, cu_seqlens_k, workspace)
-    strides = _strides([(q, "q"), (k, "k"), (v, "v"), (o, "o")])
-    with _on(q):
-        return lib().ut_xattn_fwd_varlen(_pv(q, "q"), _pv(k, "k"), _pv(v, "v"), _pv(o, "o"), _pv(lse, "lse"), strides,
-                                         _pv(key_mask, "key_mask"), _pv(cu_seqlens_q, "cu_seqlens_q"),
-                                         _pv(cu_seqlens_k, "cu_seqlens_k"), B, Tq, Tk, max_seqlen_q, max_seqlen_k,
-                                         Hq, Hk, D, softmax_scale, int(zero_rest), _p(workspace),
-                                         _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, q))
+    _like(o, q, "o")
+    _check_lse(lse, Hq * Tq)
+    a = _Args(q)
+    rows = (a.rows(q, "q"), a.rows(k, "k"), a.rows(v, "v"), a.rows(o, "o"))
+    return a.call(lib().ut_xattn_fwd_varlen,
+                  rows + (a.ptr(lse, "lse"), a.host_strides(), a.ptr(key_mask, "key_mask"),
+                          a.ptr(cu_seqlens_q, "cu_seqlens_q"), a.ptr(cu_seqlens_k, "cu_seqlens_k"), B, Tq, Tk,
+                          max_seqlen_q, max_seqlen_k, Hq, Hk, D, softmax_scale, int(zero_rest)), workspace, stream)
 
 
 def ut_xattn_bwd_workspace_size(B: int, Nq: int, Nk: int, Hq: int, Hk: int, D: int) -> int:
     return int(lib().ut_xattn_bwd_workspace_size(B, Nq, Nk, Hq, Hk, D))
 
 
-def _bwd_tensors(q, k, v, o, dout, dq, dk, dv):
+def _bwd_rows(a, q, k, v, o, dout, dq, dk, dv):
     for t, like, nm in ((o, q, "o"), (dout, q, "dout"), (dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv")):
-        _check_like(t, like, nm)
-    return _strides([(q, "q"), (k, "k"), (v, "v"), (o, "o"), (dout, "dout"), (dq, "dq"), (dk, "dk"), (dv, "dv")])
+        _like(t, like, nm)
+    return (a.rows(q, "q"), a.rows(k, "k"), a.rows(v, "v"), a.rows(o, "o"), a.rows(dout, "dout")), (
+        a.rows(dq, "dq"), a.rows(dk, "dk"), a.rows(dv, "dv"))
 
 
 def ut_xattn_bwd(q, k, v, o, dout, lse, dq, dk, dv, softmax_scale: float, key_mask=None, workspace=None,
                  stream=None) -> int:
     (B, Nq), (_, Nk), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 4)
-    strides = _bwd_tensors(q, k, v, o, dout, dq, dk, dv)
-    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() >= B * Hq * Nq, "lse: fp32 [B,Hq,Nq]")
-    _same_device(q, k, v, o, dout, lse, dq, dk, dv, key_mask, workspace)
-    with _on(q):
-        return lib().ut_xattn_bwd(_pv(q, "q"), _pv(k, "k"), _pv(v, "v"), _pv(o, "o"), _pv(dout, "dout"),
-                                  _pv(lse, "lse"), _pv(dq, "dq"), _pv(dk, "dk"), _pv(dv, "dv"), strides,
-                                  _pv(key_mask, "key_mask"), B, Nq, Nk, Hq, Hk, D, softmax_scale, _p(workspace),
-                                  _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, q))
+    _check_lse(lse, B * Hq * Nq)
+    a = _Args(q)
+    ins, outs = _bwd_rows(a, q, k, v, o, dout, dq, dk, dv)
+    return a.call(lib().ut_xattn_bwd, ins + (a.ptr(lse, "lse"),) + outs + (
+        a.host_strides(), a.ptr(key_mask, "key_mask"), B, Nq, Nk, Hq, Hk, D, softmax_scale), workspace, stream)
 
 
 def ut_xattn_bwd_varlen_workspace_size(B: int, Tq: int, Tk: int, max_seqlen_q: int, max_seqlen_k: int, Hq: int,
@@ -660,16 +676,13 @@ def ut_xattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_seq
                         workspace=None, stream=None) -> int:
     (Tq,), (Tk,), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 3)
     B = _check_cu(cu_seqlens_q, cu_seqlens_k)
-    strides = _bwd_tensors(q, k, v, o, dout, dq, dk, dv)
-    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() >= Hq * Tq, "lse: fp32 [Hq,Tq]")
-    _same_device(q, k, v, o, dout, lse, dq, dk, dv, key_mask, cu_seqlens_q, cu_seqlens_k, workspace)
-    with _on(q):
-        return lib().ut_xattn_bwd_varlen(_pv(q, "q"), _pv(k, "k"), _pv(v, "v"), _pv(o, "o"), _pv(dout, "dout"),
-                                         _pv(lse, "lse"), _pv(dq, "dq"), _pv(dk, "dk"), _pv(dv, "dv"), strides,
-                                         _pv(key_mask, "key_mask"), _pv(cu_seqlens_q, "cu_seqlens_q"),
-                                         _pv(cu_seqlens_k, "cu_seqlens_k"), B, Tq, Tk, max_seqlen_q, max_seqlen_k,
-                                         Hq, Hk, D, softmax_scale, int(zero_rest), _p(workspace),
-                                         _nbytes(workspace) if workspace is not None else 0, _stream_of(stream, q))
+    _check_lse(lse, Hq * Tq)
+    a = _Args(q)
+    ins, outs = _bwd_rows(a, q, k, v, o, dout, dq, dk, dv)
+    return a.call(lib().ut_xattn_bwd_varlen, ins + (a.ptr(lse, "lse"),) + outs + (
+        a.host_strides(), a.ptr(key_mask, "key_mask"), a.ptr(cu_seqlens_q, "cu_seqlens_q"),
+        a.ptr(cu_seqlens_k, "cu_seqlens_k"), B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, softmax_scale,
+        int(zero_rest)), workspace, stream)
 
 
 # ---------------------------------------------------------------------------
@@ -853,10 +866,18 @@ def token_mask_from_alpha(alpha, patch: int = 16, threshold: int = 0, radius: in
     return out
 
 
+_NO_STREAM = contextlib.nullcontext()
+
+
 def _alloc_on(stream):
     """Allocations of a call on `stream` belong to it: the allocator must not
     hand a workspace on while the kernels still use it."""
-    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+    return torch.cuda.stream(stream) if stream is not None else _NO_STREAM
+
+
+def _new_rows(x):
+    """Uninitialised rows like x, back to back."""
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 def _scratch(size: int, device):
@@ -870,8 +891,8 @@ def qk_rope_fwd(q, k, pos, axis_dims, theta: float = 10000.0, token_idx=None, q_
     taking axis_dims[a] elements of the head; with weights [D] the per-head RMS
     norm first. interleaved: pairs (2p, 2p + 1), else (p, p + R/2)."""
     with _alloc_on(stream):
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k is not None else None
+        q_out = _new_rows(q)
+        k_out = _new_rows(k) if k is not None else None
     _raise("ut_qk_rope_fwd", ut_qk_rope_fwd(q, k, q_out, k_out, pos, axis_dims, theta, token_idx, q_weight, k_weight,
                                             eps, interleaved, stream))
     return q_out, k_out
@@ -885,8 +906,8 @@ def qk_rope_bwd(dq_out, dk_out, pos, axis_dims, theta: float = 10000.0, token_id
     dev, D = dq_out.device, dq_out.shape[-1]
     dqw = dkw = None
     with _alloc_on(stream):
-        dq = torch.empty(dq_out.shape, dtype=dq_out.dtype, device=dev)
-        dk = torch.empty(dk_out.shape, dtype=dk_out.dtype, device=dev) if dk_out is not None else None
+        dq = _new_rows(dq_out)
+        dk = _new_rows(dk_out) if dk_out is not None else None
         if q_weight is not None:
             dqw = torch.empty(D, dtype=torch.float32, device=dev)
             dkw = torch.empty(D, dtype=torch.float32, device=dev) if dk_out is not None else None
@@ -902,7 +923,7 @@ def xattn_fwd(q, k, v, softmax_scale: float, key_mask=None, workspace=None, stre
     [B, Nk] (nonzero: in use): (o like q, lse [B, Hq, Nq])."""
     B, Nq, Hq, D = q.shape
     with _alloc_on(stream):
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        o = _new_rows(q)
         lse = torch.empty((B, Hq, Nq), dtype=torch.float32, device=q.device)
         if workspace is None:
             workspace = _scratch(ut_xattn_fwd_workspace_size(B, Nq, k.shape[1], Hq, k.shape[2], D), q.device)
@@ -914,7 +935,7 @@ def xattn_bwd(q, k, v, o, dout, lse, softmax_scale: float, key_mask=None, worksp
     """(dq, dk, dv) of xattn_fwd."""
     B, Nq, Hq, D = q.shape
     with _alloc_on(stream):
-        dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
+        dq, dk, dv = _new_rows(q), _new_rows(k), _new_rows(v)
         if workspace is None:
             workspace = _scratch(ut_xattn_bwd_workspace_size(B, Nq, k.shape[1], Hq, k.shape[2], D), q.device)
     _raise("ut_xattn_bwd", ut_xattn_bwd(q, k, v, o, dout, lse, dq, dk, dv, softmax_scale, key_mask, workspace, stream))
@@ -928,7 +949,7 @@ def xattn_fwd_varlen(q, k, v, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k, max
     the last sample are 0 and -inf."""
     Tq, Hq, D = q.shape
     with _alloc_on(stream):
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        o = _new_rows(q)
         lse = torch.empty((Hq, Tq), dtype=torch.float32, device=q.device)
         if workspace is None:
             workspace = _scratch(ut_xattn_fwd_varlen_workspace_size(cu_seqlens_q.numel() - 1, Tq, max_seqlen_q,
@@ -944,7 +965,7 @@ def xattn_bwd_varlen(q, k, v, o, dout, lse, cu_seqlens_q, max_seqlen_q: int, cu_
     """(dq, dk, dv) of xattn_fwd_varlen; rows behind the last sample are 0."""
     Tq, Hq, D = q.shape
     with _alloc_on(stream):
-        dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
+        dq, dk, dv = _new_rows(q), _new_rows(k), _new_rows(v)
         if workspace is None:
             workspace = _scratch(ut_xattn_bwd_varlen_workspace_size(cu_seqlens_q.numel() - 1, Tq, k.shape[0],
                                                                     max_seqlen_q, max_seqlen_k, Hq, k.shape[1], D),
