@@ -249,7 +249,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   };
 
   // O = O^T / l, LSE = (m + log2 l) ln 2; a row without keys: 0 and -inf.
-  auto finish = [&](const XItem& at) __attribute__((always_inline)) {
+  auto finish = [&](const XItem& at, char* lds0, char* lds1) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
     const int rows = sm.nq * x.G, r0 = at.tile * 32 * NW + 32 * w;
@@ -263,30 +263,21 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     }
     const float inv = SPLIT ? 1.f : none ? 0.f : 1.f / l_tot;
     const auto ir = __builtin_amdgcn_permlane16_swap(__float_as_uint(inv), __float_as_uint(inv), false, false);
+    if constexpr (SPLIT) {
 #pragma unroll
-    for (int qg = 0; qg < 2; ++qg) {
-      const int ro = r0 + 16 * qg + c16;
-      const XRow r = x_row(r0, ro, rows, x.G);
-      const float iv = __uint_as_float(ir[qg]);
-      if constexpr (SPLIT) {
+      for (int qg = 0; qg < 2; ++qg) {
+        const int ro = r0 + 16 * qg + c16;
         if (ro >= rows) continue;
+        const XRow r = x_row(r0, ro, rows, x.G);
         float* op = parts.o +
                     (at.part * parts.stats + sm.stat0 + (at.hk * x.G + r.head) * sm.hstep + r.tok) * x.D + 4 * gq;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
           if (16 * dt + 4 * gq < x.D) *reinterpret_cast<f32x4*>(op + 16 * dt) = oacc[dt][qg];
-      } else {
-        const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(
-            static_cast<__bf16*>(x.o) + (sm.q0 + r.first) * x.so + (int64_t)at.hk * x.G * x.D, kXOut);
-        const int off = ro < rows ? ((r.tok - r.first) * x.so + r.head * x.D + 4 * gq) * 2 : kXOut;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          bf16x4 v4;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v4[e] = (__bf16)(oacc[dt][qg][e] * iv);
-          x_store8(v4, rs, 16 * dt + 4 * gq < x.D ? off + 32 * dt : kXOut);
-        }
       }
+    } else {
+      x_store_rows<DP>(x.o, sm.q0, x.so, (int64_t)at.hk * x.G * x.D, r0, rows, x.G, x.D, lds0, lds1,
+                       [&](int dt, int qg) { return oacc[dt][qg] * __uint_as_float(ir[qg]); });
     }
   };
 
@@ -319,7 +310,9 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     __syncthreads();
     if (changed) {
       // its stores end beside the next item's first tile
-      if (have) finish(seq.cold.item(TileSeq::kCur));
+      if (have)
+        finish(seq.cold.item(TileSeq::kCur), (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024,
+               (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024);
       seq.cold.put(TileSeq::kCur, seq.cold.item(TileSeq::kAt));
       m_run = l_run = 0.f;
       fresh = true;

@@ -254,9 +254,46 @@ __device__ inline XRow x_row(int r0, int row, int rows, int G) {
 __device__ inline bf16x8 x_load16(__amdgpu_buffer_rsrc_t rs, int off) {
   return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
 }
+__device__ inline void x_store16(bf16x8 v, __amdgpu_buffer_rsrc_t rs, int off) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, off, 0, 0);
+}
 __device__ inline void x_store8(bf16x4 v, __amdgpu_buffer_rsrc_t rs, int off) {   // dropped from kXOut on
   typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
   __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), rs, off, 0, 0);
+}
+
+// Stores a wave's 32 result rows, rounded to bf16, as whole rows: 16 bytes a lane,
+// a row's lanes side by side, where the accumulators' layout would write pieces of
+// 32 bytes. The rows pass through the wave's own part of a consumed stage (row
+// group qg through `lds[qg]`, 16 rows, swizzled as the tiles), which only the
+// wave's own next loads write. val(dt, qg): columns 16 dt + 4 gq + (0..3) of row
+// 16 qg + c16 of the rows r0 .. of `rows`.
+template <int DP, class Val>
+__device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t head0, int r0, int rows, int G, int D,
+                                    char* lds0, char* lds1, Val val) {
+  constexpr int CPR = DP / 8, RPI = 64 / CPR, DT = DP / 16;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, gq = lane >> 4;
+  const int first = __builtin_amdgcn_readfirstlane(row_token(min(r0, rows - 1), G));
+  const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<__bf16*>(dst) + (tok0 + first) * stride + head0, kXOut);
+#pragma unroll
+  for (int qg = 0; qg < 2; ++qg) {
+    char* const lds = qg ? lds1 : lds0;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const f32x4 y = val(dt, qg);
+      *reinterpret_cast<bf16x4*>(lds + lds_off<CPR>(c16, 2 * dt + (gq >> 1)) + 8 * (gq & 1)) =
+          bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+  const int c = lane % CPR;
+#pragma unroll
+  for (int u = 0; u < 32 / RPI; ++u) {
+    const int r = u * RPI + lane / CPR, row = r0 + r, tok = row_token(row, G);
+    const bf16x8 v = *reinterpret_cast<const bf16x8*>((r < 16 ? lds0 : lds1) + lds_off<CPR>(r & 15, c));
+    x_store16(v, rs, row < rows && 8 * c < D ? ((tok - first) * stride + (row - tok * G) * D + 8 * c) * 2 : kXOut);
+  }
+  __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done before the next loads
 }
 
 // Direct loads of 64-row tiles into LDS by NW waves, in rows of DP elements:
