@@ -52,42 +52,53 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
-  // A row's Q and dO (the operands), O and LSE.
-  bf16x8 qop[KS], doop[KS], orow[KS];
-  float lse, lse2, ndl;   // LSE; LSE log2 e and -delta
-  auto load_rows = [&](const XItem& at) __attribute__((always_inline)) {
+  bf16x8 qop[KS], doop[KS];   // Q and dO (operands, once turned)
+  float lse2, ndl;            // the row's LSE log2 e and -delta
+  // What only the statistics need: O as loaded, and LSE. (Set between a change of
+  // item and its use alone: held in the loop otherwise.)
+  struct Extra {
+    bf16x8 o[KS];
+    float lse;
+  };
+  auto load_rows = [&](const XItem& at, Extra& ex) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
-    const int r0 = at.tile * 32 * NW + 32 * w;
-    const XRow r = x_row(r0, r0 + l32, sm.nq * x.G, x.G);
-    const int64_t tok0 = sm.q0 + r.first, head0 = (int64_t)at.hk * x.G * x.D;
-    const __amdgpu_buffer_rsrc_t rq = buffer_rsrc(static_cast<const __bf16*>(x.q) + tok0 * x.sq + head0, kXOut);
-    const __amdgpu_buffer_rsrc_t rd = buffer_rsrc(static_cast<const __bf16*>(x.dout) + tok0 * x.sdo + head0, kXOut);
-    const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(static_cast<const __bf16*>(x.o_in) + tok0 * x.so + head0, kXOut);
-    const int t = r.tok - r.first, c = r.head * x.D + 8 * g;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const bool in = 16 * ks + 8 * g < x.D;
-      qop[ks] = x_load16(rq, in ? (t * x.sq + c) * 2 + 32 * ks : kXOut);
-      doop[ks] = x_load16(rd, in ? (t * x.sdo + c) * 2 + 32 * ks : kXOut);
-      orow[ks] = x_load16(ro, in ? (t * x.so + c) * 2 + 32 * ks : kXOut);
-    }
-    lse = x.lse[sm.stat0 + (at.hk * x.G + r.head) * sm.hstep + r.tok];
+    const int r0 = at.tile * 32 * NW + 32 * w, rows = sm.nq * x.G;
+    const int64_t head0 = (int64_t)at.hk * x.G * x.D;
+    x_load_rows<DP>(qop, x.q, sm.q0, x.sq, head0, r0, rows, x.G, x.D);
+    x_load_rows<DP>(doop, x.dout, sm.q0, x.sdo, head0, r0, rows, x.G, x.D);
+    x_load_rows<DP>(ex.o, x.o_in, sm.q0, x.so, head0, r0, rows, x.G, x.D);
+    const int row = min(r0 + l32, rows - 1), tok = row_token(row, x.G);
+    ex.lse = x.lse[sm.stat0 + (at.hk * x.G + row - tok * x.G) * sm.hstep + tok];
   };
-  // The statistics of those rows, for the dK/dV pass too (part 0 writes them). A row
-  // without keys has LSE -inf; any finite value keeps its P at 0.
-  auto row_stats = [&](const XItem& at) __attribute__((always_inline)) {
+  // The statistics of those rows, for the dK/dV pass too (part 0 writes them), before
+  // they are turned: a lane has pieces of rows, and their sums pass through LDS. A
+  // row without keys has LSE -inf; any finite value keeps its P at 0.
+  auto row_stats = [&](const XItem& at, const Extra& ex, char* lds) __attribute__((always_inline)) {
+    const int ln = x_lane_again();
+    float* const piece = reinterpret_cast<float*>(lds) + ln;   // [row][CPR]
+#pragma unroll
+    for (int u = 0; u < KS; ++u) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += (float)ex.o[u][e] * (float)doop[u][e];
+      piece[64 * u] = sum;
+      pin_order();   // or all rows' fp32 values would be held at once
+    }
+    __builtin_amdgcn_wave_barrier();
+    const f32x4* const mine = reinterpret_cast<const f32x4*>(lds + (ln & 31) * CPR * 4 + (ln >> 5) * CPR * 2);
     float sum = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum += (float)orow[ks][e] * (float)doop[ks][e];
-    lse2 = lse == -INFINITY ? 0.f : lse * kLog2e;
+    for (int c = 0; c < CPR / 8; ++c) {
+      const f32x4 y = mine[c];
+      sum += (y[0] + y[1]) + (y[2] + y[3]);
+    }
+    lse2 = ex.lse == -INFINITY ? 0.f : ex.lse * kLog2e;
     ndl = -pair_sum(sum);
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
-    const int row = at.tile * 32 * NW + 32 * w + l32, tok = row_token(row, x.G);
-    if (at.part == 0 && g == 0 && row < sm.nq * x.G) {
+    const int row = at.tile * 32 * NW + 32 * w + (ln & 31), tok = row_token(row, x.G);
+    if (at.part == 0 && ln < 32 && row < sm.nq * x.G) {
       const int64_t stat = sm.stat0 + (at.hk * x.G + row - tok * x.G) * sm.hstep + tok;
       aux[stat] = lse2;
       aux[x.Tq * x.Hq + stat] = ndl;
@@ -109,8 +120,11 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
 
   // A tile as two 32-key halves: S^T and dP^T, dS^T, its exchange to the
   // 16x16 operand layout, and the half's dQ product. With `swap` the next item's
-  // rows take the place of this one's after the last score products.
-  auto step = [&](uint64_t bits, const char* kt_lds, const char* vt_lds, bool swap)
+  // rows take the place of this one's after the last score products. The next
+  // tile's loads (load(u), u < 2 IPW) stand between the first products.
+  using Load = TileLoad<DP, NW>;
+  auto step = [&](uint64_t bits, const char* kt_lds, const char* vt_lds, bool swap, Extra& ex, bool loads,
+                  auto load)
       __attribute__((always_inline)) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -119,28 +133,36 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       pin_value(ko);
       pin_value(kx);
       // S^T and dP^T in turn, operands read kAhead products before their use
-      constexpr int kAhead = DP == 64 ? 2 : 4;
+      constexpr int kAhead = 4, kPre = 4;
       bf16x8 op[kAhead];
       auto read_op = [&](int n) __attribute__((always_inline)) {
         return *reinterpret_cast<const bf16x8*>((n & 1 ? vt_lds : kt_lds) + (ko ^ (32 * (n >> 1))) + kt * 32 * ROWB);
       };
 #pragma unroll
       for (int n = 0; n < kAhead; ++n) op[n] = read_op(n);
-#pragma unroll
-      for (int n = 0; n < 2 * KS; ++n) {
+      pin_order();
+      auto product = [&](int n) __attribute__((always_inline)) {
         if (n & 1) dp = mfma32(op[n % kAhead], doop[n >> 1], dp);
         else s = mfma32(op[n % kAhead], qop[n >> 1], s);
         if (n + kAhead < 2 * KS) op[n % kAhead] = read_op(n + kAhead);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);   // DS read
+      };
+      if (kt == 0 && loads) {   // uniform
 #pragma unroll
-      for (int n = 0; n + kAhead < 2 * KS; ++n) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // MFMA
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // DS read
+        for (int n = 0; n < 2 * KS; ++n) {
+          product(n);
+#pragma unroll
+          for (int u = n * Load::IPW / KS; u < (n + 1) * Load::IPW / KS; ++u) load(u);
+          pin_order();
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < 2 * KS; ++n) {
+          product(n);
+          pin_order();
+        }
       }
-      __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
       const float l2 = lse2, nd = ndl;
-      if (kt == 1 && swap) load_rows(seq.cold.item(TileSeq::kAt));   // uniform
+      if (kt == 1 && swap) load_rows(seq.cold.item(TileSeq::kAt), ex);   // uniform
       if (bits != ~(uint64_t)0) {             // uniform
         const unsigned mine = (unsigned)(bits >> (32 * kt)) >> (4 * g);
 #pragma unroll
@@ -160,39 +182,44 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
         pq[0][v] = r[0];
         pq[1][v] = r[1];
       }
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
+      pin_order();
+      auto read_kt = [&](int dt) __attribute__((always_inline)) {
         const char* kbuf = kt_lds + 32 * kt * ROWB + (kx ^ (32 * dt));
         const s16x4 lo = lds_read_tr16(kbuf);
         const s16x4 hi = lds_read_tr16(kbuf + 16 * ROWB);
         const s16x8 k8 = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        const bf16x8 av = __builtin_bit_cast(bf16x8, k8);
-        dq[dt][0] = mfma16(av, __builtin_bit_cast(bf16x8, pq[0]), dq[dt][0]);
-        dq[dt][1] = mfma16(av, __builtin_bit_cast(bf16x8, pq[1]), dq[dt][1]);
+        return __builtin_bit_cast(bf16x8, k8);
+      };
+#pragma unroll
+      for (int dt = 0; dt < kPre; ++dt) op[dt] = read_kt(dt);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        dq[dt][0] = mfma16(op[dt % kPre], __builtin_bit_cast(bf16x8, pq[0]), dq[dt][0]);
+        dq[dt][1] = mfma16(op[dt % kPre], __builtin_bit_cast(bf16x8, pq[1]), dq[dt][1]);
+        if (dt + kPre < DT) op[dt % kPre] = read_kt(dt + kPre);
+        pin_order();
       }
     }
   };
-  auto finish = [&](const XItem& at) __attribute__((always_inline)) {
+  auto finish = [&](const XItem& at, char* lds0, char* lds1) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
     const int rows = sm.nq * x.G, r0 = at.tile * 32 * NW + 32 * w;
+    const float scale = x.scale;
+    if (!part) {
+      x_store_rows<DP>(x.dq, sm.q0, x.sdq, (int64_t)at.hk * x.G * x.D, r0, rows, x.G, x.D, lds0, lds1,
+                       [&](int dt, int qg) { return dq[dt][qg] * scale; });
+      return;
+    }
 #pragma unroll
     for (int qg = 0; qg < 2; ++qg) {
-      const int ro = r0 + 16 * qg + c16;
-      const XRow r = x_row(r0, ro, rows, x.G);
-      const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(
-          static_cast<__bf16*>(x.dq) + (sm.q0 + r.first) * x.sdq + (int64_t)at.hk * x.G * x.D, kXOut);
-      const int off = ro < rows ? ((r.tok - r.first) * x.sdq + r.head * x.D + 4 * gq) * 2 : kXOut;
-      float* const pp = part + ((at.part * x.Tq + sm.q0 + r.tok) * x.Hq + at.hk * x.G + r.head) * x.D + 4 * gq;
+      const int row = r0 + 16 * qg + c16, tok = row_token(row, x.G);
+      if (row >= rows) continue;
+      float* const pp =
+          part + ((at.part * x.Tq + sm.q0 + tok) * x.Hq + at.hk * x.G + row - tok * x.G) * x.D + 4 * gq;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const f32x4 y = dq[dt][qg] * a.scale;
-        if (!part)
-          x_store8(bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]}, rs,
-                   16 * dt + 4 * gq < x.D ? off + 32 * dt : kXOut);
-        else if (ro < rows && 16 * dt + 4 * gq < x.D)
-          *reinterpret_cast<f32x4*>(pp + 16 * dt) = y;
-      }
+      for (int dt = 0; dt < DT; ++dt)
+        if (16 * dt + 4 * gq < x.D) *reinterpret_cast<f32x4*>(pp + 16 * dt) = dq[dt][qg] * scale;
     }
   };
 
@@ -205,23 +232,37 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     bool changed;
     const bool more = seq.next(order, 32 * NW, changed);
     if (!have && !more) return false;
-    if (more) {
-      const int64_t key = seq.k0 + (int64_t)seq.tile * kXKeys;
-      const __amdgpu_buffer_rsrc_t rk = load_k.tile(static_cast<const __bf16*>(a.k) + key * a.sk + seq.hk * a.D, a.sk);
-      const __amdgpu_buffer_rsrc_t rv = load_v.tile(static_cast<const __bf16*>(a.v) + key * a.sv + seq.hk * a.D, a.sv);
-      load_k.masked(rk, a.sk, seq.bits, P ? k_lds0 : k_lds1, w, lane, a.D);
-      load_v.masked(rv, a.sv, seq.bits, P ? v_lds0 : v_lds1, w, lane, a.D);
+    char* const kn = P ? k_lds0 : k_lds1;
+    char* const vn = P ? v_lds0 : v_lds1;
+    const int64_t key = seq.k0 + (int64_t)seq.tile * kXKeys;
+    const __amdgpu_buffer_rsrc_t rk = load_k.tile(static_cast<const __bf16*>(a.k) + key * a.sk + seq.hk * a.D, a.sk);
+    const __amdgpu_buffer_rsrc_t rv = load_v.tile(static_cast<const __bf16*>(a.v) + key * a.sv + seq.hk * a.D, a.sv);
+    const bool all = more && seq.bits == ~(uint64_t)0;
+    if (more && !all) {
+      load_k.masked(rk, a.sk, seq.bits, kn, w, lane, a.D);
+      load_v.masked(rv, a.sv, seq.bits, vn, w, lane, a.D);
     }
     // before the first tile too, beside its loads: what it leaves is not used
-    step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more);
+    Extra ex;
+    step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, ex, all, [&](int u) __attribute__((always_inline)) {
+      if (u < Load::IPW) load_k.one(rk, a.sk, kn, w, u, a.D);
+      else load_v.one(rv, a.sv, vn, w, u - Load::IPW, a.D);
+    });
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (changed) {
-      // its stores end beside the next item's first tile
-      if (have) finish(seq.cold.item(TileSeq::kCur));
+      // through the wave's part of the consumed stage; the stores end beside the
+      // next item's first tile
+      char* const lds0 = (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
+      char* const lds1 = (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
+      if (have) finish(seq.cold.item(TileSeq::kCur), lds0, lds1);
       const XItem at = seq.cold.item(TileSeq::kAt);
       seq.cold.put(TileSeq::kCur, at);
-      if (more) row_stats(at);
+      if (more) {
+        row_stats(at, ex, lds0);
+        x_turn_rows<DP>(qop, lds0, lds1);
+        x_turn_rows<DP>(doop, lds0, lds1);
+      }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};
     }

@@ -53,18 +53,12 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
-  // Q operand (B of S^T = K Q^T): lane holds Q[row][16 ks + 8 g .. +7].
+  // Q operand (B of S^T = K Q^T), once turned: lane holds Q[row][16 ks + 8 g .. +7].
   bf16x8 qop[KS];
   auto load_rows = [&](const XItem& at) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
-    const int r0 = at.tile * 32 * NW + 32 * w;
-    const XRow r = x_row(r0, r0 + l32, sm.nq * x.G, x.G);
-    const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(
-        static_cast<const __bf16*>(x.q) + (sm.q0 + r.first) * x.sq + (int64_t)at.hk * x.G * x.D, kXOut);
-    const int off = ((r.tok - r.first) * x.sq + r.head * x.D + 8 * g) * 2;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qop[ks] = x_load16(rs, 16 * ks + 8 * g < x.D ? off + 32 * ks : kXOut);
+    x_load_rows<DP>(qop, x.q, sm.q0, x.sq, (int64_t)at.hk * x.G * x.D, at.tile * 32 * NW + 32 * w, sm.nq * x.G, x.G, x.D);
   };
   const TileLoad<DP, NW> load_k(lane, a.sk), load_v(lane, a.sv);
 
@@ -309,10 +303,12 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (changed) {
-      // its stores end beside the next item's first tile
-      if (have)
-        finish(seq.cold.item(TileSeq::kCur), (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024,
-               (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024);
+      // through the wave's part of the consumed stage; the stores end beside the
+      // next item's first tile
+      char* const lds0 = (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
+      char* const lds1 = (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
+      if (have) finish(seq.cold.item(TileSeq::kCur), lds0, lds1);
+      if (more) x_turn_rows<DP>(qop, lds0, lds1);
       seq.cold.put(TileSeq::kCur, seq.cold.item(TileSeq::kAt));
       m_run = l_run = 0.f;
       fresh = true;

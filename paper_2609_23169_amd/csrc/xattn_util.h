@@ -262,6 +262,16 @@ __device__ inline void x_store8(bf16x4 v, __amdgpu_buffer_rsrc_t rs, int off) { 
   __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), rs, off, 0, 0);
 }
 
+// The lane, read again where it is used: the offsets that work done once an item
+// forms from it would otherwise be kept in registers through the loop.
+__device__ inline int x_lane_again() {
+  int lane = threadIdx.x & 63;
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(lane));
+#endif
+  return lane;
+}
+
 // Stores a wave's 32 result rows, rounded to bf16, as whole rows: 16 bytes a lane,
 // a row's lanes side by side, where the accumulators' layout would write pieces of
 // 32 bytes. The rows pass through the wave's own part of a consumed stage (row
@@ -272,7 +282,7 @@ template <int DP, class Val>
 __device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t head0, int r0, int rows, int G, int D,
                                     char* lds0, char* lds1, Val val) {
   constexpr int CPR = DP / 8, RPI = 64 / CPR, DT = DP / 16;
-  const int lane = threadIdx.x & 63, c16 = lane & 15, gq = lane >> 4;
+  const int lane = x_lane_again(), c16 = lane & 15, gq = lane >> 4;
   const int first = __builtin_amdgcn_readfirstlane(row_token(min(r0, rows - 1), G));
   const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<__bf16*>(dst) + (tok0 + first) * stride + head0, kXOut);
 #pragma unroll
@@ -284,8 +294,8 @@ __device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t
       *reinterpret_cast<bf16x4*>(lds + lds_off<CPR>(c16, 2 * dt + (gq >> 1)) + 8 * (gq & 1)) =
           bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
     }
+    pin_order();
   }
-  __builtin_amdgcn_wave_barrier();
   const int c = lane % CPR;
 #pragma unroll
   for (int u = 0; u < 32 / RPI; ++u) {
@@ -294,6 +304,39 @@ __device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t
     x_store16(v, rs, row < rows && 8 * c < D ? ((tok - first) * stride + (row - tok * G) * D + 8 * c) * 2 : kXOut);
   }
   __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done before the next loads
+}
+
+// The way in: a wave's 32 operand rows r0 .. of `rows` (rows past the last repeat
+// it), loaded as whole rows, 16 bytes a lane, and then turned through the same part
+// of a stage into operands: x[ks] = columns 16 ks + 8 g .. of row l32. Loaded as
+// operands, an instruction would touch a line of every row.
+template <int DP>
+__device__ inline void x_load_rows(bf16x8 (&x)[DP / 16], const void* src, int64_t tok0, int stride, int64_t head0, int r0,
+                                   int rows, int G, int D) {
+  constexpr int CPR = DP / 8, RPI = 64 / CPR;
+  const int lane = x_lane_again(), c = lane % CPR;
+  const int first = __builtin_amdgcn_readfirstlane(row_token(min(r0, rows - 1), G));
+  const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<const __bf16*>(src) + (tok0 + first) * stride + head0, kXOut);
+#pragma unroll
+  for (int u = 0; u < DP / 16; ++u) {
+    const int row = min(r0 + u * RPI + lane / CPR, rows - 1), tok = row_token(row, G);
+    x[u] = x_load16(rs, 8 * c < D ? ((tok - first) * stride + (row - tok * G) * D + 8 * c) * 2 : kXOut);
+  }
+}
+template <int DP>
+__device__ inline void x_turn_rows(bf16x8 (&x)[DP / 16], char* lds0, char* lds1) {
+  constexpr int CPR = DP / 8, RPI = 64 / CPR;
+  const int lane = x_lane_again(), l32 = lane & 31, g = lane >> 5;
+#pragma unroll
+  for (int u = 0; u < DP / 16; ++u) {
+    const int r = u * RPI + lane / CPR;
+    *reinterpret_cast<bf16x8*>((r < 16 ? lds0 : lds1) + lds_off<CPR>(r & 15, lane % CPR)) = x[u];
+  }
+  pin_order();
+  const char* const from = l32 < 16 ? lds0 : lds1;
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) x[ks] = *reinterpret_cast<const bf16x8*>(from + lds_off<CPR>(l32 & 15, 2 * ks + g));
+  __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done before the next writes
 }
 
 // Direct loads of 64-row tiles into LDS by NW waves, in rows of DP elements:
