@@ -260,11 +260,10 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     if constexpr (SPLIT) {
 #pragma unroll
       for (int qg = 0; qg < 2; ++qg) {
-        const int ro = r0 + 16 * qg + c16;
-        if (ro >= rows) continue;
-        const XRow r = x_row(r0, ro, rows, x.G);
-        float* op = parts.o +
-                    (at.part * parts.stats + sm.stat0 + (at.hk * x.G + r.head) * sm.hstep + r.tok) * x.D + 4 * gq;
+        const int row = r0 + 16 * qg + c16, tok = row_token(row, x.G);
+        if (row >= rows) continue;
+        const int64_t stat = sm.stat0 + (at.hk * x.G + row - tok * x.G) * sm.hstep + tok;
+        float* op = parts.o + (at.part * parts.stats + stat) * x.D + 4 * gq;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
           if (16 * dt + 4 * gq < x.D) *reinterpret_cast<f32x4*>(op + 16 * dt) = oacc[dt][qg];
