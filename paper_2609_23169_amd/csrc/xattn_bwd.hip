@@ -424,23 +424,30 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
     auto advance = [&]() __attribute__((always_inline)) {
       if (++tt == ttiles) tt = 0, ++head;
     };
-    auto iter = [&](int i, auto par) __attribute__((always_inline)) {
+    auto iter = [&](int i, auto par, auto used) __attribute__((always_inline)) {
       constexpr int P = decltype(par)::value;
       advance();
       if (i + 1 < s_end) load_step(head, tt, P ? q_lds0 : q_lds1, P ? o_lds0 : o_lds1, P ? a_lds0 : a_lds1);
-      step(P ? q_lds1 : q_lds0, P ? o_lds1 : o_lds0, P ? a_lds1 : a_lds0);
+      if constexpr (decltype(used)::value) step(P ? q_lds1 : q_lds0, P ? o_lds1 : o_lds0, P ? a_lds1 : a_lds0);
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
     };
     load_step(head, tt, q_lds0, o_lds0, a_lds0);
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    int i = s_begin;
-    for (; i + 1 < s_end; i += 2) {
-      iter(i, std::integral_constant<int, 0>{});
-      iter(i + 1, std::integral_constant<int, 1>{});
-    }
-    if (i < s_end) iter(i, std::integral_constant<int, 0>{});
+    auto walk = [&](auto used) __attribute__((always_inline)) {
+      int i = s_begin;
+      for (; i + 1 < s_end; i += 2) {
+        iter(i, std::integral_constant<int, 0>{}, used);
+        iter(i + 1, std::integral_constant<int, 1>{}, used);
+      }
+      if (i < s_end) iter(i, std::integral_constant<int, 0>{}, used);
+    };
+    // a wave without keys in use loads its part of the steps and leaves the matrix
+    // cores to the others
+    const int mine = key0 + 32 * w + l32;
+    if (__ballot(mine < sm.nk && (!a.mask || a.mask[sm.k0 + mine]))) walk(std::true_type{});
+    else walk(std::false_type{});
   }
 
 #pragma unroll
@@ -513,14 +520,14 @@ int64_t dq_groups(const XArgs& a) {
 int64_t dkdv_groups(const XArgs& a) {
   return (int64_t)a.B * a.Hk * (((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys);
 }
-// Workgroups that fit at once: two a CU. Splits below four tiles are not worth their join.
+// As many parts as fit the chip at once. Splits below four tiles are not worth their join.
 int dq_splits(const XArgs& a) {
   const int64_t groups = dq_groups(a), tiles = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
-  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(512 / groups, tiles / 4));
+  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), dq_waves(a)) / groups, tiles / 4));
 }
 int dkdv_splits(const XArgs& a) {
   const int64_t groups = dkdv_groups(a), steps = (int64_t)a.G * (((int64_t)a.Nq + kRowTile - 1) / kRowTile);
-  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(512 / groups, steps / 8));
+  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), 4) / groups, steps / 8));
 }
 size_t aux_bytes(const XArgs& a) { return ((size_t)a.Tq * a.Hq * 2 * sizeof(float) + 255) / 256 * 256; }
 size_t dq_part(const XArgs& a) {
@@ -532,16 +539,12 @@ size_t dkdv_part(const XArgs& a) {
   return n > 1 ? (size_t)n * a.Tk * a.Hk * a.D * 2 * sizeof(float) : 0;
 }
 
-// Workgroups that fill the chip, as in the forward.
-template <int DP, int NW>
-constexpr int64_t kResident = 256 * (DP == 128 ? 2 : NW == 4 ? 3 : 4);
-
 template <int DP, int NW>
 void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
   const bool by_xcd = (int64_t)a.B * a.Nk * a.D * 4 <= kXcdHeadBytes;
   const int64_t items = dq_groups(a) * splits;
-  const dim3 grid((unsigned)(std::min<int64_t>(items, kResident<DP, NW>) + 7) / 8 * 8);
+  const dim3 grid((unsigned)(std::min<int64_t>(items, x_resident(DP, NW)) + 7) / 8 * 8);
   TraceScope ts_(s, "xattn_dq", DP, NW);
   hipLaunchKernelGGL((xattn_dq_kernel<DP, NW>), grid, dim3(64 * NW), 0, s, a, aux, order, by_xcd, part);
 }

@@ -402,17 +402,11 @@ int64_t fwd_groups(const XArgs& a) {
 }
 int64_t stats_of(const XArgs& a) { return a.Tq * a.Hq; }
 
-// Workgroups that a grid needs to fill the chip: those that fit 256 CUs at once,
-// by LDS (64 KB at 128 columns, 32 KB at 64) and by registers (four waves of 128
-// columns or eight to twelve of 64 on a CU's four SIMDs).
-template <int DP, int NW>
-constexpr int64_t kResident = 256 * (DP == 128 ? 2 : NW == 4 ? 3 : 4);
-
 template <int DP, int NW>
 void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
   const int64_t items = fwd_groups(a) * splits;
-  const dim3 grid((unsigned)(std::min<int64_t>(items, kResident<DP, NW>) + 7) / 8 * 8);
+  const dim3 grid((unsigned)(std::min<int64_t>(items, x_resident(DP, NW)) + 7) / 8 * 8);
   const bool by_xcd = (int64_t)a.B * a.Nk * a.D * 4 <= kXcdHeadBytes;
   TraceScope ts_(s, splits > 1 ? "xattn_fwd_split" : "xattn_fwd", DP, NW);
   if (splits > 1)
@@ -433,7 +427,7 @@ void launch_join(const XArgs& a, int splits, const Parts& parts, hipStream_t s) 
 int xattn_fwd_splits(const XArgs& a) {
   const int64_t groups = fwd_groups(a), tiles = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
   if (groups == 0) return 1;
-  return (int)std::max<int64_t>(1, std::min(512 / groups, tiles / 4));
+  return (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), fwd_waves(a)) / groups, tiles / 4));
 }
 size_t xattn_fwd_workspace(const XArgs& a) {
   const int splits = xattn_fwd_splits(a);

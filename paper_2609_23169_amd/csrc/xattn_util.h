@@ -24,18 +24,24 @@ __device__ inline const XArgs* x_args_again() {
 #endif
 }
 
-// The work items of a persistent workgroup: first, first + step, ... below end.
-// Each XCD (workgroups go to the eight in turn) takes one run of the items, its
-// workgroups in turn, so that they share keys in their L2; with by_xcd false all
-// workgroups take the items in turn. The grid is a multiple of 8 with by_xcd.
+// The work items of a persistent workgroup: first, then `step` and `turn` - `step`
+// further in turn, below end. Each XCD (workgroups go to the eight in turn) takes
+// one run of the items, its n workgroups n items a turn, so that they share keys in
+// their L2; with by_xcd false all workgroups share one run. Every other turn goes
+// backwards: a workgroup would otherwise meet the same sample whenever the samples
+// divide n, the longest each time. The grid is a multiple of 8 with by_xcd.
 struct XItems {
-  unsigned first, step, end;
+  unsigned first, step, turn, end;
 };
 __device__ inline XItems x_items(unsigned total, bool by_xcd) {
   const unsigned wg = blockIdx.x;
-  if (!by_xcd) return XItems{wg, gridDim.x, total};
-  const unsigned x = wg & 7, q = total >> 3, r = total & 7, start = x * q + min(x, r);
-  return XItems{start + (wg >> 3), gridDim.x >> 3, start + q + (x < r ? 1 : 0)};
+  unsigned at = wg, n = gridDim.x, start = 0, end = total;
+  if (by_xcd) {
+    const unsigned x = wg & 7, q = total >> 3, r = total & 7;
+    at = wg >> 3, n >>= 3;
+    start = x * q + min(x, r), end = start + q + (x < r ? 1 : 0);
+  }
+  return XItems{start + at, 2 * (n - at) - 1, 2 * n, end};
 }
 // How item numbers are read: `heads` key heads of a group fastest (their rows lie
 // side by side), then samples, whose lengths may differ, so that every run holds
@@ -46,6 +52,11 @@ struct XOrder {
 // Heads of a group: an eighth of them, so that each XCD has a group of its own
 // and the runs are alike whatever the samples' lengths.
 inline unsigned head_group(const XArgs& a) { return a.Hk % 8 == 0 ? (unsigned)a.Hk / 8 : 1; }
+// Workgroups of nw waves that fit 256 CUs at once, by LDS (64 KB at 128 columns, 32
+// to 36 at 64) and by registers (four waves of 128 columns or eight to twelve of 64
+// on a CU's four SIMDs): what a grid needs to fill the chip.
+constexpr int64_t x_resident(int DP, int nw) { return 256 * (DP == 128 ? 2 : nw == 4 ? 3 : 4); }
+inline int x_padded(const XArgs& a) { return a.D <= 64 ? 64 : 128; }
 struct XItem {
   int b, tile, part, hk;
 };
@@ -193,7 +204,8 @@ struct TileSeq {
   __device__ inline void begin(const XItems& i) {
     cold.put(4 * kItems, i.first);
     cold.put(4 * kItems + 1, i.step);
-    cold.put(4 * kItems + 2, i.end);
+    cold.put(4 * kItems + 2, i.turn);
+    cold.put(4 * kItems + 3, i.end);
     tiles.open(nullptr, 0, 0, 0);
     tile = hk = 0;
     k0 = 0;
@@ -212,11 +224,13 @@ struct TileSeq {
       changed = true;
       bool found = false;
       unsigned it = cold.get(4 * kItems);
-      const unsigned step = cold.get(4 * kItems + 1), end = cold.get(4 * kItems + 2);
+      unsigned step = cold.get(4 * kItems + 1);
+      const unsigned turn = cold.get(4 * kItems + 2), end = cold.get(4 * kItems + 3);
       while (it < end && !found) {
         const XArgs& x = *x_args_again();
         const XItem at = x_item(it, (unsigned)x.B, order);
         it += step;
+        step = turn - step;
         const XSample sm = x_sample(x, at.b);
         const int n = (sm.nk + kXKeys - 1) / kXKeys;
         int t0 = 0, t1 = n;
@@ -232,6 +246,7 @@ struct TileSeq {
         found = at.tile * rows_per_item < sm.nq * x.G;
       }
       cold.put(4 * kItems, it);
+      cold.put(4 * kItems + 1, step);
       if (!found) return false;
       fresh = true;
     }
