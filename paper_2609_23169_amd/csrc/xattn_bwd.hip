@@ -162,7 +162,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
         }
       }
       const float l2 = lse2, nd = ndl;
-      if (kt == 1 && swap) load_rows(seq.cold.item(TileSeq::kAt), ex);   // uniform
+      if (kt == 1 && swap) load_rows(seq.item(seq.at, order), ex);   // uniform
       if (bits != ~(uint64_t)0) {             // uniform
         const unsigned mine = (unsigned)(bits >> (32 * kt)) >> (4 * g);
 #pragma unroll
@@ -255,9 +255,9 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       // next item's first tile
       char* const lds0 = (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
       char* const lds1 = (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
-      if (have) finish(seq.cold.item(TileSeq::kCur), lds0, lds1);
-      const XItem at = seq.cold.item(TileSeq::kAt);
-      seq.cold.put(TileSeq::kCur, at);
+      if (have) finish(seq.item(seq.cur, order), lds0, lds1);
+      const XItem at = seq.item(seq.at, order);
+      seq.cur = seq.at;
       if (more) {
         row_stats(at, ex, lds0);
         x_turn_rows<DP>(qop, lds0, lds1);

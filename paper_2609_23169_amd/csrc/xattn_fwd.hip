@@ -212,7 +212,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       }
       pin_order();
     }
-    if (swap) load_rows(seq.cold.item(TileSeq::kAt));   // uniform
+    if (swap) load_rows(seq.item(seq.at, order));   // uniform
     settle(0);
     prepare(1);
     pin_order();
@@ -306,9 +306,9 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       // next item's first tile
       char* const lds0 = (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
       char* const lds1 = (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
-      if (have) finish(seq.cold.item(TileSeq::kCur), lds0, lds1);
+      if (have) finish(seq.item(seq.cur, order), lds0, lds1);
       if (more) x_turn_rows<DP>(qop, lds0, lds1);
-      seq.cold.put(TileSeq::kCur, seq.cold.item(TileSeq::kAt));
+      seq.cur = seq.at;
       m_run = l_run = 0.f;
       fresh = true;
 #pragma unroll

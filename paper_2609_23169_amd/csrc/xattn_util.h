@@ -24,6 +24,16 @@ __device__ inline const XArgs* x_args_again() {
 #endif
 }
 
+// The lane, read again where it is used: the offsets that work done once an item
+// forms from it would otherwise be kept in registers through the loop.
+__device__ inline int x_lane_again() {
+  int lane = threadIdx.x & 63;
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(lane));
+#endif
+  return lane;
+}
+
 // The work items of a persistent workgroup: first, then `step` and `turn` - `step`
 // further in turn, below end. Each XCD (workgroups go to the eight in turn) takes
 // one run of the items, its n workgroups n items a turn, so that they share keys in
@@ -64,23 +74,6 @@ __device__ inline XItem x_item(unsigned it, unsigned B, const XOrder& o) {
   const unsigned r = it / o.heads, s = r / B, t = s / o.tiles, u = t / o.splits;
   return XItem{(int)(r - s * B), (int)(s - t * o.tiles), (int)(t - u * o.splits), (int)(u * o.heads + it - r * o.heads)};
 }
-
-// Uniform values that a change of item needs, in the lanes of one vector register:
-// the scalar registers are left to the loop over the tiles.
-struct ColdItems {
-  unsigned v = 0;
-  __device__ inline void put(int i, unsigned x) { v = (int)(threadIdx.x & 63) == i ? x : v; }
-  __device__ inline unsigned get(int i) const { return __builtin_amdgcn_readlane(v, i); }
-  __device__ inline void put(int slot, const XItem& x) {
-    put(4 * slot, (unsigned)x.b);
-    put(4 * slot + 1, (unsigned)x.tile);
-    put(4 * slot + 2, (unsigned)x.part);
-    put(4 * slot + 3, (unsigned)x.hk);
-  }
-  __device__ inline XItem item(int slot) const {
-    return XItem{(int)get(4 * slot), (int)get(4 * slot + 1), (int)get(4 * slot + 2), (int)get(4 * slot + 3)};
-  }
-};
 
 // The key tiles of one sample that hold a key in use, and which keys of each:
 // 64 tiles at a time, one a lane, as 64-bit masks, so that a step to the next
@@ -188,29 +181,65 @@ __device__ inline bool in_sample(const int32_t* __restrict__ cu, int64_t T, int 
   return false;
 }
 
-// The tiles of a persistent workgroup's items as one sequence. The code of a change
-// of item stands once in the loop: an item whose keys are not in use yields one
-// tile without keys (bits 0), so that it is finished like the others.
+// The tiles of a persistent workgroup's items as one sequence. The items are worked
+// out kTurns at a time, one a lane, so that a change of item costs some readlanes in
+// place of three divisions, and the scalar registers are left to the loop over the
+// tiles. The code of a change stands once in the loop: an item whose keys are not in
+// use yields one tile without keys (bits 0), so that it is finished like the others.
 struct TileSeq {
+  static constexpr int kTurns = 62;             // even: every group begins with a forward turn
+  static constexpr int kKept = 63;              // the lane that keeps an item over the groups
   KeyTiles tiles;
-  ColdItems cold;     // slots kAt (the item of the last tile given), kItems, and the caller's
-  static constexpr int kAt = 0, kItems = 1, kCur = 2;
+  int b, rtile, hkpart;                         // a lane's item: sample, tile of rows, key head and part
+  unsigned first, step, turn, end;              // the next group's items (XItems)
+  uint64_t todo;                                // items of the group not begun
+  int at, cur;                                  // lanes of the item of the last tile given, and of the caller's
   int tile;
   uint64_t bits;
-  bool fresh;         // that item has given no tile yet
-  int64_t k0;         // its sample's first key
-  int hk;             // its key head
+  bool fresh;                                   // that item has given no tile yet
+  int64_t k0;                                   // its sample's first key
+  int hk;                                       // its key head
 
   __device__ inline void begin(const XItems& i) {
-    cold.put(4 * kItems, i.first);
-    cold.put(4 * kItems + 1, i.step);
-    cold.put(4 * kItems + 2, i.turn);
-    cold.put(4 * kItems + 3, i.end);
+    first = i.first, step = i.step, turn = i.turn, end = i.end;
     tiles.open(nullptr, 0, 0, 0);
-    tile = hk = 0;
+    tile = hk = b = rtile = hkpart = 0;
     k0 = 0;
-    bits = 0;
+    bits = todo = 0;
+    at = cur = kKept;
     fresh = false;
+  }
+  // Item of lane i.
+  __device__ inline XItem item(int i, const XOrder& order) const {
+    const int hp = __builtin_amdgcn_readlane(hkpart, i);
+    return XItem{__builtin_amdgcn_readlane(b, i), __builtin_amdgcn_readlane(rtile, i),
+                 order.splits > 1 ? hp >> 16 : 0, order.splits > 1 ? hp & 0xffff : hp};
+  }
+  // The next group of items, those with rows; false at the end. The caller's item
+  // moves to the lane that keeps it.
+  __device__ inline bool group(const XOrder& order, int rows_per_item) {
+    const XArgs& x = *x_args_again();
+    const int lane = x_lane_again();
+    const int cb = __builtin_amdgcn_readlane(b, cur), ct = __builtin_amdgcn_readlane(rtile, cur),
+              ch = __builtin_amdgcn_readlane(hkpart, cur);
+    while (first < end) {
+      cur = at = kKept;
+      const unsigned it = first + (lane >> 1) * turn + (lane & 1 ? step : 0);
+      const bool in = lane < kTurns && it < end;
+      const XItem m = x_item(in ? it : 0, (unsigned)x.B, order);
+      int nq = x.Nq;
+      if (x.cuq) {   // as x_sample
+        const int64_t q0 = min(max((int64_t)x.cuq[m.b], (int64_t)0), x.Tq);
+        nq = (int)min(min(max((int64_t)x.cuq[m.b + 1], q0), x.Tq) - q0, (int64_t)x.Nq);
+      }
+      b = lane == kKept ? cb : m.b;
+      rtile = lane == kKept ? ct : m.tile;
+      hkpart = lane == kKept ? ch : order.splits > 1 ? m.hk | m.part << 16 : m.hk;
+      todo = __ballot(in && (int64_t)m.tile * rows_per_item < (int64_t)nq * x.G);
+      first += kTurns / 2 * turn;
+      if (todo) return true;
+    }
+    return false;
   }
   // The next tile; false at the end. changed: it is another item's than the one before.
   __device__ inline bool next(const XOrder& order, int rows_per_item, bool& changed) {
@@ -222,32 +251,22 @@ struct TileSeq {
         break;
       }
       changed = true;
-      bool found = false;
-      unsigned it = cold.get(4 * kItems);
-      unsigned step = cold.get(4 * kItems + 1);
-      const unsigned turn = cold.get(4 * kItems + 2), end = cold.get(4 * kItems + 3);
-      while (it < end && !found) {
-        const XArgs& x = *x_args_again();
-        const XItem at = x_item(it, (unsigned)x.B, order);
-        it += step;
-        step = turn - step;
-        const XSample sm = x_sample(x, at.b);
-        const int n = (sm.nk + kXKeys - 1) / kXKeys;
-        int t0 = 0, t1 = n;
-        if (order.splits > 1) {
-          const int per = (n + (int)order.splits - 1) / (int)order.splits;
-          t0 = min(at.part * per, n);
-          t1 = min(t0 + per, n);
-        }
-        tiles.open(x.mask ? x.mask + sm.k0 : nullptr, sm.nk, t0, t1);
-        k0 = sm.k0;
-        hk = at.hk;
-        cold.put(kAt, at);
-        found = at.tile * rows_per_item < sm.nq * x.G;
+      if (todo == 0 && !group(order, rows_per_item)) return false;
+      at = __builtin_ctzll(todo);
+      todo &= todo - 1;
+      const XItem m = item(at, order);
+      const XArgs& x = *x_args_again();
+      const XSample sm = x_sample(x, m.b);
+      const int n = (sm.nk + kXKeys - 1) / kXKeys;
+      int t0 = 0, t1 = n;
+      if (order.splits > 1) {
+        const int per = (n + (int)order.splits - 1) / (int)order.splits;
+        t0 = min(m.part * per, n);
+        t1 = min(t0 + per, n);
       }
-      cold.put(4 * kItems, it);
-      cold.put(4 * kItems + 1, step);
-      if (!found) return false;
+      tiles.open(x.mask ? x.mask + sm.k0 : nullptr, sm.nk, t0, t1);
+      k0 = sm.k0;
+      hk = m.hk;
       fresh = true;
     }
     fresh = false;
@@ -266,20 +285,44 @@ __device__ inline void x_store16(bf16x8 v, __amdgpu_buffer_rsrc_t rs, int off) {
   __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, off, 0, kXStream);
 }
 
-// The lane, read again where it is used: the offsets that work done once an item
-// forms from it would otherwise be kept in registers through the loop.
-__device__ inline int x_lane_again() {
-  int lane = threadIdx.x & 63;
-#if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("" : "+v"(lane));
-#endif
-  return lane;
-}
+// Byte offsets of a wave's rows r0 + lane / CPR + u RPI, u = 0 .., at the lane's 16-byte
+// column: row r is token r / G and head r % G, which the step of RPI rows moves on
+// without another division. Offsets count from the first row's token (32 rows stay
+// below kXOut); rows from `rows` on and columns past D give kXOut, or with
+// `repeat` the last row.
+template <int DP>
+struct XRows {
+  static constexpr int CPR = DP / 8, RPI = 64 / CPR, N = DP / 16;   // N instructions of RPI rows
+  int off[N];
+  int first;   // that token, uniform
+
+  __device__ inline XRows(int lane, int r0, int rows, int G, int D, int stride, bool repeat) {
+    const int c = 8 * (lane % CPR), last = rows - 1, row0 = r0 + lane / CPR;
+    first = min(r0, last);
+    int tok = row0, head = 0, dtok = RPI, dhead = 0, ltok = last, lhead = 0;
+    if (G != 1) {   // uniform
+      first = (int)((unsigned)first / (unsigned)G);
+      ltok = (int)((unsigned)last / (unsigned)G), lhead = last - ltok * G;
+      dtok = RPI / G, dhead = RPI - dtok * G;
+      tok = (int)((unsigned)row0 / (unsigned)G), head = row0 - tok * G;
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    const int past = repeat ? ((ltok - first) * stride + lhead * D + c) * 2 : kXOut;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int x = ((tok - first) * stride + head * D + c) * 2;
+      off[u] = c >= D ? kXOut : row0 + u * RPI < rows ? x : past;
+      tok += dtok, head += dhead;
+      const bool wrap = head >= G;
+      tok += wrap ? 1 : 0, head -= wrap ? G : 0;
+    }
+  }
+};
 
 // Stores a wave's 32 result rows, rounded to bf16, as whole rows: 16 bytes a lane,
 // a row's lanes side by side, where the accumulators' layout would write pieces of
 // 32 bytes. The rows pass through the wave's own part of a consumed stage (row
-// group qg through `lds[qg]`, 16 rows, swizzled as the tiles), which only the
+// group qg through lds0 or lds1, 16 rows, swizzled as the tiles), which only the
 // wave's own next loads write. val(dt, qg): columns 16 dt + 4 gq + (0..3) of row
 // 16 qg + c16 of the rows r0 .. of `rows`.
 template <int DP, class Val>
@@ -287,8 +330,6 @@ __device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t
                                     char* lds0, char* lds1, Val val) {
   constexpr int CPR = DP / 8, RPI = 64 / CPR, DT = DP / 16;
   const int lane = x_lane_again(), c16 = lane & 15, gq = lane >> 4;
-  const int first = __builtin_amdgcn_readfirstlane(row_token(min(r0, rows - 1), G));
-  const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<__bf16*>(dst) + (tok0 + first) * stride + head0, kXOut);
 #pragma unroll
   for (int qg = 0; qg < 2; ++qg) {
     char* const lds = qg ? lds1 : lds0;
@@ -300,14 +341,17 @@ __device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t
     }
     pin_order();
   }
-  const int c = lane % CPR;
+  bf16x8 v[DP / 16];
 #pragma unroll
-  for (int u = 0; u < 32 / RPI; ++u) {
-    const int r = u * RPI + lane / CPR, row = r0 + r, tok = row_token(row, G);
-    const bf16x8 v = *reinterpret_cast<const bf16x8*>((r < 16 ? lds0 : lds1) + lds_off<CPR>(r & 15, c));
-    x_store16(v, rs, row < rows && 8 * c < D ? ((tok - first) * stride + (row - tok * G) * D + 8 * c) * 2 : kXOut);
+  for (int u = 0; u < DP / 16; ++u) {   // a row group's instructions lie on one side
+    const int r = u * RPI + lane / CPR;
+    v[u] = *reinterpret_cast<const bf16x8*>((u < DP / 32 ? lds0 : lds1) + lds_off<CPR>(r & 15, lane % CPR));
   }
+  const XRows<DP> at(lane, r0, rows, G, D, stride, false);   // beside the reads
+  const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<__bf16*>(dst) + (tok0 + at.first) * stride + head0, kXOut);
   __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done before the next loads
+#pragma unroll
+  for (int u = 0; u < DP / 16; ++u) x_store16(v[u], rs, at.off[u]);
 }
 
 // The way in: a wave's 32 operand rows r0 .. of `rows` (rows past the last repeat
@@ -317,15 +361,11 @@ __device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t
 template <int DP>
 __device__ inline void x_load_rows(bf16x8 (&x)[DP / 16], const void* src, int64_t tok0, int stride, int64_t head0, int r0,
                                    int rows, int G, int D) {
-  constexpr int CPR = DP / 8, RPI = 64 / CPR;
-  const int lane = x_lane_again(), c = lane % CPR;
-  const int first = __builtin_amdgcn_readfirstlane(row_token(min(r0, rows - 1), G));
-  const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<const __bf16*>(src) + (tok0 + first) * stride + head0, kXOut);
+  const XRows<DP> at(x_lane_again(), r0, rows, G, D, stride, true);
+  const __amdgpu_buffer_rsrc_t rs =
+      buffer_rsrc(static_cast<const __bf16*>(src) + (tok0 + at.first) * stride + head0, kXOut);
 #pragma unroll
-  for (int u = 0; u < DP / 16; ++u) {
-    const int row = min(r0 + u * RPI + lane / CPR, rows - 1), tok = row_token(row, G);
-    x[u] = x_load16(rs, 8 * c < D ? ((tok - first) * stride + (row - tok * G) * D + 8 * c) * 2 : kXOut);
-  }
+  for (int u = 0; u < DP / 16; ++u) x[u] = x_load16(rs, at.off[u]);
 }
 template <int DP>
 __device__ inline void x_turn_rows(bf16x8 (&x)[DP / 16], char* lds0, char* lds1) {
@@ -334,7 +374,7 @@ __device__ inline void x_turn_rows(bf16x8 (&x)[DP / 16], char* lds0, char* lds1)
 #pragma unroll
   for (int u = 0; u < DP / 16; ++u) {
     const int r = u * RPI + lane / CPR;
-    *reinterpret_cast<bf16x8*>((r < 16 ? lds0 : lds1) + lds_off<CPR>(r & 15, lane % CPR)) = x[u];
+    *reinterpret_cast<bf16x8*>((u < DP / 32 ? lds0 : lds1) + lds_off<CPR>(r & 15, lane % CPR)) = x[u];
   }
   pin_order();
   const char* const from = l32 < 16 ? lds0 : lds1;

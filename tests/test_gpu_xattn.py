@@ -352,6 +352,64 @@ def test_varlen_of_equal_lengths_equals_the_uniform_call():
         assert torch.equal(x.view(y.shape), y)
 
 
+@pytest.mark.parametrize("B,Hq,Hk,D", [(9000, 8, 8, 16), (2500, 8, 2, 128)])
+def test_many_short_samples(B, Hq, Hk, D):
+    """More items a workgroup than one group of its item numbers holds. Bounds by
+    element: P, dS, O (which forms delta) and every result are off by half a step of
+    bf16 each, u = 2^-8; fp32's own errors are below 2^-16 of the same sums."""
+    g = torch.Generator().manual_seed(B)
+    lq, lk = (torch.randint(0, n, (B,), generator=g) for n in (4, 5))
+    eq, ek = ([0] + x.cumsum(0).tolist() for x in (lq, lk))
+    q, do = (torch.randn(eq[-1], Hq, D, generator=g).bfloat16() for _ in range(2))
+    k, v = (torch.randn(ek[-1], Hk, D, generator=g).bfloat16() for _ in range(2))
+    at = (torch.tensor(eq, dtype=torch.int32, device=DEV), 3, torch.tensor(ek, dtype=torch.int32, device=DEV), 4)
+    scale = D ** -0.5
+    dev = [x.to(DEV) for x in (q, k, v, do)]
+    o, lse = ut.xattn_fwd_varlen(*dev[:3], *at, scale)
+    dq, dk, dv = ut.xattn_bwd_varlen(*dev[:3], o, dev[3], lse, *at, scale)
+
+    def pad(x, ends, n):   # [B, H, n, D] in fp64, heads repeated to Hq
+        out = torch.zeros(B, n, *x.shape[1:], dtype=torch.float64)
+        for i in range(n):
+            has = torch.tensor(ends[1:]) - torch.tensor(ends[:-1]) > i
+            out[has, i] = x.double()[torch.tensor(ends[:-1])[has] + i]
+        return out.permute(0, 2, 1, 3).repeat_interleave(Hq // x.shape[1], 1)
+
+    def flat(x, ends, H):   # back to [T, H, D], shared heads summed
+        x = x.unflatten(1, (H, -1)).sum(2).permute(0, 2, 1, 3)
+        n = torch.tensor(ends[1:]) - torch.tensor(ends[:-1])
+        return x[torch.arange(x.shape[1]) < n[:, None]]
+
+    Q, K, V, DO = pad(q, eq, 3), pad(k, ek, 4), pad(v, ek, 4), pad(do, eq, 3)
+    used = (torch.arange(4) < lk[:, None])[:, None, None] & (torch.arange(3) < lq[:, None])[:, None, :, None]
+    S = (Q @ K.mT * scale).masked_fill(~used, -math.inf)
+    top = S.amax(-1, keepdim=True).clamp_min(-1e300)
+    E = (S - top).exp()
+    L = E.sum(-1, keepdim=True)
+    P = E / L.clamp_min(1e-300)
+    u, f = 2.0 ** -8, 1 + 2.0 ** -8
+    O, aO = P @ V, P @ V.abs()
+    dP = DO @ V.mT
+    dS = P * (dP - (DO * O).sum(-1, keepdim=True))
+    # the error of dS: its own rounding, and delta's through O (twice rounded)
+    eS = u * dS.abs() + P * (2 * u * f) * (DO.abs() * aO).sum(-1, keepdim=True)
+    want = {"o": (o, flat(O, eq, Hq), flat(2 * u * f * aO, eq, Hq)),
+            "dq": (dq, flat(scale * (dS @ K), eq, Hq), flat(scale * f * (eS @ K.abs()), eq, Hq)),
+            "dk": (dk, flat(scale * (dS.mT @ Q), ek, Hk), flat(scale * f * (eS.mT @ Q.abs()), ek, Hk)),
+            "dv": (dv, flat(P.mT @ DO, ek, Hk), flat(u * f * (P.mT @ DO.abs()), ek, Hk))}
+    for name, (got, ref, bound) in want.items():
+        got = got.cpu().double()
+        bound = bound + u * ref.abs() + 2.0 ** -16 * (1 + bound / u)
+        worst = ((got - ref).abs() / bound).max().item()
+        assert worst <= 1, (name, worst)
+    want_lse = (top + L.clamp_min(1e-300).log()).squeeze(-1).masked_fill(~used.any(-1), -math.inf)
+    want_lse = want_lse.permute(0, 2, 1)[torch.arange(3) < lq[:, None]].T   # [Hq, T]
+    got = lse.cpu().double()
+    assert torch.equal(got == -math.inf, want_lse == -math.inf)
+    live = got != -math.inf
+    assert (got - want_lse)[live].abs().max() < 1e-4
+
+
 def test_bad_offsets_reach_nothing_outside():
     """Offsets outside the tensors are clamped (and refused in validate mode)."""
     q, k, v, do, _ = packed(23, [50, 50], [40, 40], 2, 2, 64)
