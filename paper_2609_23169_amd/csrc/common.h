@@ -226,9 +226,15 @@ size_t xattn_fwd_workspace(const XArgs& a);
 hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s);
 size_t xattn_bwd_workspace(const XArgs& a);
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s);
-// Packed rows x (and y, unless null) of `width` elements at and past the last
-// sample's end to 0, and lse [H, T] there (unless null) to -inf.
-hipError_t launch_xattn_clear(const int32_t* cu, int B, int64_t T, int width, void* x, int sx, void* y, int sy,
-                              float* lse, int H, hipStream_t s);
+// n <= 3 tensors' packed rows at and past the last sample's end to 0, and lse
+// [H, T] there (unless null; of the first's samples) to -inf.
+struct XClear {
+  const int32_t* cu;   // [B + 1]
+  int64_t T;           // tokens
+  int width;           // elements of a token
+  void* x;
+  int stride;
+};
+hipError_t launch_xattn_clear(const XClear* t, int n, int B, float* lse, int H, hipStream_t s);
 
 }  // namespace ut

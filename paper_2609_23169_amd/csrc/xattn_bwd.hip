@@ -493,20 +493,20 @@ __global__ __launch_bounds__(256) void xattn_sum_kernel(const float* __restrict_
       bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
 }
 
-// Rows at and past the last sample's end become 0 (statistics: -inf).
-__global__ __launch_bounds__(256) void xattn_clear_kernel(const int32_t* __restrict__ cu, int B, int64_t T, int width,
-                                                          __bf16* __restrict__ x, int sx, __bf16* __restrict__ y, int sy,
+// Rows at and past the last sample's end become 0 (statistics: -inf), of up to three
+// tensors in one launch.
+__global__ __launch_bounds__(256) void xattn_clear_kernel(const XClear t0, const XClear t1, const XClear t2, int B,
                                                           float* __restrict__ lse, int H) {
-  const int64_t end = min(max((int64_t)cu[B], (int64_t)0), T);
+  const XClear t = blockIdx.y == 0 ? t0 : blockIdx.y == 1 ? t1 : t2;
+  const int64_t end = min(max((int64_t)t.cu[B], (int64_t)0), t.T);
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
-  const int per = width / 8;
-  for (int64_t i = end * per + at; i < T * per; i += step) {
+  const int per = t.width / 8;
+  for (int64_t i = end * per + at; i < t.T * per; i += step) {
     const int64_t tok = i / per;
-    *reinterpret_cast<bf16x8*>(x + tok * sx + 8 * (i - tok * per)) = bf16x8{};
-    if (y) *reinterpret_cast<bf16x8*>(y + tok * sy + 8 * (i - tok * per)) = bf16x8{};
+    *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(t.x) + tok * t.stride + 8 * (i - tok * per)) = bf16x8{};
   }
-  if (lse)
-    for (int64_t i = at; i < (T - end) * H; i += step) lse[i / (T - end) * T + end + i % (T - end)] = -INFINITY;
+  if (lse && blockIdx.y == 0)
+    for (int64_t i = at; i < (t.T - end) * H; i += step) lse[i / (t.T - end) * t.T + end + i % (t.T - end)] = -INFINITY;
 }
 
 int dq_waves(const XArgs& a) {
@@ -593,11 +593,10 @@ hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_xattn_clear(const int32_t* cu, int B, int64_t T, int width, void* x, int sx, void* y, int sy,
-                              float* lse, int H, hipStream_t s) {
+hipError_t launch_xattn_clear(const XClear* t, int n, int B, float* lse, int H, hipStream_t s) {
   TraceScope ts_(s, "xattn_clear");
-  hipLaunchKernelGGL(xattn_clear_kernel, dim3(256), dim3(256), 0, s, cu, B, T, width, static_cast<__bf16*>(x), sx,
-                     static_cast<__bf16*>(y), sy, lse, H);
+  hipLaunchKernelGGL(xattn_clear_kernel, dim3(256, (unsigned)n), dim3(256), 0, s, t[0], t[n > 1 ? 1 : 0], t[n > 2 ? 2 : 0], B,
+                     lse, H);
   return hipGetLastError();
 }
 
