@@ -341,14 +341,9 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
       }
     }
     const char* const vrow = vblk_lds + 32 * w * ROWB;   // this wave's keys
-    int roff[KS], rtr[DT];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) roff[ks] = lds_off<CPR>(l32, 2 * ks + g);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const int d = 16 * dt + 4 * (c16 & 3);
-      rtr[dt] = lds_off<CPR>(8 * (gq & 1) + 4 * (gq >> 1) + (c16 >> 2), d >> 3) + 2 * (d & 7);
-    }
+    // LDS offsets, the swizzle's steps by exclusive or as in the dQ pass.
+    const int roff0 = lds_off<CPR>(l32, g);
+    const int rtr0 = lds_off<CPR>(8 * (gq & 1) + 4 * (gq >> 1) + (c16 >> 2), (c16 & 3) >> 1) + 8 * (c16 & 1);
     // Step i: 32 rows of Q and dO and their statistics (rows past the sample read zeros).
     const __bf16* const qb = static_cast<const __bf16*>(a.q) + sm.q0 * a.sq + hk * a.G * a.D;
     const __bf16* const ob = static_cast<const __bf16*>(a.dout) + sm.q0 * a.sdo + hk * a.G * a.D;
@@ -377,12 +372,49 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
 #pragma unroll
         for (int e = 0; e < 4; ++e) dp[4 * x + e] = y[e];
       }
+      // S and dP in turn, operands read kAhead pairs of products before their use. The
+      // order is held at 128 columns, where two waves a SIMD are to cover each other
+      // (77,060 rows, 512 keys, 24 heads: 920 -> 875 us); at 64 there are three, and
+      // the compiler's own order is the faster one (192 us against 201).
+      constexpr int kAhead = 3, kPre = 3;
+      auto hold = []() __attribute__((always_inline)) {
+        if constexpr (DP == 128) pin_order();
+      };
+      int ro = roff0, rt = rtr0;
+      if constexpr (DP == 128) {   // at 64 the offsets fit into registers of their own
+        pin_value(ro);
+        pin_value(rt);
+      }
+      bf16x8 op[3 * kAhead];
+      auto read_ops = [&](int ks) __attribute__((always_inline)) {
+        bf16x8* const to = op + 3 * (ks % kAhead);
+        to[0] = *reinterpret_cast<const bf16x8*>(qt_lds + (ro ^ (32 * ks)));
+        to[1] = *reinterpret_cast<const bf16x8*>(ot_lds + (ro ^ (32 * ks)));
+        to[2] = *reinterpret_cast<const bf16x8*>(vrow + (ro ^ (32 * ks)));
+      };
+#pragma unroll
+      for (int ks = 0; ks < kAhead; ++ks) read_ops(ks);
+      hold();
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s = mfma32(*reinterpret_cast<const bf16x8*>(qt_lds + roff[ks]), kop[ks], s);
-        const bf16x8 vop = *reinterpret_cast<const bf16x8*>(vrow + roff[ks]);
-        dp = mfma32(*reinterpret_cast<const bf16x8*>(ot_lds + roff[ks]), vop, dp);
+        const bf16x8* const x = op + 3 * (ks % kAhead);
+        s = mfma32(x[0], kop[ks], s);
+        dp = mfma32(x[1], x[2], dp);
+        if (ks + kAhead < KS) read_ops(ks + kAhead);
+        hold();
       }
+      auto read_tr = [&](int dt) __attribute__((always_inline)) {
+        bf16x8* const to = op + 2 * (dt % kPre);
+        const int off = rt ^ (32 * dt);
+        const s16x4 o_lo = lds_read_tr16(ot_lds + off), o_hi = lds_read_tr16(ot_lds + off + 16 * ROWB);
+        const s16x4 q_lo = lds_read_tr16(qt_lds + off), q_hi = lds_read_tr16(qt_lds + off + 16 * ROWB);
+        const s16x8 o8 = {o_lo[0], o_lo[1], o_lo[2], o_lo[3], o_hi[0], o_hi[1], o_hi[2], o_hi[3]};
+        const s16x8 q8 = {q_lo[0], q_lo[1], q_lo[2], q_lo[3], q_hi[0], q_hi[1], q_hi[2], q_hi[3]};
+        to[0] = __builtin_bit_cast(bf16x8, o8);
+        to[1] = __builtin_bit_cast(bf16x8, q8);
+      };
+#pragma unroll
+      for (int dt = 0; dt < kPre; ++dt) read_tr(dt);
       u32x4 pp[2], pd[2];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -406,18 +438,17 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
         pd[0][v] = r1[0];
         pd[1][v] = r1[1];
       }
+      hold();
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        const s16x4 o_lo = lds_read_tr16(ot_lds + rtr[dt]), o_hi = lds_read_tr16(ot_lds + rtr[dt] + 16 * ROWB);
-        const s16x4 q_lo = lds_read_tr16(qt_lds + rtr[dt]), q_hi = lds_read_tr16(qt_lds + rtr[dt] + 16 * ROWB);
-        const s16x8 o8 = {o_lo[0], o_lo[1], o_lo[2], o_lo[3], o_hi[0], o_hi[1], o_hi[2], o_hi[3]};
-        const s16x8 q8 = {q_lo[0], q_lo[1], q_lo[2], q_lo[3], q_hi[0], q_hi[1], q_hi[2], q_hi[3]};
-        const bf16x8 ao = __builtin_bit_cast(bf16x8, o8), aq = __builtin_bit_cast(bf16x8, q8);
+        const bf16x8* const x = op + 2 * (dt % kPre);
 #pragma unroll
         for (int kg = 0; kg < 2; ++kg) {
-          dv[dt][kg] = mfma16(ao, __builtin_bit_cast(bf16x8, pp[kg]), dv[dt][kg]);
-          dk[dt][kg] = mfma16(aq, __builtin_bit_cast(bf16x8, pd[kg]), dk[dt][kg]);
+          dv[dt][kg] = mfma16(x[0], __builtin_bit_cast(bf16x8, pp[kg]), dv[dt][kg]);
+          dk[dt][kg] = mfma16(x[1], __builtin_bit_cast(bf16x8, pd[kg]), dk[dt][kg]);
         }
+        if (dt + kPre < DT) read_tr(dt + kPre);
+        hold();
       }
     };
     int head = s_begin / ttiles, tt = s_begin - head * ttiles;
