@@ -53,7 +53,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
   bf16x8 qop[KS], doop[KS];   // Q and dO (operands, once turned)
-  float lse2, ndl;            // the row's LSE log2 e and -delta
+  float l2, ndl;              // the row's LSE log2 e - log2(scale), and -delta
   // What only the statistics need: O as loaded, and LSE. (Set between a change of
   // item and its use alone: held in the loop otherwise.)
   struct Extra {
@@ -65,9 +65,9 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     const XSample sm = x_sample(x, at.b);
     const int r0 = at.tile * 32 * NW + 32 * w, rows = sm.nq * x.G;
     const int64_t head0 = (int64_t)at.hk * x.G * x.D;
-    x_load_rows<DP>(qop, x.q, sm.q0, x.sq, head0, r0, rows, x.G, x.D);
-    x_load_rows<DP>(doop, x.dout, sm.q0, x.sdo, head0, r0, rows, x.G, x.D);
-    x_load_rows<DP>(ex.o, x.o_in, sm.q0, x.so, head0, r0, rows, x.G, x.D);
+    x_load_rows<DP>(qop, x.q, sm.q0, x.sq, head0, r0, sm.nq, x.G, x.D);
+    x_load_rows<DP>(doop, x.dout, sm.q0, x.sdo, head0, r0, sm.nq, x.G, x.D);
+    x_load_rows<DP>(ex.o, x.o_in, sm.q0, x.so, head0, r0, sm.nq, x.G, x.D);
     const int row = min(r0 + l32, rows - 1), tok = row_token(row, x.G);
     ex.lse = x.lse[sm.stat0 + (at.hk * x.G + row - tok * x.G) * sm.hstep + tok];
   };
@@ -75,15 +75,17 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   // they are turned: a lane has pieces of rows, and their sums pass through LDS. A
   // row without keys has LSE -inf; any finite value keeps its P at 0.
   auto row_stats = [&](const XItem& at, const Extra& ex, char* lds) __attribute__((always_inline)) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     const int ln = x_lane_again();
     float* const piece = reinterpret_cast<float*>(lds) + ln;   // [row][CPR]
 #pragma unroll
     for (int u = 0; u < KS; ++u) {
       float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += (float)ex.o[u][e] * (float)doop[u][e];
+      for (int e = 0; e < 8; e += 2)   // products of bf16 are exact in fp32, the sums fp32
+        sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{ex.o[u][e], ex.o[u][e + 1]}, bf16x2{doop[u][e], doop[u][e + 1]}, sum,
+                                              false);
       piece[64 * u] = sum;
-      pin_order();   // or all rows' fp32 values would be held at once
     }
     __builtin_amdgcn_wave_barrier();
     const f32x4* const mine = reinterpret_cast<const f32x4*>(lds + (ln & 31) * CPR * 4 + (ln >> 5) * CPR * 2);
@@ -93,9 +95,10 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       const f32x4 y = mine[c];
       sum += (y[0] + y[1]) + (y[2] + y[3]);
     }
-    lse2 = ex.lse == -INFINITY ? 0.f : ex.lse * kLog2e;
+    const float lse2 = ex.lse == -INFINITY ? 0.f : ex.lse * kLog2e;
     ndl = -pair_sum(sum);
     const XArgs& x = *x_args_again();
+    l2 = lse2 - __log2f(x.scale);   // P scale in place of P: dS comes out scaled (2^-21 off at most)
     const XSample sm = x_sample(x, at.b);
     const int row = at.tile * 32 * NW + 32 * w + (ln & 31), tok = row_token(row, x.G);
     if (at.part == 0 && ln < 32 && row < sm.nq * x.G) {
@@ -161,7 +164,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
           pin_order();
         }
       }
-      const float l2 = lse2, nd = ndl;
+      const float ls = l2, nd = ndl;
       if (kt == 1 && swap) load_rows(seq.item(seq.at, order), ex);   // uniform
       if (bits != ~(uint64_t)0) {             // uniform
         const unsigned mine = (unsigned)(bits >> (32 * kt)) >> (4 * g);
@@ -172,8 +175,8 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       u32x4 pq[2];
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        const float p0 = fast_exp2(__builtin_fmaf(s[e], c2, -l2));
-        const float p1 = fast_exp2(__builtin_fmaf(s[e + 1], c2, -l2));
+        const float p0 = fast_exp2(__builtin_fmaf(s[e], c2, -ls));
+        const float p1 = fast_exp2(__builtin_fmaf(s[e + 1], c2, -ls));
         pq[(e >> 2) & 1][((e & 3) >> 1) + 2 * (e >> 3)] = pack_bf16x2(p0 * (dp[e] + nd), p1 * (dp[e + 1] + nd));
       }
 #pragma unroll
@@ -205,10 +208,9 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
     const int rows = sm.nq * x.G, r0 = at.tile * 32 * NW + 32 * w;
-    const float scale = x.scale;
     if (!part) {
-      x_store_rows<DP>(x.dq, sm.q0, x.sdq, (int64_t)at.hk * x.G * x.D, r0, rows, x.G, x.D, lds0, lds1,
-                       [&](int dt, int qg) { return dq[dt][qg] * scale; });
+      x_store_rows<DP>(x.dq, sm.q0, x.sdq, (int64_t)at.hk * x.G * x.D, r0, sm.nq, x.G, x.D, lds0, lds1,
+                       [&](int dt, int qg) { return dq[dt][qg]; });
       return;
     }
 #pragma unroll
@@ -219,7 +221,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
           part + ((at.part * x.Tq + sm.q0 + tok) * x.Hq + at.hk * x.G + row - tok * x.G) * x.D + 4 * gq;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
-        if (16 * dt + 4 * gq < x.D) *reinterpret_cast<f32x4*>(pp + 16 * dt) = dq[dt][qg] * scale;
+        if (16 * dt + 4 * gq < x.D) *reinterpret_cast<f32x4*>(pp + 16 * dt) = dq[dt][qg];
     }
   };
 
@@ -260,8 +262,9 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       seq.cur = seq.at;
       if (more) {
         row_stats(at, ex, lds0);
-        x_turn_rows<DP>(qop, lds0, lds1);
-        x_turn_rows<DP>(doop, lds0, lds1);
+        const XTurn<DP> rows(x_lane_again());
+        rows.turn(qop, lds0, lds1);
+        rows.turn(doop, lds0, lds1);
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   auto load_rows = [&](const XItem& at) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
-    x_load_rows<DP>(qop, x.q, sm.q0, x.sq, (int64_t)at.hk * x.G * x.D, at.tile * 32 * NW + 32 * w, sm.nq * x.G, x.G, x.D);
+    x_load_rows<DP>(qop, x.q, sm.q0, x.sq, (int64_t)at.hk * x.G * x.D, at.tile * 32 * NW + 32 * w, sm.nq, x.G, x.D);
   };
   const TileLoad<DP, NW> load_k(lane, a.sk), load_v(lane, a.sv);
 
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
           if (16 * dt + 4 * gq < x.D) *reinterpret_cast<f32x4*>(op + 16 * dt) = oacc[dt][qg];
       }
     } else {
-      x_store_rows<DP>(x.o, sm.q0, x.so, (int64_t)at.hk * x.G * x.D, r0, rows, x.G, x.D, lds0, lds1,
+      x_store_rows<DP>(x.o, sm.q0, x.so, (int64_t)at.hk * x.G * x.D, r0, sm.nq, x.G, x.D, lds0, lds1,
                        [&](int dt, int qg) { return oacc[dt][qg] * __uint_as_float(ir[qg]); });
     }
   };
@@ -307,7 +307,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       char* const lds0 = (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
       char* const lds1 = (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
       if (have) finish(seq.item(seq.cur, order), lds0, lds1);
-      if (more) x_turn_rows<DP>(qop, lds0, lds1);
+      if (more) XTurn<DP>(x_lane_again()).turn(qop, lds0, lds1);
       seq.cur = seq.at;
       m_run = l_run = 0.f;
       fresh = true;

@@ -287,100 +287,112 @@ __device__ inline void x_store16(bf16x8 v, __amdgpu_buffer_rsrc_t rs, int off) {
 
 // Byte offsets of a wave's rows r0 + lane / CPR + u RPI, u = 0 .., at the lane's 16-byte
 // column: row r is token r / G and head r % G, which the step of RPI rows moves on
-// without another division. Offsets count from the first row's token (32 rows stay
-// below kXOut); rows from `rows` on and columns past D give kXOut, or with
-// `repeat` the last row.
+// without another division. Offsets count from the first row's token and head0 of
+// it. Rows past the sample's nq tokens lie past the descriptor's range, and columns
+// past D too: loads give zeros there, stores are dropped.
 template <int DP>
 struct XRows {
   static constexpr int CPR = DP / 8, RPI = 64 / CPR, N = DP / 16;   // N instructions of RPI rows
   int off[N];
-  int first;   // that token, uniform
+  __amdgpu_buffer_rsrc_t rs;
 
-  __device__ inline XRows(int lane, int r0, int rows, int G, int D, int stride, bool repeat) {
-    const int c = 8 * (lane % CPR), last = rows - 1, row0 = r0 + lane / CPR;
-    first = min(r0, last);
-    int tok = row0, head = 0, dtok = RPI, dhead = 0, ltok = last, lhead = 0;
+  __device__ inline XRows(int lane, const void* base, int64_t tok0, int stride, int64_t head0, int r0, int nq, int G,
+                          int D) {
+    const int c = 8 * (lane % CPR), row0 = r0 + lane / CPR;
+    int first = r0, tok = row0, head = 0;
     if (G != 1) {   // uniform
       first = (int)((unsigned)first / (unsigned)G);
-      ltok = (int)((unsigned)last / (unsigned)G), lhead = last - ltok * G;
-      dtok = RPI / G, dhead = RPI - dtok * G;
       tok = (int)((unsigned)row0 / (unsigned)G), head = row0 - tok * G;
     }
-    first = __builtin_amdgcn_readfirstlane(first);
-    const int past = repeat ? ((ltok - first) * stride + lhead * D + c) * 2 : kXOut;
+    first = __builtin_amdgcn_readfirstlane(min(first, nq - 1));
+    // at most 31 tokens behind the first of the wave (4 waves: 127 behind the last of
+    // the sample): with strides up to kXMaxStride all of it stays below 2^31
+    rs = buffer_rsrc(static_cast<const __bf16*>(base) + (tok0 + first) * stride + head0,
+                     (min(nq - 1 - first, 32) * stride + G * D) * 2);
+    off[0] = c < D ? ((tok - first) * stride + head * D + c) * 2 : kXOut;
+    if (G == 1) {   // uniform
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const int x = ((tok - first) * stride + head * D + c) * 2;
-      off[u] = c >= D ? kXOut : row0 + u * RPI < rows ? x : past;
-      tok += dtok, head += dhead;
-      const bool wrap = head >= G;
-      tok += wrap ? 1 : 0, head -= wrap ? G : 0;
+      for (int u = 1; u < N; ++u) off[u] = off[u - 1] + RPI * stride * 2;
+    } else {
+      const int dtok = RPI / G, dhead = RPI - dtok * G;
+      const int step = (dtok * stride + dhead * D) * 2, wrap = (stride - G * D) * 2;
+#pragma unroll
+      for (int u = 1; u < N; ++u) {
+        head += dhead;
+        const bool over = head >= G;
+        head -= over ? G : 0;
+        off[u] = off[u - 1] + step + (over ? wrap : 0);
+      }
     }
   }
 };
 
-// Stores a wave's 32 result rows, rounded to bf16, as whole rows: 16 bytes a lane,
-// a row's lanes side by side, where the accumulators' layout would write pieces of
-// 32 bytes. The rows pass through the wave's own part of a consumed stage (row
-// group qg through lds0 or lds1, 16 rows, swizzled as the tiles), which only the
-// wave's own next loads write. val(dt, qg): columns 16 dt + 4 gq + (0..3) of row
-// 16 qg + c16 of the rows r0 .. of `rows`.
+// LDS offsets of a wave's 32 rows in its own part of a stage: row group 0 or 1 of 16
+// rows in lds0 or lds1, swizzled as the tiles. As whole rows, lane / CPR + u RPI at the
+// lane's column: the swizzle of the later ones differs by the bits of u alone.
+template <int DP>
+struct XTurn {
+  static constexpr int CPR = DP / 8, ROWB = DP * 2, RPI = 64 / CPR, N = DP / 16, REP = 16 / RPI;
+  int lane, row, column;
+  __device__ inline explicit XTurn(int ln) : lane(ln) {
+    row = lane / CPR * ROWB;
+    column = lds_off<CPR>(lane / CPR, lane % CPR) & (ROWB - 1);
+  }
+  __device__ inline int whole(int u) const {
+    const int k = u % REP;
+    return row + (column ^ (CPR == 16 ? k << 4 : (4 * k) << 4)) + k * RPI * ROWB;
+  }
+  // Rows loaded whole to operands: op[ks] = columns 16 ks + 8 g .. of row l32.
+  __device__ inline void turn(bf16x8 (&x)[N], char* lds0, char* lds1) const {
+#pragma unroll
+    for (int u = 0; u < N; ++u) *reinterpret_cast<bf16x8*>((u < REP ? lds0 : lds1) + whole(u)) = x[u];
+    pin_order();
+    const char* const from = (lane & 16) ? lds1 : lds0;
+    const int op = lds_off<CPR>(lane & 15, lane >> 5);
+#pragma unroll
+    for (int ks = 0; ks < N; ++ks) x[ks] = *reinterpret_cast<const bf16x8*>(from + (op ^ (32 * ks)));
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done before the next writes
+  }
+};
+
+// A wave's 32 operand rows r0 .. loaded as whole rows, 16 bytes a lane, to be turned
+// into operands (XTurn): loaded as operands, an instruction would touch a line of
+// every row.
+template <int DP>
+__device__ inline void x_load_rows(bf16x8 (&x)[DP / 16], const void* src, int64_t tok0, int stride, int64_t head0, int r0,
+                                   int nq, int G, int D) {
+  const XRows<DP> at(x_lane_again(), src, tok0, stride, head0, r0, nq, G, D);
+#pragma unroll
+  for (int u = 0; u < DP / 16; ++u) x[u] = x_load16(at.rs, at.off[u]);
+}
+
+// Stores a wave's 32 result rows, rounded to bf16, as whole rows, where the
+// accumulators' layout would write pieces of 32 bytes: through the wave's own part of a
+// consumed stage, which only the wave's own next loads write. val(dt, qg): columns
+// 16 dt + 4 gq + (0..3) of row 16 qg + c16 of the rows r0 ...
 template <int DP, class Val>
-__device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t head0, int r0, int rows, int G, int D,
+__device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t head0, int r0, int nq, int G, int D,
                                     char* lds0, char* lds1, Val val) {
-  constexpr int CPR = DP / 8, RPI = 64 / CPR, DT = DP / 16;
-  const int lane = x_lane_again(), c16 = lane & 15, gq = lane >> 4;
+  constexpr int N = DP / 16;
+  const XTurn<DP> t(x_lane_again());
+  const int c16 = t.lane & 15, gq = t.lane >> 4, piece = lds_off<DP / 8>(c16, gq >> 1) + 8 * (gq & 1);
 #pragma unroll
   for (int qg = 0; qg < 2; ++qg) {
-    char* const lds = qg ? lds1 : lds0;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
+    for (int dt = 0; dt < N; ++dt) {
       const f32x4 y = val(dt, qg);
-      *reinterpret_cast<bf16x4*>(lds + lds_off<CPR>(c16, 2 * dt + (gq >> 1)) + 8 * (gq & 1)) =
+      *reinterpret_cast<bf16x4*>((qg ? lds1 : lds0) + (piece ^ (32 * dt))) =
           bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
     }
     pin_order();
   }
-  bf16x8 v[DP / 16];
+  bf16x8 v[N];
 #pragma unroll
-  for (int u = 0; u < DP / 16; ++u) {   // a row group's instructions lie on one side
-    const int r = u * RPI + lane / CPR;
-    v[u] = *reinterpret_cast<const bf16x8*>((u < DP / 32 ? lds0 : lds1) + lds_off<CPR>(r & 15, lane % CPR));
-  }
-  const XRows<DP> at(lane, r0, rows, G, D, stride, false);   // beside the reads
-  const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<__bf16*>(dst) + (tok0 + at.first) * stride + head0, kXOut);
+  for (int u = 0; u < N; ++u) v[u] = *reinterpret_cast<const bf16x8*>((u < t.REP ? lds0 : lds1) + t.whole(u));
+  const XRows<DP> at(t.lane, dst, tok0, stride, head0, r0, nq, G, D);   // beside the reads
   __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done before the next loads
 #pragma unroll
-  for (int u = 0; u < DP / 16; ++u) x_store16(v[u], rs, at.off[u]);
-}
-
-// The way in: a wave's 32 operand rows r0 .. of `rows` (rows past the last repeat
-// it), loaded as whole rows, 16 bytes a lane, and then turned through the same part
-// of a stage into operands: x[ks] = columns 16 ks + 8 g .. of row l32. Loaded as
-// operands, an instruction would touch a line of every row.
-template <int DP>
-__device__ inline void x_load_rows(bf16x8 (&x)[DP / 16], const void* src, int64_t tok0, int stride, int64_t head0, int r0,
-                                   int rows, int G, int D) {
-  const XRows<DP> at(x_lane_again(), r0, rows, G, D, stride, true);
-  const __amdgpu_buffer_rsrc_t rs =
-      buffer_rsrc(static_cast<const __bf16*>(src) + (tok0 + at.first) * stride + head0, kXOut);
-#pragma unroll
-  for (int u = 0; u < DP / 16; ++u) x[u] = x_load16(rs, at.off[u]);
-}
-template <int DP>
-__device__ inline void x_turn_rows(bf16x8 (&x)[DP / 16], char* lds0, char* lds1) {
-  constexpr int CPR = DP / 8, RPI = 64 / CPR;
-  const int lane = x_lane_again(), l32 = lane & 31, g = lane >> 5;
-#pragma unroll
-  for (int u = 0; u < DP / 16; ++u) {
-    const int r = u * RPI + lane / CPR;
-    *reinterpret_cast<bf16x8*>((u < DP / 32 ? lds0 : lds1) + lds_off<CPR>(r & 15, lane % CPR)) = x[u];
-  }
-  pin_order();
-  const char* const from = l32 < 16 ? lds0 : lds1;
-#pragma unroll
-  for (int ks = 0; ks < DP / 16; ++ks) x[ks] = *reinterpret_cast<const bf16x8*>(from + lds_off<CPR>(l32 & 15, 2 * ks + g));
-  __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done before the next writes
+  for (int u = 0; u < N; ++u) x_store16(v[u], at.rs, at.off[u]);
 }
 
 // Direct loads of 64-row tiles into LDS by NW waves, in rows of DP elements:
