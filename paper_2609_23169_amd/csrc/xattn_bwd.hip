@@ -19,10 +19,18 @@
 //           writes fp32 partial sums, and a join adds them in a fixed order.
 //
 // Rounding: P and dS to bf16 before their second products (half a step each,
-// 2^-9 relative), all sums in fp32. No atomics: equal results on every run.
-// Keys not in use: the dQ pass reads zeros in their place and sets their P to
-// 0; in the dK/dV pass a key is a column of its own, whatever it holds, and is
-// stored as 0.
+// 2^-9 relative), all sums in fp32. delta comes from O as stored (half a step
+// of it), or as rowsum(P o dP) in fp32 where all keys of a row lie in one tile.
+// No atomics: equal results on every run. Keys not in use: the dQ pass reads
+// zeros in their place and sets their P to 0; in the dK/dV pass a key is a
+// column of its own, whatever it holds, and is stored as 0; waves whose 32 keys
+// are all unused only load.
+//
+// What bounds it (77,060 queries, 512 keys, 24 heads of 128: dQ 807 us, dK/dV 846,
+// 900 and 1,150 TFLOP/s of the products that they form): the matrix cores are 41 and
+// 55% busy, vector work and LDS reads fill most of the rest, and the board's power
+// limit sets the clock (1.85 of 2.4 GHz): with rows of zeros the same instructions
+// run 17% faster. dQ also moves 1.9 GB, 0.39 ms at the copy rate, beside it.
 #include <algorithm>
 #include <type_traits>
 
@@ -53,7 +61,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
   bf16x8 qop[KS], doop[KS];   // Q and dO (operands, once turned)
-  float l2, ndl;              // the row's LSE log2 e - log2(scale), and -delta
+  float lse2, l2, ndl;        // the row's LSE log2 e, that less log2(scale), and -delta
   // What only the statistics need: O as loaded, and LSE. (Set between a change of
   // item and its use alone: held in the loop otherwise.)
   struct Extra {
@@ -71,10 +79,10 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     const int row = min(r0 + l32, rows - 1), tok = row_token(row, x.G);
     ex.lse = x.lse[sm.stat0 + (at.hk * x.G + row - tok * x.G) * sm.hstep + tok];
   };
-  // The statistics of those rows, for the dK/dV pass too (part 0 writes them), before
-  // they are turned: a lane has pieces of rows, and their sums pass through LDS. A
-  // row without keys has LSE -inf; any finite value keeps its P at 0.
-  auto row_stats = [&](const XItem& at, const Extra& ex, char* lds) __attribute__((always_inline)) {
+  // The statistics of those rows before they are turned: a lane has pieces of rows,
+  // and their sums pass through LDS. A row without keys has LSE -inf; any finite
+  // value keeps its P at 0.
+  auto row_stats = [&](const Extra& ex, char* lds) __attribute__((always_inline)) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     const int ln = x_lane_again();
     float* const piece = reinterpret_cast<float*>(lds) + ln;   // [row][CPR]
@@ -95,10 +103,15 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       const f32x4 y = mine[c];
       sum += (y[0] + y[1]) + (y[2] + y[3]);
     }
-    const float lse2 = ex.lse == -INFINITY ? 0.f : ex.lse * kLog2e;
     ndl = -pair_sum(sum);
+    const float scale = x_args_again()->scale;
+    lse2 = ex.lse == -INFINITY ? 0.f : ex.lse * kLog2e;
+    l2 = lse2 - __log2f(scale);   // P scale in place of P: dS comes out scaled (2^-21 off at most)
+  };
+  // For the dK/dV pass too: part 0 writes them.
+  auto put_stats = [&](const XItem& at) __attribute__((always_inline)) {
+    const int ln = x_lane_again();
     const XArgs& x = *x_args_again();
-    l2 = lse2 - __log2f(x.scale);   // P scale in place of P: dS comes out scaled (2^-21 off at most)
     const XSample sm = x_sample(x, at.b);
     const int row = at.tile * 32 * NW + 32 * w + (ln & 31), tok = row_token(row, x.G);
     if (at.part == 0 && ln < 32 && row < sm.nq * x.G) {
@@ -204,6 +217,29 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       }
     }
   };
+  // delta of rows whose keys all lie in one tile, as rowsum(P o dP) in fp32: with few
+  // keys dP - delta is a small difference, and the rounding of the O that is stored
+  // would show in it (2 keys: dQ 0.0039 off in relative norm, 0.0024 with this).
+  auto tile_delta = [&](uint64_t bits, const char* kt_lds, const char* vt_lds) __attribute__((always_inline)) {
+    float sum = 0.f;
+#pragma unroll 1
+    for (int kt = 0; kt < 2; ++kt) {
+      f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int off = (koff0 ^ (32 * ks)) + kt * 32 * ROWB;
+        s = mfma32(*reinterpret_cast<const bf16x8*>(kt_lds + off), qop[ks], s);
+        dp = mfma32(*reinterpret_cast<const bf16x8*>(vt_lds + off), doop[ks], dp);
+      }
+      const unsigned mine = (unsigned)(bits >> (32 * kt)) >> (4 * g);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = fast_exp2(__builtin_fmaf(s[e], c2, -lse2));
+        sum += mine >> (8 * (e >> 2) + (e & 3)) & 1 ? p * dp[e] : 0.f;
+      }
+    }
+    return pair_sum(sum);
+  };
   auto finish = [&](const XItem& at, char* lds0, char* lds1) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
@@ -261,10 +297,12 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       const XItem at = seq.item(seq.at, order);
       seq.cur = seq.at;
       if (more) {
-        row_stats(at, ex, lds0);
+        row_stats(ex, lds0);
         const XTurn<DP> rows(x_lane_again());
         rows.turn(qop, lds0, lds1);
         rows.turn(doop, lds0, lds1);
+        if (seq.keys <= kXKeys) ndl = -tile_delta(seq.bits, kn, vn);   // uniform
+        put_stats(at);
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};

@@ -198,12 +198,12 @@ struct TileSeq {
   uint64_t bits;
   bool fresh;                                   // that item has given no tile yet
   int64_t k0;                                   // its sample's first key
-  int hk;                                       // its key head
+  int hk, keys;                                 // its key head and number of keys
 
   __device__ inline void begin(const XItems& i) {
     first = i.first, step = i.step, turn = i.turn, end = i.end;
     tiles.open(nullptr, 0, 0, 0);
-    tile = hk = b = rtile = hkpart = 0;
+    tile = hk = keys = b = rtile = hkpart = 0;
     k0 = 0;
     bits = todo = 0;
     at = cur = kKept;
@@ -267,6 +267,7 @@ struct TileSeq {
       tiles.open(x.mask ? x.mask + sm.k0 : nullptr, sm.nk, t0, t1);
       k0 = sm.k0;
       hk = m.hk;
+      keys = sm.nk;
       fresh = true;
     }
     fresh = false;

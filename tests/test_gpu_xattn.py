@@ -274,6 +274,50 @@ def test_zero_lengths():
     assert o.numel() == 0 and dq.numel() == 0 and (dk == 0).all() and (dv == 0).all()
 
 
+@pytest.mark.parametrize("Nk", [1, 2, 3, 33, 64])
+@pytest.mark.parametrize("Hq,Hk,D", [(4, 2, 64), (3, 1, 128)])
+def test_few_keys_do_not_feel_the_rounding_of_o(Nk, Hq, Hk, D):
+    """dP - delta is a small difference there. Bounds by element: dS and the results
+    are rounded to bf16 (u = 2^-8 each); P, dP and delta are fp32, off by less than
+    2^-16 of the sums of magnitudes that they are formed from."""
+    q, k, v, do = draw(12, 1, 300, Nk, Hq, Hk, D)
+    scale = D ** -0.5
+    _, _, (dq, dk, dv) = run(q, k, v, do, scale, None)
+    Q, DO = (x[0].double().cpu().permute(1, 0, 2) for x in (q, do))                       # [Hq, Nq, D]
+    K, V = (x[0].double().cpu().permute(1, 0, 2).repeat_interleave(Hq // Hk, 0) for x in (k, v))
+    P = (Q @ K.mT * scale).softmax(-1)
+    dP, adP = DO @ V.mT, DO.abs() @ V.abs().mT
+    dS = P * (dP - (P * dP).sum(-1, keepdim=True))
+    u = 2.0 ** -8
+    eS = u * dS.abs() + 2.0 ** -16 * P * (adP + (P * adP).sum(-1, keepdim=True))
+    shared = lambda x: x.unflatten(0, (Hk, -1)).sum(1)  # noqa: E731
+    for name, got, ref, err in (("dq", dq, scale * (dS @ K), scale * (eS @ K.abs())),
+                                ("dk", dk, shared(scale * (dS.mT @ Q)), shared(scale * (eS.mT @ Q.abs())))):
+        got = got[0].double().cpu().permute(1, 0, 2)
+        worst = ((got - ref).abs() / (u * ref.abs() + (1 + u) * err)).max().item()
+        assert worst <= 1, (name, worst)
+
+
+def test_query_rows_past_32_bit_offsets():
+    """Rows of queries and results 2^22 - 8 elements apart, the last tile cut short."""
+    for Nq, Hq, Hk in ((290, 1, 1), (258, 3, 1)):
+        D, stride, width = 64, (1 << 22) - 8, 3 * 64
+        q, k, v, do = draw(13, 1, Nq, 100, Hq, Hk, D)
+        want = run(q, k, v, do, 0.125, None)
+        buf = torch.zeros((Nq - 1) * stride + 4 * width, dtype=torch.bfloat16, device=DEV)
+        at = lambda i: torch.as_strided(buf, (1, Nq, Hq, D), (Nq * stride, stride, D, 1), i * width)  # noqa: E731
+        at(0).copy_(q), at(1).copy_(do)
+        lse, dk, dv = torch.empty_like(want[1]), torch.empty_like(k), torch.empty_like(v)
+        assert ut.ut_xattn_fwd(at(0), k, v, at(2), lse, 0.125) == ut.UT_OK
+        ws = torch.empty(ut.ut_xattn_bwd_workspace_size(1, Nq, 100, Hq, Hk, D), dtype=torch.uint8, device=DEV)
+        assert ut.ut_xattn_bwd(at(0), k, v, at(2), at(1), lse, at(3), dk, dv, 0.125, workspace=ws) == ut.UT_OK
+        for x, y in ((at(2), want[0]), (lse, want[1]), (at(3), want[2][0]), (dk, want[2][1]), (dv, want[2][2])):
+            assert torch.equal(x, y)
+        assert torch.equal(at(0), q) and torch.equal(at(1), do)
+        assert int(torch.count_nonzero(buf)) <= 4 * Nq * Hq * D   # nothing between the rows was written
+        del buf, at
+
+
 # ---- packed samples --------------------------------------------------------
 
 def offsets(lens):
