@@ -219,9 +219,8 @@ struct XArgs {
   int sq, sk, sv, so, sdo, sdq, sdk, sdv;
   float scale;
 };
-// Key ranges of the forward (1: one range, no workspace) and, for more, the
-// bytes of the ranges' partial results.
-int xattn_fwd_splits(const XArgs& a);
+// Bytes of the partial results where the keys (forward, dQ) or the query tokens
+// (dK, dV) are split over workgroups, and of the backward's row statistics.
 size_t xattn_fwd_workspace(const XArgs& a);
 hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s);
 size_t xattn_bwd_workspace(const XArgs& a);

@@ -42,16 +42,16 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kBwdKeys = 128;   // keys of a dK/dV workgroup
 constexpr int kRowTile = 32;    // query tokens of a dK/dV step
+constexpr int kDqWaves = 4;     // of 32 rows each
 
 // ---------------------------------------------------------------------------
 // dQ
 // ---------------------------------------------------------------------------
 // part: fp32 [split][token][Hq][D], null with one split.
-template <int DP, int NW>
-__global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_dq_kernel(const XArgs a, float* __restrict__ aux,
-                                                                            const XOrder order, const bool by_xcd,
-                                                                            float* __restrict__ part) {
-  constexpr int ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
+template <int DP>
+__global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const XArgs a, float* __restrict__ aux,
+                                                                         const XOrder order, float* __restrict__ part) {
+  constexpr int NW = kDqWaves, ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
   __shared__ __attribute__((aligned(1024))) char k_lds0[TILEB];
   __shared__ __attribute__((aligned(1024))) char k_lds1[TILEB];
   __shared__ __attribute__((aligned(1024))) char v_lds0[TILEB];
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   };
 
   // A workgroup's items in turn, their tiles as one sequence, as in the forward.
-  seq.begin(x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk, by_xcd));
+  seq.begin(x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk));
   bool have = false;   // a tile lies in the current stage
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
@@ -320,8 +320,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
 // part: fp32 [dK, dV][split][token][Hk][D], null with one split.
 template <int DP>
 __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const float* __restrict__ aux,
-                                                            const XOrder order, const bool by_xcd,
-                                                            float* __restrict__ part) {
+                                                            const XOrder order, float* __restrict__ part) {
   constexpr int NW = 4, ROWB = DP * 2, CPR = DP / 8, KS = DP / 16, DT = DP / 16;
   constexpr int TILEB = kRowTile * ROWB, RPI = 1024 / ROWB, IPW = TILEB / 1024 / NW, VIPW = kBwdKeys * ROWB / 1024 / NW;
   __shared__ __attribute__((aligned(1024))) char q_lds0[TILEB];
@@ -335,7 +334,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
-  const XItems items = x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk, by_xcd);
+  const XItems items = x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk);
   if (items.first >= items.end) return;
   const XItem at = x_item(items.first, (unsigned)a.B, order);
   const unsigned kt = at.tile, sp = at.part;
@@ -581,21 +580,17 @@ __global__ __launch_bounds__(256) void xattn_clear_kernel(const XClear t0, const
     for (int64_t i = at; i < (t.T - end) * H; i += step) lse[i / (t.T - end) * t.T + end + i % (t.T - end)] = -INFINITY;
 }
 
-int dq_waves(const XArgs& a) {
-  const int64_t rows = (int64_t)a.Nq * a.G;
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-}
-int64_t dq_groups(const XArgs& a) {
-  const int64_t per = 32 * dq_waves(a);
-  return (int64_t)a.B * a.Hk * (((int64_t)a.Nq * a.G + per - 1) / per);
-}
+int64_t dq_tiles(const XArgs& a) { return ((int64_t)a.Nq * a.G + 32 * kDqWaves - 1) / (32 * kDqWaves); }
+int64_t dq_groups(const XArgs& a) { return (int64_t)a.B * a.Hk * dq_tiles(a); }
 int64_t dkdv_groups(const XArgs& a) {
   return (int64_t)a.B * a.Hk * (((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys);
 }
-// As many parts as fit the chip at once. Splits below four tiles are not worth their join.
+// As many parts as fit the chip at once, of four tiles or eight steps at least: at 300
+// queries and keys, 8 heads of 64, half of that takes dQ from 14.9 to 13.0 us and dK/dV
+// from 14.5 to 11.7, and their joins add 19.
 int dq_splits(const XArgs& a) {
   const int64_t groups = dq_groups(a), tiles = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
-  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), dq_waves(a)) / groups, tiles / 4));
+  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), kDqWaves) / groups, tiles / 4));
 }
 int dkdv_splits(const XArgs& a) {
   const int64_t groups = dkdv_groups(a), steps = (int64_t)a.G * (((int64_t)a.Nq + kRowTile - 1) / kRowTile);
@@ -611,21 +606,20 @@ size_t dkdv_part(const XArgs& a) {
   return n > 1 ? (size_t)n * a.Tk * a.Hk * a.D * 2 * sizeof(float) : 0;
 }
 
-template <int DP, int NW>
+template <int DP>
 void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t s) {
-  const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
-  const bool by_xcd = (int64_t)a.B * a.Nk * a.D * 4 <= kXcdHeadBytes;
+  const XOrder order{head_group(a), (unsigned)dq_tiles(a), (unsigned)splits};
   const int64_t items = dq_groups(a) * splits;
-  const dim3 grid((unsigned)(std::min<int64_t>(items, x_resident(DP, NW)) + 7) / 8 * 8);
-  TraceScope ts_(s, "xattn_dq", DP, NW);
-  hipLaunchKernelGGL((xattn_dq_kernel<DP, NW>), grid, dim3(64 * NW), 0, s, a, aux, order, by_xcd, part);
+  const dim3 grid((unsigned)(std::min<int64_t>(items, x_resident(DP, kDqWaves)) + 7) / 8 * 8);
+  TraceScope ts_(s, "xattn_dq", DP);
+  hipLaunchKernelGGL((xattn_dq_kernel<DP>), grid, dim3(64 * kDqWaves), 0, s, a, aux, order, part);
 }
 template <int DP>
 void launch_dkdv(const XArgs& a, const float* aux, int splits, float* part, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys), (unsigned)splits};
   TraceScope ts_(s, "xattn_dkdv", DP);
   hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), dim3((unsigned)(dkdv_groups(a) * splits + 7) / 8 * 8), dim3(256), 0, s,
-                     a, aux, order, true, part);
+                     a, aux, order, part);
 }
 void launch_sum(const float* part, int splits, int64_t T, int width, void* out, int stride, const int32_t* cu, int B,
                 int N, hipStream_t s) {
@@ -643,12 +637,9 @@ hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
   float* const aux = static_cast<float*>(workspace);
   float* const part = reinterpret_cast<float*>(static_cast<char*>(workspace) + aux_bytes(a));   // both joins' in turn
   if (dq_groups(a) > 0) {
-    const int n = dq_splits(a), nw = dq_waves(a);
+    const int n = dq_splits(a);
     float* const p = n > 1 ? part : nullptr;
-    if (a.D <= 64)
-      nw == 1 ? launch_dq<64, 1>(a, aux, n, p, s) : nw == 2 ? launch_dq<64, 2>(a, aux, n, p, s) : launch_dq<64, 4>(a, aux, n, p, s);
-    else
-      nw == 1 ? launch_dq<128, 1>(a, aux, n, p, s) : nw == 2 ? launch_dq<128, 2>(a, aux, n, p, s) : launch_dq<128, 4>(a, aux, n, p, s);
+    a.D <= 64 ? launch_dq<64>(a, aux, n, p, s) : launch_dq<128>(a, aux, n, p, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (n > 1) launch_sum(part, n, a.Tq, a.Hq * a.D, a.dq, a.sdq, a.cuq, a.B, a.Nq, s);
   }

@@ -22,7 +22,7 @@
 // joins them in a fixed order. No atomics: equal results on every run. Parts for
 // one round of the chip: two rounds of half the length (which would even out
 // unequal samples) took 56.5 + 8.2 us against 52.5 + 6.7 at 4 x 32 query heads on
-// 16,391 keys. Below four tiles a part costs more in the join than it saves.
+// 16,391 keys.
 //
 // What bounds it: 22,879 queries on 4,097 keys, 24 heads of 128, take 1,092 us, 1,055
 // TFLOP/s: matrix cores 49% busy, vector work 43%, LDS reads (a wave reads the tile
@@ -53,8 +53,7 @@ struct Parts {
 
 template <int DP, int NW, bool SPLIT>
 __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_fwd_kernel(const XArgs a, const XOrder order,
-                                                               const bool by_xcd,
-                                                               const Parts parts) {
+                                                                                           const Parts parts) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
   __shared__ __attribute__((aligned(1024))) char k_lds0[TILEB];
   __shared__ __attribute__((aligned(1024))) char k_lds1[TILEB];
@@ -287,7 +286,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
 
   // A workgroup's items in turn, their tiles as one sequence: a tile's loads are
   // issued while the tile before it is worked on, across items too.
-  seq.begin(x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk, by_xcd));
+  seq.begin(x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk));
   bool have = false;   // a tile lies in the current stage
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
@@ -332,8 +331,8 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   }
 }
 
-// Joins the splits of a row: GPR groups of 32 lanes take every GPR-th split,
-// four columns a lane, and the groups' sums are added in LDS.
+// Joins the parts of a row: GPR groups of 32 lanes take every GPR-th part, four
+// columns a lane, and the groups' sums are added in LDS.
 template <int GPR>
 __global__ __launch_bounds__(256) void xattn_join_kernel(const XArgs a, const int splits, const Parts parts) {
   __shared__ float4 red[256];
@@ -402,28 +401,37 @@ __global__ __launch_bounds__(256) void xattn_join_kernel(const XArgs a, const in
   }
 }
 
-// Waves of a workgroup: as many as there are tiles of 32 rows, up to four.
-int fwd_waves(const XArgs& a) {
-  const int64_t rows = (int64_t)a.Nq * a.G;
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-}
-int64_t fwd_groups(const XArgs& a) {
-  const int64_t per = 32 * fwd_waves(a);
-  return (int64_t)a.B * a.Hk * (((int64_t)a.Nq * a.G + per - 1) / per);
+// Parts of the keys, and waves of a workgroup: four, or one where up to 32 rows meet
+// split keys (4 rows of 4 x 8 key heads on 16,391 keys: 49 us against 51 with three
+// idle waves beside; unsplit keys the other way round, 14.2 against 13.0 for 16
+// samples of 20 rows and 300 keys). Parts below four tiles: the last case split in two
+// takes 11.7 + 6.4, 16 samples of 60 rows 15.9 + 7.5 against 16.2.
+struct Shape {
+  int splits, waves;
+};
+Shape fwd_shape(const XArgs& a) {
+  const int64_t rows = (int64_t)a.Nq * a.G, heads = (int64_t)a.B * a.Hk, tiles = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
+  auto splits = [&](int nw) {
+    const int64_t groups = heads * ((rows + 32 * nw - 1) / (32 * nw));
+    return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), nw) / groups, tiles / 4));
+  };
+  if (rows <= 32 && splits(1) > 1) return Shape{splits(1), 1};
+  return Shape{splits(4), 4};
 }
 int64_t stats_of(const XArgs& a) { return a.Tq * a.Hq; }
 
 template <int DP, int NW>
 void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
-  const int64_t items = fwd_groups(a) * splits;
+  const int64_t items = (int64_t)a.B * a.Hk * order.tiles * splits;
   const dim3 grid((unsigned)(std::min<int64_t>(items, x_resident(DP, NW)) + 7) / 8 * 8);
-  const bool by_xcd = (int64_t)a.B * a.Nk * a.D * 4 <= kXcdHeadBytes;
   TraceScope ts_(s, splits > 1 ? "xattn_fwd_split" : "xattn_fwd", DP, NW);
-  if (splits > 1)
-    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, true>), grid, dim3(64 * NW), 0, s, a, order, by_xcd, parts);
-  else
-    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, false>), grid, dim3(64 * NW), 0, s, a, order, by_xcd, parts);
+  if (splits > 1) {
+    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, true>), grid, dim3(64 * NW), 0, s, a, order, parts);
+  } else {
+    if constexpr (NW == 4)
+      hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, false>), grid, dim3(64 * NW), 0, s, a, order, parts);
+  }
 }
 template <int GPR>
 void launch_join(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
@@ -435,31 +443,29 @@ void launch_join(const XArgs& a, int splits, const Parts& parts, hipStream_t s) 
 
 }  // namespace
 
-int xattn_fwd_splits(const XArgs& a) {
-  const int64_t groups = fwd_groups(a), tiles = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
-  if (groups == 0) return 1;
-  return (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), fwd_waves(a)) / groups, tiles / 4));
-}
 size_t xattn_fwd_workspace(const XArgs& a) {
-  const int splits = xattn_fwd_splits(a);
+  const int splits = fwd_shape(a).splits;
   return splits > 1 ? (size_t)splits * stats_of(a) * (sizeof(float2) + (size_t)a.D * sizeof(float)) : 0;
 }
 
 hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s) {
-  const int splits = xattn_fwd_splits(a);
+  const auto [splits, waves] = fwd_shape(a);
   Parts parts{};
   parts.stats = stats_of(a);
   if (splits > 1) {   // O first: its rows are 16-byte aligned
     parts.o = static_cast<float*>(workspace);
     parts.sums = reinterpret_cast<float2*>(parts.o + (size_t)splits * parts.stats * a.D);
   }
-  const int nw = fwd_waves(a);
   if (a.D <= 64)
-    nw == 1 ? launch_fwd<64, 1>(a, splits, parts, s) : nw == 2 ? launch_fwd<64, 2>(a, splits, parts, s) : launch_fwd<64, 4>(a, splits, parts, s);
+    waves == 1 ? launch_fwd<64, 1>(a, splits, parts, s) : launch_fwd<64, 4>(a, splits, parts, s);
   else
-    nw == 1 ? launch_fwd<128, 1>(a, splits, parts, s) : nw == 2 ? launch_fwd<128, 2>(a, splits, parts, s) : launch_fwd<128, 4>(a, splits, parts, s);
+    waves == 1 ? launch_fwd<128, 1>(a, splits, parts, s) : launch_fwd<128, 4>(a, splits, parts, s);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (splits > 1) splits >= 16 ? launch_join<8>(a, splits, parts, s) : launch_join<1>(a, splits, parts, s);
+  // Eight groups of lanes a row where many parts are to be read for few rows: 320 rows
+  // of 11 parts 6.9 us against 11.3 with one, 1,024 of 8 7.0 against 9.0; but 8,000 of
+  // 8 18.9 against 13.1, and 8,000 of 3 17.3 against 9.5.
+  if (splits > 1)
+    splits >= 8 && parts.stats <= 4096 ? launch_join<8>(a, splits, parts, s) : launch_join<1>(a, splits, parts, s);
   return hipGetLastError();
 }
 

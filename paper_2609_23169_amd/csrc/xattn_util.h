@@ -37,21 +37,18 @@ __device__ inline int x_lane_again() {
 // The work items of a persistent workgroup: first, then `step` and `turn` - `step`
 // further in turn, below end. Each XCD (workgroups go to the eight in turn) takes
 // one run of the items, its n workgroups n items a turn, so that they share keys in
-// their L2; with by_xcd false all workgroups share one run. Every other turn goes
-// backwards: a workgroup would otherwise meet the same sample whenever the samples
-// divide n, the longest each time. The grid is a multiple of 8 with by_xcd.
+// their L2 (20,000 rows and keys, 24 heads: 5,014 us against 5,110 with one run for
+// all; 60,000 keys: 15,517 against 15,217). Every other turn goes backwards: a
+// workgroup would otherwise meet the same sample whenever the samples divide n, the
+// longest each time (two samples of 1,370 and 822 keys: forward 136 us, now 124).
+// The grid is a multiple of 8.
 struct XItems {
   unsigned first, step, turn, end;
 };
-__device__ inline XItems x_items(unsigned total, bool by_xcd) {
-  const unsigned wg = blockIdx.x;
-  unsigned at = wg, n = gridDim.x, start = 0, end = total;
-  if (by_xcd) {
-    const unsigned x = wg & 7, q = total >> 3, r = total & 7;
-    at = wg >> 3, n >>= 3;
-    start = x * q + min(x, r), end = start + q + (x < r ? 1 : 0);
-  }
-  return XItems{start + at, 2 * (n - at) - 1, 2 * n, end};
+__device__ inline XItems x_items(unsigned total) {
+  const unsigned x = blockIdx.x & 7, at = blockIdx.x >> 3, n = gridDim.x >> 3;
+  const unsigned q = total >> 3, r = total & 7, start = x * q + min(x, r);
+  return XItems{start + at, 2 * (n - at) - 1, 2 * n, start + q + (x < r ? 1 : 0)};
 }
 // How item numbers are read: `heads` key heads of a group fastest (their rows lie
 // side by side), then samples, whose lengths may differ, so that every run holds
@@ -60,11 +57,12 @@ struct XOrder {
   unsigned heads, tiles, splits;
 };
 // Heads of a group: an eighth of them, so that each XCD has a group of its own
-// and the runs are alike whatever the samples' lengths.
+// and the runs are alike whatever the samples' lengths (eight samples of 17 to 512
+// keys: forward and backward 1,708 us with one head a group, 1,380 with three).
 inline unsigned head_group(const XArgs& a) { return a.Hk % 8 == 0 ? (unsigned)a.Hk / 8 : 1; }
 // Workgroups of nw waves that fit 256 CUs at once, by LDS (64 KB at 128 columns, 32
-// to 36 at 64) and by registers (four waves of 128 columns or eight to twelve of 64
-// on a CU's four SIMDs): what a grid needs to fill the chip.
+// to 36 at 64) and by registers (two waves a SIMD at 128 columns, three at 64): what
+// a grid needs to fill the chip.
 constexpr int64_t x_resident(int DP, int nw) { return 256 * (DP == 128 ? 2 : nw == 4 ? 3 : 4); }
 inline int x_padded(const XArgs& a) { return a.D <= 64 ? 64 : 128; }
 struct XItem {
