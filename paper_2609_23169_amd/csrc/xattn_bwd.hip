@@ -156,6 +156,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       };
 #pragma unroll
       for (int n = 0; n < kAhead; ++n) op[n] = read_op(n);
+      // a wave in its products goes before one in its vector work (dQ of 77,060 queries on 512 keys
+      // 820 -> 793 us; the other way round 823)
+      __builtin_amdgcn_s_setprio(1);
       pin_order();
       auto product = [&](int n) __attribute__((always_inline)) {
         if (n & 1) dp = mfma32(op[n % kAhead], doop[n >> 1], dp);
@@ -177,6 +180,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
           pin_order();
         }
       }
+      __builtin_amdgcn_s_setprio(0);
       const float ls = l2, nd = ndl;
       if (kt == 1 && swap) load_rows(seq.item(seq.at, order), ex);   // uniform
       if (bits != ~(uint64_t)0) {             // uniform
@@ -208,6 +212,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       };
 #pragma unroll
       for (int dt = 0; dt < kPre; ++dt) op[dt] = read_kt(dt);
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         dq[dt][0] = mfma16(op[dt % kPre], __builtin_bit_cast(bf16x8, pq[0]), dq[dt][0]);
@@ -215,6 +220,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
         if (dt + kPre < DT) op[dt % kPre] = read_kt(dt + kPre);
         pin_order();
       }
+      __builtin_amdgcn_s_setprio(0);
     }
   };
   // delta of rows whose keys all lie in one tile, as rowsum(P o dP) in fp32: with few
@@ -417,8 +423,13 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
       // (77,060 rows, 512 keys, 24 heads: 920 -> 875 us); at 64 there are three, and
       // the compiler's own order is the faster one (192 us against 201).
       constexpr int kAhead = 3, kPre = 3;
+      // Likewise a wave in its vector work goes before one in its products (856 -> 830;
+      // the other way round 845; at 64 188 -> 195, so not there).
       auto hold = []() __attribute__((always_inline)) {
         if constexpr (DP == 128) pin_order();
+      };
+      auto vector_first = [](bool on) __attribute__((always_inline)) {
+        if constexpr (DP == 128) on ? __builtin_amdgcn_s_setprio(1) : __builtin_amdgcn_s_setprio(0);
       };
       int ro = roff0, rt = rtr0;
       if constexpr (DP == 128) {   // at 64 the offsets fit into registers of their own
@@ -434,6 +445,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
       };
 #pragma unroll
       for (int ks = 0; ks < kAhead; ++ks) read_ops(ks);
+      vector_first(false);
       hold();
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
@@ -443,6 +455,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
         if (ks + kAhead < KS) read_ops(ks + kAhead);
         hold();
       }
+      vector_first(true);
       auto read_tr = [&](int dt) __attribute__((always_inline)) {
         bf16x8* const to = op + 2 * (dt % kPre);
         const int off = rt ^ (32 * dt);
@@ -478,6 +491,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
         pd[0][v] = r1[0];
         pd[1][v] = r1[1];
       }
+      vector_first(false);
       hold();
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
@@ -490,6 +504,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
         if (dt + kPre < DT) read_tr(dt + kPre);
         hold();
       }
+      vector_first(true);
     };
     int head = s_begin / ttiles, tt = s_begin - head * ttiles;
     auto advance = [&]() __attribute__((always_inline)) {

@@ -187,7 +187,11 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
 #pragma unroll
     for (int n = 0; n < kAhead; ++n) kop[n] = read_k(n);
     pin_order();
-    // S^T of half 0, its K operands read kAhead products before their use
+    // S^T of half 0, its K operands read kAhead products before their use. Between here
+    // and the last products a wave goes before one in these two phases, which have no
+    // vector work (image case 1,071 -> 1,062 us, training forward 567 -> 557; the other
+    // way round 1,070 and 562).
+    __builtin_amdgcn_s_setprio(0);
     s[0] = f32x16{};
     if (loads) {   // uniform
 #pragma unroll
@@ -206,6 +210,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
         pin_order();
       }
     }
+    __builtin_amdgcn_s_setprio(1);
     prepare(0);
     pin_order();
     // S^T of half 1 beside the exponentials of half 0
@@ -241,6 +246,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       pin_order();
     }
     settle(1);
+    __builtin_amdgcn_s_setprio(0);
     pin_order();
 #pragma unroll
     for (int n = 0; n < DT; ++n) {
@@ -250,6 +256,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       if (n + kPre < DT) vop[n % kPre] = read_v(DT + n + kPre);
       pin_order();
     }
+    __builtin_amdgcn_s_setprio(1);
   };
 
   // O = O^T / l, LSE = (m + log2 l) ln 2; a row without keys: 0 and -inf.
