@@ -562,20 +562,30 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
 }
 
 // ---------------------------------------------------------------------------
-// join: out[token][row of the token's heads] = the sum of the splits, in order.
-// Four elements a thread; tokens of no sample are left as they are.
+// join: out[token][row of the token's heads] = the sum of the parts, in order, of up
+// to three tensors in one launch. Four elements a thread; tokens of no sample are
+// left as they are.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void xattn_sum_kernel(const float* __restrict__ part, int splits, int64_t T, int width,
-                                                        __bf16* __restrict__ out, int stride,
-                                                        const int32_t* __restrict__ cu, int B, int N) {
-  const int64_t total = T * width, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+struct Join {
+  const float* part;   // [parts][T][width]
+  int parts;
+  int64_t T;
+  int width;
+  void* out;
+  int stride;
+  const int32_t* cu;   // [B + 1], or null
+  int N;               // most tokens of a sample
+};
+__global__ __launch_bounds__(256) void xattn_sum_kernel(const Join j0, const Join j1, const Join j2, int B) {
+  const Join j = blockIdx.y == 0 ? j0 : blockIdx.y == 1 ? j1 : j2;
+  const int64_t total = j.T * j.width, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= total) return;
-  const int64_t tok = i / width;
-  if (cu && !in_sample(cu, T, B, N, tok)) return;
+  const int64_t tok = i / j.width;
+  if (j.cu && !in_sample(j.cu, j.T, B, j.N, tok)) return;
   f32x4 x = f32x4{};
 #pragma unroll 4
-  for (int s = 0; s < splits; ++s) x += *reinterpret_cast<const f32x4*>(part + s * total + i);
-  *reinterpret_cast<bf16x4*>(out + tok * stride + (i - tok * width)) =
+  for (int s = 0; s < j.parts; ++s) x += *reinterpret_cast<const f32x4*>(j.part + s * total + i);
+  *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(j.out) + tok * j.stride + (i - tok * j.width)) =
       bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
 }
 
@@ -602,7 +612,7 @@ int64_t dkdv_groups(const XArgs& a) {
 }
 // As many parts as fit the chip at once, of four tiles or eight steps at least: at 300
 // queries and keys, 8 heads of 64, half of that takes dQ from 14.9 to 13.0 us and dK/dV
-// from 14.5 to 11.7, and their joins add 19.
+// from 14.5 to 11.7, and their join adds 7.
 int dq_splits(const XArgs& a) {
   const int64_t groups = dq_groups(a), tiles = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
   return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), kDqWaves) / groups, tiles / 4));
@@ -636,38 +646,43 @@ void launch_dkdv(const XArgs& a, const float* aux, int splits, float* part, hipS
   hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), dim3((unsigned)(dkdv_groups(a) * splits + 7) / 8 * 8), dim3(256), 0, s,
                      a, aux, order, part);
 }
-void launch_sum(const float* part, int splits, int64_t T, int width, void* out, int stride, const int32_t* cu, int B,
-                int N, hipStream_t s) {
-  if (T == 0) return;
+void launch_sums(const Join* j, int n, int B, hipStream_t s) {
+  int64_t most = 0;
+  for (int i = 0; i < n; ++i) most = std::max(most, j[i].T * j[i].width);
+  if (most == 0) return;
   TraceScope ts_(s, "xattn_sum");
-  hipLaunchKernelGGL(xattn_sum_kernel, dim3((unsigned)((T * width / 4 + 255) / 256)), dim3(256), 0, s, part, splits, T,
-                     width, static_cast<__bf16*>(out), stride, cu, B, N);
+  hipLaunchKernelGGL(xattn_sum_kernel, dim3((unsigned)((most / 4 + 255) / 256), (unsigned)n), dim3(256), 0, s, j[0],
+                     j[n > 1 ? 1 : 0], j[n > 2 ? 2 : 0], B);
 }
 
 }  // namespace
 
-size_t xattn_bwd_workspace(const XArgs& a) { return aux_bytes(a) + std::max(dq_part(a), dkdv_part(a)); }
+size_t xattn_bwd_workspace(const XArgs& a) { return aux_bytes(a) + dq_part(a) + dkdv_part(a); }
 
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
   float* const aux = static_cast<float*>(workspace);
-  float* const part = reinterpret_cast<float*>(static_cast<char*>(workspace) + aux_bytes(a));   // both joins' in turn
+  float* const qpart = reinterpret_cast<float*>(static_cast<char*>(workspace) + aux_bytes(a));
+  float* const kpart = qpart + dq_part(a) / sizeof(float);
+  Join joins[3];
+  int n = 0;
   if (dq_groups(a) > 0) {
-    const int n = dq_splits(a);
-    float* const p = n > 1 ? part : nullptr;
-    a.D <= 64 ? launch_dq<64>(a, aux, n, p, s) : launch_dq<128>(a, aux, n, p, s);
+    const int splits = dq_splits(a);
+    float* const p = splits > 1 ? qpart : nullptr;
+    a.D <= 64 ? launch_dq<64>(a, aux, splits, p, s) : launch_dq<128>(a, aux, splits, p, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (n > 1) launch_sum(part, n, a.Tq, a.Hq * a.D, a.dq, a.sdq, a.cuq, a.B, a.Nq, s);
+    if (p) joins[n++] = Join{p, splits, a.Tq, a.Hq * a.D, a.dq, a.sdq, a.cuq, a.Nq};
   }
   if (dkdv_groups(a) > 0) {
-    const int n = dkdv_splits(a);
-    float* const p = n > 1 ? part : nullptr;
-    a.D <= 64 ? launch_dkdv<64>(a, aux, n, p, s) : launch_dkdv<128>(a, aux, n, p, s);
+    const int splits = dkdv_splits(a);
+    float* const p = splits > 1 ? kpart : nullptr;
+    a.D <= 64 ? launch_dkdv<64>(a, aux, splits, p, s) : launch_dkdv<128>(a, aux, splits, p, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (n > 1) {
-      launch_sum(part, n, a.Tk, a.Hk * a.D, a.dk, a.sdk, a.cuk, a.B, a.Nk, s);
-      launch_sum(part + (size_t)n * a.Tk * a.Hk * a.D, n, a.Tk, a.Hk * a.D, a.dv, a.sdv, a.cuk, a.B, a.Nk, s);
+    if (p) {
+      joins[n++] = Join{p, splits, a.Tk, a.Hk * a.D, a.dk, a.sdk, a.cuk, a.Nk};
+      joins[n++] = Join{p + (size_t)splits * a.Tk * a.Hk * a.D, splits, a.Tk, a.Hk * a.D, a.dv, a.sdv, a.cuk, a.Nk};
     }
   }
+  if (n > 0) launch_sums(joins, n, a.B, s);
   return hipGetLastError();
 }
 
