@@ -931,11 +931,8 @@ ut_status xattn_fwd(const char* fn, XArgs& a, const void* q, const void* k, cons
   UT_TRY(check_space(fn, xattn_fwd_workspace(a), workspace, workspace_bytes));
   a.q = q, a.k = k, a.v = v, a.o = o, a.lse = lse, a.mask = key_mask;
   if (a.Tq == 0) return UT_OK;
-  if (zero_rest) {
-    const XClear c{a.cuq, a.Tq, a.Hq * a.D, o, a.so};
-    UT_TRY(check_hip(launch_xattn_clear(&c, 1, a.B, lse, a.Hq, stream), "clear launch"));
-  }
-  if (a.Nq == 0) return UT_OK;
+  a.zero_rest = zero_rest;
+  if (a.Nq == 0 && !zero_rest) return UT_OK;
   return check_hip(launch_xattn_fwd(a, workspace, stream), "cross attention launch");
 }
 
@@ -952,12 +949,7 @@ ut_status xattn_bwd(const char* fn, XArgs& a, const void* q, const void* k, cons
   a.q = q, a.k = k, a.v = v, a.o_in = o, a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv;
   a.lse = const_cast<float*>(lse), a.mask = key_mask;
   if (a.Tq == 0 && a.Tk == 0) return UT_OK;
-  if (zero_rest) {   // a side without tokens has no rows
-    const XClear c[] = {{a.cuq, a.Tq, a.Hq * a.D, dq, a.sdq},
-                        {a.cuk, a.Tk, a.Hk * a.D, dk, a.sdk},
-                        {a.cuk, a.Tk, a.Hk * a.D, dv, a.sdv}};
-    UT_TRY(check_hip(launch_xattn_clear(c, 3, a.B, nullptr, 0, stream), "clear launch"));
-  }
+  a.zero_rest = zero_rest;
   return check_hip(launch_xattn_bwd(a, workspace, stream), "cross attention backward launch");
 }
 

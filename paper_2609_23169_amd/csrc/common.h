@@ -218,6 +218,7 @@ struct XArgs {
   int B, Nq, Nk, Hq, Hk, G, D;     // G = Hq / Hk
   int sq, sk, sv, so, sdo, sdq, sdk, sdv;
   float scale;
+  bool zero_rest;                  // packed: rows behind the last sample become 0
 };
 // Bytes of the partial results where the keys (forward, dQ) or the query tokens
 // (dK, dV) are split over workgroups, and of the backward's row statistics.
@@ -225,15 +226,5 @@ size_t xattn_fwd_workspace(const XArgs& a);
 hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s);
 size_t xattn_bwd_workspace(const XArgs& a);
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s);
-// n <= 3 tensors' packed rows at and past the last sample's end to 0, and lse
-// [H, T] there (unless null; of the first's samples) to -inf.
-struct XClear {
-  const int32_t* cu;   // [B + 1]
-  int64_t T;           // tokens
-  int width;           // elements of a token
-  void* x;
-  int stride;
-};
-hipError_t launch_xattn_clear(const XClear* t, int n, int B, float* lse, int H, hipStream_t s);
 
 }  // namespace ut

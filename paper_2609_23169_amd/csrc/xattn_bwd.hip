@@ -60,6 +60,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
+  if (a.zero_rest) x_clear_rest(a.cuq, a.B, a.Tq, a.Hq * a.D, a.dq, a.sdq);
+
   bf16x8 qop[KS], doop[KS];   // Q and dO (operands, once turned)
   float lse2, l2, ndl;        // the row's LSE log2 e, that less log2(scale), and -delta
   // What only the statistics need: O as loaded, and LSE. (Set between a change of
@@ -340,6 +342,10 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
+  if (a.zero_rest) {
+    x_clear_rest(a.cuk, a.B, a.Tk, a.Hk * a.D, a.dk, a.sdk);
+    x_clear_rest(a.cuk, a.B, a.Tk, a.Hk * a.D, a.dv, a.sdv);
+  }
   const XItems items = x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk);
   if (items.first >= items.end) return;
   const XItem at = x_item(items.first, (unsigned)a.B, order);
@@ -589,22 +595,6 @@ __global__ __launch_bounds__(256) void xattn_sum_kernel(const Join j0, const Joi
       bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
 }
 
-// Rows at and past the last sample's end become 0 (statistics: -inf), of up to three
-// tensors in one launch.
-__global__ __launch_bounds__(256) void xattn_clear_kernel(const XClear t0, const XClear t1, const XClear t2, int B,
-                                                          float* __restrict__ lse, int H) {
-  const XClear t = blockIdx.y == 0 ? t0 : blockIdx.y == 1 ? t1 : t2;
-  const int64_t end = min(max((int64_t)t.cu[B], (int64_t)0), t.T);
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
-  const int per = t.width / 8;
-  for (int64_t i = end * per + at; i < t.T * per; i += step) {
-    const int64_t tok = i / per;
-    *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(t.x) + tok * t.stride + 8 * (i - tok * per)) = bf16x8{};
-  }
-  if (lse && blockIdx.y == 0)
-    for (int64_t i = at; i < (t.T - end) * H; i += step) lse[i / (t.T - end) * t.T + end + i % (t.T - end)] = -INFINITY;
-}
-
 int64_t dq_tiles(const XArgs& a) { return ((int64_t)a.Nq * a.G + 32 * kDqWaves - 1) / (32 * kDqWaves); }
 int64_t dq_groups(const XArgs& a) { return (int64_t)a.B * a.Hk * dq_tiles(a); }
 int64_t dkdv_groups(const XArgs& a) {
@@ -635,7 +625,7 @@ template <int DP>
 void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)dq_tiles(a), (unsigned)splits};
   const int64_t items = dq_groups(a) * splits;
-  const dim3 grid((unsigned)(std::min<int64_t>(items, x_resident(DP, kDqWaves)) + 7) / 8 * 8);
+  const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, kDqWaves)) + 7) / 8 * 8);
   TraceScope ts_(s, "xattn_dq", DP);
   hipLaunchKernelGGL((xattn_dq_kernel<DP>), grid, dim3(64 * kDqWaves), 0, s, a, aux, order, part);
 }
@@ -643,7 +633,7 @@ template <int DP>
 void launch_dkdv(const XArgs& a, const float* aux, int splits, float* part, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys), (unsigned)splits};
   TraceScope ts_(s, "xattn_dkdv", DP);
-  hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), dim3((unsigned)(dkdv_groups(a) * splits + 7) / 8 * 8), dim3(256), 0, s,
+  hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), dim3((unsigned)(std::max<int64_t>(dkdv_groups(a) * splits, 1) + 7) / 8 * 8), dim3(256), 0, s,
                      a, aux, order, part);
 }
 void launch_sums(const Join* j, int n, int B, hipStream_t s) {
@@ -665,14 +655,14 @@ hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
   float* const kpart = qpart + dq_part(a) / sizeof(float);
   Join joins[3];
   int n = 0;
-  if (dq_groups(a) > 0) {
+  if (dq_groups(a) > 0 || (a.zero_rest && a.Tq > 0)) {
     const int splits = dq_splits(a);
     float* const p = splits > 1 ? qpart : nullptr;
     a.D <= 64 ? launch_dq<64>(a, aux, splits, p, s) : launch_dq<128>(a, aux, splits, p, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p) joins[n++] = Join{p, splits, a.Tq, a.Hq * a.D, a.dq, a.sdq, a.cuq, a.Nq};
   }
-  if (dkdv_groups(a) > 0) {
+  if (dkdv_groups(a) > 0 || (a.zero_rest && a.Tk > 0)) {
     const int splits = dkdv_splits(a);
     float* const p = splits > 1 ? kpart : nullptr;
     a.D <= 64 ? launch_dkdv<64>(a, aux, splits, p, s) : launch_dkdv<128>(a, aux, splits, p, s);
@@ -683,13 +673,6 @@ hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
     }
   }
   if (n > 0) launch_sums(joins, n, a.B, s);
-  return hipGetLastError();
-}
-
-hipError_t launch_xattn_clear(const XClear* t, int n, int B, float* lse, int H, hipStream_t s) {
-  TraceScope ts_(s, "xattn_clear");
-  hipLaunchKernelGGL(xattn_clear_kernel, dim3(256, (unsigned)n), dim3(256), 0, s, t[0], t[n > 1 ? 1 : 0], t[n > 2 ? 2 : 0], B,
-                     lse, H);
   return hipGetLastError();
 }
 

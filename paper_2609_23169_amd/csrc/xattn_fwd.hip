@@ -63,6 +63,13 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
+  if (a.zero_rest) {   // here, not in a launch of its own, which costs 6 us
+    x_clear_rest(a.cuq, a.B, a.Tq, a.Hq * a.D, a.o, a.so);
+    const int64_t end = min(max((int64_t)x_cu(a.cuq, a.B), (int64_t)0), a.Tq), rest = a.Tq - end;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + tid; i < rest * a.Hq; i += (int64_t)gridDim.x * blockDim.x)
+      a.lse[i / rest * a.Tq + end + i % rest] = -INFINITY;
+  }
+
   // Q operand (B of S^T = K Q^T), once turned: lane holds Q[row][16 ks + 8 g .. +7].
   bf16x8 qop[KS];
   auto load_rows = [&](const XItem& at) __attribute__((always_inline)) {
@@ -431,7 +438,7 @@ template <int DP, int NW>
 void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
   const int64_t items = (int64_t)a.B * a.Hk * order.tiles * splits;
-  const dim3 grid((unsigned)(std::min<int64_t>(items, x_resident(DP, NW)) + 7) / 8 * 8);
+  const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, NW)) + 7) / 8 * 8);
   TraceScope ts_(s, splits > 1 ? "xattn_fwd_split" : "xattn_fwd", DP, NW);
   if (splits > 1) {
     hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, true>), grid, dim3(64 * NW), 0, s, a, order, parts);

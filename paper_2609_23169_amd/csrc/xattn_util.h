@@ -179,6 +179,17 @@ __device__ inline bool in_sample(const int32_t* __restrict__ cu, int64_t T, int 
   return false;
 }
 
+// Rows of x at and past the last sample's end to 0, the grid's threads in turn.
+__device__ inline void x_clear_rest(const int32_t* cu, int B, int64_t T, int width, void* x, int stride) {
+  const int64_t end = min(max((int64_t)x_cu(cu, B), (int64_t)0), T);
+  const int per = width / 8;
+  for (int64_t i = end * per + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < T * per;
+       i += (int64_t)gridDim.x * blockDim.x) {
+    const int64_t tok = i / per;
+    *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(x) + tok * stride + 8 * (i - tok * per)) = bf16x8{};
+  }
+}
+
 // The tiles of a persistent workgroup's items as one sequence. The items are worked
 // out kTurns at a time, one a lane, so that a change of item costs some readlanes in
 // place of three divisions, and the scalar registers are left to the loop over the

@@ -454,6 +454,21 @@ def test_many_short_samples(B, Hq, Hk, D):
     assert (got - want_lse)[live].abs().max() < 1e-4
 
 
+@pytest.mark.parametrize("lq,lk", [([0, 0], [30, 4]), ([30, 9], [0, 0]), ([0], [0])])
+def test_varlen_sides_without_tokens(lq, lk):
+    """All rows of an empty side lie behind the last sample."""
+    q, k, v, do, _ = packed(22, lq, lk, 4, 2, 64, rest=21)
+    at = (offsets(lq), max(lq), offsets(lk), max(lk))
+    for _ in range(2):   # old values in the memory that the allocator hands out
+        junk = [torch.full_like(x, 3.0) for x in (q, q, k, v)]
+        del junk
+        o, lse = ut.xattn_fwd_varlen(q, k, v, *at, 0.125)
+        dq, dk, dv = ut.xattn_bwd_varlen(q, k, v, o, do, lse, *at, 0.125)
+        for x in (o, dq, dk, dv):
+            assert (x == 0).all()
+        assert (lse == -math.inf).all()
+
+
 def test_bad_offsets_reach_nothing_outside():
     """Offsets outside the tensors are clamped (and refused in validate mode)."""
     q, k, v, do, _ = packed(23, [50, 50], [40, 40], 2, 2, 64)
