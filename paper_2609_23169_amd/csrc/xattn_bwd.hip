@@ -288,12 +288,21 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       load_k.masked(rk, a.sk, seq.bits, kn, w, lane, a.D);
       load_v.masked(rv, a.sv, seq.bits, vn, w, lane, a.D);
     }
-    // before the first tile too, beside its loads: what it leaves is not used
     Extra ex;
-    step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, ex, all, [&](int u) __attribute__((always_inline)) {
+    auto load = [&](int u) __attribute__((always_inline)) {
       if (u < Load::IPW) load_k.one(rk, a.sk, kn, w, u, a.D);
       else load_v.one(rv, a.sv, vn, w, u - Load::IPW, a.D);
-    });
+    };
+    // At 128 columns before the first tile too, beside its loads: what it leaves is not
+    // used, and a branch around it would spill 29 registers.
+    if (DP == 128 || have) {
+      step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, ex, all, load);
+    } else {
+      if (all)
+#pragma unroll
+        for (int u = 0; u < 2 * Load::IPW; ++u) load(u);
+      load_rows(seq.item(seq.at, order), ex);
+    }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (changed) {
