@@ -26,11 +26,11 @@
 // column of its own, whatever it holds, and is stored as 0; waves whose 32 keys
 // are all unused only load.
 //
-// What bounds it (77,060 queries, 512 keys, 24 heads of 128: dQ 807 us, dK/dV 846,
-// 900 and 1,150 TFLOP/s of the products that they form): the matrix cores are 41 and
-// 55% busy, vector work and LDS reads fill most of the rest, and the board's power
-// limit sets the clock (1.85 of 2.4 GHz): with rows of zeros the same instructions
-// run 17% faster. dQ also moves 1.9 GB, 0.39 ms at the copy rate, beside it.
+// What bounds it (77,060 queries, 512 keys, 24 heads of 128: dQ 795 us, dK/dV 840,
+// 915 and 1,150 TFLOP/s of the products that they form): the matrix cores are 44 and
+// 57% busy, vector work and LDS reads fill most of the rest, and the board's power
+// limit sets the clock (1.8 to 1.9 of 2.4 GHz): with rows of zeros the same
+// instructions run 17% faster. dQ also moves 1.9 GB, 0.39 ms at the copy rate, beside it.
 #include <algorithm>
 #include <type_traits>
 

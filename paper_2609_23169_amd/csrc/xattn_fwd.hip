@@ -24,13 +24,13 @@
 // unequal samples) took 56.5 + 8.2 us against 52.5 + 6.7 at 4 x 32 query heads on
 // 16,391 keys.
 //
-// What bounds it: 22,879 queries on 4,097 keys, 24 heads of 128, take 1,092 us, 1,055
-// TFLOP/s: matrix cores 49% busy, vector work 43%, LDS reads (a wave reads the tile
-// for its 32 rows) about as long as the products, at the clock that the board's power
-// limit leaves (1.7 of 2.4 GHz; rows of zeros run 16% faster). 77,586 queries on 512
-// keys take 567 us, 861 TFLOP/s: a change of item every eight tiles (about 5,000 of
-// 37,000 cycles) and 0.19 ms of rows at the copy rate come on top. One query each of
-// 32 heads on 16,391 keys: 4.3 TB/s.
+// What bounds it: 22,879 queries on 4,097 keys, 24 heads of 128, take 1,060 to 1,080
+// us, 1,070 TFLOP/s: matrix cores 51% busy, vector work 43%, LDS reads (a wave reads
+// the tile for its 32 rows) about as long as the products, at the clock that the
+// board's power limit leaves (1.75 of 2.4 GHz; rows of zeros run 16% faster). 77,586
+// queries on 512 keys take 560 us, 870 TFLOP/s: a change of item every eight tiles
+// (about 5,000 of 37,000 cycles) and 0.19 ms of rows at the copy rate come on top. One
+// query each of 32 heads on 16,391 keys: 4.3 TB/s.
 #include <algorithm>
 #include <type_traits>
 
