@@ -137,11 +137,11 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       pin_value(lsum);
       pq[(e >> 2) & 1][((e & 3) >> 1) + 2 * (e >> 3)] = q;
     };
-    auto half_max = [&](int h) __attribute__((always_inline)) {
+    auto half_max = [&](int h) __attribute__((always_inline)) {   // of this lane's keys
       float mx = s[h][0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[h][e]);
-      return fmaxf(pair_max(mx) * c2, -3.0e38f);
+      return fmaxf(mx * c2, -3.0e38f);
     };
     // Before half h's exponentials: unused keys, and the item's reference.
     auto prepare = [&](int h) __attribute__((always_inline)) {
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
         for (int e = 0; e < 16; ++e) s[h][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[h][e] : -INFINITY;
       }
       if (fresh && half) {   // uniform
-        m_run = half_max(h);
+        m_run = pair_max(half_max(h));
         fresh = false;
       }
       m_use = m_run;
@@ -162,8 +162,11 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     // is inf or NaN), then P to the operand layout of two 16-row groups.
     bf16x8 pop[2];
     auto settle = [&](int h) __attribute__((always_inline)) {
-      if (__ballot(!(lsum <= kSumGuard)) != 0) {
-        const float to = fmaxf(half_max(h), m_run), alpha = fast_exp2(m_run - to);
+      const bool over = !(lsum <= kSumGuard);
+      if (__ballot(over) != 0) {
+        // from the lanes whose sum it is: other rows keep theirs, so that no row's
+        // result depends on its neighbours
+        const float to = fmaxf(pair_max(over ? half_max(h) : -3.0e38f), m_run), alpha = fast_exp2(m_run - to);
         l_run *= alpha;
         m_run = m_use = to;
         const auto ar = __builtin_amdgcn_permlane16_swap(__float_as_uint(alpha), __float_as_uint(alpha), false, false);

@@ -209,6 +209,20 @@ def test_unused_keys_may_hold_anything(Nq, Nk, bad):
     assert (b[2][1][off] == 0).all() and (b[2][2][off] == 0).all()
 
 
+def test_a_bad_query_row_stays_its_own():
+    q, k, v, do = draw(14, 1, 200, 150, 4, 2, 128)
+    want = run(q, k, v, do, 0.1, None)
+    for bad in (float("nan"), float("inf")):
+        q2 = q.clone()
+        q2[0, 77, 1] = bad
+        o, lse = ut.xattn_fwd(q2, k, v, 0.1)
+        dq = ut.xattn_bwd(q2, k, v, o, do, lse, 0.1)[0]
+        others = torch.ones(200, 4, dtype=torch.bool, device=DEV)
+        others[77, 1] = False
+        assert torch.equal(o[0][others], want[0][0][others]) and torch.equal(dq[0][others], want[2][0][0][others])
+        assert torch.equal(lse[0].T[others], want[1][0].T[others])
+
+
 def test_masks_at_any_address_and_as_bool():
     q, k, v, do = draw(7, 1, 30, 1111, 2, 2, 64)
     m = make_mask("random", 1, 1111, 9)
@@ -502,6 +516,23 @@ def test_equal_results_on_every_run_and_on_a_side_stream(Nq, Nk):
     b = run(q, k, v, do, 0.1, None, stream=side)
     for x, y in zip((a[0], a[1]) + a[2], (b[0], b[1]) + b[2]):
         assert torch.equal(x, y)
+
+
+def test_two_calls_at_once():
+    """On two streams, each with workspaces of its own: what they write stays their own."""
+    data = [draw(33 + i, 2, Nq, Nk, 4, 2, 64 + 64 * i) for i, (Nq, Nk) in enumerate([(3000, 130), (30, 4000)])]
+    want = [run(*d, 0.1, None) for d in data]
+    sides = [torch.cuda.Stream() for _ in data]
+    got = [[], []]
+    for _ in range(4):
+        for i, (q, k, v, do) in enumerate(data):
+            o, lse = ut.xattn_fwd(q, k, v, 0.1, stream=sides[i])
+            got[i].append((o, lse) + tuple(ut.xattn_bwd(q, k, v, o, do, lse, 0.1, stream=sides[i])))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            for x, y in zip(g, (want[i][0], want[i][1]) + tuple(want[i][2])):
+                assert torch.equal(x, y)
 
 
 @pytest.mark.parametrize("Nq,Nk", [(1, 5000), (600, 100), (77, 130)])
