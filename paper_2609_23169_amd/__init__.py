@@ -497,20 +497,21 @@ class _Args:
         """Host array of the strides, NULL where all rows lie back to back."""
         return None if self.plain else (ctypes.c_int64 * len(self.strides))(*self.strides)
 
-    def call(self, fn, args, workspace, stream):
+    def call(self, fn, args, workspace, stream, takes_workspace=True):
         """fn(*args, workspace, its bytes, stream) on the tensors' device."""
-        ws, bytes_ = None, 0
-        if workspace is not None:
-            if not workspace.is_contiguous():
-                raise ValueError("workspace must be contiguous")
-            ws, bytes_ = self.ptr(workspace, "workspace"), _nbytes(workspace)
         s = stream if stream is not None else torch.cuda.current_stream(self.device)
         if s.device_index != self.device:
             raise ValueError("the stream belongs to another device than the tensors")
+        if workspace is not None:
+            if not workspace.is_contiguous():
+                raise ValueError("workspace must be contiguous")
+            args += (self.ptr(workspace, "workspace"), _nbytes(workspace))
+        elif takes_workspace:
+            args += (None, 0)
         if torch.cuda.current_device() == self.device:
-            return fn(*args, ws, bytes_, s.cuda_stream)
+            return fn(*args, s.cuda_stream)
         with torch.cuda.device(self.device):
-            return fn(*args, ws, bytes_, s.cuda_stream)
+            return fn(*args, s.cuda_stream)
 
 
 def _like(t, like, name: str):
@@ -554,8 +555,7 @@ def ut_qk_rope_fwd(q, k, q_out, k_out, pos, axis_dims, theta: float, token_idx=N
                    a.ptr(token_idx, "token_idx"), axes, len(axis_dims), theta,
                    UT_ROPE_NEAR if interleaved else UT_ROPE_FAR, a.ptr(q_weight, "q_weight"),
                    a.ptr(k_weight, "k_weight"), wd, eps)
-    fn = lib().ut_qk_rope_fwd
-    return a.call(lambda *x: fn(*x[:-3], x[-1]), args, None, stream)   # it takes no workspace
+    return a.call(lib().ut_qk_rope_fwd, args, None, stream, takes_workspace=False)
 
 
 def ut_qk_rope_bwd_workspace_size(D: int) -> int:

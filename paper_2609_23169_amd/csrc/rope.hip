@@ -339,11 +339,16 @@ hipError_t launch_qk_rope(const RopeShape& sh, const RopeSide (&side)[2], bool b
     a.n_axes = sh.n_axes;
     a.eps = sh.eps;
     a.w_bf16 = sh.w_bf16;
-    for (int x = 0; x < sh.n_axes; ++x)
-      for (int i = 0; i < sh.dims[x] / 2; ++i) {
+    for (int x = 0; x < sh.n_axes; ++x) {
+      // one power an axis: the products are off by at most 128 steps of 2^-53, and 64
+      // powers would take the call longer than its launch
+      const double ratio = std::pow(sh.theta, -2.0 / sh.dims[x]);
+      double rev = 1 / (2 * 3.14159265358979323846);
+      for (int i = 0; i < sh.dims[x] / 2; ++i, rev *= ratio) {
         a.axis[a.half] = (uint8_t)x;
-        a.rev[a.half++] = std::pow(sh.theta, -2.0 * i / sh.dims[x]) / (2 * 3.14159265358979323846);
+        a.rev[a.half++] = rev;
       }
+    }
     wgs = sh.bf16 ? launch_t<__bf16>(a, sh.far_pairs, norm, bwd, s) : launch_t<float>(a, sh.far_pairs, norm, bwd, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
