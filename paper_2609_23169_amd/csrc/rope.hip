@@ -121,7 +121,7 @@ __device__ inline float lanes_sum(float x) {
 template <typename T, int P2, bool FAR, bool NORM, bool BWD>
 __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs a) {
   constexpr int kSlots = kThreads / P2;
-  constexpr int U = sizeof(T) == 2 ? (BWD && NORM ? 2 : 4) : (BWD && NORM ? 1 : 2);
+  constexpr int U = sizeof(T) == 2 ? 2 : 1;   // rows of 16 or 32 bytes a lane in flight; more cost occupancy
   __shared__ float2 table[kTable];
   const int tid = threadIdx.x, slot = tid / P2, j = tid % P2;
   const int H = a.side[0].H + a.side[1].H, lph = a.D / 8;
@@ -163,6 +163,15 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs a) {
     }
     __syncthreads();
 
+    // The turn's first rows, scalar; a row from there is one 64-bit multiply-add.
+    const T *x0 = static_cast<const T*>(a.side[0].x) + t0 * a.side[0].sx,
+            *x1 = static_cast<const T*>(a.side[1].x) + t0 * a.side[1].sx,
+            *dy0 = static_cast<const T*>(a.side[0].dy) + t0 * a.side[0].sdy,
+            *dy1 = static_cast<const T*>(a.side[1].dy) + t0 * a.side[1].sdy;
+    T *out0 = static_cast<T*>(a.side[0].out) + t0 * a.side[0].so, *out1 = static_cast<T*>(a.side[1].out) + t0 * a.side[1].so;
+    const int sx0 = (int)a.side[0].sx, sx1 = (int)a.side[1].sx, sdy0 = (int)a.side[0].sdy, sdy1 = (int)a.side[1].sdy,
+              so0 = (int)a.side[0].so, so1 = (int)a.side[1].so;
+
     const int items = tn * H;
     int lt = slot / H, hh = slot - lt * H;
     for (int it = slot; it < items; it += U * kSlots) {
@@ -172,14 +181,10 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs a) {
       for (int u = 0; u < U; ++u) {
         at_t[u] = lt, at_h[u] = hh;
         if (live && it + u * kSlots < items) {
-          const int s = hh >= a.side[0].H;
-          const int64_t t = t0 + lt, h = (int64_t)(hh - (s ? a.side[0].H : 0)) * a.D;
-          if constexpr (BWD)
-            cd[u].load(static_cast<const T*>(s ? a.side[1].dy : a.side[0].dy) +
-                           t * (s ? a.side[1].sdy : a.side[0].sdy) + h, o0, o1);
-          if constexpr (!BWD || NORM)
-            cx[u].load(static_cast<const T*>(s ? a.side[1].x : a.side[0].x) +
-                           t * (s ? a.side[1].sx : a.side[0].sx) + h, o0, o1);
+          const bool s = hh >= a.side[0].H;
+          const int h = (hh - (s ? a.side[0].H : 0)) * a.D;
+          if constexpr (BWD) cd[u].load((s ? dy1 : dy0) + (int64_t)lt * (s ? sdy1 : sdy0) + h, o0, o1);
+          if constexpr (!BWD || NORM) cx[u].load((s ? x1 : x0) + (int64_t)lt * (s ? sx1 : sx0) + h, o0, o1);
         }
         lt += dt, hh += dh;
         if (hh >= H) hh -= H, ++lt;
@@ -232,9 +237,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs a) {
           for (int e = 0; e < 8; ++e) y[e] = x[e];
         }
         if (live) {
-          const int64_t h = (int64_t)(at_h[u] - (s ? a.side[0].H : 0)) * a.D;
-          Chunk<T, FAR>::store(static_cast<T*>(s ? a.side[1].out : a.side[0].out) +
-                                   (t0 + at_t[u]) * (s ? a.side[1].so : a.side[0].so) + h, o0, o1, y);
+          const int h = (at_h[u] - (s ? a.side[0].H : 0)) * a.D;
+          Chunk<T, FAR>::store((s ? out1 : out0) + (int64_t)at_t[u] * (s ? so1 : so0) + h, o0, o1, y);
         }
       }
     }
@@ -281,16 +285,19 @@ __global__ __launch_bounds__(kThreads) void rope_weight_sum_kernel(const float* 
 }
 
 // Persistent workgroups, as many as fit at once (the gradients' partial rows too
-// are at most kRopeParts): at 77,586 x 48 x 128 the forward takes 404 us with the
-// 1,280 that fit, 452 with 1,024, 513 with 1,536 and 498 with one a turn. A turn
-// holds as many tokens as the table has room for, fewer where the last round would
-// be mostly idle; a turn costs about half a token's time besides.
+// are at most kRopeParts), six a CU at most: the runtime's figure leaves scalar
+// registers out, and a grid that does not fit at once ends in a second round. At
+// 77,586 x 48 x 128 the forward with the norm takes 385 us with 1,536, 409 with 1,280
+// and 462 with 2,048 (four rows in flight, of which 1,280 fit: 404); without the norm
+// 363 with 1,536 and 441 with 2,048. A turn holds as many tokens as the table has room
+// for, fewer where the last round would be mostly idle; a turn costs about half a
+// token's time besides.
 template <typename T, int P2, bool FAR, bool NORM, bool BWD>
 unsigned launch(RopeArgs& a, hipStream_t s) {
   static const int per_cu = [] {
     int n = 0;
     return hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, rope_kernel<T, P2, FAR, NORM, BWD>, kThreads, 0) ==
-                       hipSuccess && n > 0 ? n : 4;
+                       hipSuccess && n > 0 ? std::min(n, 6) : 4;
   }();
   const int64_t fit = std::min<int64_t>(256 * per_cu, BWD && NORM ? kRopeParts : 1 << 20);
   const int hp = (a.half + 3) & ~3, most = std::max(1, std::min(kMaxTok, kTable / hp));
