@@ -642,8 +642,8 @@ template <int DP>
 void launch_dkdv(const XArgs& a, const float* aux, int splits, float* part, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys), (unsigned)splits};
   TraceScope ts_(s, "xattn_dkdv", DP);
-  hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), dim3((unsigned)(std::max<int64_t>(dkdv_groups(a) * splits, 1) + 7) / 8 * 8), dim3(256), 0, s,
-                     a, aux, order, part);
+  const dim3 grid((unsigned)(std::max<int64_t>(dkdv_groups(a) * splits, 1) + 7) / 8 * 8);
+  hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), grid, dim3(256), 0, s, a, aux, order, part);
 }
 void launch_sums(const Join* j, int n, int B, hipStream_t s) {
   int64_t most = 0;
