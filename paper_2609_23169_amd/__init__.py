@@ -439,6 +439,7 @@ def ut_token_mask_from_alpha(alpha, patch: int, threshold: int, radius: int, tok
 
 # The rotary and cross-attention calls take views as well: a token's heads have
 # to be contiguous, the tokens one stride apart (a slice of a fused projection).
+# Views broadcast over tokens or samples (expand()) are refused: contiguous() them.
 # They are called once a layer on small tensors too, so their checks are written
 # to cost little where nothing is wrong.
 
@@ -451,16 +452,17 @@ def _token_stride(x, name: str) -> int:
         return row
     lead, strides = x.shape[:-2], x.stride()
     _need((D == 1 or strides[-1] == 1) and (H == 1 or strides[-2] == D), f"{name}: heads must be contiguous")
-    step, tokens = 0, 1   # stride of a token, tokens seen from the inner dimensions
+    step, tokens = None, 1   # stride of a token, tokens seen from the inner dimensions
     for n, st in zip(reversed(lead), reversed(strides[:-2])):
         if n == 1:
             continue
-        if step == 0:
+        if step is None:
             step = st
         _need(st == step * tokens, f"{name}: tokens must be evenly strided")
         tokens *= n
-    step = step or row
-    _need(step >= row, f"{name}: tokens overlap")
+    if step is None:
+        return row
+    _need(step >= row, f"{name}: tokens overlap")   # a view broadcast over its tokens has stride 0
     return step
 
 

@@ -597,3 +597,27 @@ def test_full_size_rows_of_the_2k_layer():
         x = got[0, :, h].double()
         assert (x - ref).norm() <= lim * ref.norm()
         assert (x - ref).abs().max() <= 2e-2 * ref.abs().max()
+
+
+def test_views_broadcast_over_tokens_or_samples_are_refused():
+    """Refused on the host, inputs and outputs alike; a copy of such a view is fine."""
+    q, k, v, do = draw(40, 2, 30, 20, 4, 2, 64)
+    o, lse = ut.xattn_fwd(q, k, v, 0.125)
+    flat = [x[0] for x in (q, k, v, do)]
+    at = (offsets([30]), 30, offsets([20]), 20)
+    one_q, one_k, one_do = q[:1, :1].expand(2, 1, 4, 64), k[:1, :1].expand(1, 20, 2, 64), do[:1, :1].expand(1, 30, 4, 64)
+    pos = torch.zeros(30, 1, device=DEV)
+    for call in (lambda: ut.xattn_fwd(one_q, k, v, 0.125),
+                 lambda: ut.xattn_fwd(q[:1], one_k, one_k, 0.125),
+                 lambda: ut.xattn_bwd(q[:1], k[:1], v[:1], o[:1], one_do, lse[:1], 0.125),
+                 lambda: ut.xattn_fwd_varlen(flat[0], one_k[0], flat[2], *at, 0.125),
+                 lambda: ut.xattn_bwd_varlen(*flat[:3], o[0], one_do[0], lse[0], *at, 0.125),
+                 lambda: ut.ut_xattn_fwd(q[:1], k[:1], v[:1], one_do, lse[:1], 0.125),
+                 lambda: ut.qk_rope_fwd(one_do, None, pos, (64,)),
+                 lambda: ut.qk_rope_bwd(q[0], one_do[0], pos, (64,))):
+        with pytest.raises(ValueError, match="tokens overlap"):
+            call()
+    want = ut.xattn_bwd(q[:1], k[:1], v[:1], o[:1], one_do.contiguous(), lse[:1], 0.125)
+    check_do = do[:1, :1].repeat(1, 30, 1, 1)
+    for x, y in zip(want, ut.xattn_bwd(q[:1], k[:1], v[:1], o[:1], check_do, lse[:1], 0.125)):
+        assert torch.equal(x, y)

@@ -201,3 +201,32 @@ def test_token_stride_of_views():
     for bad in (qkv[:, :5, 0], qkv[..., :32], qkv.permute(0, 1, 2, 4, 3)):
         with pytest.raises(ValueError):
             ut._token_stride(bad, "x")
+
+
+@pytest.mark.parametrize("x,msg", [
+    (_bf(1, 8, 64).expand(300, 8, 64), "tokens overlap"),              # one token for all
+    (_bf(1, 1, 8, 64).expand(4, 1, 8, 64), "tokens overlap"),          # one learned query for the batch
+    (_bf(1, 1, 4, 64).expand(1, 300, 4, 64), "tokens overlap"),        # the gradient of a sum over the tokens
+    (_bf(2, 1, 4, 64).expand(2, 6, 4, 64), "tokens"),
+    (_bf(1, 6, 4, 64).expand(2, 6, 4, 64), "evenly strided"),
+    (_bf(1, 1, 64).expand(5, 1, 64), "tokens overlap"),                # a head of its own
+    (_bf(7 * 128).as_strided((6, 4, 64), (128, 64, 1)), "tokens overlap"),
+    (_bf(6, 1, 64).expand(6, 4, 64), "heads must be contiguous"),
+    (_bf(4, 6, 64).transpose(0, 1), "heads must be contiguous"),
+    (_bf(2, 6, 2, 64)[:, :3], "evenly strided"),
+])
+def test_token_stride_refuses(x, msg):
+    """By their reason: rows that share memory would be read past their end."""
+    with pytest.raises(ValueError, match=msg):
+        ut._token_stride(x, "x")
+
+
+def test_token_stride_of_the_gradient_of_a_sum():
+    """As autograd hands it back: strides (256, 0, 64, 1) at one sample."""
+    o = torch.zeros(1, 300, 4, 64, requires_grad=True)
+    g, = torch.autograd.grad(o.sum(1), o, torch.ones(1, 4, 64))
+    assert g.stride()[1] == 0
+    with pytest.raises(ValueError, match="tokens overlap"):
+        ut._token_stride(g, "dout")
+    assert ut._token_stride(g.contiguous(), "dout") == 256
+    assert ut._token_stride(torch.zeros(0, 4, 64), "x") == 256 == ut._token_stride(torch.zeros(1, 1, 4, 64), "x")
