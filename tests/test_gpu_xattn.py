@@ -621,3 +621,35 @@ def test_views_broadcast_over_tokens_or_samples_are_refused():
     check_do = do[:1, :1].repeat(1, 30, 1, 1)
     for x, y in zip(want, ut.xattn_bwd(q[:1], k[:1], v[:1], o[:1], check_do, lse[:1], 0.125)):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("zero_rest", [False, True])
+@pytest.mark.parametrize("bad_q,bad_k", [([-7, 60, 5000], [90, 20, 1 << 30]), ([0, 100, 40], [0, 80, -5]),
+                                         ([99, 99, 101], [79, 1000, 80]), ([-(1 << 31), 0, (1 << 31) - 1],) * 2])
+@pytest.mark.parametrize("maxq,maxk,Hq,Hk,D", [(50, 40, 2, 2, 64), (50, 4000, 4, 2, 128), (4000, 40, 2, 1, 72)])
+def test_bad_offsets_write_nothing_outside(bad_q, bad_k, maxq, maxk, Hq, Hk, D, zero_rest):
+    """Every buffer that the calls write lies between margins, which stay as they were (the longer
+    maxima split the keys or the query rows, so that the workspaces hold partial results)."""
+    q, k, v, do, _ = packed(41, [50, 50], [40, 40], Hq, Hk, D)
+    cq, ck = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (bad_q, bad_k))
+    margin, held = 1 << 14, []
+
+    def inside(shape, dtype):
+        n = math.prod(shape)
+        buf = torch.full((n + 2 * margin,), 77, dtype=dtype, device=DEV)
+        held.append((buf, n))
+        return buf[margin:margin + n].view(shape)
+
+    o, dq, dk, dv = (inside(x.shape, torch.bfloat16) for x in (q, q, k, v))
+    lse = inside((Hq, 100), torch.float32)
+    wf = inside((max(16, ut.ut_xattn_fwd_varlen_workspace_size(2, 100, maxq, maxk, Hq, Hk, D)),), torch.uint8)
+    wb = inside((ut.ut_xattn_bwd_varlen_workspace_size(2, 100, 80, maxq, maxk, Hq, Hk, D),), torch.uint8)
+    ins = [x.clone() for x in (q, k, v, do)]
+    at = (cq, maxq, ck, maxk, 0.1)
+    assert ut.ut_xattn_fwd_varlen(q, k, v, o, lse, *at, zero_rest=zero_rest, workspace=wf) == ut.UT_OK
+    assert ut.ut_xattn_bwd_varlen(q, k, v, o, do, lse, dq, dk, dv, *at, zero_rest=zero_rest, workspace=wb) == ut.UT_OK
+    torch.cuda.synchronize()
+    for buf, n in held:
+        assert (buf[:margin] == 77).all() and (buf[margin + n:] == 77).all()
+    for x, y in zip((q, k, v, do), ins):
+        assert torch.equal(x, y)
