@@ -20,7 +20,7 @@
 //
 // Rounding: P and dS to bf16 before their second products (half a step each,
 // 2^-9 relative), all sums in fp32. delta comes from O as stored (half a step
-// of it), or as rowsum(P o dP) in fp32 where all keys of a row lie in one tile.
+// of it), or as rowsum(P o dP) in fp32 where a row's keys in use lie in one tile.
 // No atomics: equal results on every run. Keys not in use: the dQ pass reads
 // zeros in their place and sets their P to 0; in the dK/dV pass a key is a
 // column of its own, whatever it holds, and is stored as 0; waves whose 32 keys
@@ -110,13 +110,13 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
     lse2 = ex.lse == -INFINITY ? 0.f : ex.lse * kLog2e;
     l2 = lse2 - __log2f(scale);   // P scale in place of P: dS comes out scaled (2^-21 off at most)
   };
-  // For the dK/dV pass too: part 0 writes them.
-  auto put_stats = [&](const XItem& at) __attribute__((always_inline)) {
+  // For the dK/dV pass too: one part writes them.
+  auto put_stats = [&](const XItem& at, bool writes) __attribute__((always_inline)) {
     const int ln = x_lane_again();
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
     const int row = at.tile * 32 * NW + 32 * w + (ln & 31), tok = row_token(row, x.G);
-    if (at.part == 0 && ln < 32 && row < sm.nq * x.G) {
+    if (writes && ln < 32 && row < sm.nq * x.G) {
       const int64_t stat = sm.stat0 + (at.hk * x.G + row - tok * x.G) * sm.hstep + tok;
       aux[stat] = lse2;
       aux[x.Tq * x.Hq + stat] = ndl;
@@ -225,8 +225,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       __builtin_amdgcn_s_setprio(0);
     }
   };
-  // delta of rows whose keys all lie in one tile, as rowsum(P o dP) in fp32: with few
-  // keys dP - delta is a small difference, and the rounding of the O that is stored
+  // delta of rows whose keys in use all lie in one tile, as rowsum(P o dP) in fp32: with
+  // few keys dP - delta is a small difference, and the rounding of the O that is stored
   // would show in it (2 keys: dQ 0.0039 off in relative norm, 0.0024 with this).
   auto tile_delta = [&](uint64_t bits, const char* kt_lds, const char* vt_lds) __attribute__((always_inline)) {
     float sum = 0.f;
@@ -318,8 +318,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
         const XTurn<DP> rows(x_lane_again());
         rows.turn(qop, lds0, lds1);
         rows.turn(doop, lds0, lds1);
-        if (seq.keys <= kXKeys) ndl = -tile_delta(seq.bits, kn, vn);   // uniform
-        put_stats(at);
+        const bool one = seq.one_tile(order);   // uniform
+        if (one) ndl = -tile_delta(seq.bits, kn, vn);
+        put_stats(at, one ? seq.bits != 0 : at.part == 0);   // where delta is known
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};

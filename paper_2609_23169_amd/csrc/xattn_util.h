@@ -282,6 +282,26 @@ struct TileSeq {
     fresh = false;
     return true;
   }
+  // After an item's first tile: whether its sample has keys in use in one tile alone
+  // (of which a split item may hold nothing: bits 0).
+  __device__ inline bool one_tile(const XOrder& order) const {
+    const int n = (keys + kXKeys - 1) / kXKeys;
+    if (n <= 1) return bits != 0;
+    if (!tiles.mask) return false;
+    KeyTiles t;   // the tiles not yet looked at; of a split item, all of the sample's
+    int count = 0, from = 0;
+    if (order.splits == 1) {
+      if (tiles.left != 0) return false;
+      count = bits != 0;
+      from = tiles.base + 64;
+    }
+    t.open(tiles.mask, keys, from, n);
+    for (t.base = from; t.base < n && count <= 1; t.base += 64) {
+      t.group();
+      count += __builtin_popcountll(t.left);
+    }
+    return count == 1;
+  }
 };
 
 // 16 bytes a lane, or zeros for an offset of kXOut and more; stores from there on are

@@ -653,3 +653,73 @@ def test_bad_offsets_write_nothing_outside(bad_q, bad_k, maxq, maxk, Hq, Hk, D, 
         assert (buf[:margin] == 77).all() and (buf[margin + n:] == 77).all()
     for x, y in zip((q, k, v, do), ins):
         assert torch.equal(x, y)
+
+
+def few_keys_bounds(q, k, v, do, used, scale, dq, dk, label):
+    """Gradients of one sample [N, H, D] whose keys `used` are in use, with the bounds of
+    test_few_keys_do_not_feel_the_rounding_of_o: delta has no share of a rounded O."""
+    Hq, Hk = q.shape[1], k.shape[1]
+    Q, DO = (x.double().cpu().permute(1, 0, 2) for x in (q, do))
+    K, V = (x[used].double().cpu().permute(1, 0, 2).repeat_interleave(Hq // Hk, 0) for x in (k, v))
+    P = (Q @ K.mT * scale).softmax(-1)
+    dP, adP = DO @ V.mT, DO.abs() @ V.abs().mT
+    dS = P * (dP - (P * dP).sum(-1, keepdim=True))
+    u = 2.0 ** -8
+    eS = u * dS.abs() + 2.0 ** -16 * P * (adP + (P * adP).sum(-1, keepdim=True))
+    shared = lambda x: x.unflatten(0, (Hk, -1)).sum(1)  # noqa: E731
+    for name, got, ref, err in (("dq", dq, scale * (dS @ K), scale * (eS @ K.abs())),
+                                ("dk", dk[used], shared(scale * (dS.mT @ Q)), shared(scale * (eS.mT @ Q.abs())))):
+        got = got.double().cpu().permute(1, 0, 2)
+        worst = ((got - ref).abs() / (u * ref.abs() + (1 + u) * err)).max().item()
+        assert worst <= 1, (label, name, worst)
+
+
+# (keys in use, from where) of each sample: within one 64-key tile each time; a key
+# of its own at both ends. Rows and keys: unsplit and split work, more than 64 tiles
+# of 64 keys (a lane each), a sample whose tile lies behind them.
+@pytest.mark.parametrize("used", [[(1, 0), (2, 130)], [(33, 64), (64, 192)], [(1, -1), (7, 249)]])
+@pytest.mark.parametrize("Nq,Nk,Hq,Hk,D", [(300, 300, 4, 2, 64), (300, 300, 3, 1, 128), (300, 1030, 4, 2, 64),
+                                           (5, 9001, 4, 2, 128), (2100, 4500, 32, 16, 64)])
+def test_few_keys_in_use_do_not_feel_the_rounding_of_o(Nq, Nk, Hq, Hk, D, used):
+    q, k, v, do = draw(42, 2, Nq, Nk, Hq, Hk, D)
+    mask = np.zeros((2, Nk), np.uint8)
+    for b, (n, at) in enumerate(used):
+        at = at if at >= 0 else Nk + at
+        mask[b, at:at + n] = 1
+    scale = D ** -0.5
+    _, _, (dq, dk, _) = run(q, k, v, do, scale, mask)
+    for b in range(2):
+        few_keys_bounds(q[b], k[b], v[b], do[b], np.flatnonzero(mask[b]), scale, dq[b], dk[b], (b, used[b]))
+
+
+def test_few_keys_of_packed_and_padded_prompts_give_equal_gradients():
+    """The same prompts packed (21 and 64 keys) and padded to 300: one arithmetic."""
+    lk, Nq, Nk, Hq, Hk, D = [21, 64], 150, 300, 4, 2, 64
+    q, k, v, do = draw(43, 2, Nq, Nk, Hq, Hk, D)
+    mask = np.zeros((2, Nk), np.uint8)
+    for b, n in enumerate(lk):
+        mask[b, :n] = 1
+    _, _, (dq, dk, dv) = run(q, k, v, do, 0.125, mask)
+    at = (offsets([Nq] * 2), Nq, offsets(lk), max(lk))
+    kp, vp = (torch.cat([x[b, :n] for b, n in enumerate(lk)]) for x in (k, v))
+    o, lse = ut.xattn_fwd_varlen(q.flatten(0, 1), kp, vp, *at, 0.125)
+    want = ut.xattn_bwd_varlen(q.flatten(0, 1), kp, vp, o, do.flatten(0, 1), lse, *at, 0.125)
+    assert torch.equal(dq.flatten(0, 1), want[0])
+    for x, y in ((dk, want[1]), (dv, want[2])):
+        assert torch.equal(torch.cat([x[b, :n] for b, n in enumerate(lk)]), y)
+
+
+@pytest.mark.parametrize("Nq,Nk", [(40, 700), (300, 300), (5, 9001)])
+def test_few_keys_of_samples_with_and_without_any(Nq, Nk):
+    """Of five samples one has no key in use, two have keys in one tile, two in two tiles; the
+    statistics of the dQ pass serve the dK and dV of each."""
+    q, k, v, do = draw(44, 5, Nq, Nk, 4, 2, 64)
+    mask = np.zeros((5, Nk), np.uint8)
+    mask[1, 70:90] = 1
+    mask[2, -3:] = 1
+    mask[3, [0, Nk - 1]] = 1
+    mask[4, 60:70] = 1
+    o, lse, grads = run(q, k, v, do, 0.125, mask)
+    check(*(f64(t) for t in (q, k, v, do)), 0.125, mask, f64(o), f64(lse), [f64(t) for t in grads], f"{(Nq, Nk)}")
+    for b in (1, 2):
+        few_keys_bounds(q[b], k[b], v[b], do[b], np.flatnonzero(mask[b]), 0.125, grads[0][b], grads[1][b], b)
