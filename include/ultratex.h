@@ -566,8 +566,9 @@ ut_status ut_qk_rope_bwd(const void* dq_out, const void* dk_out, const void* q, 
  *           time need one each.
  * No atomics: results are deterministic.
  * Errors: sizes or strides out of range, Hq % Hk != 0, 2^27 rows of a head or
- *         more (B Nq Hq, B Nk Hk), null or misaligned pointers ->
- *         UT_ERR_INVALID_ARG; a head_dim outside the above, a stride of 2^22 or
+ *         more (B Nq Hq, B Nk Hk), backward launches of 2^24 workgroups (B Hk
+ *         ceil(Nk / 128); T H D / 1024 where work is split), null or misaligned
+ *         pointers -> UT_ERR_INVALID_ARG; a head_dim outside the above, a stride of 2^22 or
  *         more -> UT_ERR_UNSUPPORTED; UT_ERR_WORKSPACE. The size queries return 0
  *         for sizes that the calls refuse.
  *

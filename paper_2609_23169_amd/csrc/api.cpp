@@ -861,7 +861,7 @@ ut_status check_xattn(const char* fn, int32_t B, int64_t Tq, int64_t Tk, int32_t
   if (Tq < 0 || Tk < 0 || Tq >= ((int64_t)1 << 31) || Tk >= ((int64_t)1 << 31))
     return fail(UT_ERR_INVALID_ARG, "%s: token counts %lld, %lld outside [0, 2^31)", fn,
                 (long long)Tq, (long long)Tk);
-  // one thread or more a row, launches of less than 2^32 threads
+  // 32-bit row numbers, and launches over rows of less than 2^32 threads
   const int64_t most = (int64_t)1 << 27;
   if (Tq * Hq >= most || Tk * Hk >= most || (int64_t)B * Nq * Hq >= most || (int64_t)B * Nk * Hk >= most)
     return fail(UT_ERR_INVALID_ARG, "%s: problem too large (2^27 rows of a head or more)", fn);
@@ -875,6 +875,15 @@ ut_status check_xattn(const char* fn, int32_t B, int64_t Tq, int64_t Tk, int32_t
   a->Tq = Tq;
   a->Tk = Tk;
   a->scale = scale;
+  return UT_OK;
+}
+
+// The backward's dK/dV pass and its joins launch by size, not by what fits the chip.
+ut_status check_xattn_bwd(const char* fn, const XArgs& a) {
+  if (!xattn_bwd_launchable(a))
+    return fail(UT_ERR_INVALID_ARG,
+                "%s: problem too large (2^24 workgroups: B Hk ceil(Nk / 128), or T H D / 1024 of split work)",
+                fn);
   return UT_OK;
 }
 
@@ -1005,7 +1014,9 @@ ut_status ut_xattn_fwd_varlen(const void* q, const void* k, const void* v, void*
 
 size_t ut_xattn_bwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk, int32_t D) {
   XArgs a{};
-  return xattn_sizes(B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, &a) ? xattn_bwd_workspace(a) : 0;
+  return xattn_sizes(B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, &a) && xattn_bwd_launchable(a)
+             ? xattn_bwd_workspace(a)
+             : 0;
 }
 
 ut_status ut_xattn_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
@@ -1017,6 +1028,7 @@ ut_status ut_xattn_bwd(const void* q, const void* k, const void* v, const void* 
   g_last_error[0] = 0;
   XArgs a{};
   UT_TRY(check_xattn(fn, B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, softmax_scale, &a));
+  UT_TRY(check_xattn_bwd(fn, a));
   return xattn_bwd(fn, a, q, k, v, o, dout, lse, dq, dk, dv, strides_host, key_mask, workspace,
                    workspace_bytes, false, stream);
 }
@@ -1024,7 +1036,9 @@ ut_status ut_xattn_bwd(const void* q, const void* k, const void* v, const void* 
 size_t ut_xattn_bwd_varlen_workspace_size(int32_t B, int64_t Tq, int64_t Tk, int32_t max_seqlen_q,
                                           int32_t max_seqlen_k, int32_t Hq, int32_t Hk, int32_t D) {
   XArgs a{};
-  return xattn_sizes(B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, &a) ? xattn_bwd_workspace(a) : 0;
+  return xattn_sizes(B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, &a) && xattn_bwd_launchable(a)
+             ? xattn_bwd_workspace(a)
+             : 0;
 }
 
 ut_status ut_xattn_bwd_varlen(const void* q, const void* k, const void* v, const void* o,
@@ -1039,6 +1053,7 @@ ut_status ut_xattn_bwd_varlen(const void* q, const void* k, const void* v, const
   g_last_error[0] = 0;
   XArgs a{};
   UT_TRY(check_xattn(fn, B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, softmax_scale, &a));
+  UT_TRY(check_xattn_bwd(fn, a));
   UT_TRY(check_cu(fn, "cu_seqlens_q", cu_seqlens_q, B, Tq, max_seqlen_q, stream));
   UT_TRY(check_cu(fn, "cu_seqlens_k", cu_seqlens_k, B, Tk, max_seqlen_k, stream));
   a.cuq = cu_seqlens_q, a.cuk = cu_seqlens_k;

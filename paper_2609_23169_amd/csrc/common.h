@@ -224,6 +224,8 @@ struct XArgs {
 // (dK, dV) are split over workgroups, and of the backward's row statistics.
 size_t xattn_fwd_workspace(const XArgs& a);
 hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s);
+// Whether the backward's launches stay below 2^32 threads.
+bool xattn_bwd_launchable(const XArgs& a);
 size_t xattn_bwd_workspace(const XArgs& a);
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s);
 

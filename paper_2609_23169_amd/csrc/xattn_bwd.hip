@@ -657,6 +657,12 @@ void launch_sums(const Join* j, int n, int B, hipStream_t s) {
 
 }  // namespace
 
+bool xattn_bwd_launchable(const XArgs& a) {
+  constexpr int64_t kMost = (int64_t)1 << 24;   // workgroups of 256 threads
+  const int64_t sums = std::max(dq_part(a) > 0 ? a.Tq * a.Hq : 0, dkdv_part(a) > 0 ? a.Tk * a.Hk : 0) * a.D;
+  return (dkdv_groups(a) + 7) / 8 * 8 < kMost && (sums / 4 + 255) / 256 < kMost;
+}
+
 size_t xattn_bwd_workspace(const XArgs& a) { return aux_bytes(a) + dq_part(a) + dkdv_part(a); }
 
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {

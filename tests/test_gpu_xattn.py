@@ -723,3 +723,22 @@ def test_few_keys_of_samples_with_and_without_any(Nq, Nk):
     check(*(f64(t) for t in (q, k, v, do)), 0.125, mask, f64(o), f64(lse), [f64(t) for t in grads], f"{(Nq, Nk)}")
     for b in (1, 2):
         few_keys_bounds(q[b], k[b], v[b], do[b], np.flatnonzero(mask[b]), 0.125, grads[0][b], grads[1][b], b)
+
+
+def test_as_many_samples_as_a_launch_takes():
+    """2^24 - 8 samples of one query and one key: O is V, dV is dO, and dQ and dK are 0 but
+    for fp32's rounding."""
+    B = (1 << 24) - 8
+    g = torch.Generator(device=DEV).manual_seed(45)
+    q, k, v, do = (torch.randn(B, 1, 1, 8, generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(4))
+    o, lse, (dq, dk, dv) = run(q, k, v, do, 0.25, None)
+    assert torch.equal(o, v) and torch.equal(dv, do)
+    # P = exp2(s - lse) is off by at most 2^-20 of 1, and dS = P dP - P rowsum(P dP) by that of |dP|
+    dp = (do.float().abs() * v.float().abs()).sum(-1, keepdim=True)
+    for got, x in ((dq, k), (dk, q)):
+        assert (got.float().abs() <= 2.0 ** -18 * 0.25 * dp * x.float().abs()).all()
+    want = (q.double() * k.double()).sum(-1)[:, 0] * 0.25
+    assert (lse[:, 0, 0].double() - want[:, 0]).abs().max() <= 2.0 ** -16
+    with pytest.raises(ut.UltraTexError) as e:
+        ut.xattn_bwd(*(torch.cat([x, x[:1]]) for x in (q, k, v, o, do)), torch.zeros(B + 1, 1, 1, device=DEV), 0.25)
+    assert e.value.status == ut.UT_ERR_INVALID_ARG

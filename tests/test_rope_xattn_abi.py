@@ -230,3 +230,28 @@ def test_token_stride_of_the_gradient_of_a_sum():
         ut._token_stride(g, "dout")
     assert ut._token_stride(g.contiguous(), "dout") == 256
     assert ut._token_stride(torch.zeros(0, 4, 64), "x") == 256 == ut._token_stride(torch.zeros(1, 1, 4, 64), "x")
+
+
+@pytest.mark.parametrize("varlen", [False, True])
+@pytest.mark.parametrize("size", [dict(B=1 << 24, Nq=1, Nk=1, Hq=1, Hk=1), dict(B=1 << 21, Nq=1, Nk=7, Hq=8, Hk=8),
+                                  dict(B=(1 << 24) - 7, Nq=1, Nk=3, Hq=1, Hk=1)])
+def test_xattn_bwd_refuses_launches_of_too_many_workgroups(size, varlen):
+    """The dK/dV pass has a workgroup of 256 threads a sample, key head and 128 keys; 2^24 of
+    them are refused before anything is launched. The forward takes these sizes."""
+    size = dict(size, D=8, Tq=size["B"], Tk=size["B"])
+    n = [size["Hq"], size["Hk"], 8]
+    query = (lambda s: ut.ut_xattn_bwd_varlen_workspace_size(s["B"], s["Tq"], s["Tk"], s["Nq"], s["Nk"], *n)) if varlen else (
+        lambda s: ut.ut_xattn_bwd_workspace_size(s["B"], s["Nq"], s["Nk"], *n))
+    assert query(size) == 0
+    assert _x("bwd", varlen, **size) == BAD and "workgroups" in ut.last_error()
+    assert _x("fwd", varlen, **size, q=None) == BAD and "q is NULL" in ut.last_error()
+    less = dict(size, B=size["B"] - 1 if size["Hk"] > 1 else (1 << 24) - 8)
+    assert query(less) > 0
+    assert _x("bwd", varlen, **less, q=None) == BAD and "q is NULL" in ut.last_error()
+
+
+def test_xattn_bwd_refuses_joins_of_too_many_rows():
+    """Rows of few samples, split over keys, whose join would be a launch of 2^32 threads."""
+    at = lambda t: (1, t, 64, 1, 100000, 1, 1, 128)  # noqa: E731
+    assert ut.ut_xattn_bwd_varlen_workspace_size(*at((1 << 27) - 1)) == 0
+    assert ut.ut_xattn_bwd_varlen_workspace_size(*at((1 << 27) - 8)) > 0
