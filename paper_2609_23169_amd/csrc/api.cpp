@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <vector>
 
 #include "common.h"
@@ -284,23 +285,28 @@ bool validate_mode() {
   return e && e[0] && !(e[0] == '0' && e[1] == 0);
 }
 
+// `count` device values to the host, when the stream has come there. No exception
+// leaves the C entries: host memory that runs out is an error like the device's.
+ut_status validate_copy(const int32_t* src, size_t count, std::vector<int32_t>* out, hipStream_t stream) {
+  try {
+    out->resize(count);
+  } catch (const std::exception&) {   // bad_alloc, length_error
+    return check_hip(hipErrorOutOfMemory, "validate copy");
+  }
+  if (count == 0) return UT_OK;
+  UT_TRY(check_hip(hipMemcpyAsync(out->data(), src, count * sizeof(int32_t), hipMemcpyDeviceToHost, stream),
+                   "validate copy"));
+  return check_hip(hipStreamSynchronize(stream), "validate sync");
+}
+
 // Copies a compressed list pair to the host and checks it with check_lists.
 ut_status validate_lists(const char* fn, const char* what, const int32_t* ptr, const int32_t* idx,
                          int64_t rows, int32_t limit, hipStream_t stream) {
-  std::vector<int32_t> p((size_t)rows + 1);
-  UT_TRY(check_hip(hipMemcpyAsync(p.data(), ptr, p.size() * sizeof(int32_t), hipMemcpyDeviceToHost,
-                                  stream),
-                   "validate copy"));
-  UT_TRY(check_hip(hipStreamSynchronize(stream), "validate sync"));
+  std::vector<int32_t> p, v;
+  UT_TRY(validate_copy(ptr, (size_t)rows + 1, &p, stream));
   // well-formed pointers first, so that p[rows] is a sane entry count
   UT_TRY(check_lists(fn, what, p.data(), nullptr, 0, rows, limit));
-  std::vector<int32_t> v((size_t)p[rows]);
-  if (!v.empty()) {
-    UT_TRY(check_hip(hipMemcpyAsync(v.data(), idx, v.size() * sizeof(int32_t),
-                                    hipMemcpyDeviceToHost, stream),
-                     "validate copy"));
-    UT_TRY(check_hip(hipStreamSynchronize(stream), "validate sync"));
-  }
+  UT_TRY(validate_copy(idx, (size_t)p[rows], &v, stream));
   return check_lists(fn, what, p.data(), v.data(), (int64_t)v.size(), rows, limit);
 }
 }  // namespace
@@ -417,11 +423,8 @@ ut_status check_varlen(const char* fn, const int32_t* cu_seqlens, int32_t B, int
   if (T < 0 || T >= ((int64_t)1 << 31))
     return fail(UT_ERR_INVALID_ARG, "%s: T = %lld outside [0, 2^31)", fn, (long long)T);
   if (!validate_mode()) return UT_OK;
-  std::vector<int32_t> cu((size_t)B + 1);
-  UT_TRY(check_hip(hipMemcpyAsync(cu.data(), cu_seqlens, cu.size() * sizeof(int32_t),
-                                  hipMemcpyDeviceToHost, stream),
-                   "validate copy"));
-  UT_TRY(check_hip(hipStreamSynchronize(stream), "validate sync"));
+  std::vector<int32_t> cu;
+  UT_TRY(validate_copy(cu_seqlens, (size_t)B + 1, &cu, stream));
   return check_cu_seqlens(fn, cu.data(), B, T, max_seqlen);
 }
 }  // namespace
@@ -893,11 +896,8 @@ ut_status check_cu(const char* fn, const char* name, const int32_t* cu, int32_t 
                    int32_t max_seqlen, hipStream_t stream) {
   UT_TRY(check_ptr(fn, name, cu, 4));
   if (!validate_mode()) return UT_OK;
-  std::vector<int32_t> v((size_t)B + 1);
-  UT_TRY(check_hip(hipMemcpyAsync(v.data(), cu, v.size() * sizeof(int32_t), hipMemcpyDeviceToHost,
-                                  stream),
-                   "validate copy"));
-  UT_TRY(check_hip(hipStreamSynchronize(stream), "validate sync"));
+  std::vector<int32_t> v;
+  UT_TRY(validate_copy(cu, (size_t)B + 1, &v, stream));
   if (v[(size_t)B] > T)
     return fail(UT_ERR_INVALID_ARG, "%s: %s ends at %d, past T = %lld", fn, name, v[(size_t)B],
                 (long long)T);

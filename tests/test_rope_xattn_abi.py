@@ -1,6 +1,9 @@
 """Refusals of the rotary and cross-attention calls, on the host before any
 launch (no GPU needed), and the binding's checks of tensors."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -255,3 +258,25 @@ def test_xattn_bwd_refuses_joins_of_too_many_rows():
     at = lambda t: (1, t, 64, 1, 100000, 1, 1, 128)  # noqa: E731
     assert ut.ut_xattn_bwd_varlen_workspace_size(*at((1 << 27) - 1)) == 0
     assert ut.ut_xattn_bwd_varlen_workspace_size(*at((1 << 27) - 8)) > 0
+
+
+def test_validate_mode_without_host_memory_is_an_error():
+    """Offsets of 2^31 - 1 samples take 8 GiB on the host: an error where there is less, no exception through the
+    C entry. In a process of its own, with little address space and no HIP call before that."""
+    code = """
+import ctypes, resource
+import paper_2609_23169_amd as ut
+lib, fake = ut.lib(), ctypes.c_void_p(0x10000)
+used = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (used + (1 << 30),) * 2)
+n = (1 << 31) - 1
+for call, args in ((lib.ut_xattn_fwd_varlen, (*[fake] * 5, None, None, fake, fake, n, 10, 10, 0, 0, 1, 1, 64, 0.1, 0, None, 0, None)),
+                   (lib.ut_bsattn_fwd_varlen, (*[fake] * 6, n, 10, 1, 1, 64, 64, fake, fake, 0.1, None))):
+    st = call(*args)
+    assert st == ut.UT_ERR_HIP and "memory" in ut.last_error(), (st, ut.last_error())
+print("done")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                       env=dict(os.environ, UT_VALIDATE="1"))
+    assert r.returncode == 0 and "done" in r.stdout, r.stderr[-2000:]
