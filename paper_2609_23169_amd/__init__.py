@@ -516,6 +516,16 @@ class _Args:
             return fn(*args, s.cuda_stream)
 
 
+def _in_int32(*sizes) -> bool:
+    """Whether the C calls' int32 arguments hold them (ctypes cuts larger ones without a word)."""
+    return max(sizes) < 1 << 31 and min(sizes) >= -(1 << 31)
+
+
+def _size(query, *sizes) -> int:
+    """A workspace query; 0 for sizes that the calls refuse."""
+    return int(query(*sizes)) if _in_int32(*sizes) else 0
+
+
 def _like(t, like, name: str):
     if t.shape != like.shape or t.dtype != like.dtype:
         raise ValueError(f"{name}: the shape and dtype of its counterpart")
@@ -535,6 +545,7 @@ def _rope_args(x, y, pos, axis_dims, token_idx, q_weight, k_weight):
           "pos: contiguous fp32 [rows, axes], a column for each of axis_dims")
     _need(token_idx is None or (token_idx.dtype == torch.int32 and token_idx.is_contiguous()
                                 and token_idx.numel() == n), "token_idx: contiguous int32 [n]")
+    _need(_in_int32(Hq, Hk, *axis_dims), "sizes past 32 bits")
     wd = UT_BF16
     if q_weight is not None or k_weight is not None:
         for w in (q_weight, k_weight):
@@ -561,7 +572,7 @@ def ut_qk_rope_fwd(q, k, q_out, k_out, pos, axis_dims, theta: float, token_idx=N
 
 
 def ut_qk_rope_bwd_workspace_size(D: int) -> int:
-    return int(lib().ut_qk_rope_bwd_workspace_size(D))
+    return _size(lib().ut_qk_rope_bwd_workspace_size, D)
 
 
 def ut_qk_rope_bwd(dq_out, dk_out, q, k, dq, dk, pos, axis_dims, theta: float, token_idx=None, q_weight=None,
@@ -598,14 +609,17 @@ def _xattn_args(q, k, v, key_mask, dims: int):
     _need(key_mask is None or (key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == sk[:-2]
                                and key_mask.is_contiguous()),
           "key_mask: contiguous uint8 or bool, one value a key token")
+    if max(sq) >> 31 or max(sk) >> 31:   # as _in_int32
+        raise ValueError("sizes past 32 bits")
     return sq[:-2], sk[:-2], sq[-2], sk[-2], sq[-1]
 
 
-def _check_cu(cu_q, cu_k) -> int:
+def _check_cu(cu_q, cu_k, max_q: int, max_k: int) -> int:
     for cu in (cu_q, cu_k):
         _need(cu.dtype == torch.int32 and cu.dim() == 1 and cu.numel() >= 2 and cu.is_contiguous(),
               "cu_seqlens: contiguous int32 [B+1]")
     _need(cu_q.numel() == cu_k.numel(), "cu_seqlens_q and cu_seqlens_k: one number of samples")
+    _need(_in_int32(cu_q.numel(), max_q, max_k), "sizes past 32 bits")
     return cu_q.numel() - 1
 
 
@@ -614,7 +628,7 @@ def _check_lse(lse, n: int):
 
 
 def ut_xattn_fwd_workspace_size(B: int, Nq: int, Nk: int, Hq: int, Hk: int, D: int) -> int:
-    return int(lib().ut_xattn_fwd_workspace_size(B, Nq, Nk, Hq, Hk, D))
+    return _size(lib().ut_xattn_fwd_workspace_size, B, Nq, Nk, Hq, Hk, D)
 
 
 def ut_xattn_fwd(q, k, v, o, lse, softmax_scale: float, key_mask=None, workspace=None, stream=None) -> int:
@@ -629,14 +643,14 @@ def ut_xattn_fwd(q, k, v, o, lse, softmax_scale: float, key_mask=None, workspace
 
 def ut_xattn_fwd_varlen_workspace_size(B: int, Tq: int, max_seqlen_q: int, max_seqlen_k: int, Hq: int, Hk: int,
                                        D: int) -> int:
-    return int(lib().ut_xattn_fwd_varlen_workspace_size(B, Tq, max_seqlen_q, max_seqlen_k, Hq, Hk, D))
+    return _size(lib().ut_xattn_fwd_varlen_workspace_size, B, Tq, max_seqlen_q, max_seqlen_k, Hq, Hk, D)
 
 
 def ut_xattn_fwd_varlen(q, k, v, o, lse, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k, max_seqlen_k: int,
                         softmax_scale: float, key_mask=None, zero_rest: bool = False, workspace=None,
                         stream=None) -> int:
     (Tq,), (Tk,), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 3)
-    B = _check_cu(cu_seqlens_q, cu_seqlens_k)
+    B = _check_cu(cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k)
     _like(o, q, "o")
     _check_lse(lse, Hq * Tq)
     a = _Args(q)
@@ -648,7 +662,7 @@ def ut_xattn_fwd_varlen(q, k, v, o, lse, cu_seqlens_q, max_seqlen_q: int, cu_seq
 
 
 def ut_xattn_bwd_workspace_size(B: int, Nq: int, Nk: int, Hq: int, Hk: int, D: int) -> int:
-    return int(lib().ut_xattn_bwd_workspace_size(B, Nq, Nk, Hq, Hk, D))
+    return _size(lib().ut_xattn_bwd_workspace_size, B, Nq, Nk, Hq, Hk, D)
 
 
 def _bwd_rows(a, q, k, v, o, dout, dq, dk, dv):
@@ -670,14 +684,14 @@ def ut_xattn_bwd(q, k, v, o, dout, lse, dq, dk, dv, softmax_scale: float, key_ma
 
 def ut_xattn_bwd_varlen_workspace_size(B: int, Tq: int, Tk: int, max_seqlen_q: int, max_seqlen_k: int, Hq: int,
                                        Hk: int, D: int) -> int:
-    return int(lib().ut_xattn_bwd_varlen_workspace_size(B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D))
+    return _size(lib().ut_xattn_bwd_varlen_workspace_size, B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D)
 
 
 def ut_xattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k,
                         max_seqlen_k: int, softmax_scale: float, key_mask=None, zero_rest: bool = False,
                         workspace=None, stream=None) -> int:
     (Tq,), (Tk,), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 3)
-    B = _check_cu(cu_seqlens_q, cu_seqlens_k)
+    B = _check_cu(cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k)
     _check_lse(lse, Hq * Tq)
     a = _Args(q)
     ins, outs = _bwd_rows(a, q, k, v, o, dout, dq, dk, dv)

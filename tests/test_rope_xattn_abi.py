@@ -280,3 +280,29 @@ print("done")
                        cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                        env=dict(os.environ, UT_VALIDATE="1"))
     assert r.returncode == 0 and "done" in r.stdout, r.stderr[-2000:]
+
+
+BIG = (1 << 32) + 6    # 6 in 32 bits
+
+
+def test_sizes_past_32_bits_are_refused_not_cut():
+    """The C calls take int32 sizes; larger ones must not arrive there as their low halves."""
+    q, k, long_k = _bf(1, 6, 1, 64), _bf(1, 5, 1, 64), _bf(1, 1, 1, 64).expand(1, BIG, 1, 64)
+    cu = torch.tensor([0, 6], dtype=torch.int32)
+    pos = torch.zeros(6, 1)
+    for call in (lambda: ut._xattn_args(q, long_k, long_k, None, 4), lambda: ut._xattn_args(long_k, k, k, None, 4),
+                 lambda: ut._check_cu(cu, cu, BIG, 6), lambda: ut._check_cu(cu, cu, 6, BIG),
+                 lambda: ut._check_cu(cu, cu, 6, -BIG),
+                 lambda: ut._rope_args(q, None, pos, (BIG,), None, None, None),
+                 lambda: ut._rope_args(q, None, pos, (-BIG,), None, None, None),
+                 lambda: ut._rope_args(_bf(1, 1, 64).expand(1, BIG, 64), None, pos, (64,), None, None, None)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    for fn, args in ((ut.ut_xattn_fwd_workspace_size, (1, 1, 16384, 32, 8, 128)),
+                     (ut.ut_xattn_bwd_workspace_size, (1, 600, 16384, 32, 8, 128)),
+                     (ut.ut_xattn_fwd_varlen_workspace_size, (1, 1, 1, 16384, 32, 8, 128)),
+                     (ut.ut_xattn_bwd_varlen_workspace_size, (1, 600, 600, 600, 16384, 32, 8, 128))):
+        assert fn(*args) > 0
+        for i in range(len(args)):
+            assert fn(*args[:i], args[i] + (1 << 32), *args[i + 1:]) == 0, (fn.__name__, i)
+    assert ut.ut_qk_rope_bwd_workspace_size(64 + (1 << 32)) == 0
