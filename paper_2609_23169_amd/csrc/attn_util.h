@@ -111,10 +111,12 @@ __device__ inline unsigned pack_bf16x2(float a, float b) {
 __device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // LDS byte offset of logical 16-byte chunk c of row r in a tile of CPR chunks
-// per row. The XOR swizzle makes both access patterns conflict-free: 32-row
-// b128 reads of one chunk (the swizzle is injective over 16 consecutive rows)
-// and transposing 8-byte reads of 4 consecutive rows x 4 chunks (those rows
-// differ in the swizzle's upper two bits).
+// per row. Two access patterns: 32-row b128 reads of one chunk, free of conflicts
+// (the swizzle is injective over 16 consecutive rows), and transposing 8-byte
+// reads of 4 consecutive rows x 4 chunks. Those are free of conflicts at 16 chunks
+// (the rows differ in the swizzle's upper two bits) and take two passes a half-wave
+// at 8, where rows r and r + 2 fall on the same pair of chunks: 9% of the cycles of
+// a CU in the 64-column cross-attention dK/dV pass, 7% in the forward, 6% in dQ.
 template <int CPR>
 __device__ inline int lds_off(int r, int c) {
   static_assert(CPR == 16 || CPR == 8, "rows of 128 or 64 bf16");

@@ -12,7 +12,8 @@
 //             h = x rstd,  dw = sum over rows and heads of g h,
 //             dx = rstd (g w - h mean(g w h))
 //
-// Bytes bound it: a row is read and written once, about 110 vector instructions
+// Bytes bound it: a row is read and written once, about 150 vector instructions of
+// the built loop (forward with the norm; 163 with the table's share, by the counters)
 // stand beside 32 bytes a lane. The angles are shared by all heads: a
 // workgroup takes a few tokens, one thread computes one cos and sin (the
 // angle in turns and in 64 bits, so that a far position loses nothing), and the
