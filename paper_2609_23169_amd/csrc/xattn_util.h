@@ -285,7 +285,10 @@ struct TileSeq {
     return true;
   }
   // After an item's first tile: whether its sample has keys in use in one tile alone
-  // (of which a split item may hold nothing: bits 0).
+  // (of which a split item may hold nothing: bits 0). Split items look through the
+  // mask until they meet a second such tile: 1 us of a call where there is one in the
+  // first 4,096 keys (dQ of 40 rows on 700 keys 16.8 -> 17.9 us), 8 us at 20 keys of
+  // 16,391; unsplit ones have it from the walk.
   __device__ inline bool one_tile(const XOrder& order) const {
     const int n = (keys + kXKeys - 1) / kXKeys;
     if (n <= 1) return bits != 0;
