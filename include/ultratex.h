@@ -623,6 +623,166 @@ ut_status ut_xattn_bwd_varlen(const void* q, const void* k, const void* v, const
                               int32_t zero_rest, void* workspace, size_t workspace_bytes,
                               hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Window attention: a query sees the keys around it and a few first ones,
+ * O = softmax(Q K^T * scale) V over the visible keys in use. Self attention of the
+ * packed image tokens (a text prefix as the first keys), or Nq queries at the end
+ * of Nk keys.
+ *
+ * Query i of a sample's nq sits at position p = i + nk - nq of its nk keys. Key j is
+ * visible to it where
+ *   p - window_left <= j <= p + window_right, or
+ *   j < n_sink and (window_right > 0 or j <= p):
+ * with window_right = 0 no query sees a later key, otherwise every query sees the
+ * sinks. A query in front of the keys (p < 0) may see none.
+ *
+ * window_left, window_right  >= 0, or -1: no bound on that side.
+ * n_sink    >= 0; more than the keys is as many as there are.
+ * Everything else - tensors, strides_host, key_mask (keys in use, sinks
+ * included), lse, workspace, packed samples, zero_rest, errors - is as in
+ * ut_xattn_*. The size queries take the window too. A row without visible keys in
+ * use: o = 0, lse = -inf, zero gradients. Keys that no query sees may hold
+ * anything and get zero gradients; inf or NaN in a key that some query sees may reach
+ * the other queries of its 128-row tile, as 0 times it (mark padding in key_mask). delta = rowsum(dO o O) is formed from the
+ * stored o, except for rows whose visible keys lie in one 64-key tile.
+ * No atomics: results are deterministic.
+ * Errors: also window_left or window_right < -1, n_sink < 0 -> UT_ERR_INVALID_ARG.
+ * ---------------------------------------------------------------------- */
+size_t ut_swattn_fwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk,
+                                    int32_t D, int32_t window_left, int32_t window_right,
+                                    int32_t n_sink);
+ut_status ut_swattn_fwd(const void* q, const void* k, const void* v, void* o, float* lse,
+                        const int64_t* strides_host, const uint8_t* key_mask, int32_t B,
+                        int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk, int32_t D,
+                        int32_t window_left, int32_t window_right, int32_t n_sink,
+                        float softmax_scale, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream);
+size_t ut_swattn_fwd_varlen_workspace_size(int32_t B, int64_t Tq, int32_t max_seqlen_q,
+                                           int32_t max_seqlen_k, int32_t Hq, int32_t Hk, int32_t D,
+                                           int32_t window_left, int32_t window_right,
+                                           int32_t n_sink);
+ut_status ut_swattn_fwd_varlen(const void* q, const void* k, const void* v, void* o, float* lse,
+                               const int64_t* strides_host, const uint8_t* key_mask,
+                               const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t B,
+                               int64_t Tq, int64_t Tk, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                               int32_t Hq, int32_t Hk, int32_t D, int32_t window_left,
+                               int32_t window_right, int32_t n_sink, float softmax_scale,
+                               int32_t zero_rest, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
+size_t ut_swattn_bwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk,
+                                    int32_t D, int32_t window_left, int32_t window_right,
+                                    int32_t n_sink);
+ut_status ut_swattn_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                        const float* lse, void* dq, void* dk, void* dv, const int64_t* strides_host,
+                        const uint8_t* key_mask, int32_t B, int32_t Nq, int32_t Nk, int32_t Hq,
+                        int32_t Hk, int32_t D, int32_t window_left, int32_t window_right,
+                        int32_t n_sink, float softmax_scale, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+size_t ut_swattn_bwd_varlen_workspace_size(int32_t B, int64_t Tq, int64_t Tk, int32_t max_seqlen_q,
+                                           int32_t max_seqlen_k, int32_t Hq, int32_t Hk, int32_t D,
+                                           int32_t window_left, int32_t window_right,
+                                           int32_t n_sink);
+ut_status ut_swattn_bwd_varlen(const void* q, const void* k, const void* v, const void* o,
+                               const void* dout, const float* lse, void* dq, void* dk, void* dv,
+                               const int64_t* strides_host, const uint8_t* key_mask,
+                               const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t B,
+                               int64_t Tq, int64_t Tk, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                               int32_t Hq, int32_t Hk, int32_t D, int32_t window_left,
+                               int32_t window_right, int32_t n_sink, float softmax_scale,
+                               int32_t zero_rest, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Attention over a cache of keys and values: T tokens of each sample, the next
+ * one (T = 1), a chunk of a prompt, or a tree of drafted tokens to be verified, whose
+ * own keys and values are in the cache already.
+ *
+ * q, o      bf16 [B, T, Hq, D], T >= 1.
+ * k_cache, v_cache  bf16 [B, capacity, Hk, D]. Sample b's tokens attend to slots
+ *           0 .. cache_len[b] - 1 and to their own T slots behind them; what later
+ *           slots hold is not used.
+ * cache_len device int32 [B]: slots in use before the T tokens, 0 .. capacity - T
+ *           (clamped to that; checked first under UT_VALIDATE).
+ * tree      device uint64 [B, T], T <= 64: bit u of word (b, t) set = token t sees
+ *           token u's slot (its ancestors and itself); bits past T are ignored. NULL: a
+ *           chain, token t sees the tokens 0 .. t.
+ * window_left, n_sink  as in ut_swattn_*, with window_right = 0: token t sits at
+ *           position cache_len[b] + t, in a tree behind the tokens that it sees,
+ *           cache_len[b] + their number less itself. With a tree the window has to hold
+ *           every drafted token, window_left >= T - 1 (or -1), and sinks count in front
+ *           of cache_len[b] only.
+ * lse       fp32 [B, Hq, T].
+ * strides_host  HOST {q, k_cache, v_cache, o} or NULL, as in ut_xattn_fwd: sample b's
+ *           slots start capacity strides after those of sample b - 1.
+ * weights_in, weights_out  fp32 [B, Hk, capacity], or weights_out NULL: not wanted.
+ *           weights_out[b, hk, j] = weights_in[b, hk, j] + the sum, over the T tokens and
+ *           the heads of the group, of the softmax weight of slot j, for every slot (of
+ *           weights_in alone where nothing sees it). weights_in NULL: zeros;
+ *           weights_out may be weights_in.
+ * workspace as in ut_xattn_fwd, of the size query's bytes.
+ * A token that sees no slot (a tree word of 0 in front of an empty cache): o = 0,
+ * lse = -inf. No atomics: results are deterministic.
+ * Errors: those of ut_xattn_fwd; T < 1 or > capacity, a tree with T > 64 or
+ *         0 <= window_left < T - 1, weights_in without weights_out
+ *         -> UT_ERR_INVALID_ARG.
+ * ---------------------------------------------------------------------- */
+size_t ut_cache_attn_workspace_size(int32_t B, int32_t T, int32_t capacity, int32_t Hq, int32_t Hk,
+                                    int32_t D, int32_t window_left, int32_t n_sink);
+ut_status ut_cache_attn(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
+                        const int64_t* strides_host, const int32_t* cache_len, const uint64_t* tree,
+                        const float* weights_in, float* weights_out, int32_t B, int32_t T,
+                        int32_t capacity, int32_t Hq, int32_t Hk, int32_t D, int32_t window_left,
+                        int32_t n_sink, float softmax_scale, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The weights alone, of some of the tokens: after a tree has been verified, those
+ * that were accepted.
+ *
+ * q, k_cache, lse, cache_len, tree, window_left, n_sink, softmax_scale  of the
+ *           ut_cache_attn call, lse its output.
+ * strides_host  HOST {q, k_cache} or NULL.
+ * tokens    device uint64 [B], T <= 64: bit t of word b set = token t counts. NULL: all.
+ * Errors: as above; tokens with T > 64 -> UT_ERR_INVALID_ARG.
+ * ---------------------------------------------------------------------- */
+ut_status ut_cache_weights(const void* q, const void* k_cache, const float* lse,
+                           const int64_t* strides_host, const int32_t* cache_len,
+                           const uint64_t* tree, const uint64_t* tokens, const float* weights_in,
+                           float* weights_out, int32_t B, int32_t T, int32_t capacity, int32_t Hq,
+                           int32_t Hk, int32_t D, int32_t window_left, int32_t n_sink,
+                           float softmax_scale, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Eviction: of each sample and key head the slots that stay, by the weight that
+ * they have received, moved together into another cache.
+ *
+ * With n = cache_len[b] slots in use: all of them where n <= n_keep. Otherwise the first
+ * n_sink, the last n_recent, and of those between them the n_keep - n_sink -
+ * n_recent with the largest weights; of equal weights the lower slots stay, -0 counts
+ * as 0, and NaN is below every number. The kept slots keep their order.
+ *
+ * k_cache, v_cache  bf16 [B, capacity, Hk, D]; k_out, v_out [B, capacity_out, Hk, D].
+ * weights   fp32 [B, Hk, capacity]; weights_out [B, Hk, capacity_out]: the kept
+ *           slots' weights, then zeros.
+ * cache_len device int32 [B] (clamped to [0, capacity]; checked first under
+ *           UT_VALIDATE); len_out int32 [B]: min(cache_len, n_keep).
+ * kept_idx  int32 [B, Hk, n_keep]: the slots that stay, ascending, then -1.
+ * strides_host  HOST {k_cache, v_cache, k_out, v_out} or NULL, as in ut_xattn_fwd.
+ * zero_rest 0: rows of k_out and v_out at and past n_keep are left as they were;
+ *           else they are set to 0. Rows from len_out to n_keep are set to 0 always.
+ * n_keep >= 1, n_sink >= 0, n_recent >= 0, n_sink + n_recent <= n_keep <=
+ * capacity_out; B < 65536. Outputs must not overlap inputs (checked).
+ * Errors: sizes, strides, null or misaligned pointers, overlap
+ *         -> UT_ERR_INVALID_ARG; a head_dim that is no multiple of 8 up to 128, a
+ *         stride of 2^22 or more -> UT_ERR_UNSUPPORTED.
+ * ---------------------------------------------------------------------- */
+ut_status ut_cache_evict(const void* k_cache, const void* v_cache, const float* weights,
+                         const int32_t* cache_len, void* k_out, void* v_out, float* weights_out,
+                         int32_t* len_out, int32_t* kept_idx, const int64_t* strides_host, int32_t B,
+                         int32_t capacity, int32_t capacity_out, int32_t Hk, int32_t D,
+                         int32_t n_keep, int32_t n_sink, int32_t n_recent, int32_t zero_rest,
+                         hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

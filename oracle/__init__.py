@@ -41,6 +41,9 @@ Paper sections (arXiv 2609.23169, "UltraTex"):
   * Cross attention: Eq. 5 with queries and keys of different sequences (the
     image tokens and an encoder's states), a mask over the keys and query heads
     that share key heads.
+  * Window attention, attention over a cache and eviction from it: Eq. 5 over the
+    keys that a query sees; not in the paper. The definitions are in the
+    docstrings below.
   * Batches of differing lengths: training buckets samples by their
     foreground token count (Sec. 4.1, Implementation Details), so the kept
     counts within a batch are close but not equal. The reading taken: the
@@ -57,6 +60,7 @@ __all__ = [
     "euler_update_fg", "fg_flow_loss",
     "composite_latent", "token_mask_from_alpha",
     "rope_fwd", "rope_bwd", "xattn_fwd", "xattn_bwd",
+    "window_see", "swattn_fwd", "swattn_bwd", "cache_see", "cache_attn", "cache_evict",
 ]
 
 
@@ -551,3 +555,121 @@ def xattn_bwd(q, k, v, dout, scale: float, key_mask=None):
             dK[b, :, h // G] += scale * (dS.T @ Q[b, :, h])
             dV[b, :, h // G] += P.T @ dO[b, :, h]
     return dQ, dK, dV
+
+
+# ---------------------------------------------------------------------------
+# Window attention, a cache of keys, eviction
+# ---------------------------------------------------------------------------
+
+def window_see(nq: int, nk: int, left, right, n_sink: int = 0) -> np.ndarray:
+    """[nq, nk]: query i sits at p = i + nk - nq and sees key j where
+    p - left <= j <= p + right (None: no bound), or j < n_sink and (right != 0 or
+    j <= p)."""
+    p, j = np.arange(nq)[:, None] + nk - nq, np.arange(nk)[None]
+    inside = np.ones((nq, nk), bool)
+    if left is not None:
+        inside &= j >= p - left
+    if right is not None:
+        inside &= j <= p + right
+    return inside | ((j < n_sink) & ((right != 0) | (j <= p)))
+
+
+def _seen_p(Q, K, scale: float, see):
+    """Probabilities and log-sum-exp of one head, see [Nq, Nk]; rows that see
+    nothing: 0 and -inf."""
+    with np.errstate(invalid="ignore"):
+        S = np.where(see, (Q @ K.T) * scale, -np.inf)
+    some = see.any(1)
+    m = np.where(some, S.max(1, initial=-np.inf), 0.0)[:, None]
+    E = np.where(see, np.exp(S - m), 0.0)
+    l = E.sum(1, keepdims=True)
+    lse = np.full(Q.shape[0], -np.inf)
+    lse[some] = (m + np.log(np.where(l > 0, l, 1.0)))[some, 0]
+    return E / np.where(l > 0, l, 1.0), lse
+
+
+def _see(see, key_mask, b: int):
+    return see if key_mask is None else see & np.asarray(key_mask)[b].astype(bool)[None]
+
+
+def swattn_fwd(q, k, v, scale: float, left, right, n_sink: int = 0, key_mask=None):
+    """(O, LSE [B, Hq, Nq]) of q [B, Nq, Hq, D] on k, v [B, Nk, Hk, D]; keys that
+    key_mask [B, Nk] leaves out contribute nothing, whatever they hold."""
+    Q, K, V = _f64(q), _f64(k), _f64(v)
+    B, Nq, Hq, _ = Q.shape
+    G = Hq // K.shape[2]
+    base = window_see(Nq, K.shape[1], left, right, n_sink)
+    O, LSE = np.zeros_like(Q), np.zeros((B, Hq, Nq))
+    for b in range(B):
+        see, used = _see(base, key_mask, b), _used(key_mask, b, K.shape[1])
+        for h in range(Hq):
+            Kh, Vh = (np.where(used[:, None], x[b, :, h // G], 0.0) for x in (K, V))
+            P, LSE[b, h] = _seen_p(Q[b, :, h], Kh, scale, see)
+            O[b, :, h] = P @ Vh
+    return O, LSE
+
+
+def swattn_bwd(q, k, v, dout, scale: float, left, right, n_sink: int = 0, key_mask=None):
+    """(dQ, dK, dV) of swattn_fwd."""
+    Q, K, V, dO = _f64(q), _f64(k), _f64(v), _f64(dout)
+    G = Q.shape[2] // K.shape[2]
+    base = window_see(Q.shape[1], K.shape[1], left, right, n_sink)
+    dQ, dK, dV = np.zeros_like(Q), np.zeros_like(K), np.zeros_like(V)
+    for b in range(Q.shape[0]):
+        see, used = _see(base, key_mask, b), _used(key_mask, b, K.shape[1])
+        for h in range(Q.shape[2]):
+            Kh, Vh = (np.where(used[:, None], x[b, :, h // G], 0.0) for x in (K, V))
+            P, _ = _seen_p(Q[b, :, h], Kh, scale, see)
+            dP = dO[b, :, h] @ Vh.T
+            dS = P * (dP - (P * dP).sum(1, keepdims=True))
+            dQ[b, :, h] = scale * (dS @ Kh)
+            dK[b, :, h // G] += scale * (dS.T @ Q[b, :, h])
+            dV[b, :, h // G] += P.T @ dO[b, :, h]
+    return dQ, dK, dV
+
+
+def cache_see(T: int, capacity: int, n: int, tree=None, left=None, n_sink: int = 0) -> np.ndarray:
+    """[T, capacity]: what token t sees of a cache with n slots in use in front of
+    the T tokens' own. Without a tree it sits at p = n + t and sees the slots j <= p of
+    its window, j >= p - left (None: all) or j < n_sink. With one, tree[t] holds a bit for
+    every token that it sees; it sits behind them, p = n + their number less
+    itself, and of the n slots it sees those of its window."""
+    see = np.zeros((T, capacity), bool)
+    for t in range(T):
+        drafted = list(range(t + 1)) if tree is None else [u for u in range(T) if int(tree[t]) >> u & 1]
+        p = n + (t if tree is None else sum(u != t for u in drafted))
+        for j in list(range(n)) + [n + u for u in drafted]:
+            see[t, j] = left is None or j >= p - left or j < n_sink or (tree is not None and j >= n)
+    return see
+
+
+def cache_attn(q, k, v, lens, scale: float, tree=None, left=None, n_sink: int = 0, tokens=None):
+    """(O, LSE [B, Hq, T], W [B, Hk, capacity]): q [B, T, Hq, D] on caches [B, capacity, Hk,
+    D]; W is what every slot receives, summed over the tokens (those whose bit is
+    set in tokens[b], if given) and the heads of its group. tree [B, T]."""
+    Q, K, V = _f64(q), _f64(k), _f64(v)
+    B, T, Hq, _ = Q.shape
+    cap, Hk = K.shape[1], K.shape[2]
+    G = Hq // Hk
+    O, LSE, W = np.zeros_like(Q), np.zeros((B, Hq, T)), np.zeros((B, Hk, cap))
+    for b in range(B):
+        see = cache_see(T, cap, int(lens[b]), None if tree is None else tree[b], left, n_sink)
+        used = np.arange(cap) < int(lens[b]) + T
+        counts = np.array([tokens is None or int(tokens[b]) >> t & 1 for t in range(T)], float)
+        for h in range(Hq):
+            Kh, Vh = (np.where(used[:, None], x[b, :, h // G], 0.0) for x in (K, V))
+            P, LSE[b, h] = _seen_p(Q[b, :, h], Kh, scale, see)
+            O[b, :, h] = P @ Vh
+            W[b, h // G] += counts @ P
+    return O, LSE, W
+
+
+def cache_evict(weights, n: int, n_keep: int, n_sink: int = 0, n_recent: int = 0) -> np.ndarray:
+    """The slots of one row of weights that stay, ascending: all n where n <= n_keep,
+    else the first n_sink, the last n_recent, and between them the largest, ties and NaN
+    (below every number) by the lowest slot first."""
+    if n <= n_keep:
+        return np.arange(n)
+    w = np.asarray(weights, np.float64)
+    middle = sorted(range(n_sink, n - n_recent), key=lambda j: (np.isnan(w[j]), 0.0 if np.isnan(w[j]) else -w[j], j))
+    return np.array(sorted(list(range(n_sink)) + middle[:n_keep - n_sink - n_recent] + list(range(n - n_recent, n))))

@@ -46,6 +46,10 @@ EXPORTS = [
     "ut_xattn_fwd_workspace_size", "ut_xattn_fwd", "ut_xattn_fwd_varlen_workspace_size",
     "ut_xattn_fwd_varlen", "ut_xattn_bwd_workspace_size", "ut_xattn_bwd",
     "ut_xattn_bwd_varlen_workspace_size", "ut_xattn_bwd_varlen",
+    "ut_swattn_fwd_workspace_size", "ut_swattn_fwd", "ut_swattn_fwd_varlen_workspace_size",
+    "ut_swattn_fwd_varlen", "ut_swattn_bwd_workspace_size", "ut_swattn_bwd",
+    "ut_swattn_bwd_varlen_workspace_size", "ut_swattn_bwd_varlen",
+    "ut_cache_attn_workspace_size", "ut_cache_attn", "ut_cache_weights", "ut_cache_evict",
 ]
 
 
@@ -111,6 +115,18 @@ _SIGS = {
     "ut_xattn_bwd": (_c.c_int, [_vp] * 11 + [_i32] * 6 + [_f32, _vp, _sz, _vp]),
     "ut_xattn_bwd_varlen_workspace_size": (_sz, [_i32, _i64, _i64] + [_i32] * 5),
     "ut_xattn_bwd_varlen": (_c.c_int, [_vp] * 13 + [_i32, _i64, _i64] + [_i32] * 5 + [_f32, _i32, _vp, _sz, _vp]),
+    "ut_swattn_fwd_workspace_size": (_sz, [_i32] * 9),
+    "ut_swattn_fwd": (_c.c_int, [_vp] * 7 + [_i32] * 9 + [_f32, _vp, _sz, _vp]),
+    "ut_swattn_fwd_varlen_workspace_size": (_sz, [_i32, _i64] + [_i32] * 8),
+    "ut_swattn_fwd_varlen": (_c.c_int, [_vp] * 9 + [_i32, _i64, _i64] + [_i32] * 8 + [_f32, _i32, _vp, _sz, _vp]),
+    "ut_swattn_bwd_workspace_size": (_sz, [_i32] * 9),
+    "ut_swattn_bwd": (_c.c_int, [_vp] * 11 + [_i32] * 9 + [_f32, _vp, _sz, _vp]),
+    "ut_swattn_bwd_varlen_workspace_size": (_sz, [_i32, _i64, _i64] + [_i32] * 8),
+    "ut_swattn_bwd_varlen": (_c.c_int, [_vp] * 13 + [_i32, _i64, _i64] + [_i32] * 8 + [_f32, _i32, _vp, _sz, _vp]),
+    "ut_cache_attn_workspace_size": (_sz, [_i32] * 8),
+    "ut_cache_attn": (_c.c_int, [_vp] * 10 + [_i32] * 8 + [_f32, _vp, _sz, _vp]),
+    "ut_cache_weights": (_c.c_int, [_vp] * 9 + [_i32] * 8 + [_f32, _vp]),
+    "ut_cache_evict": (_c.c_int, [_vp] * 10 + [_i32] * 9 + [_vp]),
 }
 
 _lib = None
@@ -701,6 +717,169 @@ def ut_xattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_seq
         int(zero_rest)), workspace, stream)
 
 
+def _window(window, n_sink: int):
+    """(left, right, n_sink) of a window (left, right), None: no bound on that side."""
+    left, right = (-1 if w is None else int(w) for w in window)
+    _need(min(left, right) >= -1 and _in_int32(left, right, n_sink), "window: two numbers of keys >= 0, or None")
+    return left, right, n_sink
+
+
+def ut_swattn_fwd_workspace_size(B: int, Nq: int, Nk: int, Hq: int, Hk: int, D: int, window, n_sink: int = 0) -> int:
+    return _size(lib().ut_swattn_fwd_workspace_size, B, Nq, Nk, Hq, Hk, D, *_window(window, n_sink))
+
+
+def ut_swattn_fwd(q, k, v, o, lse, window, softmax_scale: float, n_sink: int = 0, key_mask=None, workspace=None,
+                  stream=None) -> int:
+    (B, Nq), (_, Nk), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 4)
+    _like(o, q, "o")
+    _check_lse(lse, B * Hq * Nq)
+    a = _Args(q)
+    rows = (a.rows(q, "q"), a.rows(k, "k"), a.rows(v, "v"), a.rows(o, "o"))
+    return a.call(lib().ut_swattn_fwd, rows + (a.ptr(lse, "lse"), a.host_strides(), a.ptr(key_mask, "key_mask"), B, Nq,
+                                               Nk, Hq, Hk, D) + _window(window, n_sink) + (softmax_scale,), workspace,
+                  stream)
+
+
+def ut_swattn_fwd_varlen_workspace_size(B: int, Tq: int, max_seqlen_q: int, max_seqlen_k: int, Hq: int, Hk: int,
+                                        D: int, window, n_sink: int = 0) -> int:
+    return _size(lib().ut_swattn_fwd_varlen_workspace_size, B, Tq, max_seqlen_q, max_seqlen_k, Hq, Hk, D,
+                 *_window(window, n_sink))
+
+
+def ut_swattn_fwd_varlen(q, k, v, o, lse, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k, max_seqlen_k: int, window,
+                         softmax_scale: float, n_sink: int = 0, key_mask=None, zero_rest: bool = False,
+                         workspace=None, stream=None) -> int:
+    (Tq,), (Tk,), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 3)
+    B = _check_cu(cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k)
+    _like(o, q, "o")
+    _check_lse(lse, Hq * Tq)
+    a = _Args(q)
+    rows = (a.rows(q, "q"), a.rows(k, "k"), a.rows(v, "v"), a.rows(o, "o"))
+    return a.call(lib().ut_swattn_fwd_varlen,
+                  rows + (a.ptr(lse, "lse"), a.host_strides(), a.ptr(key_mask, "key_mask"),
+                          a.ptr(cu_seqlens_q, "cu_seqlens_q"), a.ptr(cu_seqlens_k, "cu_seqlens_k"), B, Tq, Tk,
+                          max_seqlen_q, max_seqlen_k, Hq, Hk, D) + _window(window, n_sink)
+                  + (softmax_scale, int(zero_rest)), workspace, stream)
+
+
+def ut_swattn_bwd_workspace_size(B: int, Nq: int, Nk: int, Hq: int, Hk: int, D: int, window, n_sink: int = 0) -> int:
+    return _size(lib().ut_swattn_bwd_workspace_size, B, Nq, Nk, Hq, Hk, D, *_window(window, n_sink))
+
+
+def ut_swattn_bwd(q, k, v, o, dout, lse, dq, dk, dv, window, softmax_scale: float, n_sink: int = 0, key_mask=None,
+                  workspace=None, stream=None) -> int:
+    (B, Nq), (_, Nk), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 4)
+    _check_lse(lse, B * Hq * Nq)
+    a = _Args(q)
+    ins, outs = _bwd_rows(a, q, k, v, o, dout, dq, dk, dv)
+    return a.call(lib().ut_swattn_bwd, ins + (a.ptr(lse, "lse"),) + outs + (
+        a.host_strides(), a.ptr(key_mask, "key_mask"), B, Nq, Nk, Hq, Hk, D) + _window(window, n_sink)
+        + (softmax_scale,), workspace, stream)
+
+
+def ut_swattn_bwd_varlen_workspace_size(B: int, Tq: int, Tk: int, max_seqlen_q: int, max_seqlen_k: int, Hq: int,
+                                        Hk: int, D: int, window, n_sink: int = 0) -> int:
+    return _size(lib().ut_swattn_bwd_varlen_workspace_size, B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D,
+                 *_window(window, n_sink))
+
+
+def ut_swattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k,
+                         max_seqlen_k: int, window, softmax_scale: float, n_sink: int = 0, key_mask=None,
+                         zero_rest: bool = False, workspace=None, stream=None) -> int:
+    (Tq,), (Tk,), Hq, Hk, D = _xattn_args(q, k, v, key_mask, 3)
+    B = _check_cu(cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k)
+    _check_lse(lse, Hq * Tq)
+    a = _Args(q)
+    ins, outs = _bwd_rows(a, q, k, v, o, dout, dq, dk, dv)
+    return a.call(lib().ut_swattn_bwd_varlen, ins + (a.ptr(lse, "lse"),) + outs + (
+        a.host_strides(), a.ptr(key_mask, "key_mask"), a.ptr(cu_seqlens_q, "cu_seqlens_q"),
+        a.ptr(cu_seqlens_k, "cu_seqlens_k"), B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D)
+        + _window(window, n_sink) + (softmax_scale, int(zero_rest)), workspace, stream)
+
+
+def _check_slots(cache_len, B: int, name: str = "cache_len"):
+    _need(cache_len.dtype == torch.int32 and cache_len.shape == (B,) and cache_len.is_contiguous(),
+          f"{name}: contiguous int32 [B]")
+
+
+def _check_words(t, shape, name: str):
+    _need(t is None or (t.dtype in (torch.int64, torch.uint64) and t.shape == shape and t.is_contiguous()),
+          f"{name}: contiguous int64 or uint64 {list(shape)}")
+
+
+def _check_weights(t, shape, name: str):
+    _need(t is None or (t.dtype == torch.float32 and t.shape == shape and t.is_contiguous()),
+          f"{name}: contiguous fp32 {list(shape)}")
+
+
+def ut_cache_attn_workspace_size(B: int, T: int, capacity: int, Hq: int, Hk: int, D: int, window_left=None,
+                                 n_sink: int = 0) -> int:
+    return _size(lib().ut_cache_attn_workspace_size, B, T, capacity, Hq, Hk, D, _window((window_left, 0), n_sink)[0],
+                 n_sink)
+
+
+def ut_cache_attn(q, k_cache, v_cache, o, lse, cache_len, softmax_scale: float, tree=None, window_left=None,
+                  n_sink: int = 0, weights_in=None, weights_out=None, workspace=None, stream=None) -> int:
+    (B, T), (_, cap), Hq, Hk, D = _xattn_args(q, k_cache, v_cache, None, 4)
+    _like(o, q, "o")
+    _check_lse(lse, B * Hq * T)
+    _check_slots(cache_len, B)
+    _check_words(tree, (B, T), "tree")
+    for w, nm in ((weights_in, "weights_in"), (weights_out, "weights_out")):
+        _check_weights(w, (B, Hk, cap), nm)
+    left, _, n_sink = _window((window_left, 0), n_sink)
+    a = _Args(q)
+    rows = (a.rows(q, "q"), a.rows(k_cache, "k_cache"), a.rows(v_cache, "v_cache"), a.rows(o, "o"))
+    return a.call(lib().ut_cache_attn,
+                  rows + (a.ptr(lse, "lse"), a.host_strides(), a.ptr(cache_len, "cache_len"), a.ptr(tree, "tree"),
+                          a.ptr(weights_in, "weights_in"), a.ptr(weights_out, "weights_out"), B, T, cap, Hq, Hk, D,
+                          left, n_sink, softmax_scale), workspace, stream)
+
+
+def ut_cache_weights(q, k_cache, lse, cache_len, weights_out, softmax_scale: float, tree=None, tokens=None,
+                     window_left=None, n_sink: int = 0, weights_in=None, stream=None) -> int:
+    (B, T), (_, cap), Hq, Hk, D = _xattn_args(q, k_cache, k_cache, None, 4)
+    _check_lse(lse, B * Hq * T)
+    _check_slots(cache_len, B)
+    _check_words(tree, (B, T), "tree")
+    _check_words(tokens, (B,), "tokens")
+    for w, nm in ((weights_in, "weights_in"), (weights_out, "weights_out")):
+        _check_weights(w, (B, Hk, cap), nm)
+    left, _, n_sink = _window((window_left, 0), n_sink)
+    a = _Args(q)
+    rows = (a.rows(q, "q"), a.rows(k_cache, "k_cache"))
+    return a.call(lib().ut_cache_weights,
+                  rows + (a.ptr(lse, "lse"), a.host_strides(), a.ptr(cache_len, "cache_len"), a.ptr(tree, "tree"),
+                          a.ptr(tokens, "tokens"), a.ptr(weights_in, "weights_in"), a.ptr(weights_out, "weights_out"),
+                          B, T, cap, Hq, Hk, D, left, n_sink, softmax_scale), None, stream, takes_workspace=False)
+
+
+def ut_cache_evict(k_cache, v_cache, weights, cache_len, k_out, v_out, weights_out, len_out, kept_idx, n_keep: int,
+                   n_sink: int = 0, n_recent: int = 0, zero_rest: bool = False, stream=None) -> int:
+    bf, shape = torch.bfloat16, k_cache.shape
+    for t in (k_cache, v_cache, k_out, v_out):
+        _need(t.dtype == bf and t.dim() == 4, "k_cache, v_cache, k_out, v_out: bf16 [B, capacity, Hk, D]")
+    _need(v_cache.shape == shape and v_out.shape == k_out.shape and k_out.shape[0] == shape[0]
+          and k_out.shape[2:] == shape[2:], "k_cache, v_cache and k_out, v_out: pairs of one shape, one B, Hk and D")
+    B, cap, Hk, D = shape
+    cap_out = k_out.shape[1]
+    _need(_in_int32(B, cap, cap_out, Hk, D, n_keep, n_sink, n_recent), "sizes past 32 bits")
+    _check_weights(weights, (B, Hk, cap), "weights")
+    _check_weights(weights_out, (B, Hk, cap_out), "weights_out")
+    _check_slots(cache_len, B)
+    _check_slots(len_out, B, "len_out")
+    _need(kept_idx.dtype == torch.int32 and kept_idx.shape == (B, Hk, n_keep) and kept_idx.is_contiguous(),
+          "kept_idx: contiguous int32 [B, Hk, n_keep]")
+    a = _Args(k_cache)
+    rows = (a.rows(k_cache, "k_cache"), a.rows(v_cache, "v_cache"))
+    outs = (a.rows(k_out, "k_out"), a.rows(v_out, "v_out"))
+    return a.call(lib().ut_cache_evict,
+                  rows + (a.ptr(weights, "weights"), a.ptr(cache_len, "cache_len")) + outs + (
+                      a.ptr(weights_out, "weights_out"), a.ptr(len_out, "len_out"), a.ptr(kept_idx, "kept_idx"),
+                      a.host_strides(), B, cap, cap_out, Hk, D, n_keep, n_sink, n_recent, int(zero_rest)), None,
+                  stream, takes_workspace=False)
+
+
 # ---------------------------------------------------------------------------
 # Allocating helpers (raise on error)
 # ---------------------------------------------------------------------------
@@ -990,3 +1169,122 @@ def xattn_bwd_varlen(q, k, v, o, dout, lse, cu_seqlens_q, max_seqlen_q: int, cu_
            ut_xattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_seqlen_q, cu_seqlens_k,
                                max_seqlen_k, softmax_scale, key_mask, True, workspace, stream))
     return dq, dk, dv
+
+
+def swattn_fwd(q, k, v, window, softmax_scale: float, n_sink: int = 0, key_mask=None, workspace=None, stream=None):
+    """Window attention of q [B, Nq, Hq, D] to k, v [B, Nk, Hk, D]: query i, at position
+    p = i + Nk - Nq, sees the keys p - left .. p + right of window (left, right) - None: no
+    bound - and the first n_sink keys (with right = 0 none behind p), of key_mask
+    [B, Nk] those in use: (o like q, lse [B, Hq, Nq])."""
+    B, Nq, Hq, D = q.shape
+    with _alloc_on(stream):
+        o = _new_rows(q)
+        lse = torch.empty((B, Hq, Nq), dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = _scratch(ut_swattn_fwd_workspace_size(B, Nq, k.shape[1], Hq, k.shape[2], D, window, n_sink),
+                                 q.device)
+    _raise("ut_swattn_fwd", ut_swattn_fwd(q, k, v, o, lse, window, softmax_scale, n_sink, key_mask, workspace, stream))
+    return o, lse
+
+
+def swattn_bwd(q, k, v, o, dout, lse, window, softmax_scale: float, n_sink: int = 0, key_mask=None, workspace=None,
+               stream=None):
+    """(dq, dk, dv) of swattn_fwd."""
+    B, Nq, Hq, D = q.shape
+    with _alloc_on(stream):
+        dq, dk, dv = _new_rows(q), _new_rows(k), _new_rows(v)
+        if workspace is None:
+            workspace = _scratch(ut_swattn_bwd_workspace_size(B, Nq, k.shape[1], Hq, k.shape[2], D, window, n_sink),
+                                 q.device)
+    _raise("ut_swattn_bwd", ut_swattn_bwd(q, k, v, o, dout, lse, dq, dk, dv, window, softmax_scale, n_sink, key_mask,
+                                          workspace, stream))
+    return dq, dk, dv
+
+
+def swattn_fwd_varlen(q, k, v, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k, max_seqlen_k: int, window,
+                      softmax_scale: float, n_sink: int = 0, key_mask=None, workspace=None, stream=None):
+    """swattn_fwd of packed samples, q [Tq, Hq, D], k, v [Tk, Hk, D]: positions and
+    sinks count within each sample: (o like q, lse [Hq, Tq]). Rows behind the last
+    sample are 0 and -inf."""
+    Tq, Hq, D = q.shape
+    with _alloc_on(stream):
+        o = _new_rows(q)
+        lse = torch.empty((Hq, Tq), dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = _scratch(ut_swattn_fwd_varlen_workspace_size(cu_seqlens_q.numel() - 1, Tq, max_seqlen_q,
+                                                                     max_seqlen_k, Hq, k.shape[1], D, window, n_sink),
+                                 q.device)
+    _raise("ut_swattn_fwd_varlen",
+           ut_swattn_fwd_varlen(q, k, v, o, lse, cu_seqlens_q, max_seqlen_q, cu_seqlens_k, max_seqlen_k, window,
+                                softmax_scale, n_sink, key_mask, True, workspace, stream))
+    return o, lse
+
+
+def swattn_bwd_varlen(q, k, v, o, dout, lse, cu_seqlens_q, max_seqlen_q: int, cu_seqlens_k, max_seqlen_k: int, window,
+                      softmax_scale: float, n_sink: int = 0, key_mask=None, workspace=None, stream=None):
+    """(dq, dk, dv) of swattn_fwd_varlen; rows behind the last sample are 0."""
+    Tq, Hq, D = q.shape
+    with _alloc_on(stream):
+        dq, dk, dv = _new_rows(q), _new_rows(k), _new_rows(v)
+        if workspace is None:
+            workspace = _scratch(ut_swattn_bwd_varlen_workspace_size(cu_seqlens_q.numel() - 1, Tq, k.shape[0],
+                                                                     max_seqlen_q, max_seqlen_k, Hq, k.shape[1], D,
+                                                                     window, n_sink), q.device)
+    _raise("ut_swattn_bwd_varlen",
+           ut_swattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_seqlen_q, cu_seqlens_k,
+                                max_seqlen_k, window, softmax_scale, n_sink, key_mask, True, workspace, stream))
+    return dq, dk, dv
+
+
+def cache_attn(q, k_cache, v_cache, cache_len, softmax_scale: float, tree=None, window_left=None, n_sink: int = 0,
+               weights=None, weights_out=None, workspace=None, stream=None):
+    """Attention of the tokens q [B, T, Hq, D] over caches [B, capacity, Hk, D] that hold
+    cache_len [B] (int32) slots in front of the tokens' own T: (o like q, lse [B, Hq, T]).
+    tree: int64 [B, T], bit u of token t's word set where it sees token u, itself
+    included; without one token t sees tokens 0 .. t. With weights [B, Hk, capacity] also
+    their sum with what every slot receives from these tokens (into weights_out if
+    given, which may be weights)."""
+    B, T, Hq, D = q.shape
+    cap, Hk = k_cache.shape[1], k_cache.shape[2]
+    with _alloc_on(stream):
+        o = _new_rows(q)
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device)
+        if weights is not None and weights_out is None:
+            weights_out = torch.empty_like(weights)
+        if workspace is None:
+            workspace = _scratch(ut_cache_attn_workspace_size(B, T, cap, Hq, Hk, D, window_left, n_sink), q.device)
+    _raise("ut_cache_attn", ut_cache_attn(q, k_cache, v_cache, o, lse, cache_len, softmax_scale, tree, window_left,
+                                          n_sink, weights, weights_out, workspace, stream))
+    return (o, lse) if weights_out is None else (o, lse, weights_out)
+
+
+def cache_weights(q, k_cache, lse, cache_len, softmax_scale: float, weights=None, tree=None, tokens=None,
+                  window_left=None, n_sink: int = 0, weights_out=None, stream=None):
+    """weights (None: zeros) and what every slot receives from the tokens of a
+    cache_attn call whose bit is set in tokens, int64 [B] (None: all): fp32
+    [B, Hk, capacity], into weights_out if given (which may be weights)."""
+    B, cap, Hk, _ = k_cache.shape
+    with _alloc_on(stream):
+        if weights_out is None:
+            weights_out = torch.empty((B, Hk, cap), dtype=torch.float32, device=q.device)
+    _raise("ut_cache_weights", ut_cache_weights(q, k_cache, lse, cache_len, weights_out, softmax_scale, tree, tokens,
+                                                window_left, n_sink, weights, stream))
+    return weights_out
+
+
+def cache_evict(k_cache, v_cache, weights, cache_len, n_keep: int, n_sink: int = 0, n_recent: int = 0, capacity=None,
+                stream=None):
+    """The n_keep slots of each sample and key head that stay - the first n_sink, the
+    last n_recent, and between them those of the largest weights - moved into caches
+    of `capacity` slots (n_keep by default): (k, v, weights, cache_len, kept_idx
+    [B, Hk, n_keep]). Slots behind are 0, and -1 in kept_idx."""
+    B, _, Hk, D = k_cache.shape
+    cap, dev = n_keep if capacity is None else capacity, k_cache.device
+    with _alloc_on(stream):
+        k, v = (torch.empty((B, cap, Hk, D), dtype=torch.bfloat16, device=dev) for _ in range(2))
+        w = torch.empty((B, Hk, cap), dtype=torch.float32, device=dev)
+        n = torch.empty(B, dtype=torch.int32, device=dev)
+        idx = torch.empty((B, Hk, n_keep), dtype=torch.int32, device=dev)
+    _raise("ut_cache_evict", ut_cache_evict(k_cache, v_cache, weights, cache_len, k, v, w, n, idx, n_keep, n_sink,
+                                            n_recent, True, stream))
+    return k, v, w, n, idx

@@ -1061,4 +1061,294 @@ ut_status ut_xattn_bwd_varlen(const void* q, const void* k, const void* v, const
                    workspace_bytes, zero_rest != 0, stream);
 }
 
+// ---- window attention ----
+namespace {
+// check_xattn and the window; a side without a bound becomes wider than any sample.
+ut_status check_window(const char* fn, int32_t B, int64_t Tq, int64_t Tk, int32_t Nq, int32_t Nk,
+                       int32_t Hq, int32_t Hk, int32_t D, int32_t left, int32_t right, int32_t n_sink,
+                       float scale, XArgs* a) {
+  UT_TRY(check_xattn(fn, B, Tq, Tk, Nq, Nk, Hq, Hk, D, scale, a));
+  if (left < -1 || right < -1)
+    return fail(UT_ERR_INVALID_ARG, "%s: window of %d and %d keys (>= 0, or -1: no bound)", fn, left, right);
+  if (n_sink < 0) return fail(UT_ERR_INVALID_ARG, "%s: n_sink must be >= 0 (got %d)", fn, n_sink);
+  a->window = true;
+  a->left = left < 0 ? kXMaxWindow : std::min(left, kXMaxWindow);
+  a->right = right < 0 ? kXMaxWindow : std::min(right, kXMaxWindow);
+  a->sinks = std::min(n_sink, std::max(Nk, 0));
+  return UT_OK;
+}
+bool window_sizes(int32_t B, int64_t Tq, int64_t Tk, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk,
+                  int32_t D, int32_t left, int32_t right, int32_t n_sink, XArgs* a) {
+  const bool ok = check_window("ut_swattn", B, Tq, Tk, Nq, Nk, Hq, Hk, D, left, right, n_sink, 1.f, a) == UT_OK;
+  g_last_error[0] = 0;
+  return ok;
+}
+}  // namespace
+
+size_t ut_swattn_fwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk,
+                                    int32_t D, int32_t window_left, int32_t window_right,
+                                    int32_t n_sink) {
+  XArgs a{};
+  return window_sizes(B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, window_left, window_right,
+                      n_sink, &a)
+             ? xattn_fwd_workspace(a)
+             : 0;
+}
+
+ut_status ut_swattn_fwd(const void* q, const void* k, const void* v, void* o, float* lse,
+                        const int64_t* strides_host, const uint8_t* key_mask, int32_t B,
+                        int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk, int32_t D,
+                        int32_t window_left, int32_t window_right, int32_t n_sink,
+                        float softmax_scale, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream) {
+  static const char* fn = "ut_swattn_fwd";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_window(fn, B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, window_left, window_right,
+                      n_sink, softmax_scale, &a));
+  return xattn_fwd(fn, a, q, k, v, o, lse, strides_host, key_mask, workspace, workspace_bytes, false,
+                   stream);
+}
+
+size_t ut_swattn_fwd_varlen_workspace_size(int32_t B, int64_t Tq, int32_t max_seqlen_q,
+                                           int32_t max_seqlen_k, int32_t Hq, int32_t Hk, int32_t D,
+                                           int32_t window_left, int32_t window_right,
+                                           int32_t n_sink) {
+  XArgs a{};
+  return window_sizes(B, Tq, 0, max_seqlen_q, max_seqlen_k, Hq, Hk, D, window_left, window_right, n_sink, &a)
+             ? xattn_fwd_workspace(a)
+             : 0;
+}
+
+ut_status ut_swattn_fwd_varlen(const void* q, const void* k, const void* v, void* o, float* lse,
+                               const int64_t* strides_host, const uint8_t* key_mask,
+                               const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t B,
+                               int64_t Tq, int64_t Tk, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                               int32_t Hq, int32_t Hk, int32_t D, int32_t window_left,
+                               int32_t window_right, int32_t n_sink, float softmax_scale,
+                               int32_t zero_rest, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream) {
+  static const char* fn = "ut_swattn_fwd_varlen";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_window(fn, B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, window_left, window_right, n_sink,
+                      softmax_scale, &a));
+  UT_TRY(check_cu(fn, "cu_seqlens_q", cu_seqlens_q, B, Tq, max_seqlen_q, stream));
+  UT_TRY(check_cu(fn, "cu_seqlens_k", cu_seqlens_k, B, Tk, max_seqlen_k, stream));
+  a.cuq = cu_seqlens_q, a.cuk = cu_seqlens_k;
+  return xattn_fwd(fn, a, q, k, v, o, lse, strides_host, key_mask, workspace, workspace_bytes,
+                   zero_rest != 0, stream);
+}
+
+size_t ut_swattn_bwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk,
+                                    int32_t D, int32_t window_left, int32_t window_right,
+                                    int32_t n_sink) {
+  XArgs a{};
+  return window_sizes(B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, window_left, window_right,
+                      n_sink, &a) &&
+                 xattn_bwd_launchable(a)
+             ? xattn_bwd_workspace(a)
+             : 0;
+}
+
+ut_status ut_swattn_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                        const float* lse, void* dq, void* dk, void* dv, const int64_t* strides_host,
+                        const uint8_t* key_mask, int32_t B, int32_t Nq, int32_t Nk, int32_t Hq,
+                        int32_t Hk, int32_t D, int32_t window_left, int32_t window_right,
+                        int32_t n_sink, float softmax_scale, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream) {
+  static const char* fn = "ut_swattn_bwd";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_window(fn, B, (int64_t)B * Nq, (int64_t)B * Nk, Nq, Nk, Hq, Hk, D, window_left, window_right,
+                      n_sink, softmax_scale, &a));
+  UT_TRY(check_xattn_bwd(fn, a));
+  return xattn_bwd(fn, a, q, k, v, o, dout, lse, dq, dk, dv, strides_host, key_mask, workspace,
+                   workspace_bytes, false, stream);
+}
+
+size_t ut_swattn_bwd_varlen_workspace_size(int32_t B, int64_t Tq, int64_t Tk, int32_t max_seqlen_q,
+                                           int32_t max_seqlen_k, int32_t Hq, int32_t Hk, int32_t D,
+                                           int32_t window_left, int32_t window_right,
+                                           int32_t n_sink) {
+  XArgs a{};
+  return window_sizes(B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, window_left, window_right, n_sink,
+                      &a) &&
+                 xattn_bwd_launchable(a)
+             ? xattn_bwd_workspace(a)
+             : 0;
+}
+
+ut_status ut_swattn_bwd_varlen(const void* q, const void* k, const void* v, const void* o,
+                               const void* dout, const float* lse, void* dq, void* dk, void* dv,
+                               const int64_t* strides_host, const uint8_t* key_mask,
+                               const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t B,
+                               int64_t Tq, int64_t Tk, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                               int32_t Hq, int32_t Hk, int32_t D, int32_t window_left,
+                               int32_t window_right, int32_t n_sink, float softmax_scale,
+                               int32_t zero_rest, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream) {
+  static const char* fn = "ut_swattn_bwd_varlen";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_window(fn, B, Tq, Tk, max_seqlen_q, max_seqlen_k, Hq, Hk, D, window_left, window_right, n_sink,
+                      softmax_scale, &a));
+  UT_TRY(check_xattn_bwd(fn, a));
+  UT_TRY(check_cu(fn, "cu_seqlens_q", cu_seqlens_q, B, Tq, max_seqlen_q, stream));
+  UT_TRY(check_cu(fn, "cu_seqlens_k", cu_seqlens_k, B, Tk, max_seqlen_k, stream));
+  a.cuq = cu_seqlens_q, a.cuk = cu_seqlens_k;
+  return xattn_bwd(fn, a, q, k, v, o, dout, lse, dq, dk, dv, strides_host, key_mask, workspace,
+                   workspace_bytes, zero_rest != 0, stream);
+}
+
+// ---- attention over a cache, its weights, eviction ----
+namespace {
+ut_status check_cache(const char* fn, int32_t B, int32_t T, int32_t capacity, int32_t Hq, int32_t Hk,
+                      int32_t D, int32_t left, int32_t n_sink, bool tree, float scale, XArgs* a) {
+  if (T < 1 || T > capacity)
+    return fail(UT_ERR_INVALID_ARG, "%s: T must be in 1 .. capacity (got %d of %d)", fn, T, capacity);
+  UT_TRY(check_window(fn, B, (int64_t)B * T, (int64_t)B * capacity, T, capacity, Hq, Hk, D, left, 0, n_sink,
+                      scale, a));
+  if (tree && T > 64) return fail(UT_ERR_INVALID_ARG, "%s: a tree of %d tokens (at most 64)", fn, T);
+  if (tree && a->left < T - 1)
+    return fail(UT_ERR_INVALID_ARG, "%s: with a tree the window must hold its %d tokens (window_left %d)", fn, T,
+                left);
+  return UT_OK;
+}
+
+// Slots in use, on the device; under UT_VALIDATE copied to the host and checked.
+ut_status check_lens(const char* fn, const int32_t* lens, int32_t B, int32_t most, hipStream_t stream) {
+  UT_TRY(check_ptr(fn, "cache_len", lens, 4));
+  if (!validate_mode()) return UT_OK;
+  std::vector<int32_t> v;
+  UT_TRY(validate_copy(lens, (size_t)B, &v, stream));
+  for (int32_t b = 0; b < B; ++b)
+    if (v[(size_t)b] < 0 || v[(size_t)b] > most)
+      return fail(UT_ERR_INVALID_ARG, "%s: cache_len of sample %d is %d, outside [0, %d]", fn, b, v[(size_t)b], most);
+  return UT_OK;
+}
+
+ut_status check_words(const char* fn, const char* name, const uint64_t* p) {
+  return p ? check_ptr(fn, name, p, 8) : UT_OK;
+}
+
+struct Range {   // bytes
+  const char* p;
+  int64_t n;
+};
+bool overlap(const Range& x, const Range& y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+  return a < b + (uintptr_t)y.n && b < a + (uintptr_t)x.n;
+}
+}  // namespace
+
+size_t ut_cache_attn_workspace_size(int32_t B, int32_t T, int32_t capacity, int32_t Hq, int32_t Hk,
+                                    int32_t D, int32_t window_left, int32_t n_sink) {
+  XArgs a{};
+  const bool ok = check_cache("ut_cache_attn", B, T, capacity, Hq, Hk, D, window_left, n_sink, false, 1.f, &a) == UT_OK;
+  g_last_error[0] = 0;
+  return ok ? xattn_fwd_workspace(a) : 0;
+}
+
+ut_status ut_cache_attn(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
+                        const int64_t* strides_host, const int32_t* cache_len, const uint64_t* tree,
+                        const float* weights_in, float* weights_out, int32_t B, int32_t T,
+                        int32_t capacity, int32_t Hq, int32_t Hk, int32_t D, int32_t window_left,
+                        int32_t n_sink, float softmax_scale, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream) {
+  static const char* fn = "ut_cache_attn";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_cache(fn, B, T, capacity, Hq, Hk, D, window_left, n_sink, tree != nullptr, softmax_scale, &a));
+  UT_TRY(check_words(fn, "tree", tree));
+  if (weights_in) UT_TRY(check_ptr(fn, "weights_in", weights_in, 4));
+  if (weights_in || weights_out) UT_TRY(check_ptr(fn, "weights_out", weights_out, 4));
+  UT_TRY(check_lens(fn, cache_len, B, capacity - T, stream));
+  a.lens = cache_len, a.tree = tree;
+  UT_TRY(xattn_fwd(fn, a, q, k_cache, v_cache, o, lse, strides_host, nullptr, workspace, workspace_bytes, false,
+                   stream));
+  if (!weights_out) return UT_OK;
+  return check_hip(launch_cache_weights(a, CacheWeights{weights_in, weights_out, nullptr}, stream),
+                   "cache weights launch");
+}
+
+ut_status ut_cache_weights(const void* q, const void* k_cache, const float* lse,
+                           const int64_t* strides_host, const int32_t* cache_len,
+                           const uint64_t* tree, const uint64_t* tokens, const float* weights_in,
+                           float* weights_out, int32_t B, int32_t T, int32_t capacity, int32_t Hq,
+                           int32_t Hk, int32_t D, int32_t window_left, int32_t n_sink,
+                           float softmax_scale, hipStream_t stream) {
+  static const char* fn = "ut_cache_weights";
+  g_last_error[0] = 0;
+  XArgs a{};
+  UT_TRY(check_cache(fn, B, T, capacity, Hq, Hk, D, window_left, n_sink, tree != nullptr, softmax_scale, &a));
+  if (tokens && T > 64) return fail(UT_ERR_INVALID_ARG, "%s: bits for %d tokens (at most 64)", fn, T);
+  const XTensor t[] = {{"q", q, &a.sq, false}, {"k_cache", k_cache, &a.sk, true}};
+  UT_TRY(check_xtensors(fn, t, 2, strides_host, a));
+  UT_TRY(check_ptr(fn, "lse", lse, 4));
+  UT_TRY(check_words(fn, "tree", tree));
+  UT_TRY(check_words(fn, "tokens", tokens));
+  if (weights_in) UT_TRY(check_ptr(fn, "weights_in", weights_in, 4));
+  UT_TRY(check_ptr(fn, "weights_out", weights_out, 4));
+  UT_TRY(check_lens(fn, cache_len, B, capacity - T, stream));
+  a.q = q, a.k = k_cache, a.lse = const_cast<float*>(lse), a.lens = cache_len, a.tree = tree;
+  return check_hip(launch_cache_weights(a, CacheWeights{weights_in, weights_out, tokens}, stream),
+                   "cache weights launch");
+}
+
+ut_status ut_cache_evict(const void* k_cache, const void* v_cache, const float* weights,
+                         const int32_t* cache_len, void* k_out, void* v_out, float* weights_out,
+                         int32_t* len_out, int32_t* kept_idx, const int64_t* strides_host, int32_t B,
+                         int32_t capacity, int32_t capacity_out, int32_t Hk, int32_t D,
+                         int32_t n_keep, int32_t n_sink, int32_t n_recent, int32_t zero_rest,
+                         hipStream_t stream) {
+  static const char* fn = "ut_cache_evict";
+  g_last_error[0] = 0;
+  if (B < 1 || B > 65535 || Hk < 1 || capacity < 1)
+    return fail(UT_ERR_INVALID_ARG, "%s: B in 1 .. 65535, Hk and capacity >= 1 (got %d, %d, %d)", fn, B, Hk, capacity);
+  if (n_keep < 1 || n_keep > capacity_out)
+    return fail(UT_ERR_INVALID_ARG, "%s: n_keep must be in 1 .. capacity_out (got %d of %d)", fn, n_keep, capacity_out);
+  if (n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > n_keep)
+    return fail(UT_ERR_INVALID_ARG, "%s: n_sink and n_recent must be >= 0 and at most n_keep together (got %d, %d of %d)",
+                fn, n_sink, n_recent, n_keep);
+  if (D < 8 || D % 8 != 0 || D > 128)
+    return fail(UT_ERR_UNSUPPORTED, "%s: head_dim %d unsupported (a multiple of 8 up to 128)", fn, D);
+  const int64_t most = (int64_t)1 << 27;
+  if ((int64_t)B * capacity >= most || (int64_t)B * capacity * Hk >= most || (int64_t)B * capacity_out >= most ||
+      (int64_t)B * capacity_out * Hk >= most)
+    return fail(UT_ERR_INVALID_ARG, "%s: problem too large (2^27 rows of a head or more)", fn);
+  CacheEvict a{};
+  const int64_t row = (int64_t)Hk * D;
+  const char* const names[] = {"k_cache", "v_cache", "k_out", "v_out"};
+  const void* const rows[] = {k_cache, v_cache, k_out, v_out};
+  int64_t* const strides[] = {&a.sk, &a.sv, &a.sko, &a.svo};
+  Range at[6];
+  for (int i = 0; i < 4; ++i) {
+    UT_TRY(check_stride(fn, names[i], strides_host, i, row, 8, kXMaxStride, strides[i]));
+    UT_TRY(check_ptr(fn, names[i], rows[i], 16));
+    at[i] = Range{static_cast<const char*>(rows[i]),
+                  (((int64_t)B * (i < 2 ? capacity : capacity_out) - 1) * *strides[i] + row) * 2};
+  }
+  UT_TRY(check_ptr(fn, "weights", weights, 4));
+  UT_TRY(check_ptr(fn, "weights_out", weights_out, 4));
+  UT_TRY(check_ptr(fn, "len_out", len_out, 4));
+  UT_TRY(check_ptr(fn, "kept_idx", kept_idx, 4));
+  at[4] = Range{reinterpret_cast<const char*>(weights), (int64_t)B * Hk * capacity * 4};
+  at[5] = Range{reinterpret_cast<const char*>(weights_out), (int64_t)B * Hk * capacity_out * 4};
+  for (int i : {0, 1, 4})
+    for (int o : {2, 3, 5})
+      if (overlap(at[i], at[o]))
+        return fail(UT_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, o < 4 ? names[o] : "weights_out",
+                    i < 4 ? names[i] : "weights");
+  if (overlap(Range{reinterpret_cast<const char*>(len_out), (int64_t)B * 4},
+              Range{reinterpret_cast<const char*>(cache_len), (int64_t)B * 4}))
+    return fail(UT_ERR_INVALID_ARG, "%s: len_out overlaps cache_len", fn);
+  UT_TRY(check_lens(fn, cache_len, B, capacity, stream));
+  a.k = k_cache, a.v = v_cache, a.k_out = k_out, a.v_out = v_out;
+  a.weights = weights, a.weights_out = weights_out, a.lens = cache_len, a.len_out = len_out, a.idx = kept_idx;
+  a.B = B, a.cap = capacity, a.cap_out = capacity_out, a.Hk = Hk, a.D = D;
+  a.keep = n_keep, a.sinks = n_sink, a.recent = n_recent, a.zero_rest = zero_rest != 0;
+  return check_hip(launch_cache_evict(a, stream), "cache eviction launch");
+}
+
 }  // extern "C"

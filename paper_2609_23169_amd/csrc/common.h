@@ -219,7 +219,16 @@ struct XArgs {
   int sq, sk, sv, so, sdo, sdq, sdk, sdv;
   float scale;
   bool zero_rest;                  // packed: rows behind the last sample become 0
+  // Window attention (window): a query at position p = its token + nk - nq of its sample
+  // sees the keys p - left .. p + right, and the first `sinks` keys (right = 0: up to p).
+  bool window;
+  int left, right, sinks;
+  // A cache (lens): sample b has lens[b] + Nq of its Nk slots in use, clamped to them;
+  // tree: which of the last Nq a query sees, a bit each, in place of those up to its own.
+  const int32_t* lens;
+  const uint64_t* tree;
 };
+constexpr int kXMaxWindow = 1 << 29;   // wider windows are the same: positions stay below 2^28
 // Bytes of the partial results where the keys (forward, dQ) or the query tokens
 // (dK, dV) are split over workgroups, and of the backward's row statistics.
 size_t xattn_fwd_workspace(const XArgs& a);
@@ -228,5 +237,26 @@ hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s);
 bool xattn_bwd_launchable(const XArgs& a);
 size_t xattn_bwd_workspace(const XArgs& a);
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s);
+
+// ---- Weights received by a cache's slots, and eviction (cache.hip) ----
+struct CacheWeights {
+  const float* in;          // [B, Hk, Nk], or null: zeros
+  float* out;
+  const uint64_t* tokens;   // [B] which of the Nq tokens count, a bit each, or null: all
+};
+// a: q, k, lse, a cache (lens).
+hipError_t launch_cache_weights(const XArgs& a, const CacheWeights& c, hipStream_t s);
+struct CacheEvict {
+  const void *k, *v;
+  void *k_out, *v_out;
+  const float* weights;
+  float* weights_out;
+  const int32_t* lens;
+  int32_t *len_out, *idx;
+  int B, cap, cap_out, Hk, D, keep, sinks, recent;
+  int64_t sk, sv, sko, svo;
+  bool zero_rest;
+};
+hipError_t launch_cache_evict(const CacheEvict& a, hipStream_t s);
 
 }  // namespace ut

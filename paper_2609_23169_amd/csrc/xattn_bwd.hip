@@ -48,7 +48,7 @@ constexpr int kDqWaves = 4;     // of 32 rows each
 // dQ
 // ---------------------------------------------------------------------------
 // part: fp32 [split][token][Hq][D], null with one split.
-template <int DP>
+template <int DP, bool WIN>
 __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const XArgs a, float* __restrict__ aux,
                                                                          const XOrder order, float* __restrict__ part) {
   constexpr int NW = kDqWaves, ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
@@ -134,16 +134,29 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};
 
-  TileSeq seq;
+  TileSeq<WIN> seq;
+  RowWindow see{};   // WIN: the lane's row
+  // WIN: whether rows of the wave differ in the keys of a tile that they see, and the
+  // keys k .. k + 31 that the lane's row of item `at` sees.
+  auto partial = [&](int at, int tile) __attribute__((always_inline)) {
+    const XArgs& x = *x_args_again();
+    return !see.whole(x, x_sample<WIN>(x, seq.item(at, order).b), tile);
+  };
+  auto row_bits = [&](int at, int k) __attribute__((always_inline)) {
+    const XArgs& x = *x_args_again();
+    return see.bits(x, x_sample<WIN>(x, seq.item(at, order).b), k);
+  };
 
   // A tile as two 32-key halves: S^T and dP^T, dS^T, its exchange to the
   // 16x16 operand layout, and the half's dQ product. With `swap` the next item's
   // rows take the place of this one's after the last score products. The next
   // tile's loads (load(u), u < 2 IPW) stand between the first products.
   using Load = TileLoad<DP, NW>;
-  auto step = [&](uint64_t bits, const char* kt_lds, const char* vt_lds, bool swap, Extra& ex, bool loads,
+  auto step = [&](uint64_t bits, int tile, const char* kt_lds, const char* vt_lds, bool swap, Extra& ex, bool loads,
                   auto load)
       __attribute__((always_inline)) {
+    bool part = false;
+    if constexpr (WIN) part = partial(seq.cur, tile);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       f32x16 s = f32x16{}, dp = f32x16{};
@@ -185,8 +198,10 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       __builtin_amdgcn_s_setprio(0);
       const float ls = l2, nd = ndl;
       if (kt == 1 && swap) load_rows(seq.item(seq.at, order), ex);   // uniform
-      if (bits != ~(uint64_t)0) {             // uniform
-        const unsigned mine = (unsigned)(bits >> (32 * kt)) >> (4 * g);
+      if (bits != ~(uint64_t)0 || part) {     // uniform
+        unsigned mine = (unsigned)(bits >> (32 * kt));
+        if constexpr (WIN) mine &= row_bits(seq.cur, kXKeys * tile + 32 * kt);
+        mine >>= 4 * g;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           s[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[e] : -INFINITY;
@@ -228,7 +243,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
   // delta of rows whose keys in use all lie in one tile, as rowsum(P o dP) in fp32: with
   // few keys dP - delta is a small difference, and the rounding of the O that is stored
   // would show in it (2 keys: dQ 0.0039 off in relative norm, 0.0024 with this).
-  auto tile_delta = [&](uint64_t bits, const char* kt_lds, const char* vt_lds) __attribute__((always_inline)) {
+  auto tile_delta = [&](uint64_t bits, int tile, const char* kt_lds, const char* vt_lds) __attribute__((always_inline)) {
     float sum = 0.f;
 #pragma unroll 1
     for (int kt = 0; kt < 2; ++kt) {
@@ -239,7 +254,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
         s = mfma32(*reinterpret_cast<const bf16x8*>(kt_lds + off), qop[ks], s);
         dp = mfma32(*reinterpret_cast<const bf16x8*>(vt_lds + off), doop[ks], dp);
       }
-      const unsigned mine = (unsigned)(bits >> (32 * kt)) >> (4 * g);
+      unsigned mine = (unsigned)(bits >> (32 * kt));
+      if constexpr (WIN) mine &= row_bits(seq.at, kXKeys * tile + 32 * kt);
+      mine >>= 4 * g;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float p = fast_exp2(__builtin_fmaf(s[e], c2, -lse2));
@@ -275,6 +292,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
     const uint64_t now = seq.bits;
+    const int tile = seq.tile;
     bool changed;
     const bool more = seq.next(order, 32 * NW, changed);
     if (!have && !more) return false;
@@ -296,7 +314,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
     // At 128 columns before the first tile too, beside its loads: what it leaves is not
     // used, and a branch around it would spill 29 registers.
     if (DP == 128 || have) {
-      step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, ex, all, load);
+      step(now, tile, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, ex, all, load);
     } else {
       if (all)
 #pragma unroll
@@ -318,8 +336,12 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
         const XTurn<DP> rows(x_lane_again());
         rows.turn(qop, lds0, lds1);
         rows.turn(doop, lds0, lds1);
+        if constexpr (WIN) {
+          const XArgs& x = *x_args_again();
+          see.open(x, x_sample<WIN>(x, at.b), at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
+        }
         const bool one = seq.one_tile(order);   // uniform
-        if (one) ndl = -tile_delta(seq.bits, kn, vn);
+        if (one) ndl = -tile_delta(seq.bits, seq.tile, kn, vn);
         put_stats(at, one ? seq.bits != 0 : at.part == 0);   // where delta is known
       }
 #pragma unroll
@@ -335,10 +357,20 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
 // ---------------------------------------------------------------------------
 // dK, dV
 // ---------------------------------------------------------------------------
+// Window attention: the first `tiles` key tiles hold sinks and take `splits` parts, the
+// others `others`. part: fp32 [dK, dV][splits][sample][key of those tiles][Hk][D],
+// null where nothing is split.
+struct SinkParts {
+  int64_t tiles, splits, others;
+  float* part;
+};
 // part: fp32 [dK, dV][split][token][Hk][D], null with one split.
-template <int DP>
+// WIN: the steps are those of the tokens that see a key of the workgroup, and
+// the keys' tiles that hold sinks, which most tokens see, have splits of their own.
+template <int DP, bool WIN>
 __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const float* __restrict__ aux,
-                                                            const XOrder order, float* __restrict__ part) {
+                                                            const XOrder order, float* __restrict__ part,
+                                                            const SinkParts sinks) {
   constexpr int NW = 4, ROWB = DP * 2, CPR = DP / 8, KS = DP / 16, DT = DP / 16;
   constexpr int TILEB = kRowTile * ROWB, RPI = 1024 / ROWB, IPW = TILEB / 1024 / NW, VIPW = kBwdKeys * ROWB / 1024 / NW;
   __shared__ __attribute__((aligned(1024))) char q_lds0[TILEB];
@@ -359,15 +391,28 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
   const XItems items = x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk);
   if (items.first >= items.end) return;
   const XItem at = x_item(items.first, (unsigned)a.B, order);
-  const unsigned kt = at.tile, sp = at.part;
+  unsigned kt = at.tile, sp = at.part, splits = order.splits;
+  if constexpr (WIN) {   // units of work: the parts of the tiles with sinks, then those of the others
+    const unsigned u = at.tile, m = sinks.tiles * sinks.splits;
+    splits = u < m ? sinks.splits : sinks.others;
+    kt = u < m ? u / splits : sinks.tiles + (u - m) / splits;
+    sp = u < m ? u % splits : (u - m) % splits;
+  }
   const int hk = at.hk;
   const XSample sm = x_sample(a, at.b);
   const int key0 = (int)kt * kBwdKeys;
   if (key0 >= sm.nk) return;   // uniform over the workgroup
 
   // Steps: the 32-token tiles of each head of the group; this split's share.
-  const int ttiles = (sm.nq + kRowTile - 1) / kRowTile, all = ttiles * a.G;
-  const int per = (all + (int)order.splits - 1) / (int)order.splits;
+  int t_first = 0, t_end = sm.nq;
+  if constexpr (WIN) {
+    const int off = sm.nk - sm.nq;
+    const bool sink = key0 < a.sinks;
+    t_first = sink && a.right > 0 ? 0 : min(max(key0 - a.right - off, 0), sm.nq);
+    t_end = sink ? sm.nq : max(min(min(key0 + kBwdKeys, sm.nk) + a.left - off, sm.nq), t_first);
+  }
+  const int ttiles = (t_end - t_first + kRowTile - 1) / kRowTile, all = ttiles * a.G;
+  const int per = (all + (int)splits - 1) / (int)splits;
   const int s_begin = min((int)sp * per, all), s_end = min(s_begin + per, all);
 
   f32x4 dk[DT][2], dv[DT][2];   // [dt][kg]: lane holds X^T[16 dt + 4 gq + (0..3)][key 32 w + 16 kg + c16]
@@ -410,7 +455,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
     const __bf16* const qb = static_cast<const __bf16*>(a.q) + sm.q0 * a.sq + hk * a.G * a.D;
     const __bf16* const ob = static_cast<const __bf16*>(a.dout) + sm.q0 * a.sdo + hk * a.G * a.D;
     auto load_step = [&](int head, int tt, char* qd, char* od, char* ad) __attribute__((always_inline)) {
-      const int t0 = tt * kRowTile, left = min(sm.nq - t0, kRowTile);
+      const int t0 = t_first + tt * kRowTile, left = min(sm.nq - t0, kRowTile);
       const __amdgpu_buffer_rsrc_t rq = buffer_rsrc(qb + (int64_t)t0 * a.sq + head * a.D, (left - 1) * a.sq * 2 + 2 * a.D);
       const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(ob + (int64_t)t0 * a.sdo + head * a.D, (left - 1) * a.sdo * 2 + 2 * a.D);
 #pragma unroll
@@ -425,7 +470,17 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
       }
     };
     const float c2 = a.scale * kLog2e;
-    auto step = [&](const char* qt_lds, const char* ot_lds, const char* at_lds) __attribute__((always_inline)) {
+    // WIN: the tokens that see the lane's key are from .. to - 1.
+    int from = 0, to = 0;
+    if constexpr (WIN) {
+      const int key = key0 + 32 * w + l32, off = sm.nk - sm.nq;
+      const bool sink = key < a.sinks;
+      from = sink && a.right > 0 ? 0 : key - a.right - off;
+      to = sink ? sm.nq : key + a.left - off + 1;
+    }
+    // rows: the tile's tokens that the lane's key is visible to, a bit each
+    auto step = [&](const char* qt_lds, const char* ot_lds, const char* at_lds,
+                    unsigned rows) __attribute__((always_inline)) {
       const float* const a_pl = reinterpret_cast<const float*>(at_lds) + 4 * g;
       f32x16 s = f32x16{}, dp;
 #pragma unroll
@@ -484,6 +539,16 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
       };
 #pragma unroll
       for (int dt = 0; dt < kPre; ++dt) read_tr(dt);
+      if constexpr (WIN)
+        if (__ballot(rows != ~0u) != 0) {   // uniform
+          const unsigned mine = rows >> (4 * g);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {   // dP too: a key that no token sees may hold anything
+            const bool in = mine >> (8 * (e >> 2) + (e & 3)) & 1;
+            s[e] = in ? s[e] : -INFINITY;
+            dp[e] = in ? dp[e] : 0.f;
+          }
+        }
       u32x4 pp[2], pd[2];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -528,9 +593,13 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
     };
     auto iter = [&](int i, auto par, auto used) __attribute__((always_inline)) {
       constexpr int P = decltype(par)::value;
+      unsigned rows = ~0u;
+      if constexpr (WIN) rows = bits32_from_to(from - t_first - tt * kRowTile, to - t_first - tt * kRowTile);
       advance();
       if (i + 1 < s_end) load_step(head, tt, P ? q_lds0 : q_lds1, P ? o_lds0 : o_lds1, P ? a_lds0 : a_lds1);
-      if constexpr (decltype(used)::value) step(P ? q_lds1 : q_lds0, P ? o_lds1 : o_lds0, P ? a_lds1 : a_lds0);
+      if constexpr (decltype(used)::value)
+        if (!WIN || __ballot(rows != 0) != 0)   // uniform
+          step(P ? q_lds1 : q_lds0, P ? o_lds1 : o_lds0, P ? a_lds1 : a_lds0, rows);
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
     };
@@ -558,15 +627,23 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
     if (key >= sm.nk) continue;
     const bool used = !a.mask || a.mask[sm.k0 + key];
     const int64_t tok = sm.k0 + key;
-    float* const pk = part + ((sp * a.Tk + tok) * a.Hk + hk) * a.D + 4 * gq;
-    float* const pv = pk + order.splits * a.Tk * a.Hk * a.D;
+    float* pk = part + ((sp * a.Tk + tok) * a.Hk + hk) * a.D + 4 * gq;
+    float* pv = pk + splits * a.Tk * a.Hk * a.D;
+    bool parts = part;
+    if constexpr (WIN)
+      if (kt < sinks.tiles && sinks.part) {   // uniform
+        const int64_t rows = (int64_t)sinks.tiles * kBwdKeys;
+        pk = sinks.part + ((sp * a.B + at.b) * rows + key) * a.Hk * a.D + hk * a.D + 4 * gq;
+        pv = pk + splits * a.B * rows * a.Hk * a.D;
+        parts = true;
+      }
     __bf16* const ok = static_cast<__bf16*>(a.dk) + tok * a.sdk + hk * a.D + 4 * gq;
     __bf16* const ov = static_cast<__bf16*>(a.dv) + tok * a.sdv + hk * a.D + 4 * gq;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       if (16 * dt + 4 * gq >= a.D) continue;
       const f32x4 x = used ? dk[dt][kg] * a.scale : f32x4{}, y = used ? dv[dt][kg] : f32x4{};
-      if (part) {
+      if (parts) {
         *reinterpret_cast<f32x4*>(pk + 16 * dt) = x;
         *reinterpret_cast<f32x4*>(pv + 16 * dt) = y;
       } else {
@@ -592,17 +669,62 @@ struct Join {
   const int32_t* cu;   // [B + 1], or null
   int N;               // most tokens of a sample
 };
-__global__ __launch_bounds__(256) void xattn_sum_kernel(const Join j0, const Join j1, const Join j2, int B) {
-  const Join j = blockIdx.y == 0 ? j0 : blockIdx.y == 1 ? j1 : j2;
-  const int64_t total = j.T * j.width, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+__device__ inline void sum_parts(const float* from, int parts, int64_t step, void* to) {
+  f32x4 x = f32x4{};
+#pragma unroll 4
+  for (int s = 0; s < parts; ++s) x += *reinterpret_cast<const f32x4*>(from + s * step);
+  *reinterpret_cast<bf16x4*>(to) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+}
+__device__ inline void sum_join(const Join& j, int B, int64_t i) {
+  const int64_t total = j.T * j.width;
   if (i >= total) return;
   const int64_t tok = i / j.width;
   if (j.cu && !in_sample(j.cu, j.T, B, j.N, tok)) return;
-  f32x4 x = f32x4{};
-#pragma unroll 4
-  for (int s = 0; s < j.parts; ++s) x += *reinterpret_cast<const f32x4*>(j.part + s * total + i);
-  *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(j.out) + tok * j.stride + (i - tok * j.width)) =
-      bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+  sum_parts(j.part + i, j.parts, total, static_cast<__bf16*>(j.out) + tok * j.stride + (i - tok * j.width));
+}
+__global__ __launch_bounds__(256) void xattn_sum_kernel(const Join j0, const Join j1, const Join j2, int B) {
+  const Join j = blockIdx.y == 0 ? j0 : blockIdx.y == 1 ? j1 : j2;
+  sum_join(j, B, ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4);
+}
+// The same for window attention: dK and dV (blockIdx.y 0 and 1), whose keys in the
+// tiles with sinks have parts of their own, and dQ (2). part null: of dK and dV only
+// those keys are joined.
+__global__ __launch_bounds__(256) void swattn_sum_kernel(const XArgs a, const SinkParts sinks, const float* part,
+                                                         const Join dq) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (blockIdx.y == 2) return sum_join(dq, a.B, i);
+  const int64_t width = (int64_t)a.Hk * a.D, rows = sinks.tiles * kBwdKeys, r = i / width;
+  if (r >= (part ? a.Tk : a.B * rows)) return;
+  int b = 0;
+  int64_t key;
+  if (!part) {
+    b = (int)(r / rows);
+    key = r - b * rows;
+  } else if (!a.cuk) {
+    b = (int)(r / a.Nk);
+    key = r - (int64_t)b * a.Nk;
+  } else {
+    key = -1;
+    for (; b < a.B; ++b) {
+      const XSample sm = x_sample(a, b);
+      if (r >= sm.k0 && r < sm.k0 + sm.nk) {
+        key = r - sm.k0;
+        break;
+      }
+    }
+    if (key < 0) return;   // of no sample
+  }
+  const XSample sm = x_sample(a, b);
+  if (key >= sm.nk) return;
+  const int64_t col = i - r * width, tok = sm.k0 + key, y = blockIdx.y;
+  void* const to = static_cast<__bf16*>(y ? a.dv : a.dk) + tok * (y ? a.sdv : a.sdk) + col;
+  if (key < rows) {
+    const int64_t step = a.B * rows * width;
+    sum_parts(sinks.part + y * sinks.splits * step + (b * rows + key) * width + col, (int)sinks.splits, step, to);
+  } else {
+    const int64_t step = a.Tk * width;
+    sum_parts(part + y * sinks.others * step + tok * width + col, (int)sinks.others, step, to);
+  }
 }
 
 int64_t dq_tiles(const XArgs& a) { return ((int64_t)a.Nq * a.G + 32 * kDqWaves - 1) / (32 * kDqWaves); }
@@ -614,12 +736,35 @@ int64_t dkdv_groups(const XArgs& a) {
 // queries and keys, 8 heads of 64, half of that takes dQ from 14.9 to 13.0 us and dK/dV
 // from 14.5 to 11.7, and their join adds 7.
 int dq_splits(const XArgs& a) {
-  const int64_t groups = dq_groups(a), tiles = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
+  const int64_t groups = dq_groups(a), tiles = x_item_tiles(a, 32 * kDqWaves);
   return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), kDqWaves) / groups, tiles / 4));
 }
+// Steps of a dK/dV workgroup that is not split and whose keys are seen by `tokens`.
+int64_t dkdv_steps(const XArgs& a, int64_t tokens) {
+  return (int64_t)a.G * ((std::min<int64_t>(a.Nq, tokens) + kRowTile - 1) / kRowTile);
+}
+// Tokens that see a key which is no sink: those in reach of a tile of keys.
+int64_t dkdv_reach(const XArgs& a) { return a.window ? (int64_t)a.left + a.right + kBwdKeys : a.Nq; }
 int dkdv_splits(const XArgs& a) {
-  const int64_t groups = dkdv_groups(a), steps = (int64_t)a.G * (((int64_t)a.Nq + kRowTile - 1) / kRowTile);
+  const int64_t groups = dkdv_groups(a), steps = dkdv_steps(a, dkdv_reach(a));
   return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), 4) / groups, steps / 8));
+}
+// Sinks are seen by nearly all tokens: parts of about as many steps as the other
+// workgroups', 32 at least, so that no workgroup is left with the whole sequence.
+SinkParts sink_parts(const XArgs& a) {
+  SinkParts p{};
+  p.others = dkdv_splits(a);
+  p.splits = 1;
+  if (!a.window) return p;
+  p.tiles = (std::min(a.sinks, a.Nk) + kBwdKeys - 1) / kBwdKeys;
+  const int64_t per = std::max<int64_t>(dkdv_steps(a, dkdv_reach(a)) / p.others, 32), all = dkdv_steps(a, a.Nq);
+  p.splits = std::max<int64_t>(p.others, std::min<int64_t>((all + per - 1) / per, 64));
+  return p;
+}
+int64_t dkdv_units(const XArgs& a) {   // workgroups of a key head of a sample
+  const SinkParts p = sink_parts(a);
+  const int64_t tiles = ((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys;
+  return p.tiles * p.splits + (tiles - p.tiles) * p.others;
 }
 size_t aux_bytes(const XArgs& a) { return ((size_t)a.Tq * a.Hq * 2 * sizeof(float) + 255) / 256 * 256; }
 size_t dq_part(const XArgs& a) {
@@ -631,20 +776,28 @@ size_t dkdv_part(const XArgs& a) {
   return n > 1 ? (size_t)n * a.Tk * a.Hk * a.D * 2 * sizeof(float) : 0;
 }
 
-template <int DP>
+size_t sink_part(const XArgs& a) {
+  const SinkParts p = sink_parts(a);
+  return p.tiles > 0 && (p.splits > 1 || p.others > 1)
+             ? (size_t)p.splits * a.B * p.tiles * kBwdKeys * a.Hk * a.D * 2 * sizeof(float)
+             : 0;
+}
+
+template <int DP, bool WIN>
 void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)dq_tiles(a), (unsigned)splits};
   const int64_t items = dq_groups(a) * splits;
   const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, kDqWaves)) + 7) / 8 * 8);
-  TraceScope ts_(s, "xattn_dq", DP);
-  hipLaunchKernelGGL((xattn_dq_kernel<DP>), grid, dim3(64 * kDqWaves), 0, s, a, aux, order, part);
+  TraceScope ts_(s, WIN ? "swattn_dq" : "xattn_dq", DP);
+  hipLaunchKernelGGL((xattn_dq_kernel<DP, WIN>), grid, dim3(64 * kDqWaves), 0, s, a, aux, order, part);
 }
-template <int DP>
-void launch_dkdv(const XArgs& a, const float* aux, int splits, float* part, hipStream_t s) {
-  const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys), (unsigned)splits};
-  TraceScope ts_(s, "xattn_dkdv", DP);
-  const dim3 grid((unsigned)(std::max<int64_t>(dkdv_groups(a) * splits, 1) + 7) / 8 * 8);
-  hipLaunchKernelGGL((xattn_dkdv_kernel<DP>), grid, dim3(256), 0, s, a, aux, order, part);
+template <int DP, bool WIN>
+void launch_dkdv(const XArgs& a, const float* aux, float* part, const SinkParts& sinks, hipStream_t s) {
+  const int64_t tiles = ((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys;
+  const XOrder order{head_group(a), (unsigned)(WIN ? dkdv_units(a) : tiles), WIN ? 1 : (unsigned)sinks.others};
+  TraceScope ts_(s, WIN ? "swattn_dkdv" : "xattn_dkdv", DP);
+  const dim3 grid((unsigned)(std::max<int64_t>((int64_t)a.B * a.Hk * order.tiles * order.splits, 1) + 7) / 8 * 8);
+  hipLaunchKernelGGL((xattn_dkdv_kernel<DP, WIN>), grid, dim3(256), 0, s, a, aux, order, part, sinks);
 }
 void launch_sums(const Join* j, int n, int B, hipStream_t s) {
   int64_t most = 0;
@@ -655,15 +808,26 @@ void launch_sums(const Join* j, int n, int B, hipStream_t s) {
                      j[n > 1 ? 1 : 0], j[n > 2 ? 2 : 0], B);
 }
 
+void launch_window_sums(const XArgs& a, const SinkParts& sinks, const float* part, const Join& dq, hipStream_t s) {
+  const int64_t rows = part ? a.Tk : (int64_t)a.B * sinks.tiles * kBwdKeys;
+  const int64_t most = std::max(rows * a.Hk * a.D, dq.T * dq.width);
+  if (most == 0) return;
+  TraceScope ts_(s, "swattn_sum");
+  hipLaunchKernelGGL(swattn_sum_kernel, dim3((unsigned)((most / 4 + 255) / 256), dq.part ? 3 : 2), dim3(256), 0, s, a,
+                     sinks, part, dq);
+}
+
 }  // namespace
 
 bool xattn_bwd_launchable(const XArgs& a) {
   constexpr int64_t kMost = (int64_t)1 << 24;   // workgroups of 256 threads
-  const int64_t sums = std::max(dq_part(a) > 0 ? a.Tq * a.Hq : 0, dkdv_part(a) > 0 ? a.Tk * a.Hk : 0) * a.D;
-  return (dkdv_groups(a) + 7) / 8 * 8 < kMost && (sums / 4 + 255) / 256 < kMost;
+  int64_t sums = std::max(dq_part(a) > 0 ? a.Tq * a.Hq : 0, dkdv_part(a) > 0 ? a.Tk * a.Hk : 0) * a.D;
+  if (sink_part(a) > 0) sums = std::max(sums, (int64_t)a.B * sink_parts(a).tiles * kBwdKeys * a.Hk * a.D);
+  return ((a.window ? (int64_t)a.B * a.Hk * dkdv_units(a) : dkdv_groups(a)) + 7) / 8 * 8 < kMost &&
+         (sums / 4 + 255) / 256 < kMost;
 }
 
-size_t xattn_bwd_workspace(const XArgs& a) { return aux_bytes(a) + dq_part(a) + dkdv_part(a); }
+size_t xattn_bwd_workspace(const XArgs& a) { return aux_bytes(a) + dq_part(a) + dkdv_part(a) + sink_part(a); }
 
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
   float* const aux = static_cast<float*>(workspace);
@@ -674,18 +838,30 @@ hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
   if (dq_groups(a) > 0 || (a.zero_rest && a.Tq > 0)) {
     const int splits = dq_splits(a);
     float* const p = splits > 1 ? qpart : nullptr;
-    a.D <= 64 ? launch_dq<64>(a, aux, splits, p, s) : launch_dq<128>(a, aux, splits, p, s);
+    if (a.window) a.D <= 64 ? launch_dq<64, true>(a, aux, splits, p, s) : launch_dq<128, true>(a, aux, splits, p, s);
+    else a.D <= 64 ? launch_dq<64, false>(a, aux, splits, p, s) : launch_dq<128, false>(a, aux, splits, p, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p) joins[n++] = Join{p, splits, a.Tq, a.Hq * a.D, a.dq, a.sdq, a.cuq, a.Nq};
   }
   if (dkdv_groups(a) > 0 || (a.zero_rest && a.Tk > 0)) {
     const int splits = dkdv_splits(a);
     float* const p = splits > 1 ? kpart : nullptr;
-    a.D <= 64 ? launch_dkdv<64>(a, aux, splits, p, s) : launch_dkdv<128>(a, aux, splits, p, s);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (p) {
-      joins[n++] = Join{p, splits, a.Tk, a.Hk * a.D, a.dk, a.sdk, a.cuk, a.Nk};
-      joins[n++] = Join{p + (size_t)splits * a.Tk * a.Hk * a.D, splits, a.Tk, a.Hk * a.D, a.dv, a.sdv, a.cuk, a.Nk};
+    SinkParts sinks = sink_parts(a);
+    sinks.part = sink_part(a) > 0 ? kpart + dkdv_part(a) / sizeof(float) : nullptr;
+    if (a.window) {
+      a.D <= 64 ? launch_dkdv<64, true>(a, aux, p, sinks, s) : launch_dkdv<128, true>(a, aux, p, sinks, s);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      if (p || sinks.part) {
+        launch_window_sums(a, sinks, p, n > 0 ? joins[0] : Join{}, s);
+        n = 0;
+      }
+    } else {
+      a.D <= 64 ? launch_dkdv<64, false>(a, aux, p, sinks, s) : launch_dkdv<128, false>(a, aux, p, sinks, s);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      if (p) {
+        joins[n++] = Join{p, splits, a.Tk, a.Hk * a.D, a.dk, a.sdk, a.cuk, a.Nk};
+        joins[n++] = Join{p + (size_t)splits * a.Tk * a.Hk * a.D, splits, a.Tk, a.Hk * a.D, a.dv, a.sdv, a.cuk, a.Nk};
+      }
     }
   }
   if (n > 0) launch_sums(joins, n, a.B, s);

@@ -51,7 +51,7 @@ struct Parts {
   int64_t stats;
 };
 
-template <int DP, int NW, bool SPLIT>
+template <int DP, int NW, bool SPLIT, bool WIN>
 __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_fwd_kernel(const XArgs a, const XOrder order,
                                                                                            const Parts parts) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   bf16x8 qop[KS];
   auto load_rows = [&](const XItem& at) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
-    const XSample sm = x_sample(x, at.b);
+    const XSample sm = x_sample<WIN>(x, at.b);
     x_load_rows<DP>(qop, x.q, sm.q0, x.sq, (int64_t)at.hk * x.G * x.D, at.tile * 32 * NW + 32 * w, sm.nq, x.G, x.D);
   };
   const TileLoad<DP, NW> load_k(lane, a.sk), load_v(lane, a.sv);
@@ -97,7 +97,8 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   float m_run = 0.f, l_run = 0.f;
   bool fresh = true;                   // no key of the item seen yet: no reference (uniform)
 
-  TileSeq seq;
+  TileSeq<WIN> seq;
+  RowWindow see{};                     // WIN: the lane's row
 
   // One tile in two 32-key halves, so that a wave's vector work has matrix work of
   // its own beside it: S of half 1 runs beside the exponentials of half 0, and the
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   // rows of the next item take the place of this one's once the scores are formed.
   // The next tile's loads (load(u), u < 2 IPW) stand between the first products.
   using Load = TileLoad<DP, NW>;
-  auto step = [&](uint64_t bits, const char* kt_lds, const char* vt_lds, bool swap, bool loads,
+  auto step = [&](uint64_t bits, int tile, const char* kt_lds, const char* vt_lds, bool swap, bool loads,
                   auto load) __attribute__((always_inline)) {
     constexpr int kAhead = 4, kPre = 4;
     bf16x8 kop[kAhead], vop[kPre];
@@ -143,11 +144,21 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[h][e]);
       return fmaxf(mx * c2, -3.0e38f);
     };
+    bool part = false;   // WIN: rows of the wave differ in the keys that they see
+    if constexpr (WIN) {
+      const XArgs& x = *x_args_again();
+      part = !see.whole(x, x_sample<WIN>(x, seq.item(seq.cur, order).b), tile);
+    }
     // Before half h's exponentials: unused keys, and the item's reference.
     auto prepare = [&](int h) __attribute__((always_inline)) {
       const unsigned half = (unsigned)(bits >> (32 * h));
-      if (half != ~0u) {   // uniform
-        const unsigned mine = half >> (4 * g);
+      if (half != ~0u || part) {   // uniform
+        unsigned mine = half;
+        if constexpr (WIN) {
+          const XArgs& x = *x_args_again();
+          mine &= see.bits(x, x_sample<WIN>(x, seq.item(seq.cur, order).b), kXKeys * tile + 32 * h);
+        }
+        mine >>= 4 * g;
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[h][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[h][e] : -INFINITY;
       }
@@ -272,7 +283,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   // O = O^T / l, LSE = (m + log2 l) ln 2; a row without keys: 0 and -inf.
   auto finish = [&](const XItem& at, char* lds0, char* lds1) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
-    const XSample sm = x_sample(x, at.b);
+    const XSample sm = x_sample<WIN>(x, at.b);
     const int rows = sm.nq * x.G, r0 = at.tile * 32 * NW + 32 * w;
     const float l_tot = pair_sum(l_run);
     const bool none = l_tot == 0.f;
@@ -308,6 +319,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
     const uint64_t now = seq.bits;
+    const int tile = seq.tile;
     bool changed;
     const bool more = seq.next(order, 32 * NW, changed);
     if (!have && !more) return false;
@@ -329,7 +341,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     // used, and a branch around it costs the loop more (packed case 259 -> 275 us). At
     // 64 the branch takes 1 us off a call's 10.
     if (DP == 128 || have) {
-      step(now, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, all, load);
+      step(now, tile, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, all, load);
     } else {
       if (all)
 #pragma unroll
@@ -344,7 +356,14 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       char* const lds0 = (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
       char* const lds1 = (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
       if (have) finish(seq.item(seq.cur, order), lds0, lds1);
-      if (more) XTurn<DP>(x_lane_again()).turn(qop, lds0, lds1);
+      if (more) {
+        XTurn<DP>(x_lane_again()).turn(qop, lds0, lds1);
+        if constexpr (WIN) {
+          const XArgs& x = *x_args_again();
+          const XItem at = seq.item(seq.at, order);
+          see.open(x, x_sample<WIN>(x, at.b), at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
+        }
+      }
       seq.cur = seq.at;
       m_run = l_run = 0.f;
       fresh = true;
@@ -437,9 +456,9 @@ struct Shape {
   int splits, waves;
 };
 Shape fwd_shape(const XArgs& a) {
-  const int64_t rows = (int64_t)a.Nq * a.G, heads = (int64_t)a.B * a.Hk, tiles = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
+  const int64_t rows = (int64_t)a.Nq * a.G, heads = (int64_t)a.B * a.Hk;
   auto splits = [&](int nw) {
-    const int64_t groups = heads * ((rows + 32 * nw - 1) / (32 * nw));
+    const int64_t groups = heads * ((rows + 32 * nw - 1) / (32 * nw)), tiles = x_item_tiles(a, 32 * nw);
     return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), nw) / groups, tiles / 4));
   };
   if (rows <= 32 && splits(1) > 1) return Shape{splits(1), 1};
@@ -447,18 +466,26 @@ Shape fwd_shape(const XArgs& a) {
 }
 int64_t stats_of(const XArgs& a) { return a.Tq * a.Hq; }
 
-template <int DP, int NW>
+template <int DP, int NW, bool WIN>
 void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
   const int64_t items = (int64_t)a.B * a.Hk * order.tiles * splits;
   const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, NW)) + 7) / 8 * 8);
-  TraceScope ts_(s, splits > 1 ? "xattn_fwd_split" : "xattn_fwd", DP, NW);
+  TraceScope ts_(s, WIN ? splits > 1 ? "swattn_fwd_split" : "swattn_fwd" : splits > 1 ? "xattn_fwd_split" : "xattn_fwd",
+                 DP, NW);
   if (splits > 1) {
-    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, true>), grid, dim3(64 * NW), 0, s, a, order, parts);
+    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, true, WIN>), grid, dim3(64 * NW), 0, s, a, order, parts);
   } else {
     if constexpr (NW == 4)
-      hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, false>), grid, dim3(64 * NW), 0, s, a, order, parts);
+      hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, false, WIN>), grid, dim3(64 * NW), 0, s, a, order, parts);
   }
+}
+template <bool WIN>
+void launch_fwd(const XArgs& a, int splits, int waves, const Parts& parts, hipStream_t s) {
+  if (a.D <= 64)
+    waves == 1 ? launch_fwd<64, 1, WIN>(a, splits, parts, s) : launch_fwd<64, 4, WIN>(a, splits, parts, s);
+  else
+    waves == 1 ? launch_fwd<128, 1, WIN>(a, splits, parts, s) : launch_fwd<128, 4, WIN>(a, splits, parts, s);
 }
 template <int GPR>
 void launch_join(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
@@ -483,10 +510,7 @@ hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s) {
     parts.o = static_cast<float*>(workspace);
     parts.sums = reinterpret_cast<float2*>(parts.o + (size_t)splits * parts.stats * a.D);
   }
-  if (a.D <= 64)
-    waves == 1 ? launch_fwd<64, 1>(a, splits, parts, s) : launch_fwd<64, 4>(a, splits, parts, s);
-  else
-    waves == 1 ? launch_fwd<128, 1>(a, splits, parts, s) : launch_fwd<128, 4>(a, splits, parts, s);
+  a.window ? launch_fwd<true>(a, splits, waves, parts, s) : launch_fwd<false>(a, splits, waves, parts, s);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   // Eight groups of lanes a row where many parts are to be read for few rows: 320 rows
   // of 11 parts 6.9 us against 11.3 with one, 1,024 of 8 7.0 against 9.0; but 8,000 of

@@ -4,6 +4,8 @@
 // and all of them read the key head's tiles once.
 #pragma once
 
+#include <algorithm>
+
 #include "attn_util.h"
 
 namespace ut {
@@ -66,6 +68,13 @@ inline unsigned head_group(const XArgs& a) { return a.Hk % 8 == 0 ? (unsigned)a.
 // to 36 at 64) and by registers (two waves a SIMD at 128 columns, three at 64): what
 // a grid needs to fill the chip.
 constexpr int64_t x_resident(int DP, int nw) { return 256 * (DP == 128 ? 2 : nw == 4 ? 3 : 4); }
+// Most key tiles of an item of `rows` rows.
+inline int64_t x_item_tiles(const XArgs& a, int rows) {
+  const int64_t all = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
+  if (!a.window) return all;
+  const int64_t first = (a.sinks + kXKeys - 1) / kXKeys, keys = (int64_t)a.left + a.right + 1 + (rows - 1) / a.G;
+  return std::min(all, first + keys / kXKeys + 2);
+}
 inline int x_padded(const XArgs& a) { return a.D <= 64 ? 64 : 128; }
 struct XItem {
   int b, tile, part, hk;
@@ -75,15 +84,36 @@ __device__ inline XItem x_item(unsigned it, unsigned B, const XOrder& o) {
   return XItem{(int)(r - s * B), (int)(s - t * o.tiles), (int)(t - u * o.splits), (int)(u * o.heads + it - r * o.heads)};
 }
 
+// Window attention: the keys that some row of an item sees, [0, send) and [lo, hi).
+// Their tiles as one list: the first `first`, then those from first + skip on, `count`
+// in all.
+struct XSpan {
+  int send, lo, hi;
+  int first, skip, count;
+};
+// Bits 0 .. n - 1, and bits lo .. hi - 1.
+__device__ inline uint64_t bits_below(int n) { return n >= 64 ? ~(uint64_t)0 : n <= 0 ? 0 : ((uint64_t)1 << n) - 1; }
+__device__ inline unsigned bits32_from_to(int lo, int hi) {
+  const unsigned below = hi >= 32 ? ~0u : (1u << max(hi, 0)) - 1;
+  return lo >= 32 ? 0u : below & (~0u << max(lo, 0));
+}
+
 // The key tiles of one sample that hold a key in use, and which keys of each:
 // 64 tiles at a time, one a lane, as 64-bit masks, so that a step to the next
 // tile costs a few scalar instructions and unused tiles none. Tiles
-// [begin, end); n keys; mask: a byte a key, or null.
+// [begin, end) (WIN: of the span's list); n keys; mask: a byte a key, or null.
+template <bool WIN>
 struct KeyTiles {
   const uint8_t* mask;
   int n, end, base;
   uint64_t mine, left;   // this lane's tile; the group's tiles not yet visited
+  XSpan span;            // WIN only
 
+  // Tile number i of the list.
+  __device__ inline int number(int i) const {
+    if constexpr (WIN) return i + (i >= span.first ? span.skip : 0);
+    return i;
+  }
   __device__ inline void open(const uint8_t* m, int keys, int begin, int stop) {
     mask = m;
     n = keys;
@@ -93,10 +123,10 @@ struct KeyTiles {
   }
 
   __device__ inline void group() {
-    const int lane = threadIdx.x & 63, t = base + lane;
+    const int lane = threadIdx.x & 63, i = base + lane, t = number(i);
     mine = 0;
     if (mask) {
-      if (t < end && kXKeys * (t + 1) <= n) {
+      if (i < end && kXKeys * (t + 1) <= n) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           u32x4 v;
@@ -112,14 +142,20 @@ struct KeyTiles {
           }
         }
       }
-    } else if (t < end) {
+    } else if (i < end) {
       mine = kXKeys * (t + 1) <= n ? ~(uint64_t)0 : 0;
     }
     const int last = n / kXKeys, rest = n % kXKeys;   // the short last tile
-    if (rest && last < end && last >= base && last < base + 64) {
+    if (WIN ? rest && __ballot(i < end && t == last) != 0
+            : rest && last < end && last >= base && last < base + 64) {
       const bool in = lane < rest && (!mask || mask[(int64_t)kXKeys * last + lane]);
       const uint64_t bits = __ballot(in);
       if (t == last) mine = bits;
+    }
+    if constexpr (WIN) {
+      const int k = kXKeys * t;
+      mine &= (bits_below(span.hi - k) & ~bits_below(span.lo - k)) | bits_below(span.send - k);
+      if (i >= end) mine = 0;
     }
     left = __ballot(mine != 0);
   }
@@ -132,7 +168,7 @@ struct KeyTiles {
     }
     const int i = __builtin_ctzll(left);
     left &= left - 1;
-    tile = base + i;
+    tile = number(base + i);
     const unsigned lo = __builtin_amdgcn_readlane((unsigned)mine, i);
     const unsigned hi = __builtin_amdgcn_readlane((unsigned)(mine >> 32), i);
     bits = (uint64_t)hi << 32 | lo;
@@ -156,7 +192,13 @@ __device__ inline int x_cu(const int32_t* cu, int i) {
   return cu[i];
 #endif
 }
+template <bool WIN = false>
 __device__ inline XSample x_sample(const XArgs& a, int b) {
+  if constexpr (WIN)
+    if (a.lens) {   // clamped, so that no length can send an access outside the cache
+      const int used = min(max(x_cu(a.lens, b), 0), a.Nk - a.Nq) + a.Nq;
+      return XSample{(int64_t)b * a.Nq, (int64_t)b * a.Nk, a.Nq, used, (int64_t)b * a.Hq * a.Nq, (int64_t)a.Nq};
+    }
   if (!a.cuq)
     return XSample{(int64_t)b * a.Nq, (int64_t)b * a.Nk, a.Nq, a.Nk, (int64_t)b * a.Hq * a.Nq, (int64_t)a.Nq};
   // clamped as in sample_rows: no offsets can send an access outside the tensors
@@ -171,6 +213,58 @@ __device__ inline int row_token(int row, int G) {
   if (G == 1) return row;
   return (int)((unsigned)row / (unsigned)G);
 }
+
+// What the rows r0 .. r0 + n - 1 of a sample see, as a span.
+__device__ inline XSpan x_span(const XArgs& a, const XSample& sm, int r0, int n) {
+  const int off = sm.nk - sm.nq;
+  const int p0 = off + row_token(r0, a.G), p1 = off + row_token(min(r0 + n, sm.nq * a.G) - 1, a.G);
+  XSpan s;
+  s.lo = max(0, (a.tree ? off : p0) - a.left);
+  s.hi = a.tree ? sm.nk : max(0, min(sm.nk, p1 + a.right + 1));
+  s.send = max(0, min(min(a.sinks, sm.nk), a.tree ? off : a.right > 0 ? sm.nk : p1 + 1));
+  s.first = (s.send + kXKeys - 1) / kXKeys;
+  const int w0 = max(s.first, s.lo / kXKeys), w1 = s.lo < s.hi ? (s.hi + kXKeys - 1) / kXKeys : 0;
+  s.skip = w0 - s.first;
+  s.count = s.first + max(0, w1 - w0);
+  return s;
+}
+
+// What a lane's row sees, for the items' tiles that its wave does not see whole.
+struct RowWindow {
+  int p;          // the row's position
+  uint64_t tree;  // the last nq keys that it sees, a bit each (a tree only)
+
+  __device__ inline void open(const XArgs& a, const XSample& sm, int b, int row) {
+    const int tok = row_token(min(row, sm.nq * a.G - 1), a.G);
+    p = sm.nk - sm.nq + tok;
+    tree = 0;
+    if (a.tree) {   // its position is behind the keys of the tree that it sees, less itself
+      tree = a.tree[(int64_t)b * a.Nq + tok] & bits_below(a.Nq);
+      p += __builtin_popcountll(tree & ~((uint64_t)1 << tok)) - tok;
+    }
+  }
+  // Whether every row of the wave sees all keys of a tile (uniform; the rows'
+  // positions ascend from lane 0 to lane 31, in a tree by any order within nq).
+  __device__ inline bool whole(const XArgs& a, const XSample& sm, int tile) const {
+    const int k = kXKeys * tile, off = sm.nk - sm.nq;
+    const int p0 = __builtin_amdgcn_readfirstlane(p), p1 = a.tree ? off + sm.nq : __builtin_amdgcn_readlane(p, 31);
+    const int end = a.tree ? off : p0 + a.right + 1;
+    if (k >= p1 - a.left && k + kXKeys <= end) return true;
+    return k + kXKeys <= min(a.sinks, a.right > 0 ? sm.nk : end);
+  }
+  // Keys k .. k + 31 that the row sees, a bit each.
+  __device__ inline unsigned bits(const XArgs& a, const XSample& sm, int k) const {
+    const int off = sm.nk - sm.nq, end = a.tree ? off : p + a.right + 1;
+    unsigned m = bits32_from_to(p - a.left - k, end - k) |
+                 bits32_from_to(0, min(a.sinks, a.right > 0 ? sm.nk : end) - k);
+    if (a.tree) {
+      const int at = off - k;   // bit 0 of the tree
+      if (at >= 0) m |= at < 32 ? (unsigned)(tree << at) : 0u;
+      else m |= at > -64 ? (unsigned)(tree >> -at) : 0u;
+    }
+    return m;
+  }
+};
 
 // Whether packed token `tok` belongs to one of the B samples (lengths up to N).
 __device__ inline bool in_sample(const int32_t* __restrict__ cu, int64_t T, int B, int N, int64_t tok) {
@@ -197,10 +291,11 @@ __device__ inline void x_clear_rest(const int32_t* cu, int B, int64_t T, int wid
 // place of three divisions, and the scalar registers are left to the loop over the
 // tiles. The code of a change stands once in the loop: an item whose keys are not in
 // use yields one tile without keys (bits 0), so that it is finished like the others.
+template <bool WIN>
 struct TileSeq {
   static constexpr int kTurns = 62;             // even: every group begins with a forward turn
   static constexpr int kKept = 63;              // the lane that keeps an item over the groups
-  KeyTiles tiles;
+  KeyTiles<WIN> tiles;
   int b, rtile, hkpart;                         // a lane's item: sample, tile of rows, key head and part
   unsigned first, step, turn, end;              // the next group's items (XItems)
   uint64_t todo;                                // items of the group not begun
@@ -267,8 +362,12 @@ struct TileSeq {
       todo &= todo - 1;
       const XItem m = item(at, order);
       const XArgs& x = *x_args_again();
-      const XSample sm = x_sample(x, m.b);
-      const int n = (sm.nk + kXKeys - 1) / kXKeys;
+      const XSample sm = x_sample<WIN>(x, m.b);
+      int n = (sm.nk + kXKeys - 1) / kXKeys;
+      if constexpr (WIN) {
+        tiles.span = x_span(x, sm, m.tile * rows_per_item, rows_per_item);
+        n = tiles.span.count;
+      }
       int t0 = 0, t1 = n;
       if (order.splits > 1) {
         const int per = (n + (int)order.splits - 1) / (int)order.splits;
@@ -290,10 +389,11 @@ struct TileSeq {
   // first 4,096 keys (dQ of 40 rows on 700 keys 16.8 -> 17.9 us), 8 us at 20 keys of
   // 16,391; unsplit ones have it from the walk.
   __device__ inline bool one_tile(const XOrder& order) const {
-    const int n = (keys + kXKeys - 1) / kXKeys;
+    const int n = WIN ? tiles.span.count : (keys + kXKeys - 1) / kXKeys;
     if (n <= 1) return bits != 0;
     if (!tiles.mask) return false;
-    KeyTiles t;   // the tiles not yet looked at; of a split item, all of the sample's
+    KeyTiles<WIN> t;   // the tiles not yet looked at; of a split item, all of the sample's
+    if constexpr (WIN) t.span = tiles.span;
     int count = 0, from = 0;
     if (order.splits == 1) {
       if (tiles.left != 0) return false;
