@@ -39,12 +39,12 @@ __global__ __launch_bounds__(256) void cache_weights_kernel(const XArgs a, const
   const unsigned hk = blockIdx.x % (unsigned)a.Hk, rest = blockIdx.x / (unsigned)a.Hk;
   const unsigned chunks = (unsigned)((a.Nk + kWKeys - 1) / kWKeys);
   const int b = (int)(rest / chunks), key0 = (int)(rest % chunks) * kWKeys;
-  const XSample sm = x_sample<true>(a, b);
+  const XSample sm = x_sample<kSeeCache>(a, b);
   const int off = sm.nk - sm.nq, key = key0 + 32 * w + l32;
   const int64_t at = ((int64_t)b * a.Hk + hk) * a.Nk + key;
   float sum = 0.f;
 
-  const XSpan span = x_span(a, sm, 0, sm.nq * a.G);
+  const XSpan span = x_span<kSeeCache>(a, sm, 0, sm.nq * a.G);
   const bool any = (key0 < span.hi && key0 + kWKeys > span.lo) || key0 < span.send;   // uniform
   if (any) {
     // every row sees every key of the workgroup, whatever its place in the chunk or tree
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void cache_weights_kernel(const XArgs a, const
       }
       if (tid < kWRows) {
         const int row = r0 + tid, tok = row_token(min(row, rows - 1), a.G);
-        RowWindow see;
+        RowWindow<kSeeCache> see;
         see.open(a, sm, b, row);
         p_lds[tid] = see.p;
         tree_lds[tid] = see.tree;

@@ -122,7 +122,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       aux[x.Tq * x.Hq + stat] = ndl;
     }
   };
-  const TileLoad<DP, NW> load_k(lane, a.sk), load_v(lane, a.sv);
+  using Load = TileLoad<DP, NW, WIN>;
+  const Load load_k(lane, a.sk), load_v(lane, a.sv);
   // LDS offsets, as in the forward: chunk 2 ks + g of row l32, and K^T's operand.
   // The swizzle is an exclusive or, and so is the step to another ks or dt: one
   // register each and an instruction a use, where sixteen would not fit.
@@ -134,29 +135,18 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};
 
-  TileSeq<WIN> seq;
-  RowWindow see{};   // WIN: the lane's row
-  // WIN: whether rows of the wave differ in the keys of a tile that they see, and the
-  // keys k .. k + 31 that the lane's row of item `at` sees.
-  auto partial = [&](int at, int tile) __attribute__((always_inline)) {
-    const XArgs& x = *x_args_again();
-    return !see.whole(x, x_sample<WIN>(x, seq.item(at, order).b), tile);
-  };
-  auto row_bits = [&](int at, int k) __attribute__((always_inline)) {
-    const XArgs& x = *x_args_again();
-    return see.bits(x, x_sample<WIN>(x, seq.item(at, order).b), k);
-  };
+  constexpr int SEE = WIN ? kSeeWindow : kSeeAll;
+  TileSeq<SEE> seq;
+  RowWindow<SEE> see{};   // the lane's row, unless all is seen
 
   // A tile as two 32-key halves: S^T and dP^T, dS^T, its exchange to the
   // 16x16 operand layout, and the half's dQ product. With `swap` the next item's
   // rows take the place of this one's after the last score products. The next
   // tile's loads (load(u), u < 2 IPW) stand between the first products.
-  using Load = TileLoad<DP, NW>;
   auto step = [&](uint64_t bits, int tile, const char* kt_lds, const char* vt_lds, bool swap, Extra& ex, bool loads,
                   auto load)
       __attribute__((always_inline)) {
-    bool part = false;
-    if constexpr (WIN) part = partial(seq.cur, tile);
+    const bool part = WIN && !see.whole(a, tile);   // rows of the wave differ in the keys that they see
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       f32x16 s = f32x16{}, dp = f32x16{};
@@ -200,7 +190,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       if (kt == 1 && swap) load_rows(seq.item(seq.at, order), ex);   // uniform
       if (bits != ~(uint64_t)0 || part) {     // uniform
         unsigned mine = (unsigned)(bits >> (32 * kt));
-        if constexpr (WIN) mine &= row_bits(seq.cur, kXKeys * tile + 32 * kt);
+        if constexpr (WIN) mine &= see.bits(a, kXKeys * tile + 32 * kt);
         mine >>= 4 * g;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -255,7 +245,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
         dp = mfma32(*reinterpret_cast<const bf16x8*>(vt_lds + off), doop[ks], dp);
       }
       unsigned mine = (unsigned)(bits >> (32 * kt));
-      if constexpr (WIN) mine &= row_bits(seq.at, kXKeys * tile + 32 * kt);
+      if constexpr (WIN) mine &= see.bits(a, kXKeys * tile + 32 * kt);
       mine >>= 4 * g;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -338,7 +328,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
         rows.turn(doop, lds0, lds1);
         if constexpr (WIN) {
           const XArgs& x = *x_args_again();
-          see.open(x, x_sample<WIN>(x, at.b), at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
+          see.open(x, x_sample<SEE>(x, at.b), at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
         }
         const bool one = seq.one_tile(order);   // uniform
         if (one) ndl = -tile_delta(seq.bits, seq.tile, kn, vn);
@@ -368,7 +358,7 @@ struct SinkParts {
 // WIN: the steps are those of the tokens that see a key of the workgroup, and
 // the keys' tiles that hold sinks, which most tokens see, have splits of their own.
 template <int DP, bool WIN>
-__global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const float* __restrict__ aux,
+__global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kernel(const XArgs a, const float* __restrict__ aux,
                                                             const XOrder order, float* __restrict__ part,
                                                             const SinkParts sinks) {
   constexpr int NW = 4, ROWB = DP * 2, CPR = DP / 8, KS = DP / 16, DT = DP / 16;
@@ -470,14 +460,12 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
       }
     };
     const float c2 = a.scale * kLog2e;
-    // WIN: the tokens that see the lane's key are from .. to - 1.
-    int from = 0, to = 0;
-    if constexpr (WIN) {
-      const int key = key0 + 32 * w + l32, off = sm.nk - sm.nq;
+    // WIN: which of the tokens from t on see the lane's key, a bit each.
+    auto seen_by = [&](int t) __attribute__((always_inline)) {
+      const int key = key0 + 32 * w + (x_lane_again() & 31), p = t + sm.nk - sm.nq;
       const bool sink = key < a.sinks;
-      from = sink && a.right > 0 ? 0 : key - a.right - off;
-      to = sink ? sm.nq : key + a.left - off + 1;
-    }
+      return bits32_from_to(sink && a.right > 0 ? 0 : key - a.right - p, sink ? 32 : key + a.left + 1 - p);
+    };
     // rows: the tile's tokens that the lane's key is visible to, a bit each
     auto step = [&](const char* qt_lds, const char* ot_lds, const char* at_lds,
                     unsigned rows) __attribute__((always_inline)) {
@@ -594,7 +582,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(const XArgs a, const
     auto iter = [&](int i, auto par, auto used) __attribute__((always_inline)) {
       constexpr int P = decltype(par)::value;
       unsigned rows = ~0u;
-      if constexpr (WIN) rows = bits32_from_to(from - t_first - tt * kRowTile, to - t_first - tt * kRowTile);
+      if constexpr (WIN) rows = seen_by(t_first + tt * kRowTile);
       advance();
       if (i + 1 < s_end) load_step(head, tt, P ? q_lds0 : q_lds1, P ? o_lds0 : o_lds1, P ? a_lds0 : a_lds1);
       if constexpr (decltype(used)::value)

@@ -51,7 +51,7 @@ struct Parts {
   int64_t stats;
 };
 
-template <int DP, int NW, bool SPLIT, bool WIN>
+template <int DP, int NW, bool SPLIT, int SEE>
 __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_fwd_kernel(const XArgs a, const XOrder order,
                                                                                            const Parts parts) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
 
-  if (a.zero_rest) {   // here, not in a launch of its own, which costs 6 us
+  if (SEE != kSeeCache && a.zero_rest) {   // here, not in a launch of its own, which costs 6 us
     x_clear_rest(a.cuq, a.B, a.Tq, a.Hq * a.D, a.o, a.so);
     const int64_t end = min(max((int64_t)x_cu(a.cuq, a.B), (int64_t)0), a.Tq), rest = a.Tq - end;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + tid; i < rest * a.Hq; i += (int64_t)gridDim.x * blockDim.x)
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   bf16x8 qop[KS];
   auto load_rows = [&](const XItem& at) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
-    const XSample sm = x_sample<WIN>(x, at.b);
+    const XSample sm = x_sample<SEE>(x, at.b);
     x_load_rows<DP>(qop, x.q, sm.q0, x.sq, (int64_t)at.hk * x.G * x.D, at.tile * 32 * NW + 32 * w, sm.nq, x.G, x.D);
   };
   const TileLoad<DP, NW> load_k(lane, a.sk), load_v(lane, a.sv);
@@ -97,8 +97,8 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   float m_run = 0.f, l_run = 0.f;
   bool fresh = true;                   // no key of the item seen yet: no reference (uniform)
 
-  TileSeq<WIN> seq;
-  RowWindow see{};                     // WIN: the lane's row
+  TileSeq<SEE> seq;
+  RowWindow<SEE> see{};                // the lane's row, unless all is seen
 
   // One tile in two 32-key halves, so that a wave's vector work has matrix work of
   // its own beside it: S of half 1 runs beside the exponentials of half 0, and the
@@ -144,20 +144,13 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[h][e]);
       return fmaxf(mx * c2, -3.0e38f);
     };
-    bool part = false;   // WIN: rows of the wave differ in the keys that they see
-    if constexpr (WIN) {
-      const XArgs& x = *x_args_again();
-      part = !see.whole(x, x_sample<WIN>(x, seq.item(seq.cur, order).b), tile);
-    }
+    const bool part = SEE != kSeeAll && !see.whole(a, tile);   // rows of the wave differ in the keys that they see
     // Before half h's exponentials: unused keys, and the item's reference.
     auto prepare = [&](int h) __attribute__((always_inline)) {
       const unsigned half = (unsigned)(bits >> (32 * h));
       if (half != ~0u || part) {   // uniform
         unsigned mine = half;
-        if constexpr (WIN) {
-          const XArgs& x = *x_args_again();
-          mine &= see.bits(x, x_sample<WIN>(x, seq.item(seq.cur, order).b), kXKeys * tile + 32 * h);
-        }
+        if constexpr (SEE != kSeeAll) mine &= see.bits(a, kXKeys * tile + 32 * h);
         mine >>= 4 * g;
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[h][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[h][e] : -INFINITY;
@@ -283,7 +276,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   // O = O^T / l, LSE = (m + log2 l) ln 2; a row without keys: 0 and -inf.
   auto finish = [&](const XItem& at, char* lds0, char* lds1) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
-    const XSample sm = x_sample<WIN>(x, at.b);
+    const XSample sm = x_sample<SEE>(x, at.b);
     const int rows = sm.nq * x.G, r0 = at.tile * 32 * NW + 32 * w;
     const float l_tot = pair_sum(l_run);
     const bool none = l_tot == 0.f;
@@ -358,10 +351,10 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       if (have) finish(seq.item(seq.cur, order), lds0, lds1);
       if (more) {
         XTurn<DP>(x_lane_again()).turn(qop, lds0, lds1);
-        if constexpr (WIN) {
+        if constexpr (SEE != kSeeAll) {
           const XArgs& x = *x_args_again();
           const XItem at = seq.item(seq.at, order);
-          see.open(x, x_sample<WIN>(x, at.b), at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
+          see.open(x, x_sample<SEE>(x, at.b), at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
         }
       }
       seq.cur = seq.at;
@@ -466,26 +459,27 @@ Shape fwd_shape(const XArgs& a) {
 }
 int64_t stats_of(const XArgs& a) { return a.Tq * a.Hq; }
 
-template <int DP, int NW, bool WIN>
+template <int DP, int NW, int SEE>
 void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
   const int64_t items = (int64_t)a.B * a.Hk * order.tiles * splits;
   const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, NW)) + 7) / 8 * 8);
-  TraceScope ts_(s, WIN ? splits > 1 ? "swattn_fwd_split" : "swattn_fwd" : splits > 1 ? "xattn_fwd_split" : "xattn_fwd",
-                 DP, NW);
+  static const char* const names[][2] = {
+      {"xattn_fwd", "xattn_fwd_split"}, {"swattn_fwd", "swattn_fwd_split"}, {"cache_fwd", "cache_fwd_split"}};
+  TraceScope ts_(s, names[SEE][splits > 1], DP, NW);
   if (splits > 1) {
-    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, true, WIN>), grid, dim3(64 * NW), 0, s, a, order, parts);
+    hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, true, SEE>), grid, dim3(64 * NW), 0, s, a, order, parts);
   } else {
     if constexpr (NW == 4)
-      hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, false, WIN>), grid, dim3(64 * NW), 0, s, a, order, parts);
+      hipLaunchKernelGGL((xattn_fwd_kernel<DP, NW, false, SEE>), grid, dim3(64 * NW), 0, s, a, order, parts);
   }
 }
-template <bool WIN>
+template <int SEE>
 void launch_fwd(const XArgs& a, int splits, int waves, const Parts& parts, hipStream_t s) {
   if (a.D <= 64)
-    waves == 1 ? launch_fwd<64, 1, WIN>(a, splits, parts, s) : launch_fwd<64, 4, WIN>(a, splits, parts, s);
+    waves == 1 ? launch_fwd<64, 1, SEE>(a, splits, parts, s) : launch_fwd<64, 4, SEE>(a, splits, parts, s);
   else
-    waves == 1 ? launch_fwd<128, 1, WIN>(a, splits, parts, s) : launch_fwd<128, 4, WIN>(a, splits, parts, s);
+    waves == 1 ? launch_fwd<128, 1, SEE>(a, splits, parts, s) : launch_fwd<128, 4, SEE>(a, splits, parts, s);
 }
 template <int GPR>
 void launch_join(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
@@ -510,7 +504,9 @@ hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s) {
     parts.o = static_cast<float*>(workspace);
     parts.sums = reinterpret_cast<float2*>(parts.o + (size_t)splits * parts.stats * a.D);
   }
-  a.window ? launch_fwd<true>(a, splits, waves, parts, s) : launch_fwd<false>(a, splits, waves, parts, s);
+  if (a.lens) launch_fwd<kSeeCache>(a, splits, waves, parts, s);
+  else if (a.window) launch_fwd<kSeeWindow>(a, splits, waves, parts, s);
+  else launch_fwd<kSeeAll>(a, splits, waves, parts, s);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   // Eight groups of lanes a row where many parts are to be read for few rows: 320 rows
   // of 11 parts 6.9 us against 11.3 with one, 1,024 of 8 7.0 against 9.0; but 8,000 of

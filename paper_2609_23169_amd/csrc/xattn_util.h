@@ -13,6 +13,10 @@ namespace ut {
 constexpr int kXKeys = 64;                 // keys of a tile
 constexpr int kXOut = 0x40000000;          // a byte offset past every descriptor's range: reads zeros
 
+// What a query sees: every key in use; those of its window and the sinks; or of a cache
+// the slots in use, in a window and by a tree.
+constexpr int kSeeAll = 0, kSeeWindow = 1, kSeeCache = 2;
+
 // The kernel's arguments (an XArgs in front of the others), read again where they
 // are used: work done once an item would otherwise hold some fifty more scalar
 // registers through the loop over the tiles. The compiler still keeps 25 to 48 in
@@ -101,17 +105,17 @@ __device__ inline unsigned bits32_from_to(int lo, int hi) {
 // The key tiles of one sample that hold a key in use, and which keys of each:
 // 64 tiles at a time, one a lane, as 64-bit masks, so that a step to the next
 // tile costs a few scalar instructions and unused tiles none. Tiles
-// [begin, end) (WIN: of the span's list); n keys; mask: a byte a key, or null.
-template <bool WIN>
+// [begin, end) (unless all is seen: of the span's list); n keys; mask: a byte a key, or null.
+template <int SEE>
 struct KeyTiles {
   const uint8_t* mask;
   int n, end, base;
   uint64_t mine, left;   // this lane's tile; the group's tiles not yet visited
-  XSpan span;            // WIN only
+  XSpan span;            // unless all is seen
 
   // Tile number i of the list.
   __device__ inline int number(int i) const {
-    if constexpr (WIN) return i + (i >= span.first ? span.skip : 0);
+    if constexpr (SEE != kSeeAll) return i + (i >= span.first ? span.skip : 0);
     return i;
   }
   __device__ inline void open(const uint8_t* m, int keys, int begin, int stop) {
@@ -146,13 +150,13 @@ struct KeyTiles {
       mine = kXKeys * (t + 1) <= n ? ~(uint64_t)0 : 0;
     }
     const int last = n / kXKeys, rest = n % kXKeys;   // the short last tile
-    if (WIN ? rest && __ballot(i < end && t == last) != 0
+    if (SEE != kSeeAll ? rest && __ballot(i < end && t == last) != 0
             : rest && last < end && last >= base && last < base + 64) {
       const bool in = lane < rest && (!mask || mask[(int64_t)kXKeys * last + lane]);
       const uint64_t bits = __ballot(in);
       if (t == last) mine = bits;
     }
-    if constexpr (WIN) {
+    if constexpr (SEE != kSeeAll) {
       const int k = kXKeys * t;
       mine &= (bits_below(span.hi - k) & ~bits_below(span.lo - k)) | bits_below(span.send - k);
       if (i >= end) mine = 0;
@@ -192,13 +196,12 @@ __device__ inline int x_cu(const int32_t* cu, int i) {
   return cu[i];
 #endif
 }
-template <bool WIN = false>
+template <int SEE = kSeeAll>
 __device__ inline XSample x_sample(const XArgs& a, int b) {
-  if constexpr (WIN)
-    if (a.lens) {   // clamped, so that no length can send an access outside the cache
-      const int used = min(max(x_cu(a.lens, b), 0), a.Nk - a.Nq) + a.Nq;
-      return XSample{(int64_t)b * a.Nq, (int64_t)b * a.Nk, a.Nq, used, (int64_t)b * a.Hq * a.Nq, (int64_t)a.Nq};
-    }
+  if constexpr (SEE == kSeeCache) {   // clamped, so that no length can send an access outside the cache
+    const int used = min(max(x_cu(a.lens, b), 0), a.Nk - a.Nq) + a.Nq;
+    return XSample{(int64_t)b * a.Nq, (int64_t)b * a.Nk, a.Nq, used, (int64_t)b * a.Hq * a.Nq, (int64_t)a.Nq};
+  }
   if (!a.cuq)
     return XSample{(int64_t)b * a.Nq, (int64_t)b * a.Nk, a.Nq, a.Nk, (int64_t)b * a.Hq * a.Nq, (int64_t)a.Nq};
   // clamped as in sample_rows: no offsets can send an access outside the tensors
@@ -215,13 +218,15 @@ __device__ inline int row_token(int row, int G) {
 }
 
 // What the rows r0 .. r0 + n - 1 of a sample see, as a span.
+template <int SEE>
 __device__ inline XSpan x_span(const XArgs& a, const XSample& sm, int r0, int n) {
-  const int off = sm.nk - sm.nq;
+  const bool tree = SEE == kSeeCache && a.tree;
+  const int off = sm.nk - sm.nq, right = SEE == kSeeCache ? 0 : a.right;
   const int p0 = off + row_token(r0, a.G), p1 = off + row_token(min(r0 + n, sm.nq * a.G) - 1, a.G);
   XSpan s;
-  s.lo = max(0, (a.tree ? off : p0) - a.left);
-  s.hi = a.tree ? sm.nk : max(0, min(sm.nk, p1 + a.right + 1));
-  s.send = max(0, min(min(a.sinks, sm.nk), a.tree ? off : a.right > 0 ? sm.nk : p1 + 1));
+  s.lo = max(0, (tree ? off : p0) - a.left);
+  s.hi = tree ? sm.nk : max(0, min(sm.nk, p1 + right + 1));
+  s.send = max(0, min(min(a.sinks, sm.nk), tree ? off : right > 0 ? sm.nk : p1 + 1));
   s.first = (s.send + kXKeys - 1) / kXKeys;
   const int w0 = max(s.first, s.lo / kXKeys), w1 = s.lo < s.hi ? (s.hi + kXKeys - 1) / kXKeys : 0;
   s.skip = w0 - s.first;
@@ -229,39 +234,50 @@ __device__ inline XSpan x_span(const XArgs& a, const XSample& sm, int r0, int n)
   return s;
 }
 
-// What a lane's row sees, for the items' tiles that its wave does not see whole.
+// What a lane's row sees: the tiles that a wave does not see whole take a mask a row.
+template <int SEE>
 struct RowWindow {
   int p;          // the row's position
-  uint64_t tree;  // the last nq keys that it sees, a bit each (a tree only)
+  int end;        // kSeeCache: the first slot that it does not see by place
+  uint64_t tree;  // kSeeCache: which of the slots from there on it sees, a bit each
 
   __device__ inline void open(const XArgs& a, const XSample& sm, int b, int row) {
     const int tok = row_token(min(row, sm.nq * a.G - 1), a.G);
     p = sm.nk - sm.nq + tok;
-    tree = 0;
-    if (a.tree) {   // its position is behind the keys of the tree that it sees, less itself
-      tree = a.tree[(int64_t)b * a.Nq + tok] & bits_below(a.Nq);
-      p += __builtin_popcountll(tree & ~((uint64_t)1 << tok)) - tok;
+    if constexpr (SEE == kSeeCache) {
+      end = p + 1;
+      tree = 0;
+      if (a.tree) {   // its position is behind the tokens of the tree that it sees, less itself
+        tree = a.tree[(int64_t)b * a.Nq + tok] & bits_below(a.Nq);
+        end = sm.nk - sm.nq;
+        p = end + __builtin_popcountll(tree & ~((uint64_t)1 << tok));
+      }
     }
   }
-  // Whether every row of the wave sees all keys of a tile (uniform; the rows'
-  // positions ascend from lane 0 to lane 31, in a tree by any order within nq).
-  __device__ inline bool whole(const XArgs& a, const XSample& sm, int tile) const {
-    const int k = kXKeys * tile, off = sm.nk - sm.nq;
-    const int p0 = __builtin_amdgcn_readfirstlane(p), p1 = a.tree ? off + sm.nq : __builtin_amdgcn_readlane(p, 31);
-    const int end = a.tree ? off : p0 + a.right + 1;
-    if (k >= p1 - a.left && k + kXKeys <= end) return true;
-    return k + kXKeys <= min(a.sinks, a.right > 0 ? sm.nk : end);
+  __device__ inline int stop(const XArgs& a, int at) const { return SEE == kSeeCache ? end : at + a.right + 1; }
+  __device__ inline int sinks(const XArgs& a, int stop) const {
+    return SEE == kSeeWindow && a.right > 0 ? a.sinks : min(a.sinks, stop);
   }
-  // Keys k .. k + 31 that the row sees, a bit each.
-  __device__ inline unsigned bits(const XArgs& a, const XSample& sm, int k) const {
-    const int off = sm.nk - sm.nq, end = a.tree ? off : p + a.right + 1;
-    unsigned m = bits32_from_to(p - a.left - k, end - k) |
-                 bits32_from_to(0, min(a.sinks, a.right > 0 ? sm.nk : end) - k);
-    if (a.tree) {
-      const int at = off - k;   // bit 0 of the tree
-      if (at >= 0) m |= at < 32 ? (unsigned)(tree << at) : 0u;
-      else m |= at > -64 ? (unsigned)(tree >> -at) : 0u;
-    }
+  // Whether every row of the wave sees all keys of a tile (uniform). The rows'
+  // positions ascend from lane 0 to lane 31; in a tree they lie within Nq.
+  __device__ inline bool whole(const XArgs& a, int tile) const {
+    const int k = kXKeys * tile, first = __builtin_amdgcn_readfirstlane(stop(a, p));
+    const int last = SEE == kSeeCache && a.tree ? first + a.Nq : __builtin_amdgcn_readlane(p, 31);
+    return (k >= last - a.left && k + kXKeys <= first) || k + kXKeys <= sinks(a, first);
+  }
+  // Keys k .. k + 31 that the row sees, a bit each (keys that the sample lacks
+  // included).
+  __device__ inline unsigned bits(const XArgs& a, int k) const {
+    int at = p;
+    pin_value(at);   // what follows is formed here: kept in registers through the loop otherwise
+    const int to = stop(a, at);
+    unsigned m = bits32_from_to(at - a.left - k, to - k) | bits32_from_to(0, sinks(a, to) - k);
+    if constexpr (SEE == kSeeCache)
+      if (a.tree) {   // uniform
+        const int bit = end - k;   // of token 0
+        if (bit >= 0) m |= bit < 32 ? (unsigned)(tree << bit) : 0u;
+        else m |= bit > -64 ? (unsigned)(tree >> -bit) : 0u;
+      }
     return m;
   }
 };
@@ -291,11 +307,11 @@ __device__ inline void x_clear_rest(const int32_t* cu, int B, int64_t T, int wid
 // place of three divisions, and the scalar registers are left to the loop over the
 // tiles. The code of a change stands once in the loop: an item whose keys are not in
 // use yields one tile without keys (bits 0), so that it is finished like the others.
-template <bool WIN>
+template <int SEE>
 struct TileSeq {
   static constexpr int kTurns = 62;             // even: every group begins with a forward turn
   static constexpr int kKept = 63;              // the lane that keeps an item over the groups
-  KeyTiles<WIN> tiles;
+  KeyTiles<SEE> tiles;
   int b, rtile, hkpart;                         // a lane's item: sample, tile of rows, key head and part
   unsigned first, step, turn, end;              // the next group's items (XItems)
   uint64_t todo;                                // items of the group not begun
@@ -334,7 +350,7 @@ struct TileSeq {
       const bool in = lane < kTurns && it < end;
       const XItem m = x_item(in ? it : 0, (unsigned)x.B, order);
       int nq = x.Nq;
-      if (x.cuq) {   // as x_sample
+      if (SEE != kSeeCache && x.cuq) {   // as x_sample
         const int64_t q0 = min(max((int64_t)x.cuq[m.b], (int64_t)0), x.Tq);
         nq = (int)min(min(max((int64_t)x.cuq[m.b + 1], q0), x.Tq) - q0, (int64_t)x.Nq);
       }
@@ -362,10 +378,10 @@ struct TileSeq {
       todo &= todo - 1;
       const XItem m = item(at, order);
       const XArgs& x = *x_args_again();
-      const XSample sm = x_sample<WIN>(x, m.b);
+      const XSample sm = x_sample<SEE>(x, m.b);
       int n = (sm.nk + kXKeys - 1) / kXKeys;
-      if constexpr (WIN) {
-        tiles.span = x_span(x, sm, m.tile * rows_per_item, rows_per_item);
+      if constexpr (SEE != kSeeAll) {
+        tiles.span = x_span<SEE>(x, sm, m.tile * rows_per_item, rows_per_item);
         n = tiles.span.count;
       }
       int t0 = 0, t1 = n;
@@ -374,7 +390,7 @@ struct TileSeq {
         t0 = min(m.part * per, n);
         t1 = min(t0 + per, n);
       }
-      tiles.open(x.mask ? x.mask + sm.k0 : nullptr, sm.nk, t0, t1);
+      tiles.open(SEE != kSeeCache && x.mask ? x.mask + sm.k0 : nullptr, sm.nk, t0, t1);
       k0 = sm.k0;
       hk = m.hk;
       keys = sm.nk;
@@ -389,11 +405,11 @@ struct TileSeq {
   // first 4,096 keys (dQ of 40 rows on 700 keys 16.8 -> 17.9 us), 8 us at 20 keys of
   // 16,391; unsplit ones have it from the walk.
   __device__ inline bool one_tile(const XOrder& order) const {
-    const int n = WIN ? tiles.span.count : (keys + kXKeys - 1) / kXKeys;
+    const int n = SEE != kSeeAll ? tiles.span.count : (keys + kXKeys - 1) / kXKeys;
     if (n <= 1) return bits != 0;
     if (!tiles.mask) return false;
-    KeyTiles<WIN> t;   // the tiles not yet looked at; of a split item, all of the sample's
-    if constexpr (WIN) t.span = tiles.span;
+    KeyTiles<SEE> t;   // the tiles not yet looked at; of a split item, all of the sample's
+    if constexpr (SEE != kSeeAll) t.span = tiles.span;
     int count = 0, from = 0;
     if (order.splits == 1) {
       if (tiles.left != 0) return false;
@@ -534,7 +550,9 @@ __device__ inline void x_store_rows(void* dst, int64_t tok0, int stride, int64_t
 // instruction u of wave w writes 1 KB of rows. Within 16 rows the swizzle only
 // flips bits of the column that the instruction's number gives, so a lane keeps
 // its row's offset and its column, and the rest is scalar.
-template <int DP, int NW>
+// FEW: the lane's offsets are formed again for every tile, where the loop has no
+// registers to keep them in.
+template <int DP, int NW, bool FEW = false>
 struct TileLoad {
   static constexpr int ROWB = DP * 2, CPR = DP / 8;
   static constexpr int RPI = 1024 / ROWB;                      // rows per instruction
@@ -562,7 +580,9 @@ struct TileLoad {
   // Instruction u of wave w of a tile whose keys are all in use. Columns past D
   // become zeros.
   __device__ inline void one(__amdgpu_buffer_rsrc_t rs, int stride, char* dst, int w, int u, int D) const {
-    const int i = w * IPW + u, c = column ^ flip(u % REP);
+    int first = column;
+    if constexpr (FEW) pin_value(first);
+    const int i = w * IPW + u, c = first ^ flip(u % REP);
     int step = RPI * stride * 2;   // not kept in a register for each instruction
     UT_DEV_ASM("" : "+s"(step));
     buffer_load_lds16(rs, dst + i * 1024, c < 2 * D ? row + c : kXOut, i * step);
@@ -571,9 +591,11 @@ struct TileLoad {
   // there, and are not read.
   __device__ inline void masked(__amdgpu_buffer_rsrc_t rs, int stride, uint64_t bits, char* dst, int w, int lane,
                                 int D) const {
+    int first = column;
+    if constexpr (FEW) pin_value(first);
 #pragma unroll
     for (int u = 0; u < IPW; ++u) {
-      const int i = w * IPW + u, c = column ^ flip(u % REP);
+      const int i = w * IPW + u, c = first ^ flip(u % REP);
       const unsigned run = (unsigned)(bits >> (i * RPI));   // scalar: this instruction's rows
       buffer_load_lds16(rs, dst + i * 1024, run >> (lane / CPR) & 1 && c < 2 * D ? row + c : kXOut,
                         i * RPI * stride * 2);
