@@ -719,7 +719,8 @@ ut_status ut_swattn_bwd_varlen(const void* q, const void* k, const void* v, cons
  *           the heads of the group, of the softmax weight of slot j, for every slot (of
  *           weights_in alone where nothing sees it). weights_in NULL: zeros;
  *           weights_out may be weights_in.
- * workspace as in ut_xattn_fwd, of the size query's bytes.
+ * workspace as in ut_xattn_fwd, of the size query's bytes (with_weights: nonzero for
+ *           a call with weights_out).
  * A token that sees no slot (a tree word of 0 in front of an empty cache): o = 0,
  * lse = -inf. No atomics: results are deterministic.
  * Errors: those of ut_xattn_fwd; T < 1 or > capacity, a tree with T > 64 or
@@ -727,7 +728,8 @@ ut_status ut_swattn_bwd_varlen(const void* q, const void* k, const void* v, cons
  *         -> UT_ERR_INVALID_ARG.
  * ---------------------------------------------------------------------- */
 size_t ut_cache_attn_workspace_size(int32_t B, int32_t T, int32_t capacity, int32_t Hq, int32_t Hk,
-                                    int32_t D, int32_t window_left, int32_t n_sink);
+                                    int32_t D, int32_t window_left, int32_t n_sink,
+                                    int32_t with_weights);
 ut_status ut_cache_attn(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
                         const int64_t* strides_host, const int32_t* cache_len, const uint64_t* tree,
                         const float* weights_in, float* weights_out, int32_t B, int32_t T,

@@ -123,7 +123,7 @@ _SIGS = {
     "ut_swattn_bwd": (_c.c_int, [_vp] * 11 + [_i32] * 9 + [_f32, _vp, _sz, _vp]),
     "ut_swattn_bwd_varlen_workspace_size": (_sz, [_i32, _i64, _i64] + [_i32] * 8),
     "ut_swattn_bwd_varlen": (_c.c_int, [_vp] * 13 + [_i32, _i64, _i64] + [_i32] * 8 + [_f32, _i32, _vp, _sz, _vp]),
-    "ut_cache_attn_workspace_size": (_sz, [_i32] * 8),
+    "ut_cache_attn_workspace_size": (_sz, [_i32] * 9),
     "ut_cache_attn": (_c.c_int, [_vp] * 10 + [_i32] * 8 + [_f32, _vp, _sz, _vp]),
     "ut_cache_weights": (_c.c_int, [_vp] * 9 + [_i32] * 8 + [_f32, _vp]),
     "ut_cache_evict": (_c.c_int, [_vp] * 10 + [_i32] * 9 + [_vp]),
@@ -813,9 +813,9 @@ def _check_weights(t, shape, name: str):
 
 
 def ut_cache_attn_workspace_size(B: int, T: int, capacity: int, Hq: int, Hk: int, D: int, window_left=None,
-                                 n_sink: int = 0) -> int:
+                                 n_sink: int = 0, with_weights: bool = False) -> int:
     return _size(lib().ut_cache_attn_workspace_size, B, T, capacity, Hq, Hk, D, _window((window_left, 0), n_sink)[0],
-                 n_sink)
+                 n_sink, int(with_weights))
 
 
 def ut_cache_attn(q, k_cache, v_cache, o, lse, cache_len, softmax_scale: float, tree=None, window_left=None,
@@ -1252,7 +1252,8 @@ def cache_attn(q, k_cache, v_cache, cache_len, softmax_scale: float, tree=None, 
         if weights is not None and weights_out is None:
             weights_out = torch.empty_like(weights)
         if workspace is None:
-            workspace = _scratch(ut_cache_attn_workspace_size(B, T, cap, Hq, Hk, D, window_left, n_sink), q.device)
+            workspace = _scratch(ut_cache_attn_workspace_size(B, T, cap, Hq, Hk, D, window_left, n_sink,
+                                                              weights_out is not None), q.device)
     _raise("ut_cache_attn", ut_cache_attn(q, k_cache, v_cache, o, lse, cache_len, softmax_scale, tree, window_left,
                                           n_sink, weights, weights_out, workspace, stream))
     return (o, lse) if weights_out is None else (o, lse, weights_out)

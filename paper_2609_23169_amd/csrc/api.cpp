@@ -1232,6 +1232,8 @@ ut_status check_words(const char* fn, const char* name, const uint64_t* p) {
   return p ? check_ptr(fn, name, p, 8) : UT_OK;
 }
 
+constexpr int32_t kNoLens = 0;   // stands for a cache in the workspace query; not read
+
 struct Range {   // bytes
   const char* p;
   int64_t n;
@@ -1243,11 +1245,14 @@ bool overlap(const Range& x, const Range& y) {
 }  // namespace
 
 size_t ut_cache_attn_workspace_size(int32_t B, int32_t T, int32_t capacity, int32_t Hq, int32_t Hk,
-                                    int32_t D, int32_t window_left, int32_t n_sink) {
+                                    int32_t D, int32_t window_left, int32_t n_sink,
+                                    int32_t with_weights) {
   XArgs a{};
   const bool ok = check_cache("ut_cache_attn", B, T, capacity, Hq, Hk, D, window_left, n_sink, false, 1.f, &a) == UT_OK;
   g_last_error[0] = 0;
-  return ok ? xattn_fwd_workspace(a) : 0;
+  a.lens = &kNoLens;
+  a.scores = with_weights && (int64_t)T * a.G <= kScoreRows;
+  return ok ? cache_attn_workspace(a) : 0;
 }
 
 ut_status ut_cache_attn(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
@@ -1264,12 +1269,15 @@ ut_status ut_cache_attn(const void* q, const void* k_cache, const void* v_cache,
   if (weights_in) UT_TRY(check_ptr(fn, "weights_in", weights_in, 4));
   if (weights_in || weights_out) UT_TRY(check_ptr(fn, "weights_out", weights_out, 4));
   UT_TRY(check_lens(fn, cache_len, B, capacity - T, stream));
-  a.lens = cache_len, a.tree = tree;
-  UT_TRY(xattn_fwd(fn, a, q, k_cache, v_cache, o, lse, strides_host, nullptr, workspace, workspace_bytes, false,
-                   stream));
-  if (!weights_out) return UT_OK;
-  return check_hip(launch_cache_weights(a, CacheWeights{weights_in, weights_out, nullptr}, stream),
-                   "cache weights launch");
+  const XTensor t[] = {{"q", q, &a.sq, false}, {"k_cache", k_cache, &a.sk, true}, {"v_cache", v_cache, &a.sv, true},
+                       {"o", o, &a.so, false}};
+  UT_TRY(check_xtensors(fn, t, 4, strides_host, a));
+  UT_TRY(check_ptr(fn, "lse", lse, 4));
+  a.q = q, a.k = k_cache, a.v = v_cache, a.o = o, a.lse = lse, a.lens = cache_len, a.tree = tree;
+  a.scores = weights_out && (int64_t)T * a.G <= kScoreRows;
+  UT_TRY(check_space(fn, cache_attn_workspace(a), workspace, workspace_bytes));
+  return check_hip(launch_cache_attn(a, CacheWeights{weights_in, weights_out, nullptr}, workspace, stream),
+                   "cache attention launch");
 }
 
 ut_status ut_cache_weights(const void* q, const void* k_cache, const float* lse,

@@ -4,10 +4,12 @@
 //
 // Weights: out[b, hk, j] = in[b, hk, j] + sum over the tokens t and the heads h of the
 // group of P = exp(S scale - LSE). The attention knows a row's LSE only at its end, so
-// this pass forms the scores again: a wave takes 32 keys, whose rows stay in registers,
-// and walks the rows of the group in tiles of 32 through LDS; S = Q K^T on 32x32x16 bf16
-// MFMA in the layout where a lane holds one key, so that the sum over the rows is the
-// lane's own but for one exchange. fp32 throughout, a fixed order: no atomics.
+// this pass forms the scores again (of few rows the attention leaves them instead): a
+// workgroup keeps the rows of the group in LDS, up to 192 at once, a wave takes tiles of
+// 32 keys, whose rows pass through its registers, the next tile's loads beside the
+// products; S = Q K^T on 32x32x16 bf16 MFMA in the layout where a lane holds one key, so
+// that the sum over the rows is the lane's own but for one exchange. fp32 throughout, a
+// fixed order: no atomics.
 //
 // Eviction: of a row of weights the middle slots (behind the sinks, before the recent
 // ones) are bisected by value for the smallest weight that stays. A workgroup holds the
@@ -23,13 +25,12 @@ namespace ut {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kWKeys = 128;   // keys of a workgroup
-constexpr int kWRows = 32;    // rows of a step
+constexpr int kWRows = 192;   // rows in LDS: 48 KB at 128 columns, three workgroups a CU
+constexpr int kWTiles = 4;    // most tiles of 32 keys of a wave
 
 template <int DP>
-__global__ __launch_bounds__(256) void cache_weights_kernel(const XArgs a, const CacheWeights c) {
-  constexpr int ROWB = DP * 2, CPR = DP / 8, KS = DP / 16, IPT = kWRows * CPR / 256;   // 16-byte pieces a thread
-  static_assert(IPT >= 1, "a step's rows are loaded by all threads");
+__global__ __launch_bounds__(256, 3) void cache_weights_kernel(const XArgs a, const CacheWeights c, const int per_wave) {
+  constexpr int ROWB = DP * 2, CPR = DP / 8, KS = DP / 16;
   __shared__ __attribute__((aligned(16))) char q_lds[kWRows * ROWB];
   __shared__ __attribute__((aligned(16))) float lse_lds[kWRows];
   __shared__ int p_lds[kWRows];
@@ -37,77 +38,110 @@ __global__ __launch_bounds__(256) void cache_weights_kernel(const XArgs a, const
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned hk = blockIdx.x % (unsigned)a.Hk, rest = blockIdx.x / (unsigned)a.Hk;
-  const unsigned chunks = (unsigned)((a.Nk + kWKeys - 1) / kWKeys);
-  const int b = (int)(rest / chunks), key0 = (int)(rest % chunks) * kWKeys;
+  const int keys = 128 * per_wave;   // of the workgroup
+  const unsigned chunks = (unsigned)((a.Nk + keys - 1) / keys);
+  const int b = (int)(rest / chunks), key0 = (int)(rest % chunks) * keys;
   const XSample sm = x_sample<kSeeCache>(a, b);
-  const int off = sm.nk - sm.nq, key = key0 + 32 * w + l32;
-  const int64_t at = ((int64_t)b * a.Hk + hk) * a.Nk + key;
-  float sum = 0.f;
-
-  const XSpan span = x_span<kSeeCache>(a, sm, 0, sm.nq * a.G);
-  const bool any = (key0 < span.hi && key0 + kWKeys > span.lo) || key0 < span.send;   // uniform
-  if (any) {
-    // every row sees every key of the workgroup, whatever its place in the chunk or tree
-    const bool whole = key0 + kWKeys <= off && (key0 >= off + sm.nq - a.left || key0 + kWKeys <= a.sinks);
-    const __bf16* const kp = static_cast<const __bf16*>(a.k) + (sm.k0 + min(key, a.Nk - 1)) * a.sk + hk * a.D + 8 * g;
-    bf16x8 kop[KS];
+  const int off = sm.nk - sm.nq, rows = sm.nq * a.G;
+  const XSpan span = x_span<kSeeCache>(a, sm, 0, rows);
+  const float c2 = a.scale * kLog2e;
+  // The wave's tiles: one of every four in turn. Whether some row sees keys from k on.
+  auto tile_key = [&](int i) __attribute__((always_inline)) { return key0 + 32 * (4 * i + w); };
+  auto seen = [&](int k) __attribute__((always_inline)) {
+    return (k < span.hi && k + 32 > span.lo) || k < span.send;
+  };
+  auto load = [&](bf16x8 (&kop)[KS], int k) __attribute__((always_inline)) {
+    const __bf16* const kp =
+        static_cast<const __bf16*>(a.k) + (sm.k0 + min(k + l32, a.Nk - 1)) * a.sk + hk * a.D + 8 * g;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       kop[ks] = bf16x8{};
       if (16 * ks + 8 * g < a.D) kop[ks] = *reinterpret_cast<const bf16x8*>(kp + 16 * ks);
     }
-    const float c2 = a.scale * kLog2e;
-    const int rows = sm.nq * a.G;
-    for (int r0 = 0; r0 < rows; r0 += kWRows) {
-      if (r0 > 0) __syncthreads();
+  };
+  float sum[kWTiles];
 #pragma unroll
-      for (int u = 0; u < IPT; ++u) {
-        const int i = u * 256 + tid, r = i / CPR, ch = i % CPR, tok = row_token(r0 + r, a.G);
-        bf16x8 x = bf16x8{};
-        if (r0 + r < rows && 8 * ch < a.D)
-          x = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + (sm.q0 + tok) * a.sq +
-                                               (hk * a.G + r0 + r - tok * a.G) * a.D + 8 * ch);
-        *reinterpret_cast<bf16x8*>(q_lds + lds_off<CPR>(r, ch)) = x;
+  for (int i = 0; i < kWTiles; ++i) sum[i] = 0.f;
+  // uniform over the workgroup
+  const bool any = (key0 < span.hi && key0 + keys > span.lo) || key0 < span.send;
+  for (int r0 = 0; any && r0 < rows; r0 += kWRows) {
+    const int n = min(rows - r0, kWRows);
+    if (r0 > 0) __syncthreads();
+    constexpr int kLoads = kWRows * CPR / 256;   // 16-byte pieces a thread, loaded together
+    bf16x8 piece[kLoads];
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int i = u * 256 + tid, r = i / CPR, ch = i % CPR, tok = row_token(r0 + r, a.G);
+      piece[u] = bf16x8{};
+      if (r < n && 8 * ch < a.D)
+        piece[u] = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + (sm.q0 + tok) * a.sq +
+                                                    (hk * a.G + r0 + r - tok * a.G) * a.D + 8 * ch);
+    }
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int i = u * 256 + tid;
+      *reinterpret_cast<bf16x8*>(q_lds + lds_off<CPR>(i / CPR, i % CPR)) = piece[u];
+    }
+    if (tid < (n + 31) / 32 * 32) {
+      const int row = r0 + tid, tok = row_token(min(row, rows - 1), a.G);
+      RowWindow<kSeeCache> see;
+      see.open(a, sm, b, row);
+      p_lds[tid] = see.p;
+      tree_lds[tid] = see.tree;
+      // rows that are not counted, and rows without keys: P = 0
+      float l = INFINITY;
+      if (row < rows && (!c.tokens || c.tokens[b] >> tok & 1)) {
+        l = a.lse[sm.stat0 + (hk * a.G + row - tok * a.G) * sm.hstep + tok] * kLog2e;
+        if (l == -INFINITY) l = INFINITY;
       }
-      if (tid < kWRows) {
-        const int row = r0 + tid, tok = row_token(min(row, rows - 1), a.G);
-        RowWindow<kSeeCache> see;
-        see.open(a, sm, b, row);
-        p_lds[tid] = see.p;
-        tree_lds[tid] = see.tree;
-        // rows that are not counted, and rows without keys: P = 0
-        float l = INFINITY;
-        if (row < rows && (!c.tokens || c.tokens[b] >> tok & 1)) {
-          l = a.lse[sm.stat0 + (hk * a.G + row - tok * a.G) * sm.hstep + tok] * kLog2e;
-          if (l == -INFINITY) l = INFINITY;
-        }
-        lse_lds[tid] = l;
-      }
-      __syncthreads();
-      f32x16 s = f32x16{};
+      lse_lds[tid] = l;
+    }
+    bf16x8 next[KS];
+    load(next, tile_key(0));
+    __syncthreads();
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        s = mfma32(*reinterpret_cast<const bf16x8*>(q_lds + lds_off<CPR>(l32, 2 * ks + g)), kop[ks], s);
+    for (int i = 0; i < kWTiles; ++i) {
+      if (i >= per_wave) break;   // uniform
+      bf16x8 kop[KS];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_lds + 8 * x + 4 * g);
+      for (int ks = 0; ks < KS; ++ks) kop[ks] = next[ks];
+      if (i + 1 < per_wave) load(next, tile_key(i + 1));
+      const int k = tile_key(i), key = k + l32;
+      if (!seen(k)) continue;     // uniform
+      // every row sees every key of the tile, whatever its place in the chunk or tree
+      const bool whole = k + 32 <= off && (k >= off + sm.nq - a.left || k + 32 <= a.sinks);
+      for (int r = 0; r < n; r += 32) {
+        f32x16 s = f32x16{};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = fast_exp2(__builtin_fmaf(s[4 * x + e], c2, -ls[e]));
-          if (whole) {   // uniform
-            sum += p;
-          } else {
-            const int r = 8 * x + 4 * g + e, pos = p_lds[r], end = a.tree ? off : pos + 1;
-            const bool in = (key < end && (key >= pos - a.left || key < a.sinks)) ||
-                            (a.tree && key >= off && key < sm.nk && (tree_lds[r] >> (key - off) & 1));
-            sum += in ? p : 0.f;
+        for (int ks = 0; ks < KS; ++ks)
+          s = mfma32(*reinterpret_cast<const bf16x8*>(q_lds + lds_off<CPR>(r + l32, 2 * ks + g)), kop[ks], s);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_lds + r + 8 * x + 4 * g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = fast_exp2(__builtin_fmaf(s[4 * x + e], c2, -ls[e]));
+            if (whole) {   // uniform
+              sum[i] += p;
+            } else {
+              const int row = r + 8 * x + 4 * g + e, pos = p_lds[row], end = a.tree ? off : pos + 1;
+              const bool in = (key < end && (key >= pos - a.left || key < a.sinks)) ||
+                              (a.tree && key >= off && key < sm.nk && (tree_lds[row] >> (key - off) & 1));
+              sum[i] += in ? p : 0.f;
+            }
           }
         }
       }
     }
   }
-  sum = pair_sum(sum);
-  if (g == 0 && key < a.Nk) c.out[at] = (c.in ? c.in[at] : 0.f) + sum;
+#pragma unroll
+  for (int i = 0; i < kWTiles; ++i) {
+    if (i >= per_wave) break;
+    const int key = tile_key(i) + l32;
+    const float x = pair_sum(sum[i]);
+    const int64_t at = ((int64_t)b * a.Hk + hk) * a.Nk + key;
+    if (g == 0 && key < a.Nk) c.out[at] = (c.in ? c.in[at] : 0.f) + x;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -140,10 +174,7 @@ __global__ __launch_bounds__(64 * kEvictWaves) void cache_select_kernel(const Ca
   if (tid == 0 && row % a.Hk == 0) a.len_out[b] = count;
   for (int i = count + tid; i < a.keep; i += 64 * W) idx[i] = -1;
   for (int i = count + tid; i < a.cap_out; i += 64 * W) wo[i] = 0.f;
-  auto put = [&](int place, int slot) __attribute__((always_inline)) {
-    idx[place] = slot;
-    wo[place] = wt[slot];
-  };
+  auto put = [&](int place, int slot) __attribute__((always_inline)) { idx[place] = slot; };
   if (n <= a.keep) {   // uniform
     for (int i = tid; i < n; i += 64 * W) put(i, i);
     return;
@@ -218,8 +249,9 @@ __global__ __launch_bounds__(64 * kEvictWaves) void cache_select_kernel(const Ca
   });
 }
 
-// Rows of K and V to their places, 16 bytes a thread of each; rows behind the kept ones 0
-// up to `rows`.
+// Rows of K and V to their places, 16 bytes a thread of each, and the slots' weights
+// (written beside the selection they would wait for a load each: 23 us in place of 10);
+// rows behind the kept ones 0 up to `rows`.
 __global__ __launch_bounds__(256) void cache_move_kernel(const CacheEvict a, const int rows) {
   const int per = a.Hk * a.D / 8, b = blockIdx.y;
   const int count = min(min(max(x_cu(a.lens, b), 0), a.cap), a.keep);
@@ -236,7 +268,10 @@ __global__ __launch_bounds__(256) void cache_move_kernel(const CacheEvict a, con
       to_k[u] = ((int64_t)b * a.cap_out + place) * a.sko + col;
       to_v[u] = ((int64_t)b * a.cap_out + place) * a.svo + col;
       if (i < total && place < count) {
-        const int64_t slot = (int64_t)b * a.cap + a.idx[((int64_t)b * a.Hk + hk) * a.keep + place];
+        const int64_t row = (int64_t)b * a.Hk + hk;
+        const int from = a.idx[row * a.keep + place];
+        if (col == hk * a.D) a.weights_out[row * a.cap_out + place] = a.weights[row * a.cap + from];
+        const int64_t slot = (int64_t)b * a.cap + from;
         k[u] = __builtin_nontemporal_load(
             reinterpret_cast<const u32x4*>(static_cast<const __bf16*>(a.k) + slot * a.sk + col));
         v[u] = __builtin_nontemporal_load(
@@ -255,11 +290,14 @@ __global__ __launch_bounds__(256) void cache_move_kernel(const CacheEvict a, con
 }  // namespace
 
 hipError_t launch_cache_weights(const XArgs& a, const CacheWeights& c, hipStream_t s) {
-  const int64_t chunks = ((int64_t)a.Nk + kWKeys - 1) / kWKeys;
+  // as many tiles a wave as leave a workgroup for each place on the chip
+  const int64_t heads = (int64_t)a.B * a.Hk, blocks = ((int64_t)a.Nk + 127) / 128;
+  const int per_wave = (int)std::max<int64_t>(1, std::min<int64_t>(kWTiles, (heads * blocks + 767) / 768));
+  const int64_t chunks = ((int64_t)a.Nk + 128 * per_wave - 1) / (128 * per_wave);
   TraceScope ts_(s, "cache_weights", x_padded(a));
-  const dim3 grid((unsigned)(a.B * a.Hk * chunks));
-  if (a.D <= 64) hipLaunchKernelGGL(cache_weights_kernel<64>, grid, dim3(256), 0, s, a, c);
-  else hipLaunchKernelGGL(cache_weights_kernel<128>, grid, dim3(256), 0, s, a, c);
+  const dim3 grid((unsigned)(heads * chunks));
+  if (a.D <= 64) hipLaunchKernelGGL(cache_weights_kernel<64>, grid, dim3(256), 0, s, a, c, per_wave);
+  else hipLaunchKernelGGL(cache_weights_kernel<128>, grid, dim3(256), 0, s, a, c, per_wave);
   return hipGetLastError();
 }
 

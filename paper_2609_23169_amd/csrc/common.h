@@ -227,6 +227,7 @@ struct XArgs {
   // tree: which of the last Nq a query sees, a bit each, in place of those up to its own.
   const int32_t* lens;
   const uint64_t* tree;
+  bool scores;                     // the forward leaves its scores for the slots' weights
 };
 constexpr int kXMaxWindow = 1 << 29;   // wider windows are the same: positions stay below 2^28
 // Bytes of the partial results where the keys (forward, dQ) or the query tokens
@@ -238,13 +239,20 @@ bool xattn_bwd_launchable(const XArgs& a);
 size_t xattn_bwd_workspace(const XArgs& a);
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s);
 
-// ---- Weights received by a cache's slots, and eviction (cache.hip) ----
+// ---- A cache: attention with the slots' weights (xattn_fwd.hip), eviction (cache.hip) ----
 struct CacheWeights {
   const float* in;          // [B, Hk, Nk], or null: zeros
   float* out;
   const uint64_t* tokens;   // [B] which of the Nq tokens count, a bit each, or null: all
 };
-// a: q, k, lse, a cache (lens).
+// Up to so many rows of a key head (tokens times heads of the group) the forward keeps
+// its scores, 4 bytes a row and key against the 2 D of the key's own row, and the
+// weights need no second pass over the keys.
+constexpr int kScoreRows = 32;
+size_t cache_attn_workspace(const XArgs& a);
+// w.out null: no weights wanted. a: q, k, v, o, lse, a cache (lens).
+hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* workspace, hipStream_t s);
+// The weights alone, from q, k and lse.
 hipError_t launch_cache_weights(const XArgs& a, const CacheWeights& c, hipStream_t s);
 struct CacheEvict {
   const void *k, *v;

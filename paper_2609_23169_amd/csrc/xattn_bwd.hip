@@ -320,7 +320,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       char* const lds1 = (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
       if (have) finish(seq.item(seq.cur, order), lds0, lds1);
       const XItem at = seq.item(seq.at, order);
-      seq.cur = seq.at;
+      seq.keep();
       if (more) {
         row_stats(ex, lds0);
         const XTurn<DP> rows(x_lane_again());

@@ -45,11 +45,16 @@ constexpr float kSumGuard = 18446744073709551616.0f;   // 2^64: per-lane tile su
 
 // Partial results of split s: sums[s][stat] = {maximum (log2 units), sum} and
 // O[s][stat][D], stat a row's index in the LSE tensor.
+// A cache call: how the items are cut (cache_share) and the scores, in log2
+// units, -inf where a row does not see the key: [b][hk][row][Nk up to whole tiles].
 struct Parts {
   float2* sums;
   float* o;
   int64_t stats;
+  int* cuts;
+  float* scores;
 };
+inline __host__ __device__ int score_keys(const XArgs& a) { return (a.Nk + kXKeys - 1) / kXKeys * kXKeys; }
 
 template <int DP, int NW, bool SPLIT, int SEE>
 __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_fwd_kernel(const XArgs a, const XOrder order,
@@ -59,6 +64,10 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   __shared__ __attribute__((aligned(1024))) char k_lds1[TILEB];
   __shared__ __attribute__((aligned(1024))) char v_lds0[TILEB];
   __shared__ __attribute__((aligned(1024))) char v_lds1[TILEB];
+  // Rows are turned in a wave's own part of a consumed stage; eight waves have too little.
+  constexpr int TURNB = 32 * ROWB;
+  constexpr bool OWN = 2 * TILEB < NW * TURNB;
+  __shared__ __attribute__((aligned(1024))) char turn_lds[OWN ? NW * TURNB : 16];
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g = lane >> 5, c16 = lane & 15, gq = lane >> 4;
@@ -97,7 +106,8 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
   float m_run = 0.f, l_run = 0.f;
   bool fresh = true;                   // no key of the item seen yet: no reference (uniform)
 
-  TileSeq<SEE> seq;
+  constexpr bool kShare = SEE == kSeeCache && SPLIT;
+  std::conditional_t<kShare, CacheSeq, TileSeq<SEE>> seq;
   RowWindow<SEE> see{};                // the lane's row, unless all is seen
 
   // One tile in two 32-key halves, so that a wave's vector work has matrix work of
@@ -155,6 +165,20 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[h][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[h][e] : -INFINITY;
       }
+      if constexpr (SEE == kSeeCache && (NW == 1 || !SPLIT))
+        if (a.scores && bits) {   // uniform
+          const XArgs& x = *x_args_again();
+          const XItem at = seq.item(seq.cur, order);
+          const int row = 32 * w + l32, rows = x.Nq * x.G;
+          if (row < rows) {
+            float* const to = parts.scores + (((int64_t)at.b * x.Hk + at.hk) * rows + row) * score_keys(x) +
+                              kXKeys * tile + 32 * h + 4 * g;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              *reinterpret_cast<f32x4*>(to + 8 * c) =
+                  f32x4{s[h][4 * c], s[h][4 * c + 1], s[h][4 * c + 2], s[h][4 * c + 3]} * c2;
+          }
+        }
       if (fresh && half) {   // uniform
         m_run = pair_max(half_max(h));
         fresh = false;
@@ -307,7 +331,11 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
 
   // A workgroup's items in turn, their tiles as one sequence: a tile's loads are
   // issued while the tile before it is worked on, across items too.
-  seq.begin(x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk));
+  if constexpr (kShare)
+    seq.begin(cache_share(a, (int)blockIdx.x, (int)gridDim.x, a.Hk * (int)order.tiles,
+                          blockIdx.x == 0 && w == 0 ? parts.cuts : nullptr));
+  else
+    seq.begin(x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk));
   bool have = false;   // a tile lies in the current stage
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
@@ -346,18 +374,19 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     if (changed) {
       // through the wave's part of the consumed stage; the stores end beside the
       // next item's first tile
-      char* const lds0 = (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
-      char* const lds1 = (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
+      char* const lds0 = OWN ? turn_lds + w * TURNB : (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
+      char* const lds1 = OWN ? lds0 + TURNB / 2 : (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
       if (have) finish(seq.item(seq.cur, order), lds0, lds1);
       if (more) {
         XTurn<DP>(x_lane_again()).turn(qop, lds0, lds1);
         if constexpr (SEE != kSeeAll) {
           const XArgs& x = *x_args_again();
           const XItem at = seq.item(seq.at, order);
-          see.open(x, x_sample<SEE>(x, at.b), at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
+          const XSample sm = x_sample<SEE>(x, at.b);
+          see.open(x, sm, at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
         }
       }
-      seq.cur = seq.at;
+      seq.keep();
       m_run = l_run = 0.f;
       fresh = true;
 #pragma unroll
@@ -440,6 +469,120 @@ __global__ __launch_bounds__(256) void xattn_join_kernel(const XArgs a, const in
   }
 }
 
+// The end of a cache call: the parts of its rows joined, as above (SPLIT), and with
+// scores the weights that the slots receive, a workgroup 256 slots of a key head: a
+// row's maximum and sum come from its parts again, or from its LSE.
+template <int GPR, bool SPLIT>
+__global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const int tiles, const int rows_per_item,
+                                                           const int joins, const Parts parts, const CacheWeights wt) {
+  __shared__ float4 red[256];
+  __shared__ float red_l[8];
+  // Parts of sample b's item g.
+  auto count = [&](int b, int g) __attribute__((always_inline)) {
+    return cache_parts(parts.cuts[0], parts.cuts[1 + b], cache_tiles(a, b), g);
+  };
+  if (SPLIT && (int)blockIdx.x < joins) {
+    constexpr int kRows = 8 / GPR;
+    const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, sub = grp % GPR;
+    const int64_t r = (int64_t)blockIdx.x * kRows + grp / GPR;   // [B, Hq, T]
+    const bool live = r < parts.stats;
+    int64_t tok = 0;
+    int head = 0, splits = 0;
+    if (live) {
+      const int64_t bh = r / a.Nq;
+      const int b = (int)(bh / a.Hq), t = (int)(r - bh * a.Nq);
+      head = (int)(bh - (int64_t)b * a.Hq);
+      tok = (int64_t)b * a.Nq + t;
+      const int hk = head / a.G;
+      splits = count(b, hk * tiles + (t * a.G + head - hk * a.G) / rows_per_item);
+    }
+    float M = -INFINITY;
+    for (int s = lane; s < splits; s += 32) {
+      const float2 p = parts.sums[s * parts.stats + r];
+      M = p.y != 0.f ? fmaxf(M, p.x) : M;
+    }
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) M = fmaxf(M, __shfl_xor(M, m, 64));
+    float L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int s = sub; s < splits; s += GPR) {
+      const float2 p = parts.sums[s * parts.stats + r];
+      if (p.y == 0.f) continue;   // no keys in use here
+      const float f = fast_exp2(p.x - M);
+      L += p.y * f;
+      if (4 * lane < a.D) {
+        const float4 o = *reinterpret_cast<const float4*>(parts.o + (s * parts.stats + r) * a.D + 4 * lane);
+        acc.x += o.x * f, acc.y += o.y * f, acc.z += o.z * f, acc.w += o.w * f;
+      }
+    }
+    if constexpr (GPR > 1) {
+      red[threadIdx.x] = acc;
+      if (lane == 0) red_l[grp] = L;
+      __syncthreads();
+      if (sub == 0)
+        for (int k = 1; k < GPR; ++k) {
+          const float4 o = red[threadIdx.x + 32 * k];
+          acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
+          L += red_l[grp + k];
+        }
+    }
+    if (!live || sub != 0) return;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    if (lane == 0) a.lse[r] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
+    if (4 * lane < a.D) {
+      const bf16x4 v = {(__bf16)(acc.x * inv), (__bf16)(acc.y * inv), (__bf16)(acc.z * inv), (__bf16)(acc.w * inv)};
+      *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.o) + tok * a.so + head * a.D + 4 * lane) = v;
+    }
+    return;
+  }
+  // Weights of 256 slots. rows <= kScoreRows, so an item holds all of them.
+  float* const lse2 = reinterpret_cast<float*>(red);
+  const unsigned at = blockIdx.x - (SPLIT ? joins : 0), chunks = (unsigned)((a.Nk + 255) / 256);
+  const unsigned bh = at / chunks;
+  const int b = (int)(bh / (unsigned)a.Hk), hk = (int)(bh - b * a.Hk), rows = a.Nq * a.G;
+  const int key = (int)(at - bh * chunks) * 256 + threadIdx.x;
+  const float* const sc = parts.scores + (int64_t)bh * rows * score_keys(a) + key;
+  const int row = threadIdx.x >> 3, sub = threadIdx.x & 7;   // eight lanes a row
+  if (row < rows) {
+    const int t = row / a.G, head = hk * a.G + row - t * a.G;
+    const int64_t r = ((int64_t)b * a.Hq + head) * a.Nq + t;
+    float m = -INFINITY, l = 0.f;
+    if constexpr (SPLIT) {
+      const int n = count(b, hk);
+      for (int s = sub; s < n; s += 8) {
+        const float2 p = parts.sums[s * parts.stats + r];
+        if (p.y == 0.f) continue;   // no keys in use here
+        const float to = fmaxf(m, p.x);
+        l = l * fast_exp2(m - to) + p.y * fast_exp2(p.x - to);
+        m = to;
+      }
+#pragma unroll
+      for (int x = 1; x < 8; x <<= 1) {
+        const float mo = __shfl_xor(m, x, 64), lo = __shfl_xor(l, x, 64), to = fmaxf(m, mo);
+        l = (l == 0.f ? 0.f : l * fast_exp2(m - to)) + (lo == 0.f ? 0.f : lo * fast_exp2(mo - to));
+        m = to;
+      }
+      m += __log2f(l);
+    } else {
+      m = a.lse[r] * kLog2e;
+    }
+    if (sub == 0) lse2[row] = m == -INFINITY || m != m ? INFINITY : m;   // no keys: P = 0
+  }
+  __syncthreads();
+  if (key >= a.Nk) return;
+  const XSample sm = x_sample<kSeeCache>(a, b);
+  const XSpan span = x_span<kSeeCache>(a, sm, 0, rows);
+  const int tile = key / kXKeys, last = span.skip + span.count;   // of the list, as tile numbers
+  float sum = 0.f;
+  if (tile < span.first || (tile >= span.first + span.skip && tile < last)) {
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r) sum += fast_exp2(sc[(int64_t)r * score_keys(a)] - lse2[r]);
+  }
+  const int64_t to = (int64_t)bh * a.Nk + key;
+  wt.out[to] = (wt.in ? wt.in[to] : 0.f) + sum;
+}
+
 // Parts of the keys, and waves of a workgroup: four, or one where up to 32 rows meet
 // split keys (4 rows of 4 x 8 key heads on 16,391 keys: 49 us against 51 with three
 // idle waves beside; unsplit keys the other way round, 14.2 against 13.0 for 16
@@ -449,6 +592,15 @@ struct Shape {
   int splits, waves;
 };
 Shape fwd_shape(const XArgs& a) {
+  if (a.lens) {   // shared out by cache_share where the items would not fill the chip
+    const int64_t rows = (int64_t)a.Nq * a.G, heads = (int64_t)a.B * a.Hk;
+    const int waves = rows <= 32 ? 1 : rows <= 128 || a.D <= 64 ? 4 : 8, wgs = (int)x_resident(x_padded(a), waves);
+    const int64_t groups = (int64_t)a.Hk * ((rows + 32 * waves - 1) / (32 * waves));
+    const int64_t tiles = x_item_tiles(a, (int)std::min<int64_t>(rows, INT32_MAX));
+    if (a.B * groups >= wgs || tiles < 2 * kPartTiles || heads == 0) return Shape{1, 4};
+    // parts of an item, at most: of its tiles by what a workgroup takes, and one more
+    return Shape{(int)std::min((tiles + kPartTiles - 1) / kPartTiles, (wgs + groups - 1) / groups) + 1, waves};
+  }
   const int64_t rows = (int64_t)a.Nq * a.G, heads = (int64_t)a.B * a.Hk;
   auto splits = [&](int nw) {
     const int64_t groups = heads * ((rows + 32 * nw - 1) / (32 * nw)), tiles = x_item_tiles(a, 32 * nw);
@@ -463,7 +615,9 @@ template <int DP, int NW, int SEE>
 void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
   const XOrder order{head_group(a), (unsigned)(((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW)), (unsigned)splits};
   const int64_t items = (int64_t)a.B * a.Hk * order.tiles * splits;
-  const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, NW)) + 7) / 8 * 8);
+  const dim3 grid(SEE == kSeeCache && splits > 1
+                      ? (unsigned)x_resident(DP, NW)
+                      : (unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, NW)) + 7) / 8 * 8);
   static const char* const names[][2] = {
       {"xattn_fwd", "xattn_fwd_split"}, {"swattn_fwd", "swattn_fwd_split"}, {"cache_fwd", "cache_fwd_split"}};
   TraceScope ts_(s, names[SEE][splits > 1], DP, NW);
@@ -476,6 +630,8 @@ void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
 }
 template <int SEE>
 void launch_fwd(const XArgs& a, int splits, int waves, const Parts& parts, hipStream_t s) {
+  if constexpr (SEE == kSeeCache)
+    if (waves == 8) return launch_fwd<128, 8, SEE>(a, splits, parts, s);
   if (a.D <= 64)
     waves == 1 ? launch_fwd<64, 1, SEE>(a, splits, parts, s) : launch_fwd<64, 4, SEE>(a, splits, parts, s);
   else
@@ -504,8 +660,7 @@ hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s) {
     parts.o = static_cast<float*>(workspace);
     parts.sums = reinterpret_cast<float2*>(parts.o + (size_t)splits * parts.stats * a.D);
   }
-  if (a.lens) launch_fwd<kSeeCache>(a, splits, waves, parts, s);
-  else if (a.window) launch_fwd<kSeeWindow>(a, splits, waves, parts, s);
+  if (a.window) launch_fwd<kSeeWindow>(a, splits, waves, parts, s);
   else launch_fwd<kSeeAll>(a, splits, waves, parts, s);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   // Eight groups of lanes a row where many parts are to be read for few rows: 320 rows
@@ -514,6 +669,58 @@ hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s) {
   if (splits > 1)
     splits >= 8 && parts.stats <= 4096 ? launch_join<8>(a, splits, parts, s) : launch_join<1>(a, splits, parts, s);
   return hipGetLastError();
+}
+
+// Workspace of a cache call: the parts' O and sums, how items are cut, the scores.
+namespace {
+struct CacheSpace {
+  size_t o, sums, cuts, scores;   // bytes
+};
+CacheSpace cache_space(const XArgs& a) {
+  const int splits = fwd_shape(a).splits;
+  CacheSpace c{};
+  if (splits > 1) {
+    c.o = (size_t)splits * stats_of(a) * a.D * sizeof(float);
+    c.sums = (size_t)splits * stats_of(a) * sizeof(float2);
+    c.cuts = ((size_t)a.B + 1 + 3) / 4 * 4 * sizeof(int);
+  }
+  if (a.scores) c.scores = (size_t)a.B * a.Hq * a.Nq * score_keys(a) * sizeof(float);
+  // 16-byte pieces: sums and starts end on one
+  c.sums = (c.sums + 15) / 16 * 16;
+  return c;
+}
+}  // namespace
+
+size_t cache_attn_workspace(const XArgs& a) {
+  const CacheSpace c = cache_space(a);
+  return c.o + c.sums + c.cuts + c.scores;
+}
+
+hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* workspace, hipStream_t s) {
+  const auto [splits, waves] = fwd_shape(a);
+  const CacheSpace c = cache_space(a);
+  char* const at = static_cast<char*>(workspace);
+  const Parts parts{reinterpret_cast<float2*>(at + c.o), reinterpret_cast<float*>(at), stats_of(a),
+                    reinterpret_cast<int*>(at + c.o + c.sums), reinterpret_cast<float*>(at + c.o + c.sums + c.cuts)};
+  launch_fwd<kSeeCache>(a, splits, waves, parts, s);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  const bool many = splits >= 8 && parts.stats <= 4096;   // as xattn_join
+  const int64_t joins = splits > 1 ? (parts.stats + (many ? 0 : 7)) / (many ? 1 : 8) : 0;
+  const int64_t chunks = a.scores ? (int64_t)a.B * a.Hk * (((int64_t)a.Nk + 255) / 256) : 0;
+  if (joins + chunks > 0) {
+    TraceScope ts_(s, "cache_finish");
+    const int rows = 32 * waves;
+    const int tiles = (int)(((int64_t)a.Nq * a.G + rows - 1) / rows);
+    const dim3 grid((unsigned)(joins + chunks));
+    if (splits == 1)
+      hipLaunchKernelGGL((cache_finish_kernel<1, false>), grid, dim3(256), 0, s, a, tiles, rows, 0, parts, w);
+    else if (many)
+      hipLaunchKernelGGL((cache_finish_kernel<8, true>), grid, dim3(256), 0, s, a, tiles, rows, (int)joins, parts, w);
+    else
+      hipLaunchKernelGGL((cache_finish_kernel<1, true>), grid, dim3(256), 0, s, a, tiles, rows, (int)joins, parts, w);
+  }
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  return w.out && !a.scores ? launch_cache_weights(a, w, s) : hipSuccess;
 }
 
 }  // namespace ut

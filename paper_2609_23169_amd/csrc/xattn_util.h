@@ -71,7 +71,7 @@ inline unsigned head_group(const XArgs& a) { return a.Hk % 8 == 0 ? (unsigned)a.
 // Workgroups of nw waves that fit 256 CUs at once, by LDS (64 KB at 128 columns, 32
 // to 36 at 64) and by registers (two waves a SIMD at 128 columns, three at 64): what
 // a grid needs to fill the chip.
-constexpr int64_t x_resident(int DP, int nw) { return 256 * (DP == 128 ? 2 : nw == 4 ? 3 : 4); }
+constexpr int64_t x_resident(int DP, int nw) { return 256 * (nw == 8 ? 1 : DP == 128 ? 2 : nw == 4 ? 3 : 4); }
 // Most key tiles of an item of `rows` rows.
 inline int64_t x_item_tiles(const XArgs& a, int rows) {
   const int64_t all = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
@@ -223,10 +223,12 @@ __device__ inline XSpan x_span(const XArgs& a, const XSample& sm, int r0, int n)
   const bool tree = SEE == kSeeCache && a.tree;
   const int off = sm.nk - sm.nq, right = SEE == kSeeCache ? 0 : a.right;
   const int p0 = off + row_token(r0, a.G), p1 = off + row_token(min(r0 + n, sm.nq * a.G) - 1, a.G);
+  // uniform, kept in scalar registers
+  auto u = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
   XSpan s;
-  s.lo = max(0, (tree ? off : p0) - a.left);
-  s.hi = tree ? sm.nk : max(0, min(sm.nk, p1 + right + 1));
-  s.send = max(0, min(min(a.sinks, sm.nk), tree ? off : right > 0 ? sm.nk : p1 + 1));
+  s.lo = u(max(0, (tree ? off : p0) - a.left));
+  s.hi = u(tree ? sm.nk : max(0, min(sm.nk, p1 + right + 1)));
+  s.send = u(max(0, min(min(a.sinks, sm.nk), tree ? off : right > 0 ? sm.nk : p1 + 1)));
   s.first = (s.send + kXKeys - 1) / kXKeys;
   const int w0 = max(s.first, s.lo / kXKeys), w1 = s.lo < s.hi ? (s.hi + kXKeys - 1) / kXKeys : 0;
   s.skip = w0 - s.first;
@@ -331,6 +333,8 @@ struct TileSeq {
     at = cur = kKept;
     fresh = false;
   }
+  // The item of the last tile given becomes the caller's.
+  __device__ inline void keep() { cur = at; }
   // Item of lane i.
   __device__ inline XItem item(int i, const XOrder& order) const {
     const int hp = __builtin_amdgcn_readlane(hkpart, i);
@@ -422,6 +426,152 @@ struct TileSeq {
       count += __builtin_popcountll(t.left);
     }
     return count == 1;
+  }
+};
+
+// The tiles of a cache call whose keys are split, shared out evenly among n workgroups:
+// lengths are known on the device only, and samples of any lengths are to keep all busy
+// to the end. An item (sample, key head, tile of rows) of t tiles of keys is cut into
+// parts of `per`, the least that n workgroups can take one each of. Where that leaves
+// many idle, the tiles of all items in a row are cut at every `per`-th: a workgroup then
+// begins within an item, has whole ones perhaps and ends within one (a change of item
+// costs about as much as two tiles: 8 samples of 66 tiles 28.7 us one each, 32.6 cut).
+constexpr int kPartTiles = 4;   // of a workgroup, at least
+struct CacheShare {
+  int b, g;               // its first item: sample, and key head and tile of rows
+  int t0, t1;             // first tile of the first item, end of the last one's
+  int items, part;        // part: of the first item
+};
+// Tiles of keys that sample b's rows see together.
+__device__ inline int cache_tiles(const XArgs& a, int b) {
+  const int used = min(max(a.lens[b], 0), a.Nk - a.Nq), nk = used + a.Nq;   // as x_sample
+  const int first = (min(a.sinks, a.tree ? used : nk) + kXKeys - 1) / kXKeys;
+  return first + max(0, (nk + kXKeys - 1) / kXKeys - max(first, max(0, used - a.left) / kXKeys));
+}
+// How the items are cut, as the launches that join the parts need it: `per`, negative
+// for one row, and there the samples' first tiles in the row.
+__device__ inline int cache_parts(int per, int start, int n, int g) {
+  if (per > 0) return (n + per - 1) / per;
+  const int x = start + g * n;
+  return (x + n - 1) / -per - x / -per + 1;
+}
+// cuts: per and the samples' starts, or null; each sample has `groups` items.
+__device__ inline CacheShare cache_share(const XArgs& a, int wg, int wgs, int groups, int* cuts) {
+  const int lane = threadIdx.x & 63, n0 = lane < a.B ? cache_tiles(a, lane) : 0;
+  auto tiles_of = [&](int b0) __attribute__((always_inline)) {   // of sample b0 + lane
+    return b0 == 0 ? n0 : b0 + lane < a.B ? cache_tiles(a, b0 + lane) : 0;
+  };
+  auto sum_of = [&](auto f) __attribute__((always_inline)) {
+    int total = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {   // uniform
+      int x = f(tiles_of(b0));
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m, 64);
+      total += x * groups;
+    }
+    return __builtin_amdgcn_readfirstlane(total);
+  };
+  const int total = sum_of([](int n) { return n; });
+  const int even = max((total + wgs - 1) / wgs, kPartTiles);
+  int per = even;
+  bool row = true;
+  for (int i = 0; i < 3 && row; ++i) {   // up to an eighth more than an even share
+    const int to = even + i * ((even + 15) / 16);
+    if (sum_of([to](int n) { return (n + to - 1) / to; }) <= wgs) per = to, row = false;
+  }
+  const int x0 = row ? wg * per : wg, x1 = row ? min(x0 + per, total) - 1 : wg;
+  CacheShare s{0, 0, 0, 0, 0, 0};
+  int first = -1, last = 0, at = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int n = tiles_of(b0), units = row ? n : (n + per - 1) / per;
+    int end = units * groups;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int y = __shfl_up(end, m, 64);
+      end += lane >= m ? y : 0;
+    }
+    end += at;
+    const int start = end - units * groups;
+    if (cuts && b0 + lane < a.B) cuts[1 + b0 + lane] = start;
+    if (const uint64_t here = __ballot(x0 >= start && x0 < end)) {   // the sample of x0
+      const int i = __builtin_ctzll(here), st = __builtin_amdgcn_readlane(start, i),
+                un = __builtin_amdgcn_readlane(units, i), g = (x0 - st) / un, r = x0 - st - g * un;
+      s.b = b0 + i, s.g = g;
+      s.t0 = row ? r : r * per;
+      s.part = row ? wg - (x0 - r) / per : r;
+      if (!row) s.t1 = min(s.t0 + per, __builtin_amdgcn_readlane(n, i));
+      first = (b0 + i) * groups + g;
+      last = max(last, first);
+    }
+    if (row)
+      if (const uint64_t here = __ballot(x1 >= start && x1 < end)) {
+        const int i = __builtin_ctzll(here), st = __builtin_amdgcn_readlane(start, i),
+                  un = __builtin_amdgcn_readlane(units, i), g = (x1 - st) / un;
+        s.t1 = x1 - st - g * un + 1;
+        last = (b0 + i) * groups + g;
+      }
+    at = __builtin_amdgcn_readlane(end, 63);
+  }
+  if (cuts && lane == 0) cuts[0] = row ? -per : per;
+  s.items = first < 0 ? 0 : last - first + 1;
+  // uniform, to be kept in scalar registers
+  auto u = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
+  return CacheShare{u(s.b), u(s.g), u(s.t0), u(s.t1), u(s.items), u(s.part)};
+}
+
+// TileSeq for such a share.
+struct CacheSeq {
+  KeyTiles<kSeeCache> tiles;
+  CacheShare share;        // b, g, t0, part: of the item of the last tile given
+  bool first;              // that item is the share's first one
+  XItem next_item, cur_item;
+  int at, cur;             // as TileSeq: the arguments of item()
+  int tile;
+  uint64_t bits;
+  bool fresh;
+  int64_t k0;
+  int hk;
+
+  __device__ inline void begin(const CacheShare& s) {
+    share = s;
+    --share.g;             // the first step leads there
+    tiles.open(nullptr, 0, 0, 0);
+    at = 1, cur = 0;
+    tile = hk = 0;
+    k0 = 0;
+    bits = 0;
+    first = true;
+    fresh = false;
+    next_item = cur_item = XItem{0, 0, 0, 0};
+  }
+  __device__ inline XItem item(int i, const XOrder&) const { return i ? next_item : cur_item; }
+  __device__ inline void keep() { cur_item = next_item; }
+  __device__ inline bool next(const XOrder& order, int rows_per_item, bool& changed) {
+    changed = false;
+    while (true) {
+      if (tiles.next(tile, bits)) break;
+      if (fresh) {   // the item ends in front of the share's part, or has no tiles
+        bits = 0;
+        break;
+      }
+      changed = true;
+      if (share.items == 0) return false;
+      const XArgs& x = *x_args_again();
+      if (++share.g == x.Hk * (int)order.tiles) share.g = 0, ++share.b;
+      const XSample sm = x_sample<kSeeCache>(x, share.b);
+      const int h = __builtin_amdgcn_readfirstlane(share.g / (int)order.tiles), t = share.g - h * (int)order.tiles;
+      tiles.span = x_span<kSeeCache>(x, sm, t * rows_per_item, rows_per_item);
+      tiles.open(nullptr, sm.nk, first ? share.t0 : 0,
+                 share.items == 1 ? min(share.t1, tiles.span.count) : tiles.span.count);
+      next_item = XItem{share.b, t, first ? share.part : 0, h};
+      --share.items;
+      first = false;
+      k0 = sm.k0;
+      hk = h;
+      fresh = true;
+    }
+    fresh = false;
+    return true;
   }
 };
 
@@ -558,7 +708,7 @@ struct TileLoad {
   static constexpr int RPI = 1024 / ROWB;                      // rows per instruction
   static constexpr int IPW = kXKeys * ROWB / 1024 / NW;        // instructions per wave
   static constexpr int REP = 16 / RPI;                         // instructions of 16 rows
-  static_assert(IPW % REP == 0, "a wave takes whole runs of 16 rows");
+  static constexpr bool RUNS = IPW % REP == 0;                 // a wave takes whole runs of 16 rows
   int row;      // bytes from the instruction's first row to this lane's
   int column;   // this lane's byte in it, instruction 0
 
@@ -569,6 +719,8 @@ struct TileLoad {
   // Instruction u's column: rows u RPI further on differ in the swizzle by u's
   // bits (CPR 16: rows 4 u + r, CPR 8: rows 8 u + r).
   static constexpr int flip(int u) { return CPR == 16 ? u << 4 : (4 * u) << 4; }
+  // The same of wave w, whose first instruction is another one of a run without RUNS.
+  __device__ static inline int turn(int w, int u) { return flip((RUNS ? u : w * IPW + u) % REP); }
 
   // A tile's descriptor, from its first key's row of this head.
   __device__ inline __amdgpu_buffer_rsrc_t tile(const __bf16* src, int stride) const {
@@ -582,7 +734,7 @@ struct TileLoad {
   __device__ inline void one(__amdgpu_buffer_rsrc_t rs, int stride, char* dst, int w, int u, int D) const {
     int first = column;
     if constexpr (FEW) pin_value(first);
-    const int i = w * IPW + u, c = first ^ flip(u % REP);
+    const int i = w * IPW + u, c = first ^ turn(w, u);
     int step = RPI * stride * 2;   // not kept in a register for each instruction
     UT_DEV_ASM("" : "+s"(step));
     buffer_load_lds16(rs, dst + i * 1024, c < 2 * D ? row + c : kXOut, i * step);
@@ -595,7 +747,7 @@ struct TileLoad {
     if constexpr (FEW) pin_value(first);
 #pragma unroll
     for (int u = 0; u < IPW; ++u) {
-      const int i = w * IPW + u, c = first ^ flip(u % REP);
+      const int i = w * IPW + u, c = first ^ turn(w, u);
       const unsigned run = (unsigned)(bits >> (i * RPI));   // scalar: this instruction's rows
       buffer_load_lds16(rs, dst + i * 1024, run >> (lane / CPR) & 1 && c < 2 * D ? row + c : kXOut,
                         i * RPI * stride * 2);
