@@ -27,7 +27,7 @@ OBJ = os.path.join(HERE, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["api.cpp", "trace.cpp", "btd.hip", "block_index.hip", "bsattn_fwd.hip", "bsattn_bwd.hip",
            "topk_mask.hip", "fg_step.hip", "composite.hip", "rope.hip",
-           "xattn_fwd.hip", "xattn_bwd.hip", "cache.hip"]
+           "xattn_fwd.hip", "xattn_bwd.hip", "cache.hip", "cache_one.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Wall", "-Wno-unused-function",

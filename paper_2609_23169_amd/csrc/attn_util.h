@@ -101,6 +101,28 @@ __device__ inline float quad_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The sum over a wave's lanes, in a scalar register.
+__device__ inline int wave_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);    // 1, 2, 4, 8 lanes down within rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // a row's last lane to the next row
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// The least over a wave's lanes, likewise.
+__device__ inline unsigned wave_min(unsigned x) {
+  x = min(x, (unsigned)__builtin_amdgcn_update_dpp(~0, (int)x, 0x111, 0xf, 0xf, false));
+  x = min(x, (unsigned)__builtin_amdgcn_update_dpp(~0, (int)x, 0x112, 0xf, 0xf, false));
+  x = min(x, (unsigned)__builtin_amdgcn_update_dpp(~0, (int)x, 0x114, 0xf, 0xf, false));
+  x = min(x, (unsigned)__builtin_amdgcn_update_dpp(~0, (int)x, 0x118, 0xf, 0xf, false));
+  x = min(x, (unsigned)__builtin_amdgcn_update_dpp(~0, (int)x, 0x142, 0xa, 0xf, false));
+  x = min(x, (unsigned)__builtin_amdgcn_update_dpp(~0, (int)x, 0x143, 0xc, 0xf, false));
+  return (unsigned)__builtin_amdgcn_readlane((int)x, 63);
+}
+
 // Two floats rounded to bf16 (nearest even) and packed, a in the low half.
 __device__ inline unsigned pack_bf16x2(float a, float b) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

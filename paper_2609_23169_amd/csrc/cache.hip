@@ -5,19 +5,24 @@
 // Weights: out[b, hk, j] = in[b, hk, j] + sum over the tokens t and the heads h of the
 // group of P = exp(S scale - LSE). The attention knows a row's LSE only at its end, so
 // this pass forms the scores again (of few rows the attention leaves them instead): a
-// workgroup keeps the rows of the group in LDS, up to 192 at once, a wave takes tiles of
-// 32 keys, whose rows pass through its registers, the next tile's loads beside the
-// products; S = Q K^T on 32x32x16 bf16 MFMA in the layout where a lane holds one key, so
-// that the sum over the rows is the lane's own but for one exchange. fp32 throughout, a
-// fixed order: no atomics.
+// workgroup keeps the rows of the group in LDS, up to 192 at once, and a wave takes tiles
+// of 32 keys: whole rows into its own part of LDS by direct loads (as operands, straight
+// from memory, an instruction touches 32 rows: twice the time), from there into
+// registers, the next tile's loads beside the products; S = Q K^T on 32x32x16 bf16 MFMA
+// in the layout where a lane holds one key, so that the sum over the rows is the lane's
+// own but for one exchange. fp32 throughout, a fixed order: no atomics.
 //
 // Eviction: of a row of weights the middle slots (behind the sinks, before the recent
-// ones) are bisected by value for the smallest weight that stays. A workgroup holds the
-// row in registers (up to 32,768 slots, longer rows are read again), a step is a
-// compare and a ballot a register and one barrier, and it ends as soon as the count
-// fits. Then ballots give every kept slot its place in ascending order, equal weights
-// the lowest slots first, and a second launch copies the rows of K and V.
+// ones) are searched by value for the smallest weight that stays: its order as an
+// unsigned number is bracketed, and the next number is taken where the counts at the
+// ends would have it on a straight line, every fourth time in the middle (that number
+// grows with the float's logarithm): some five steps leave 64 slots, which are ranked
+// against each other, where bisection took over twenty. A workgroup holds the row in registers (up to 32,768 slots,
+// longer rows are read again), a step is a compare and an add a register and one
+// barrier. Then ballots give every kept slot its place in ascending order, equal
+// weights the lowest slots first, and a second launch copies the rows of K and V.
 #include <algorithm>
+#include <type_traits>
 
 #include "xattn_util.h"
 
@@ -25,39 +30,49 @@ namespace ut {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kWRows = 192;   // rows in LDS: 48 KB at 128 columns, three workgroups a CU
-constexpr int kWTiles = 4;    // most tiles of 32 keys of a wave
+constexpr int kWWaves = 8;    // of a workgroup: at 128 columns 64 KB of keys and 48 KB of rows, one workgroup a CU
+constexpr int kWRows = 192;   // rows in LDS, a multiple of 64
+constexpr int kWTiles = 8;    // most tiles of 32 keys of a wave
 
 template <int DP>
-__global__ __launch_bounds__(256, 3) void cache_weights_kernel(const XArgs a, const CacheWeights c, const int per_wave) {
+__global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XArgs a, const CacheWeights c, const int per_wave) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, KS = DP / 16;
+  constexpr int KI = 32 * ROWB / 1024;   // direct loads of a tile
+  __shared__ __attribute__((aligned(1024))) char k_lds[kWWaves * 32 * ROWB];
   __shared__ __attribute__((aligned(16))) char q_lds[kWRows * ROWB];
   __shared__ __attribute__((aligned(16))) float lse_lds[kWRows];
   __shared__ int p_lds[kWRows];
   __shared__ uint64_t tree_lds[kWRows];
+  __shared__ unsigned see_lds[kWWaves][64];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned hk = blockIdx.x % (unsigned)a.Hk, rest = blockIdx.x / (unsigned)a.Hk;
-  const int keys = 128 * per_wave;   // of the workgroup
+  constexpr int T = 64 * kWWaves;
+  const int keys = 32 * kWWaves * per_wave;   // of the workgroup
   const unsigned chunks = (unsigned)((a.Nk + keys - 1) / keys);
   const int b = (int)(rest / chunks), key0 = (int)(rest % chunks) * keys;
   const XSample sm = x_sample<kSeeCache>(a, b);
   const int off = sm.nk - sm.nq, rows = sm.nq * a.G;
   const XSpan span = x_span<kSeeCache>(a, sm, 0, rows);
   const float c2 = a.scale * kLog2e;
-  // The wave's tiles: one of every four in turn. Whether some row sees keys from k on.
-  auto tile_key = [&](int i) __attribute__((always_inline)) { return key0 + 32 * (4 * i + w); };
+  // The wave's tiles: one of every eight in turn. Whether some row sees keys from k on.
+  auto tile_key = [&](int i) __attribute__((always_inline)) { return key0 + 32 * (kWWaves * i + w); };
   auto seen = [&](int k) __attribute__((always_inline)) {
     return (k < span.hi && k + 32 > span.lo) || k < span.send;
   };
-  auto load = [&](bf16x8 (&kop)[KS], int k) __attribute__((always_inline)) {
-    const __bf16* const kp =
-        static_cast<const __bf16*>(a.k) + (sm.k0 + min(k + l32, a.Nk - 1)) * a.sk + hk * a.D + 8 * g;
+  char* const k_mine = k_lds + w * 32 * ROWB;
+  int k_off[KI];   // row and column of this lane's piece of direct load i
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      kop[ks] = bf16x8{};
-      if (16 * ks + 8 * g < a.D) kop[ks] = *reinterpret_cast<const bf16x8*>(kp + 16 * ks);
-    }
+  for (int i = 0; i < KI; ++i) {
+    const int r = i * (1024 / ROWB) + lane / CPR, ch = lds_off<CPR>(r, lane % CPR) / 16 % CPR;
+    k_off[i] = 8 * ch < a.D ? r * a.sk * 2 + 16 * ch : kXOut;
+  }
+  auto load = [&](int k) __attribute__((always_inline)) {   // slots that the sample lacks read zeros
+    const int left = min(sm.nk - k, 32);
+    const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<const __bf16*>(a.k) + (sm.k0 + min(k, sm.nk - 1)) * a.sk + hk * a.D,
+                                                  left > 0 ? ((left - 1) * a.sk + a.D) * 2 : 0);
+#pragma unroll
+    for (int i = 0; i < KI; ++i) buffer_load_lds16(rs, k_mine + i * 1024, k_off[i]);
   };
   float sum[kWTiles];
 #pragma unroll
@@ -67,22 +82,18 @@ __global__ __launch_bounds__(256, 3) void cache_weights_kernel(const XArgs a, co
   for (int r0 = 0; any && r0 < rows; r0 += kWRows) {
     const int n = min(rows - r0, kWRows);
     if (r0 > 0) __syncthreads();
-    constexpr int kLoads = kWRows * CPR / 256;   // 16-byte pieces a thread, loaded together
+    constexpr int kLoads = kWRows * CPR / T;   // 16-byte pieces a thread, loaded together
     bf16x8 piece[kLoads];
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
-      const int i = u * 256 + tid, r = i / CPR, ch = i % CPR, tok = row_token(r0 + r, a.G);
+      const int i = u * T + tid, r = i / CPR, ch = i % CPR, tok = row_token(r0 + r, a.G);
       piece[u] = bf16x8{};
       if (r < n && 8 * ch < a.D)
         piece[u] = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + (sm.q0 + tok) * a.sq +
                                                     (hk * a.G + r0 + r - tok * a.G) * a.D + 8 * ch);
     }
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const int i = u * 256 + tid;
-      *reinterpret_cast<bf16x8*>(q_lds + lds_off<CPR>(i / CPR, i % CPR)) = piece[u];
-    }
-    if (tid < (n + 31) / 32 * 32) {
+    load(tile_key(0));
+    if (tid < (n + 63) / 64 * 64) {
       const int row = r0 + tid, tok = row_token(min(row, rows - 1), a.G);
       RowWindow<kSeeCache> see;
       see.open(a, sm, b, row);
@@ -96,42 +107,60 @@ __global__ __launch_bounds__(256, 3) void cache_weights_kernel(const XArgs a, co
       }
       lse_lds[tid] = l;
     }
-    bf16x8 next[KS];
-    load(next, tile_key(0));
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int i = u * T + tid;
+      *reinterpret_cast<bf16x8*>(q_lds + lds_off<CPR>(i / CPR, i % CPR)) = piece[u];
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kWTiles; ++i) {
       if (i >= per_wave) break;   // uniform
+      __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): the tile is there
       bf16x8 kop[KS];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kop[ks] = next[ks];
-      if (i + 1 < per_wave) load(next, tile_key(i + 1));
+      for (int ks = 0; ks < KS; ++ks) kop[ks] = *reinterpret_cast<const bf16x8*>(k_mine + lds_off<CPR>(l32, 2 * ks + g));
+      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): and read
+      pin_order();
+      if (i + 1 < per_wave) load(tile_key(i + 1));
       const int k = tile_key(i), key = k + l32;
       if (!seen(k)) continue;     // uniform
       // every row sees every key of the tile, whatever its place in the chunk or tree
       const bool whole = k + 32 <= off && (k >= off + sm.nq - a.left || k + 32 <= a.sinks);
-      for (int r = 0; r < n; r += 32) {
-        f32x16 s = f32x16{};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-          s = mfma32(*reinterpret_cast<const bf16x8*>(q_lds + lds_off<CPR>(r + l32, 2 * ks + g)), kop[ks], s);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_lds + r + 8 * x + 4 * g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = fast_exp2(__builtin_fmaf(s[4 * x + e], c2, -ls[e]));
-            if (whole) {   // uniform
-              sum[i] += p;
-            } else {
-              const int row = r + 8 * x + 4 * g + e, pos = p_lds[row], end = a.tree ? off : pos + 1;
-              const bool in = (key < end && (key >= pos - a.left || key < a.sinks)) ||
-                              (a.tree && key >= off && key < sm.nk && (tree_lds[row] >> (key - off) & 1));
-              sum[i] += in ? p : 0.f;
-            }
+      float add = 0.f;
+      auto walk = [&](auto all_seen) __attribute__((always_inline)) {
+        for (int r = 0; r < n; r += 64) {   // 64 rows, so that products and exponentials overlap
+          if constexpr (!decltype(all_seen)::value) {   // which of the keys a row sees, a lane a row
+            const int row = r + lane, p = p_lds[row];
+            const RowWindow<kSeeCache> see{p, a.tree ? off : p + 1, tree_lds[row]};
+            see_lds[w][lane] = see.bits(a, k) & bits32_from_to(0, sm.nk - k);
+            __builtin_amdgcn_wave_barrier();
           }
+          f32x16 s[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+              s[y] = mfma32(*reinterpret_cast<const bf16x8*>(q_lds + lds_off<CPR>(r + 32 * y + l32, 2 * ks + g)), kop[ks],
+                            s[y]);
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int row0 = r + 32 * y + 8 * x + 4 * g;
+              const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_lds + row0);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float p = fast_exp2(__builtin_fmaf(s[y][4 * x + e], c2, -ls[e]));
+                if constexpr (decltype(all_seen)::value) add += p;
+                else add += see_lds[w][row0 - r + e] >> l32 & 1 ? p : 0.f;
+              }
+            }
         }
-      }
+      };
+      if (whole) walk(std::true_type{});   // uniform
+      else walk(std::false_type{});
+      sum[i] += add;
     }
   }
 #pragma unroll
@@ -162,7 +191,7 @@ __device__ inline unsigned weight_key(float x) {
 template <int R>
 __global__ __launch_bounds__(64 * kEvictWaves) void cache_select_kernel(const CacheEvict a) {
   constexpr int W = kEvictWaves;
-  __shared__ unsigned cnt[2][W], cnt2[W];
+  __shared__ unsigned cnt[2][W], cnt2[W], ends[2][W], few[64], found;
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = blockIdx.x;
@@ -216,30 +245,67 @@ __global__ __launch_bounds__(64 * kEvictWaves) void cache_select_kernel(const Ca
     turn ^= 1;
     return t;
   };
-  // The largest t such that `need` slots or more have a key of t or above.
-  unsigned t = 0;
-  bool exact = false;   // just `need` have one
-  for (unsigned bit = 0x80000000u; bit != 0 && !exact; bit >>= 1) {   // uniform
-    const unsigned to = t | bit;
-    unsigned c = 0;
-    each([&](int, unsigned k) { c += __builtin_popcountll(__ballot(k >= to)); });
-    const unsigned all = total(c);
-    if (all >= (unsigned)need) t = to, exact = all == (unsigned)need;
+  // The least and the largest key bracket it: `need` slots or more have t or more, fewer
+  // have `to` or more (at_t and at_to of them).
+  unsigned lo = ~0u, hi = 0;
+  each([&](int at, unsigned k) {
+    lo = min(lo, at < end ? k : ~0u);
+    hi = max(hi, k);
+  });
+  lo = wave_min(lo);
+  hi = ~wave_min(~hi);
+  if (lane == 0) ends[0][w] = lo, ends[1][w] = hi;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < W; ++i) lo = min(lo, ends[0][i]), hi = max(hi, ends[1][i]);
+  unsigned long long t = lo, to = (unsigned long long)hi + 1;
+  unsigned at_t = m, at_to = 0;
+  for (int step = 1; at_t != (unsigned)need && to - t > 1 && at_t - at_to > 64; ++step) {   // uniform
+    const unsigned long long width = to - t;
+    unsigned long long by = width / 2;
+    if (step % 4 != 0)
+      by = (unsigned long long)((float)width * (((float)(at_t - need) + 0.5f) / (float)(at_t - at_to)));
+    const unsigned long long mid = t + (by < 1 ? 1 : by > width - 1 ? width - 1 : by);
+    const unsigned limit = (unsigned)mid;
+    int c = 0;
+    each([&](int, unsigned k) { c += k >= limit ? 1 : 0; });
+    const unsigned all = total((unsigned)wave_sum(c));
+    if (all >= (unsigned)need) t = mid, at_t = all;
+    else to = mid, at_to = all;
+  }
+  if (at_t != (unsigned)need && to - t > 1) {   // uniform: the last 64 or fewer, each against all others
+    if (tid == 0) found = 0;
+    __syncthreads();
+    each([&](int at, unsigned k) {
+      if (at < end && k >= (unsigned)t && k <= (unsigned)(to - 1)) few[atomicAdd(&found, 1u)] = k;   // values alone: any order
+    });
+    __syncthreads();
+    const unsigned n_few = at_t - at_to, mine = lane < (int)n_few ? few[lane] : 0u;
+    unsigned more = 0, same = 0;   // of them above the lane's, and equal to it
+    for (unsigned i = 0; i < n_few; ++i) {
+      more += few[i] > mine;
+      same += few[i] == mine;
+    }
+    // the one with which `need` is reached: at_to + more < need <= at_to + more + same
+    const bool is = lane < (int)n_few && at_to + more < (unsigned)need && (unsigned)need <= at_to + more + same;
+    t = (unsigned)__builtin_amdgcn_readlane((int)mine, __builtin_ctzll(__ballot(is)));
   }
   // Slots above t, and of those equal to it the first ones (behind the row's end keys
   // are 0: no slot, where t is 0).
-  unsigned over = 0, same = 0;
+  const unsigned least = (unsigned)t;
+  int over_mine = 0, same_mine = 0;
   each([&](int at, unsigned k) {
-    over += __builtin_popcountll(__ballot(k > t && at < end));
-    same += __builtin_popcountll(__ballot(k == t && at < end));
+    over_mine += k > least ? 1 : 0;
+    same_mine += k == least && at < end ? 1 : 0;
   });
+  const unsigned over = wave_sum(over_mine), same = wave_sum(same_mine);
   if (lane == 0) cnt2[w] = same;
   const unsigned above = total(over);   // its barrier covers cnt2 too
   unsigned before_over = 0, before_same = 0;
   for (int i = 0; i < w; ++i) before_over += cnt[turn ^ 1][i], before_same += cnt2[i];
   const unsigned ties = (unsigned)need - above;
   each([&](int at, unsigned k) {
-    const uint64_t o = __ballot(k > t && at < end), s = __ballot(k == t && at < end);
+    const uint64_t o = __ballot(k > least), s = __ballot(k == least && at < end);
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     const unsigned mo = before_over + __builtin_popcountll(o & below), ms = before_same + __builtin_popcountll(s & below);
     const bool in = (o >> lane & 1) || ((s >> lane & 1) && ms < ties);
@@ -290,14 +356,14 @@ __global__ __launch_bounds__(256) void cache_move_kernel(const CacheEvict a, con
 }  // namespace
 
 hipError_t launch_cache_weights(const XArgs& a, const CacheWeights& c, hipStream_t s) {
-  // as many tiles a wave as leave a workgroup for each place on the chip
-  const int64_t heads = (int64_t)a.B * a.Hk, blocks = ((int64_t)a.Nk + 127) / 128;
-  const int per_wave = (int)std::max<int64_t>(1, std::min<int64_t>(kWTiles, (heads * blocks + 767) / 768));
-  const int64_t chunks = ((int64_t)a.Nk + 128 * per_wave - 1) / (128 * per_wave);
+  // as many tiles a wave as leave a workgroup for each CU
+  const int64_t heads = (int64_t)a.B * a.Hk, keys = 32 * kWWaves, blocks = ((int64_t)a.Nk + keys - 1) / keys;
+  const int per_wave = (int)std::max<int64_t>(1, std::min<int64_t>(kWTiles, (heads * blocks + 255) / 256));
+  const int64_t chunks = ((int64_t)a.Nk + keys * per_wave - 1) / (keys * per_wave);
   TraceScope ts_(s, "cache_weights", x_padded(a));
   const dim3 grid((unsigned)(heads * chunks));
-  if (a.D <= 64) hipLaunchKernelGGL(cache_weights_kernel<64>, grid, dim3(256), 0, s, a, c, per_wave);
-  else hipLaunchKernelGGL(cache_weights_kernel<128>, grid, dim3(256), 0, s, a, c, per_wave);
+  if (a.D <= 64) hipLaunchKernelGGL(cache_weights_kernel<64>, grid, dim3(64 * kWWaves), 0, s, a, c, per_wave);
+  else hipLaunchKernelGGL(cache_weights_kernel<128>, grid, dim3(64 * kWWaves), 0, s, a, c, per_wave);
   return hipGetLastError();
 }
 

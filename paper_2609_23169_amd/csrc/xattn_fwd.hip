@@ -43,18 +43,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSumGuard = 18446744073709551616.0f;   // 2^64: per-lane tile sum bound
 
-// Partial results of split s: sums[s][stat] = {maximum (log2 units), sum} and
-// O[s][stat][D], stat a row's index in the LSE tensor.
-// A cache call: how the items are cut (cache_share) and the scores, in log2
-// units, -inf where a row does not see the key: [b][hk][row][Nk up to whole tiles].
-struct Parts {
-  float2* sums;
-  float* o;
-  int64_t stats;
-  int* cuts;
-  float* scores;
-};
-inline __host__ __device__ int score_keys(const XArgs& a) { return (a.Nk + kXKeys - 1) / kXKeys * kXKeys; }
+// Partial results of split s, and what a cache call leaves beside them.
+using Parts = CacheParts;
 
 template <int DP, int NW, bool SPLIT, int SEE>
 __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_fwd_kernel(const XArgs a, const XOrder order,
@@ -165,20 +155,6 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[h][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[h][e] : -INFINITY;
       }
-      if constexpr (SEE == kSeeCache && (NW == 1 || !SPLIT))
-        if (a.scores && bits) {   // uniform
-          const XArgs& x = *x_args_again();
-          const XItem at = seq.item(seq.cur, order);
-          const int row = 32 * w + l32, rows = x.Nq * x.G;
-          if (row < rows) {
-            float* const to = parts.scores + (((int64_t)at.b * x.Hk + at.hk) * rows + row) * score_keys(x) +
-                              kXKeys * tile + 32 * h + 4 * g;
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-              *reinterpret_cast<f32x4*>(to + 8 * c) =
-                  f32x4{s[h][4 * c], s[h][4 * c + 1], s[h][4 * c + 2], s[h][4 * c + 3]} * c2;
-          }
-        }
       if (fresh && half) {   // uniform
         m_run = pair_max(half_max(h));
         fresh = false;
@@ -496,6 +472,8 @@ __global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const 
       const int hk = head / a.G;
       splits = count(b, hk * tiles + (t * a.G + head - hk * a.G) / rows_per_item);
     }
+    const bool whole = splits == 1 && a.Nq * a.G <= kScoreRows;   // cache_one finishes these
+    if (whole) splits = 0;
     float M = -INFINITY;
     for (int s = lane; s < splits; s += 32) {
       const float2 p = parts.sums[s * parts.stats + r];
@@ -528,6 +506,7 @@ __global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const 
         }
     }
     if (!live || sub != 0) return;
+    if (whole) return;   // finished by its workgroup
     const float inv = L == 0.f ? 0.f : 1.f / L;
     if (lane == 0) a.lse[r] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
     if (4 * lane < a.D) {
@@ -548,8 +527,8 @@ __global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const 
     const int t = row / a.G, head = hk * a.G + row - t * a.G;
     const int64_t r = ((int64_t)b * a.Hq + head) * a.Nq + t;
     float m = -INFINITY, l = 0.f;
-    if constexpr (SPLIT) {
-      const int n = count(b, hk);
+    const int n = SPLIT ? count(b, hk) : 1;
+    if (n > 1) {
       for (int s = sub; s < n; s += 8) {
         const float2 p = parts.sums[s * parts.stats + r];
         if (p.y == 0.f) continue;   // no keys in use here
@@ -564,7 +543,7 @@ __global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const 
         m = to;
       }
       m += __log2f(l);
-    } else {
+    } else {   // finished by its workgroup
       m = a.lse[r] * kLog2e;
     }
     if (sub == 0) lse2[row] = m == -INFINITY || m != m ? INFINITY : m;   // no keys: P = 0
@@ -573,9 +552,8 @@ __global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const 
   if (key >= a.Nk) return;
   const XSample sm = x_sample<kSeeCache>(a, b);
   const XSpan span = x_span<kSeeCache>(a, sm, 0, rows);
-  const int tile = key / kXKeys, last = span.skip + span.count;   // of the list, as tile numbers
   float sum = 0.f;
-  if (tile < span.first || (tile >= span.first + span.skip && tile < last)) {
+  if (key < sm.nk && span.has(key / kXKeys)) {
 #pragma unroll 4
     for (int r = 0; r < rows; ++r) sum += fast_exp2(sc[(int64_t)r * score_keys(a)] - lse2[r]);
   }
@@ -592,16 +570,17 @@ struct Shape {
   int splits, waves;
 };
 Shape fwd_shape(const XArgs& a) {
-  if (a.lens) {   // shared out by cache_share where the items would not fill the chip
-    const int64_t rows = (int64_t)a.Nq * a.G, heads = (int64_t)a.B * a.Hk;
-    const int waves = rows <= 32 ? 1 : rows <= 128 || a.D <= 64 ? 4 : 8, wgs = (int)x_resident(x_padded(a), waves);
-    const int64_t groups = (int64_t)a.Hk * ((rows + 32 * waves - 1) / (32 * waves));
-    const int64_t tiles = x_item_tiles(a, (int)std::min<int64_t>(rows, INT32_MAX));
-    if (a.B * groups >= wgs || tiles < 2 * kPartTiles || heads == 0) return Shape{1, 4};
-    // parts of an item, at most: of its tiles by what a workgroup takes, and one more
-    return Shape{(int)std::min((tiles + kPartTiles - 1) / kPartTiles, (wgs + groups - 1) / groups) + 1, waves};
-  }
   const int64_t rows = (int64_t)a.Nq * a.G, heads = (int64_t)a.B * a.Hk;
+  if (a.lens) {   // shared out by cache_share where the items would not fill the chip
+    const int waves = rows <= 128 || a.D <= 64 ? 4 : 8;
+    const bool few = rows <= kScoreRows;   // cache_one.hip
+    const int wgs = few ? kCacheOneGroups : (int)x_resident(x_padded(a), waves), least = cache_least(a);
+    const int64_t groups = few ? a.Hk : (int64_t)a.Hk * ((rows + 32 * waves - 1) / (32 * waves));
+    const int64_t tiles = x_item_tiles(a, (int)std::min<int64_t>(rows, INT32_MAX));
+    if (few ? tiles <= least && a.B * groups <= wgs : a.B * groups >= wgs || tiles < 2 * least) return Shape{1, 4};
+    // parts of an item, at most: of its tiles by what a workgroup takes, and one more
+    return Shape{(int)std::min((tiles + least - 1) / least, (wgs + groups - 1) / groups) + 1, waves};
+  }
   auto splits = [&](int nw) {
     const int64_t groups = heads * ((rows + 32 * nw - 1) / (32 * nw)), tiles = x_item_tiles(a, 32 * nw);
     return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), nw) / groups, tiles / 4));
@@ -630,12 +609,14 @@ void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
 }
 template <int SEE>
 void launch_fwd(const XArgs& a, int splits, int waves, const Parts& parts, hipStream_t s) {
+  constexpr int one = SEE == kSeeCache ? 4 : 1;   // a cache call's few rows have a kernel of their own
   if constexpr (SEE == kSeeCache)
     if (waves == 8) return launch_fwd<128, 8, SEE>(a, splits, parts, s);
   if (a.D <= 64)
-    waves == 1 ? launch_fwd<64, 1, SEE>(a, splits, parts, s) : launch_fwd<64, 4, SEE>(a, splits, parts, s);
+    SEE != kSeeCache && waves == 1 ? launch_fwd<64, one, SEE>(a, splits, parts, s) : launch_fwd<64, 4, SEE>(a, splits, parts, s);
   else
-    waves == 1 ? launch_fwd<128, 1, SEE>(a, splits, parts, s) : launch_fwd<128, 4, SEE>(a, splits, parts, s);
+    SEE != kSeeCache && waves == 1 ? launch_fwd<128, one, SEE>(a, splits, parts, s)
+                                   : launch_fwd<128, 4, SEE>(a, splits, parts, s);
 }
 template <int GPR>
 void launch_join(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
@@ -702,14 +683,21 @@ hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* worksp
   char* const at = static_cast<char*>(workspace);
   const Parts parts{reinterpret_cast<float2*>(at + c.o), reinterpret_cast<float*>(at), stats_of(a),
                     reinterpret_cast<int*>(at + c.o + c.sums), reinterpret_cast<float*>(at + c.o + c.sums + c.cuts)};
-  launch_fwd<kSeeCache>(a, splits, waves, parts, s);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  const bool few = a.Nq * a.G <= kScoreRows;
+  // no item is cut, and the weights are few enough for the workgroup that has the scores
+  const bool weights_here = few && splits == 1 && a.scores && a.Nk <= 2048;
+  if (few) {
+    if (hipError_t e = launch_cache_one(a, parts, w, weights_here, s); e != hipSuccess) return e;
+  } else {
+    launch_fwd<kSeeCache>(a, splits, waves, parts, s);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
   const bool many = splits >= 8 && parts.stats <= 4096;   // as xattn_join
   const int64_t joins = splits > 1 ? (parts.stats + (many ? 0 : 7)) / (many ? 1 : 8) : 0;
-  const int64_t chunks = a.scores ? (int64_t)a.B * a.Hk * (((int64_t)a.Nk + 255) / 256) : 0;
+  const int64_t chunks = a.scores && !weights_here ? (int64_t)a.B * a.Hk * (((int64_t)a.Nk + 255) / 256) : 0;
   if (joins + chunks > 0) {
     TraceScope ts_(s, "cache_finish");
-    const int rows = 32 * waves;
+    const int rows = few ? kScoreRows : 32 * waves;
     const int tiles = (int)(((int64_t)a.Nq * a.G + rows - 1) / rows);
     const dim3 grid((unsigned)(joins + chunks));
     if (splits == 1)

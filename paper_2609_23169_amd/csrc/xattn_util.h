@@ -94,6 +94,7 @@ __device__ inline XItem x_item(unsigned it, unsigned B, const XOrder& o) {
 struct XSpan {
   int send, lo, hi;
   int first, skip, count;
+  __device__ inline bool has(int tile) const { return tile < first || (tile >= first + skip && tile < skip + count); }
 };
 // Bits 0 .. n - 1, and bits lo .. hi - 1.
 __device__ inline uint64_t bits_below(int n) { return n >= 64 ? ~(uint64_t)0 : n <= 0 ? 0 : ((uint64_t)1 << n) - 1; }
@@ -436,12 +437,13 @@ struct TileSeq {
 // many idle, the tiles of all items in a row are cut at every `per`-th: a workgroup then
 // begins within an item, has whole ones perhaps and ends within one (a change of item
 // costs about as much as two tiles: 8 samples of 66 tiles 28.7 us one each, 32.6 cut).
-constexpr int kPartTiles = 4;   // of a workgroup, at least
 struct CacheShare {
   int b, g;               // its first item: sample, and key head and tile of rows
   int t0, t1;             // first tile of the first item, end of the last one's
   int items, part;        // part: of the first item
 };
+// Tiles of a workgroup, at least.
+inline __host__ __device__ int cache_least(const XArgs& a) { return a.Nq * a.G <= kScoreRows ? 8 : 4; }
 // Tiles of keys that sample b's rows see together.
 __device__ inline int cache_tiles(const XArgs& a, int b) {
   const int used = min(max(a.lens[b], 0), a.Nk - a.Nq), nk = used + a.Nq;   // as x_sample
@@ -457,22 +459,18 @@ __device__ inline int cache_parts(int per, int start, int n, int g) {
 }
 // cuts: per and the samples' starts, or null; each sample has `groups` items.
 __device__ inline CacheShare cache_share(const XArgs& a, int wg, int wgs, int groups, int* cuts) {
+  const int least = cache_least(a);
   const int lane = threadIdx.x & 63, n0 = lane < a.B ? cache_tiles(a, lane) : 0;
   auto tiles_of = [&](int b0) __attribute__((always_inline)) {   // of sample b0 + lane
     return b0 == 0 ? n0 : b0 + lane < a.B ? cache_tiles(a, b0 + lane) : 0;
   };
   auto sum_of = [&](auto f) __attribute__((always_inline)) {
     int total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {   // uniform
-      int x = f(tiles_of(b0));
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m, 64);
-      total += x * groups;
-    }
-    return __builtin_amdgcn_readfirstlane(total);
+    for (int b0 = 0; b0 < a.B; b0 += 64) total += wave_sum(f(tiles_of(b0)));   // uniform
+    return total * groups;
   };
   const int total = sum_of([](int n) { return n; });
-  const int even = max((total + wgs - 1) / wgs, kPartTiles);
+  const int even = max((total + wgs - 1) / wgs, least);
   int per = even;
   bool row = true;
   for (int i = 0; i < 3 && row; ++i) {   // up to an eighth more than an even share
@@ -484,13 +482,11 @@ __device__ inline CacheShare cache_share(const XArgs& a, int wg, int wgs, int gr
   int first = -1, last = 0, at = 0;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     const int n = tiles_of(b0), units = row ? n : (n + per - 1) / per;
-    int end = units * groups;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const int y = __shfl_up(end, m, 64);
-      end += lane >= m ? y : 0;
+    int end = 0, run = at;   // the lane's sample ends there
+    for (int i = 0; i < min(a.B - b0, 64); ++i) {
+      run += __builtin_amdgcn_readlane(units, i) * groups;
+      end = lane == i ? run : end;
     }
-    end += at;
     const int start = end - units * groups;
     if (cuts && b0 + lane < a.B) cuts[1 + b0 + lane] = start;
     if (const uint64_t here = __ballot(x0 >= start && x0 < end)) {   // the sample of x0
@@ -510,7 +506,7 @@ __device__ inline CacheShare cache_share(const XArgs& a, int wg, int wgs, int gr
         s.t1 = x1 - st - g * un + 1;
         last = (b0 + i) * groups + g;
       }
-    at = __builtin_amdgcn_readlane(end, 63);
+    at = run;
   }
   if (cuts && lane == 0) cuts[0] = row ? -per : per;
   s.items = first < 0 ? 0 : last - first + 1;
@@ -518,6 +514,23 @@ __device__ inline CacheShare cache_share(const XArgs& a, int wg, int wgs, int gr
   auto u = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
   return CacheShare{u(s.b), u(s.g), u(s.t0), u(s.t1), u(s.items), u(s.part)};
 }
+
+// Results of parts of an item: sums[part][stat] = {maximum (log2 units), sum} and
+// O[part][stat][D], stat a row's index in the LSE tensor; how the items are cut; the
+// scores, in log2 units, -inf where a row does not see the key: [b][hk][row][Nk up to
+// whole tiles].
+struct CacheParts {
+  float2* sums;
+  float* o;
+  int64_t stats;
+  int* cuts;
+  float* scores;
+};
+inline __host__ __device__ int score_keys(const XArgs& a) { return (a.Nk + kXKeys - 1) / kXKeys * kXKeys; }
+constexpr int kCacheOneGroups = 256;   // workgroups of the few-rows kernel: one a CU, by its LDS
+// Few rows (cache_one.hip). weights_here: no item is cut, and each workgroup adds its items'
+// weights itself.
+hipError_t launch_cache_one(const XArgs& a, const CacheParts& parts, const CacheWeights& w, bool weights_here, hipStream_t s);
 
 // TileSeq for such a share.
 struct CacheSeq {
