@@ -17,8 +17,8 @@
 // unsigned number is bracketed, and the next number is taken where the counts at the
 // ends would have it on a straight line, every fourth time in the middle (that number
 // grows with the float's logarithm): some five steps leave 64 slots, which are ranked
-// against each other, where bisection took over twenty. A workgroup holds the row in registers (up to 32,768 slots,
-// longer rows are read again), a step is a compare and an add a register and one
+// against each other, where bisection took over twenty. A workgroup holds the row in registers, and longer ones
+// in LDS too (up to 69,632 slots; beyond they are read again), a step is a compare and an add a register and one
 // barrier. Then ballots give every kept slot its place in ascending order, equal
 // weights the lowest slots first, and a second launch copies the rows of K and V.
 #include <algorithm>
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XA
       __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): and read
       pin_order();
       if (i + 1 < per_wave) load(tile_key(i + 1));
-      const int k = tile_key(i), key = k + l32;
+      const int k = tile_key(i);
       if (!seen(k)) continue;     // uniform
       // every row sees every key of the tile, whatever its place in the chunk or tree
       const bool whole = k + 32 <= off && (k >= off + sm.nq - a.left || k + 32 <= a.sinks);
@@ -176,140 +176,182 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XA
 // ---------------------------------------------------------------------------
 // Eviction
 // ---------------------------------------------------------------------------
-constexpr int kEvictWaves = 16;
-
-// Weights as unsigned numbers of the same order; NaN below all, -0 as +0.
+// Weights as unsigned numbers of the same order, 1 or above; NaN below all, -0 as +0.
 __device__ inline unsigned weight_key(float x) {
   const unsigned u = __float_as_uint(x);
-  if (x != x) return 0u;
+  if (x != x) return 1u;
   if (u == 0x80000000u) return 0x80000000u;
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// One workgroup a row (sample and key head). R: registers a lane for the row's middle,
-// 0: it is read again in every pass.
-template <int R>
-__global__ __launch_bounds__(64 * kEvictWaves) void cache_select_kernel(const CacheEvict a) {
-  constexpr int W = kEvictWaves;
-  __shared__ unsigned cnt[2][W], cnt2[W], ends[2][W], few[64], found;
+// One workgroup of W waves a row (sample and key head). R: registers a lane for the row's
+// middle, L: words of LDS a lane for more of it; R = 0: it is read again in every pass. Few waves where they hold the row: the
+// arithmetic of a step is done by each of them (300 slots 5.7 us with 4, 9.3 with 16;
+// 16,000 slots 22 and 16).
+template <int W, int R, int L = 0>
+__global__ __launch_bounds__(64 * W) void cache_select_kernel(const CacheEvict a) {
+  __shared__ __attribute__((aligned(16))) unsigned cnt[2][W], cnt2[W], ends[4][W];
+  __shared__ unsigned few[64], found;
+  __shared__ unsigned key_lds[L ? L * 64 * W : 1];
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = blockIdx.x;
   const int b = (int)(row / a.Hk);
-  const int n = min(max(x_cu(a.lens, b), 0), a.cap), count = min(n, a.keep);
   const float* const wt = a.weights + row * a.cap;
   float* const wo = a.weights_out + row * a.cap_out;
   int32_t* const idx = a.idx + row * a.keep;
-  if (tid == 0 && row % a.Hk == 0) a.len_out[b] = count;
-  for (int i = count + tid; i < a.keep; i += 64 * W) idx[i] = -1;
-  for (int i = count + tid; i < a.cap_out; i += 64 * W) wo[i] = 0.f;
-  auto put = [&](int place, int slot) __attribute__((always_inline)) { idx[place] = slot; };
-  if (n <= a.keep) {   // uniform
-    for (int i = tid; i < n; i += 64 * W) put(i, i);
-    return;
-  }
-  // The first and the last slots stay; `need` >= 0 of the m > need between them.
-  for (int i = tid; i < a.sinks; i += 64 * W) put(i, i);
-  for (int i = tid; i < a.recent; i += 64 * W) put(a.keep - a.recent + i, n - a.recent + i);
-  const int m = n - a.sinks - a.recent, need = a.keep - a.sinks - a.recent;
+  // Wave w holds the slots [begin, begin + per) of the middle, in order of register and
+  // lane: by the capacity, so that they load beside the length.
   const float* const mid = wt + a.sinks;
-  if (need == 0) return;   // uniform
-
-  // Wave w holds the slots [begin, end) of the middle, in order of register and lane.
-  const int per = ((m + W - 1) / W + 63) / 64 * 64, begin = w * per, end = min(m, begin + per);
-  unsigned key[R ? R : 1];
+  const int room = max(a.cap - a.sinks - a.recent, 0), per = ((room + W - 1) / W + 63) / 64 * 64, begin = w * per;
+  float x[R ? R : 1];
   if constexpr (R > 0) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int at = begin + 64 * i + lane;
-      key[i] = at < end ? weight_key(mid[at]) : 0u;
+      x[i] = 64 * i < per && at < room ? mid[at] : 0.f;
     }
   }
-  // f(slot of the lane, its key) over the wave's slots (R > 0: its registers, slots
-  // behind `end` with key 0)
+  const int n = min(max(x_cu(a.lens, b), 0), a.cap), count = min(n, a.keep);
+  if (tid == 0 && row % a.Hk == 0) a.len_out[b] = count;
+  for (int i = count + tid; i < a.keep; i += 64 * W) idx[i] = -1;
+  for (int i = count + tid; i < a.cap_out; i += 64 * W) wo[i] = 0.f;
+  if (n <= a.keep) {   // uniform
+    for (int i = tid; i < n; i += 64 * W) idx[i] = i;
+    return;
+  }
+  // The first and the last slots stay; `need` >= 0 of the m > need between them.
+  for (int i = tid; i < a.sinks; i += 64 * W) idx[i] = i;
+  for (int i = tid; i < a.recent; i += 64 * W) idx[a.keep - a.recent + i] = n - a.recent + i;
+  const int m = n - a.sinks - a.recent, need = a.keep - a.sinks - a.recent;
+  if (need == 0) return;   // uniform
+  const int end = min(m, begin + per);
+  unsigned key[R ? R : 1];   // behind the middle 0: below every key
+  if constexpr (R > 0) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) key[i] = begin + 64 * i + lane < end ? weight_key(x[i]) : 0u;
+  }
+#pragma unroll 12
+  for (int i = 0; i < L; ++i) {   // a lane reads what it wrote: no barrier
+    const int at = begin + 64 * (R + i) + lane;
+    key_lds[i * 64 * W + tid] = at < end ? weight_key(mid[at]) : 0u;
+  }
+  // f(slot of the lane, its key) over the wave's slots
   auto each = [&](auto f) __attribute__((always_inline)) {
     if constexpr (R > 0) {
 #pragma unroll
       for (int i = 0; i < R; ++i) f(begin + 64 * i + lane, key[i]);
+#pragma unroll 12
+      for (int i = 0; i < L; ++i) f(begin + 64 * (R + i) + lane, key_lds[i * 64 * W + tid]);
     } else {
-      for (int at = begin + lane; at - lane < end; at += 64) f(at, at < end ? weight_key(mid[at]) : 0u);
+      constexpr int U = 8;   // loaded together
+      for (int at = begin + lane; at - lane < end; at += 64 * U) {
+        float y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) y[u] = at + 64 * u < end ? mid[at + 64 * u] : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) f(at + 64 * u, at + 64 * u < end ? weight_key(y[u]) : 0u);
+      }
     }
   };
   int turn = 0;
   auto total = [&](unsigned mine) __attribute__((always_inline)) {   // over the waves; one barrier
     if (lane == 0) cnt[turn][w] = mine;
     __syncthreads();
-    unsigned t = 0;
+    unsigned sum = 0;
 #pragma unroll
-    for (int i = 0; i < W; ++i) t += cnt[turn][i];
+    for (int i = 0; i < W; ++i) sum += cnt[turn][i];
     turn ^= 1;
-    return t;
+    return sum;
   };
-  // The least and the largest key bracket it: `need` slots or more have t or more, fewer
-  // have `to` or more (at_t and at_to of them).
-  unsigned lo = ~0u, hi = 0;
-  each([&](int at, unsigned k) {
-    lo = min(lo, at < end ? k : ~0u);
-    hi = max(hi, k);
+  // [t, last] holds the largest key that `need` slots or more have or exceed: at_t of
+  // them have t or more, at_last more than `last`. At first all keys, or those above 0:
+  // many slots have received nothing, and no key lies between 0 and the rest.
+  constexpr unsigned kZero = 0x80000000u;
+  unsigned t = ~0u, from = ~0u, last = 0;
+  int positive = 0;
+  each([&](int, unsigned k) {
+    t = min(t, k - 1);   // 0: the largest
+    from = min(from, k > kZero ? k : ~0u);
+    positive += k > kZero ? 1 : 0;
+    last = max(last, k);
   });
-  lo = wave_min(lo);
-  hi = ~wave_min(~hi);
-  if (lane == 0) ends[0][w] = lo, ends[1][w] = hi;
+  t = wave_min(t);
+  from = wave_min(from);
+  last = ~wave_min(~last);
+  positive = wave_sum(positive);
+  if (lane == 0) ends[0][w] = t, ends[1][w] = last, ends[2][w] = from, ends[3][w] = positive;
   __syncthreads();
+  positive = 0;
 #pragma unroll
-  for (int i = 0; i < W; ++i) lo = min(lo, ends[0][i]), hi = max(hi, ends[1][i]);
-  unsigned long long t = lo, to = (unsigned long long)hi + 1;
-  unsigned at_t = m, at_to = 0;
-  for (int step = 1; at_t != (unsigned)need && to - t > 1 && at_t - at_to > 64; ++step) {   // uniform
-    const unsigned long long width = to - t;
-    unsigned long long by = width / 2;
-    if (step % 4 != 0)
-      by = (unsigned long long)((float)width * (((float)(at_t - need) + 0.5f) / (float)(at_t - at_to)));
-    const unsigned long long mid = t + (by < 1 ? 1 : by > width - 1 ? width - 1 : by);
-    const unsigned limit = (unsigned)mid;
+  for (int i = 0; i < W; ++i) {
+    t = min(t, ends[0][i]), last = max(last, ends[1][i]), from = min(from, ends[2][i]);
+    positive += ends[3][i];
+  }
+  const bool above_0 = positive >= need;
+  t = above_0 ? from : t + 1;
+  unsigned at_t = above_0 ? positive : m, at_last = 0;
+  for (int step = 1; at_t != (unsigned)need && last > t && at_t - at_last > 64; ++step) {   // uniform
+    const unsigned width = last - t;
+    unsigned by = width / 2;
+    if (step % 4 != 0)   // any number within the bracket will do
+      by = (unsigned)((float)width * ((float)(at_t - need) + 0.5f) * __builtin_amdgcn_rcpf((float)(at_t - at_last)));
+    const unsigned limit = t + 1 + min(by, width - 1);
     int c = 0;
     each([&](int, unsigned k) { c += k >= limit ? 1 : 0; });
     const unsigned all = total((unsigned)wave_sum(c));
-    if (all >= (unsigned)need) t = mid, at_t = all;
-    else to = mid, at_to = all;
+    if (all >= (unsigned)need) t = limit, at_t = all;
+    else last = limit - 1, at_last = all;
   }
-  if (at_t != (unsigned)need && to - t > 1) {   // uniform: the last 64 or fewer, each against all others
+  if (at_t != (unsigned)need && last > t) {   // uniform: the last 64 or fewer, each against all others
     if (tid == 0) found = 0;
     __syncthreads();
-    each([&](int at, unsigned k) {
-      if (at < end && k >= (unsigned)t && k <= (unsigned)(to - 1)) few[atomicAdd(&found, 1u)] = k;   // values alone: any order
+    each([&](int, unsigned k) {
+      if (k >= t && k <= last) few[atomicAdd(&found, 1u)] = k;   // values alone: any order
     });
     __syncthreads();
-    const unsigned n_few = at_t - at_to, mine = lane < (int)n_few ? few[lane] : 0u;
+    const int n_few = at_t - at_last;
+    const unsigned mine = lane < n_few ? few[lane] : 0u;
     unsigned more = 0, same = 0;   // of them above the lane's, and equal to it
-    for (unsigned i = 0; i < n_few; ++i) {
-      more += few[i] > mine;
-      same += few[i] == mine;
+    for (int i = 0; i < n_few; ++i) {
+      const unsigned other = (unsigned)__builtin_amdgcn_readlane((int)mine, i);
+      more += other > mine;
+      same += other == mine;
     }
-    // the one with which `need` is reached: at_to + more < need <= at_to + more + same
-    const bool is = lane < (int)n_few && at_to + more < (unsigned)need && (unsigned)need <= at_to + more + same;
+    // the one with which `need` is reached
+    const bool is = lane < n_few && at_last + more < (unsigned)need && (unsigned)need <= at_last + more + same;
     t = (unsigned)__builtin_amdgcn_readlane((int)mine, __builtin_ctzll(__ballot(is)));
   }
-  // Slots above t, and of those equal to it the first ones (behind the row's end keys
-  // are 0: no slot, where t is 0).
-  const unsigned least = (unsigned)t;
+  // Slots above t, and of those equal to it the first ones.
   int over_mine = 0, same_mine = 0;
-  each([&](int at, unsigned k) {
-    over_mine += k > least ? 1 : 0;
-    same_mine += k == least && at < end ? 1 : 0;
+  each([&](int, unsigned k) {
+    over_mine += k > t ? 1 : 0;
+    same_mine += k == t ? 1 : 0;
   });
   const unsigned over = wave_sum(over_mine), same = wave_sum(same_mine);
   if (lane == 0) cnt2[w] = same;
   const unsigned above = total(over);   // its barrier covers cnt2 too
   unsigned before_over = 0, before_same = 0;
-  for (int i = 0; i < w; ++i) before_over += cnt[turn ^ 1][i], before_same += cnt2[i];
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    before_over += i < w ? cnt[turn ^ 1][i] : 0;
+    before_same += i < w ? cnt2[i] : 0;
+  }
   const unsigned ties = (unsigned)need - above;
+  if (same == 0) {   // uniform: as a rule
+    each([&](int at, unsigned k) {
+      const uint64_t o = __ballot(k > t);
+      const unsigned mo = __builtin_amdgcn_mbcnt_hi((unsigned)(o >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)o, before_over));
+      if (k > t) idx[a.sinks + (int)(mo + min(before_same, ties))] = a.sinks + at;
+      before_over += __builtin_popcountll(o);
+    });
+    return;
+  }
   each([&](int at, unsigned k) {
-    const uint64_t o = __ballot(k > least), s = __ballot(k == least && at < end);
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    const unsigned mo = before_over + __builtin_popcountll(o & below), ms = before_same + __builtin_popcountll(s & below);
-    const bool in = (o >> lane & 1) || ((s >> lane & 1) && ms < ties);
-    if (in) put(a.sinks + (int)(mo + min(ms, ties)), a.sinks + at);
+    const uint64_t o = __ballot(k > t), s = __ballot(k == t);
+    const unsigned mo = __builtin_amdgcn_mbcnt_hi((unsigned)(o >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)o, before_over));
+    const unsigned ms = __builtin_amdgcn_mbcnt_hi((unsigned)(s >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)s, before_same));
+    if (k > t || (k == t && ms < ties)) idx[a.sinks + (int)(mo + min(ms, ties))] = a.sinks + at;
     before_over += __builtin_popcountll(o);
     before_same += __builtin_popcountll(s);
   });
@@ -368,14 +410,16 @@ hipError_t launch_cache_weights(const XArgs& a, const CacheWeights& c, hipStream
 }
 
 hipError_t launch_cache_evict(const CacheEvict& a, hipStream_t s) {
-  const int64_t most = ((int64_t)a.cap - a.sinks - a.recent + 64 * kEvictWaves - 1) / (64 * kEvictWaves);   // a lane's
+  const int64_t room = std::max<int64_t>((int64_t)a.cap - a.sinks - a.recent, 0);   // slots of a row's middle, at most
   {
     TraceScope ts_(s, "cache_select");
-    const dim3 grid((unsigned)(a.B * a.Hk)), block(64 * kEvictWaves);
-    if (most <= 4) hipLaunchKernelGGL(cache_select_kernel<4>, grid, block, 0, s, a);
-    else if (most <= 16) hipLaunchKernelGGL(cache_select_kernel<16>, grid, block, 0, s, a);
-    else if (most <= 32) hipLaunchKernelGGL(cache_select_kernel<32>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(cache_select_kernel<0>, grid, block, 0, s, a);
+    const dim3 grid((unsigned)(a.B * a.Hk));
+    if (room <= 1024) hipLaunchKernelGGL((cache_select_kernel<4, 4>), grid, dim3(256), 0, s, a);
+    else if (room <= 4096) hipLaunchKernelGGL((cache_select_kernel<4, 16>), grid, dim3(256), 0, s, a);
+    else if (room <= 16384) hipLaunchKernelGGL((cache_select_kernel<16, 16>), grid, dim3(1024), 0, s, a);
+    else if (room <= 32768) hipLaunchKernelGGL((cache_select_kernel<16, 32>), grid, dim3(1024), 0, s, a);
+    else if (room <= 1024 * 68) hipLaunchKernelGGL((cache_select_kernel<16, 32, 36>), grid, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((cache_select_kernel<16, 0>), grid, dim3(1024), 0, s, a);
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const int rows = a.zero_rest ? a.cap_out : a.keep;

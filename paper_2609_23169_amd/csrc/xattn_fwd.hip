@@ -470,9 +470,9 @@ __global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const 
       head = (int)(bh - (int64_t)b * a.Hq);
       tok = (int64_t)b * a.Nq + t;
       const int hk = head / a.G;
-      splits = count(b, hk * tiles + (t * a.G + head - hk * a.G) / rows_per_item);
+      splits = count(b, parts.heads > 0 ? hk / parts.heads : hk * tiles + (t * a.G + head - hk * a.G) / rows_per_item);
     }
-    const bool whole = splits == 1 && a.Nq * a.G <= kScoreRows;   // cache_one finishes these
+    const bool whole = splits == 1 && parts.heads > 0;   // cache_one finishes these
     if (whole) splits = 0;
     float M = -INFINITY;
     for (int s = lane; s < splits; s += 32) {
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const 
     const int t = row / a.G, head = hk * a.G + row - t * a.G;
     const int64_t r = ((int64_t)b * a.Hq + head) * a.Nq + t;
     float m = -INFINITY, l = 0.f;
-    const int n = SPLIT ? count(b, hk) : 1;
+    const int n = SPLIT ? count(b, hk / parts.heads) : 1;
     if (n > 1) {
       for (int s = sub; s < n; s += 8) {
         const float2 p = parts.sums[s * parts.stats + r];
@@ -575,7 +575,7 @@ Shape fwd_shape(const XArgs& a) {
     const int waves = rows <= 128 || a.D <= 64 ? 4 : 8;
     const bool few = rows <= kScoreRows;   // cache_one.hip
     const int wgs = few ? kCacheOneGroups : (int)x_resident(x_padded(a), waves), least = cache_least(a);
-    const int64_t groups = few ? a.Hk : (int64_t)a.Hk * ((rows + 32 * waves - 1) / (32 * waves));
+    const int64_t groups = few ? a.Hk / cache_heads(a) : (int64_t)a.Hk * ((rows + 32 * waves - 1) / (32 * waves));
     const int64_t tiles = x_item_tiles(a, (int)std::min<int64_t>(rows, INT32_MAX));
     if (few ? tiles <= least && a.B * groups <= wgs : a.B * groups >= wgs || tiles < 2 * least) return Shape{1, 4};
     // parts of an item, at most: of its tiles by what a workgroup takes, and one more
@@ -682,7 +682,8 @@ hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* worksp
   const CacheSpace c = cache_space(a);
   char* const at = static_cast<char*>(workspace);
   const Parts parts{reinterpret_cast<float2*>(at + c.o), reinterpret_cast<float*>(at), stats_of(a),
-                    reinterpret_cast<int*>(at + c.o + c.sums), reinterpret_cast<float*>(at + c.o + c.sums + c.cuts)};
+                    reinterpret_cast<int*>(at + c.o + c.sums), reinterpret_cast<float*>(at + c.o + c.sums + c.cuts),
+                    a.Nq * a.G <= kScoreRows ? cache_heads(a) : 0};
   const bool few = a.Nq * a.G <= kScoreRows;
   // no item is cut, and the weights are few enough for the workgroup that has the scores
   const bool weights_here = few && splits == 1 && a.scores && a.Nk <= 2048;

@@ -442,8 +442,17 @@ struct CacheShare {
   int t0, t1;             // first tile of the first item, end of the last one's
   int items, part;        // part: of the first item
 };
+// Few rows: key heads of an item, four where that leaves every workgroup 24 tiles or more
+// of full caches and the registers hold them (one token on four caches of 16,500 slots, 8
+// heads: 55 us with the join against 53; eight of 4,100: 35 against 37).
+inline __host__ __device__ int cache_heads(const XArgs& a) {
+  const int64_t tiles = (int64_t)a.B * a.Hk * ((std::min<int64_t>(a.Nk, (int64_t)a.left + a.sinks) + kXKeys - 1) / kXKeys);
+  return a.Nq * a.G <= 16 && a.Hk % 4 == 0 && tiles >= 24 * 256 ? 4 : 1;
+}
 // Tiles of a workgroup, at least.
-inline __host__ __device__ int cache_least(const XArgs& a) { return a.Nq * a.G <= kScoreRows ? 8 : 4; }
+inline __host__ __device__ int cache_least(const XArgs& a) {
+  return a.Nq * a.G <= kScoreRows && cache_heads(a) == 1 ? 8 : 4;
+}
 // Tiles of keys that sample b's rows see together.
 __device__ inline int cache_tiles(const XArgs& a, int b) {
   const int used = min(max(a.lens[b], 0), a.Nk - a.Nq), nk = used + a.Nq;   // as x_sample
@@ -525,6 +534,7 @@ struct CacheParts {
   int64_t stats;
   int* cuts;
   float* scores;
+  int heads;     // key heads of an item
 };
 inline __host__ __device__ int score_keys(const XArgs& a) { return (a.Nk + kXKeys - 1) / kXKeys * kXKeys; }
 constexpr int kCacheOneGroups = 256;   // workgroups of the few-rows kernel: one a CU, by its LDS

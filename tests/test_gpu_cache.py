@@ -230,7 +230,7 @@ def test_eviction_by_kinds_of_weights(kind, cap, lens, keep, sinks, recent):
 @pytest.mark.parametrize("cap,lens,keep,sinks,recent,Hk,D", [
     (1, [1], 1, 0, 0, 1, 8), (2, [2, 1], 1, 1, 0, 1, 64), (2, [2, 2], 1, 0, 1, 3, 128), (65, [65], 64, 10, 54, 1, 40),
     (65, [65], 64, 10, 53, 2, 40), (4096, [4096], 4095, 0, 0, 1, 64), (4200, [4200], 1, 0, 0, 1, 64), (17000, [16999, 5], 4096, 4, 1000, 2, 128),
-    (33000, [33000], 300, 1, 0, 1, 64), (70001, [70001, 66000], 20000, 64, 256, 1, 16), (500, [400, 500], 500, 4, 4, 2, 96),
+    (33000, [33000], 300, 1, 0, 1, 64), (70001, [70001, 66000], 20000, 64, 256, 1, 16), (68000, [68000, 33000, 40], 20000, 4, 256, 1, 16), (500, [400, 500], 500, 4, 4, 2, 96),
     (20000, [20000], 12345, 7, 333, 5, 24),
 ])
 def test_eviction_by_sizes(cap, lens, keep, sinks, recent, Hk, D):
