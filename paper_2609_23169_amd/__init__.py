@@ -495,7 +495,7 @@ class _Args:
     def ptr(self, t, name: str):
         if t is None:
             return None
-        if not t.is_cuda or t.get_device() != self.device:
+        if t.get_device() != self.device:   # -1 in host memory
             raise ValueError(f"{name} must live on the device of the first tensor")
         return t.data_ptr()
 
@@ -505,7 +505,8 @@ class _Args:
             self.strides.append(0)
             return None
         if t.is_contiguous():
-            self.strides.append(t.shape[-1] * t.shape[-2])
+            shape = t.shape
+            self.strides.append(shape[-1] * shape[-2])
         else:
             self.strides.append(_token_stride(t, name))
             self.plain = False
@@ -517,9 +518,12 @@ class _Args:
 
     def call(self, fn, args, workspace, stream, takes_workspace=True):
         """fn(*args, workspace, its bytes, stream) on the tensors' device."""
-        s = stream if stream is not None else torch.cuda.current_stream(self.device)
-        if s.device_index != self.device:
+        if stream is None:
+            raw = torch._C._cuda_getCurrentRawStream(self.device)   # a microsecond less than its Stream
+        elif stream.device_index != self.device:
             raise ValueError("the stream belongs to another device than the tensors")
+        else:
+            raw = stream.cuda_stream
         if workspace is not None:
             if not workspace.is_contiguous():
                 raise ValueError("workspace must be contiguous")
@@ -527,9 +531,9 @@ class _Args:
         elif takes_workspace:
             args += (None, 0)
         if torch.cuda.current_device() == self.device:
-            return fn(*args, s.cuda_stream)
+            return fn(*args, raw)
         with torch.cuda.device(self.device):
-            return fn(*args, s.cuda_stream)
+            return fn(*args, raw)
 
 
 def _in_int32(*sizes) -> bool:
@@ -719,8 +723,10 @@ def ut_xattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_seq
 
 def _window(window, n_sink: int):
     """(left, right, n_sink) of a window (left, right), None: no bound on that side."""
-    left, right = (-1 if w is None else int(w) for w in window)
-    _need(min(left, right) >= -1 and _in_int32(left, right, n_sink), "window: two numbers of keys >= 0, or None")
+    left, right = window
+    left, right = -1 if left is None else left, -1 if right is None else right
+    if not (-1 <= left < 1 << 31 and -1 <= right < 1 << 31 and -(1 << 31) <= n_sink < 1 << 31):
+        raise ValueError("window: two numbers of keys >= 0, or None")
     return left, right, n_sink
 
 
@@ -798,18 +804,18 @@ def ut_swattn_bwd_varlen(q, k, v, o, dout, lse, dq, dk, dv, cu_seqlens_q, max_se
 
 
 def _check_slots(cache_len, B: int, name: str = "cache_len"):
-    _need(cache_len.dtype == torch.int32 and cache_len.shape == (B,) and cache_len.is_contiguous(),
-          f"{name}: contiguous int32 [B]")
+    if cache_len.dtype != torch.int32 or cache_len.shape != (B,) or not cache_len.is_contiguous():
+        raise ValueError(f"{name}: contiguous int32 [B]")
 
 
 def _check_words(t, shape, name: str):
-    _need(t is None or (t.dtype in (torch.int64, torch.uint64) and t.shape == shape and t.is_contiguous()),
-          f"{name}: contiguous int64 or uint64 {list(shape)}")
+    if t is not None and (t.dtype not in (torch.int64, torch.uint64) or t.shape != shape or not t.is_contiguous()):
+        raise ValueError(f"{name}: contiguous int64 or uint64 {list(shape)}")
 
 
 def _check_weights(t, shape, name: str):
-    _need(t is None or (t.dtype == torch.float32 and t.shape == shape and t.is_contiguous()),
-          f"{name}: contiguous fp32 {list(shape)}")
+    if t is not None and (t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous()):
+        raise ValueError(f"{name}: contiguous fp32 {list(shape)}")
 
 
 def ut_cache_attn_workspace_size(B: int, T: int, capacity: int, Hq: int, Hk: int, D: int, window_left=None,
@@ -825,8 +831,8 @@ def ut_cache_attn(q, k_cache, v_cache, o, lse, cache_len, softmax_scale: float, 
     _check_lse(lse, B * Hq * T)
     _check_slots(cache_len, B)
     _check_words(tree, (B, T), "tree")
-    for w, nm in ((weights_in, "weights_in"), (weights_out, "weights_out")):
-        _check_weights(w, (B, Hk, cap), nm)
+    _check_weights(weights_in, (B, Hk, cap), "weights_in")
+    _check_weights(weights_out, (B, Hk, cap), "weights_out")
     left, _, n_sink = _window((window_left, 0), n_sink)
     a = _Args(q)
     rows = (a.rows(q, "q"), a.rows(k_cache, "k_cache"), a.rows(v_cache, "v_cache"), a.rows(o, "o"))
@@ -843,8 +849,8 @@ def ut_cache_weights(q, k_cache, lse, cache_len, weights_out, softmax_scale: flo
     _check_slots(cache_len, B)
     _check_words(tree, (B, T), "tree")
     _check_words(tokens, (B,), "tokens")
-    for w, nm in ((weights_in, "weights_in"), (weights_out, "weights_out")):
-        _check_weights(w, (B, Hk, cap), nm)
+    _check_weights(weights_in, (B, Hk, cap), "weights_in")
+    _check_weights(weights_out, (B, Hk, cap), "weights_out")
     left, _, n_sink = _window((window_left, 0), n_sink)
     a = _Args(q)
     rows = (a.rows(q, "q"), a.rows(k_cache, "k_cache"))
@@ -856,13 +862,14 @@ def ut_cache_weights(q, k_cache, lse, cache_len, weights_out, softmax_scale: flo
 
 def ut_cache_evict(k_cache, v_cache, weights, cache_len, k_out, v_out, weights_out, len_out, kept_idx, n_keep: int,
                    n_sink: int = 0, n_recent: int = 0, zero_rest: bool = False, stream=None) -> int:
-    bf, shape = torch.bfloat16, k_cache.shape
-    for t in (k_cache, v_cache, k_out, v_out):
-        _need(t.dtype == bf and t.dim() == 4, "k_cache, v_cache, k_out, v_out: bf16 [B, capacity, Hk, D]")
-    _need(v_cache.shape == shape and v_out.shape == k_out.shape and k_out.shape[0] == shape[0]
-          and k_out.shape[2:] == shape[2:], "k_cache, v_cache and k_out, v_out: pairs of one shape, one B, Hk and D")
+    bf, shape, out = torch.bfloat16, k_cache.shape, k_out.shape
+    if (k_cache.dtype != bf or v_cache.dtype != bf or k_out.dtype != bf or v_out.dtype != bf or len(shape) != 4
+            or len(out) != 4):
+        raise ValueError("k_cache, v_cache, k_out, v_out: bf16 [B, capacity, Hk, D]")
     B, cap, Hk, D = shape
-    cap_out = k_out.shape[1]
+    Bo, cap_out, Ho, Do = out
+    if v_cache.shape != shape or v_out.shape != out or (Bo, Ho, Do) != (B, Hk, D):
+        raise ValueError("k_cache, v_cache and k_out, v_out: pairs of one shape, one B, Hk and D")
     _need(_in_int32(B, cap, cap_out, Hk, D, n_keep, n_sink, n_recent), "sizes past 32 bits")
     _check_weights(weights, (B, Hk, cap), "weights")
     _check_weights(weights_out, (B, Hk, cap_out), "weights_out")
@@ -1280,12 +1287,11 @@ def cache_evict(k_cache, v_cache, weights, cache_len, n_keep: int, n_sink: int =
     of `capacity` slots (n_keep by default): (k, v, weights, cache_len, kept_idx
     [B, Hk, n_keep]). Slots behind are 0, and -1 in kept_idx."""
     B, _, Hk, D = k_cache.shape
-    cap, dev = n_keep if capacity is None else capacity, k_cache.device
+    cap = n_keep if capacity is None else capacity
     with _alloc_on(stream):
-        k, v = (torch.empty((B, cap, Hk, D), dtype=torch.bfloat16, device=dev) for _ in range(2))
-        w = torch.empty((B, Hk, cap), dtype=torch.float32, device=dev)
-        n = torch.empty(B, dtype=torch.int32, device=dev)
-        idx = torch.empty((B, Hk, n_keep), dtype=torch.int32, device=dev)
+        k, v = k_cache.new_empty((B, cap, Hk, D)), v_cache.new_empty((B, cap, Hk, D))
+        w, n = weights.new_empty((B, Hk, cap)), torch.empty_like(cache_len)
+        idx = cache_len.new_empty((B, Hk, n_keep))
     _raise("ut_cache_evict", ut_cache_evict(k_cache, v_cache, weights, cache_len, k, v, w, n, idx, n_keep, n_sink,
                                             n_recent, True, stream))
     return k, v, w, n, idx
