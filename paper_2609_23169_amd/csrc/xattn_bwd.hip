@@ -277,7 +277,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
   };
 
   // A workgroup's items in turn, their tiles as one sequence, as in the forward.
-  seq.begin(x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk));
+  seq.begin(x_items((unsigned)x_total(order, a.B, a.Hk)));
   bool have = false;   // a tile lies in the current stage
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
@@ -378,9 +378,10 @@ __global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kerne
     x_clear_rest(a.cuk, a.B, a.Tk, a.Hk * a.D, a.dk, a.sdk);
     x_clear_rest(a.cuk, a.B, a.Tk, a.Hk * a.D, a.dv, a.sdv);
   }
-  const XItems items = x_items((unsigned)a.B * order.tiles * order.splits * (unsigned)a.Hk);
+  const XItems items = x_items((unsigned)x_total(order, a.B, a.Hk));
   if (items.first >= items.end) return;
-  const XItem at = x_item(items.first, (unsigned)a.B, order);
+  const XItem at = x_item<WIN ? kSeeWindow : kSeeAll>(items.first, (unsigned)a.B, order);
+  if (WIN && (unsigned)at.tile >= order.tiles) return;   // uniform over the workgroup
   unsigned kt = at.tile, sp = at.part, splits = order.splits;
   if constexpr (WIN) {   // units of work: the parts of the tiles with sinks, then those of the others
     const unsigned u = at.tile, m = sinks.tiles * sinks.splits;
@@ -749,10 +750,10 @@ SinkParts sink_parts(const XArgs& a) {
   p.splits = std::max<int64_t>(p.others, std::min<int64_t>((all + per - 1) / per, 64));
   return p;
 }
-int64_t dkdv_units(const XArgs& a) {   // workgroups of a key head of a sample
+XOrder dkdv_order(const XArgs& a) {   // window attention: the units of work of a key head of a sample
   const SinkParts p = sink_parts(a);
-  const int64_t tiles = ((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys;
-  return p.tiles * p.splits + (tiles - p.tiles) * p.others;
+  const int64_t tiles = ((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys, units = p.tiles * p.splits + (tiles - p.tiles) * p.others;
+  return XOrder{1, (unsigned)units, 1, window_chunk(units)};
 }
 size_t aux_bytes(const XArgs& a) { return ((size_t)a.Tq * a.Hq * 2 * sizeof(float) + 255) / 256 * 256; }
 size_t dq_part(const XArgs& a) {
@@ -773,7 +774,7 @@ size_t sink_part(const XArgs& a) {
 
 template <int DP, bool WIN>
 void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t s) {
-  const XOrder order{head_group(a), (unsigned)dq_tiles(a), (unsigned)splits};
+  const XOrder order{head_group(a), (unsigned)dq_tiles(a), (unsigned)splits, WIN ? window_chunk(dq_tiles(a)) : 0};
   const int64_t items = dq_groups(a) * splits;
   const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, kDqWaves)) + 7) / 8 * 8);
   TraceScope ts_(s, WIN ? "swattn_dq" : "xattn_dq", DP);
@@ -782,9 +783,9 @@ void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t 
 template <int DP, bool WIN>
 void launch_dkdv(const XArgs& a, const float* aux, float* part, const SinkParts& sinks, hipStream_t s) {
   const int64_t tiles = ((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys;
-  const XOrder order{head_group(a), (unsigned)(WIN ? dkdv_units(a) : tiles), WIN ? 1 : (unsigned)sinks.others};
+  const XOrder order = WIN ? dkdv_order(a) : XOrder{head_group(a), (unsigned)tiles, (unsigned)sinks.others, 0};
   TraceScope ts_(s, WIN ? "swattn_dkdv" : "xattn_dkdv", DP);
-  const dim3 grid((unsigned)(std::max<int64_t>((int64_t)a.B * a.Hk * order.tiles * order.splits, 1) + 7) / 8 * 8);
+  const dim3 grid((unsigned)(std::max<int64_t>(x_total(order, a.B, a.Hk), 1) + 7) / 8 * 8);
   hipLaunchKernelGGL((xattn_dkdv_kernel<DP, WIN>), grid, dim3(256), 0, s, a, aux, order, part, sinks);
 }
 void launch_sums(const Join* j, int n, int B, hipStream_t s) {
@@ -811,7 +812,7 @@ bool xattn_bwd_launchable(const XArgs& a) {
   constexpr int64_t kMost = (int64_t)1 << 24;   // workgroups of 256 threads
   int64_t sums = std::max(dq_part(a) > 0 ? a.Tq * a.Hq : 0, dkdv_part(a) > 0 ? a.Tk * a.Hk : 0) * a.D;
   if (sink_part(a) > 0) sums = std::max(sums, (int64_t)a.B * sink_parts(a).tiles * kBwdKeys * a.Hk * a.D);
-  return ((a.window ? (int64_t)a.B * a.Hk * dkdv_units(a) : dkdv_groups(a)) + 7) / 8 * 8 < kMost &&
+  return ((a.window ? x_total(dkdv_order(a), a.B, a.Hk) : dkdv_groups(a)) + 7) / 8 * 8 < kMost &&
          (sums / 4 + 255) / 256 < kMost;
 }
 

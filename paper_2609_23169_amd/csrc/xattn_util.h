@@ -61,9 +61,23 @@ __device__ inline XItems x_items(unsigned total) {
 // How item numbers are read: `heads` key heads of a group fastest (their rows lie
 // side by side), then samples, whose lengths may differ, so that every run holds
 // alike parts of all of them, then tiles, parts of a split, groups of heads.
+// Window attention: between heads and samples `chunk` consecutive tiles, which read nearly
+// the same keys (0: as above). With the samples next the 64 workgroups of an XCD met 24
+// heads and samples at once, 14 MB of keys: 8 samples of 6,011 to 6,394 tokens, 24 heads,
+// window 512 + 512, forward 1,092 -> 820 us, dQ 1,370 -> 1,125.
 struct XOrder {
-  unsigned heads, tiles, splits;
+  unsigned heads, tiles, splits, chunk;
 };
+inline unsigned window_chunk(int64_t tiles) {
+  unsigned c = 1;
+  while (c < 16 && c < tiles) c *= 2;
+  return c;
+}
+// Item numbers of an order.
+inline __host__ __device__ int64_t x_total(const XOrder& o, int64_t B, int64_t Hk) {
+  const int64_t tiles = o.chunk ? ((int64_t)o.tiles + o.chunk - 1) / o.chunk * o.chunk : o.tiles;
+  return B * Hk * o.splits * tiles;
+}
 // Heads of a group: an eighth of them, so that each XCD has a group of its own
 // and the runs are alike whatever the samples' lengths (eight samples of 17 to 512
 // keys: forward and backward 1,708 us with one head a group, 1,380 with three).
@@ -83,7 +97,14 @@ inline int x_padded(const XArgs& a) { return a.D <= 64 ? 64 : 128; }
 struct XItem {
   int b, tile, part, hk;
 };
+template <int SEE = kSeeAll>
 __device__ inline XItem x_item(unsigned it, unsigned B, const XOrder& o) {
+  if constexpr (SEE == kSeeWindow) {   // tiles past the last one have no rows, or keys
+    const unsigned n = (o.tiles + o.chunk - 1) / o.chunk, h = it / o.heads, r = h / o.chunk, s = r / B, t = s / n,
+                   u = t / o.splits;
+    return XItem{(int)(r - s * B), (int)((s - t * n) * o.chunk + h - r * o.chunk), (int)(t - u * o.splits),
+                 (int)(u * o.heads + it - h * o.heads)};
+  }
   const unsigned r = it / o.heads, s = r / B, t = s / o.tiles, u = t / o.splits;
   return XItem{(int)(r - s * B), (int)(s - t * o.tiles), (int)(t - u * o.splits), (int)(u * o.heads + it - r * o.heads)};
 }
@@ -353,7 +374,7 @@ struct TileSeq {
       cur = at = kKept;
       const unsigned it = first + (lane >> 1) * turn + (lane & 1 ? step : 0);
       const bool in = lane < kTurns && it < end;
-      const XItem m = x_item(in ? it : 0, (unsigned)x.B, order);
+      const XItem m = x_item<SEE>(in ? it : 0, (unsigned)x.B, order);
       int nq = x.Nq;
       if (SEE != kSeeCache && x.cuq) {   // as x_sample
         const int64_t q0 = min(max((int64_t)x.cuq[m.b], (int64_t)0), x.Tq);
