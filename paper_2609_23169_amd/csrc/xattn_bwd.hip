@@ -277,7 +277,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
   };
 
   // A workgroup's items in turn, their tiles as one sequence, as in the forward.
-  seq.begin(x_items((unsigned)x_total(order, a.B, a.Hk)));
+  seq.begin(x_items(order.total));
   bool have = false;   // a tile lies in the current stage
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
@@ -378,16 +378,17 @@ __global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kerne
     x_clear_rest(a.cuk, a.B, a.Tk, a.Hk * a.D, a.dk, a.sdk);
     x_clear_rest(a.cuk, a.B, a.Tk, a.Hk * a.D, a.dv, a.sdv);
   }
-  const XItems items = x_items((unsigned)x_total(order, a.B, a.Hk));
+  const XItems items = x_items(order.total);
   if (items.first >= items.end) return;
   const XItem at = x_item<WIN ? kSeeWindow : kSeeAll>(items.first, (unsigned)a.B, order);
   if (WIN && (unsigned)at.tile >= order.tiles) return;   // uniform over the workgroup
   unsigned kt = at.tile, sp = at.part, splits = order.splits;
   if constexpr (WIN) {   // units of work: the parts of the tiles with sinks, then those of the others
-    const unsigned u = at.tile, m = sinks.tiles * sinks.splits;
+    const unsigned u = at.tile, first = sinks.tiles, m = first * (unsigned)sinks.splits, r = u < m ? u : u - m;
     splits = u < m ? sinks.splits : sinks.others;
-    kt = u < m ? u / splits : sinks.tiles + (u - m) / splits;
-    sp = u < m ? u % splits : (u - m) % splits;
+    kt = div_by(r, splits);
+    sp = r - kt * splits;
+    kt += u < m ? 0 : first;
   }
   const int hk = at.hk;
   const XSample sm = x_sample(a, at.b);
@@ -403,7 +404,7 @@ __global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kerne
     t_end = sink ? sm.nq : max(min(min(key0 + kBwdKeys, sm.nk) + a.left - off, sm.nq), t_first);
   }
   const int ttiles = (t_end - t_first + kRowTile - 1) / kRowTile, all = ttiles * a.G;
-  const int per = (all + (int)splits - 1) / (int)splits;
+  const int per = (int)div_by((unsigned)all + splits - 1, splits);
   const int s_begin = min((int)sp * per, all), s_end = min(s_begin + per, all);
 
   f32x4 dk[DT][2], dv[DT][2];   // [dt][kg]: lane holds X^T[16 dt + 4 gq + (0..3)][key 32 w + 16 kg + c16]
@@ -610,6 +611,25 @@ __global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kerne
     else walk(std::false_type{});
   }
 
+  // Whole rows, through the rows of V in LDS that the wave alone has read: the pieces of 8
+  // bytes that follow the accumulators' layout took 5 us of a workgroup's 35 to 130.
+  if constexpr (WIN)
+    if (!part && !(kt < sinks.tiles && sinks.part)) {   // uniform
+      bool used[2];
+#pragma unroll
+      for (int kg = 0; kg < 2; ++kg) {
+        const int key = key0 + 32 * w + 16 * kg + c16;
+        used[kg] = key < sm.nk && (!a.mask || a.mask[sm.k0 + key]);
+      }
+      char* const rows = vblk_lds + 32 * w * ROWB;
+      if (key0 + 32 * w < sm.nk) {   // uniform
+        x_store_rows<DP>(a.dk, sm.k0, a.sdk, (int64_t)hk * a.D, key0 + 32 * w, sm.nk, 1, a.D, rows, rows + 16 * ROWB,
+                         [&](int dt, int kg) { return used[kg] ? dk[dt][kg] * a.scale : f32x4{}; });
+        x_store_rows<DP>(a.dv, sm.k0, a.sdv, (int64_t)hk * a.D, key0 + 32 * w, sm.nk, 1, a.D, rows, rows + 16 * ROWB,
+                         [&](int dt, int kg) { return used[kg] ? dv[dt][kg] : f32x4{}; });
+      }
+      return;
+    }
 #pragma unroll
   for (int kg = 0; kg < 2; ++kg) {
     const int key = key0 + 32 * w + 16 * kg + c16;
@@ -750,10 +770,10 @@ SinkParts sink_parts(const XArgs& a) {
   p.splits = std::max<int64_t>(p.others, std::min<int64_t>((all + per - 1) / per, 64));
   return p;
 }
-XOrder dkdv_order(const XArgs& a) {   // window attention: the units of work of a key head of a sample
+int64_t dkdv_units(const XArgs& a) {   // window attention: units of work of a key head of a sample
   const SinkParts p = sink_parts(a);
-  const int64_t tiles = ((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys, units = p.tiles * p.splits + (tiles - p.tiles) * p.others;
-  return XOrder{1, (unsigned)units, 1, window_chunk(units)};
+  const int64_t tiles = ((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys;
+  return p.tiles * p.splits + (tiles - p.tiles) * p.others;
 }
 size_t aux_bytes(const XArgs& a) { return ((size_t)a.Tq * a.Hq * 2 * sizeof(float) + 255) / 256 * 256; }
 size_t dq_part(const XArgs& a) {
@@ -774,7 +794,8 @@ size_t sink_part(const XArgs& a) {
 
 template <int DP, bool WIN>
 void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t s) {
-  const XOrder order{head_group(a), (unsigned)dq_tiles(a), (unsigned)splits, WIN ? window_chunk(dq_tiles(a)) : 0};
+  const XOrder order = WIN ? window_order(head_group(a), a.B, a.Hk, dq_tiles(a), splits)
+                           : x_order(head_group(a), a.B, a.Hk, dq_tiles(a), splits);
   const int64_t items = dq_groups(a) * splits;
   const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, kDqWaves)) + 7) / 8 * 8);
   TraceScope ts_(s, WIN ? "swattn_dq" : "xattn_dq", DP);
@@ -783,9 +804,9 @@ void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t 
 template <int DP, bool WIN>
 void launch_dkdv(const XArgs& a, const float* aux, float* part, const SinkParts& sinks, hipStream_t s) {
   const int64_t tiles = ((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys;
-  const XOrder order = WIN ? dkdv_order(a) : XOrder{head_group(a), (unsigned)tiles, (unsigned)sinks.others, 0};
+  const XOrder order = WIN ? window_order(1, a.B, a.Hk, dkdv_units(a), 1) : x_order(head_group(a), a.B, a.Hk, tiles, sinks.others);
   TraceScope ts_(s, WIN ? "swattn_dkdv" : "xattn_dkdv", DP);
-  const dim3 grid((unsigned)(std::max<int64_t>(x_total(order, a.B, a.Hk), 1) + 7) / 8 * 8);
+  const dim3 grid((unsigned)(std::max<int64_t>(order.total, 1) + 7) / 8 * 8);
   hipLaunchKernelGGL((xattn_dkdv_kernel<DP, WIN>), grid, dim3(256), 0, s, a, aux, order, part, sinks);
 }
 void launch_sums(const Join* j, int n, int B, hipStream_t s) {
@@ -812,7 +833,7 @@ bool xattn_bwd_launchable(const XArgs& a) {
   constexpr int64_t kMost = (int64_t)1 << 24;   // workgroups of 256 threads
   int64_t sums = std::max(dq_part(a) > 0 ? a.Tq * a.Hq : 0, dkdv_part(a) > 0 ? a.Tk * a.Hk : 0) * a.D;
   if (sink_part(a) > 0) sums = std::max(sums, (int64_t)a.B * sink_parts(a).tiles * kBwdKeys * a.Hk * a.D);
-  return ((a.window ? x_total(dkdv_order(a), a.B, a.Hk) : dkdv_groups(a)) + 7) / 8 * 8 < kMost &&
+  return ((a.window ? window_total(a.B, a.Hk, std::max<int64_t>(dkdv_units(a), 1), 1) : dkdv_groups(a)) + 7) / 8 * 8 < kMost &&
          (sums / 4 + 255) / 256 < kMost;
 }
 

@@ -311,7 +311,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     seq.begin(cache_share(a, (int)blockIdx.x, (int)gridDim.x, a.Hk * (int)order.tiles,
                           blockIdx.x == 0 && w == 0 ? parts.cuts : nullptr));
   else
-    seq.begin(x_items((unsigned)x_total(order, a.B, a.Hk)));
+    seq.begin(x_items(order.total));
   bool have = false;   // a tile lies in the current stage
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
@@ -593,7 +593,8 @@ int64_t stats_of(const XArgs& a) { return a.Tq * a.Hq; }
 template <int DP, int NW, int SEE>
 void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
   const int64_t tiles = ((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW);
-  const XOrder order{head_group(a), (unsigned)tiles, (unsigned)splits, SEE == kSeeWindow ? window_chunk(tiles) : 0};
+  const XOrder order = SEE == kSeeWindow ? window_order(head_group(a), a.B, a.Hk, tiles, splits)
+                                         : x_order(head_group(a), a.B, a.Hk, tiles, splits);
   const int64_t items = (int64_t)a.B * a.Hk * order.tiles * splits;
   const dim3 grid(SEE == kSeeCache && splits > 1
                       ? (unsigned)x_resident(DP, NW)

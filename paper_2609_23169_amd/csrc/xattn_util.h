@@ -66,17 +66,26 @@ __device__ inline XItems x_items(unsigned total) {
 // heads and samples at once, 14 MB of keys: 8 samples of 6,011 to 6,394 tokens, 24 heads,
 // window 512 + 512, forward 1,092 -> 820 us, dQ 1,370 -> 1,125.
 struct XOrder {
-  unsigned heads, tiles, splits, chunk;
+  unsigned heads, tiles, splits, total;   // total: item numbers
+  unsigned shift, chunks;                 // window attention: log2 of a chunk, chunks of a sample
 };
-inline unsigned window_chunk(int64_t tiles) {
-  unsigned c = 1;
-  while (c < 16 && c < tiles) c *= 2;
-  return c;
+inline XOrder x_order(unsigned heads, int64_t B, int64_t Hk, int64_t tiles, int64_t splits) {
+  return XOrder{heads, (unsigned)tiles, (unsigned)splits, (unsigned)(B * Hk * tiles * splits), 0, 0};
 }
-// Item numbers of an order.
-inline __host__ __device__ int64_t x_total(const XOrder& o, int64_t B, int64_t Hk) {
-  const int64_t tiles = o.chunk ? ((int64_t)o.tiles + o.chunk - 1) / o.chunk * o.chunk : o.tiles;
-  return B * Hk * o.splits * tiles;
+inline int window_shift(int64_t tiles) { return tiles >= 9 ? 4 : tiles >= 5 ? 3 : tiles >= 3 ? 2 : tiles == 2 ? 1 : 0; }
+inline int64_t window_total(int64_t B, int64_t Hk, int64_t tiles, int64_t splits) {
+  const int shift = window_shift(tiles);
+  return B * Hk * splits * (((tiles - 1) >> shift) + 1 << shift);
+}
+inline XOrder window_order(unsigned heads, int64_t B, int64_t Hk, int64_t tiles, int64_t splits) {
+  const int shift = window_shift(tiles);
+  return XOrder{heads, (unsigned)tiles, (unsigned)splits, (unsigned)window_total(B, Hk, tiles, splits), (unsigned)shift,
+                (unsigned)((tiles - 1) >> shift) + 1};
+}
+// x / d; a division takes some forty instructions.
+__device__ inline unsigned div_by(unsigned x, unsigned d) {
+  if (d == 1) return x;   // uniform
+  return x / d;
 }
 // Heads of a group: an eighth of them, so that each XCD has a group of its own
 // and the runs are alike whatever the samples' lengths (eight samples of 17 to 512
@@ -100,9 +109,8 @@ struct XItem {
 template <int SEE = kSeeAll>
 __device__ inline XItem x_item(unsigned it, unsigned B, const XOrder& o) {
   if constexpr (SEE == kSeeWindow) {   // tiles past the last one have no rows, or keys
-    const unsigned n = (o.tiles + o.chunk - 1) / o.chunk, h = it / o.heads, r = h / o.chunk, s = r / B, t = s / n,
-                   u = t / o.splits;
-    return XItem{(int)(r - s * B), (int)((s - t * n) * o.chunk + h - r * o.chunk), (int)(t - u * o.splits),
+    const unsigned h = div_by(it, o.heads), r = h >> o.shift, s = div_by(r, B), t = div_by(s, o.chunks), u = div_by(t, o.splits);
+    return XItem{(int)(r - s * B), (int)((s - t * o.chunks << o.shift) + h - (r << o.shift)), (int)(t - u * o.splits),
                  (int)(u * o.heads + it - h * o.heads)};
   }
   const unsigned r = it / o.heads, s = r / B, t = s / o.tiles, u = t / o.splits;
