@@ -146,7 +146,6 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
   auto step = [&](uint64_t bits, int tile, const char* kt_lds, const char* vt_lds, bool swap, Extra& ex, bool loads,
                   auto load)
       __attribute__((always_inline)) {
-    const bool part = WIN && !see.whole(a, tile);   // rows of the wave differ in the keys that they see
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       f32x16 s = f32x16{}, dp = f32x16{};
@@ -188,13 +187,15 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       __builtin_amdgcn_s_setprio(0);
       const float ls = l2, nd = ndl;
       if (kt == 1 && swap) load_rows(seq.item(seq.at, order), ex);   // uniform
-      if (bits != ~(uint64_t)0 || part) {     // uniform
+      // uniform; WIN: also where rows of the wave differ in the keys that they see
+      if (bits != ~(uint64_t)0 || (WIN && !see.whole(a, kXKeys * tile + 32 * kt))) {
         unsigned mine = (unsigned)(bits >> (32 * kt));
         if constexpr (WIN) mine &= see.bits(a, kXKeys * tile + 32 * kt);
         mine >>= 4 * g;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          s[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[e] : -INFINITY;
+          if constexpr (WIN) s[e] = bit_or(s[e], mine, 8 * (e >> 2) + (e & 3), kMinusInf);
+          else s[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[e] : -INFINITY;
       }
       u32x4 pq[2];
 #pragma unroll
@@ -534,9 +535,8 @@ __global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kerne
           const unsigned mine = rows >> (4 * g);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {   // dP too: a key that no token sees may hold anything
-            const bool in = mine >> (8 * (e >> 2) + (e & 3)) & 1;
-            s[e] = in ? s[e] : -INFINITY;
-            dp[e] = in ? dp[e] : 0.f;
+            s[e] = bit_or(s[e], mine, 8 * (e >> 2) + (e & 3), kMinusInf);
+            dp[e] = bit_or(dp[e], mine, 8 * (e >> 2) + (e & 3), 0);
           }
         }
       u32x4 pp[2], pd[2];

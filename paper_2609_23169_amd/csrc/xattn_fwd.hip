@@ -144,16 +144,21 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[h][e]);
       return fmaxf(mx * c2, -3.0e38f);
     };
-    const bool part = SEE != kSeeAll && !see.whole(a, tile);   // rows of the wave differ in the keys that they see
+    // Whether rows of the wave differ in the keys of half h that they see: here, where it
+    // delays no product.
+    bool part[2] = {false, false};
+    if constexpr (SEE != kSeeAll) part[0] = !see.whole(a, kXKeys * tile), part[1] = !see.whole(a, kXKeys * tile + 32);
     // Before half h's exponentials: unused keys, and the item's reference.
     auto prepare = [&](int h) __attribute__((always_inline)) {
       const unsigned half = (unsigned)(bits >> (32 * h));
-      if (half != ~0u || part) {   // uniform
+      if (half != ~0u || part[h]) {   // uniform
         unsigned mine = half;
         if constexpr (SEE != kSeeAll) mine &= see.bits(a, kXKeys * tile + 32 * h);
         mine >>= 4 * g;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[h][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[h][e] : -INFINITY;
+        for (int e = 0; e < 16; ++e)
+          if constexpr (SEE == kSeeAll) s[h][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[h][e] : -INFINITY;
+          else s[h][e] = bit_or(s[h][e], mine, 8 * (e >> 2) + (e & 3), kMinusInf);
       }
       if (fresh && half) {   // uniform
         m_run = pair_max(half_max(h));

@@ -266,6 +266,13 @@ __device__ inline XSpan x_span(const XArgs& a, const XSample& sm, int r0, int n)
   return s;
 }
 
+// x where bit i of the word is set, else `other`: two instructions.
+__device__ inline float bit_or(float x, unsigned word, int i, unsigned other) {
+  const unsigned m = (unsigned)__builtin_amdgcn_sbfe((int)word, i, 1);
+  return __uint_as_float((__float_as_uint(x) & m) | (other & ~m));
+}
+constexpr unsigned kMinusInf = 0xff800000u;
+
 // What a lane's row sees: the tiles that a wave does not see whole take a mask a row.
 template <int SEE>
 struct RowWindow {
@@ -290,12 +297,12 @@ struct RowWindow {
   __device__ inline int sinks(const XArgs& a, int stop) const {
     return SEE == kSeeWindow && a.right > 0 ? a.sinks : min(a.sinks, stop);
   }
-  // Whether every row of the wave sees all keys of a tile (uniform). The rows'
+  // Whether every row of the wave sees all 32 keys from k on (uniform). The rows'
   // positions ascend from lane 0 to lane 31; in a tree they lie within Nq.
-  __device__ inline bool whole(const XArgs& a, int tile) const {
-    const int k = kXKeys * tile, first = __builtin_amdgcn_readfirstlane(stop(a, p));
+  __device__ inline bool whole(const XArgs& a, int k) const {
+    const int first = __builtin_amdgcn_readfirstlane(stop(a, p));
     const int last = SEE == kSeeCache && a.tree ? first + a.Nq : __builtin_amdgcn_readlane(p, 31);
-    return (k >= last - a.left && k + kXKeys <= first) || k + kXKeys <= sinks(a, first);
+    return (k >= last - a.left && k + 32 <= first) || k + 32 <= sinks(a, first);
   }
   // Keys k .. k + 31 that the row sees, a bit each (keys that the sample lacks
   // included).
