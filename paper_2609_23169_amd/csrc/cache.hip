@@ -1,6 +1,6 @@
 // What a cache of keys and values needs beside the attention that reads it, on
-// gfx950: the attention weight that every slot receives, summed over the queries,
-// and eviction of the slots that received least.
+// gfx950: the end of a split attention call, the attention weight that every slot
+// receives, summed over the queries, and eviction of the slots that received least.
 //
 // Weights: out[b, hk, j] = in[b, hk, j] + sum over the tokens t and the heads h of the
 // group of P = exp(S scale - LSE). The attention knows a row's LSE only at its end, so
@@ -30,12 +30,160 @@ namespace ut {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// How the rows of a cache call lie in its items: tiles of `per` rows of a key head.
+struct CacheRows {
+  int tiles, per;
+};
+// Parts of sample b's row `row` of key head hk, and its place in the statistics.
+__device__ inline int row_parts(const XArgs& a, const CacheParts& parts, const CacheRows& at, int b, int hk, int row) {
+  const int g = parts.heads > 0 ? hk / parts.heads : hk * at.tiles + row / at.per;
+  return cache_parts(parts.cuts[0], parts.cuts[1 + b], cache_tiles(a, b), g);
+}
+__device__ inline int64_t row_stat(const XArgs& a, int b, int hk, int row) {
+  const int t = row_token(row, a.G);
+  return ((int64_t)b * a.Hq + hk * a.G + row - t * a.G) * a.Nq + t;
+}
+// A row's LSE in log2 units from its n parts, the parts from `first` on in steps; {maximum,
+// sum} of parts that hold nothing are left out.
+__device__ inline float2 part_sums(const CacheParts& parts, int64_t stat, int n, int first, int step) {
+  float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+  for (int s = first; s < n; s += step) {
+    const float2 p = parts.sums[s * parts.stats + stat];
+    const float to = p.y == 0.f ? m : fmaxf(m, p.x);
+    l = (l == 0.f ? 0.f : l * fast_exp2(m - to)) + (p.y == 0.f ? 0.f : p.y * fast_exp2(p.x - to));
+    m = to;
+  }
+  return make_float2(m, l);
+}
+
+// The parts of rows joined: GPR groups of 32 lanes a row take every GPR-th part, four
+// columns a lane, and the groups' sums are added in LDS. Block `block` of T threads.
+template <int GPR, int T>
+__device__ inline void join_rows(const XArgs& a, const CacheParts& parts, const CacheRows& at, int block, float4* red,
+                                 float* red_l) {
+  constexpr int kRows = T / 32 / GPR;
+  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, sub = grp % GPR;
+  const int64_t r = (int64_t)block * kRows + grp / GPR;   // [B, Hq, T]
+  const bool live = r < parts.stats;
+  int64_t tok = 0;
+  int head = 0, splits = 0;
+  if (live) {
+    const int64_t bh = r / a.Nq;
+    const int b = (int)(bh / a.Hq), t = (int)(r - bh * a.Nq);
+    head = (int)(bh - (int64_t)b * a.Hq);
+    tok = (int64_t)b * a.Nq + t;
+    const int hk = head / a.G;
+    splits = row_parts(a, parts, at, b, hk, t * a.G + head - hk * a.G);
+  }
+  const bool whole = splits == 1 && parts.heads > 0;   // cache_one finishes these
+  if (whole) splits = 0;
+  float M = -INFINITY;
+  for (int s = lane; s < splits; s += 32) {
+    const float2 p = parts.sums[s * parts.stats + r];
+    M = p.y != 0.f ? fmaxf(M, p.x) : M;
+  }
+#pragma unroll
+  for (int m = 1; m < 32; m <<= 1) M = fmaxf(M, __shfl_xor(M, m, 64));
+  float L = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int s = sub; s < splits; s += GPR) {
+    const float2 p = parts.sums[s * parts.stats + r];
+    if (p.y == 0.f) continue;   // no keys in use here
+    const float f = fast_exp2(p.x - M);
+    L += p.y * f;
+    if (4 * lane < a.D) {
+      const float4 o = *reinterpret_cast<const float4*>(parts.o + (s * parts.stats + r) * a.D + 4 * lane);
+      acc.x += o.x * f, acc.y += o.y * f, acc.z += o.z * f, acc.w += o.w * f;
+    }
+  }
+  if constexpr (GPR > 1) {
+    red[threadIdx.x] = acc;
+    if (lane == 0) red_l[grp] = L;
+    __syncthreads();
+    if (sub == 0)
+      for (int k = 1; k < GPR; ++k) {
+        const float4 o = red[threadIdx.x + 32 * k];
+        acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
+        L += red_l[grp + k];
+      }
+  }
+  if (!live || sub != 0 || whole) return;
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  if (lane == 0) a.lse[r] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
+  if (4 * lane < a.D) {
+    const bf16x4 v = {(__bf16)(acc.x * inv), (__bf16)(acc.y * inv), (__bf16)(acc.z * inv), (__bf16)(acc.w * inv)};
+    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.o) + tok * a.so + head * a.D + 4 * lane) = v;
+  }
+}
+
+// The end of a cache call: its rows joined (the first `joins` workgroups), and with the
+// scores of few rows the weights that the slots receive, a workgroup 256 slots of a key
+// head; a row's maximum and sum come from its parts again, or from its LSE. The scores
+// are loaded beside them.
+template <int GPR, bool SPLIT>
+__global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const CacheRows rows_at, const int joins,
+                                                           const CacheParts parts, const CacheWeights wt) {
+  __shared__ float4 red[256];
+  __shared__ float red_l[8];
+  if (SPLIT && (int)blockIdx.x < joins) return join_rows<GPR, 256>(a, parts, rows_at, blockIdx.x, red, red_l);
+  float* const lse2 = reinterpret_cast<float*>(red);
+  const unsigned at = blockIdx.x - (SPLIT ? joins : 0), chunks = (unsigned)((a.Nk + 255) / 256);
+  const unsigned bh = at / chunks;
+  const int b = (int)(bh / (unsigned)a.Hk), hk = (int)(bh - b * a.Hk), rows = a.Nq * a.G;
+  const int key = (int)(at - bh * chunks) * 256 + threadIdx.x;
+  const float* const sc = parts.scores + (int64_t)bh * rows * score_keys(a) + min(key, a.Nk - 1);
+  const int64_t to = (int64_t)bh * a.Nk + key;
+  constexpr int kEarly = 8;   // rows whose scores are loaded at once; what lies there may be anything
+  float early[kEarly];
+#pragma unroll
+  for (int r = 0; r < kEarly; ++r) early[r] = sc[(int64_t)min(r, rows - 1) * score_keys(a)];
+  const float before = wt.in && key < a.Nk ? wt.in[to] : 0.f;
+  const int row = threadIdx.x >> 3, sub = threadIdx.x & 7;   // eight lanes a row
+  if (row < rows) {
+    const int64_t stat = row_stat(a, b, hk, row);
+    const int n = SPLIT ? row_parts(a, parts, rows_at, b, hk, row) : 1;
+    float m;
+    if (n > 1) {
+      float2 p = part_sums(parts, stat, n, sub, 8);
+#pragma unroll
+      for (int x = 1; x < 8; x <<= 1) {
+        const float mo = __shfl_xor(p.x, x, 64), lo = __shfl_xor(p.y, x, 64), top = fmaxf(p.x, mo);
+        p.y = (p.y == 0.f ? 0.f : p.y * fast_exp2(p.x - top)) + (lo == 0.f ? 0.f : lo * fast_exp2(mo - top));
+        p.x = top;
+      }
+      m = p.y == 0.f ? -INFINITY : p.x + __log2f(p.y);
+    } else {   // finished by its workgroup
+      m = a.lse[stat] * kLog2e;
+    }
+    if (sub == 0) lse2[row] = m == -INFINITY ? INFINITY : m;   // no keys: P = 0
+  }
+  __syncthreads();
+  if (key >= a.Nk) return;
+  const XSample sm = x_sample<kSeeCache>(a, b);
+  const XSpan span = x_span<kSeeCache>(a, sm, 0, rows);
+  float sum = 0.f;
+  if (key < sm.nk && span.has(key / kXKeys)) {
+#pragma unroll
+    for (int r = 0; r < kEarly; ++r) sum += r < rows ? fast_exp2(early[r] - lse2[r]) : 0.f;
+#pragma unroll 4
+    for (int r = kEarly; r < rows; ++r) sum += fast_exp2(sc[(int64_t)r * score_keys(a)] - lse2[r]);
+  }
+  wt.out[to] = before + sum;
+}
+
 constexpr int kWWaves = 8;    // of a workgroup: at 128 columns 64 KB of keys and 48 KB of rows, one workgroup a CU
 constexpr int kWRows = 192;   // rows in LDS, a multiple of 64
 constexpr int kWTiles = 8;    // most tiles of 32 keys of a wave
 
-template <int DP>
-__global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XArgs a, const CacheWeights c, const int per_wave) {
+// JOIN: the rows' parts are not joined yet. The workgroups behind the first `weigh` join
+// them, and the others take the rows' LSE from the parts' sums.
+template <int DP, bool JOIN>
+__global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XArgs a, const CacheWeights c, const int per_wave,
+                                                                        const CacheRows rows_at, const CacheParts parts,
+                                                                        const int weigh) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, KS = DP / 16;
   constexpr int KI = 32 * ROWB / 1024;   // direct loads of a tile
   __shared__ __attribute__((aligned(1024))) char k_lds[kWWaves * 32 * ROWB];
@@ -48,6 +196,8 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XA
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned hk = blockIdx.x % (unsigned)a.Hk, rest = blockIdx.x / (unsigned)a.Hk;
   constexpr int T = 64 * kWWaves;
+  if (JOIN && (int)blockIdx.x >= weigh)
+    return join_rows<1, T>(a, parts, rows_at, blockIdx.x - weigh, nullptr, nullptr);
   const int keys = 32 * kWWaves * per_wave;   // of the workgroup
   const unsigned chunks = (unsigned)((a.Nk + keys - 1) / keys);
   const int b = (int)(rest / chunks), key0 = (int)(rest % chunks) * keys;
@@ -102,7 +252,12 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XA
       // rows that are not counted, and rows without keys: P = 0
       float l = INFINITY;
       if (row < rows && (!c.tokens || c.tokens[b] >> tok & 1)) {
-        l = a.lse[sm.stat0 + (hk * a.G + row - tok * a.G) * sm.hstep + tok] * kLog2e;
+        if constexpr (JOIN) {
+          const float2 p = part_sums(parts, row_stat(a, b, hk, row), row_parts(a, parts, rows_at, b, hk, row), 0, 1);
+          l = p.y == 0.f ? -INFINITY : p.x + __log2f(p.y);
+        } else {
+          l = a.lse[row_stat(a, b, hk, row)] * kLog2e;
+        }
         if (l == -INFINITY) l = INFINITY;
       }
       lse_lds[tid] = l;
@@ -397,16 +552,81 @@ __global__ __launch_bounds__(256) void cache_move_kernel(const CacheEvict a, con
 
 }  // namespace
 
-hipError_t launch_cache_weights(const XArgs& a, const CacheWeights& c, hipStream_t s) {
+// Workspace of a cache call: the parts' O and sums, how items are cut, the scores.
+namespace {
+struct CacheSpace {
+  size_t o, sums, cuts, scores;   // bytes
+};
+CacheSpace cache_space(const XArgs& a) {
+  const int splits = cache_shape(a).splits;
+  const int64_t stats = a.Tq * a.Hq;
+  CacheSpace c{};
+  if (splits > 1) {
+    c.o = (size_t)splits * stats * a.D * sizeof(float);
+    c.sums = ((size_t)splits * stats * sizeof(float2) + 15) / 16 * 16;
+    c.cuts = ((size_t)a.B + 1 + 3) / 4 * 4 * sizeof(int);
+  }
+  if (a.scores) c.scores = (size_t)stats * score_keys(a) * sizeof(float);
+  return c;
+}
+
+template <bool JOIN>
+hipError_t launch_weights(const XArgs& a, const CacheWeights& c, const CacheRows& rows, const CacheParts& parts,
+                          hipStream_t s) {
   // as many tiles a wave as leave a workgroup for each CU
   const int64_t heads = (int64_t)a.B * a.Hk, keys = 32 * kWWaves, blocks = ((int64_t)a.Nk + keys - 1) / keys;
   const int per_wave = (int)std::max<int64_t>(1, std::min<int64_t>(kWTiles, (heads * blocks + 255) / 256));
-  const int64_t chunks = ((int64_t)a.Nk + keys * per_wave - 1) / (keys * per_wave);
+  const int64_t weigh = heads * (((int64_t)a.Nk + keys * per_wave - 1) / (keys * per_wave));
+  const int64_t joins = JOIN ? (parts.stats + 2 * kWWaves - 1) / (2 * kWWaves) : 0;
   TraceScope ts_(s, "cache_weights", x_padded(a));
-  const dim3 grid((unsigned)(heads * chunks));
-  if (a.D <= 64) hipLaunchKernelGGL(cache_weights_kernel<64>, grid, dim3(64 * kWWaves), 0, s, a, c, per_wave);
-  else hipLaunchKernelGGL(cache_weights_kernel<128>, grid, dim3(64 * kWWaves), 0, s, a, c, per_wave);
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(weigh + joins)), dim3(64 * kWWaves), 0, s, a, c, per_wave, rows, parts, (int)weigh);
+  };
+  a.D <= 64 ? launch(cache_weights_kernel<64, JOIN>) : launch(cache_weights_kernel<128, JOIN>);
   return hipGetLastError();
+}
+}  // namespace
+
+size_t cache_attn_workspace(const XArgs& a) {
+  const CacheSpace c = cache_space(a);
+  return c.o + c.sums + c.cuts + c.scores;
+}
+
+hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* workspace, hipStream_t s) {
+  const XShape shape = cache_shape(a);
+  const CacheSpace c = cache_space(a);
+  char* const at = static_cast<char*>(workspace);
+  const bool few = a.Nq * a.G <= kScoreRows, split = shape.splits > 1;
+  const CacheParts parts{reinterpret_cast<float2*>(at + c.o), reinterpret_cast<float*>(at), a.Tq * a.Hq,
+                         reinterpret_cast<int*>(at + c.o + c.sums), reinterpret_cast<float*>(at + c.o + c.sums + c.cuts),
+                         few ? cache_heads(a) : 0};
+  const int per = few ? kScoreRows : 32 * shape.waves;
+  const CacheRows rows{(int)(((int64_t)a.Nq * a.G + per - 1) / per), per};
+  if (few) {
+    // no item is cut, and the weights are few enough for the workgroup that has the scores
+    const bool weights_here = !split && a.scores && a.Nk <= 2048;
+    if (hipError_t e = launch_cache_one(a, parts, w, weights_here, s); e != hipSuccess) return e;
+    if (!split && (!a.scores || weights_here)) return hipSuccess;
+  } else {
+    if (hipError_t e = launch_cache_fwd(a, shape, parts, s); e != hipSuccess) return e;
+    if (w.out) return split ? launch_weights<true>(a, w, rows, parts, s) : launch_weights<false>(a, w, rows, parts, s);
+    if (!split) return hipSuccess;
+  }
+  // Eight groups of lanes a row where many parts are to be read for few rows, as in
+  // cross attention.
+  const bool many = shape.splits >= 8 && parts.stats <= 4096;
+  const int64_t joins = split ? (parts.stats + (many ? 0 : 7)) / (many ? 1 : 8) : 0;
+  const int64_t chunks = a.scores ? (int64_t)a.B * a.Hk * (((int64_t)a.Nk + 255) / 256) : 0;
+  TraceScope ts_(s, "cache_finish");
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(joins + chunks)), dim3(256), 0, s, a, rows, (int)joins, parts, w);
+  };
+  !split ? launch(cache_finish_kernel<1, false>) : many ? launch(cache_finish_kernel<8, true>) : launch(cache_finish_kernel<1, true>);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_weights(const XArgs& a, const CacheWeights& c, hipStream_t s) {
+  return launch_weights<false>(a, c, CacheRows{}, CacheParts{}, s);
 }
 
 hipError_t launch_cache_evict(const CacheEvict& a, hipStream_t s) {

@@ -450,148 +450,19 @@ __global__ __launch_bounds__(256) void xattn_join_kernel(const XArgs a, const in
   }
 }
 
-// The end of a cache call: the parts of its rows joined, as above (SPLIT), and with
-// scores the weights that the slots receive, a workgroup 256 slots of a key head: a
-// row's maximum and sum come from its parts again, or from its LSE.
-template <int GPR, bool SPLIT>
-__global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const int tiles, const int rows_per_item,
-                                                           const int joins, const Parts parts, const CacheWeights wt) {
-  __shared__ float4 red[256];
-  __shared__ float red_l[8];
-  // Parts of sample b's item g.
-  auto count = [&](int b, int g) __attribute__((always_inline)) {
-    return cache_parts(parts.cuts[0], parts.cuts[1 + b], cache_tiles(a, b), g);
-  };
-  if (SPLIT && (int)blockIdx.x < joins) {
-    constexpr int kRows = 8 / GPR;
-    const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, sub = grp % GPR;
-    const int64_t r = (int64_t)blockIdx.x * kRows + grp / GPR;   // [B, Hq, T]
-    const bool live = r < parts.stats;
-    int64_t tok = 0;
-    int head = 0, splits = 0;
-    if (live) {
-      const int64_t bh = r / a.Nq;
-      const int b = (int)(bh / a.Hq), t = (int)(r - bh * a.Nq);
-      head = (int)(bh - (int64_t)b * a.Hq);
-      tok = (int64_t)b * a.Nq + t;
-      const int hk = head / a.G;
-      splits = count(b, parts.heads > 0 ? hk / parts.heads : hk * tiles + (t * a.G + head - hk * a.G) / rows_per_item);
-    }
-    const bool whole = splits == 1 && parts.heads > 0;   // cache_one finishes these
-    if (whole) splits = 0;
-    float M = -INFINITY;
-    for (int s = lane; s < splits; s += 32) {
-      const float2 p = parts.sums[s * parts.stats + r];
-      M = p.y != 0.f ? fmaxf(M, p.x) : M;
-    }
-#pragma unroll
-    for (int m = 1; m < 32; m <<= 1) M = fmaxf(M, __shfl_xor(M, m, 64));
-    float L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int s = sub; s < splits; s += GPR) {
-      const float2 p = parts.sums[s * parts.stats + r];
-      if (p.y == 0.f) continue;   // no keys in use here
-      const float f = fast_exp2(p.x - M);
-      L += p.y * f;
-      if (4 * lane < a.D) {
-        const float4 o = *reinterpret_cast<const float4*>(parts.o + (s * parts.stats + r) * a.D + 4 * lane);
-        acc.x += o.x * f, acc.y += o.y * f, acc.z += o.z * f, acc.w += o.w * f;
-      }
-    }
-    if constexpr (GPR > 1) {
-      red[threadIdx.x] = acc;
-      if (lane == 0) red_l[grp] = L;
-      __syncthreads();
-      if (sub == 0)
-        for (int k = 1; k < GPR; ++k) {
-          const float4 o = red[threadIdx.x + 32 * k];
-          acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
-          L += red_l[grp + k];
-        }
-    }
-    if (!live || sub != 0) return;
-    if (whole) return;   // finished by its workgroup
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    if (lane == 0) a.lse[r] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
-    if (4 * lane < a.D) {
-      const bf16x4 v = {(__bf16)(acc.x * inv), (__bf16)(acc.y * inv), (__bf16)(acc.z * inv), (__bf16)(acc.w * inv)};
-      *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.o) + tok * a.so + head * a.D + 4 * lane) = v;
-    }
-    return;
-  }
-  // Weights of 256 slots. rows <= kScoreRows, so an item holds all of them.
-  float* const lse2 = reinterpret_cast<float*>(red);
-  const unsigned at = blockIdx.x - (SPLIT ? joins : 0), chunks = (unsigned)((a.Nk + 255) / 256);
-  const unsigned bh = at / chunks;
-  const int b = (int)(bh / (unsigned)a.Hk), hk = (int)(bh - b * a.Hk), rows = a.Nq * a.G;
-  const int key = (int)(at - bh * chunks) * 256 + threadIdx.x;
-  const float* const sc = parts.scores + (int64_t)bh * rows * score_keys(a) + key;
-  const int row = threadIdx.x >> 3, sub = threadIdx.x & 7;   // eight lanes a row
-  if (row < rows) {
-    const int t = row / a.G, head = hk * a.G + row - t * a.G;
-    const int64_t r = ((int64_t)b * a.Hq + head) * a.Nq + t;
-    float m = -INFINITY, l = 0.f;
-    const int n = SPLIT ? count(b, hk / parts.heads) : 1;
-    if (n > 1) {
-      for (int s = sub; s < n; s += 8) {
-        const float2 p = parts.sums[s * parts.stats + r];
-        if (p.y == 0.f) continue;   // no keys in use here
-        const float to = fmaxf(m, p.x);
-        l = l * fast_exp2(m - to) + p.y * fast_exp2(p.x - to);
-        m = to;
-      }
-#pragma unroll
-      for (int x = 1; x < 8; x <<= 1) {
-        const float mo = __shfl_xor(m, x, 64), lo = __shfl_xor(l, x, 64), to = fmaxf(m, mo);
-        l = (l == 0.f ? 0.f : l * fast_exp2(m - to)) + (lo == 0.f ? 0.f : lo * fast_exp2(mo - to));
-        m = to;
-      }
-      m += __log2f(l);
-    } else {   // finished by its workgroup
-      m = a.lse[r] * kLog2e;
-    }
-    if (sub == 0) lse2[row] = m == -INFINITY || m != m ? INFINITY : m;   // no keys: P = 0
-  }
-  __syncthreads();
-  if (key >= a.Nk) return;
-  const XSample sm = x_sample<kSeeCache>(a, b);
-  const XSpan span = x_span<kSeeCache>(a, sm, 0, rows);
-  float sum = 0.f;
-  if (key < sm.nk && span.has(key / kXKeys)) {
-#pragma unroll 4
-    for (int r = 0; r < rows; ++r) sum += fast_exp2(sc[(int64_t)r * score_keys(a)] - lse2[r]);
-  }
-  const int64_t to = (int64_t)bh * a.Nk + key;
-  wt.out[to] = (wt.in ? wt.in[to] : 0.f) + sum;
-}
-
 // Parts of the keys, and waves of a workgroup: four, or one where up to 32 rows meet
 // split keys (4 rows of 4 x 8 key heads on 16,391 keys: 49 us against 51 with three
 // idle waves beside; unsplit keys the other way round, 14.2 against 13.0 for 16
 // samples of 20 rows and 300 keys). Parts below four tiles: the last case split in two
 // takes 11.7 + 6.4, 16 samples of 60 rows 15.9 + 7.5 against 16.2.
-struct Shape {
-  int splits, waves;
-};
-Shape fwd_shape(const XArgs& a) {
+XShape fwd_shape(const XArgs& a) {
   const int64_t rows = (int64_t)a.Nq * a.G, heads = (int64_t)a.B * a.Hk;
-  if (a.lens) {   // shared out by cache_share where the items would not fill the chip
-    const int waves = rows <= 128 || a.D <= 64 ? 4 : 8;
-    const bool few = rows <= kScoreRows;   // cache_one.hip
-    const int wgs = few ? kCacheOneGroups : (int)x_resident(x_padded(a), waves), least = cache_least(a);
-    const int64_t groups = few ? a.Hk / cache_heads(a) : (int64_t)a.Hk * ((rows + 32 * waves - 1) / (32 * waves));
-    const int64_t tiles = x_item_tiles(a, (int)std::min<int64_t>(rows, INT32_MAX));
-    if (few ? tiles <= least && a.B * groups <= wgs : a.B * groups >= wgs || tiles < 2 * least) return Shape{1, 4};
-    // parts of an item, at most: of its tiles by what a workgroup takes, and one more
-    return Shape{(int)std::min((tiles + least - 1) / least, (wgs + groups - 1) / groups) + 1, waves};
-  }
   auto splits = [&](int nw) {
     const int64_t groups = heads * ((rows + 32 * nw - 1) / (32 * nw)), tiles = x_item_tiles(a, 32 * nw);
     return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), nw) / groups, tiles / 4));
   };
-  if (rows <= 32 && splits(1) > 1) return Shape{splits(1), 1};
-  return Shape{splits(4), 4};
+  if (rows <= 32 && splits(1) > 1) return XShape{splits(1), 1};
+  return XShape{splits(4), 4};
 }
 int64_t stats_of(const XArgs& a) { return a.Tq * a.Hq; }
 
@@ -659,64 +530,21 @@ hipError_t launch_xattn_fwd(const XArgs& a, void* workspace, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Workspace of a cache call: the parts' O and sums, how items are cut, the scores.
-namespace {
-struct CacheSpace {
-  size_t o, sums, cuts, scores;   // bytes
-};
-CacheSpace cache_space(const XArgs& a) {
-  const int splits = fwd_shape(a).splits;
-  CacheSpace c{};
-  if (splits > 1) {
-    c.o = (size_t)splits * stats_of(a) * a.D * sizeof(float);
-    c.sums = (size_t)splits * stats_of(a) * sizeof(float2);
-    c.cuts = ((size_t)a.B + 1 + 3) / 4 * 4 * sizeof(int);
-  }
-  if (a.scores) c.scores = (size_t)a.B * a.Hq * a.Nq * score_keys(a) * sizeof(float);
-  // 16-byte pieces: sums and starts end on one
-  c.sums = (c.sums + 15) / 16 * 16;
-  return c;
-}
-}  // namespace
-
-size_t cache_attn_workspace(const XArgs& a) {
-  const CacheSpace c = cache_space(a);
-  return c.o + c.sums + c.cuts + c.scores;
+XShape cache_shape(const XArgs& a) {   // shared out by cache_share where the items would not fill the chip
+  const int64_t rows = (int64_t)a.Nq * a.G;
+  const int waves = rows <= 128 || a.D <= 64 ? 4 : 8;
+  const bool few = rows <= kScoreRows;   // cache_one.hip
+  const int wgs = few ? kCacheOneGroups : (int)x_resident(x_padded(a), waves), least = cache_least(a);
+  const int64_t groups = few ? a.Hk / cache_heads(a) : (int64_t)a.Hk * ((rows + 32 * waves - 1) / (32 * waves));
+  const int64_t tiles = x_item_tiles(a, (int)std::min<int64_t>(rows, INT32_MAX));
+  if (few ? tiles <= least && a.B * groups <= wgs : a.B * groups >= wgs || tiles < 2 * least) return XShape{1, 4};
+  // parts of an item, at most: of its tiles by what a workgroup takes, and one more
+  return XShape{(int)std::min((tiles + least - 1) / least, (wgs + groups - 1) / groups) + 1, waves};
 }
 
-hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* workspace, hipStream_t s) {
-  const auto [splits, waves] = fwd_shape(a);
-  const CacheSpace c = cache_space(a);
-  char* const at = static_cast<char*>(workspace);
-  const Parts parts{reinterpret_cast<float2*>(at + c.o), reinterpret_cast<float*>(at), stats_of(a),
-                    reinterpret_cast<int*>(at + c.o + c.sums), reinterpret_cast<float*>(at + c.o + c.sums + c.cuts),
-                    a.Nq * a.G <= kScoreRows ? cache_heads(a) : 0};
-  const bool few = a.Nq * a.G <= kScoreRows;
-  // no item is cut, and the weights are few enough for the workgroup that has the scores
-  const bool weights_here = few && splits == 1 && a.scores && a.Nk <= 2048;
-  if (few) {
-    if (hipError_t e = launch_cache_one(a, parts, w, weights_here, s); e != hipSuccess) return e;
-  } else {
-    launch_fwd<kSeeCache>(a, splits, waves, parts, s);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  }
-  const bool many = splits >= 8 && parts.stats <= 4096;   // as xattn_join
-  const int64_t joins = splits > 1 ? (parts.stats + (many ? 0 : 7)) / (many ? 1 : 8) : 0;
-  const int64_t chunks = a.scores && !weights_here ? (int64_t)a.B * a.Hk * (((int64_t)a.Nk + 255) / 256) : 0;
-  if (joins + chunks > 0) {
-    TraceScope ts_(s, "cache_finish");
-    const int rows = few ? kScoreRows : 32 * waves;
-    const int tiles = (int)(((int64_t)a.Nq * a.G + rows - 1) / rows);
-    const dim3 grid((unsigned)(joins + chunks));
-    if (splits == 1)
-      hipLaunchKernelGGL((cache_finish_kernel<1, false>), grid, dim3(256), 0, s, a, tiles, rows, 0, parts, w);
-    else if (many)
-      hipLaunchKernelGGL((cache_finish_kernel<8, true>), grid, dim3(256), 0, s, a, tiles, rows, (int)joins, parts, w);
-    else
-      hipLaunchKernelGGL((cache_finish_kernel<1, true>), grid, dim3(256), 0, s, a, tiles, rows, (int)joins, parts, w);
-  }
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  return w.out && !a.scores ? launch_cache_weights(a, w, s) : hipSuccess;
+hipError_t launch_cache_fwd(const XArgs& a, const XShape& shape, const CacheParts& parts, hipStream_t s) {
+  launch_fwd<kSeeCache>(a, shape.splits, shape.waves, parts, s);
+  return hipGetLastError();
 }
 
 }  // namespace ut

@@ -573,6 +573,12 @@ struct CacheParts {
   int heads;     // key heads of an item
 };
 inline __host__ __device__ int score_keys(const XArgs& a) { return (a.Nk + kXKeys - 1) / kXKeys * kXKeys; }
+// Parts of the keys (1: none) and waves of a workgroup.
+struct XShape {
+  int splits, waves;
+};
+XShape cache_shape(const XArgs& a);
+hipError_t launch_cache_fwd(const XArgs& a, const XShape& shape, const CacheParts& parts, hipStream_t s);
 constexpr int kCacheOneGroups = 256;   // workgroups of the few-rows kernel: one a CU, by its LDS
 // Few rows (cache_one.hip). weights_here: no item is cut, and each workgroup adds its items'
 // weights itself.
