@@ -718,13 +718,13 @@ ut_status ut_swattn_bwd_varlen(const void* q, const void* k, const void* v, cons
  *           weights_out[b, hk, j] = weights_in[b, hk, j] + the sum, over the T tokens and
  *           the heads of the group, of the softmax weight of slot j, for every slot (of
  *           weights_in alone where nothing sees it). weights_in NULL: zeros;
- *           weights_out may be weights_in.
+ *           weights_out may be weights_in, but not overlap it otherwise.
  * workspace as in ut_xattn_fwd, of the size query's bytes (with_weights: nonzero for
  *           a call with weights_out).
  * A token that sees no slot (a tree word of 0 in front of an empty cache): o = 0,
  * lse = -inf. No atomics: results are deterministic.
  * Errors: those of ut_xattn_fwd; T < 1 or > capacity, a tree with T > 64 or
- *         0 <= window_left < T - 1, weights_in without weights_out
+ *         0 <= window_left < T - 1, weights_in without weights_out or overlapping it
  *         -> UT_ERR_INVALID_ARG.
  * ---------------------------------------------------------------------- */
 size_t ut_cache_attn_workspace_size(int32_t B, int32_t T, int32_t capacity, int32_t Hq, int32_t Hk,

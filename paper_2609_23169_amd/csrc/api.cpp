@@ -1242,6 +1242,17 @@ bool overlap(const Range& x, const Range& y) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
   return a < b + (uintptr_t)y.n && b < a + (uintptr_t)x.n;
 }
+
+// Weights in and out: one buffer or two that lie apart. Each slot's sum is read and
+// written by one thread, in no order across slots.
+ut_status check_sums(const char* fn, const float* in, const float* out, int32_t B, int32_t Hk, int32_t capacity) {
+  if (in) UT_TRY(check_ptr(fn, "weights_in", in, 4));
+  if (in || out) UT_TRY(check_ptr(fn, "weights_out", out, 4));
+  const int64_t n = (int64_t)B * Hk * capacity * 4;
+  if (in && in != out && overlap(Range{reinterpret_cast<const char*>(in), n}, Range{reinterpret_cast<const char*>(out), n}))
+    return fail(UT_ERR_INVALID_ARG, "%s: weights_out overlaps weights_in (the same buffer, or another)", fn);
+  return UT_OK;
+}
 }  // namespace
 
 size_t ut_cache_attn_workspace_size(int32_t B, int32_t T, int32_t capacity, int32_t Hq, int32_t Hk,
@@ -1266,8 +1277,7 @@ ut_status ut_cache_attn(const void* q, const void* k_cache, const void* v_cache,
   XArgs a{};
   UT_TRY(check_cache(fn, B, T, capacity, Hq, Hk, D, window_left, n_sink, tree != nullptr, softmax_scale, &a));
   UT_TRY(check_words(fn, "tree", tree));
-  if (weights_in) UT_TRY(check_ptr(fn, "weights_in", weights_in, 4));
-  if (weights_in || weights_out) UT_TRY(check_ptr(fn, "weights_out", weights_out, 4));
+  UT_TRY(check_sums(fn, weights_in, weights_out, B, Hk, capacity));
   UT_TRY(check_lens(fn, cache_len, B, capacity - T, stream));
   const XTensor t[] = {{"q", q, &a.sq, false}, {"k_cache", k_cache, &a.sk, true}, {"v_cache", v_cache, &a.sv, true},
                        {"o", o, &a.so, false}};
@@ -1296,8 +1306,8 @@ ut_status ut_cache_weights(const void* q, const void* k_cache, const float* lse,
   UT_TRY(check_ptr(fn, "lse", lse, 4));
   UT_TRY(check_words(fn, "tree", tree));
   UT_TRY(check_words(fn, "tokens", tokens));
-  if (weights_in) UT_TRY(check_ptr(fn, "weights_in", weights_in, 4));
   UT_TRY(check_ptr(fn, "weights_out", weights_out, 4));
+  UT_TRY(check_sums(fn, weights_in, weights_out, B, Hk, capacity));
   UT_TRY(check_lens(fn, cache_len, B, capacity - T, stream));
   a.q = q, a.k = k_cache, a.lse = const_cast<float*>(lse), a.lens = cache_len, a.tree = tree;
   return check_hip(launch_cache_weights(a, CacheWeights{weights_in, weights_out, tokens}, stream),

@@ -127,6 +127,16 @@ def test_cache_weights_refusals():
     assert _ca("weights", wout=FAKE, tokens=ODD) == BAD and "tokens must be 8-byte" in ut.last_error()
 
 
+@pytest.mark.parametrize("fn", ["attn", "weights"])
+def test_weights_in_and_out_lie_apart_or_are_one(fn):
+    n = 2 * 2 * 300 * 4
+    for by in (4, n - 4, -4, 4 - n):
+        assert _ca(fn, win=0x10000000, wout=0x10000000 + by, lens=None) == BAD
+        assert "weights_out overlaps weights_in" in ut.last_error()
+    for by in (0, n, -n):   # accepted: the next refusal
+        assert _ca(fn, win=0x10000000, wout=0x10000000 + by, lens=None) == BAD and "cache_len is NULL" in ut.last_error()
+
+
 def test_cache_workspaces():
     need = ut.ut_cache_attn_workspace_size(4, 1, 16500, 32, 8, 128)
     assert need > 0
