@@ -598,7 +598,8 @@ hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* worksp
   char* const at = static_cast<char*>(workspace);
   const bool few = a.Nq * a.G <= kScoreRows, split = shape.splits > 1;
   const CacheParts parts{reinterpret_cast<float2*>(at + c.o), reinterpret_cast<float*>(at), a.Tq * a.Hq,
-                         reinterpret_cast<int*>(at + c.o + c.sums), reinterpret_cast<float*>(at + c.o + c.sums + c.cuts),
+                         split ? reinterpret_cast<int*>(at + c.o + c.sums) : nullptr,
+                         reinterpret_cast<float*>(at + c.o + c.sums + c.cuts),
                          few ? cache_heads(a) : 0};
   const int per = few ? kScoreRows : 32 * shape.waves;
   const CacheRows rows{(int)(((int64_t)a.Nq * a.G + per - 1) / per), per};

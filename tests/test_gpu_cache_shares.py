@@ -141,6 +141,24 @@ def test_graphs_with_a_workspace_of_both():
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("B,T,cap,Hq,Hk", [(200, 1, 64, 1, 1), (2, 1, 300, 8, 2), (1, 1, 5000, 8, 2), (1, 40, 5000, 2, 1)])
+def test_nothing_outside_the_workspace_is_written(B, T, cap, Hq, Hk, weighted):
+    """Of many samples too short to be cut, whose workspace is none or the scores alone."""
+    q, k, v = rnd(67, B, T, Hq, 64), rnd(68, B, cap, Hk, 64), rnd(69, B, cap, Hk, 64)
+    lens = ramp(B, cap - T, 70)
+    w = torch.rand((B, Hk, cap), device=DEV) if weighted else None
+    got = torch.empty_like(w) if weighted else None
+    need = ut.ut_cache_attn_workspace_size(B, T, cap, Hq, Hk, 64, with_weights=weighted)
+    room = torch.full((need + 8192,), 91, dtype=torch.uint8, device=DEV)
+    o, lse = torch.empty_like(q), torch.empty((B, Hq, T), device=DEV)
+    assert ut.ut_cache_attn(q, k, v, o, lse, dev(lens), 0.125, weights_in=w, weights_out=got,
+                            workspace=room[4096:4096 + need]) == ut.UT_OK
+    torch.cuda.synchronize()
+    assert (room[:4096] == 91).all() and (room[4096 + need:] == 91).all()
+    check_attn(q, k, v, lens, 0.125, o, lse, None, None, 0, w, got)
+
+
 # ---- validate mode ---------------------------------------------------------
 
 def test_validate_mode_checks_the_lengths(monkeypatch):
