@@ -59,63 +59,96 @@ __device__ inline float2 part_sums(const CacheParts& parts, int64_t stat, int n,
 }
 
 // The parts of rows joined: GPR groups of 32 lanes a row take every GPR-th part, four
-// columns a lane, and the groups' sums are added in LDS. Block `block` of T threads.
-template <int GPR, int T>
-__device__ inline void join_rows(const XArgs& a, const CacheParts& parts, const CacheRows& at, int block, float4* red,
-                                 float* red_l) {
+// columns a lane, and the groups' sums are added in LDS. Of blocks of T / 32 / GPR rows:
+// `block` and, R = 2, the one a grid further on, whose loads are under way together.
+template <int GPR, int T, int R = 1>
+__device__ inline void join_rows(const XArgs& a, const CacheParts& parts, const CacheRows& at, int block, float4* red) {
   constexpr int kRows = T / 32 / GPR;
   const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, sub = grp % GPR;
-  const int64_t r = (int64_t)block * kRows + grp / GPR;   // [B, Hq, T]
-  const bool live = r < parts.stats;
-  int64_t tok = 0;
-  int head = 0, splits = 0;
-  if (live) {
-    const int64_t bh = r / a.Nq;
-    const int b = (int)(bh / a.Hq), t = (int)(r - bh * a.Nq);
-    head = (int)(bh - (int64_t)b * a.Hq);
-    tok = (int64_t)b * a.Nq + t;
-    const int hk = head / a.G;
-    splits = row_parts(a, parts, at, b, hk, t * a.G + head - hk * a.G);
+  const bool col = 4 * lane < a.D;
+  int64_t r[R], tok[R];   // row [B, Hq, T], its token
+  bool live[R];
+  int head[R], splits[R];
+#pragma unroll
+  for (int y = 0; y < R; ++y) {
+    r[y] = ((int64_t)block + y * (int64_t)gridDim.x) * kRows + grp / GPR;
+    live[y] = r[y] < parts.stats;
+    tok[y] = 0;
+    head[y] = splits[y] = 0;
+    if (live[y]) {
+      const int64_t bh = r[y] / a.Nq;
+      const int b = (int)(bh / a.Hq), t = (int)(r[y] - bh * a.Nq);
+      head[y] = (int)(bh - (int64_t)b * a.Hq);
+      tok[y] = (int64_t)b * a.Nq + t;
+      const int hk = head[y] / a.G;
+      splits[y] = row_parts(a, parts, at, b, hk, t * a.G + head[y] - hk * a.G);
+    }
+    if (splits[y] == 1 && parts.heads > 0) live[y] = false, splits[y] = 0;   // cache_one finishes these
   }
-  const bool whole = splits == 1 && parts.heads > 0;   // cache_one finishes these
-  if (whole) splits = 0;
-  float M = -INFINITY;
-  for (int s = lane; s < splits; s += 32) {
-    const float2 p = parts.sums[s * parts.stats + r];
-    M = p.y != 0.f ? fmaxf(M, p.x) : M;
+  // O of the first parts is loaded beside their sums, of which each lane has one.
+  constexpr int kEarly = GPR == 1 ? 8 : 4;
+  float4 o[R][kEarly];
+  auto load = [&](int y, int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kEarly; ++u) {
+      const int s = s0 + u * GPR;
+      o[y][u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (s < splits[y] && col)
+        o[y][u] = *reinterpret_cast<const float4*>(parts.o + (s * parts.stats + r[y]) * a.D + 4 * lane);
+    }
+  };
+  float2 mine[R];
+#pragma unroll
+  for (int y = 0; y < R; ++y) {
+    mine[y] = make_float2(-INFINITY, 0.f);
+    if (lane < splits[y]) mine[y] = parts.sums[lane * parts.stats + r[y]];
+    load(y, sub);
   }
 #pragma unroll
-  for (int m = 1; m < 32; m <<= 1) M = fmaxf(M, __shfl_xor(M, m, 64));
-  float L = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int s = sub; s < splits; s += GPR) {
-    const float2 p = parts.sums[s * parts.stats + r];
-    if (p.y == 0.f) continue;   // no keys in use here
-    const float f = fast_exp2(p.x - M);
-    L += p.y * f;
-    if (4 * lane < a.D) {
-      const float4 o = *reinterpret_cast<const float4*>(parts.o + (s * parts.stats + r) * a.D + 4 * lane);
-      acc.x += o.x * f, acc.y += o.y * f, acc.z += o.z * f, acc.w += o.w * f;
+  for (int y = 0; y < R; ++y) {
+    float M = mine[y].y != 0.f ? mine[y].x : -INFINITY;
+    for (int s = lane + 32; s < splits[y]; s += 32) {
+      const float2 p = parts.sums[s * parts.stats + r[y]];
+      M = p.y != 0.f ? fmaxf(M, p.x) : M;
     }
-  }
-  if constexpr (GPR > 1) {
-    red[threadIdx.x] = acc;
-    if (lane == 0) red_l[grp] = L;
-    __syncthreads();
-    if (sub == 0)
-      for (int k = 1; k < GPR; ++k) {
-        const float4 o = red[threadIdx.x + 32 * k];
-        acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
-        L += red_l[grp + k];
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) M = fmaxf(M, __shfl_xor(M, m, 64));
+    auto factor = [&](const float2& p) { return p.y == 0.f ? 0.f : fast_exp2(p.x - M); };   // 0: no keys in use there
+    const float f_mine = factor(mine[y]);
+    float L = mine[y].y * f_mine;
+    for (int s = lane + 32; s < splits[y]; s += 32) {
+      const float2 p = parts.sums[s * parts.stats + r[y]];
+      L += p.y * factor(p);
+    }
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) L += __shfl_xor(L, m, 64);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = sub; s0 < splits[y]; s0 += kEarly * GPR) {
+      if (s0 != sub) load(y, s0);
+#pragma unroll
+      for (int u = 0; u < kEarly; ++u) {
+        const int s = s0 + u * GPR;
+        if (s >= splits[y]) break;
+        const float f = s < 32 ? __shfl(f_mine, s, 32) : factor(parts.sums[s * parts.stats + r[y]]);
+        if (f != 0.f) acc.x += o[y][u].x * f, acc.y += o[y][u].y * f, acc.z += o[y][u].z * f, acc.w += o[y][u].w * f;
       }
-  }
-  if (!live || sub != 0 || whole) return;
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  if (lane == 0) a.lse[r] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
-  if (4 * lane < a.D) {
-    const bf16x4 v = {(__bf16)(acc.x * inv), (__bf16)(acc.y * inv), (__bf16)(acc.z * inv), (__bf16)(acc.w * inv)};
-    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.o) + tok * a.so + head * a.D + 4 * lane) = v;
+    }
+    if constexpr (GPR > 1) {
+      red[threadIdx.x] = acc;
+      __syncthreads();
+      if (sub == 0)
+        for (int k = 1; k < GPR; ++k) {
+          const float4 x = red[threadIdx.x + 32 * k];
+          acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
+        }
+    }
+    if (!live[y] || sub != 0) continue;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    if (lane == 0) a.lse[r[y]] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
+    if (col) {
+      const bf16x4 v = {(__bf16)(acc.x * inv), (__bf16)(acc.y * inv), (__bf16)(acc.z * inv), (__bf16)(acc.w * inv)};
+      *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.o) + tok[y] * a.so + head[y] * a.D + 4 * lane) = v;
+    }
   }
 }
 
@@ -127,8 +160,7 @@ template <int GPR, bool SPLIT>
 __global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const CacheRows rows_at, const int joins,
                                                            const CacheParts parts, const CacheWeights wt) {
   __shared__ float4 red[256];
-  __shared__ float red_l[8];
-  if (SPLIT && (int)blockIdx.x < joins) return join_rows<GPR, 256>(a, parts, rows_at, blockIdx.x, red, red_l);
+  if (SPLIT && (int)blockIdx.x < joins) return join_rows<GPR, 256>(a, parts, rows_at, blockIdx.x, red);
   float* const lse2 = reinterpret_cast<float*>(red);
   const unsigned at = blockIdx.x - (SPLIT ? joins : 0), chunks = (unsigned)((a.Nk + 255) / 256);
   const unsigned bh = at / chunks;
@@ -178,12 +210,14 @@ constexpr int kWWaves = 8;    // of a workgroup: at 128 columns 64 KB of keys an
 constexpr int kWRows = 192;   // rows in LDS, a multiple of 64
 constexpr int kWTiles = 8;    // most tiles of 32 keys of a wave
 
-// JOIN: the rows' parts are not joined yet. The workgroups behind the first `weigh` join
-// them, and the others take the rows' LSE from the parts' sums.
+// JOIN: the rows' parts are not joined yet. Each workgroup joins some first (as workgroups
+// of their own they would wait for a place, one a CU: 36 us in place of 29 at 4 x 1,536
+// rows), those behind the first `weigh` nothing else, and the rows' LSE come from the
+// parts' sums.
 template <int DP, bool JOIN>
 __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XArgs a, const CacheWeights c, const int per_wave,
                                                                         const CacheRows rows_at, const CacheParts parts,
-                                                                        const int weigh) {
+                                                                        const int weigh, const int joins) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, KS = DP / 16;
   constexpr int KI = 32 * ROWB / 1024;   // direct loads of a tile
   __shared__ __attribute__((aligned(1024))) char k_lds[kWWaves * 32 * ROWB];
@@ -196,8 +230,10 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XA
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned hk = blockIdx.x % (unsigned)a.Hk, rest = blockIdx.x / (unsigned)a.Hk;
   constexpr int T = 64 * kWWaves;
-  if (JOIN && (int)blockIdx.x >= weigh)
-    return join_rows<1, T>(a, parts, rows_at, blockIdx.x - weigh, nullptr, nullptr);
+  if constexpr (JOIN) {
+    for (int i = blockIdx.x; i < joins; i += 2 * gridDim.x) join_rows<1, T, 2>(a, parts, rows_at, i, nullptr);
+    if ((int)blockIdx.x >= weigh) return;
+  }
   const int keys = 32 * kWWaves * per_wave;   // of the workgroup
   const unsigned chunks = (unsigned)((a.Nk + keys - 1) / keys);
   const int b = (int)(rest / chunks), key0 = (int)(rest % chunks) * keys;
@@ -578,9 +614,10 @@ hipError_t launch_weights(const XArgs& a, const CacheWeights& c, const CacheRows
   const int per_wave = (int)std::max<int64_t>(1, std::min<int64_t>(kWTiles, (heads * blocks + 255) / 256));
   const int64_t weigh = heads * (((int64_t)a.Nk + keys * per_wave - 1) / (keys * per_wave));
   const int64_t joins = JOIN ? (parts.stats + 2 * kWWaves - 1) / (2 * kWWaves) : 0;
+  const int64_t grid = std::max<int64_t>(weigh, std::min<int64_t>(joins, 256));
   TraceScope ts_(s, "cache_weights", x_padded(a));
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(weigh + joins)), dim3(64 * kWWaves), 0, s, a, c, per_wave, rows, parts, (int)weigh);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWWaves), 0, s, a, c, per_wave, rows, parts, (int)weigh, (int)joins);
   };
   a.D <= 64 ? launch(cache_weights_kernel<64, JOIN>) : launch(cache_weights_kernel<128, JOIN>);
   return hipGetLastError();
