@@ -214,10 +214,12 @@ constexpr int kWTiles = 8;    // most tiles of 32 keys of a wave
 // of their own they would wait for a place, one a CU: 36 us in place of 29 at 4 x 1,536
 // rows), those behind the first `weigh` nothing else, and the rows' LSE come from the
 // parts' sums.
-template <int DP, bool JOIN>
-__global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XArgs a, const CacheWeights c, const int per_wave,
+// SHARED: the steps of four tiles that are seen are shared out; else a workgroup has `per`
+// steps of one sample and key head, seen or not.
+template <int DP, bool JOIN, bool SHARED>
+__global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XArgs a, const CacheWeights c,
                                                                         const CacheRows rows_at, const CacheParts parts,
-                                                                        const int weigh, const int joins) {
+                                                                        const int weigh, const int per, const int joins) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, KS = DP / 16;
   constexpr int KI = 32 * ROWB / 1024;   // direct loads of a tile
   __shared__ __attribute__((aligned(1024))) char k_lds[kWWaves * 32 * ROWB];
@@ -228,24 +230,22 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XA
   __shared__ unsigned see_lds[kWWaves][64];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const unsigned hk = blockIdx.x % (unsigned)a.Hk, rest = blockIdx.x / (unsigned)a.Hk;
   constexpr int T = 64 * kWWaves;
-  if constexpr (JOIN) {
+  if constexpr (JOIN)
     for (int i = blockIdx.x; i < joins; i += 2 * gridDim.x) join_rows<1, T, 2>(a, parts, rows_at, i, nullptr);
-    if ((int)blockIdx.x >= weigh) return;
+  const int rows = a.Nq * a.G;
+  if (SHARED && c.in != c.out) {   // tiles that no row sees keep what they had
+    const int chunks = (a.Nk + T - 1) / T;
+    for (int i = blockIdx.x; i < a.B * a.Hk * chunks; i += gridDim.x) {
+      const int bh = i / chunks, b = bh / a.Hk, key = (i - bh * chunks) * T + tid;
+      const XSample sm = x_sample<kSeeCache>(a, b);
+      if (key >= a.Nk || x_span<kSeeCache>(a, sm, 0, rows).has(key / kXKeys)) continue;
+      const int64_t at = (int64_t)bh * a.Nk + key;
+      c.out[at] = c.in ? c.in[at] : 0.f;
+    }
   }
-  const int keys = 32 * kWWaves * per_wave;   // of the workgroup
-  const unsigned chunks = (unsigned)((a.Nk + keys - 1) / keys);
-  const int b = (int)(rest / chunks), key0 = (int)(rest % chunks) * keys;
-  const XSample sm = x_sample<kSeeCache>(a, b);
-  const int off = sm.nk - sm.nq, rows = sm.nq * a.G;
-  const XSpan span = x_span<kSeeCache>(a, sm, 0, rows);
+  if ((int)blockIdx.x >= weigh) return;
   const float c2 = a.scale * kLog2e;
-  // The wave's tiles: one of every eight in turn. Whether some row sees keys from k on.
-  auto tile_key = [&](int i) __attribute__((always_inline)) { return key0 + 32 * (kWWaves * i + w); };
-  auto seen = [&](int k) __attribute__((always_inline)) {
-    return (k < span.hi && k + 32 > span.lo) || k < span.send;
-  };
   char* const k_mine = k_lds + w * 32 * ROWB;
   int k_off[KI];   // row and column of this lane's piece of direct load i
 #pragma unroll
@@ -253,114 +253,148 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XA
     const int r = i * (1024 / ROWB) + lane / CPR, ch = lds_off<CPR>(r, lane % CPR) / 16 % CPR;
     k_off[i] = 8 * ch < a.D ? r * a.sk * 2 + 16 * ch : kXOut;
   }
-  auto load = [&](int k) __attribute__((always_inline)) {   // slots that the sample lacks read zeros
-    const int left = min(sm.nk - k, 32);
-    const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<const __bf16*>(a.k) + (sm.k0 + min(k, sm.nk - 1)) * a.sk + hk * a.D,
-                                                  left > 0 ? ((left - 1) * a.sk + a.D) * 2 : 0);
-#pragma unroll
-    for (int i = 0; i < KI; ++i) buffer_load_lds16(rs, k_mine + i * 1024, k_off[i]);
-  };
-  float sum[kWTiles];
-#pragma unroll
-  for (int i = 0; i < kWTiles; ++i) sum[i] = 0.f;
-  // uniform over the workgroup
-  const bool any = (key0 < span.hi && key0 + keys > span.lo) || key0 < span.send;
-  for (int r0 = 0; any && r0 < rows; r0 += kWRows) {
-    const int n = min(rows - r0, kWRows);
-    if (r0 > 0) __syncthreads();
-    constexpr int kLoads = kWRows * CPR / T;   // 16-byte pieces a thread, loaded together
-    bf16x8 piece[kLoads];
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const int i = u * T + tid, r = i / CPR, ch = i % CPR, tok = row_token(r0 + r, a.G);
-      piece[u] = bf16x8{};
-      if (r < n && 8 * ch < a.D)
-        piece[u] = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + (sm.q0 + tok) * a.sq +
-                                                    (hk * a.G + r0 + r - tok * a.G) * a.D + 8 * ch);
-    }
-    load(tile_key(0));
-    if (tid < (n + 63) / 64 * 64) {
-      const int row = r0 + tid, tok = row_token(min(row, rows - 1), a.G);
-      RowWindow<kSeeCache> see;
-      see.open(a, sm, b, row);
-      p_lds[tid] = see.p;
-      tree_lds[tid] = see.tree;
-      // rows that are not counted, and rows without keys: P = 0
-      float l = INFINITY;
-      if (row < rows && (!c.tokens || c.tokens[b] >> tok & 1)) {
-        if constexpr (JOIN) {
-          const float2 p = part_sums(parts, row_stat(a, b, hk, row), row_parts(a, parts, rows_at, b, hk, row), 0, 1);
-          l = p.y == 0.f ? -INFINITY : p.x + __log2f(p.y);
-        } else {
-          l = a.lse[row_stat(a, b, hk, row)] * kLog2e;
-        }
-        if (l == -INFINITY) l = INFINITY;
-      }
-      lse_lds[tid] = l;
-    }
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const int i = u * T + tid;
-      *reinterpret_cast<bf16x8*>(q_lds + lds_off<CPR>(i / CPR, i % CPR)) = piece[u];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kWTiles; ++i) {
-      if (i >= per_wave) break;   // uniform
-      __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): the tile is there
-      bf16x8 kop[KS];
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kop[ks] = *reinterpret_cast<const bf16x8*>(k_mine + lds_off<CPR>(l32, 2 * ks + g));
-      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): and read
-      pin_order();
-      if (i + 1 < per_wave) load(tile_key(i + 1));
-      const int k = tile_key(i);
-      if (!seen(k)) continue;     // uniform
-      // every row sees every key of the tile, whatever its place in the chunk or tree
-      const bool whole = k + 32 <= off && (k >= off + sm.nq - a.left || k + 32 <= a.sinks);
-      float add = 0.f;
-      auto walk = [&](auto all_seen) __attribute__((always_inline)) {
-        for (int r = 0; r < n; r += 64) {   // 64 rows, so that products and exponentials overlap
-          if constexpr (!decltype(all_seen)::value) {   // which of the keys a row sees, a lane a row
-            const int row = r + lane, p = p_lds[row];
-            const RowWindow<kSeeCache> see{p, a.tree ? off : p + 1, tree_lds[row]};
-            see_lds[w][lane] = see.bits(a, k) & bits32_from_to(0, sm.nk - k);
-            __builtin_amdgcn_wave_barrier();
-          }
-          f32x16 s[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-              s[y] = mfma32(*reinterpret_cast<const bf16x8*>(q_lds + lds_off<CPR>(r + 32 * y + l32, 2 * ks + g)), kop[ks],
-                            s[y]);
-#pragma unroll
-          for (int y = 0; y < 2; ++y)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const int row0 = r + 32 * y + 8 * x + 4 * g;
-              const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_lds + row0);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float p = fast_exp2(__builtin_fmaf(s[y][4 * x + e], c2, -ls[e]));
-                if constexpr (decltype(all_seen)::value) add += p;
-                else add += see_lds[w][row0 - r + e] >> l32 & 1 ? p : 0.f;
-              }
-            }
-        }
-      };
-      if (whole) walk(std::true_type{});   // uniform
-      else walk(std::false_type{});
-      sum[i] += add;
-    }
+  bool again = false;   // the rows in LDS are in use (uniform)
+  CacheShare share;
+  if constexpr (SHARED) {
+    share = cache_share<4>(a, (int)blockIdx.x, weigh, a.Hk, nullptr);
+  } else {
+    const unsigned rest = blockIdx.x / (unsigned)a.Hk, chunks = (unsigned)((a.Nk + 4 * kXKeys * per - 1) / (4 * kXKeys * per));
+    const int b = (int)(rest / chunks), t0 = (int)(rest % chunks) * per;
+    share = CacheShare{b, (int)(blockIdx.x % (unsigned)a.Hk), t0, t0 + per, 1, 0};
   }
+  for (bool first = true; share.items > 0; first = false) {   // uniform over the workgroup
+    const int b = share.b, hk = share.g;
+    const XSample sm = x_sample<kSeeCache>(a, b);
+    const int off = sm.nk - sm.nq;
+    const XSpan span = x_span<kSeeCache>(a, sm, 0, rows);
+    // The tiles in turn: all of them, or those that some row sees.
+    const int tiles = SHARED ? span.count : (a.Nk + kXKeys - 1) / kXKeys;
+    const int all = (tiles + 3) / 4, end = share.items == 1 ? min(share.t1, all) : all;
+    for (int step0 = first ? share.t0 : 0; step0 < end; step0 += kWTiles) {
+      const int per_wave = min(end - step0, kWTiles);
+      // The wave's half of one of the four tiles of step i; behind the last tile no row sees it.
+      auto tile_of = [&](int i) __attribute__((always_inline)) { return 4 * (step0 + i) + (w >> 1); };
+      auto tile_key = [&](int i) __attribute__((always_inline)) {
+        const int t = tile_of(i);
+        return kXKeys * (t + (SHARED && t >= span.first ? span.skip : 0)) + 32 * (w & 1);
+      };
+      auto seen = [&](int k) __attribute__((always_inline)) {   // keys from k on, by some row
+        return (k < span.hi && k + 32 > span.lo) || k < span.send;
+      };
+      auto load = [&](int k) __attribute__((always_inline)) {   // slots that the sample lacks read zeros
+        const int left = min(sm.nk - k, 32);
+        const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(static_cast<const __bf16*>(a.k) + (sm.k0 + min(k, sm.nk - 1)) * a.sk + hk * a.D,
+                                                      left > 0 ? ((left - 1) * a.sk + a.D) * 2 : 0);
 #pragma unroll
-  for (int i = 0; i < kWTiles; ++i) {
-    if (i >= per_wave) break;
-    const int key = tile_key(i) + l32;
-    const float x = pair_sum(sum[i]);
-    const int64_t at = ((int64_t)b * a.Hk + hk) * a.Nk + key;
-    if (g == 0 && key < a.Nk) c.out[at] = (c.in ? c.in[at] : 0.f) + x;
+        for (int i = 0; i < KI; ++i) buffer_load_lds16(rs, k_mine + i * 1024, k_off[i]);
+      };
+      float sum[kWTiles];
+#pragma unroll
+      for (int i = 0; i < kWTiles; ++i) sum[i] = 0.f;
+      const int key0 = 4 * kXKeys * step0;
+      const bool any = SHARED || (key0 < span.hi && key0 + 4 * kXKeys * per_wave > span.lo) || key0 < span.send;   // uniform
+      for (int r0 = 0; any && r0 < rows; r0 += kWRows) {
+        const int n = min(rows - r0, kWRows);
+        if (again) __syncthreads();
+        again = true;
+        constexpr int kLoads = kWRows * CPR / T;   // 16-byte pieces a thread, loaded together
+        bf16x8 piece[kLoads];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+          const int i = u * T + tid, r = i / CPR, ch = i % CPR, tok = row_token(r0 + r, a.G);
+          piece[u] = bf16x8{};
+          if (r < n && 8 * ch < a.D)
+            piece[u] = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + (sm.q0 + tok) * a.sq +
+                                                        (hk * a.G + r0 + r - tok * a.G) * a.D + 8 * ch);
+        }
+        load(tile_key(0));
+        if (tid < (n + 63) / 64 * 64) {
+          const int row = r0 + tid, tok = row_token(min(row, rows - 1), a.G);
+          RowWindow<kSeeCache> see;
+          see.open(a, sm, b, row);
+          p_lds[tid] = see.p;
+          tree_lds[tid] = see.tree;
+          // rows that are not counted, and rows without keys: P = 0
+          float l = INFINITY;
+          if (row < rows && (!c.tokens || c.tokens[b] >> tok & 1)) {
+            if constexpr (JOIN) {
+              const float2 p = part_sums(parts, row_stat(a, b, hk, row), row_parts(a, parts, rows_at, b, hk, row), 0, 1);
+              l = p.y == 0.f ? -INFINITY : p.x + __log2f(p.y);
+            } else {
+              l = a.lse[row_stat(a, b, hk, row)] * kLog2e;
+            }
+            if (l == -INFINITY) l = INFINITY;
+          }
+          lse_lds[tid] = l;
+        }
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+          const int i = u * T + tid;
+          *reinterpret_cast<bf16x8*>(q_lds + lds_off<CPR>(i / CPR, i % CPR)) = piece[u];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kWTiles; ++i) {
+          if (i >= per_wave) break;   // uniform
+          __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): the tile is there
+          bf16x8 kop[KS];
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) kop[ks] = *reinterpret_cast<const bf16x8*>(k_mine + lds_off<CPR>(l32, 2 * ks + g));
+          __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): and read
+          pin_order();
+          if (i + 1 < per_wave) load(tile_key(i + 1));
+          const int k = tile_key(i);
+          if (!seen(k)) continue;     // uniform
+          // every row sees every key of the tile, whatever its place in the chunk or tree
+          const bool whole = k + 32 <= off && (k >= off + sm.nq - a.left || k + 32 <= a.sinks);
+          float add = 0.f;
+          auto walk = [&](auto all_seen) __attribute__((always_inline)) {
+            for (int r = 0; r < n; r += 64) {   // 64 rows, so that products and exponentials overlap
+              if constexpr (!decltype(all_seen)::value) {   // which of the keys a row sees, a lane a row
+                const int row = r + lane, p = p_lds[row];
+                const RowWindow<kSeeCache> see{p, a.tree ? off : p + 1, tree_lds[row]};
+                see_lds[w][lane] = see.bits(a, k) & bits32_from_to(0, sm.nk - k);
+                __builtin_amdgcn_wave_barrier();
+              }
+              f32x16 s[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+              for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                  s[y] = mfma32(*reinterpret_cast<const bf16x8*>(q_lds + lds_off<CPR>(r + 32 * y + l32, 2 * ks + g)), kop[ks],
+                                s[y]);
+#pragma unroll
+              for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                  const int row0 = r + 32 * y + 8 * x + 4 * g;
+                  const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_lds + row0);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    const float p = fast_exp2(__builtin_fmaf(s[y][4 * x + e], c2, -ls[e]));
+                    if constexpr (decltype(all_seen)::value) add += p;
+                    else add += see_lds[w][row0 - r + e] >> l32 & 1 ? p : 0.f;
+                  }
+                }
+            }
+          };
+          if (whole) walk(std::true_type{});   // uniform
+          else walk(std::false_type{});
+          sum[i] += add;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kWTiles; ++i) {
+        if (i >= per_wave) break;   // uniform
+        const int key = tile_key(i) + l32;
+        const float x = pair_sum(sum[i]);
+        const int64_t at = ((int64_t)b * a.Hk + hk) * a.Nk + key;
+        if (g == 0 && tile_of(i) < tiles && key < a.Nk) c.out[at] = (c.in ? c.in[at] : 0.f) + x;
+      }
+      if (!SHARED) return;   // per <= kWTiles
+    }
+    if (++share.g == a.Hk) share.g = 0, ++share.b;
+    --share.items;
   }
 }
 
@@ -609,17 +643,22 @@ CacheSpace cache_space(const XArgs& a) {
 template <bool JOIN>
 hipError_t launch_weights(const XArgs& a, const CacheWeights& c, const CacheRows& rows, const CacheParts& parts,
                           hipStream_t s) {
-  // as many tiles a wave as leave a workgroup for each CU
-  const int64_t heads = (int64_t)a.B * a.Hk, keys = 32 * kWWaves, blocks = ((int64_t)a.Nk + keys - 1) / keys;
-  const int per_wave = (int)std::max<int64_t>(1, std::min<int64_t>(kWTiles, (heads * blocks + 255) / 256));
-  const int64_t weigh = heads * (((int64_t)a.Nk + keys * per_wave - 1) / (keys * per_wave));
+  // Steps of four tiles: as many a workgroup as leave one for each CU, by the capacity, or
+  // where a window leaves most of it unseen shared out by what is seen (48 tokens of 32
+  // heads, four samples: 24,576 slots with a window of 4,096 54 -> 38 us, but 4,096 slots
+  // seen whole 29 -> 33).
+  const int64_t heads = (int64_t)a.B * a.Hk, all = ((int64_t)a.Nk + 4 * kXKeys - 1) / (4 * kXKeys);
+  const int64_t steps = (x_item_tiles(a, a.Nq * a.G) + 3) / 4;
+  const int64_t per = 2 * steps <= all ? 0 : std::max<int64_t>(1, std::min<int64_t>(kWTiles, (heads * all + 255) / 256));
+  const int64_t weigh = per ? heads * ((all + per - 1) / per) : std::min<int64_t>(heads * steps, 256);
   const int64_t joins = JOIN ? (parts.stats + 2 * kWWaves - 1) / (2 * kWWaves) : 0;
   const int64_t grid = std::max<int64_t>(weigh, std::min<int64_t>(joins, 256));
   TraceScope ts_(s, "cache_weights", x_padded(a));
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWWaves), 0, s, a, c, per_wave, rows, parts, (int)weigh, (int)joins);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWWaves), 0, s, a, c, rows, parts, (int)weigh, (int)per, (int)joins);
   };
-  a.D <= 64 ? launch(cache_weights_kernel<64, JOIN>) : launch(cache_weights_kernel<128, JOIN>);
+  if (per > 0) a.D <= 64 ? launch(cache_weights_kernel<64, JOIN, false>) : launch(cache_weights_kernel<128, JOIN, false>);
+  else a.D <= 64 ? launch(cache_weights_kernel<64, JOIN, true>) : launch(cache_weights_kernel<128, JOIN, true>);
   return hipGetLastError();
 }
 }  // namespace

@@ -502,12 +502,15 @@ __device__ inline int cache_parts(int per, int start, int n, int g) {
   const int x = start + g * n;
   return (x + n - 1) / -per - x / -per + 1;
 }
-// cuts: per and the samples' starts, or null; each sample has `groups` items.
+// cuts: per and the samples' starts, or null; each sample has `groups` items. UNIT: tiles
+// that are not parted (t0 and t1 count those); more than one: a workgroup may have one.
+template <int UNIT = 1>
 __device__ inline CacheShare cache_share(const XArgs& a, int wg, int wgs, int groups, int* cuts) {
-  const int least = cache_least(a);
-  const int lane = threadIdx.x & 63, n0 = lane < a.B ? cache_tiles(a, lane) : 0;
+  const int least = UNIT == 1 ? cache_least(a) : 1;
+  auto units_of = [&](int b) __attribute__((always_inline)) { return b < a.B ? (cache_tiles(a, b) + UNIT - 1) / UNIT : 0; };
+  const int lane = threadIdx.x & 63, n0 = units_of(lane);
   auto tiles_of = [&](int b0) __attribute__((always_inline)) {   // of sample b0 + lane
-    return b0 == 0 ? n0 : b0 + lane < a.B ? cache_tiles(a, b0 + lane) : 0;
+    return b0 == 0 ? n0 : units_of(b0 + lane);
   };
   auto sum_of = [&](auto f) __attribute__((always_inline)) {
     int total = 0;
