@@ -643,8 +643,9 @@ ut_status ut_xattn_bwd_varlen(const void* q, const void* k, const void* v, const
  * ut_xattn_*. The size queries take the window too. A row without visible keys in
  * use: o = 0, lse = -inf, zero gradients. Keys that no query sees may hold
  * anything and get zero gradients; inf or NaN in a key that some query sees may reach
- * the other queries of its 128-row tile, as 0 times it (mark padding in key_mask). delta = rowsum(dO o O) is formed from the
- * stored o, except for rows whose visible keys lie in one 64-key tile.
+ * the other queries of its 128-row tile, as 0 times it (mark padding in key_mask).
+ * delta = rowsum(dO o O) is formed from the stored o, except for rows whose visible
+ * keys lie in one 64-key tile.
  * No atomics: results are deterministic.
  * Errors: also window_left or window_right < -1, n_sink < 0 -> UT_ERR_INVALID_ARG.
  * ---------------------------------------------------------------------- */

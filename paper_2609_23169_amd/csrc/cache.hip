@@ -10,16 +10,18 @@
 // from memory, an instruction touches 32 rows: twice the time), from there into
 // registers, the next tile's loads beside the products; S = Q K^T on 32x32x16 bf16 MFMA
 // in the layout where a lane holds one key, so that the sum over the rows is the lane's
-// own but for one exchange. fp32 throughout, a fixed order: no atomics.
+// own but for one exchange. fp32 throughout, a fixed order: no atomics. 192 rows on four
+// caches of 8,300 slots, 8 key heads of 128: 37 us with the joins of the attention's parts
+// (28 alone), vector work and the latency of a workgroup's start and few steps.
 //
 // Eviction: of a row of weights the middle slots (behind the sinks, before the recent
 // ones) are searched by value for the smallest weight that stays: its order as an
 // unsigned number is bracketed, and the next number is taken where the counts at the
 // ends would have it on a straight line, every fourth time in the middle (that number
 // grows with the float's logarithm): some five steps leave 64 slots, which are ranked
-// against each other, where bisection took over twenty. A workgroup holds the row in registers, and longer ones
-// in LDS too (up to 69,632 slots; beyond they are read again), a step is a compare and an add a register and one
-// barrier. Then ballots give every kept slot its place in ascending order, equal
+// against each other, where bisection took over twenty. A workgroup holds the row in
+// registers, and longer ones in LDS too (up to 69,632 slots; beyond they are read again), a
+// step is a compare and an add a register and one barrier. Then ballots give every kept slot its place in ascending order, equal
 // weights the lowest slots first, and a second launch copies the rows of K and V.
 #include <algorithm>
 #include <type_traits>
@@ -410,9 +412,9 @@ __device__ inline unsigned weight_key(float x) {
 }
 
 // One workgroup of W waves a row (sample and key head). R: registers a lane for the row's
-// middle, L: words of LDS a lane for more of it; R = 0: it is read again in every pass. Few waves where they hold the row: the
-// arithmetic of a step is done by each of them (300 slots 5.7 us with 4, 9.3 with 16;
-// 16,000 slots 22 and 16).
+// middle, L: words of LDS a lane for more of it; R = 0: it is read again in every pass. Few
+// waves where they hold the row: the arithmetic of a step is done by each of them (300
+// slots 5.7 us with 4, 9.3 with 16; 16,000 slots 22 and 16).
 template <int W, int R, int L = 0>
 __global__ __launch_bounds__(64 * W) void cache_select_kernel(const CacheEvict a) {
   __shared__ __attribute__((aligned(16))) unsigned cnt[2][W], cnt2[W], ends[4][W];

@@ -31,6 +31,16 @@
 // queries on 512 keys take 560 us, 870 TFLOP/s: a change of item every eight tiles
 // (about 5,000 of 37,000 cycles) and 0.19 ms of rows at the copy rate come on top. One
 // query each of 32 heads on 16,391 keys: 4.3 TB/s.
+//
+// Window attention (SEE = kSeeWindow) visits the tiles that some row of the item sees:
+// two runs, those with sinks and those of the window. A half tile that every row sees
+// whole goes as above, of others a row's keys are a word of 32 bits. 77,586 queries
+// that see 1,024 keys to each side and 512 sinks, 24 heads of 128: 2,750 to 2,830 us,
+// 860 TFLOP/s of visible pairs, matrix cores 42% busy, five vector instructions an MFMA.
+// A cache (kSeeCache) is a window with nothing behind a token, lengths on the device
+// and a tree's words; calls of few rows have cache_one.hip. Its parts are shared out by
+// cache_share, eight waves where 128 columns have more than 128 rows: 2 x 509 tokens on
+// 11,111 slots, 24 heads of 128, 150 to 165 us, 740 to 820 TFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
