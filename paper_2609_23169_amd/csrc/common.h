@@ -239,7 +239,7 @@ bool xattn_bwd_launchable(const XArgs& a);
 size_t xattn_bwd_workspace(const XArgs& a);
 hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s);
 
-// ---- A cache: attention with the slots' weights (xattn_fwd.hip), eviction (cache.hip) ----
+// ---- A cache: attention with the slots' weights (cache_one.hip, xattn_fwd.hip, cache.hip), eviction (cache.hip) ----
 struct CacheWeights {
   const float* in;          // [B, Hk, Nk], or null: zeros
   float* out;

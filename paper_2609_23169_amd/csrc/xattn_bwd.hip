@@ -765,14 +765,17 @@ int dkdv_splits(const XArgs& a) {
   return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), 4) / groups, steps / 8));
 }
 // Sinks are seen by nearly all tokens: parts of about as many steps as the other
-// workgroups', 32 at least, so that no workgroup is left with the whole sequence.
+// workgroups', 32 at least, so that no workgroup is left with the whole sequence; 16 where
+// the chip holds all workgroups at once and waits for the longest (2,048 tokens, 3 heads
+// of 128, window 128: 46 -> 29 us; but 22,879 tokens, 24 heads, 259 -> 282 with the sums).
 SinkParts sink_parts(const XArgs& a) {
   SinkParts p{};
   p.others = dkdv_splits(a);
   p.splits = 1;
   if (!a.window) return p;
   p.tiles = (std::min(a.sinks, a.Nk) + kBwdKeys - 1) / kBwdKeys;
-  const int64_t per = std::max<int64_t>(dkdv_steps(a, dkdv_reach(a)) / p.others, 32), all = dkdv_steps(a, a.Nq);
+  const int64_t least = dkdv_groups(a) <= x_resident(x_padded(a), 4) ? 16 : 32;
+  const int64_t per = std::max<int64_t>(dkdv_steps(a, dkdv_reach(a)) / p.others, least), all = dkdv_steps(a, a.Nq);
   p.splits = std::max<int64_t>(p.others, std::min<int64_t>((all + per - 1) / per, 64));
   return p;
 }
@@ -802,7 +805,7 @@ template <int DP, bool WIN>
 void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t s) {
   const XOrder order = WIN ? window_order(head_group(a), a.B, a.Hk, dq_tiles(a), splits)
                            : x_order(head_group(a), a.B, a.Hk, dq_tiles(a), splits);
-  const int64_t items = dq_groups(a) * splits;
+  const int64_t items = order.total;   // of window attention also those that fill chunks up
   const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, kDqWaves)) + 7) / 8 * 8);
   TraceScope ts_(s, WIN ? "swattn_dq" : "xattn_dq", DP);
   hipLaunchKernelGGL((xattn_dq_kernel<DP, WIN>), grid, dim3(64 * kDqWaves), 0, s, a, aux, order, part);

@@ -481,7 +481,7 @@ void launch_fwd(const XArgs& a, int splits, const Parts& parts, hipStream_t s) {
   const int64_t tiles = ((int64_t)a.Nq * a.G + 32 * NW - 1) / (32 * NW);
   const XOrder order = SEE == kSeeWindow ? window_order(head_group(a), a.B, a.Hk, tiles, splits)
                                          : x_order(head_group(a), a.B, a.Hk, tiles, splits);
-  const int64_t items = (int64_t)a.B * a.Hk * order.tiles * splits;
+  const int64_t items = order.total;   // of window attention also those that fill chunks up
   const dim3 grid(SEE == kSeeCache && splits > 1
                       ? (unsigned)x_resident(DP, NW)
                       : (unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, NW)) + 7) / 8 * 8);
