@@ -752,7 +752,7 @@ int64_t dkdv_groups(const XArgs& a) {
 // from 14.5 to 11.7, and their join adds 7.
 int dq_splits(const XArgs& a) {
   const int64_t groups = dq_groups(a), tiles = x_item_tiles(a, 32 * kDqWaves);
-  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), kDqWaves) / groups, tiles / 4));
+  return x_splits(a, groups, tiles, x_resident(x_padded(a), kDqWaves));
 }
 // Steps of a dK/dV workgroup that is not split and whose keys are seen by `tokens`.
 int64_t dkdv_steps(const XArgs& a, int64_t tokens) {
@@ -762,7 +762,7 @@ int64_t dkdv_steps(const XArgs& a, int64_t tokens) {
 int64_t dkdv_reach(const XArgs& a) { return a.window ? (int64_t)a.left + a.right + kBwdKeys : a.Nq; }
 int dkdv_splits(const XArgs& a) {
   const int64_t groups = dkdv_groups(a), steps = dkdv_steps(a, dkdv_reach(a));
-  return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), 4) / groups, steps / 8));
+  return x_splits(a, groups, steps / 2, x_resident(x_padded(a), 4));   // two steps are about a tile
 }
 // Sinks are seen by nearly all tokens: parts of about as many steps as the other
 // workgroups', 32 at least, so that no workgroup is left with the whole sequence; 16 where

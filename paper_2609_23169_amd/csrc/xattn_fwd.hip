@@ -469,7 +469,7 @@ XShape fwd_shape(const XArgs& a) {
   const int64_t rows = (int64_t)a.Nq * a.G, heads = (int64_t)a.B * a.Hk;
   auto splits = [&](int nw) {
     const int64_t groups = heads * ((rows + 32 * nw - 1) / (32 * nw)), tiles = x_item_tiles(a, 32 * nw);
-    return groups == 0 ? 1 : (int)std::max<int64_t>(1, std::min(x_resident(x_padded(a), nw) / groups, tiles / 4));
+    return x_splits(a, groups, tiles, x_resident(x_padded(a), nw));
   };
   if (rows <= 32 && splits(1) > 1) return XShape{splits(1), 1};
   return XShape{splits(4), 4};

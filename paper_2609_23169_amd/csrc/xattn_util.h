@@ -95,6 +95,17 @@ inline unsigned head_group(const XArgs& a) { return a.Hk % 8 == 0 ? (unsigned)a.
 // to 36 at 64) and by registers (two waves a SIMD at 128 columns, three at 64): what
 // a grid needs to fill the chip.
 constexpr int64_t x_resident(int DP, int nw) { return 256 * (nw == 8 ? 1 : DP == 128 ? 2 : nw == 4 ? 3 : 4); }
+// Parts of the keys (forward, dQ) of `groups` items of up to `tiles` tiles: as many as fit
+// the chip at once, of four tiles at least. In window attention those beyond one workgroup
+// a CU, which share its units, take a dozen tiles to pay for their join (3,000 tokens, 8
+// heads of 128, window 256: forward 23 us whole, 24 + 13 in halves; 5,000 tokens, 2 heads,
+// seen to the front: 41 + 12 in six, 46 + 10 in five).
+inline int x_splits(const XArgs& a, int64_t groups, int64_t tiles, int64_t resident) {
+  if (groups == 0) return 1;
+  const int64_t n = a.window && !a.lens ? std::max(std::min(256 / groups, tiles / 4), std::min(resident / groups, tiles / 12))
+                                        : std::min(resident / groups, tiles / 4);
+  return (int)std::max<int64_t>(1, n);
+}
 // Most key tiles of an item of `rows` rows.
 inline int64_t x_item_tiles(const XArgs& a, int rows) {
   const int64_t all = ((int64_t)a.Nk + kXKeys - 1) / kXKeys;
