@@ -46,18 +46,22 @@ __device__ inline int64_t row_stat(const XArgs& a, int b, int hk, int row) {
   const int t = row_token(row, a.G);
   return ((int64_t)b * a.Hq + hk * a.G + row - t * a.G) * a.Nq + t;
 }
-// A row's LSE in log2 units from its n parts, the parts from `first` on in steps; {maximum,
-// sum} of parts that hold nothing are left out.
-__device__ inline float2 part_sums(const CacheParts& parts, int64_t stat, int n, int first, int step) {
+// A row's LSE in log2 units (-inf: no keys) from the sums of its n parts, by `lanes`
+// neighbouring lanes, this one the sub-th; parts that hold nothing are left out.
+__device__ inline float part_lse(const CacheParts& parts, int64_t stat, int n, int sub, int lanes) {
   float m = -INFINITY, l = 0.f;
-#pragma unroll 4
-  for (int s = first; s < n; s += step) {
-    const float2 p = parts.sums[s * parts.stats + stat];
-    const float to = p.y == 0.f ? m : fmaxf(m, p.x);
-    l = (l == 0.f ? 0.f : l * fast_exp2(m - to)) + (p.y == 0.f ? 0.f : p.y * fast_exp2(p.x - to));
+  auto add = [&](float mo, float lo) __attribute__((always_inline)) {
+    const float to = lo == 0.f ? m : fmaxf(m, mo);
+    l = (l == 0.f ? 0.f : l * fast_exp2(m - to)) + (lo == 0.f ? 0.f : lo * fast_exp2(mo - to));
     m = to;
+  };
+#pragma unroll 4
+  for (int s = sub; s < n; s += lanes) {
+    const float2 p = parts.sums[s * parts.stats + stat];
+    add(p.x, p.y);
   }
-  return make_float2(m, l);
+  for (int x = 1; x < lanes; x <<= 1) add(__shfl_xor(m, x, 64), __shfl_xor(l, x, 64));
+  return l == 0.f ? -INFINITY : m + __log2f(l);
 }
 
 // The parts of rows joined: GPR groups of 32 lanes a row take every GPR-th part, four
@@ -181,14 +185,7 @@ __global__ __launch_bounds__(256) void cache_finish_kernel(const XArgs a, const 
     const int n = SPLIT ? row_parts(a, parts, rows_at, b, hk, row) : 1;
     float m;
     if (n > 1) {
-      float2 p = part_sums(parts, stat, n, sub, 8);
-#pragma unroll
-      for (int x = 1; x < 8; x <<= 1) {
-        const float mo = __shfl_xor(p.x, x, 64), lo = __shfl_xor(p.y, x, 64), top = fmaxf(p.x, mo);
-        p.y = (p.y == 0.f ? 0.f : p.y * fast_exp2(p.x - top)) + (lo == 0.f ? 0.f : lo * fast_exp2(mo - top));
-        p.x = top;
-      }
-      m = p.y == 0.f ? -INFINITY : p.x + __log2f(p.y);
+      m = part_lse(parts, stat, n, sub, 8);
     } else {   // finished by its workgroup
       m = a.lse[stat] * kLog2e;
     }
@@ -221,7 +218,7 @@ constexpr int kWTiles = 8;    // most tiles of 32 keys of a wave
 template <int DP, bool JOIN, bool SHARED>
 __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XArgs a, const CacheWeights c,
                                                                         const CacheRows rows_at, const CacheParts parts,
-                                                                        const int weigh, const int per, const int joins) {
+                                                                        const int weigh, const int per, const int joins, const bool many) {
   constexpr int ROWB = DP * 2, CPR = DP / 8, KS = DP / 16;
   constexpr int KI = 32 * ROWB / 1024;   // direct loads of a tile
   __shared__ __attribute__((aligned(1024))) char k_lds[kWWaves * 32 * ROWB];
@@ -233,8 +230,16 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XA
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   constexpr int T = 64 * kWWaves;
-  if constexpr (JOIN)
-    for (int i = blockIdx.x; i < joins; i += 2 * gridDim.x) join_rows<1, T, 2>(a, parts, rows_at, i, nullptr);
+  if constexpr (JOIN) {
+    if (many) {   // uniform: a row a turn
+      for (int i = blockIdx.x; i < joins; i += gridDim.x) {
+        join_rows<T / 32, T>(a, parts, rows_at, i, reinterpret_cast<float4*>(k_lds));
+        __syncthreads();
+      }
+    } else {
+      for (int i = blockIdx.x; i < joins; i += 2 * gridDim.x) join_rows<1, T, 2>(a, parts, rows_at, i, nullptr);
+    }
+  }
   const int rows = a.Nq * a.G;
   if (SHARED && c.in != c.out) {   // tiles that no row sees keep what they had
     const int chunks = (a.Nk + T - 1) / T;
@@ -310,24 +315,28 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache_weights_kernel(const XA
                                                         (hk * a.G + r0 + r - tok * a.G) * a.D + 8 * ch);
         }
         load(tile_key(0));
-        if (tid < (n + 63) / 64 * 64) {
+        const int pad = (n + 63) / 64 * 64;
+        if (tid < pad) {
           const int row = r0 + tid, tok = row_token(min(row, rows - 1), a.G);
           RowWindow<kSeeCache> see;
           see.open(a, sm, b, row);
           p_lds[tid] = see.p;
           tree_lds[tid] = see.tree;
-          // rows that are not counted, and rows without keys: P = 0
-          float l = INFINITY;
-          if (row < rows && (!c.tokens || c.tokens[b] >> tok & 1)) {
-            if constexpr (JOIN) {
-              const float2 p = part_sums(parts, row_stat(a, b, hk, row), row_parts(a, parts, rows_at, b, hk, row), 0, 1);
-              l = p.y == 0.f ? -INFINITY : p.x + __log2f(p.y);
-            } else {
-              l = a.lse[row_stat(a, b, hk, row)] * kLog2e;
-            }
-            if (l == -INFINITY) l = INFINITY;
+          if constexpr (!JOIN) {   // rows that are not counted, and rows without keys: P = 0
+            float l = INFINITY;
+            if (row < rows && (!c.tokens || c.tokens[b] >> tok & 1)) l = a.lse[row_stat(a, b, hk, row)] * kLog2e;
+            lse_lds[tid] = l == -INFINITY ? INFINITY : l;
           }
-          lse_lds[tid] = l;
+        }
+        if constexpr (JOIN) {   // all lanes: parts may be many where rows are few
+          static_assert(2 * kWRows <= T);
+          const int shift = pad <= T / 8 ? 3 : pad <= T / 4 ? 2 : 1, at = tid >> shift, row = r0 + at;
+          if (at < pad) {
+            float l = INFINITY;
+            if (row < rows)
+              l = part_lse(parts, row_stat(a, b, hk, row), row_parts(a, parts, rows_at, b, hk, row), tid - (at << shift), 1 << shift);
+            lse_lds[at] = l == -INFINITY ? INFINITY : l;
+          }
         }
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
@@ -643,7 +652,7 @@ CacheSpace cache_space(const XArgs& a) {
 }
 
 template <bool JOIN>
-hipError_t launch_weights(const XArgs& a, const CacheWeights& c, const CacheRows& rows, const CacheParts& parts,
+hipError_t launch_weights(const XArgs& a, const CacheWeights& c, const CacheRows& rows, const CacheParts& parts, bool many,
                           hipStream_t s) {
   // Steps of four tiles: as many a workgroup as leave one for each CU, by the capacity, or
   // where a window leaves most of it unseen shared out by what is seen (48 tokens of 32
@@ -653,11 +662,11 @@ hipError_t launch_weights(const XArgs& a, const CacheWeights& c, const CacheRows
   const int64_t steps = (x_item_tiles(a, a.Nq * a.G) + 3) / 4;
   const int64_t per = 2 * steps <= all ? 0 : std::max<int64_t>(1, std::min<int64_t>(kWTiles, (heads * all + 255) / 256));
   const int64_t weigh = per ? heads * ((all + per - 1) / per) : std::min<int64_t>(heads * steps, 256);
-  const int64_t joins = JOIN ? (parts.stats + 2 * kWWaves - 1) / (2 * kWWaves) : 0;
+  const int64_t joins = !JOIN ? 0 : many ? parts.stats : (parts.stats + 2 * kWWaves - 1) / (2 * kWWaves);
   const int64_t grid = std::max<int64_t>(weigh, std::min<int64_t>(joins, 256));
   TraceScope ts_(s, "cache_weights", x_padded(a));
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWWaves), 0, s, a, c, rows, parts, (int)weigh, (int)per, (int)joins);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWWaves), 0, s, a, c, rows, parts, (int)weigh, (int)per, (int)joins, many);
   };
   if (per > 0) a.D <= 64 ? launch(cache_weights_kernel<64, JOIN, false>) : launch(cache_weights_kernel<128, JOIN, false>);
   else a.D <= 64 ? launch(cache_weights_kernel<64, JOIN, true>) : launch(cache_weights_kernel<128, JOIN, true>);
@@ -679,6 +688,12 @@ hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* worksp
                          split ? reinterpret_cast<int*>(at + c.o + c.sums) : nullptr,
                          reinterpret_cast<float*>(at + c.o + c.sums + c.cuts),
                          few ? cache_heads(a) : 0};
+  // Eight groups of lanes a row where many parts are to be read for few rows, as in
+  // cross attention. Beside the weights sixteen where a workgroup's turns, a row each, pay
+  // for themselves (80 rows of up to 235 parts 84 -> 29 us, 256 of 17 14 -> 12; but 1,024 of
+  // 17 18 -> 22, 4,096 of 9 26 -> 51).
+  const bool many = few || !w.out ? shape.splits >= 8 && parts.stats <= 4096
+                                  : shape.splits >= 16 * ((parts.stats + 255) / 256);
   const int per = few ? kScoreRows : 32 * shape.waves;
   const CacheRows rows{(int)(((int64_t)a.Nq * a.G + per - 1) / per), per};
   if (few) {
@@ -688,12 +703,9 @@ hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* worksp
     if (!split && (!a.scores || weights_here)) return hipSuccess;
   } else {
     if (hipError_t e = launch_cache_fwd(a, shape, parts, s); e != hipSuccess) return e;
-    if (w.out) return split ? launch_weights<true>(a, w, rows, parts, s) : launch_weights<false>(a, w, rows, parts, s);
+    if (w.out) return split ? launch_weights<true>(a, w, rows, parts, many, s) : launch_weights<false>(a, w, rows, parts, false, s);
     if (!split) return hipSuccess;
   }
-  // Eight groups of lanes a row where many parts are to be read for few rows, as in
-  // cross attention.
-  const bool many = shape.splits >= 8 && parts.stats <= 4096;
   const int64_t joins = split ? (parts.stats + (many ? 0 : 7)) / (many ? 1 : 8) : 0;
   const int64_t chunks = a.scores ? (int64_t)a.B * a.Hk * (((int64_t)a.Nk + 255) / 256) : 0;
   TraceScope ts_(s, "cache_finish");
@@ -705,7 +717,7 @@ hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* worksp
 }
 
 hipError_t launch_cache_weights(const XArgs& a, const CacheWeights& c, hipStream_t s) {
-  return launch_weights<false>(a, c, CacheRows{}, CacheParts{}, s);
+  return launch_weights<false>(a, c, CacheRows{}, CacheParts{}, false, s);
 }
 
 hipError_t launch_cache_evict(const CacheEvict& a, hipStream_t s) {
