@@ -102,8 +102,8 @@ constexpr int64_t x_resident(int DP, int nw) { return 256 * (nw == 8 ? 1 : DP ==
 // seen to the front: 41 + 12 in six, 46 + 10 in five).
 inline int x_splits(const XArgs& a, int64_t groups, int64_t tiles, int64_t resident) {
   if (groups == 0) return 1;
-  const int64_t n = a.window && !a.lens ? std::max(std::min(256 / groups, tiles / 4), std::min(resident / groups, tiles / 12))
-                                        : std::min(resident / groups, tiles / 4);
+  const int64_t n = a.window ? std::max(std::min(256 / groups, tiles / 4), std::min(resident / groups, tiles / 12))
+                             : std::min(resident / groups, tiles / 4);
   return (int)std::max<int64_t>(1, n);
 }
 // Most key tiles of an item of `rows` rows.
