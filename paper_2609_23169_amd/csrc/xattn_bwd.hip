@@ -19,7 +19,7 @@
 //           writes fp32 partial sums, and a join adds them in a fixed order.
 //
 // Rounding: P and dS to bf16 before their second products (half a step each,
-// 2^-9 relative), all sums in fp32. delta comes from O as stored (half a step
+// 2^-9 relative; in small grids of window attention dS as two, FINE), all sums in fp32. delta comes from O as stored (half a step
 // of it), or as rowsum(P o dP) in fp32 where a row's keys in use lie in one tile.
 // No atomics: equal results on every run. Keys not in use: the dQ pass reads
 // zeros in their place and sets their P to 0; in the dK/dV pass a key is a
@@ -50,12 +50,21 @@ constexpr int kBwdKeys = 128;   // keys of a dK/dV workgroup
 constexpr int kRowTile = 32;    // query tokens of a dK/dV step
 constexpr int kDqWaves = 4;     // of 32 rows each
 
+// FINE: dS goes into its products as two bf16, the rounded value and what the rounding left
+// of it (2^-18 of it off), for grids that leave the chip room. There are few rows then,
+// those with few keys weigh most, and their roundings do not average out: dQ and dK
+// of 384 tokens, window 96, 0.0025 off in relative norm, 0.0018 with this (the result's
+// own rounding 0.0017, the rest delta's O), for 2 us of 17 a pass.
+__device__ inline unsigned pack_rest(float a, float b, unsigned rounded) {
+  return pack_bf16x2(a - __uint_as_float(rounded << 16), b - __uint_as_float(rounded & 0xffff0000u));
+}
+
 // ---------------------------------------------------------------------------
 // dQ
 // ---------------------------------------------------------------------------
 // part: fp32 [split][token][Hq][D], null with one split.
-template <int DP, bool WIN>
-__global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const XArgs a, float* __restrict__ aux,
+template <int DP, bool WIN, bool FINE>
+__global__ __launch_bounds__(256, FINE ? 1 : DP == 64 ? 3 : 2) void xattn_dq_kernel(const XArgs a, float* __restrict__ aux,
                                                                          const XOrder order, float* __restrict__ part) {
   constexpr int NW = kDqWaves, ROWB = DP * 2, CPR = DP / 8, TILEB = kXKeys * ROWB, KS = DP / 16, DT = DP / 16;
   __shared__ __attribute__((aligned(1024))) char k_lds0[TILEB];
@@ -203,18 +212,25 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
           if constexpr (WIN) s[e] = bit_or(s[e], mine, 8 * (e >> 2) + (e & 3), kMinusInf);
           else s[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[e] : -INFINITY;
       }
-      u32x4 pq[2];
+      u32x4 pq[2], lq[2];   // lq: FINE
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         const float p0 = fast_exp2(__builtin_fmaf(s[e], c2, -ls));
         const float p1 = fast_exp2(__builtin_fmaf(s[e + 1], c2, -ls));
-        pq[(e >> 2) & 1][((e & 3) >> 1) + 2 * (e >> 3)] = pack_bf16x2(p0 * (dp[e] + nd), p1 * (dp[e + 1] + nd));
+        const int r = (e >> 2) & 1, c = ((e & 3) >> 1) + 2 * (e >> 3);
+        pq[r][c] = pack_bf16x2(p0 * (dp[e] + nd), p1 * (dp[e + 1] + nd));
+        if constexpr (FINE) lq[r][c] = pack_rest(p0 * (dp[e] + nd), p1 * (dp[e + 1] + nd), pq[r][c]);
       }
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         const auto r = __builtin_amdgcn_permlane16_swap(pq[0][v], pq[1][v], false, false);
         pq[0][v] = r[0];
         pq[1][v] = r[1];
+        if constexpr (FINE) {
+          const auto x = __builtin_amdgcn_permlane16_swap(lq[0][v], lq[1][v], false, false);
+          lq[0][v] = x[0];
+          lq[1][v] = x[1];
+        }
       }
       pin_order();
       auto read_kt = [&](int dt) __attribute__((always_inline)) {
@@ -231,6 +247,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void xattn_dq_kernel(const X
       for (int dt = 0; dt < DT; ++dt) {
         dq[dt][0] = mfma16(op[dt % kPre], __builtin_bit_cast(bf16x8, pq[0]), dq[dt][0]);
         dq[dt][1] = mfma16(op[dt % kPre], __builtin_bit_cast(bf16x8, pq[1]), dq[dt][1]);
+        if constexpr (FINE)
+          for (int qg = 0; qg < 2; ++qg) dq[dt][qg] = mfma16(op[dt % kPre], __builtin_bit_cast(bf16x8, lq[qg]), dq[dt][qg]);
         if (dt + kPre < DT) op[dt % kPre] = read_kt(dt + kPre);
         pin_order();
       }
@@ -364,8 +382,8 @@ struct SinkParts {
 // part: fp32 [dK, dV][split][token][Hk][D], null with one split.
 // WIN: the steps are those of the tokens that see a key of the workgroup, and
 // the keys' tiles that hold sinks, which most tokens see, have splits of their own.
-template <int DP, bool WIN>
-__global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kernel(const XArgs a, const float* __restrict__ aux,
+template <int DP, bool WIN, bool FINE>
+__global__ __launch_bounds__(256, FINE ? 1 : WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kernel(const XArgs a, const float* __restrict__ aux,
                                                             const XOrder order, float* __restrict__ part,
                                                             const SinkParts sinks) {
   constexpr int NW = 4, ROWB = DP * 2, CPR = DP / 8, KS = DP / 16, DT = DP / 16;
@@ -545,7 +563,7 @@ __global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kerne
             dp[e] = bit_or(dp[e], mine, 8 * (e >> 2) + (e & 3), 0);
           }
         }
-      u32x4 pp[2], pd[2];
+      u32x4 pp[2], pd[2], ld[2];   // ld: FINE
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const f32x4 ls = *reinterpret_cast<const f32x4*>(a_pl + 8 * x);
@@ -557,6 +575,7 @@ __global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kerne
           const int r = (i >> 2) & 1, c = ((i & 3) >> 1) + 2 * (i >> 3);
           pp[r][c] = pack_bf16x2(p0, p1);
           pd[r][c] = pack_bf16x2(p0 * dp[i], p1 * dp[i + 1]);
+          if constexpr (FINE) ld[r][c] = pack_rest(p0 * dp[i], p1 * dp[i + 1], pd[r][c]);
         }
       }
 #pragma unroll
@@ -567,6 +586,11 @@ __global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kerne
         const auto r1 = __builtin_amdgcn_permlane16_swap(pd[0][v], pd[1][v], false, false);
         pd[0][v] = r1[0];
         pd[1][v] = r1[1];
+        if constexpr (FINE) {
+          const auto r2 = __builtin_amdgcn_permlane16_swap(ld[0][v], ld[1][v], false, false);
+          ld[0][v] = r2[0];
+          ld[1][v] = r2[1];
+        }
       }
       vector_first(false);
       hold();
@@ -577,6 +601,7 @@ __global__ __launch_bounds__(256, WIN && DP == 64 ? 3 : 2) void xattn_dkdv_kerne
         for (int kg = 0; kg < 2; ++kg) {
           dv[dt][kg] = mfma16(x[0], __builtin_bit_cast(bf16x8, pp[kg]), dv[dt][kg]);
           dk[dt][kg] = mfma16(x[1], __builtin_bit_cast(bf16x8, pd[kg]), dk[dt][kg]);
+          if constexpr (FINE) dk[dt][kg] = mfma16(x[1], __builtin_bit_cast(bf16x8, ld[kg]), dk[dt][kg]);
         }
         if (dt + kPre < DT) read_tr(dt + kPre);
         hold();
@@ -801,22 +826,27 @@ size_t sink_part(const XArgs& a) {
              : 0;
 }
 
-template <int DP, bool WIN>
+// FINE: window attention whose workgroups of either pass take half of the CUs or fewer.
+bool fine_grads(const XArgs& a) {
+  return a.window && dq_groups(a) * dq_splits(a) <= 128 && a.B * a.Hk * dkdv_units(a) <= 128;
+}
+
+template <int DP, bool WIN, bool FINE = false>
 void launch_dq(const XArgs& a, float* aux, int splits, float* part, hipStream_t s) {
   const XOrder order = WIN ? window_order(head_group(a), a.B, a.Hk, dq_tiles(a), splits)
                            : x_order(head_group(a), a.B, a.Hk, dq_tiles(a), splits);
   const int64_t items = order.total;   // of window attention also those that fill chunks up
   const dim3 grid((unsigned)(std::min<int64_t>(std::max<int64_t>(items, 1), x_resident(DP, kDqWaves)) + 7) / 8 * 8);
   TraceScope ts_(s, WIN ? "swattn_dq" : "xattn_dq", DP);
-  hipLaunchKernelGGL((xattn_dq_kernel<DP, WIN>), grid, dim3(64 * kDqWaves), 0, s, a, aux, order, part);
+  hipLaunchKernelGGL((xattn_dq_kernel<DP, WIN, FINE>), grid, dim3(64 * kDqWaves), 0, s, a, aux, order, part);
 }
-template <int DP, bool WIN>
+template <int DP, bool WIN, bool FINE = false>
 void launch_dkdv(const XArgs& a, const float* aux, float* part, const SinkParts& sinks, hipStream_t s) {
   const int64_t tiles = ((int64_t)a.Nk + kBwdKeys - 1) / kBwdKeys;
   const XOrder order = WIN ? window_order(1, a.B, a.Hk, dkdv_units(a), 1) : x_order(head_group(a), a.B, a.Hk, tiles, sinks.others);
   TraceScope ts_(s, WIN ? "swattn_dkdv" : "xattn_dkdv", DP);
   const dim3 grid((unsigned)(std::max<int64_t>(order.total, 1) + 7) / 8 * 8);
-  hipLaunchKernelGGL((xattn_dkdv_kernel<DP, WIN>), grid, dim3(256), 0, s, a, aux, order, part, sinks);
+  hipLaunchKernelGGL((xattn_dkdv_kernel<DP, WIN, FINE>), grid, dim3(256), 0, s, a, aux, order, part, sinks);
 }
 void launch_sums(const Join* j, int n, int B, hipStream_t s) {
   int64_t most = 0;
@@ -854,10 +884,12 @@ hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
   float* const kpart = qpart + dq_part(a) / sizeof(float);
   Join joins[3];
   int n = 0;
+  const bool fine = fine_grads(a);
   if (dq_groups(a) > 0 || (a.zero_rest && a.Tq > 0)) {
     const int splits = dq_splits(a);
     float* const p = splits > 1 ? qpart : nullptr;
-    if (a.window) a.D <= 64 ? launch_dq<64, true>(a, aux, splits, p, s) : launch_dq<128, true>(a, aux, splits, p, s);
+    if (fine) a.D <= 64 ? launch_dq<64, true, true>(a, aux, splits, p, s) : launch_dq<128, true, true>(a, aux, splits, p, s);
+    else if (a.window) a.D <= 64 ? launch_dq<64, true>(a, aux, splits, p, s) : launch_dq<128, true>(a, aux, splits, p, s);
     else a.D <= 64 ? launch_dq<64, false>(a, aux, splits, p, s) : launch_dq<128, false>(a, aux, splits, p, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p) joins[n++] = Join{p, splits, a.Tq, a.Hq * a.D, a.dq, a.sdq, a.cuq, a.Nq};
@@ -868,7 +900,8 @@ hipError_t launch_xattn_bwd(const XArgs& a, void* workspace, hipStream_t s) {
     SinkParts sinks = sink_parts(a);
     sinks.part = sink_part(a) > 0 ? kpart + dkdv_part(a) / sizeof(float) : nullptr;
     if (a.window) {
-      a.D <= 64 ? launch_dkdv<64, true>(a, aux, p, sinks, s) : launch_dkdv<128, true>(a, aux, p, sinks, s);
+      if (fine) a.D <= 64 ? launch_dkdv<64, true, true>(a, aux, p, sinks, s) : launch_dkdv<128, true, true>(a, aux, p, sinks, s);
+      else a.D <= 64 ? launch_dkdv<64, true>(a, aux, p, sinks, s) : launch_dkdv<128, true>(a, aux, p, sinks, s);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
       if (p || sinks.part) {
         launch_window_sums(a, sinks, p, n > 0 ? joins[0] : Join{}, s);

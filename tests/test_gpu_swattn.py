@@ -170,6 +170,33 @@ def test_sinks_that_a_long_sequence_sees():
         check_case(9, 1, 4000, 4000, Hq, Hk, D, window, sinks)
 
 
+@pytest.mark.parametrize("n,Hq,Hk,D,window,sinks", [(2, 24, 24, 80, (17, 17), 4), (40, 4, 2, 64, (9, 0), 2), (64, 3, 3, 128, (63, 63), 0)])
+def test_small_grids_round_ds_once_less(n, Hq, Hk, D, window, sinks):
+    """dS goes into its products with what its rounding left: its error is 2^-16 of it (two
+    half steps of bf16, 2^-8 each) in place of 2^-8, so that dQ and dK are off by their
+    own rounding and little else. One tile of keys: delta is formed in fp32."""
+    q, k, v, do = draw(40 + n, 2, n, n, Hq, Hk, D)
+    scale = D ** -0.5
+    _, _, grads = run(q, k, v, do, scale, window, sinks)
+    Q, K, V, dO = f64(q), f64(k), f64(v), f64(do)
+    ref = oracle.swattn_bwd(Q, K, V, dO, scale, *window, sinks, None)
+    see, G = oracle.window_see(n, n, *window, sinks), Hq // Hk
+    tdk = np.zeros(K.shape)
+    for b in range(2):
+        for h in range(Hq):
+            qh, kh, vh, dh = Q[b, :, h], K[b, :, h // G], V[b, :, h // G], dO[b, :, h]
+            P, _ = oracle._seen_p(qh, kh, scale, see)
+            x = float((np.abs(qh) @ np.abs(kh).T).max()) * scale * 2 * (D + 8) * E24 + 2.0 ** -18
+            dP = dh @ vh.T
+            dS = P * (dP - (P * dP).sum(1, keepdims=True))
+            wide = np.abs(dh) @ np.abs(vh).T
+            t = (2.0 ** -16 + 2 * x) * np.abs(dS) + P * ((2 * D * E24 + 2 * x) * (wide + (P * wide).sum(1, keepdims=True)))
+            tq = scale * (t @ np.abs(kh)) + U * np.abs(ref[0][b, :, h])
+            assert np.all(np.abs(f64(grads[0])[b, :, h] - ref[0][b, :, h]) <= tq + 1e-30)
+            tdk[b, :, h // G] += scale * (t.T @ np.abs(qh))
+    assert np.all(np.abs(f64(grads[1]) - ref[1]) <= tdk + U * np.abs(ref[1]) + 1e-30)
+
+
 def test_seeded_sweep():
     rng = np.random.default_rng(12)
     for i in range(30):
