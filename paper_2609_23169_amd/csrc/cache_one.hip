@@ -16,7 +16,7 @@
 // order that the scores' layout leaves (keys 4 g .. of both 16-key tiles in lane
 // group g), so P needs no exchange, and V's transposing reads follow it. The softmax
 // keeps a running maximum and sum; P is rounded to bf16 for the second product (half a
-// step, 2^-9 relative, as V's own), everything else is fp32.
+// step, 2^-8 relative at most, as V's own), everything else is fp32.
 //
 // At an item's end the waves' results meet in LDS. A whole item is finished there;
 // of others the workgroup's part goes to the workspace, and a second launch joins the

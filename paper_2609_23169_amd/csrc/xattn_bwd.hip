@@ -18,9 +18,10 @@
 //           workgroups, so the query tiles are split over workgroups, each
 //           writes fp32 partial sums, and a join adds them in a fixed order.
 //
-// Rounding: P and dS to bf16 before their second products (half a step each,
-// 2^-9 relative; in small grids of window attention dS as two, FINE), all sums in fp32. delta comes from O as stored (half a step
-// of it), or as rowsum(P o dP) in fp32 where a row's keys in use lie in one tile.
+// Rounding: P and dS to bf16 before their second products (half a step each, 2^-8
+// relative at most; in small grids of window attention dS as two, FINE), all sums in
+// fp32. delta comes from O as stored (half a step of it), or as rowsum(P o dP) in fp32
+// where a row's keys in use lie in one tile.
 // No atomics: equal results on every run. Keys not in use: the dQ pass reads
 // zeros in their place and sets their P to 0; in the dK/dV pass a key is a
 // column of its own, whatever it holds, and is stored as 0; waves whose 32 keys
@@ -51,7 +52,7 @@ constexpr int kRowTile = 32;    // query tokens of a dK/dV step
 constexpr int kDqWaves = 4;     // of 32 rows each
 
 // FINE: dS goes into its products as two bf16, the rounded value and what the rounding left
-// of it (2^-18 of it off), for grids that leave the chip room. There are few rows then,
+// of it (2^-16 of it off), for grids that leave the chip room. There are few rows then,
 // those with few keys weigh most, and their roundings do not average out: dQ and dK
 // of 384 tokens, window 96, 0.0025 off in relative norm, 0.0018 with this (the result's
 // own rounding 0.0017, the rest delta's O), for 2 us of 17 a pass.

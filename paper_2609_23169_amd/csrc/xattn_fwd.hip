@@ -14,7 +14,7 @@
 // result is exact in real arithmetic. Then
 // O^T += V^T P^T on 16x16x32 after one v_permlane16_swap per register. Sums,
 // maxima and O are fp32; P is rounded to bf16 for the second product (half a
-// step, 2^-9 relative, as large as that of V itself).
+// step, 2^-8 relative at most, as large as that of V itself).
 //
 // With few rows the grid would leave the chip idle, and one workgroup would
 // read a long sequence alone: then the keys are split over workgroups, each
