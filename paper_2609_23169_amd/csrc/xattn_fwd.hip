@@ -327,14 +327,51 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
                           blockIdx.x == 0 && w == 0 ? parts.cuts : nullptr));
   else
     seq.begin(x_items(order.total));
+  // A new item: its rows to operands, through the wave's part of a stage that is not in use.
+  auto open_rows = [&](char* lds0, char* lds1) __attribute__((always_inline)) {
+    XTurn<DP>(x_lane_again()).turn(qop, lds0, lds1);
+    if constexpr (SEE != kSeeAll) {
+      const XArgs& x = *x_args_again();
+      const XItem at = seq.item(seq.at, order);
+      const XSample sm = x_sample<SEE>(x, at.b);
+      see.open(x, sm, at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
+    }
+  };
+  auto clear = [&]() __attribute__((always_inline)) {
+    seq.keep();
+    m_run = l_run = 0.f;
+    fresh = true;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt][0] = oacc[dt][1] = f32x4{};
+  };
   bool have = false;   // a tile lies in the current stage
+  // With a window, or in a cache, the first tile is loaded in front of the loop, which is
+  // shorter by what it would do there (22,879 tokens, 24 heads, window 512 + 512: 405 -> 392
+  // us; a first step of nothing at 128 columns: 1 us of a call's 12).
+  constexpr bool kFront = SEE != kSeeAll;
+  if constexpr (kFront) {
+    bool changed;
+    if (!seq.next(order, 32 * NW, changed)) return;   // uniform
+    const int64_t key = seq.k0 + (int64_t)seq.tile * kXKeys;
+    const __amdgpu_buffer_rsrc_t rk = load_k.tile(static_cast<const __bf16*>(a.k) + key * a.sk + seq.hk * a.D, a.sk);
+    const __amdgpu_buffer_rsrc_t rv = load_v.tile(static_cast<const __bf16*>(a.v) + key * a.sv + seq.hk * a.D, a.sv);
+    load_k.masked(rk, a.sk, seq.bits, k_lds0, w, lane, a.D);
+    load_v.masked(rv, a.sv, seq.bits, v_lds0, w, lane, a.D);
+    load_rows(seq.item(seq.at, order));
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    char* const lds0 = OWN ? turn_lds + w * TURNB : k_lds1 + w * Load::IPW * 1024;
+    open_rows(lds0, OWN ? lds0 + TURNB / 2 : v_lds1 + w * Load::IPW * 1024);
+    clear();
+    have = true;
+  }
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
     const uint64_t now = seq.bits;
     const int tile = seq.tile;
     bool changed;
     const bool more = seq.next(order, 32 * NW, changed);
-    if (!have && !more) return false;
+    if (!kFront && !have && !more) return false;
     char* const kn = P ? k_lds0 : k_lds1;
     char* const vn = P ? v_lds0 : v_lds1;
     const int64_t key = seq.k0 + (int64_t)seq.tile * kXKeys;
@@ -352,7 +389,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
     // At 128 columns before the first tile too, beside its loads: what it leaves is not
     // used, and a branch around it costs the loop more (packed case 259 -> 275 us). At
     // 64 the branch takes 1 us off a call's 10.
-    if (DP == 128 || have) {
+    if (kFront || DP == 128 || have) {
       step(now, tile, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, all, load);
     } else {
       if (all)
@@ -367,21 +404,9 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : DP == 64 ? 3 : 2) void xattn_
       // next item's first tile
       char* const lds0 = OWN ? turn_lds + w * TURNB : (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
       char* const lds1 = OWN ? lds0 + TURNB / 2 : (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
-      if (have) finish(seq.item(seq.cur, order), lds0, lds1);
-      if (more) {
-        XTurn<DP>(x_lane_again()).turn(qop, lds0, lds1);
-        if constexpr (SEE != kSeeAll) {
-          const XArgs& x = *x_args_again();
-          const XItem at = seq.item(seq.at, order);
-          const XSample sm = x_sample<SEE>(x, at.b);
-          see.open(x, sm, at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
-        }
-      }
-      seq.keep();
-      m_run = l_run = 0.f;
-      fresh = true;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) oacc[dt][0] = oacc[dt][1] = f32x4{};
+      if (kFront || have) finish(seq.item(seq.cur, order), lds0, lds1);
+      if (more) open_rows(lds0, lds1);
+      clear();
     }
     have = true;
     return more;
