@@ -304,14 +304,47 @@ __global__ __launch_bounds__(256, FINE ? 1 : DP == 64 ? 3 : 2) void xattn_dq_ker
 
   // A workgroup's items in turn, their tiles as one sequence, as in the forward.
   seq.begin(x_items(order.total));
+  // A new item, whose first tile lies in k_at and v_at: its rows' statistics, and the rows to
+  // operands, through the wave's part of a stage that is not in use.
+  auto open_rows = [&](const XItem& at, const Extra& ex, char* lds0, char* lds1, const char* k_at,
+                       const char* v_at) __attribute__((always_inline)) {
+    row_stats(ex, lds0);
+    const XTurn<DP> rows(x_lane_again());
+    rows.turn(qop, lds0, lds1);
+    rows.turn(doop, lds0, lds1);
+    if constexpr (WIN) {
+      const XArgs& x = *x_args_again();
+      see.open(x, x_sample<SEE>(x, at.b), at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
+    }
+    const bool one = seq.one_tile(order);   // uniform
+    if (one) ndl = -tile_delta(seq.bits, seq.tile, k_at, v_at);
+    put_stats(at, one ? seq.bits != 0 : at.part == 0);   // where delta is known
+  };
   bool have = false;   // a tile lies in the current stage
+  if constexpr (WIN) {   // as in the forward, the first tile in front of the loop
+    bool changed;
+    if (!seq.next(order, 32 * NW, changed)) return;   // uniform
+    const int64_t key = seq.k0 + (int64_t)seq.tile * kXKeys;
+    const __amdgpu_buffer_rsrc_t rk = load_k.tile(static_cast<const __bf16*>(a.k) + key * a.sk + seq.hk * a.D, a.sk);
+    const __amdgpu_buffer_rsrc_t rv = load_v.tile(static_cast<const __bf16*>(a.v) + key * a.sv + seq.hk * a.D, a.sv);
+    load_k.masked(rk, a.sk, seq.bits, k_lds0, w, lane, a.D);
+    load_v.masked(rv, a.sv, seq.bits, v_lds0, w, lane, a.D);
+    Extra ex;
+    const XItem at = seq.item(seq.at, order);
+    load_rows(at, ex);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    seq.keep();
+    open_rows(at, ex, k_lds1 + w * Load::IPW * 1024, v_lds1 + w * Load::IPW * 1024, k_lds0, v_lds0);
+    have = true;
+  }
   auto iter = [&](auto par) __attribute__((always_inline)) {   // false: done
     constexpr int P = decltype(par)::value;
     const uint64_t now = seq.bits;
     const int tile = seq.tile;
     bool changed;
     const bool more = seq.next(order, 32 * NW, changed);
-    if (!have && !more) return false;
+    if (!WIN && !have && !more) return false;
     char* const kn = P ? k_lds0 : k_lds1;
     char* const vn = P ? v_lds0 : v_lds1;
     const int64_t key = seq.k0 + (int64_t)seq.tile * kXKeys;
@@ -329,7 +362,7 @@ __global__ __launch_bounds__(256, FINE ? 1 : DP == 64 ? 3 : 2) void xattn_dq_ker
     };
     // At 128 columns before the first tile too, beside its loads: what it leaves is not
     // used, and a branch around it would spill 29 registers.
-    if (DP == 128 || have) {
+    if (WIN || DP == 128 || have) {
       step(now, tile, P ? k_lds1 : k_lds0, P ? v_lds1 : v_lds0, changed && more, ex, all, load);
     } else {
       if (all)
@@ -344,22 +377,10 @@ __global__ __launch_bounds__(256, FINE ? 1 : DP == 64 ? 3 : 2) void xattn_dq_ker
       // next item's first tile
       char* const lds0 = (P ? k_lds1 : k_lds0) + w * Load::IPW * 1024;
       char* const lds1 = (P ? v_lds1 : v_lds0) + w * Load::IPW * 1024;
-      if (have) finish(seq.item(seq.cur, order), lds0, lds1);
+      if (WIN || have) finish(seq.item(seq.cur, order), lds0, lds1);
       const XItem at = seq.item(seq.at, order);
       seq.keep();
-      if (more) {
-        row_stats(ex, lds0);
-        const XTurn<DP> rows(x_lane_again());
-        rows.turn(qop, lds0, lds1);
-        rows.turn(doop, lds0, lds1);
-        if constexpr (WIN) {
-          const XArgs& x = *x_args_again();
-          see.open(x, x_sample<SEE>(x, at.b), at.b, at.tile * 32 * NW + 32 * w + (x_lane_again() & 31));
-        }
-        const bool one = seq.one_tile(order);   // uniform
-        if (one) ndl = -tile_delta(seq.bits, seq.tile, kn, vn);
-        put_stats(at, one ? seq.bits != 0 : at.part == 0);   // where delta is known
-      }
+      if (more) open_rows(at, ex, lds0, lds1, kn, vn);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) dq[dt][0] = dq[dt][1] = f32x4{};
     }
