@@ -35,8 +35,8 @@
 // Window attention (SEE = kSeeWindow) visits the tiles that some row of the item sees:
 // two runs, those with sinks and those of the window. A half tile that every row sees
 // whole goes as above, of others a row's keys are a word of 32 bits. 77,586 queries
-// that see 1,024 keys to each side and 512 sinks, 24 heads of 128: 2,750 to 2,830 us,
-// 860 TFLOP/s of visible pairs, matrix cores 42% busy, five vector instructions an MFMA.
+// that see 1,024 keys to each side and 512 sinks, 24 heads of 128: 2,700 to 2,800 us,
+// 890 TFLOP/s of visible pairs, matrix cores 42% busy, five vector instructions an MFMA.
 // A cache (kSeeCache) is a window with nothing behind a token, lengths on the device
 // and a tree's words; calls of few rows have cache_one.hip. Its parts are shared out by
 // cache_share, eight waves where 128 columns have more than 128 rows: 2 x 509 tokens on
