@@ -102,9 +102,9 @@ __global__ __launch_bounds__(256, 1) void cache_one_kernel(const XArgs a, const 
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)   // kXOut and a tile further on is past the range too
-          k[kt][ks] = __builtin_bit_cast(
-              bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rk, k_off[ks], 16 * kt * a.sk * 2, kXStream));
+        for (int ks = 0; ks < KS; ++ks)   // kXOut and 16 slots further on is past the range too
+          k[kt][ks] = __builtin_bit_cast(   // in the vector offset: the range's check leaves scalar ones out
+              bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rk, k_off[ks] + 16 * kt * a.sk * 2, 0, kXStream));
       char* const to = v + w * STEPB;
       if ((key >= span.lo && key + 32 <= span.hi) || key + 32 <= span.send) {   // uniform
 #pragma unroll
