@@ -774,7 +774,8 @@ ut_status ut_cache_weights(const void* q, const void* k_cache, const float* lse,
  * zero_rest 0: rows of k_out and v_out at and past n_keep are left as they were;
  *           else they are set to 0. Rows from len_out to n_keep are set to 0 always.
  * n_keep >= 1, n_sink >= 0, n_recent >= 0, n_sink + n_recent <= n_keep <=
- * capacity_out; B < 65536. Outputs must not overlap inputs (checked).
+ * capacity_out; B < 65536. Outputs must not overlap inputs or each other (checked; k_out
+ * and v_out may be interleaved views of one buffer, of one stride).
  * Errors: sizes, strides, null or misaligned pointers, overlap
  *         -> UT_ERR_INVALID_ARG; a head_dim that is no multiple of 8 up to 128, a
  *         stride of 2^22 or more -> UT_ERR_UNSUPPORTED.

@@ -1337,30 +1337,32 @@ ut_status ut_cache_evict(const void* k_cache, const void* v_cache, const float* 
     return fail(UT_ERR_INVALID_ARG, "%s: problem too large (2^27 rows of a head or more)", fn);
   CacheEvict a{};
   const int64_t row = (int64_t)Hk * D;
-  const char* const names[] = {"k_cache", "v_cache", "k_out", "v_out"};
-  const void* const rows[] = {k_cache, v_cache, k_out, v_out};
+  // Inputs, then outputs, each with the bytes from its first to its last one.
+  constexpr int kIn = 4, kAll = 9;
+  const char* const names[kAll] = {"k_cache", "v_cache", "weights", "cache_len", "k_out", "v_out", "weights_out", "len_out", "kept_idx"};
+  const void* const at[kAll] = {k_cache, v_cache, weights, cache_len, k_out, v_out, weights_out, len_out, kept_idx};
+  int64_t bytes[kAll] = {0, 0, (int64_t)B * Hk * capacity * 4, (int64_t)B * 4, 0, 0, (int64_t)B * Hk * capacity_out * 4,
+                         (int64_t)B * 4, (int64_t)B * Hk * n_keep * 4};
+  const int rows[] = {0, 1, 4, 5};   // K and V, in the order of their strides
   int64_t* const strides[] = {&a.sk, &a.sv, &a.sko, &a.svo};
-  Range at[6];
   for (int i = 0; i < 4; ++i) {
-    UT_TRY(check_stride(fn, names[i], strides_host, i, row, 8, kXMaxStride, strides[i]));
-    UT_TRY(check_ptr(fn, names[i], rows[i], 16));
-    at[i] = Range{static_cast<const char*>(rows[i]),
-                  (((int64_t)B * (i < 2 ? capacity : capacity_out) - 1) * *strides[i] + row) * 2};
+    const char* name = names[rows[i]];
+    UT_TRY(check_stride(fn, name, strides_host, i, row, 8, kXMaxStride, strides[i]));
+    UT_TRY(check_ptr(fn, name, at[rows[i]], 16));
+    bytes[rows[i]] = (((int64_t)B * (i < 2 ? capacity : capacity_out) - 1) * *strides[i] + row) * 2;
   }
-  UT_TRY(check_ptr(fn, "weights", weights, 4));
-  UT_TRY(check_ptr(fn, "weights_out", weights_out, 4));
-  UT_TRY(check_ptr(fn, "len_out", len_out, 4));
-  UT_TRY(check_ptr(fn, "kept_idx", kept_idx, 4));
-  at[4] = Range{reinterpret_cast<const char*>(weights), (int64_t)B * Hk * capacity * 4};
-  at[5] = Range{reinterpret_cast<const char*>(weights_out), (int64_t)B * Hk * capacity_out * 4};
-  for (int i : {0, 1, 4})
-    for (int o : {2, 3, 5})
-      if (overlap(at[i], at[o]))
-        return fail(UT_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, o < 4 ? names[o] : "weights_out",
-                    i < 4 ? names[i] : "weights");
-  if (overlap(Range{reinterpret_cast<const char*>(len_out), (int64_t)B * 4},
-              Range{reinterpret_cast<const char*>(cache_len), (int64_t)B * 4}))
-    return fail(UT_ERR_INVALID_ARG, "%s: len_out overlaps cache_len", fn);
+  for (int i : {2, 6, 7, 8}) UT_TRY(check_ptr(fn, names[i], at[i], 4));
+  auto range = [&](int i) { return Range{static_cast<const char*>(at[i]), bytes[i]}; };
+  for (int o = kIn; o < kAll; ++o)
+    for (int i = 0; i < o; ++i) {
+      if (!overlap(range(i), range(o))) continue;
+      if (i == 4 && o == 5 && a.sko == a.svo) {   // rows of one buffer in turn: apart by less than a stride
+        const int64_t stride = a.sko * 2, by = static_cast<const char*>(v_out) - static_cast<const char*>(k_out),
+                      off = (by % stride + stride) % stride;
+        if (off >= row * 2 && off <= stride - row * 2) continue;
+      }
+      return fail(UT_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, names[o], names[i]);
+    }
   UT_TRY(check_lens(fn, cache_len, B, capacity, stream));
   a.k = k_cache, a.v = v_cache, a.k_out = k_out, a.v_out = v_out;
   a.weights = weights, a.weights_out = weights_out, a.lens = cache_len, a.len_out = len_out, a.idx = kept_idx;

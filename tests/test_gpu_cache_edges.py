@@ -31,3 +31,15 @@ def test_full_caches_of_any_length(cap, Hq, Hk, D):
     want = ut.cache_attn(q[1:], k[1:], v[1:], dev([cap - 1]), D ** -0.5, weights=w[1:])
     for x, y in zip(alone, want):
         assert torch.equal(x, y)
+
+
+def test_eviction_into_neighbouring_views_of_one_buffer():
+    B, cap, Hk, D, keep, lens = 2, 300, 2, 64, 100, [300, 70]
+    k, v, w = rnd(4, B, cap, Hk, D), rnd(5, B, cap, Hk, D), torch.rand((B, Hk, cap), device=DEV)
+    want = ut.cache_evict(k, v, w, dev(lens), keep, 2, 9)
+    for first, second, count in ((0, 1, 2), (1, 0, 2), (2, 1, 3)):
+        kv = torch.empty((B, keep, count, Hk, D), dtype=torch.bfloat16, device=DEV)
+        wo, lo, idx = (torch.empty_like(x) for x in want[2:])
+        assert ut.ut_cache_evict(k, v, w, dev(lens), kv[:, :, first], kv[:, :, second], wo, lo, idx, keep, 2, 9) == ut.UT_OK
+        for x, y in zip((kv[:, :, first], kv[:, :, second], wo, lo, idx), want):
+            assert torch.equal(x, y)
