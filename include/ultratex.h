@@ -725,7 +725,8 @@ ut_status ut_swattn_bwd_varlen(const void* q, const void* k, const void* v, cons
  * A token that sees no slot (a tree word of 0 in front of an empty cache): o = 0,
  * lse = -inf. No atomics: results are deterministic.
  * Errors: those of ut_xattn_fwd; T < 1 or > capacity, a tree with T > 64 or
- *         0 <= window_left < T - 1, weights_in without weights_out or overlapping it
+ *         0 <= window_left < T - 1, weights_in without weights_out or overlapping it,
+ *         launches of 2^32 threads (never below 2^21 sample-heads, B Hk)
  *         -> UT_ERR_INVALID_ARG.
  * ---------------------------------------------------------------------- */
 size_t ut_cache_attn_workspace_size(int32_t B, int32_t T, int32_t capacity, int32_t Hq, int32_t Hk,
@@ -776,7 +777,8 @@ ut_status ut_cache_weights(const void* q, const void* k_cache, const float* lse,
  * n_keep >= 1, n_sink >= 0, n_recent >= 0, n_sink + n_recent <= n_keep <=
  * capacity_out; B < 65536. Outputs must not overlap inputs or each other (checked; k_out
  * and v_out may be interleaved views of one buffer, of one stride).
- * Errors: sizes, strides, null or misaligned pointers, overlap
+ * Errors: sizes (2^27 rows of K or V of a head, 2^24 rows of weights, or more),
+ *         strides, null or misaligned pointers, overlap
  *         -> UT_ERR_INVALID_ARG; a head_dim that is no multiple of 8 up to 128, a
  *         stride of 2^22 or more -> UT_ERR_UNSUPPORTED.
  * ---------------------------------------------------------------------- */

@@ -1216,6 +1216,13 @@ ut_status check_cache(const char* fn, int32_t B, int32_t T, int32_t capacity, in
   return UT_OK;
 }
 
+// The launches behind the attention go by sample-heads and slots, not by what fits the chip.
+ut_status check_cache_launch(const char* fn, bool ok) {
+  if (!ok)
+    return fail(UT_ERR_INVALID_ARG, "%s: problem too large (a launch of 2^32 threads: millions of sample-heads)", fn);
+  return UT_OK;
+}
+
 // Slots in use, on the device; under UT_VALIDATE copied to the host and checked.
 ut_status check_lens(const char* fn, const int32_t* lens, int32_t B, int32_t most, hipStream_t stream) {
   UT_TRY(check_ptr(fn, "cache_len", lens, 4));
@@ -1263,7 +1270,7 @@ size_t ut_cache_attn_workspace_size(int32_t B, int32_t T, int32_t capacity, int3
   g_last_error[0] = 0;
   a.lens = &kNoLens;
   a.scores = with_weights && (int64_t)T * a.G <= kScoreRows;
-  return ok ? cache_attn_workspace(a) : 0;
+  return ok && cache_attn_launchable(a, with_weights != 0) ? cache_attn_workspace(a) : 0;
 }
 
 ut_status ut_cache_attn(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
@@ -1276,6 +1283,8 @@ ut_status ut_cache_attn(const void* q, const void* k_cache, const void* v_cache,
   g_last_error[0] = 0;
   XArgs a{};
   UT_TRY(check_cache(fn, B, T, capacity, Hq, Hk, D, window_left, n_sink, tree != nullptr, softmax_scale, &a));
+  a.scores = weights_out && (int64_t)T * a.G <= kScoreRows;
+  UT_TRY(check_cache_launch(fn, cache_attn_launchable(a, weights_out != nullptr)));
   UT_TRY(check_words(fn, "tree", tree));
   UT_TRY(check_sums(fn, weights_in, weights_out, B, Hk, capacity));
   UT_TRY(check_lens(fn, cache_len, B, capacity - T, stream));
@@ -1284,7 +1293,6 @@ ut_status ut_cache_attn(const void* q, const void* k_cache, const void* v_cache,
   UT_TRY(check_xtensors(fn, t, 4, strides_host, a));
   UT_TRY(check_ptr(fn, "lse", lse, 4));
   a.q = q, a.k = k_cache, a.v = v_cache, a.o = o, a.lse = lse, a.lens = cache_len, a.tree = tree;
-  a.scores = weights_out && (int64_t)T * a.G <= kScoreRows;
   UT_TRY(check_space(fn, cache_attn_workspace(a), workspace, workspace_bytes));
   return check_hip(launch_cache_attn(a, CacheWeights{weights_in, weights_out, nullptr}, workspace, stream),
                    "cache attention launch");
@@ -1300,6 +1308,7 @@ ut_status ut_cache_weights(const void* q, const void* k_cache, const float* lse,
   g_last_error[0] = 0;
   XArgs a{};
   UT_TRY(check_cache(fn, B, T, capacity, Hq, Hk, D, window_left, n_sink, tree != nullptr, softmax_scale, &a));
+  UT_TRY(check_cache_launch(fn, cache_weights_launchable(a)));
   if (tokens && T > 64) return fail(UT_ERR_INVALID_ARG, "%s: bits for %d tokens (at most 64)", fn, T);
   const XTensor t[] = {{"q", q, &a.sq, false}, {"k_cache", k_cache, &a.sk, true}};
   UT_TRY(check_xtensors(fn, t, 2, strides_host, a));
@@ -1335,6 +1344,9 @@ ut_status ut_cache_evict(const void* k_cache, const void* v_cache, const float* 
   if ((int64_t)B * capacity >= most || (int64_t)B * capacity * Hk >= most || (int64_t)B * capacity_out >= most ||
       (int64_t)B * capacity_out * Hk >= most)
     return fail(UT_ERR_INVALID_ARG, "%s: problem too large (2^27 rows of a head or more)", fn);
+  // a workgroup of 256 threads a row of weights, of 1,024 above 4,096 slots (fewer rows then, by the above)
+  if ((int64_t)B * Hk >= (int64_t)1 << 24)
+    return fail(UT_ERR_INVALID_ARG, "%s: problem too large (2^24 rows of weights, B Hk, or more)", fn);
   CacheEvict a{};
   const int64_t row = (int64_t)Hk * D;
   // Inputs, then outputs, each with the bytes from its first to its last one.

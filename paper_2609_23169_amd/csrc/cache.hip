@@ -651,28 +651,48 @@ CacheSpace cache_space(const XArgs& a) {
   return c;
 }
 
-template <bool JOIN>
-hipError_t launch_weights(const XArgs& a, const CacheWeights& c, const CacheRows& rows, const CacheParts& parts, bool many,
-                          hipStream_t s) {
-  // Steps of four tiles: as many a workgroup as leave one for each CU, by the capacity, or
-  // where a window leaves most of it unseen shared out by what is seen (48 tokens of 32
-  // heads, four samples: 24,576 slots with a window of 4,096 54 -> 38 us, but 4,096 slots
-  // seen whole 29 -> 33).
+// Workgroups of the weights' launch. Steps of four tiles: as many a workgroup (`per`) as
+// leave one for each CU, by the capacity, or where a window leaves most of it unseen (0)
+// shared out by what is seen (48 tokens of 32 heads, four samples: 24,576 slots with a
+// window of 4,096 54 -> 38 us, but 4,096 slots seen whole 29 -> 33).
+struct WeightsGrid {
+  int64_t per, weigh;
+};
+WeightsGrid weights_grid(const XArgs& a) {
   const int64_t heads = (int64_t)a.B * a.Hk, all = ((int64_t)a.Nk + 4 * kXKeys - 1) / (4 * kXKeys);
   const int64_t steps = (x_item_tiles(a, a.Nq * a.G) + 3) / 4;
   const int64_t per = 2 * steps <= all ? 0 : std::max<int64_t>(1, std::min<int64_t>(kWTiles, (heads * all + 255) / 256));
-  const int64_t weigh = per ? heads * ((all + per - 1) / per) : std::min<int64_t>(heads * steps, 256);
+  return WeightsGrid{per, per ? heads * ((all + per - 1) / per) : std::min<int64_t>(heads * steps, 256)};
+}
+// Workgroups behind the attention: of the joins, and of the weights from the scores.
+int64_t finish_joins(const XArgs& a, bool many) { return (a.Tq * a.Hq + (many ? 0 : 7)) / (many ? 1 : 8); }
+int64_t finish_chunks(const XArgs& a) { return a.scores ? (int64_t)a.B * a.Hk * (((int64_t)a.Nk + 255) / 256) : 0; }
+constexpr int64_t kMostThreads = (int64_t)1 << 32;   // of a launch: fewer
+
+template <bool JOIN>
+hipError_t launch_weights(const XArgs& a, const CacheWeights& c, const CacheRows& rows, const CacheParts& parts, bool many,
+                          hipStream_t s) {
+  const auto [per, weigh] = weights_grid(a);
   const int64_t joins = !JOIN ? 0 : many ? parts.stats : (parts.stats + 2 * kWWaves - 1) / (2 * kWWaves);
   const int64_t grid = std::max<int64_t>(weigh, std::min<int64_t>(joins, 256));
   TraceScope ts_(s, "cache_weights", x_padded(a));
+  const int most = (int)weigh, each = (int)per;
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWWaves), 0, s, a, c, rows, parts, (int)weigh, (int)per, (int)joins, many);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWWaves), 0, s, a, c, rows, parts, most, each, (int)joins, many);
   };
   if (per > 0) a.D <= 64 ? launch(cache_weights_kernel<64, JOIN, false>) : launch(cache_weights_kernel<128, JOIN, false>);
   else a.D <= 64 ? launch(cache_weights_kernel<64, JOIN, true>) : launch(cache_weights_kernel<128, JOIN, true>);
   return hipGetLastError();
 }
 }  // namespace
+
+bool cache_weights_launchable(const XArgs& a) { return weights_grid(a).weigh * (64 * kWWaves) < kMostThreads; }
+
+bool cache_attn_launchable(const XArgs& a, bool weights) {
+  if (weights && !a.scores && !cache_weights_launchable(a)) return false;
+  const int64_t joins = cache_shape(a).splits > 1 ? finish_joins(a, false) : 0;   // `many` are few enough
+  return (joins + finish_chunks(a)) * 256 < kMostThreads;
+}
 
 size_t cache_attn_workspace(const XArgs& a) {
   const CacheSpace c = cache_space(a);
@@ -706,8 +726,7 @@ hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* worksp
     if (w.out) return split ? launch_weights<true>(a, w, rows, parts, many, s) : launch_weights<false>(a, w, rows, parts, false, s);
     if (!split) return hipSuccess;
   }
-  const int64_t joins = split ? (parts.stats + (many ? 0 : 7)) / (many ? 1 : 8) : 0;
-  const int64_t chunks = a.scores ? (int64_t)a.B * a.Hk * (((int64_t)a.Nk + 255) / 256) : 0;
+  const int64_t joins = split ? finish_joins(a, many) : 0, chunks = finish_chunks(a);
   TraceScope ts_(s, "cache_finish");
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)(joins + chunks)), dim3(256), 0, s, a, rows, (int)joins, parts, w);

@@ -249,6 +249,9 @@ struct CacheWeights {
 // its scores, 4 bytes a row and key against the 2 D of the key's own row, and the
 // weights need no second pass over the keys.
 constexpr int kScoreRows = 32;
+// Whether their launches stay below 2^32 threads (a.scores set as for the call).
+bool cache_attn_launchable(const XArgs& a, bool weights);
+bool cache_weights_launchable(const XArgs& a);
 size_t cache_attn_workspace(const XArgs& a);
 // w.out null: no weights wanted. a: q, k, v, o, lse, a cache (lens).
 hipError_t launch_cache_attn(const XArgs& a, const CacheWeights& w, void* workspace, hipStream_t s);
