@@ -39,6 +39,7 @@
 // joins them. 22,879 tokens, window 2,048, 24 heads of 128: dQ 840 to 890 us, dK/dV
 // 1,010 to 1,090, matrix cores 49 and 51% busy at 2.0 GHz.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "xattn_util.h"
@@ -815,14 +816,24 @@ int dkdv_splits(const XArgs& a) {
 // workgroups', 32 at least, so that no workgroup is left with the whole sequence; 16 where
 // the chip holds all workgroups at once and waits for the longest (2,048 tokens, 3 heads
 // of 128, window 128: 46 -> 29 us; but 22,879 tokens, 24 heads, 259 -> 282 with the sums).
+// Not shorter than an eighth of what a place on the chip has to do in all, and where a
+// join's part (its fp32 sums written and read) costs what it saves at the end: with t steps
+// a part some 15 / t of the sinks' work on one side and t / 2 a place on the other. Many
+// sinks fill the chip by themselves; with the sums and 24 heads of 128, before this bound
+// and with it: 4,096 sinks of 22,879 tokens, window 128 + 128, 2,508 + 458 -> 2,110 + 89 us,
+// 2.3 -> 0.4 GB of sums; 512 of 77,060, 512 + 512, 3,048 + 144 -> 2,844 + 37; 8 samples with
+// 77 of 6,200 1,409 + 36 -> 1,394 + 22 (with a quarter in place of an eighth 1,430 + 18). At
+// most 8 places' and one a tile in all, near a gigabyte.
 SinkParts sink_parts(const XArgs& a) {
   SinkParts p{};
   p.others = dkdv_splits(a);
   p.splits = 1;
   if (!a.window) return p;
   p.tiles = (std::min(a.sinks, a.Nk) + kBwdKeys - 1) / kBwdKeys;
-  const int64_t least = dkdv_groups(a) <= x_resident(x_padded(a), 4) ? 16 : 32;
-  const int64_t per = std::max<int64_t>(dkdv_steps(a, dkdv_reach(a)) / p.others, least), all = dkdv_steps(a, a.Nq);
+  const int64_t places = x_resident(x_padded(a), 4), groups = dkdv_groups(a), firsts = (int64_t)a.B * a.Hk * p.tiles;
+  const int64_t reach = dkdv_steps(a, dkdv_reach(a)), all = dkdv_steps(a, a.Nq), sinks = firsts * all;
+  const int64_t per = std::max({reach / p.others, groups <= places ? (int64_t)16 : 32,
+                                (sinks + (groups - firsts) * reach) / (8 * places), (int64_t)std::sqrt(30. * sinks / places)});
   p.splits = std::max<int64_t>(p.others, std::min<int64_t>((all + per - 1) / per, 64));
   return p;
 }
