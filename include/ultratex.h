@@ -644,9 +644,12 @@ ut_status ut_xattn_bwd_varlen(const void* q, const void* k, const void* v, const
  * use: o = 0, lse = -inf, zero gradients. Keys that no query sees may hold
  * anything and get zero gradients; inf or NaN in a key that some query sees may reach
  * the other queries of its 128-row tile, as 0 times it (mark padding in key_mask).
- * delta = rowsum(dO o O) is formed from the stored o, except for rows whose visible
- * keys lie in one 64-key tile.
- * No atomics: results are deterministic.
+ * delta = rowsum(dO o O) is formed from the stored o, except for rows that see 16
+ * keys or fewer (key_mask aside), and rows of a 128-row tile whose visible keys in use
+ * all lie in one 64-key tile: theirs is rowsum(P o dP) in fp32.
+ * No atomics: results are deterministic. How they are rounded goes by the sizes of the
+ * call (small ones carry dS with more bits), so that a sample's gradients may differ
+ * in their last bits with the number of samples beside it.
  * Errors: also window_left or window_right < -1, n_sink < 0 -> UT_ERR_INVALID_ARG.
  * ---------------------------------------------------------------------- */
 size_t ut_swattn_fwd_workspace_size(int32_t B, int32_t Nq, int32_t Nk, int32_t Hq, int32_t Hk,

@@ -21,7 +21,8 @@
 // Rounding: P and dS to bf16 before their second products (half a step each, 2^-8
 // relative at most; in small grids of window attention dS as two, FINE), all sums in
 // fp32. delta comes from O as stored (half a step of it), or as rowsum(P o dP) in fp32
-// where a row's keys in use lie in one tile.
+// where the keys in use of a workgroup's rows lie in one tile or, with a window, a row
+// sees few.
 // No atomics: equal results on every run. Keys not in use: the dQ pass reads
 // zeros in their place and sets their P to 0; in the dK/dV pass a key is a
 // column of its own, whatever it holds, and is stored as 0; waves whose 32 keys
@@ -51,6 +52,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kBwdKeys = 128;   // keys of a dK/dV workgroup
 constexpr int kRowTile = 32;    // query tokens of a dK/dV step
 constexpr int kDqWaves = 4;     // of 32 rows each
+constexpr int kFewKeys = 16;    // of a row: its delta is formed in fp32
 
 // FINE: dS goes into its products as two bf16, the rounded value and what the rounding left
 // of it (2^-16 of it off), for grids that leave the chip room. There are few rows then,
@@ -282,6 +284,55 @@ __global__ __launch_bounds__(256, FINE ? 1 : DP == 64 ? 3 : 2) void xattn_dq_ker
     }
     return pair_sum(sum);
   };
+  // WIN: likewise for the rows of a wave one of which sees kFewKeys keys or fewer, in
+  // however many tiles they lie (2 keys a row: dQ 0.0035 off in relative norm and elements
+  // up to three times as far as its roundings allow, 0.0024 with this). Those rows'
+  // windows are at most 47 keys together, and the sinks outside kFewKeys: two halves of 32
+  // and one, straight from memory (20,000 tokens, 24 heads of 128, 2 keys: dQ 162 -> 233
+  // us; windows of more keys take it at a sequence's start alone).
+  auto few_keys = [&]() __attribute__((always_inline)) {   // uniform; the count is least at either end
+    const XArgs& x = *x_args_again();
+    const int n = seq.keys, sinks = min(x.sinks, n);
+    auto count = [&](int p) __attribute__((always_inline)) {
+      const int lo = max(p - x.left, 0), hi = max(min(p + x.right + 1, n), lo), s = x.right > 0 ? sinks : max(min(sinks, p + 1), 0);
+      return hi - lo + s - max(min(s, hi) - lo, 0);
+    };
+    return min(count(__builtin_amdgcn_readfirstlane(see.p)), count(__builtin_amdgcn_readlane(see.p, 31))) <= kFewKeys;
+  };
+  auto few_delta = [&](int hk) __attribute__((always_inline)) {
+    const XArgs& x = *x_args_again();
+    const int n = seq.keys, sinks = min(x.sinks, n), lo = max(__builtin_amdgcn_readfirstlane(see.p) - x.left, 0),
+              hi = max(min(__builtin_amdgcn_readlane(see.p, 31) + x.right + 1, n), 0);
+    const int ln = x_lane_again(), col = 8 * (ln >> 5);
+    float sum = 0.f;
+#pragma unroll 1
+    for (int k = sinks > 0 ? -32 : lo; k < hi; k = k < 0 ? lo : k + 32) {   // -32: sinks outside the window
+      const int k0 = max(k, 0), key = k0 + (ln & 31);
+      const bool in = k < 0 ? key < sinks && (key < lo || key >= hi) : key < hi;
+      const int64_t tok = seq.k0 + min(key, n - 1);
+      const __bf16* const kp = static_cast<const __bf16*>(x.k) + tok * x.sk + hk * x.D + col;
+      const __bf16* const vp = static_cast<const __bf16*>(x.v) + tok * x.sv + hk * x.D + col;
+      unsigned mine = (unsigned)__ballot(in && (!x.mask || x.mask[tok])) & see.bits(x, k0);
+      f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 kx = bf16x8{}, vx = bf16x8{};
+        if (16 * ks + col < x.D) {
+          kx = *reinterpret_cast<const bf16x8*>(kp + 16 * ks);
+          vx = *reinterpret_cast<const bf16x8*>(vp + 16 * ks);
+        }
+        s = mfma32(kx, qop[ks], s);
+        dp = mfma32(vx, doop[ks], dp);
+      }
+      mine >>= 4 * g;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = fast_exp2(__builtin_fmaf(s[e], c2, -lse2));
+        sum += mine >> (8 * (e >> 2) + (e & 3)) & 1 ? p * dp[e] : 0.f;
+      }
+    }
+    return pair_sum(sum);
+  };
   auto finish = [&](const XItem& at, char* lds0, char* lds1) __attribute__((always_inline)) {
     const XArgs& x = *x_args_again();
     const XSample sm = x_sample(x, at.b);
@@ -319,6 +370,8 @@ __global__ __launch_bounds__(256, FINE ? 1 : DP == 64 ? 3 : 2) void xattn_dq_ker
     }
     const bool one = seq.one_tile(order);   // uniform
     if (one) ndl = -tile_delta(seq.bits, seq.tile, k_at, v_at);
+    if constexpr (WIN)
+      if (!one && few_keys()) ndl = -few_delta(at.hk);
     put_stats(at, one ? seq.bits != 0 : at.part == 0);   // where delta is known
   };
   bool have = false;   // a tile lies in the current stage
