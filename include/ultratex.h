@@ -704,7 +704,11 @@ ut_status ut_swattn_bwd_varlen(const void* q, const void* k, const void* v, cons
  * q, o      bf16 [B, T, Hq, D], T >= 1.
  * k_cache, v_cache  bf16 [B, capacity, Hk, D]. Sample b's tokens attend to slots
  *           0 .. cache_len[b] - 1 and to their own T slots behind them; what later
- *           slots hold is not used.
+ *           slots hold is not used, nor those in front of every token's window. Of a
+ *           slot that some token's window or sinks hold, or one of the T, inf or NaN in V
+ *           may reach the sample's other tokens, hidden from them or not, as 0 times it
+ *           (in K it reaches those alone that see the slot): pad drafted tokens with
+ *           finite values.
  * cache_len device int32 [B]: slots in use before the T tokens, 0 .. capacity - T
  *           (clamped to that; checked first under UT_VALIDATE).
  * tree      device uint64 [B, T], T <= 64: bit u of word (b, t) set = token t sees
