@@ -11,7 +11,7 @@
 // registers, the next tile's loads beside the products; S = Q K^T on 32x32x16 bf16 MFMA
 // in the layout where a lane holds one key, so that the sum over the rows is the lane's
 // own but for one exchange. fp32 throughout, a fixed order: no atomics. 192 rows on four
-// caches of 8,300 slots, 8 key heads of 128: 37 us with the joins of the attention's parts
+// caches of 8,300 slots, 8 key heads of 128: 39 us with the joins of the attention's parts
 // (28 alone), vector work and the latency of a workgroup's start and few steps.
 //
 // Eviction: of a row of weights the middle slots (behind the sinks, before the recent
@@ -654,7 +654,7 @@ CacheSpace cache_space(const XArgs& a) {
 // Workgroups of the weights' launch. Steps of four tiles: as many a workgroup (`per`) as
 // leave one for each CU, by the capacity, or where a window leaves most of it unseen (0)
 // shared out by what is seen (48 tokens of 32 heads, four samples: 24,576 slots with a
-// window of 4,096 54 -> 38 us, but 4,096 slots seen whole 29 -> 33).
+// window of 4,096 57 -> 39 us, but 4,096 slots seen whole 31 -> 34).
 struct WeightsGrid {
   int64_t per, weigh;
 };

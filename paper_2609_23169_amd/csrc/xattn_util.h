@@ -62,9 +62,10 @@ __device__ inline XItems x_items(unsigned total) {
 // side by side), then samples, whose lengths may differ, so that every run holds
 // alike parts of all of them, then tiles, parts of a split, groups of heads.
 // Window attention: between heads and samples `chunk` consecutive tiles, which read nearly
-// the same keys (0: as above). With the samples next the 64 workgroups of an XCD met 24
+// the same keys (0: as above). With the samples next the 64 workgroups of an XCD meet 24
 // heads and samples at once, 14 MB of keys: 8 samples of 6,011 to 6,394 tokens, 24 heads,
-// window 512 + 512, forward 1,092 -> 820 us, dQ 1,370 -> 1,125.
+// window 512 + 512, forward 920 us, 907 in chunks of 16 tiles, 913 of 8, 909 of 32; dQ
+// 1,220, 1,195, 1,207 and 1,204. One sample: all alike.
 struct XOrder {
   unsigned heads, tiles, splits, total;   // total: item numbers
   unsigned shift, chunks;                 // window attention: log2 of a chunk, chunks of a sample
