@@ -1248,7 +1248,8 @@ def cache_attn(q, k_cache, v_cache, cache_len, softmax_scale: float, tree=None, 
     """Attention of the tokens q [B, T, Hq, D] over caches [B, capacity, Hk, D] that hold
     cache_len [B] (int32) slots in front of the tokens' own T: (o like q, lse [B, Hq, T]).
     tree: int64 [B, T], bit u of token t's word set where it sees token u, itself
-    included; without one token t sees tokens 0 .. t. With weights [B, Hk, capacity] also
+    included; without one token t sees tokens 0 .. t. Every one of the T slots has to
+    hold finite values, seen or not (pad with zeros). With weights [B, Hk, capacity] also
     their sum with what every slot receives from these tokens (into weights_out if
     given, which may be weights)."""
     B, T, Hq, D = q.shape
